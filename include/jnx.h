@@ -662,6 +662,11 @@ jnx_status jnx_pack_gate_up(const uint16_t* w_gate, const uint16_t* w_up, int32_
 #define JNX_K_FLOW_ATTN 20 /* flow expert: attention forward / backward; work = FLOPs */
 #define JNX_K_FLOW_MISC 21 /* flow expert: time / embedding / output / norms / reductions */
 #define JNX_K_FLOW_WGRAD 22 /* flow expert: weight gradients; work = FLOPs */
+#define JNX_K_QK_ROPE 23         /* norms and rotations of queries and keys; work = 0 */
+#define JNX_K_PROMPT_ATTN 24     /* prompt attention; work = 0 */
+#define JNX_K_PROMPT_ATTN_BWD 25 /* its gradients; work = 0 */
+#define JNX_K_DECODE_ATTN 26     /* single tokens against a cache; work = 0 */
+#define JNX_K_VOCAB 27           /* next-token losses and their gradients; work = 0 */
 
 /* While enabled on the calling thread, each kernel launch of the library is
  * bracketed by two CUDA events on its stream (up to `capacity` launches are

@@ -197,6 +197,149 @@ jnx_status jnx_diag_ex2_poly(const float* x, float* y, int32_t n, void* stream);
 jnx_status jnx_diag_bounded_wait(int64_t limit_cycles, int32_t arrive, int32_t* status,
                                  void* stream);
 
+/* ---- operators of text tenants ----
+ * A tenant whose module reads and writes text (or actions as tokens) behind the
+ * shared prefix: norms and rotations of queries and keys, causal attention of
+ * packed prompts, attention of single tokens against a cache, and next-token
+ * losses over the vocabulary.  `status` (device int, may be NULL) receives what a
+ * kernel detects: JNX_ERR_DEVICE_BOUNDS, JNX_ERR_TIMEOUT; the caller clears it.
+ * No call uploads from host memory, so each can be captured into a CUDA graph. */
+
+/* Rows of attention heads, bf16: element c of head h of row t is
+ * ptr[t * row_stride + h * head_stride + c].  ptr is 16-byte aligned and the
+ * strides are multiples of 8 elements (JNX_ERR_INVALID_ARG otherwise). */
+typedef struct {
+    uint16_t* ptr;
+    int64_t row_stride, head_stride;
+} jnx_head_rows;
+
+/* Norms of each query and key head with the position rotation.  head_dim in
+ * {64, 128, 256}.  gamma_q / gamma_k [head_dim] bf16: a head row x becomes
+ * x / sqrt(mean(x^2) + eps) * gamma first; NULL: no norm.  Then rotate-half RoPE
+ * over up to four position axes: frequency i of head_dim / 2,
+ * theta^(-2 i / head_dim), turns the pair (i, i + head_dim / 2) by the position on
+ * the axis in whose section i lies (sections[0] frequencies belong to axis 0, the
+ * next sections[1] to axis 1, ...); frequencies beyond the sections do not turn.
+ * Positions are exact over the whole int32 range. */
+typedef struct {
+    int32_t n_heads, n_kv_heads, head_dim;
+    int32_t n_axes, sections[4];
+    float theta, eps;
+    const uint16_t *gamma_q, *gamma_k;
+} jnx_qk_rope;
+
+/* A cache of keys and values, bf16: element c of head h of token t of slot s is
+ * k[s * slot_stride + t * row_stride + h * head_stride + c], v alike; n_slots slots
+ * of `room` tokens.  Alignment as jnx_head_rows. */
+typedef struct {
+    uint16_t *k, *v;
+    int32_t n_slots, room;
+    int64_t slot_stride, row_stride, head_stride;
+} jnx_kv_cache;
+
+/* q = rotated normed query heads, k = key heads of qkv [n_tokens, ldqkv] bf16 (q
+ * heads, then k heads, then v heads, which are not read), at positions
+ * pos [n_axes, n_tokens].  q and k may be qkv's own rows. */
+jnx_status jnx_op_qk_norm_rope(const jnx_qk_rope* p, const uint16_t* qkv, int64_t ldqkv,
+                               const int32_t* pos, int32_t n_tokens, const jnx_head_rows* q,
+                               const jnx_head_rows* k, void* stream);
+
+/* The same for new tokens of live sequences: token t's key and value heads go to
+ * row at[t] of slot slot[t].  A row outside the cache is not written and reported. */
+jnx_status jnx_op_qk_norm_rope_append(const jnx_qk_rope* p, const uint16_t* qkv, int64_t ldqkv,
+                                      const int32_t* pos, int32_t n_tokens,
+                                      const jnx_head_rows* q, const jnx_kv_cache* cache,
+                                      const int32_t* slot, const int32_t* at, int32_t* status,
+                                      void* stream);
+
+/* Gradients: dqkv's query and key columns [n_tokens, ldqkv] from dq and dk (its value
+ * columns are not written), and the norms' gains' gradients dgamma_q / dgamma_k
+ * [head_dim] fp32 (overwritten; NULL where there is no norm).  dq and dk may be
+ * dqkv's own rows.  Sums run in an order set by the sizes. */
+size_t jnx_op_qk_norm_rope_backward_workspace_bytes(const jnx_qk_rope* p, int32_t n_tokens);
+jnx_status jnx_op_qk_norm_rope_backward(const jnx_qk_rope* p, const uint16_t* qkv, int64_t ldqkv,
+                                        const int32_t* pos, int32_t n_tokens,
+                                        const jnx_head_rows* dq, const jnx_head_rows* dk,
+                                        uint16_t* dqkv, float* dgamma_q, float* dgamma_k,
+                                        void* workspace, size_t ws_bytes, void* stream);
+
+/* Packed prompts.  Sequence s has query rows [cu_q[s], cu_q[s + 1]) and key rows
+ * [cu_kv[s], cu_kv[s + 1]); its queries are the last of its positions, so row i of
+ * Lq sees keys j < min(Lk, max(Lk - Lq + i + 1, prefix[s])).  A row that sees none
+ * has output 0, log-sum-exp -inf and gradient 0.  The arrays are on the device, the
+ * h_ ones the same on the host; prefix may be NULL (0).  items: the work list of
+ * jnx_prompt_items for the same heads, on the device. */
+typedef struct {
+    int32_t n_seqs;
+    const int32_t *cu_q, *cu_kv, *prefix;
+    const int32_t *h_cu_q, *h_cu_kv, *h_prefix;
+    const int32_t* items;
+    int32_t n_forward, n_keys, n_queries; /* items of each pass, as jnx_prompt_items sets them */
+} jnx_prompt;
+
+/* The work list of a prompt for a head layout: writes up to cap pairs of int32 to out
+ * (NULL: none), sets p's n_forward, n_keys, n_queries and returns the number of pairs,
+ * the longest work first in each pass.  Negative: a jnx_status. */
+int32_t jnx_prompt_items(jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                         int32_t* out, int32_t cap);
+
+/* out = softmax(q k^T / sqrt(head_dim)) v over what each row sees; query head h reads
+ * key/value head h / (n_heads / n_kv_heads).  n_heads / n_kv_heads <= 64, head_dim in
+ * {64, 128, 256}.  lse [rows, n_heads] fp32 (NULL: not written): log2 of the row's sum
+ * of 2^(s log2(e) / sqrt(head_dim)).  q, k, v are finite; other sequences' rows may
+ * hold anything. */
+jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads,
+                                   int32_t head_dim, const jnx_head_rows* q,
+                                   const jnx_head_rows* k, const jnx_head_rows* v,
+                                   const jnx_head_rows* out, float* lse, int32_t* status,
+                                   void* stream);
+
+/* Gradients of q, k and v from out's gradient dout, with the forward's out and lse.  The
+ * same bits whatever else is packed beside a sequence. */
+size_t jnx_op_prompt_attention_backward_workspace_bytes(int32_t n_q, int32_t n_heads);
+jnx_status jnx_op_prompt_attention_backward(const jnx_prompt* p, int32_t n_heads,
+                                            int32_t n_kv_heads, int32_t head_dim,
+                                            const jnx_head_rows* q, const jnx_head_rows* k,
+                                            const jnx_head_rows* v, const jnx_head_rows* out,
+                                            const float* lse, const jnx_head_rows* dout,
+                                            const jnx_head_rows* dq, const jnx_head_rows* dk,
+                                            const jnx_head_rows* dv, void* workspace,
+                                            size_t ws_bytes, int32_t* status, void* stream);
+
+/* One token of each of `batch` live sequences against its cache: sequence b's query
+ * heads (row b of q) over the first n_cached[b] tokens of slot slot[b] (0: output 0).
+ * A slot or length outside the cache is read as length 0 and reported.  The bits of a
+ * sequence do not depend on the others. */
+size_t jnx_op_decode_attention_workspace_bytes(int32_t batch, int32_t n_heads, int32_t head_dim);
+jnx_status jnx_op_decode_attention(const jnx_kv_cache* cache, int32_t batch, int32_t n_heads,
+                                   int32_t n_kv_heads, int32_t head_dim, const jnx_head_rows* q,
+                                   const int32_t* slot, const int32_t* n_cached,
+                                   const jnx_head_rows* out, void* workspace, size_t ws_bytes,
+                                   int32_t* status, void* stream);
+
+/* Next-token losses: loss[i] = log(sum_v exp(x_iv)) - x_i,targets[i] with logits
+ * x = h w^T of h [n_rows, d] (row stride ldh) and w [vocab, d] (ldw), bf16; 0 where
+ * targets[i] < 0.  A target >= vocab is reported and read as negative.  The logits are
+ * never stored.  d and the strides are multiples of 8. */
+size_t jnx_op_vocab_loss_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d);
+jnx_status jnx_op_vocab_loss(const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw,
+                             const int32_t* targets, int32_t n_rows, int32_t vocab, int32_t d,
+                             float* loss, void* workspace, size_t ws_bytes, int32_t* status,
+                             void* stream);
+
+/* The losses and the gradients of sum_i row_weight[i] loss[i]: dh [n_rows, d] (lddh) and
+ * dw [vocab, d] (lddw; NULL: a frozen vocabulary), bf16, summed in fp32.  Rows are taken
+ * in pieces of piece_rows (0: at most 8,192): the workspace holds one piece's
+ * probabilities in bf16. */
+size_t jnx_op_vocab_loss_train_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d,
+                                               int32_t piece_rows);
+jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw,
+                                   const int32_t* targets, const float* row_weight,
+                                   int32_t n_rows, int32_t vocab, int32_t d, int32_t piece_rows,
+                                   float* loss, uint16_t* dh, int64_t lddh, uint16_t* dw,
+                                   int64_t lddw, void* workspace, size_t ws_bytes,
+                                   int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,53 @@
+// What the operators of text tenants share: argument checks, the visibility rule and
+// the tiles of packed prompts.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/jnx_ops.h"
+#include "jnx_host.h"
+
+namespace jnx {
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+inline bool rows_ok(const jnx_head_rows* r) {
+    return r && r->ptr && aligned16(r->ptr) && r->row_stride % 8 == 0 && r->head_stride % 8 == 0;
+}
+
+inline bool cache_ok(const jnx_kv_cache* c) {
+    return c && c->k && c->v && aligned16(c->k) && aligned16(c->v) && c->n_slots >= 0 &&
+           c->room >= 0 && c->slot_stride % 8 == 0 && c->row_stride % 8 == 0 &&
+           c->head_stride % 8 == 0;
+}
+
+inline jnx_status launched(const char* what) {
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? JNX_OK : fail(JNX_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// Keys that row i of a sequence's Lq query rows sees of its Lk keys.
+__host__ __device__ inline int keys_seen(int i, int Lq, int Lk, int prefix) {
+    const int causal = Lk - Lq + i + 1;
+    const int n = causal > prefix ? causal : prefix;
+    return n < 0 ? 0 : n < Lk ? n : Lk;
+}
+
+// First row of Lq that sees key j (Lq: none).
+__host__ __device__ inline int first_row(int j, int Lq, int Lk, int prefix) {
+    if (j < prefix) return 0;
+    const int i = j - (Lk - Lq);
+    return i < 0 ? 0 : i < Lq ? i : Lq;
+}
+
+// Rows of a 128-row tile are (token, query head of the group): whole tokens only.
+__host__ __device__ inline int tile_tokens(int group) { return 128 / group; }
+
+// Row tiles of one forward item, which share its keys.
+__host__ __device__ inline int item_tiles(int head_dim) { return head_dim == 256 ? 1 : 2; }
+
+constexpr int kMaxGroup = 64;
+
+jnx_status heads_ok(int n_heads, int n_kv_heads, int head_dim, const char* what);
+
+}  // namespace jnx

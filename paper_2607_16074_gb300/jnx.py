@@ -165,6 +165,30 @@ class jnx_adam_tensor(C.Structure):
                 ("step", C.POINTER(C.c_int32))]
 
 
+class jnx_head_rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class jnx_qk_rope(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "n_axes")] + \
+               [("sections", C.c_int32 * 4), ("theta", C.c_float), ("eps", C.c_float),
+                ("gamma_q", C.c_void_p), ("gamma_k", C.c_void_p)]
+
+
+class jnx_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_slots", C.c_int32),
+                ("room", C.c_int32), ("slot_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
+class jnx_prompt(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("cu_q", "cu_kv", "prefix")] + \
+               [(n, P32) for n in ("h_cu_q", "h_cu_kv", "h_prefix")] + \
+               [("items", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_forward", "n_keys", "n_queries")]
+
+
 _LIB: Optional[C.CDLL] = None
 
 EXPORTS = ("jnx_last_error", "jnx_version", "jnx_group_plan", "jnx_group_attn_items",
@@ -182,7 +206,14 @@ EXPORTS = ("jnx_last_error", "jnx_version", "jnx_group_plan", "jnx_group_attn_it
            "jnx_op_attention_lse", "jnx_op_attention_backward_prep",
            "jnx_op_attention_backward_workspace_bytes", "jnx_op_attention_backward",
            "jnx_op_rms_backward", "jnx_op_gemm_glu_backward", "jnx_op_ffn_glu_backward", "jnx_flow_workspace_bytes",
-           "jnx_flow_forward", "jnx_flow_backward", "jnx_flow_sample", "jnx_adamw_tensors")
+           "jnx_flow_forward", "jnx_flow_backward", "jnx_flow_sample", "jnx_adamw_tensors",
+           "jnx_op_qk_norm_rope", "jnx_op_qk_norm_rope_append",
+           "jnx_op_qk_norm_rope_backward_workspace_bytes", "jnx_op_qk_norm_rope_backward",
+           "jnx_prompt_items", "jnx_op_prompt_attention",
+           "jnx_op_prompt_attention_backward_workspace_bytes",
+           "jnx_op_prompt_attention_backward", "jnx_op_decode_attention_workspace_bytes",
+           "jnx_op_decode_attention", "jnx_op_vocab_loss_workspace_bytes", "jnx_op_vocab_loss",
+           "jnx_op_vocab_loss_train_workspace_bytes", "jnx_op_vocab_loss_train")
 
 
 def lib() -> C.CDLL:
@@ -195,6 +226,8 @@ def lib() -> C.CDLL:
                            "`python -m paper_2607_16074_gb300.build`")
     L = C.CDLL(LIB_PATH)
     vp, i32, i64, sz, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
+    qkr, rows, cache, prompt = (C.POINTER(x) for x in (jnx_qk_rope, jnx_head_rows, jnx_kv_cache,
+                                                       jnx_prompt))
     sig = {
         "jnx_last_error": (C.c_char_p, []),
         "jnx_version": (i32, []),
@@ -267,6 +300,25 @@ def lib() -> C.CDLL:
         "jnx_op_gemm_rope_noalloc_status": (i32, [vp]),
         "jnx_diag_ex2_poly": (i32, [vp, vp, i32, vp]),
         "jnx_diag_bounded_wait": (i32, [C.c_int64, i32, vp, vp]),
+        "jnx_op_qk_norm_rope": (i32, [qkr, vp, i64, vp, i32, rows, rows, vp]),
+        "jnx_op_qk_norm_rope_append": (i32, [qkr, vp, i64, vp, i32, rows, cache, vp, vp, vp, vp]),
+        "jnx_op_qk_norm_rope_backward_workspace_bytes": (sz, [qkr, i32]),
+        "jnx_op_qk_norm_rope_backward": (i32, [qkr, vp, i64, vp, i32, rows, rows, vp, vp, vp, vp,
+                                               sz, vp]),
+        "jnx_prompt_items": (i32, [prompt, i32, i32, i32, vp, i32]),
+        "jnx_op_prompt_attention": (i32, [prompt, i32, i32, i32, rows, rows, rows, rows, vp, vp,
+                                          vp]),
+        "jnx_op_prompt_attention_backward_workspace_bytes": (sz, [i32, i32]),
+        "jnx_op_prompt_attention_backward": (i32, [prompt, i32, i32, i32, rows, rows, rows, rows,
+                                                   vp, rows, rows, rows, rows, vp, sz, vp, vp]),
+        "jnx_op_decode_attention_workspace_bytes": (sz, [i32, i32, i32]),
+        "jnx_op_decode_attention": (i32, [cache, i32, i32, i32, i32, rows, vp, vp, rows, vp, sz,
+                                          vp, vp]),
+        "jnx_op_vocab_loss_workspace_bytes": (sz, [i32, i32, i32]),
+        "jnx_op_vocab_loss": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, vp, vp, sz, vp, vp]),
+        "jnx_op_vocab_loss_train_workspace_bytes": (sz, [i32, i32, i32, i32]),
+        "jnx_op_vocab_loss_train": (i32, [vp, i64, vp, i64, vp, vp, i32, i32, i32, i32, vp, vp,
+                                          i64, vp, i64, vp, sz, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -396,7 +448,8 @@ KERNEL_NAMES = {1: "pack", 2: "rmsnorm", 3: "gemm_qkv_rope", 4: "attention", 5: 
                 9: "rope_table", 10: "heads_fwd", 11: "heads_bwd", 12: "gemm", 13: "lora_down",
                 14: "heads_adamw", 15: "gemm_bwd", 16: "attention_bwd", 17: "norm_bwd",
                 18: "lora_bwd", 19: "flow_gemm", 20: "flow_attention", 21: "flow_misc",
-                22: "flow_wgrad"}
+                22: "flow_wgrad", 23: "qk_norm_rope", 24: "prompt_attention",
+                25: "prompt_attention_bwd", 26: "decode_attention", 27: "vocab_loss"}
 TENSOR_KERNELS = (3, 4, 5, 6, 7, 12, 13, 15, 16, 18, 19, 20, 22)
 
 

@@ -547,3 +547,264 @@ class StepPipeline:
         self.done[(n - 1) & 1].synchronize()
         if on_result is not None:
             on_result(n - 1, self.loss_h[(n - 1) & 1], self.preds_h[(n - 1) & 1])
+
+
+# ---------------------------------------------------------------------------
+# operators of text tenants
+# ---------------------------------------------------------------------------
+
+def _bf16(t: torch.Tensor, *shape) -> torch.Tensor:
+    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != shape or \
+            (t.stride(-1) != 1 and shape[-1] > 1):
+        raise ValueError(f"expected a bf16 CUDA tensor {shape} with contiguous last axis, got "
+                         f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return t
+
+
+def _rows(t: torch.Tensor, *shape) -> J.jnx_head_rows:
+    """Head rows [n, heads, head_dim] of any row and head stride."""
+    _bf16(t, *shape)
+    return J.jnx_head_rows(t.data_ptr() or None, t.stride(0), t.stride(1))
+
+
+def _dense(t: torch.Tensor, dtype, *shape) -> int:
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} CUDA tensor {shape}, got {t.dtype} "
+                         f"{tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _cache(k: torch.Tensor, v: torch.Tensor, n_kv_heads: int, head_dim: int) -> J.jnx_kv_cache:
+    """A cache [slots, room, kv heads, head_dim]; k and v with the same strides."""
+    slots, room = k.shape[:2]
+    _bf16(k, slots, room, n_kv_heads, head_dim)
+    _bf16(v, slots, room, n_kv_heads, head_dim)
+    if k.stride() != v.stride():
+        raise ValueError(f"cache strides differ: {k.stride()} and {v.stride()}")
+    return J.jnx_kv_cache(k.data_ptr() or None, v.data_ptr() or None, slots, room, k.stride(0),
+                          k.stride(1), k.stride(2))
+
+
+class _TextOperator:
+    """What the operators share: the status word their kernels report to and scratch
+    memory, both the object's own (calls on several streams at once take an object each)."""
+
+    def __init__(self, ws_bytes: int = 0, device="cuda"):
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.ws = torch.empty(max(int(ws_bytes), 16), dtype=torch.uint8, device=device)
+        self._status, self._ws, self._nws = (self.status.data_ptr(), self.ws.data_ptr(),
+                                             self.ws.numel())
+
+    def check(self) -> None:
+        """Raise what a kernel reported since the last check (waits for the device)."""
+        code = int(self.status.item())
+        self.status.zero_()
+        if code != J.JNX_OK:
+            raise J.JnxError(code, "reported by a kernel")
+
+
+class QKNormRope(_TextOperator):
+    """Norms of each query and key head (gains gamma_q, gamma_k; None: no norm) and
+    rotate-half RoPE over one or more position axes, `sections` frequencies to each."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int,
+                 gamma_q: Optional[torch.Tensor] = None, gamma_k: Optional[torch.Tensor] = None,
+                 sections: Optional[Sequence[int]] = None, theta: float = 10000.0,
+                 eps: float = 1e-6, device="cuda"):
+        self.sections = tuple(sections) if sections is not None else (head_dim // 2,)
+        if len(self.sections) > 4:
+            raise ValueError("at most four position axes")
+        self.dims = (n_heads, n_kv_heads, head_dim)
+        self.gains = tuple(None if g is None else _bf16(g, head_dim) for g in (gamma_q, gamma_k))
+        self.struct = J.jnx_qk_rope(n_heads, n_kv_heads, head_dim, len(self.sections),
+                                    (J.C.c_int32 * 4)(*self.sections), theta, eps,
+                                    _ptr(gamma_q), _ptr(gamma_k))
+        self._ref = C.byref(self.struct)
+        # enough for any number of tokens: the gradient's CTAs are bounded
+        super().__init__(J.lib().jnx_op_qk_norm_rope_backward_workspace_bytes(self._ref, 1 << 30),
+                         device)
+
+    def _args(self, qkv: torch.Tensor, pos: torch.Tensor):
+        h, hkv, hd = self.dims
+        n = qkv.shape[0]
+        _bf16(qkv, n, (h + 2 * hkv) * hd)
+        return n, self._ref, qkv.data_ptr(), qkv.stride(0), \
+            _dense(pos, torch.int32, len(self.sections), n)
+
+    def forward(self, qkv: torch.Tensor, pos: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                stream=None) -> None:
+        """q [n, H, hd] and k [n, Hkv, hd] from qkv [n, (H + 2 Hkv) hd] at pos [axes, n]."""
+        h, hkv, hd = self.dims
+        n, ref, x, ld, p = self._args(qkv, pos)
+        J.check(J.lib().jnx_op_qk_norm_rope(ref, x, ld, p, n, C.byref(_rows(q, n, h, hd)),
+                                            C.byref(_rows(k, n, hkv, hd)), _stream(stream)))
+
+    def append(self, qkv: torch.Tensor, pos: torch.Tensor, q: torch.Tensor,
+               k_cache: torch.Tensor, v_cache: torch.Tensor, slot: torch.Tensor,
+               at: torch.Tensor, stream=None) -> None:
+        """q as forward; key and value rows go to cache rows [slot[i], at[i]]."""
+        h, hkv, hd = self.dims
+        n, ref, x, ld, p = self._args(qkv, pos)
+        J.check(J.lib().jnx_op_qk_norm_rope_append(
+            ref, x, ld, p, n, C.byref(_rows(q, n, h, hd)),
+            C.byref(_cache(k_cache, v_cache, hkv, hd)), _dense(slot, torch.int32, n),
+            _dense(at, torch.int32, n), self._status, _stream(stream)))
+
+    def backward(self, qkv: torch.Tensor, pos: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
+                 dqkv: torch.Tensor, dgamma_q: Optional[torch.Tensor] = None,
+                 dgamma_k: Optional[torch.Tensor] = None, stream=None) -> None:
+        """dqkv's query and key columns (same strides as qkv) and the gains' gradients."""
+        h, hkv, hd = self.dims
+        n, ref, x, ld, p = self._args(qkv, pos)
+        _bf16(dqkv, *qkv.shape)
+        if dqkv.stride(0) != ld:
+            raise ValueError("dqkv and qkv differ in their row strides")
+        gains = [None if g is None else _dense(g, torch.float32, hd) for g in (dgamma_q, dgamma_k)]
+        J.check(J.lib().jnx_op_qk_norm_rope_backward(
+            ref, x, ld, p, n, C.byref(_rows(dq, n, h, hd)), C.byref(_rows(dk, n, hkv, hd)),
+            dqkv.data_ptr(), *gains, self._ws, self._nws, _stream(stream)))
+
+
+class PromptPlan:
+    """Packed prompts: query and key lengths of each sequence and the keys at its start
+    that every row sees.  The queries are the last of a sequence's positions."""
+
+    def __init__(self, q_lens: Sequence[int], kv_lens: Optional[Sequence[int]] = None,
+                 prefix: Optional[Sequence[int]] = None, device="cuda"):
+        kv_lens = q_lens if kv_lens is None else kv_lens
+        if len(kv_lens) != len(q_lens) or (prefix is not None and len(prefix) != len(q_lens)):
+            raise ValueError("lengths of different numbers of sequences")
+        cu = lambda n: np.concatenate([[0], np.cumsum(n, dtype=np.int64)]).astype(np.int64)
+        both = [cu(q_lens), cu(kv_lens)]
+        if any(int(x[-1]) >= 2 ** 31 for x in both):
+            raise ValueError("2^31 rows or more")
+        self.h = [x.astype(np.int32) for x in both]
+        if prefix is not None and any(prefix):
+            self.h.append(np.asarray(prefix, dtype=np.int32))
+        self.n_seqs, self.device = len(q_lens), device
+        self.n_q, self.n_kv = int(self.h[0][-1]), int(self.h[1][-1])
+        self.d = [torch.from_numpy(x).to(device) for x in self.h]
+
+    def struct(self, n_heads: int, n_kv_heads: int, head_dim: int):
+        """The prompt with its work lists for a head layout, and what they lie in."""
+        ptrs = [x.data_ptr() for x in self.d] + [None] * (3 - len(self.d))
+        host = [x.ctypes.data_as(J.P32) for x in self.h] + [None] * (3 - len(self.h))
+        p = J.jnx_prompt(self.n_seqs, *ptrs, *host, None, 0, 0, 0)
+        L = J.lib()
+        n = L.jnx_prompt_items(C.byref(p), n_heads, n_kv_heads, head_dim, None, 0)
+        if n < 0:
+            J.check(n)
+        items = np.zeros((max(n, 1), 2), dtype=np.int32)
+        L.jnx_prompt_items(C.byref(p), n_heads, n_kv_heads, head_dim, items.ctypes.data, n)
+        items = torch.from_numpy(items).to(self.device)
+        p.items = items.data_ptr()
+        return p, items
+
+
+class PromptAttention(_TextOperator):
+    """Attention of packed prompts, causal behind the plan's prefixes, and its gradients."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, plan: PromptPlan,
+                 gradients: bool = False):
+        self.plan, self.dims = plan, (n_heads, n_kv_heads, head_dim)
+        self.struct, self.items = plan.struct(*self.dims)
+        self._ref = C.byref(self.struct)
+        super().__init__(J.lib().jnx_op_prompt_attention_backward_workspace_bytes(
+            plan.n_q, n_heads) if gradients else 0, plan.device)
+
+    def _q(self, t):
+        return C.byref(_rows(t, self.plan.n_q, self.dims[0], self.dims[2]))
+
+    def _kv(self, t):
+        return C.byref(_rows(t, self.plan.n_kv, self.dims[1], self.dims[2]))
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                lse: Optional[torch.Tensor] = None, stream=None) -> None:
+        """out [n_q, H, hd]; lse [n_q, H] fp32 where the gradients are wanted later."""
+        if lse is not None:
+            lse = _dense(lse, torch.float32, self.plan.n_q, self.dims[0])
+        J.check(J.lib().jnx_op_prompt_attention(
+            self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out), lse,
+            self._status, _stream(stream)))
+
+    def backward(self, q, k, v, out, lse, dout, dq, dk, dv, stream=None) -> None:
+        """dq, dk, dv from dout, with the forward's out and lse."""
+        J.check(J.lib().jnx_op_prompt_attention_backward(
+            self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out),
+            _dense(lse, torch.float32, self.plan.n_q, self.dims[0]), self._q(dout), self._q(dq),
+            self._kv(dk), self._kv(dv), self._ws, self._nws, self._status, _stream(stream)))
+
+
+class DecodeAttention(_TextOperator):
+    """Attention of one new token of each live sequence against its cache."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, max_batch: int,
+                 device="cuda"):
+        self.dims, self.max_batch = (n_heads, n_kv_heads, head_dim), max_batch
+        super().__init__(J.lib().jnx_op_decode_attention_workspace_bytes(max_batch, n_heads,
+                                                                         head_dim), device)
+
+    def forward(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                slot: torch.Tensor, n_cached: torch.Tensor, out: torch.Tensor,
+                stream=None) -> None:
+        """out [b, H, hd] of q [b, H, hd] over the first n_cached[i] tokens of slot[i] in
+        the cache [slots, room, Hkv, hd]."""
+        h, hkv, hd = self.dims
+        b = q.shape[0]
+        if b > self.max_batch:
+            raise ValueError(f"batch of {b}, at most {self.max_batch}")
+        cache = _cache(k_cache, v_cache, hkv, hd)
+        J.check(J.lib().jnx_op_decode_attention(
+            C.byref(cache), b, h, hkv, hd, C.byref(_rows(q, b, h, hd)),
+            _dense(slot, torch.int32, b), _dense(n_cached, torch.int32, b),
+            C.byref(_rows(out, b, h, hd)), self._ws, self._nws, self._status, _stream(stream)))
+
+
+class VocabLoss(_TextOperator):
+    """Next-token losses of hidden rows over a vocabulary w [vocab, d], and their
+    gradients; the logits are never stored."""
+
+    def __init__(self, w: torch.Tensor, max_rows: int, gradients: bool = True,
+                 piece_rows: int = 0):
+        self.w, (self.vocab, self.d) = _bf16(w, *w.shape), w.shape
+        self.max_rows, self.piece_rows, self.gradients = max_rows, piece_rows, gradients
+        L = J.lib()
+        need = L.jnx_op_vocab_loss_workspace_bytes(max_rows, self.vocab, self.d)
+        if gradients:
+            need = max(need, L.jnx_op_vocab_loss_train_workspace_bytes(max_rows, self.vocab,
+                                                                       self.d, piece_rows))
+        super().__init__(need, w.device)
+
+    def _args(self, h: torch.Tensor, targets: torch.Tensor):
+        n = h.shape[0]
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, at most {self.max_rows}")
+        _bf16(h, n, self.d)
+        return n, h.data_ptr(), h.stride(0), self.w.data_ptr(), self.w.stride(0), \
+            _dense(targets, torch.int32, n)
+
+    def loss(self, h: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor,
+             stream=None) -> None:
+        """loss [n] fp32 of h [n, d]; 0 where targets [n] is negative."""
+        n, *args = self._args(h, targets)
+        J.check(J.lib().jnx_op_vocab_loss(
+            *args, n, self.vocab, self.d, _dense(loss, torch.float32, n), self._ws, self._nws,
+            self._status, _stream(stream)))
+
+    def train(self, h: torch.Tensor, targets: torch.Tensor, row_weight: torch.Tensor,
+              loss: torch.Tensor, dh: torch.Tensor, dw: Optional[torch.Tensor] = None,
+              stream=None) -> None:
+        """Also the gradients of sum(row_weight * loss): dh [n, d] and dw [vocab, d] (None:
+        a frozen vocabulary), bf16."""
+        if not self.gradients:
+            raise ValueError("made for losses only (gradients=False)")
+        n, *args = self._args(h, targets)
+        _bf16(dh, n, self.d)
+        grads = [dh.data_ptr(), dh.stride(0), None, 0]
+        if dw is not None:
+            _bf16(dw, self.vocab, self.d)
+            grads[2:] = [dw.data_ptr(), dw.stride(0)]
+        J.check(J.lib().jnx_op_vocab_loss_train(
+            *args, _dense(row_weight, torch.float32, n), n, self.vocab, self.d, self.piece_rows,
+            _dense(loss, torch.float32, n), *grads, self._ws, self._nws, self._status,
+            _stream(stream)))

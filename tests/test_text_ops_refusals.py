@@ -1,0 +1,177 @@
+"""What the text operators refuse, on the host before any launch (no GPU needed), and the
+work lists of packed prompts."""
+import ctypes as C
+import itertools
+
+import numpy as np
+import pytest
+
+from paper_2607_16074_gb300 import build as B
+from paper_2607_16074_gb300 import jnx as J
+
+BUF = C.create_string_buffer(1 << 16)
+PTR = (C.addressof(BUF) + 63) & ~63
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    B.build()
+
+
+def rows(ptr=PTR, row=1024, head=128):
+    return C.byref(J.jnx_head_rows(ptr, row, head))
+
+
+def rope(h=8, hkv=2, hd=128, sections=(64,), theta=1e4, eps=1e-6, gq=None):
+    return C.byref(J.jnx_qk_rope(h, hkv, hd, len(sections), (C.c_int32 * 4)(*sections), theta, eps,
+                                 gq, None))
+
+
+def prompt(q=(5, 3), kv=(5, 3), prefix=None, device=True):
+    keep = [np.concatenate([[0], np.cumsum(x)]).astype(np.int32) for x in (q, kv)]
+    if prefix is not None:
+        keep.append(np.asarray(prefix, np.int32))
+    host = [x.ctypes.data_as(J.P32) for x in keep] + [None] * (3 - len(keep))
+    dev = [PTR if device else None] * 2 + [PTR if prefix is not None else None]
+    p = J.jnx_prompt(len(q), *dev, *host, PTR, 1, 1, 1)
+    p.keep = keep
+    return p
+
+
+def refused(code, expected):
+    assert code == expected and J.jnx_last_error()
+
+
+INV, UNS, WS = J.JNX_ERR_INVALID_ARG, J.JNX_ERR_UNSUPPORTED, J.JNX_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(hd=96), UNS), (dict(sections=(65,)), INV), (dict(sections=(32, 40)), INV),
+    (dict(sections=(-1,)), INV), (dict(theta=0.0), INV), (dict(eps=-1.0), INV), (dict(h=-1), INV),
+    (dict(gq=PTR + 2), INV)])
+def test_rope_refuses(bad, code):
+    L = J.lib()
+    refused(L.jnx_op_qk_norm_rope(rope(**bad), PTR, 1536, PTR, 4, rows(), rows(), None), code)
+    refused(L.jnx_op_qk_norm_rope_backward(rope(**bad), PTR, 1536, PTR, 4, rows(), rows(), PTR, PTR,
+                                           PTR, PTR, 1 << 20, None), code)
+
+
+def test_rope_refuses_pointers_and_strides():
+    L, r = J.lib(), rope()
+    f = lambda x=PTR, ld=1536, pos=PTR, n=4, q=rows(), k=rows(): L.jnx_op_qk_norm_rope(  # noqa: E731
+        r, x, ld, pos, n, q, k, None)
+    for bad in (dict(x=None), dict(x=PTR + 8), dict(ld=1535), dict(ld=1528), dict(pos=None),
+                dict(n=-1), dict(q=rows(PTR + 4)), dict(q=rows(row=1020)), dict(k=rows(head=4)),
+                dict(k=rows(None))):
+        refused(f(**bad), INV)
+    assert f(n=0) == J.JNX_OK
+    refused(L.jnx_op_qk_norm_rope_backward(rope(gq=PTR), PTR, 1536, PTR, 4, rows(), rows(), PTR, PTR,
+                                           None, PTR, 8, None), WS)
+    refused(L.jnx_op_qk_norm_rope_backward(rope(gq=PTR), PTR, 1536, PTR, 4, rows(), rows(), PTR,
+                                           None, None, PTR, 1 << 20, None), INV)
+    cache = J.jnx_kv_cache(PTR, PTR, 2, 4, 1024, 256, 128)
+    a = lambda c, slot=PTR, at=PTR: L.jnx_op_qk_norm_rope_append(  # noqa: E731
+        r, PTR, 1536, PTR, 4, rows(), C.byref(c) if c else None, slot, at, None, None)
+    for c, kw in ((None, {}), (cache, dict(slot=None)), (cache, dict(at=None)),
+                  (J.jnx_kv_cache(PTR, None, 2, 4, 1024, 256, 128), {}),
+                  (J.jnx_kv_cache(PTR, PTR, -1, 4, 1024, 256, 128), {}),
+                  (J.jnx_kv_cache(PTR, PTR, 2, 4, 1024, 250, 128), {})):
+        refused(a(c, **kw), INV)
+
+
+def attend(p, h=8, hkv=2, hd=128, q=rows(), k=rows(), v=rows(), out=rows()):
+    return J.lib().jnx_op_prompt_attention(C.byref(p), h, hkv, hd, q, k, v, out, None, None, None)
+
+
+def test_prompt_attention_refuses():
+    for kw, code in ((dict(h=7), INV), (dict(hkv=0), INV), (dict(hd=80), UNS), (dict(h=130), UNS),
+                     (dict(q=rows(None)), INV), (dict(k=rows(PTR + 2)), INV),
+                     (dict(v=rows(row=129)), INV), (dict(out=rows(head=12)), INV)):
+        refused(attend(prompt(), **kw), code)
+    bad = prompt()
+    bad.keep[0][1] = 9
+    refused(attend(bad), INV)
+    refused(attend(prompt(prefix=(0, -1))), INV)
+    refused(attend(prompt(device=False)), INV)
+    bad = prompt()
+    bad.items = None
+    refused(attend(bad), INV)
+    assert attend(prompt(q=(), kv=())) == J.JNX_OK
+
+
+def test_prompt_attention_backward_refuses():
+    L = J.lib()
+    f = lambda p=prompt(), lse=PTR, ws=PTR, n=1 << 16, dk=rows(): \
+        L.jnx_op_prompt_attention_backward(C.byref(p), 8, 2, 128, rows(), rows(), rows(), rows(), lse,
+                                           rows(), rows(), dk, rows(), ws, n, None, None)
+    refused(f(lse=None), INV)
+    refused(f(dk=rows(None)), INV)
+    refused(f(ws=None), WS)
+    refused(f(n=L.jnx_op_prompt_attention_backward_workspace_bytes(8, 8) - 1), WS)
+    assert f(p=prompt(q=(0,), kv=(0,))) == J.JNX_OK
+
+
+def test_decode_refuses():
+    L = J.lib()
+    cache = J.jnx_kv_cache(PTR, PTR, 2, 4, 1024, 256, 128)
+    need = L.jnx_op_decode_attention_workspace_bytes(3, 8, 128)
+
+    def f(b=3, h=8, hkv=2, hd=128, c=cache, q=rows(), slot=PTR, n=PTR, out=rows(), ws=PTR, nws=need):
+        return L.jnx_op_decode_attention(C.byref(c), b, h, hkv, hd, q, slot, n, out, ws, nws, None,
+                                         None)
+    for kw, code in ((dict(b=-1), INV), (dict(h=9), INV), (dict(hd=32), UNS), (dict(q=rows(None)), INV),
+                     (dict(out=rows(row=100)), INV), (dict(slot=None), INV), (dict(n=None), INV),
+                     (dict(c=J.jnx_kv_cache(None, PTR, 2, 4, 1024, 256, 128)), INV)):
+        refused(f(**kw), code)
+    assert f(b=0) == J.JNX_OK
+
+
+def test_vocab_loss_refuses():
+    L = J.lib()
+    need = L.jnx_op_vocab_loss_train_workspace_bytes(4, 100, 64, 0)
+
+    def f(h=PTR, ldh=64, w=PTR, ldw=64, t=PTR, rw=PTR, n=4, v=100, d=64, loss=PTR, dh=PTR, lddh=64,
+          dw=PTR, lddw=64, ws=PTR, nws=need):
+        return L.jnx_op_vocab_loss_train(h, ldh, w, ldw, t, rw, n, v, d, 0, loss, dh, lddh, dw, lddw,
+                                         ws, nws, None, None)
+    for kw in (dict(h=None), dict(h=PTR + 8), dict(ldh=60), dict(ldh=68), dict(w=None), dict(ldw=62),
+               dict(t=None), dict(rw=None), dict(n=-1), dict(v=0), dict(d=60), dict(d=0),
+               dict(loss=None), dict(dh=None), dict(dh=PTR + 4), dict(lddh=63), dict(dw=PTR + 6),
+               dict(lddw=56)):
+        refused(f(**kw), INV)
+    refused(f(ws=None), WS)
+    refused(f(nws=need - 1), WS)
+    assert f(n=0, dw=None) == J.JNX_OK
+
+
+@pytest.mark.parametrize("heads", [(4, 4, 64), (8, 1, 256), (12, 4, 128), (14, 2, 64)])
+def test_work_lists_cover_every_row_and_key_once(heads):
+    """Each pass visits every row (or key) of every sequence, the longest work first."""
+    h, hkv, hd = heads
+    q, kv, pre = (300, 0, 1, 129, 40), (300, 7, 5, 60, 400), (0, 3, 0, 9, 390)
+    p = prompt(q, kv, pre)
+    n = J.lib().jnx_prompt_items(C.byref(p), h, hkv, hd, None, 0)
+    out = np.zeros((n, 2), np.int32)
+    assert J.lib().jnx_prompt_items(C.byref(p), h, hkv, hd, out.ctypes.data, n) == n
+    assert n == p.n_forward + p.n_keys + p.n_queries
+    tok = 128 // (h // hkv)
+    steps = (tok * (1 if hd == 256 else 2), 128, tok)
+    at = 0
+    for count, step, lens, pass_ in zip((p.n_forward, p.n_keys, p.n_queries), steps, (q, kv, q), range(3)):
+        items, at = out[at:at + count], at + count
+        seen = set()
+        for s, a in items:
+            for i in range(a, min(a + step, lens[s])):
+                assert (s, i) not in seen
+                seen.add((int(s), i))
+        assert seen == {(s, i) for s, n_ in enumerate(lens) for i in range(n_)}
+
+        def visible(s, i):  # keys that row i sees
+            return max(0, min(kv[s], max(kv[s] - q[s] + i + 1, pre[s])))
+
+        def cost(s, a):
+            if pass_ == 1:
+                return sum(1 for i in range(q[s]) if visible(s, i) > a)
+            return visible(s, min(a + step, q[s]) - 1)
+        costs = [cost(int(s), int(a)) for s, a in items]
+        assert all(x >= y for x, y in itertools.pairwise(costs))
