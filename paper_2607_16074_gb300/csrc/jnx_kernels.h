@@ -7,6 +7,7 @@
 #include <atomic>
 #include <vector>
 
+#include "../../include/jnx_ops.h"
 #include "jnx_host.h"
 
 namespace jnx {
@@ -196,6 +197,10 @@ jnx_status gemm_launch(const uint16_t* A, int lda, const uint16_t* B, int ldb, G
 bool make_tmap_bf16(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols,
                     uint64_t row_stride_elems, uint32_t box_rows, uint32_t box_cols,
                     int swizzle_bytes = 128);
+// Head rows [n_rows][heads][hd] of any row and head stride (elements, multiples of 8):
+// boxes of 64 columns x box_heads x box_rows, 128-byte swizzled.
+bool make_tmap_heads(CUtensorMap* m, const jnx_head_rows& r, int n_rows, int heads, int hd,
+                     int box_heads, int box_rows);
 int num_sms();
 
 // Raise fn's dynamic shared-memory limit to `bytes` on the current device,

@@ -1,5 +1,31 @@
 // Attention of packed prompts: causal behind a prefix that every row sees, query rows
 // the last of a sequence's positions, grouped heads.
+//
+// O = softmax(Q K^T / sqrt(hd)) V in one pass over the keys with a running maximum m and
+// sum l: P = 2^(S c - m), O <- O 2^(m_old - m) + P V, l likewise; O / l does not depend
+// on m, so m (and O) only move when a tile's maximum is over 2^8 times the old one.
+//
+// A 128-row tile holds (token, query head of one group) pairs: 128 / group tokens times
+// the group's heads, so the heads that share a key head share its tiles, and a causal
+// edge wastes 128 / group tokens of a tile and not 128.  An item is two such tiles in a
+// row (one at head dim 256, whose O leaves no TMEM for a second) of one key head and
+// walks the 128-key tiles that its last row sees.
+//
+// One CTA per SM, persistent, over the items from the longest to the shortest, forwards
+// and backwards in turn so that the rounds' inequalities cancel.  Roles:
+//   warp 0       TMA: the item's Q tiles (3-D boxes: 64 columns x heads x tokens), then
+//                K and V through one ring of 16 KB units (K: 128 keys x 64 columns,
+//                V: 8,192 / hd keys x hd columns), in the order the MMAs take them
+//   warp 1       MMA issuer.  Two tiles: S of a tile overwrites its P once PV is issued
+//                and the other tile's products run while this one's softmax does.  One
+//                tile (head dim 256): two score buffers, S two key tiles ahead of PV.
+//   warps 4-     softmax and epilogue, a warpgroup a tile, a thread a row: the row's 128
+//                scores are in registers, so no row quantity is exchanged
+// P (bf16) overwrites the first 64 columns of its scores and is the TMEM A operand of
+// the PV product; V is the MN-major B operand as it lies.
+//
+// Rows beyond a sequence's keys in its last V tile are zeroed in shared memory: they
+// belong to another sequence and may be NaN, and 0 * NaN would reach O.
 #include <algorithm>
 #include <vector>
 
@@ -10,48 +36,529 @@
 
 namespace jnx {
 
+namespace pattn {
+constexpr int BM = 128, BN = 128;
+constexpr int UNIT = 16384;  // bytes of a ring unit
+constexpr int RING = 10;
+constexpr float kLazy = 8.0f;  // log2 growth of the maximum that moves it
+// barriers: ring full / empty, then
+enum { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_FULL = 6, PV_DONE = 8, O_FULL = 10, O_FREE = 12,
+       DRAIN = 14, N_BARS = 15 };
+}  // namespace pattn
+
+template <int HD>
+struct PromptCfg {
+    static constexpr int NST = HD == 256 ? 1 : 2;  // row tiles of an item
+    static constexpr int NU = HD / 64;             // units of a K or V tile
+    static constexpr int VKEYS = pattn::BN / NU;   // keys of a V unit
+    static constexpr int QB = pattn::BM * HD * 2;
+    static constexpr int OFF_RING = NST * QB;
+    static constexpr int OFF_BAR = OFF_RING + pattn::RING * pattn::UNIT;
+    static constexpr int SMEM = OFF_BAR + (2 * pattn::RING + pattn::N_BARS) * 8 + 16 + 1024;
+    static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
+    static constexpr int THREADS = 128 + 128 * NST;
+    static constexpr uint32_t O_COL = 256;
+};
+
 struct PromptArgs {
     const int *cu_q, *cu_kv, *prefix;
     const int2* items;
-    int H, Hkv, group;
+    int n_work, H, Hkv, group;
     float scale_log2;
-    jnx_head_rows q, k, v, out;
+    uint16_t* out;
+    long long o_row, o_head;
     float* lse;
+    int* status;
 };
 
-// One warp a row (token, head), one key at a time.
-template <int HD>
-__global__ void __launch_bounds__(256) k_prompt_attn(const __grid_constant__ PromptArgs a) {
-    constexpr int E = HD / 32;
-    pdl_entry();
-    const int2 it = a.items[blockIdx.x / a.Hkv];
-    const int kvh = blockIdx.x % a.Hkv, s = it.x;
-    const int q0 = a.cu_q[s], Lq = a.cu_q[s + 1] - q0, k0 = a.cu_kv[s], Lk = a.cu_kv[s + 1] - k0;
-    const int pre = a.prefix ? a.prefix[s] : 0, lane = threadIdx.x & 31;
-    const int rows = min(tile_tokens(a.group) * item_tiles(HD), Lq - it.y) * a.group;
-    for (int r = threadIdx.x >> 5; r < rows; r += 8) {
-        const int i = it.y + r / a.group, h = kvh * a.group + r % a.group;
-        const int n = keys_seen(i, Lq, Lk, pre);
-        float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
-        for (int e = 0; e < E; ++e)
-            q[e] = bf2f(a.q.ptr[(q0 + i) * a.q.row_stride + h * a.q.head_stride + e * 32 + lane]);
-        for (int j = 0; j < n; ++j) {
-            const size_t ko = (k0 + j) * a.k.row_stride + kvh * a.k.head_stride + lane;
-            const size_t vo = (k0 + j) * a.v.row_stride + kvh * a.v.head_stride + lane;
-            float d = 0.f;
-            for (int e = 0; e < E; ++e) d += q[e] * bf2f(a.k.ptr[ko + e * 32]);
-            for (int x = 16; x; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
-            d *= a.scale_log2;
-            const float mn = fmaxf(m, d), c = exp2f(m - mn), p = exp2f(d - mn);
-            for (int e = 0; e < E; ++e) o[e] = o[e] * c + p * bf2f(a.v.ptr[vo + e * 32]);
-            l = l * c + p;
-            m = mn;
-        }
-        for (int e = 0; e < E; ++e)
-            a.out.ptr[(q0 + i) * a.out.row_stride + h * a.out.head_stride + e * 32 + lane] =
-                f2bf(n ? o[e] / l : 0.f);
-        if (a.lse && lane == 0) a.lse[(size_t)(q0 + i) * a.H + h] = n ? m + log2f(l) : -INFINITY;
+// One item: rows from token i0 of a sequence (global row q0 + i0) over its keys.
+struct PromptWork {
+    int q0, i0, Lq, k0, Lk, pre, kvh;
+    bool valid;
+
+    // key tiles that row tile t (T tokens) visits
+    __device__ __forceinline__ int key_tiles(int t, int T) const {
+        const int a = i0 + t * T;
+        if (a >= Lq) return 0;
+        return (keys_seen(min(a + T, Lq) - 1, Lq, Lk, pre) + pattn::BN - 1) / pattn::BN;
     }
+};
+
+__device__ __forceinline__ PromptWork prompt_fetch(const PromptArgs& a, int round) {
+    const int G = gridDim.x, b = blockIdx.x;
+    const int w = round * G + ((round & 1) ? G - 1 - b : b);
+    PromptWork x{0, 0, 0, 0, 0, 0, 0, false};
+    if (w >= a.n_work) return x;
+    const int2 it = a.items[w / a.Hkv];
+    x.kvh = w % a.Hkv;
+    x.i0 = it.y;
+    x.q0 = a.cu_q[it.x];
+    x.Lq = a.cu_q[it.x + 1] - x.q0;
+    x.k0 = a.cu_kv[it.x];
+    x.Lk = a.cu_kv[it.x + 1] - x.k0;
+    x.pre = a.prefix ? a.prefix[it.x] : 0;
+    x.valid = true;
+    return x;
+}
+
+__device__ __forceinline__ PromptWork prompt_uniform(PromptWork x) {
+    x.q0 = warp_uniform(x.q0);
+    x.i0 = warp_uniform(x.i0);
+    x.Lq = warp_uniform(x.Lq);
+    x.k0 = warp_uniform(x.k0);
+    x.Lk = warp_uniform(x.Lk);
+    x.pre = warp_uniform(x.pre);
+    x.kvh = warp_uniform(x.kvh);
+    x.valid = warp_uniform(x.valid);
+    return x;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
+    k_prompt_attn(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+                  const __grid_constant__ CUtensorMap tv, const __grid_constant__ PromptArgs a) {
+    using C = PromptCfg<HD>;
+    using namespace pattn;
+    constexpr int NST = C::NST, NU = C::NU;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* ring = sm + C::OFF_RING;
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + C::OFF_BAR);
+    uint64_t* empty = full + RING;
+    uint64_t* bar = empty + RING;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + N_BARS);
+    volatile int* fail_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int T = tile_tokens(a.group);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2 * RING; ++i) mbar_init(&full[i], 1);
+        for (int i = 0; i < N_BARS; ++i)
+            mbar_init(&bar[i], i == P_FULL || i == P_FULL + 1 || i == O_FREE || i == O_FREE + 1 ? BM
+                                                                                              : 1);
+        *fail_flag = 0;
+        fence_barrier_init();
+        fence_proxy_async();
+    }
+    pdl_entry();  // TMEM is taken once the grid ahead has given its own back
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = warp_uniform(*tmem_slot);
+    const int rounds = (a.n_work + gridDim.x - 1) / gridDim.x;
+
+    if (warp == 0) {
+        // ---------------- TMA producer ----------------
+        if (elect_one()) {
+            tma_prefetch_desc(&tq);
+            tma_prefetch_desc(&tk);
+            tma_prefetch_desc(&tv);
+        }
+        bool ok = true;
+        uint32_t u = 0;               // units loaded
+        uint32_t nq[2] = {0, 0};      // Q tiles loaded
+        const int qbytes = a.group * T * HD * 2;
+        auto load_tile = [&](bool is_v, const PromptWork& x, int kt) -> bool {
+            for (int c = 0; c < NU; ++c, ++u) {
+                const int s = u % RING;
+                if (!mbar_wait_warp(&empty[s], ((u / RING) & 1) ^ 1)) return false;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&full[s], UNIT);
+                    uint8_t* dst = ring + s * UNIT;
+                    const int row = x.k0 + kt * BN;
+                    if (!is_v) {
+                        tma_load_3d(dst, &tk, c * 64, x.kvh, row, &full[s]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < NU; ++j)
+                            tma_load_3d(dst + j * C::VKEYS * 128, &tv, j * 64, x.kvh,
+                                        row + c * C::VKEYS, &full[s]);
+                    }
+                }
+                __syncwarp();
+            }
+            return true;
+        };
+        PromptWork nxt = prompt_fetch(a, 0);
+        for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
+            const PromptWork x = prompt_uniform(nxt);
+            nxt = prompt_fetch(a, r + 1);
+            if (!x.valid) continue;
+            int n = 0;
+            for (int t = 0; t < NST && ok; ++t) {
+                const int nt = x.key_tiles(t, T);
+                n = max(n, nt);
+                if (nt == 0) continue;
+                if (nq[t] > 0 && !(ok = mbar_wait_warp(&bar[Q_EMPTY + t], (nq[t] - 1) & 1))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[Q_FULL + t], qbytes);
+#pragma unroll
+                    for (int c = 0; c < NU; ++c)
+                        tma_load_3d(sm + t * C::QB + c * BM * 128, &tq, c * 64, x.kvh * a.group,
+                                    x.q0 + x.i0 + t * T, &bar[Q_FULL + t]);
+                }
+                __syncwarp();
+                ++nq[t];
+            }
+            // K runs ahead of V by as many tiles as S runs ahead of PV
+            constexpr int AHEAD = NST == 1 ? 2 : 1;
+            for (int kt = 0; kt < AHEAD && kt < n && ok; ++kt) ok = load_tile(false, x, kt);
+            for (int kt = 0; kt < n && ok; ++kt) {
+                ok = load_tile(true, x, kt);
+                if (ok && kt + AHEAD < n) ok = load_tile(false, x, kt + AHEAD);
+            }
+        }
+        if (!ok) *fail_flag = 1;
+        // every copy has landed before the CTA may exit (at once in a normal run)
+        for (int t = 0; t < NST; ++t)
+            if (nq[t] > 0) mbar_wait_warp(&bar[Q_FULL + t], (nq[t] - 1) & 1, 100000000LL);
+        for (uint32_t i = u > RING ? u - RING : 0; i < u; ++i)
+            mbar_wait_warp(&full[i % RING], (i / RING) & 1, 100000000LL);
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
+        constexpr uint32_t IDESC_PV = idesc_bf16_f32(BM, HD) | (1u << 16);  // B MN-major
+        bool ok = true, issued = false;
+        uint32_t u = 0;                           // units taken
+        uint32_t nq[2] = {0, 0}, gp[2] = {0, 0};  // Q tiles, P tiles taken (by P barrier)
+        uint32_t no[2] = {0, 0};                  // items begun (per O accumulator)
+        uint32_t gs = 0;                          // score tiles issued (NST == 1)
+        const uint32_t q_lo = sw128_desc_lo(smem_u32(sm)), r_lo = sw128_desc_lo(smem_u32(ring));
+        auto commit = [&](uint64_t* b) {
+            if (elect_one()) tc_commit(b);
+            __syncwarp();
+        };
+        auto wait_units = [&](uint32_t first) -> bool {
+            for (uint32_t i = first; i < first + NU; ++i)
+                if (!mbar_wait_warp(&full[i % RING], (i / RING) & 1)) return false;
+            tc_fence_after();
+            return true;
+        };
+        auto free_units = [&](uint32_t first) {
+            if (elect_one())
+                for (uint32_t i = first; i < first + NU; ++i) tc_commit(&empty[i % RING]);
+            __syncwarp();
+        };
+        // S (columns d) of row tile t against the K tile in units [first, first + NU)
+        auto issue_s = [&](int t, uint32_t first, uint32_t d, uint64_t* done) {
+            if (elect_one()) {
+#pragma unroll
+                for (int c = 0; c < NU; ++c) {
+                    const uint32_t k_lo = r_lo + ((first + c) % RING) * (UNIT >> 4);
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        tc_mma_f16(d,
+                                   desc_of(q_lo + ((t * C::QB + c * BM * 128) >> 4) + ks * 2,
+                                           kSw128DescHi),
+                                   desc_of(k_lo + ks * 2, kSw128DescHi), IDESC_S, (c | ks) != 0);
+                }
+                tc_commit(done);
+            }
+            __syncwarp();
+            issued = true;
+        };
+        // O (columns d) += P (columns p) times the V tile in units [first, first + NU)
+        auto issue_pv = [&](uint32_t p, uint32_t first, uint32_t d, bool accumulate) {
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < BN / 16; ++ks) {
+                    const int un = ks * 16 / C::VKEYS, off = ks * 16 % C::VKEYS;
+                    const uint32_t va = smem_u32(ring) + ((first + un) % RING) * UNIT + off * 128;
+                    tc_mma_f16_ts(d, p + ks * 8, sw128_desc_mn(va, C::VKEYS * 128, 1024), IDESC_PV,
+                                  accumulate || ks > 0);
+                }
+            }
+            __syncwarp();
+        };
+        // rows of the V tile from `valid` on are not the sequence's: zero them
+        auto zero_tail = [&](uint32_t first, int valid) {
+            for (int r = valid; r < BN; ++r) {
+                uint8_t* row = ring + ((first + r / C::VKEYS) % RING) * UNIT + r % C::VKEYS * 128;
+                for (int i = lane; i < HD / 8; i += 32)
+                    *reinterpret_cast<uint4*>(row + (i >> 3) * C::VKEYS * 128 + (i & 7) * 16) =
+                        make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async();
+            __syncwarp();
+        };
+        PromptWork nxt = prompt_fetch(a, 0);
+        for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
+            const PromptWork x = prompt_uniform(nxt);
+            nxt = prompt_fetch(a, r + 1);
+            if (!x.valid) continue;
+            int nt[2] = {x.key_tiles(0, T), NST == 2 ? x.key_tiles(1, T) : 0};
+            const int n = max(nt[0], nt[1]);
+            if (n == 0) continue;
+            for (int t = 0; t < NST && ok; ++t)
+                if (nt[t] > 0) {
+                    ok = mbar_wait_warp(&bar[Q_FULL + t], nq[t] & 1);
+                    ++nq[t];
+                }
+            tc_fence_after();
+            if constexpr (NST == 2) {
+                if (!ok || !(ok = wait_units(u))) break;
+                for (int t = 0; t < 2; ++t)
+                    if (nt[t] > 0) {
+                        issue_s(t, u, tbase + t * BN, &bar[S_FULL + t]);
+                        if (nt[t] == 1) commit(&bar[Q_EMPTY + t]);
+                    }
+                free_units(u);
+                u += NU;
+                for (int kt = 0; kt < n && ok; ++kt) {
+                    const uint32_t uv = u, uk = u + NU;  // V(kt), K(kt + 1)
+                    bool have_v = false, have_k = false;
+                    for (int t = 0; t < 2; ++t) {
+                        if (kt >= nt[t]) continue;
+                        if (!(ok = mbar_wait_warp(&bar[P_FULL + t], gp[t] & 1))) break;
+                        ++gp[t];
+                        // the item's first product overwrites O: the last epilogue has read it
+                        if (kt == 0) {
+                            if (no[t] > 0 && !(ok = mbar_wait_warp(&bar[O_FREE + t], (no[t] - 1) & 1)))
+                                break;
+                            ++no[t];
+                        }
+                        if (!have_v) {
+                            if (!(ok = wait_units(uv))) break;
+                            if (x.Lk - kt * BN < BN) zero_tail(uv, x.Lk - kt * BN);
+                            have_v = true;
+                        }
+                        tc_fence_after();
+                        issue_pv(tbase + t * BN, uv, tbase + C::O_COL + t * HD, kt > 0);
+                        if (kt + 1 < nt[t]) {
+                            if (!have_k) {
+                                if (!(ok = wait_units(uk))) break;
+                                have_k = true;
+                            }
+                            issue_s(t, uk, tbase + t * BN, &bar[S_FULL + t]);
+                            if (kt + 2 == nt[t]) commit(&bar[Q_EMPTY + t]);
+                        } else {
+                            commit(&bar[O_FULL + t]);
+                        }
+                    }
+                    if (!ok) break;
+                    free_units(uv);
+                    u = uk;
+                    if (kt + 1 < n) {
+                        free_units(uk);
+                        u += NU;
+                    }
+                }
+            } else {
+                // score tile i goes to buffer gs % 2
+                auto next_s = [&](int kt) -> bool {
+                    if (!wait_units(u)) return false;
+                    issue_s(0, u, tbase + (gs & 1) * BN, &bar[S_FULL + (gs & 1)]);
+                    free_units(u);
+                    u += NU;
+                    ++gs;
+                    if (kt + 1 == n) commit(&bar[Q_EMPTY]);
+                    return true;
+                };
+                ok = ok && next_s(0) && (n < 2 || next_s(1));
+                for (int kt = 0; kt < n && ok; ++kt) {
+                    const uint32_t b = gp[0] & 1;
+                    if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (gp[0] >> 1) & 1))) break;
+                    ++gp[0];
+                    if (kt == 0) {
+                        if (no[0] > 0 && !(ok = mbar_wait_warp(&bar[O_FREE], (no[0] - 1) & 1))) break;
+                        ++no[0];
+                    }
+                    if (!(ok = wait_units(u))) break;
+                    if (x.Lk - kt * BN < BN) zero_tail(u, x.Lk - kt * BN);
+                    issue_pv(tbase + b * BN, u, tbase + C::O_COL, kt > 0);
+                    commit(&bar[PV_DONE + b]);
+                    free_units(u);
+                    u += NU;
+                    if (kt + 2 < n) ok = next_s(kt + 2);
+                }
+                if (ok) commit(&bar[O_FULL]);
+            }
+        }
+        if (!ok) *fail_flag = 1;
+        if (issued) {
+            commit(&bar[DRAIN]);
+            mbar_wait_warp(&bar[DRAIN], 0, 100000000LL);
+        }
+    } else if (warp >= 4) {
+        // ---------------- softmax + epilogue of row tile t ----------------
+        const int t = (warp - 4) >> 2;
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tO = tbase + lane_base + C::O_COL + t * HD;
+        uint32_t g = 0, items_done = 0;  // score tiles, items with keys
+        bool ok = true;
+        const int tok = row / a.group, hg = row % a.group;
+        PromptWork nxt = prompt_fetch(a, 0);
+        for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
+            const PromptWork x = nxt;
+            nxt = prompt_fetch(a, r + 1);
+            if (!x.valid) continue;
+            const int n = x.key_tiles(t, T);
+            const int i = x.i0 + t * T + tok;
+            const bool live = tok < T && i < x.Lq;
+            // keys of this row; a row that is none of the tile's has no say in the masks
+            const int lim = live ? keys_seen(i, x.Lq, x.Lk, x.pre) : 0x7fffffff;
+            float m = -INFINITY, l = 0.f;
+            for (int kt = 0; kt < n; ++kt) {
+                const uint32_t b = NST == 1 ? g & 1 : t;
+                const uint32_t ph = NST == 1 ? (g >> 1) & 1 : g & 1;
+                const uint32_t tS = tbase + lane_base + b * BN;
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[S_FULL + b], ph)))) break;
+                tc_fence_after();
+                uint32_t v[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, v[c]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld_wait_regs(v[c]);
+                const bool whole = __all_sync(0xffffffffu, lim >= (kt + 1) * BN);
+                if (!whole) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (kt * BN + c * 32 + e >= lim) v[c][e] = 0xff800000u;  // -inf
+                }
+                float mx[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    mx[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+                    for (int e = 1; e < 31; e += 2)
+                        mx[c] = fmax3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
+                    mx[c] = fmaxf(mx[c], __uint_as_float(v[c][31]));
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+                float alpha = 1.f;
+                if (kt == 0) {
+                    m = top;
+                } else if (top > m + kLazy) {
+                    alpha = ex2_approx(m - top);
+                    m = top;
+                }
+                if (kt > 0 && __any_sync(0xffffffffu, alpha < 1.f)) {
+                    // every earlier PV of the item is done: with one score buffer S was
+                    // issued behind it, with two it is waited for
+                    if (NST == 1) {
+                        const uint32_t pb = (g - 1) & 1;
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[PV_DONE + pb],
+                                                                     ((g - 1) >> 1) & 1))))
+                            break;
+                        tc_fence_after();
+                    }
+#pragma unroll 1
+                    for (int c = 0; c < HD / 16; ++c) {
+                        uint32_t o16[16];
+                        tmem_ld16(tO + c * 16, o16);
+                        tmem_ld_wait_regs16(o16);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            o16[e] = __float_as_uint(__uint_as_float(o16[e]) * alpha);
+                        tmem_st16(tO + c * 16, o16);
+                    }
+                    tmem_st_wait();
+                }
+                // a row that has seen no key yet subtracts nothing
+                const float sub = m == -INFINITY ? 0.f : m;
+                const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2), nm2 = f2_pack(-sub, -sub);
+                uint64_t rs[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float x0, x1, p0, p1;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(v[2 * h + c][e]),
+                                                     __uint_as_float(v[2 * h + c][e + 1])),
+                                             sc2, nm2),
+                                      x0, x1);
+                            p0 = ex2_approx(x0);
+                            p1 = ex2_approx(x1);
+                            rs[(e >> 1) & 1] = f2_add(rs[(e >> 1) & 1], f2_pack(p0, p1));
+                            pk[c * 16 + e / 2] = pack_bf2(p0, p1);
+                        }
+                    tmem_st32(tS + h * 32, pk);
+                }
+                float r0, r1, r2, r3;
+                f2_unpack(rs[0], r0, r1);
+                f2_unpack(rs[1], r2, r3);
+                l = l * alpha + ((r0 + r1) + (r2 + r3));
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(&bar[P_FULL + b]);
+                ++g;
+            }
+            if (!ok) break;
+            if (n > 0) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[O_FULL + t], items_done & 1)))) break;
+                tc_fence_after();
+                ++items_done;
+            }
+            const int h = x.kvh * a.group + hg;
+            uint16_t* o = a.out + (long long)(x.q0 + i) * a.o_row + h * a.o_head;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            if (live && a.lse) a.lse[(size_t)(x.q0 + i) * a.H + h] = m + log2f(l);
+#pragma unroll 1
+            for (int c = 0; c < HD / 32; ++c) {
+                uint32_t w[32];
+                if (n > 0) {
+                    tmem_ld32(tO + c * 32, w);
+                    tmem_ld_wait_regs(w);
+                    if (c + 1 == HD / 32) {
+                        tc_fence_before();
+                        mbar_arrive(&bar[O_FREE + t]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) w[e] = 0;
+                }
+                if (live) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint4 q;
+                        uint32_t* qp = &q.x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            // a row without keys: O holds products of zeros
+                            qp[e] = l > 0.f ? pack_bf2(__uint_as_float(w[8 * j + 2 * e]) * inv,
+                                                       __uint_as_float(w[8 * j + 2 * e + 1]) * inv)
+                                            : 0u;
+                        *reinterpret_cast<uint4*>(o + c * 32 + j * 8) = q;
+                    }
+                }
+            }
+        }
+        if (!ok) *fail_flag = 1;
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (*fail_flag && threadIdx.x == 0) report(a.status, JNX_ERR_TIMEOUT);
+    if (warp == 1) tmem_dealloc(tbase, 512);
+}
+
+template <int HD>
+static jnx_status launch_prompt(const PromptArgs& a, const jnx_head_rows& q, const jnx_head_rows& k,
+                                const jnx_head_rows& v, int rows, int keys, cudaStream_t s) {
+    using C = PromptCfg<HD>;
+    static std::atomic<uint64_t> attr{0};
+    if (set_smem_limit(reinterpret_cast<const void*>(k_prompt_attn<HD>), C::SMEM, attr) != cudaSuccess)
+        return fail(JNX_ERR_CUDA, "prompt attention: smem attribute");
+    CUtensorMap tq, tk, tv;
+    if (!make_tmap_heads(&tq, q, rows, a.H, HD, a.group, tile_tokens(a.group)) ||
+        !make_tmap_heads(&tk, k, keys, a.Hkv, HD, 1, pattn::BN) ||
+        !make_tmap_heads(&tv, v, keys, a.Hkv, HD, 1, C::VKEYS))
+        return fail(JNX_ERR_CUDA, "prompt attention: tensor map encode failed");
+    const int grid = std::min(a.n_work, num_sms());
+    pdl(k_prompt_attn<HD>, grid, C::THREADS, C::SMEM, s)(tq, tk, tv, a);
+    return launched("prompt attention");
 }
 
 jnx_status heads_ok(int H, int Hkv, int hd, const char* what) {
@@ -155,19 +662,20 @@ extern "C" jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_hea
     if (rows == 0) return JNX_OK;
     if (!rows_ok(q) || !rows_ok(out) || (keys > 0 && (!rows_ok(k) || !rows_ok(v))))
         return fail(JNX_ERR_INVALID_ARG, "prompt attention: null or misaligned rows");
-    const jnx_head_rows none{nullptr, 0, 0};
-    PromptArgs a{p->cu_q, p->cu_kv, p->prefix, reinterpret_cast<const int2*>(p->items),
+    const long long n_work = (long long)p->n_forward * n_kv_heads;
+    if (n_work > 0x7FFFFFFFLL - 2 * num_sms())
+        return fail(JNX_ERR_UNSUPPORTED, "prompt attention: too many work items");
+    if (n_work == 0) return JNX_OK;
+    // without any key no tile is loaded, but the maps want an address
+    const jnx_head_rows kk = keys ? *k : *q, vv = keys ? *v : *q;
+    if (!keys) keys = 1;
+    PromptArgs a{p->cu_q, p->cu_kv, p->prefix, reinterpret_cast<const int2*>(p->items), (int)n_work,
                  n_heads, n_kv_heads, n_heads / n_kv_heads,
-                 (float)(1.4426950408889634 / sqrt((double)head_dim)), *q, keys ? *k : none,
-                 keys ? *v : none, *out, lse};
+                 (float)(1.4426950408889634 / sqrt((double)head_dim)), out->ptr, out->row_stride,
+                 out->head_stride, lse, status};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN, 0.0, s);
-    const int grid = p->n_forward * n_kv_heads;
-    if (head_dim == 64)
-        pdl(k_prompt_attn<64>, grid, 256, 0, s)(a);
-    else if (head_dim == 128)
-        pdl(k_prompt_attn<128>, grid, 256, 0, s)(a);
-    else
-        pdl(k_prompt_attn<256>, grid, 256, 0, s)(a);
-    return launched("prompt attention");
+    if (head_dim == 64) return launch_prompt<64>(a, *q, kk, vv, rows, keys, s);
+    if (head_dim == 128) return launch_prompt<128>(a, *q, kk, vv, rows, keys, s);
+    return launch_prompt<256>(a, *q, kk, vv, rows, keys, s);
 }
