@@ -1713,6 +1713,20 @@ bool make_tmap_heads(CUtensorMap* m, const jnx_head_rows& r, int n_rows, int hea
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tmap_cache(CUtensorMap* m, const uint16_t* ptr, const jnx_kv_cache& c, int heads, int hd,
+                     int box) {
+    PFN_tmapEncodeTiled fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)hd, (cuuint64_t)heads, (cuuint64_t)c.room, (cuuint64_t)c.n_slots};
+    cuuint64_t strides[3] = {(cuuint64_t)c.head_stride * 2, (cuuint64_t)c.row_stride * 2,
+                             (cuuint64_t)c.slot_stride * 2};
+    cuuint32_t boxes[4] = {64, 1, (cuuint32_t)box, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<uint16_t*>(ptr), dims, strides, boxes,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int num_sms() {
     int dev = 0, n = 0;
     cudaGetDevice(&dev);

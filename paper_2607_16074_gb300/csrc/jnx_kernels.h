@@ -201,6 +201,10 @@ bool make_tmap_bf16(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t col
 // boxes of 64 columns x box_heads x box_rows, 128-byte swizzled.
 bool make_tmap_heads(CUtensorMap* m, const jnx_head_rows& r, int n_rows, int heads, int hd,
                      int box_heads, int box_rows);
+// A cache's keys (or values) [slots][room][heads][hd]: boxes of 64 columns of `box` tokens
+// of one head.
+bool make_tmap_cache(CUtensorMap* m, const uint16_t* ptr, const jnx_kv_cache& c, int heads, int hd,
+                     int box);
 int num_sms();
 
 // Raise fn's dynamic shared-memory limit to `bytes` on the current device,
