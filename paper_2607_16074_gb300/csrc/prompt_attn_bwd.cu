@@ -3,6 +3,31 @@
 // With P = 2^(s c - lse) recomputed from the forward's log2-sum-exp, c = log2(e) /
 // sqrt(hd), and D = rowsum(dO * O):  dV = P^T dO,  dS = P (dO V^T - D) / sqrt(hd),
 // dQ = dS K,  dK = dS^T Q; a key head's gradients add over its group's query heads.
+//
+// Two passes of one launch, each summing in TMEM and writing its rows once, so no sum's
+// order depends on anything but the sequence:
+//   keys     a 128-key tile of a key head against the 128-row tiles (tokens x the
+//            group's heads, as the forward's) that see it:
+//            S^T = K Q^T, dP^T = V dO^T, dV += P^T dO, dK += dS^T Q
+//   queries  a row tile against the 128-key tiles it sees:
+//            S = Q K^T, dP = dO V^T, dQ += dS K
+// Seven products for the gradients' five; keeping dS for a second pass would move two
+// bytes a score and head twice, which costs more than the two products do.
+//
+// TMEM at head dim 128 holds S, dP and two accumulators of 128 columns each, so neither
+// is double-buffered; instead the products and the elementwise warps take the halves of a
+// tile in turn: P^T (over S) feeds dV, and S of the next tile follows dV while dS is
+// formed; dS (over dP) feeds dK, and the next dP follows dK while P is formed.
+//
+// Warps (one CTA an SM, items claimed from one queue, the longest of each pass first):
+//   0     claims items and hands them out; TMA: the item's outer tiles (K and V, or Q
+//         and dO), inner tiles through two rings of two or three
+//   1     MMA issuer
+//   2     the rows' lse, D and key limits of each inner row tile (keys pass)
+//   4-11  elementwise: warps 4-7 a tile's first 64 columns, 8-11 the others; then the
+//         accumulators out
+// Inner rows past a sequence's end belong to others and may be NaN: they are zeroed in
+// shared memory, and their lse is +inf, which makes their probabilities zero.
 #include <algorithm>
 
 #include "jnx_dev.cuh"
@@ -14,7 +39,626 @@ namespace jnx {
 
 jnx_status prompt_launchable(const jnx_prompt* p, const char* what, int& rows, int& keys);
 
+namespace pbwd {
+constexpr int BM = 128;
+enum { KEYS = 0, QUERIES = 1 };
+// barriers of a pass
+enum { O_FULL = 0, O_EMPTY = 1, B1_FULL = 2, B1_EMPTY = 5, B2_FULL = 8, B2_EMPTY = 11, S_FULL = 14,
+       DP_FULL = 15, P_FULL = 16, DS_FULL = 17, ACC_FULL = 18, ACC_FREE = 19, DRAIN = 20,
+       ST_FULL = 21, ST_EMPTY = 23, W_FULL = 25, W_EMPTY = 27, N_BARS = 29 };
+constexpr int THREADS = 384, EW = 8;
+constexpr int READERS = 2 + EW;  // warps that an item is handed to: MMA, row values, elementwise
+}  // namespace pbwd
+
+template <int HD>
+struct PromptBwdCfg {
+    static_assert(HD == 64 || HD == 128, "head dim");
+    static constexpr int TILE = pbwd::BM * HD * 2;
+    static constexpr int SLOTS = HD == 64 ? 3 : 2;  // of each ring
+    static constexpr int OFF_B1 = 2 * TILE, OFF_B2 = OFF_B1 + SLOTS * TILE;
+    static constexpr int OFF_ST = OFF_B2 + SLOTS * TILE;  // [2][lse, D, limit][128]
+    static constexpr int OFF_BAR = OFF_ST + 2 * 3 * pbwd::BM * 4;
+    static constexpr int SMEM = OFF_BAR + 2 * pbwd::N_BARS * 8 + 80 + 1024;
+    static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
+    static constexpr uint32_t S_COL = 0, DP_COL = 128, ACC_COL = 256;
+};
+
 struct PromptBwdArgs {
+    const int *cu_q, *cu_kv, *prefix;
+    const int2* items;  // of the keys pass, then of the queries pass
+    int n_keys, n_queries, H, Hkv, group;
+    int* claimed;       // items taken beyond the grid's first: 0 at launch
+    float scale_log2, scale;
+    const float2* row;  // [rows][H]: lse (+inf where a row sees no key), D
+    jnx_head_rows dq, dk, dv;
+    int* status;
+};
+
+// What the warps of a CTA are told of an item.
+struct PromptBwdItem {
+    int at, kvh, q0, Lq, k0, Lk, pre;  // at: first key or row; Lq < 0: no more in this pass
+};
+
+// The rows' (lse, D), and the claim counter to zero.  A warp a (row, head).
+__global__ void __launch_bounds__(256)
+    k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, const float* lse, int rows, int H,
+                      int hd, float2* row, int* claimed) {
+    pdl_entry();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *claimed = 0;
+    // hd / 8 lanes a row, 16 bytes each
+    const int lanes = hd / 8, per = 256 / lanes;
+    const long long w = (long long)blockIdx.x * per + threadIdx.x / lanes;
+    const int c = threadIdx.x % lanes * 8;
+    float d = 0.f;
+    if (w < (long long)rows * H) {
+        const long long r = w / H;
+        const int h = (int)(w % H);
+        const uint4 a = *reinterpret_cast<const uint4*>(out.ptr + r * out.row_stride +
+                                                        h * out.head_stride + c);
+        const uint4 b = *reinterpret_cast<const uint4*>(dout.ptr + r * dout.row_stride +
+                                                        h * dout.head_stride + c);
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            d += __uint_as_float(x[e] << 16) * __uint_as_float(y[e] << 16) +
+                 __uint_as_float(x[e] & 0xffff0000u) * __uint_as_float(y[e] & 0xffff0000u);
+    }
+    for (int o = lanes / 2; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    if (w < (long long)rows * H && c == 0) {
+        const float l = lse[w];
+        row[w] = l == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(l, d);
+    }
+}
+
+template <int HD, int PASS>
+__device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUtensorMap& tk,
+                                               const CUtensorMap& tv, const CUtensorMap& tdo,
+                                               const PromptBwdArgs& p, uint8_t* sm, uint64_t* bar,
+                                               volatile int* fail_flag, uint32_t tbase, int q_first,
+                                               int claim) {
+    using C = PromptBwdCfg<HD>;
+    using namespace pbwd;
+    constexpr bool KP = PASS == KEYS;
+    constexpr int NCH = HD / 64, SLOTS = C::SLOTS;
+    const int T = tile_tokens(p.group), row_bytes = p.group * T * HD * 2;
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    uint8_t* b1 = sm + C::OFF_B1;
+    uint8_t* b2 = sm + C::OFF_B2;
+    float* st = reinterpret_cast<float*>(sm + C::OFF_ST);
+    volatile int* slot = fail_flag + 1;  // [2][8]: items handed out
+    const int2* items = p.items + (KP ? 0 : p.n_keys);
+    const int n_work = (KP ? p.n_keys : p.n_queries) * p.Hkv;
+
+    int seen = 0;
+    auto next_item = [&](bool& ok) -> PromptBwdItem {
+        const int b = seen & 1;
+        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0};
+        if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen >> 1) & 1))) return x;
+        x.at = warp_uniform(slot[8 * b]);
+        x.kvh = warp_uniform(slot[8 * b + 1]);
+        x.q0 = warp_uniform(slot[8 * b + 2]);
+        x.Lq = warp_uniform(slot[8 * b + 3]);
+        x.k0 = warp_uniform(slot[8 * b + 4]);
+        x.Lk = warp_uniform(slot[8 * b + 5]);
+        x.pre = warp_uniform(slot[8 * b + 6]);
+        if (elect_one()) mbar_arrive(&bar[W_EMPTY + b]);
+        __syncwarp();
+        ++seen;
+        return x;
+    };
+    // keys pass: the first row that an item's tile j holds
+    auto first_tok = [&](const PromptBwdItem& x) { return first_row(x.at, x.Lq, x.Lk, x.pre); };
+    auto n_inner = [&](const PromptBwdItem& x) {
+        if (KP) return (x.Lq - first_tok(x) + T - 1) / T;
+        return (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BM - 1) / BM;
+    };
+
+    if (warp == 0) {
+        // ---------------- claims and TMA ----------------
+        bool ok = true;
+        int told = 0;
+        auto tell = [&](const PromptBwdItem& x) {
+            const int b = told & 1;
+            if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told >> 1) & 1) ^ 1)) return false;
+            if (elect_one()) {
+                slot[8 * b] = x.at;
+                slot[8 * b + 1] = x.kvh;
+                slot[8 * b + 2] = x.q0;
+                slot[8 * b + 3] = x.Lq;
+                slot[8 * b + 4] = x.k0;
+                slot[8 * b + 5] = x.Lk;
+                slot[8 * b + 6] = x.pre;
+                mbar_arrive(&bar[W_FULL + b]);
+            }
+            __syncwarp();
+            ++told;
+            return true;
+        };
+        int no = 0;       // outer pairs loaded
+        uint32_t g = 0;   // inner pairs loaded
+        auto load = [&](const CUtensorMap* m, uint8_t* dst, int head, int row, uint64_t* full) {
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) tma_load_3d(dst + c * BM * 128, m, c * 64, head, row, full);
+        };
+        // the item claimed: its list entry, then its sequence's rows
+        int2 e = make_int2(0, 0);
+        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0};
+        auto fetch = [&]() {
+            claim = __shfl_sync(0xffffffffu, claim, 0);
+            if (claim - q_first >= n_work) return;
+            e = items[(claim - q_first) / p.Hkv];
+            nx.at = e.y;
+            nx.kvh = (claim - q_first) % p.Hkv;
+            nx.q0 = p.cu_q[e.x];
+            nx.Lq = p.cu_q[e.x + 1] - nx.q0;
+            nx.k0 = p.cu_kv[e.x];
+            nx.Lk = p.cu_kv[e.x + 1] - nx.k0;
+            nx.pre = p.prefix ? p.prefix[e.x] : 0;
+        };
+        fetch();
+        while (claim - q_first < n_work) {
+            if (__any_sync(0xffffffffu, *fail_flag)) {
+                ok = false;
+                break;
+            }
+            PromptBwdItem x;
+            x.at = warp_uniform(nx.at);
+            x.kvh = warp_uniform(nx.kvh);
+            x.q0 = warp_uniform(nx.q0);
+            x.Lq = warp_uniform(nx.Lq);
+            x.k0 = warp_uniform(nx.k0);
+            x.Lk = warp_uniform(nx.Lk);
+            x.pre = warp_uniform(nx.pre);
+            if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
+            __syncwarp();
+            if (!(ok = tell(x))) break;
+            const int n = n_inner(x), i0 = KP ? first_tok(x) : x.at;
+            if (n > 0) {
+                if (no > 0 && !(ok = mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[O_FULL], KP ? 2 * C::TILE : 2 * row_bytes);
+                    if (KP) {
+                        load(&tk, sm, x.kvh, x.k0 + x.at, &bar[O_FULL]);
+                        load(&tv, sm + C::TILE, x.kvh, x.k0 + x.at, &bar[O_FULL]);
+                    } else {
+                        load(&tq, sm, x.kvh * p.group, x.q0 + x.at, &bar[O_FULL]);
+                        load(&tdo, sm + C::TILE, x.kvh * p.group, x.q0 + x.at, &bar[O_FULL]);
+                    }
+                }
+                __syncwarp();
+                ++no;
+            }
+            for (int j = 0; j < n && ok; ++j, ++g) {
+                const int s = g % SLOTS;
+                const uint32_t ph = ((g / SLOTS) & 1) ^ 1;
+                if (!(ok = mbar_wait_warp(&bar[B1_EMPTY + s], ph))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[B1_FULL + s], KP ? row_bytes : C::TILE);
+                    if (KP) load(&tq, b1 + s * C::TILE, x.kvh * p.group, x.q0 + i0 + j * T, &bar[B1_FULL + s]);
+                    else load(&tk, b1 + s * C::TILE, x.kvh, x.k0 + j * BM, &bar[B1_FULL + s]);
+                }
+                __syncwarp();
+                if (!(ok = mbar_wait_warp(&bar[B2_EMPTY + s], ph))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[B2_FULL + s], KP ? row_bytes : C::TILE);
+                    if (KP) load(&tdo, b2 + s * C::TILE, x.kvh * p.group, x.q0 + i0 + j * T, &bar[B2_FULL + s]);
+                    else load(&tv, b2 + s * C::TILE, x.kvh, x.k0 + j * BM, &bar[B2_FULL + s]);
+                }
+                __syncwarp();
+            }
+            if (!ok) break;
+            fetch();
+        }
+        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0});
+        if (!ok) *fail_flag = 1;
+        // every copy has landed before the pass ends (at once in a normal run)
+        if (no > 0) mbar_wait_warp(&bar[O_FULL], (no - 1) & 1, 100000000LL);
+        for (uint32_t i = g > SLOTS ? g - SLOTS : 0; i < g; ++i) {
+            mbar_wait_warp(&bar[B1_FULL + i % SLOTS], (i / SLOTS) & 1, 100000000LL);
+            mbar_wait_warp(&bar[B2_FULL + i % SLOTS], (i / SLOTS) & 1, 100000000LL);
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BM);
+        constexpr uint32_t IDESC_ACC = idesc_bf16_f32(BM, HD) | (1u << 16);  // B MN-major
+        bool ok = true, issued = false;
+        int no = 0, done = 0;  // outer pairs taken, items finished
+        uint32_t g1 = 0, g2 = 0, gp = 0;  // inner tiles taken by S and by dP; P / dS tiles taken
+        auto commit = [&](uint64_t* b) {
+            if (elect_one()) tc_commit(b);
+            __syncwarp();
+        };
+        auto score = [&](uint32_t d, uint32_t outer, uint8_t* inner) {
+            const uint32_t a_lo = sw128_desc_lo(outer), b_lo = sw128_desc_lo(smem_u32(inner));
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < HD / 16; ++ks) {
+                    const uint32_t off = (ks >> 2) * BM * 8 + (ks & 3) * 2;
+                    tc_mma_f16(d, desc_of(a_lo + off, kSw128DescHi), desc_of(b_lo + off, kSw128DescHi),
+                               IDESC_S, ks > 0);
+                }
+            }
+            __syncwarp();
+            issued = true;
+        };
+        // acc += X B, X bf16 in TMEM: 64 inner rows at column x, 64 at x + 64
+        auto gather = [&](uint32_t acc, uint32_t x, uint8_t* inner, bool accumulate) {
+            const uint32_t b = smem_u32(inner);
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < BM / 16; ++ks)
+                    tc_mma_f16_ts(acc, x + (ks >> 2) * 64 + (ks & 3) * 8,
+                                  sw128_desc_mn(b + ks * 16 * 128, BM * 128, 1024), IDESC_ACC,
+                                  accumulate || ks > 0);
+            }
+            __syncwarp();
+        };
+        auto zero_tail = [&](uint8_t* tile, int valid, int end) {
+            for (int i = lane; i < (end - valid) * (HD / 8); i += 32) {
+                const int r = valid + i / (HD / 8), u = i % (HD / 8);
+                *reinterpret_cast<uint4*>(tile + (u >> 3) * BM * 128 + r * 128 + (u & 7) * 16) =
+                    make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async();
+            __syncwarp();
+        };
+        while (ok) {
+            const PromptBwdItem x = next_item(ok);
+            if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            if (n == 0) continue;
+            if (!(ok = mbar_wait_warp(&bar[O_FULL], no & 1))) break;
+            ++no;
+            tc_fence_after();
+            const uint32_t o1 = smem_u32(sm), o2 = o1 + C::TILE;
+            // inner rows of tile j that are the sequence's, of those a box loads
+            const int box = KP ? p.group * T : BM;
+            auto valid = [&](int j) {
+                return KP ? min(T, x.Lq - i0 - j * T) * p.group : min(BM, x.Lk - j * BM);
+            };
+            auto next_s = [&](int j) -> bool {
+                const int s = g1 % SLOTS;
+                if (!mbar_wait_warp(&bar[B1_FULL + s], (g1 / SLOTS) & 1)) return false;
+                if (valid(j) < box) zero_tail(b1 + s * C::TILE, valid(j), box);
+                tc_fence_after();
+                score(tbase + C::S_COL, o1, b1 + s * C::TILE);
+                commit(&bar[S_FULL]);
+                ++g1;
+                return true;
+            };
+            auto next_dp = [&](int j) -> bool {
+                const int s = g2 % SLOTS;
+                if (!mbar_wait_warp(&bar[B2_FULL + s], (g2 / SLOTS) & 1)) return false;
+                if (KP && valid(j) < box) zero_tail(b2 + s * C::TILE, valid(j), box);
+                tc_fence_after();
+                score(tbase + C::DP_COL, o2, b2 + s * C::TILE);
+                commit(&bar[DP_FULL]);
+                if (!KP) commit(&bar[B2_EMPTY + s]);  // V is done with
+                ++g2;
+                return true;
+            };
+            ok = next_s(0) && next_dp(0);
+            if (ok && n == 1) commit(&bar[O_EMPTY]);
+            for (int j = 0; j < n && ok; ++j, ++gp) {
+                const int s = gp % SLOTS;
+                // P^T over S (keys pass), or S read (queries pass)
+                if (!(ok = mbar_wait_warp(&bar[P_FULL], gp & 1))) break;
+                // the item's first sums overwrite the accumulators: the last epilogue has read them
+                if (j == 0 && done > 0 && !(ok = mbar_wait_warp(&bar[ACC_FREE], (done - 1) & 1))) break;
+                tc_fence_after();
+                if (KP) {
+                    gather(tbase + C::ACC_COL + HD, tbase + C::S_COL, b2 + s * C::TILE, j > 0);
+                    commit(&bar[B2_EMPTY + s]);
+                }
+                if (j + 1 < n && !(ok = next_s(j + 1))) break;
+                if (!(ok = mbar_wait_warp(&bar[DS_FULL], gp & 1))) break;
+                tc_fence_after();
+                gather(tbase + C::ACC_COL, tbase + C::DP_COL, b1 + s * C::TILE, j > 0);
+                commit(&bar[B1_EMPTY + s]);
+                if (j + 1 < n) {
+                    if (!(ok = next_dp(j + 1))) break;
+                    if (j + 2 == n) commit(&bar[O_EMPTY]);
+                }
+            }
+            if (!ok) break;
+            commit(&bar[ACC_FULL]);
+            ++done;
+        }
+        if (!ok) *fail_flag = 1;
+        if (issued) {
+            commit(&bar[DRAIN]);
+            mbar_wait_warp(&bar[DRAIN], 0, 100000000LL);
+        }
+    } else if (warp == 2) {
+        // ---------------- values of the inner rows (keys pass) ----------------
+        bool ok = true;
+        uint32_t g = 0;
+        while (ok) {
+            const PromptBwdItem x = next_item(ok);
+            if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            if (!KP) continue;
+            const int n = n_inner(x), i0 = first_tok(x);
+            for (int j = 0; j < n; ++j, ++g) {
+                const int b = g & 1;
+                float2 v[4];
+                int lim[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = e * 32 + lane, t = r / p.group, i = i0 + j * T + t;
+                    const bool live = t < T && i < x.Lq;
+                    v[e] = live ? p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + r % p.group]
+                                : make_float2(INFINITY, 0.f);
+                    lim[e] = live ? keys_seen(i, x.Lq, x.Lk, x.pre) : 0;
+                }
+                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g >> 1) & 1) ^ 1))) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = e * 32 + lane;
+                    st[b * 384 + r] = v[e].x;
+                    st[b * 384 + 128 + r] = v[e].y;
+                    st[b * 384 + 256 + r] = __int_as_float(lim[e]);
+                }
+                mbar_arrive(&bar[ST_FULL + b]);
+            }
+        }
+        if (!ok) *fail_flag = 1;
+    } else if (warp >= 4) {
+        // ---------------- elementwise + epilogue ----------------
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tS = tbase + lane_base + C::S_COL + half * 64;
+        const uint32_t tP = tbase + lane_base + C::DP_COL + half * 64;
+        const int r = quarter * 32 + lane;
+        uint32_t g = 0;
+        int done = 0;
+        bool ok = true;
+        while (ok) {
+            const PromptBwdItem x = next_item(ok);
+            if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            // the outer row of this thread: a key, or a (token, head)
+            const int tok = r / p.group, hg = r % p.group;
+            const int key = x.at + r, i = x.at + tok;
+            const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
+            float lse = INFINITY, D = 0.f;
+            int lim = 0x7fffffff;
+            if (!KP && live) {
+                const float2 v = p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + hg];
+                lse = v.x;
+                D = v.y;
+                lim = keys_seen(i, x.Lq, x.Lk, x.pre);
+            }
+            for (int j = 0; j < n; ++j, ++g) {
+                const float* sv = st + (g & 1) * 384 + half * 64;
+                bool whole;  // every score of the tile counts
+                if (KP) {
+                    whole = keys_seen(min(i0 + j * T, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
+                            min(x.at + BM, x.Lk);
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + (g & 1)], (g >> 1) & 1))))
+                        break;
+                } else {
+                    whole = __all_sync(0xffffffffu, lim >= (j + 1) * BM);
+                }
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[S_FULL], g & 1)))) break;
+                tc_fence_after();
+                float pr[64];
+                {
+                    uint32_t s[2][32];
+                    tmem_ld32(tS, s[0]);
+                    tmem_ld32(tS + 32, s[1]);
+                    tmem_ld_wait_regs(s[0]);
+                    tmem_ld_wait_regs(s[1]);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            float4 l4 = make_float4(lse, lse, lse, lse);
+                            if (KP) l4 = *reinterpret_cast<const float4*>(sv + c * 32 + e);
+                            const float* lp = &l4.x;
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                pr[c * 32 + e + u] =
+                                    ex2_approx(fmaf(__uint_as_float(s[c][e + u]), p.scale_log2, -lp[u]));
+                        }
+                }
+                if (!whole) {
+                    if (KP) {
+                        const int* lm = reinterpret_cast<const int*>(sv + 256);
+#pragma unroll
+                        for (int e = 0; e < 64; ++e)
+                            if (key >= lm[e]) pr[e] = 0.f;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 64; ++e)
+                            if (j * BM + half * 64 + e >= lim) pr[e] = 0.f;
+                    }
+                }
+                if (KP) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) pk[e] = pack_bf2(pr[2 * e], pr[2 * e + 1]);
+                    tmem_st32(tS, pk);
+                    tmem_st_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (elect_one()) mbar_arrive(&bar[P_FULL]);
+                __syncwarp();
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[DP_FULL], g & 1)))) break;
+                tc_fence_after();
+                uint32_t dk[32];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t d[32];
+                    tmem_ld32(tP + c * 32, d);
+                    tmem_ld_wait_regs(d);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        float4 d4 = make_float4(D, D, D, D);
+                        if (KP) d4 = *reinterpret_cast<const float4*>(sv + 128 + c * 32 + e);
+                        const float* dp = &d4.x;
+                        float v[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            v[u] = pr[c * 32 + e + u] * (__uint_as_float(d[e + u]) - dp[u]);
+                            // V beyond the sequence's keys may be NaN
+                            if (!KP && !whole && pr[c * 32 + e + u] == 0.f) v[u] = 0.f;
+                        }
+                        dk[c * 16 + e / 2] = pack_bf2(v[0], v[1]);
+                        dk[c * 16 + e / 2 + 1] = pack_bf2(v[2], v[3]);
+                    }
+                }
+                tmem_st32(tP, dk);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (elect_one()) {
+                    mbar_arrive(&bar[DS_FULL]);
+                    if (KP) mbar_arrive(&bar[ST_EMPTY + (g & 1)]);
+                }
+                __syncwarp();
+            }
+            if (!ok) break;
+            // ---- the accumulators out: this warp's half of the columns ----
+            if (n > 0) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ACC_FULL], done & 1)))) break;
+                tc_fence_after();
+                ++done;
+            }
+#pragma unroll
+            for (int acc = 0; acc < (KP ? 2 : 1); ++acc) {
+                const float f = acc ? 1.f : p.scale;
+                uint16_t* o;
+                if (KP) {
+                    const jnx_head_rows& to = acc ? p.dv : p.dk;
+                    o = to.ptr + (long long)(x.k0 + key) * to.row_stride + x.kvh * to.head_stride;
+                } else {
+                    o = p.dq.ptr + (long long)(x.q0 + i) * p.dq.row_stride +
+                        (x.kvh * p.group + hg) * p.dq.head_stride;
+                }
+                o += half * (HD / 2);
+#pragma unroll
+                for (int c = 0; c < HD / 64; ++c) {
+                    uint32_t v[32];
+                    if (n > 0) {
+                        tmem_ld32(tbase + lane_base + C::ACC_COL + acc * HD + half * (HD / 2) + c * 32, v);
+                        tmem_ld_wait_regs(v);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0;
+                    }
+                    if (live) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            *reinterpret_cast<uint4*>(o + c * 32 + e * 8) = make_uint4(
+                                pack_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
+                                pack_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
+                                pack_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
+                                pack_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
+                    }
+                }
+            }
+            if (n > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (elect_one()) mbar_arrive(&bar[ACC_FREE]);
+                __syncwarp();
+            }
+        }
+        if (!ok) *fail_flag = 1;
+    }
+    return claim;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(pbwd::THREADS, 1)
+    k_prompt_attn_bwd(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+                      const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap tdo,
+                      const __grid_constant__ PromptBwdArgs p) {
+    using C = PromptBwdCfg<HD>;
+    using namespace pbwd;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* bar = reinterpret_cast<uint64_t*>(sm + C::OFF_BAR);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 2 * N_BARS);
+    volatile int* fail_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = warp_uniform(threadIdx.x >> 5);
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < 2 * N_BARS; ++k) {
+            const int i = k % N_BARS;
+            mbar_init(&bar[k], i == P_FULL || i == DS_FULL || i == ACC_FREE ? EW
+                               : i >= ST_EMPTY && i < W_FULL                ? EW
+                               : i >= ST_FULL && i < ST_EMPTY               ? 32
+                               : i >= W_EMPTY                               ? READERS
+                                                                            : 1);
+        }
+        *fail_flag = 0;
+        fence_barrier_init();
+    }
+    // rows that no box reaches (128 no multiple of the group) are zero for good
+    const int box = p.group * tile_tokens(p.group);
+    for (int i = threadIdx.x; i < 2 * C::SLOTS * (HD / 64) * (BM - box) * 8; i += THREADS) {
+        const int u = i & 7, r = box + (i >> 3) % (BM - box), t = (i >> 3) / (BM - box);
+        *reinterpret_cast<uint4*>(sm + C::OFF_B1 + t * BM * 128 + r * 128 + u * 16) =
+            make_uint4(0, 0, 0, 0);
+    }
+    fence_proxy_async();
+    pdl_entry();  // TMEM is taken once the grid ahead has given its own back
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    if (threadIdx.x == 0) {
+        tma_prefetch_desc(&tq);
+        tma_prefetch_desc(&tk);
+        tma_prefetch_desc(&tv);
+        tma_prefetch_desc(&tdo);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = warp_uniform(*tmem_slot);
+    // a pass leaves no copy, MMA or TMEM read of its own behind; its barriers are its own
+    int claim = prompt_bwd_pass<HD, KEYS>(tq, tk, tv, tdo, p, sm, bar, fail_flag, tbase, 0, blockIdx.x);
+    __syncwarp();
+    tc_fence_before();
+    bool failed = __syncthreads_or(*fail_flag);
+    tc_fence_after();
+    if (!failed) {
+        prompt_bwd_pass<HD, QUERIES>(tq, tk, tv, tdo, p, sm, bar + N_BARS, fail_flag, tbase,
+                                     p.n_keys * p.Hkv, claim);
+        __syncwarp();
+        tc_fence_before();
+        failed = __syncthreads_or(*fail_flag);
+        tc_fence_after();
+    }
+    if (failed && threadIdx.x == 0) report(p.status, JNX_ERR_TIMEOUT);
+    if (warp == 1) tmem_dealloc(tbase, 512);
+}
+
+template <int HD>
+static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows& q,
+                                    const jnx_head_rows& k, const jnx_head_rows& v,
+                                    const jnx_head_rows& dout, int rows, int keys, cudaStream_t s) {
+    using C = PromptBwdCfg<HD>;
+    const char* what = "prompt attention backward";
+    static std::atomic<uint64_t> attr{0};
+    if (set_smem_limit(reinterpret_cast<const void*>(k_prompt_attn_bwd<HD>), C::SMEM, attr) != cudaSuccess)
+        return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
+    CUtensorMap tq, tk, tv, tdo;
+    const int T = tile_tokens(a.group);
+    if (!make_tmap_heads(&tq, q, rows, a.H, HD, a.group, T) ||
+        !make_tmap_heads(&tdo, dout, rows, a.H, HD, a.group, T) ||
+        !make_tmap_heads(&tk, k, keys, a.Hkv, HD, 1, pbwd::BM) ||
+        !make_tmap_heads(&tv, v, keys, a.Hkv, HD, 1, pbwd::BM))
+        return fail(JNX_ERR_CUDA, "%s: tensor map encode failed", what);
+    const int grid = (int)std::min<long long>((long long)(a.n_keys + a.n_queries) * a.Hkv, num_sms());
+    pdl(k_prompt_attn_bwd<HD>, grid, pbwd::THREADS, C::SMEM, s)(tq, tk, tv, tdo, a);
+    return launched(what);
+}
+
+struct PromptSimpleArgs {
     const int *cu_q, *cu_kv, *prefix;
     const int2* items;
     int H, Hkv, group;
@@ -41,7 +685,7 @@ __device__ __forceinline__ float row_dot(const float (&x)[E], const float (&y)[E
 
 // Query rows, one warp each: D and dQ.
 template <int HD>
-__global__ void __launch_bounds__(256) k_prompt_attn_dq(const __grid_constant__ PromptBwdArgs a) {
+__global__ void __launch_bounds__(256) k_prompt_attn_dq(const __grid_constant__ PromptSimpleArgs a) {
     constexpr int E = HD / 32;
     pdl_entry();
     const int2 it = a.items[blockIdx.x / a.Hkv];
@@ -73,7 +717,7 @@ __global__ void __launch_bounds__(256) k_prompt_attn_dq(const __grid_constant__ 
 
 // Keys, one warp each.
 template <int HD>
-__global__ void __launch_bounds__(256) k_prompt_attn_dkv(const __grid_constant__ PromptBwdArgs a) {
+__global__ void __launch_bounds__(256) k_prompt_attn_dkv(const __grid_constant__ PromptSimpleArgs a) {
     constexpr int E = HD / 32;
     pdl_entry();
     const int2 it = a.items[blockIdx.x / a.Hkv];
@@ -110,7 +754,7 @@ using namespace jnx;
 
 extern "C" size_t jnx_op_prompt_attention_backward_workspace_bytes(int32_t n_q, int32_t n_heads) {
     if (n_q < 0 || n_heads <= 0) return 0;
-    return (size_t)n_q * n_heads * sizeof(float);
+    return 256 + (size_t)n_q * n_heads * sizeof(float2);  // the claims; each row's lse and D
 }
 
 extern "C" jnx_status jnx_op_prompt_attention_backward(
@@ -128,30 +772,42 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     if ((rows > 0 && (!rows_ok(q) || !rows_ok(out) || !rows_ok(dout) || !rows_ok(dq) || !lse)) ||
         (keys > 0 && (!rows_ok(k) || !rows_ok(v) || !rows_ok(dk) || !rows_ok(dv))))
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned rows", what);
-    if (rows > 0 && (!workspace || ws_bytes < jnx_op_prompt_attention_backward_workspace_bytes(
-                                                  rows, n_heads)))
-        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small", what);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7) ||
+        ws_bytes < jnx_op_prompt_attention_backward_workspace_bytes(rows, n_heads))
+        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
+    const long long n_work = ((long long)p->n_keys + p->n_queries) * n_kv_heads;
+    // (claims run past the last item by one for each CTA and pass)
+    if (n_work > 0x7FFFFFFFLL - 4 * num_sms() || (long long)rows * n_heads > 0x7FFFFFF00LL)
+        return fail(JNX_ERR_UNSUPPORTED, "%s: too many work items", what);
+    if (n_work == 0) return JNX_OK;
     const jnx_head_rows none{nullptr, 0, 0};
     auto or_none = [&](const jnx_head_rows* r, int n) { return n ? *r : none; };
+    int* claimed = static_cast<int*>(workspace);
+    float2* row = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + 256);
     PromptBwdArgs a{p->cu_q, p->cu_kv, p->prefix,
-                    reinterpret_cast<const int2*>(p->items) + p->n_forward + p->n_keys, n_heads,
-                    n_kv_heads, n_heads / n_kv_heads,
+                    reinterpret_cast<const int2*>(p->items) + p->n_forward, p->n_keys, p->n_queries,
+                    n_heads, n_kv_heads, n_heads / n_kv_heads, claimed,
                     (float)(1.4426950408889634 / sqrt((double)head_dim)),
-                    (float)(1.0 / sqrt((double)head_dim)), or_none(q, rows), or_none(k, keys),
-                    or_none(v, keys), or_none(out, rows), or_none(dout, rows), or_none(dq, rows),
-                    or_none(dk, keys), or_none(dv, keys), lse, static_cast<float*>(workspace)};
+                    (float)(1.0 / sqrt((double)head_dim)), row, or_none(dq, rows),
+                    or_none(dk, keys), or_none(dv, keys), status};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN_BWD, 0.0, s);
-    auto go = [&](auto dq_kernel, auto dkv_kernel) {
-        if (p->n_queries) pdl(dq_kernel, p->n_queries * n_kv_heads, 256, 0, s)(a);
-        a.items -= p->n_keys;
-        if (p->n_keys) pdl(dkv_kernel, p->n_keys * n_kv_heads, 256, 0, s)(a);
-    };
-    if (head_dim == 64)
-        go(k_prompt_attn_dq<64>, k_prompt_attn_dkv<64>);
-    else if (head_dim == 128)
-        go(k_prompt_attn_dq<128>, k_prompt_attn_dkv<128>);
-    else
-        go(k_prompt_attn_dq<256>, k_prompt_attn_dkv<256>);
+    const int per = 256 / (head_dim / 8);
+    pdl(k_prompt_bwd_rows, std::max(1, (int)(((long long)rows * n_heads + per - 1) / per)), 256, 0,
+        s)(or_none(out, rows), or_none(dout, rows), lse, rows, n_heads, head_dim, row, claimed);
+    // where there are no rows or keys nothing is loaded, but the maps want an address
+    const jnx_head_rows& any = rows ? *q : *k;
+    const jnx_head_rows qq = rows ? *q : any, dd = rows ? *dout : any, kk = keys ? *k : any,
+                        vv = keys ? *v : any;
+    const int nr = std::max(rows, 1), nk = std::max(keys, 1);
+    if (head_dim == 64) return launch_prompt_bwd<64>(a, qq, kk, vv, dd, nr, nk, s);
+    if (head_dim == 128) return launch_prompt_bwd<128>(a, qq, kk, vv, dd, nr, nk, s);
+    PromptSimpleArgs b{p->cu_q, p->cu_kv, p->prefix, a.items + p->n_keys, n_heads, n_kv_heads, a.group,
+                       a.scale_log2, a.scale, or_none(q, rows), or_none(k, keys), or_none(v, keys),
+                       or_none(out, rows), or_none(dout, rows), a.dq, a.dk, a.dv, lse,
+                       reinterpret_cast<float*>(row)};
+    if (p->n_queries) pdl(k_prompt_attn_dq<256>, p->n_queries * n_kv_heads, 256, 0, s)(b);
+    b.items -= p->n_keys;
+    if (p->n_keys) pdl(k_prompt_attn_dkv<256>, p->n_keys * n_kv_heads, 256, 0, s)(b);
     return launched(what);
 }
