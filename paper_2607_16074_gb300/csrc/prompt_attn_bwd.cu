@@ -658,94 +658,573 @@ static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows&
     return launched(what);
 }
 
-struct PromptSimpleArgs {
-    const int *cu_q, *cu_kv, *prefix;
-    const int2* items;
-    int H, Hkv, group;
-    float scale_log2, scale;
-    jnx_head_rows q, k, v, out, dout, dq, dk, dv;
-    const float* lse;
-    float* D;
-};
+// ---------------------------------------------------------------------------
+// Head dim 256.  An accumulator is 256 columns, so the keys' pass is two, dK then dV, and
+// the outer tiles take 128 KB of shared memory, so an inner tile is 64 rows: S and dP are
+// 64 columns, double-buffered, and a tile's two scores are issued two tiles ahead of the
+// product that takes dS (or P), which the elementwise warps write over S.
+//   DK   S^T = K Q^T, dP^T = V dO^T, dK += dS^T Q
+//   DV   S^T = K Q^T, dV += P^T dO
+//   DQ   S = Q K^T, dP = dO V^T, dQ += dS K
+// ---------------------------------------------------------------------------
+namespace pwide {
+constexpr int BM = 128, BN = 64, HD = 256, NCH = 4;
+enum { DK = 0, DV = 1, DQ = 2 };
+constexpr int OB = BM * HD * 2, IB = BN * HD * 2;
+// barriers of a pass
+enum { O_FULL = 0, O_EMPTY = 1, B1_FULL = 2, B1_EMPTY = 4, B2_FULL = 6, B2_EMPTY = 8, S_FULL = 10,
+       P_FULL = 12, ACC_FULL = 14, ACC_FREE = 15, DRAIN = 16, ST_FULL = 17, ST_EMPTY = 19, W_FULL = 21,
+       W_EMPTY = 23, N_BARS = 25 };
+constexpr int OFF_B1 = 2 * OB;           // two slots
+constexpr int OFF_B2 = OFF_B1 + 2 * IB;  // one; DV has two in the second outer tile's place
+constexpr int OFF_ST = OFF_B2 + IB;      // [2][lse, D, limit][64]
+constexpr int OFF_BAR = OFF_ST + 2 * 3 * BN * 4;
+constexpr int SMEM = OFF_BAR + N_BARS * 8 + 80 + 1024;
+static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
+constexpr int THREADS = 384, EW = 8, READERS = 2 + EW;
+constexpr uint32_t S_COL = 0, DP_COL = 2 * BN, ACC_COL = 256;
+}  // namespace pwide
 
-template <int E>
-__device__ __forceinline__ void row_load(float (&f)[E], const jnx_head_rows& r, long long row,
-                                         int head, int lane) {
-    for (int e = 0; e < E; ++e)
-        f[e] = bf2f(r.ptr[row * r.row_stride + head * r.head_stride + e * 32 + lane]);
-}
+template <int PASS>
+__device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, const CUtensorMap& tqi,
+                                                    const CUtensorMap& tko, const CUtensorMap& tki,
+                                                    const CUtensorMap& tvo, const CUtensorMap& tvi,
+                                                    const CUtensorMap& tdo, const CUtensorMap& tdi,
+                                                    const PromptBwdArgs& p, uint8_t* sm, uint64_t* bar,
+                                                    volatile int* fail_flag, uint32_t tbase,
+                                                    int q_first, int claim) {
+    using namespace pwide;
+    constexpr bool KP = PASS != DQ, NEED_DP = PASS != DV;
+    // B1 holds a tile from its score to its product, so with two slots the next scores would
+    // wait for their whole load right behind each product: tiles go in pairs instead, two
+    // products, then two tiles' scores, whose loads have been under way since
+    constexpr bool PAIRED = NEED_DP;
+    constexpr int NB2 = NEED_DP ? 1 : 2;
+    const int T = tile_tokens(p.group), Ti = BN / p.group;  // tokens of outer and inner row tiles
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    uint8_t* b1 = sm + OFF_B1;
+    uint8_t* b2 = sm + (NEED_DP ? OFF_B2 : OB);
+    float* st = reinterpret_cast<float*>(sm + OFF_ST);
+    volatile int* slot = fail_flag + 1;  // [2][8]: items handed out
+    const int2* items = p.items + (KP ? 0 : p.n_keys);
+    const int n_work = (KP ? p.n_keys : p.n_queries) * p.Hkv;
 
-template <int E>
-__device__ __forceinline__ float row_dot(const float (&x)[E], const float (&y)[E]) {
-    float d = 0.f;
-    for (int e = 0; e < E; ++e) d += x[e] * y[e];
-    for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-    return d;
-}
+    int seen = 0;
+    auto next_item = [&](bool& ok) -> PromptBwdItem {
+        const int b = seen & 1;
+        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0};
+        if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen >> 1) & 1))) return x;
+        x.at = warp_uniform(slot[8 * b]);
+        x.kvh = warp_uniform(slot[8 * b + 1]);
+        x.q0 = warp_uniform(slot[8 * b + 2]);
+        x.Lq = warp_uniform(slot[8 * b + 3]);
+        x.k0 = warp_uniform(slot[8 * b + 4]);
+        x.Lk = warp_uniform(slot[8 * b + 5]);
+        x.pre = warp_uniform(slot[8 * b + 6]);
+        if (elect_one()) mbar_arrive(&bar[W_EMPTY + b]);
+        __syncwarp();
+        ++seen;
+        return x;
+    };
+    auto first_tok = [&](const PromptBwdItem& x) { return first_row(x.at, x.Lq, x.Lk, x.pre); };
+    auto n_inner = [&](const PromptBwdItem& x) {
+        if (KP) return (x.Lq - first_tok(x) + Ti - 1) / Ti;
+        return (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BN - 1) / BN;
+    };
 
-// Query rows, one warp each: D and dQ.
-template <int HD>
-__global__ void __launch_bounds__(256) k_prompt_attn_dq(const __grid_constant__ PromptSimpleArgs a) {
-    constexpr int E = HD / 32;
-    pdl_entry();
-    const int2 it = a.items[blockIdx.x / a.Hkv];
-    const int kvh = blockIdx.x % a.Hkv, s = it.x;
-    const int q0 = a.cu_q[s], Lq = a.cu_q[s + 1] - q0, k0 = a.cu_kv[s], Lk = a.cu_kv[s + 1] - k0;
-    const int pre = a.prefix ? a.prefix[s] : 0, lane = threadIdx.x & 31;
-    const int rows = min(tile_tokens(a.group), Lq - it.y) * a.group;
-    for (int r = threadIdx.x >> 5; r < rows; r += 8) {
-        const int i = it.y + r / a.group, h = kvh * a.group + r % a.group;
-        const int n = keys_seen(i, Lq, Lk, pre);
-        float q[E], o[E], go[E], dq[E] = {};
-        row_load(q, a.q, q0 + i, h, lane);
-        row_load(o, a.out, q0 + i, h, lane);
-        row_load(go, a.dout, q0 + i, h, lane);
-        const float D = row_dot(o, go), lse = a.lse[(size_t)(q0 + i) * a.H + h];
-        if (lane == 0) a.D[(size_t)(q0 + i) * a.H + h] = D;
-        for (int j = 0; j < n; ++j) {
-            float k[E], v[E];
-            row_load(k, a.k, k0 + j, kvh, lane);
-            row_load(v, a.v, k0 + j, kvh, lane);
-            const float p = exp2f(row_dot(q, k) * a.scale_log2 - lse);
-            const float ds = p * (row_dot(go, v) - D) * a.scale;
-            for (int e = 0; e < E; ++e) dq[e] += ds * k[e];
+    if (warp == 0) {
+        // ---------------- claims and TMA ----------------
+        bool ok = true;
+        int told = 0;
+        auto tell = [&](const PromptBwdItem& x) {
+            const int b = told & 1;
+            if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told >> 1) & 1) ^ 1)) return false;
+            if (elect_one()) {
+                slot[8 * b] = x.at;
+                slot[8 * b + 1] = x.kvh;
+                slot[8 * b + 2] = x.q0;
+                slot[8 * b + 3] = x.Lq;
+                slot[8 * b + 4] = x.k0;
+                slot[8 * b + 5] = x.Lk;
+                slot[8 * b + 6] = x.pre;
+                mbar_arrive(&bar[W_FULL + b]);
+            }
+            __syncwarp();
+            ++told;
+            return true;
+        };
+        int no = 0;
+        uint32_t g1 = 0, g2 = 0;  // inner tiles loaded into each ring
+        auto load = [&](const CUtensorMap* m, uint8_t* dst, int rows, int head, int row, uint64_t* full) {
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) tma_load_3d(dst + c * rows * 128, m, c * 64, head, row, full);
+        };
+        int2 e = make_int2(0, 0);
+        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0};
+        auto fetch = [&]() {
+            claim = __shfl_sync(0xffffffffu, claim, 0);
+            if (claim - q_first >= n_work) return;
+            e = items[(claim - q_first) / p.Hkv];
+            nx.at = e.y;
+            nx.kvh = (claim - q_first) % p.Hkv;
+            nx.q0 = p.cu_q[e.x];
+            nx.Lq = p.cu_q[e.x + 1] - nx.q0;
+            nx.k0 = p.cu_kv[e.x];
+            nx.Lk = p.cu_kv[e.x + 1] - nx.k0;
+            nx.pre = p.prefix ? p.prefix[e.x] : 0;
+        };
+        const uint32_t orow = p.group * T * HD * 2, irow = p.group * Ti * HD * 2;
+        fetch();
+        while (claim - q_first < n_work) {
+            if (__any_sync(0xffffffffu, *fail_flag)) {
+                ok = false;
+                break;
+            }
+            PromptBwdItem x;
+            x.at = warp_uniform(nx.at);
+            x.kvh = warp_uniform(nx.kvh);
+            x.q0 = warp_uniform(nx.q0);
+            x.Lq = warp_uniform(nx.Lq);
+            x.k0 = warp_uniform(nx.k0);
+            x.Lk = warp_uniform(nx.Lk);
+            x.pre = warp_uniform(nx.pre);
+            if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
+            __syncwarp();
+            if (!(ok = tell(x))) break;
+            const int n = n_inner(x), i0 = KP ? first_tok(x) : x.at;
+            const int qh = x.kvh * p.group;
+            if (n > 0) {
+                if (no > 0 && !(ok = mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[O_FULL],
+                                          PASS == DK ? 2 * OB : PASS == DV ? OB : 2 * orow);
+                    if (KP) {
+                        load(&tko, sm, BM, x.kvh, x.k0 + x.at, &bar[O_FULL]);
+                        if (NEED_DP) load(&tvo, sm + OB, BM, x.kvh, x.k0 + x.at, &bar[O_FULL]);
+                    } else {
+                        load(&tqo, sm, BM, qh, x.q0 + x.at, &bar[O_FULL]);
+                        load(&tdo, sm + OB, BM, qh, x.q0 + x.at, &bar[O_FULL]);
+                    }
+                }
+                __syncwarp();
+                ++no;
+            }
+            for (int j = 0; j < n && ok; ++j) {
+                const int s1 = g1 & 1, s2 = g2 % NB2;
+                if (!(ok = mbar_wait_warp(&bar[B1_EMPTY + s1], ((g1 >> 1) & 1) ^ 1))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[B1_FULL + s1], KP ? irow : IB);
+                    if (KP) load(&tqi, b1 + s1 * IB, BN, qh, x.q0 + i0 + j * Ti, &bar[B1_FULL + s1]);
+                    else load(&tki, b1 + s1 * IB, BN, x.kvh, x.k0 + j * BN, &bar[B1_FULL + s1]);
+                }
+                __syncwarp();
+                ++g1;
+                if (!(ok = mbar_wait_warp(&bar[B2_EMPTY + s2], ((g2 / NB2) & 1) ^ 1))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[B2_FULL + s2], KP ? irow : IB);
+                    if (KP) load(&tdi, b2 + s2 * IB, BN, qh, x.q0 + i0 + j * Ti, &bar[B2_FULL + s2]);
+                    else load(&tvi, b2 + s2 * IB, BN, x.kvh, x.k0 + j * BN, &bar[B2_FULL + s2]);
+                }
+                __syncwarp();
+                ++g2;
+            }
+            if (!ok) break;
+            fetch();
         }
-        for (int e = 0; e < E; ++e)
-            a.dq.ptr[(q0 + i) * a.dq.row_stride + h * a.dq.head_stride + e * 32 + lane] = f2bf(dq[e]);
-    }
-}
-
-// Keys, one warp each.
-template <int HD>
-__global__ void __launch_bounds__(256) k_prompt_attn_dkv(const __grid_constant__ PromptSimpleArgs a) {
-    constexpr int E = HD / 32;
-    pdl_entry();
-    const int2 it = a.items[blockIdx.x / a.Hkv];
-    const int kvh = blockIdx.x % a.Hkv, s = it.x;
-    const int q0 = a.cu_q[s], Lq = a.cu_q[s + 1] - q0, k0 = a.cu_kv[s], Lk = a.cu_kv[s + 1] - k0;
-    const int pre = a.prefix ? a.prefix[s] : 0, lane = threadIdx.x & 31;
-    for (int j = it.y + (threadIdx.x >> 5); j < min(it.y + 128, Lk); j += 8) {
-        float k[E], v[E], dk[E] = {}, dv[E] = {};
-        row_load(k, a.k, k0 + j, kvh, lane);
-        row_load(v, a.v, k0 + j, kvh, lane);
-        for (int i = first_row(j, Lq, Lk, pre); i < Lq; ++i)
-            for (int h = kvh * a.group; h < (kvh + 1) * a.group; ++h) {
-                float q[E], go[E];
-                row_load(q, a.q, q0 + i, h, lane);
-                row_load(go, a.dout, q0 + i, h, lane);
-                const size_t at = (size_t)(q0 + i) * a.H + h;
-                const float p = exp2f(row_dot(q, k) * a.scale_log2 - a.lse[at]);
-                const float ds = p * (row_dot(go, v) - a.D[at]) * a.scale;
-                for (int e = 0; e < E; ++e) {
-                    dk[e] += ds * q[e];
-                    dv[e] += p * go[e];
+        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0});
+        if (!ok) *fail_flag = 1;
+        // every copy has landed before the pass ends (at once in a normal run)
+        if (no > 0) mbar_wait_warp(&bar[O_FULL], (no - 1) & 1, 100000000LL);
+        for (uint32_t i = g1 > 2 ? g1 - 2 : 0; i < g1; ++i)
+            mbar_wait_warp(&bar[B1_FULL + (i & 1)], (i >> 1) & 1, 100000000LL);
+        for (uint32_t i = g2 > NB2 ? g2 - NB2 : 0; i < g2; ++i)
+            mbar_wait_warp(&bar[B2_FULL + i % NB2], (i / NB2) & 1, 100000000LL);
+        // ... and every release has arrived before the barriers are made anew
+        if (no > 0) mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1, 100000000LL);
+        for (uint32_t i = g1 > 2 ? g1 - 2 : 0; i < g1; ++i)
+            mbar_wait_warp(&bar[B1_EMPTY + (i & 1)], (i >> 1) & 1, 100000000LL);
+        for (uint32_t i = g2 > NB2 ? g2 - NB2 : 0; i < g2; ++i)
+            mbar_wait_warp(&bar[B2_EMPTY + i % NB2], (i / NB2) & 1, 100000000LL);
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
+        constexpr uint32_t IDESC_ACC = idesc_bf16_f32(BM, HD) | (1u << 16);  // B MN-major
+        bool ok = true, issued = false;
+        int no = 0, done = 0;
+        uint32_t c1 = 0, c2 = 0;          // tiles of B1 / B2 taken by scores
+        uint32_t a1 = 0, a2 = 0;          // ... by the sums
+        uint32_t gs = 0, gp = 0;          // scores issued, P / dS tiles taken
+        const uint32_t o1 = smem_u32(sm), o2 = o1 + OB;
+        auto commit = [&](uint64_t* b) {
+            if (elect_one()) tc_commit(b);
+            __syncwarp();
+        };
+        auto score = [&](uint32_t d, uint32_t outer, uint8_t* inner) {
+            const uint32_t a_lo = sw128_desc_lo(outer), b_lo = sw128_desc_lo(smem_u32(inner));
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < HD / 16; ++ks)
+                    tc_mma_f16(d, desc_of(a_lo + (ks >> 2) * BM * 8 + (ks & 3) * 2, kSw128DescHi),
+                               desc_of(b_lo + (ks >> 2) * BN * 8 + (ks & 3) * 2, kSw128DescHi), IDESC_S,
+                               ks > 0);
+            }
+            __syncwarp();
+            issued = true;
+        };
+        auto gather = [&](uint32_t x, uint8_t* inner, bool accumulate) {
+            const uint32_t b = smem_u32(inner);
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < BN / 16; ++ks)
+                    tc_mma_f16_ts(tbase + ACC_COL, x + (ks >> 1) * 32 + (ks & 1) * 8,
+                                  sw128_desc_mn(b + ks * 16 * 128, BN * 128, 1024), IDESC_ACC,
+                                  accumulate || ks > 0);
+            }
+            __syncwarp();
+        };
+        auto zero_tail = [&](uint8_t* tile, int valid, int end) {
+            for (int i = lane; i < (end - valid) * (HD / 8); i += 32) {
+                const int r = valid + i / (HD / 8), u = i % (HD / 8);
+                *reinterpret_cast<uint4*>(tile + (u >> 3) * BN * 128 + r * 128 + (u & 7) * 16) =
+                    make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async();
+            __syncwarp();
+        };
+        while (ok) {
+            const PromptBwdItem x = next_item(ok);
+            if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            if (n == 0) continue;
+            if (!(ok = mbar_wait_warp(&bar[O_FULL], no & 1))) break;
+            ++no;
+            tc_fence_after();
+            const int box = KP ? p.group * Ti : BN;
+            auto valid = [&](int j) {
+                return KP ? min(Ti, x.Lq - i0 - j * Ti) * p.group : min(BN, x.Lk - j * BN);
+            };
+            auto scores = [&](int j) -> bool {
+                const uint32_t b = gs & 1;
+                const int s1 = c1 & 1, s2 = c2 % NB2;
+                if (!mbar_wait_warp(&bar[B1_FULL + s1], (c1 >> 1) & 1)) return false;
+                if (valid(j) < box) zero_tail(b1 + s1 * IB, valid(j), box);
+                tc_fence_after();
+                score(tbase + S_COL + b * BN, o1, b1 + s1 * IB);
+                if (PASS == DV) commit(&bar[B1_EMPTY + s1]);
+                ++c1;
+                if (NEED_DP) {
+                    if (!mbar_wait_warp(&bar[B2_FULL + s2], (c2 / NB2) & 1)) return false;
+                    if (KP && valid(j) < box) zero_tail(b2 + s2 * IB, valid(j), box);
+                    tc_fence_after();
+                    score(tbase + DP_COL + b * BN, o2, b2 + s2 * IB);
+                    commit(&bar[B2_EMPTY + s2]);
+                    ++c2;
+                }
+                commit(&bar[S_FULL + b]);
+                ++gs;
+                return true;
+            };
+            ok = scores(0) && (n < 2 || scores(1));
+            int ns = min(n, 2);
+            if (ok && ns == n) commit(&bar[O_EMPTY]);
+            for (int j = 0; j < n && ok; ++j) {
+                const uint32_t b = gp & 1;
+                if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (gp >> 1) & 1))) break;
+                ++gp;
+                // the item's first product overwrites the sums: the last epilogue has read them
+                if (j == 0 && done > 0 && !(ok = mbar_wait_warp(&bar[ACC_FREE], (done - 1) & 1))) break;
+                if (PASS == DV) {
+                    const int s2 = a2 % NB2;
+                    if (!(ok = mbar_wait_warp(&bar[B2_FULL + s2], (a2 / NB2) & 1))) break;
+                    if (valid(j) < box) zero_tail(b2 + s2 * IB, valid(j), box);
+                    tc_fence_after();
+                    gather(tbase + S_COL + b * BN, b2 + s2 * IB, j > 0);
+                    commit(&bar[B2_EMPTY + s2]);
+                    ++a2;
+                } else {
+                    tc_fence_after();
+                    gather(tbase + S_COL + b * BN, b1 + (a1 & 1) * IB, j > 0);
+                    commit(&bar[B1_EMPTY + (a1 & 1)]);
+                    ++a1;
+                }
+                // scores of tile j + 2 reuse buffer b: the products above have read it, the
+                // tensor core running this thread's MMAs in issue order
+                const int upto = !PAIRED || (j & 1) ? j + 3 : 0;
+                for (; ok && ns < min(upto, n); ++ns) {
+                    ok = scores(ns);
+                    if (ok && ns + 1 == n) commit(&bar[O_EMPTY]);
                 }
             }
-        for (int e = 0; e < E; ++e) {
-            a.dk.ptr[(k0 + j) * a.dk.row_stride + kvh * a.dk.head_stride + e * 32 + lane] = f2bf(dk[e]);
-            a.dv.ptr[(k0 + j) * a.dv.row_stride + kvh * a.dv.head_stride + e * 32 + lane] = f2bf(dv[e]);
+            if (!ok) break;
+            commit(&bar[ACC_FULL]);
+            ++done;
         }
+        if (!ok) *fail_flag = 1;
+        if (issued) {
+            commit(&bar[DRAIN]);
+            mbar_wait_warp(&bar[DRAIN], 0, 100000000LL);
+        }
+    } else if (warp == 2) {
+        // ---------------- values of the inner rows (keys' passes) ----------------
+        bool ok = true;
+        uint32_t g = 0;
+        while (ok) {
+            const PromptBwdItem x = next_item(ok);
+            if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            if (!KP) continue;
+            const int n = n_inner(x), i0 = first_tok(x);
+            for (int j = 0; j < n; ++j, ++g) {
+                const int b = g & 1;
+                float2 v[2];
+                int lim[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = e * 32 + lane, t = r / p.group, i = i0 + j * Ti + t;
+                    const bool live = t < Ti && i < x.Lq;
+                    v[e] = live ? p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + r % p.group]
+                                : make_float2(INFINITY, 0.f);
+                    lim[e] = live ? keys_seen(i, x.Lq, x.Lk, x.pre) : 0;
+                }
+                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g >> 1) & 1) ^ 1))) break;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = e * 32 + lane;
+                    st[b * 192 + r] = v[e].x;
+                    st[b * 192 + 64 + r] = v[e].y;
+                    st[b * 192 + 128 + r] = __int_as_float(lim[e]);
+                }
+                mbar_arrive(&bar[ST_FULL + b]);
+            }
+        }
+        if (!ok) *fail_flag = 1;
+    } else if (warp >= 4) {
+        // ---------------- elementwise + epilogue ----------------
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const int r = quarter * 32 + lane;
+        uint32_t g = 0;
+        int done = 0;
+        bool ok = true;
+        while (ok) {
+            const PromptBwdItem x = next_item(ok);
+            if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            const int tok = r / p.group, hg = r % p.group;
+            const int key = x.at + r, i = x.at + tok;
+            const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
+            float lse = INFINITY, D = 0.f;
+            int lim = 0x7fffffff;
+            if (!KP && live) {
+                const float2 v = p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + hg];
+                lse = v.x;
+                D = v.y;
+                lim = keys_seen(i, x.Lq, x.Lk, x.pre);
+            }
+            for (int j = 0; j < n; ++j, ++g) {
+                const float* sv = st + (g & 1) * 192 + half * 32;
+                const uint32_t b = g & 1, ph = (g >> 1) & 1;
+                const uint32_t tS = tbase + lane_base + S_COL + b * BN + half * 32;
+                const uint32_t tP = tbase + lane_base + DP_COL + b * BN + half * 32;
+                bool whole;
+                if (KP) {
+                    whole = keys_seen(min(i0 + j * Ti, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
+                            min(x.at + BM, x.Lk);
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + b], ph)))) break;
+                } else {
+                    whole = __all_sync(0xffffffffu, lim >= (j + 1) * BN);
+                }
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[S_FULL + b], ph)))) break;
+                tc_fence_after();
+                uint32_t s[32], d[32], pk[16];
+                tmem_ld32(tS, s);
+                if (NEED_DP) tmem_ld32(tP, d);
+                tmem_ld_wait_regs(s);
+                if (NEED_DP) tmem_ld_wait_regs(d);
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    float4 l4 = make_float4(lse, lse, lse, lse), d4 = make_float4(D, D, D, D);
+                    if (KP) {
+                        l4 = *reinterpret_cast<const float4*>(sv + e);
+                        if (NEED_DP) d4 = *reinterpret_cast<const float4*>(sv + 64 + e);
+                    }
+                    const float *lp = &l4.x, *dp = &d4.x;
+                    float v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const float pr =
+                            ex2_approx(fmaf(__uint_as_float(s[e + u]), p.scale_log2, -lp[u]));
+                        v[u] = NEED_DP ? pr * (__uint_as_float(d[e + u]) - dp[u]) : pr;
+                        if (!whole) {
+                            const bool hidden = KP ? key >= __float_as_int(sv[128 + e + u])
+                                                   : j * BN + half * 32 + e + u >= lim;
+                            if (hidden) v[u] = 0.f;
+                        }
+                    }
+                    pk[e / 2] = pack_bf2(v[0], v[1]);
+                    pk[e / 2 + 1] = pack_bf2(v[2], v[3]);
+                }
+                tmem_st16(tS, pk);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (elect_one()) {
+                    mbar_arrive(&bar[P_FULL + b]);
+                    if (KP) mbar_arrive(&bar[ST_EMPTY + b]);
+                }
+                __syncwarp();
+            }
+            if (!ok) break;
+            if (n > 0) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ACC_FULL], done & 1)))) break;
+                tc_fence_after();
+                ++done;
+            }
+            const float f = PASS == DV ? 1.f : p.scale;
+            uint16_t* o;
+            if (KP) {
+                const jnx_head_rows& to = PASS == DV ? p.dv : p.dk;
+                o = to.ptr + (long long)(x.k0 + key) * to.row_stride + x.kvh * to.head_stride;
+            } else {
+                o = p.dq.ptr + (long long)(x.q0 + i) * p.dq.row_stride +
+                    (x.kvh * p.group + hg) * p.dq.head_stride;
+            }
+            o += half * (HD / 2);
+#pragma unroll 1
+            for (int c = 0; c < HD / 64; ++c) {
+                uint32_t v[32];
+                if (n > 0) {
+                    tmem_ld32(tbase + lane_base + ACC_COL + half * (HD / 2) + c * 32, v);
+                    tmem_ld_wait_regs(v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = 0;
+                }
+                if (live) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint4*>(o + c * 32 + e * 8) = make_uint4(
+                            pack_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
+                            pack_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
+                            pack_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
+                            pack_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
+                }
+            }
+            if (n > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (elect_one()) mbar_arrive(&bar[ACC_FREE]);
+                __syncwarp();
+            }
+        }
+        if (!ok) *fail_flag = 1;
     }
+    return claim;
+}
+
+__global__ void __launch_bounds__(pwide::THREADS, 1)
+    k_prompt_attn_bwd_wide(const __grid_constant__ CUtensorMap tqo, const __grid_constant__ CUtensorMap tqi,
+                           const __grid_constant__ CUtensorMap tko, const __grid_constant__ CUtensorMap tki,
+                           const __grid_constant__ CUtensorMap tvo, const __grid_constant__ CUtensorMap tvi,
+                           const __grid_constant__ CUtensorMap tdo, const __grid_constant__ CUtensorMap tdi,
+                           const __grid_constant__ PromptBwdArgs p) {
+    using namespace pwide;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* bar = reinterpret_cast<uint64_t*>(sm + OFF_BAR);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + N_BARS);
+    volatile int* fail_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = warp_uniform(threadIdx.x >> 5);
+    auto init_bars = [&](bool again) {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < N_BARS; ++i) {
+                if (again) mbar_inval(&bar[i]);
+                mbar_init(&bar[i], i == P_FULL || i == P_FULL + 1 || i == ACC_FREE ? EW
+                                   : i >= ST_EMPTY && i < W_FULL                   ? EW
+                                   : i >= ST_FULL && i < ST_EMPTY                  ? 32
+                                   : i >= W_EMPTY                                  ? READERS
+                                                                                   : 1);
+            }
+            fence_barrier_init();
+        }
+    };
+    // inner rows that no box reaches (64 no multiple of the group) are zero in the keys'
+    // passes: all slots, and what DV puts in the second outer tile's place
+    const int box = p.group * (BN / p.group);
+    auto zero_rows = [&](uint8_t* at, int tiles) {
+        for (int i = threadIdx.x; i < tiles * NCH * (BN - box) * 8; i += THREADS) {
+            const int u = i & 7, r = box + (i >> 3) % (BN - box), t = (i >> 3) / (BN - box);
+            *reinterpret_cast<uint4*>(at + t * BN * 128 + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async();
+    };
+    init_bars(false);
+    if (threadIdx.x == 0) *fail_flag = 0;
+    zero_rows(sm + OFF_B1, 3);
+    pdl_entry();  // TMEM is taken once the grid ahead has given its own back
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = warp_uniform(*tmem_slot);
+    // a pass leaves no copy, MMA or TMEM read of its own behind
+    bool failed;
+    auto end_pass = [&]() {
+        __syncwarp();
+        tc_fence_before();
+        failed = __syncthreads_or(*fail_flag);
+        init_bars(true);
+        tc_fence_after();
+    };
+    const int nk = p.n_keys * p.Hkv;
+    int claim = prompt_bwd_wide_pass<DK>(tqo, tqi, tko, tki, tvo, tvi, tdo, tdi, p, sm, bar, fail_flag,
+                                         tbase, 0, blockIdx.x);
+    end_pass();
+    zero_rows(sm + OB, 2);
+    __syncthreads();
+    if (!failed) {
+        claim = prompt_bwd_wide_pass<DV>(tqo, tqi, tko, tki, tvo, tvi, tdo, tdi, p, sm, bar, fail_flag,
+                                         tbase, nk, claim);
+        end_pass();
+        __syncthreads();
+    }
+    if (!failed) {
+        prompt_bwd_wide_pass<DQ>(tqo, tqi, tko, tki, tvo, tvi, tdo, tdi, p, sm, bar, fail_flag, tbase,
+                                 2 * nk, claim);
+        __syncwarp();
+        tc_fence_before();
+        failed = __syncthreads_or(*fail_flag);
+        tc_fence_after();
+    }
+    if (failed && threadIdx.x == 0) report(p.status, JNX_ERR_TIMEOUT);
+    if (warp == 1) tmem_dealloc(tbase, 512);
+}
+
+static jnx_status launch_prompt_bwd_wide(const PromptBwdArgs& a, const jnx_head_rows& q,
+                                         const jnx_head_rows& k, const jnx_head_rows& v,
+                                         const jnx_head_rows& dout, int rows, int keys, cudaStream_t s) {
+    using namespace pwide;
+    const char* what = "prompt attention backward";
+    static std::atomic<uint64_t> attr{0};
+    if (set_smem_limit(reinterpret_cast<const void*>(k_prompt_attn_bwd_wide), SMEM, attr) != cudaSuccess)
+        return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
+    const int T = tile_tokens(a.group), Ti = BN / a.group;
+    CUtensorMap m[8];
+    if (!make_tmap_heads(&m[0], q, rows, a.H, HD, a.group, T) ||
+        !make_tmap_heads(&m[1], q, rows, a.H, HD, a.group, Ti) ||
+        !make_tmap_heads(&m[2], k, keys, a.Hkv, HD, 1, BM) ||
+        !make_tmap_heads(&m[3], k, keys, a.Hkv, HD, 1, BN) ||
+        !make_tmap_heads(&m[4], v, keys, a.Hkv, HD, 1, BM) ||
+        !make_tmap_heads(&m[5], v, keys, a.Hkv, HD, 1, BN) ||
+        !make_tmap_heads(&m[6], dout, rows, a.H, HD, a.group, T) ||
+        !make_tmap_heads(&m[7], dout, rows, a.H, HD, a.group, Ti))
+        return fail(JNX_ERR_CUDA, "%s: tensor map encode failed", what);
+    const int grid = (int)std::min<long long>(((long long)2 * a.n_keys + a.n_queries) * a.Hkv, num_sms());
+    pdl(k_prompt_attn_bwd_wide, grid, THREADS, SMEM, s)(m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], a);
+    return launched(what);
 }
 
 }  // namespace jnx
@@ -775,7 +1254,7 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7) ||
         ws_bytes < jnx_op_prompt_attention_backward_workspace_bytes(rows, n_heads))
         return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
-    const long long n_work = ((long long)p->n_keys + p->n_queries) * n_kv_heads;
+    const long long n_work = ((long long)2 * p->n_keys + p->n_queries) * n_kv_heads;
     // (claims run past the last item by one for each CTA and pass)
     if (n_work > 0x7FFFFFFFLL - 4 * num_sms() || (long long)rows * n_heads > 0x7FFFFFF00LL)
         return fail(JNX_ERR_UNSUPPORTED, "%s: too many work items", what);
@@ -802,12 +1281,5 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     const int nr = std::max(rows, 1), nk = std::max(keys, 1);
     if (head_dim == 64) return launch_prompt_bwd<64>(a, qq, kk, vv, dd, nr, nk, s);
     if (head_dim == 128) return launch_prompt_bwd<128>(a, qq, kk, vv, dd, nr, nk, s);
-    PromptSimpleArgs b{p->cu_q, p->cu_kv, p->prefix, a.items + p->n_keys, n_heads, n_kv_heads, a.group,
-                       a.scale_log2, a.scale, or_none(q, rows), or_none(k, keys), or_none(v, keys),
-                       or_none(out, rows), or_none(dout, rows), a.dq, a.dk, a.dv, lse,
-                       reinterpret_cast<float*>(row)};
-    if (p->n_queries) pdl(k_prompt_attn_dq<256>, p->n_queries * n_kv_heads, 256, 0, s)(b);
-    b.items -= p->n_keys;
-    if (p->n_keys) pdl(k_prompt_attn_dkv<256>, p->n_keys * n_kv_heads, 256, 0, s)(b);
-    return launched(what);
+    return launch_prompt_bwd_wide(a, qq, kk, vv, dd, nr, nk, s);
 }
