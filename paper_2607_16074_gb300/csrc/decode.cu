@@ -23,7 +23,7 @@ namespace decode {
 constexpr int WARPS = 4;
 constexpr int STAGES = 3;
 constexpr int ROWS = 16;       // query heads of a unit
-constexpr int BATCH = 2048;    // sequences of one launch
+constexpr int BATCH = 1024;    // sequences of one launch
 constexpr int MAX_RUNS = 128;  // runs of a sequence
 
 // Tokens of a sequence's runs: short ones for short sequences, so that a few sequences
@@ -71,7 +71,7 @@ struct DecodeCfg {
     static constexpr int RING = decode::STAGES * 2 * KV;
     static constexpr int OFF_BAR = decode::WARPS * RING;
     static constexpr int OFF_FIRST = OFF_BAR + decode::WARPS * decode::STAGES * 8;
-    static constexpr int SMEM = OFF_FIRST + (2 * decode::BATCH + 1) * 4 + 1024;
+    static constexpr int SMEM = OFF_FIRST + (3 * decode::BATCH + 1) * 4 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -92,6 +92,7 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     int* first = reinterpret_cast<int*>(sm + C::OFF_FIRST);  // [batch + 1] first run of each
     int* length = first + BATCH + 1;                         // [batch]
+    int* slots = length + BATCH;                             // [batch]
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     uint8_t* ring = sm + warp * C::RING;
     uint64_t* full = reinterpret_cast<uint64_t*>(sm + C::OFF_BAR) + warp * STAGES;
@@ -107,7 +108,7 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
     }
     // first runs: a warp scans the lengths
     for (int b = threadIdx.x; b < a.batch; b += 32 * WARPS)
-        length[b] = decode_length(a, b, blockIdx.x == 0);
+        slots[b] = a.slot[b], length[b] = decode_length(a, b, blockIdx.x == 0);
     __syncthreads();
     if (warp == 0) {
         int total = 0;
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
     __syncthreads();
     const int per_run = a.Hkv * a.blocks;  // units of a run: its heads, which lie together
     const int n_units = first[a.batch] * per_run;
-    const int step = gridDim.x * WARPS;
+    const int step = gridDim.x * WARPS, u0 = blockIdx.x + gridDim.x * warp;  // over the SMs first
 
     auto open = [&](int u) {
         DecodeAt x{u, 0, 0, 0, 0, 0, 0, 0};
@@ -150,12 +151,12 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
         return x;
     };
     // tiles are asked for by `ask`, STAGES ahead of the ones taken
-    DecodeAt ask = open(blockIdx.x * WARPS + warp);
+    DecodeAt ask = open(u0);
     uint32_t asked = 0, taken = 0;
     auto ask_one = [&]() {
         while (ask.u < n_units && ask.at >= ask.end) ask = open(ask.u + step);
         if (ask.u >= n_units) return;
-        const int s = asked % STAGES, slot = a.slot[ask.b];
+        const int s = asked % STAGES, slot = slots[ask.b];
         if (elect_one()) {
             mbar_arrive_expect_tx(&full[s], 2 * C::KV);
             uint8_t* dst = ring + s * 2 * C::KV;
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
     for (int i = 0; i < STAGES; ++i) ask_one();
 
     bool ok = true;
-    for (DecodeAt x = open(blockIdx.x * WARPS + warp); ok && x.u < n_units; x = open(x.u + step)) {
+    for (DecodeAt x = open(u0); ok && x.u < n_units; x = open(x.u + step)) {
         const int h0 = x.kvh * a.group + x.block * ROWS;             // first query head
         const int heads = min(ROWS, a.group - x.block * ROWS);
         const int r0 = lane >> 2, cq = (lane & 3) * 2;               // fragment row and column
@@ -305,12 +306,13 @@ template <int HD>
 __global__ void __launch_bounds__(128) k_decode_join(const __grid_constant__ DecodeArgs a) {
     using namespace decode;
     constexpr int E = HD / 32, R = MAX_RUNS / 32;
-    pdl_entry();
     const int w = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (w >= a.batch * a.H) return;
-    const int b = w / a.H, h = w % a.H;
+    // the lengths are older than the grid ahead, which starts this one only once all its
+    // CTAs have waited for what came before: they need no wait
+    const int b = min(w / a.H, a.batch - 1), h = w % a.H;
     const int n = decode_length(a, b, false), nr = runs(n);
-    if (nr == 1) return;
+    pdl_entry();
+    if (w >= a.batch * a.H || nr == 1) return;
     const float* src = a.part + (size_t)w * MAX_RUNS * (HD + 2);
     float m[R], l[R], top = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -367,11 +369,14 @@ static jnx_status launch_decode(const jnx_kv_cache& c, DecodeArgs a, cudaStream_
     const int batch = a.batch;
     for (int b0 = 0; b0 < batch; b0 += BATCH) {
         a.batch = std::min(BATCH, batch - b0);
-        // one CTA an SM, or a warp for each unit that the cache could hold
-        const long long units = (long long)a.batch * runs(c.room) * a.Hkv * a.blocks;
-        const int grid = (int)std::min<long long>((units + WARPS - 1) / WARPS, num_sms());
+        // a CTA an SM, or for each unit that the cache could hold (the runs of a length are
+        // fewest just beyond a border: 33 of 128 tokens at 4,097, 64 of 64 below)
+        long long most = 1;
+        for (int n : {1024, 4096, 16384, c.room}) most = std::max<long long>(most, runs(std::min(n, c.room)));
+        const long long units = (long long)a.batch * most * a.Hkv * a.blocks;
+        const int grid = (int)std::min<long long>(units, num_sms());
         pdl(k_decode_attn<HD>, grid, 32 * WARPS, C::SMEM, s)(tk, tv, a);
-        if (runs(c.room) > 1) pdl(k_decode_join<HD>, (a.batch * a.H + 3) / 4, 128, 0, s)(a);
+        if (most > 1) pdl(k_decode_join<HD>, (a.batch * a.H + 3) / 4, 128, 0, s)(a);
         a.q += a.batch * a.q_row;
         a.out += a.batch * a.o_row;
         a.slot += a.batch;

@@ -553,36 +553,44 @@ class StepPipeline:
 # operators of text tenants
 # ---------------------------------------------------------------------------
 
+_BF16 = torch.bfloat16
+
+
+def _refuse(t: torch.Tensor, dtype, shape) -> None:
+    raise ValueError(f"expected a {dtype} CUDA tensor {shape}, its last axis contiguous, got "
+                     f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+
+
 def _bf16(t: torch.Tensor, *shape) -> torch.Tensor:
-    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != shape or \
+    if t.dtype is not _BF16 or not t.is_cuda or t.shape != shape or \
             (t.stride(-1) != 1 and shape[-1] > 1):
-        raise ValueError(f"expected a bf16 CUDA tensor {shape} with contiguous last axis, got "
-                         f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+        _refuse(t, _BF16, shape)
     return t
 
 
 def _rows(t: torch.Tensor, *shape) -> J.jnx_head_rows:
     """Head rows [n, heads, head_dim] of any row and head stride."""
-    _bf16(t, *shape)
-    return J.jnx_head_rows(t.data_ptr() or None, t.stride(0), t.stride(1))
+    s = t.stride()
+    if t.dtype is not _BF16 or t.shape != shape or s[2] != 1 or not t.is_cuda:
+        _refuse(t, _BF16, shape)
+    return J.jnx_head_rows(t.data_ptr(), s[0], s[1])
 
 
 def _dense(t: torch.Tensor, dtype, *shape) -> int:
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"expected a contiguous {dtype} CUDA tensor {shape}, got {t.dtype} "
-                         f"{tuple(t.shape)} strides {t.stride()} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        _refuse(t, dtype, shape)
     return t.data_ptr()
 
 
 def _cache(k: torch.Tensor, v: torch.Tensor, n_kv_heads: int, head_dim: int) -> J.jnx_kv_cache:
     """A cache [slots, room, kv heads, head_dim]; k and v with the same strides."""
-    slots, room = k.shape[:2]
-    _bf16(k, slots, room, n_kv_heads, head_dim)
-    _bf16(v, slots, room, n_kv_heads, head_dim)
-    if k.stride() != v.stride():
-        raise ValueError(f"cache strides differ: {k.stride()} and {v.stride()}")
-    return J.jnx_kv_cache(k.data_ptr() or None, v.data_ptr() or None, slots, room, k.stride(0),
-                          k.stride(1), k.stride(2))
+    s, shape = k.stride(), k.shape
+    if k.dtype is not _BF16 or v.dtype is not _BF16 or v.shape != shape or v.stride() != s or \
+            shape[2:] != (n_kv_heads, head_dim) or s[3] != 1 or not k.is_cuda or not v.is_cuda:
+        raise ValueError(f"expected bf16 CUDA caches [slots, room, {n_kv_heads}, {head_dim}] of one "
+                         f"layout, got {k.dtype} {tuple(shape)} strides {s} and {v.dtype} "
+                         f"{tuple(v.shape)} strides {v.stride()}")
+    return J.jnx_kv_cache(k.data_ptr(), v.data_ptr(), shape[0], shape[1], s[0], s[1], s[2])
 
 
 class _TextOperator:
@@ -594,6 +602,12 @@ class _TextOperator:
         self.ws = torch.empty(max(int(ws_bytes), 16), dtype=torch.uint8, device=device)
         self._status, self._ws, self._nws = (self.status.data_ptr(), self.ws.data_ptr(),
                                              self.ws.numel())
+        self._lib, self._device = J.lib(), self.ws.device.index
+
+    def _on(self, stream: Optional[torch.cuda.Stream]) -> int:
+        if stream is not None:
+            return stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self._device)
 
     def check(self) -> None:
         """Raise what a kernel reported since the last check (waits for the device)."""
@@ -636,8 +650,8 @@ class QKNormRope(_TextOperator):
         """q [n, H, hd] and k [n, Hkv, hd] from qkv [n, (H + 2 Hkv) hd] at pos [axes, n]."""
         h, hkv, hd = self.dims
         n, ref, x, ld, p = self._args(qkv, pos)
-        J.check(J.lib().jnx_op_qk_norm_rope(ref, x, ld, p, n, C.byref(_rows(q, n, h, hd)),
-                                            C.byref(_rows(k, n, hkv, hd)), _stream(stream)))
+        J.check(self._lib.jnx_op_qk_norm_rope(ref, x, ld, p, n, C.byref(_rows(q, n, h, hd)),
+                                            C.byref(_rows(k, n, hkv, hd)), self._on(stream)))
 
     def append(self, qkv: torch.Tensor, pos: torch.Tensor, q: torch.Tensor,
                k_cache: torch.Tensor, v_cache: torch.Tensor, slot: torch.Tensor,
@@ -645,10 +659,10 @@ class QKNormRope(_TextOperator):
         """q as forward; key and value rows go to cache rows [slot[i], at[i]]."""
         h, hkv, hd = self.dims
         n, ref, x, ld, p = self._args(qkv, pos)
-        J.check(J.lib().jnx_op_qk_norm_rope_append(
+        J.check(self._lib.jnx_op_qk_norm_rope_append(
             ref, x, ld, p, n, C.byref(_rows(q, n, h, hd)),
             C.byref(_cache(k_cache, v_cache, hkv, hd)), _dense(slot, torch.int32, n),
-            _dense(at, torch.int32, n), self._status, _stream(stream)))
+            _dense(at, torch.int32, n), self._status, self._on(stream)))
 
     def backward(self, qkv: torch.Tensor, pos: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
                  dqkv: torch.Tensor, dgamma_q: Optional[torch.Tensor] = None,
@@ -660,9 +674,9 @@ class QKNormRope(_TextOperator):
         if dqkv.stride(0) != ld:
             raise ValueError("dqkv and qkv differ in their row strides")
         gains = [None if g is None else _dense(g, torch.float32, hd) for g in (dgamma_q, dgamma_k)]
-        J.check(J.lib().jnx_op_qk_norm_rope_backward(
+        J.check(self._lib.jnx_op_qk_norm_rope_backward(
             ref, x, ld, p, n, C.byref(_rows(dq, n, h, hd)), C.byref(_rows(dk, n, hkv, hd)),
-            dqkv.data_ptr(), *gains, self._ws, self._nws, _stream(stream)))
+            dqkv.data_ptr(), *gains, self._ws, self._nws, self._on(stream)))
 
 
 class PromptPlan:
@@ -723,16 +737,16 @@ class PromptAttention(_TextOperator):
         """out [n_q, H, hd]; lse [n_q, H] fp32 where the gradients are wanted later."""
         if lse is not None:
             lse = _dense(lse, torch.float32, self.plan.n_q, self.dims[0])
-        J.check(J.lib().jnx_op_prompt_attention(
+        J.check(self._lib.jnx_op_prompt_attention(
             self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out), lse,
-            self._status, _stream(stream)))
+            self._status, self._on(stream)))
 
     def backward(self, q, k, v, out, lse, dout, dq, dk, dv, stream=None) -> None:
         """dq, dk, dv from dout, with the forward's out and lse."""
-        J.check(J.lib().jnx_op_prompt_attention_backward(
+        J.check(self._lib.jnx_op_prompt_attention_backward(
             self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out),
             _dense(lse, torch.float32, self.plan.n_q, self.dims[0]), self._q(dout), self._q(dq),
-            self._kv(dk), self._kv(dv), self._ws, self._nws, self._status, _stream(stream)))
+            self._kv(dk), self._kv(dv), self._ws, self._nws, self._status, self._on(stream)))
 
 
 class DecodeAttention(_TextOperator):
@@ -754,10 +768,10 @@ class DecodeAttention(_TextOperator):
         if b > self.max_batch:
             raise ValueError(f"batch of {b}, at most {self.max_batch}")
         cache = _cache(k_cache, v_cache, hkv, hd)
-        J.check(J.lib().jnx_op_decode_attention(
+        J.check(self._lib.jnx_op_decode_attention(
             C.byref(cache), b, h, hkv, hd, C.byref(_rows(q, b, h, hd)),
             _dense(slot, torch.int32, b), _dense(n_cached, torch.int32, b),
-            C.byref(_rows(out, b, h, hd)), self._ws, self._nws, self._status, _stream(stream)))
+            C.byref(_rows(out, b, h, hd)), self._ws, self._nws, self._status, self._on(stream)))
 
 
 class VocabLoss(_TextOperator):
@@ -787,9 +801,9 @@ class VocabLoss(_TextOperator):
              stream=None) -> None:
         """loss [n] fp32 of h [n, d]; 0 where targets [n] is negative."""
         n, *args = self._args(h, targets)
-        J.check(J.lib().jnx_op_vocab_loss(
+        J.check(self._lib.jnx_op_vocab_loss(
             *args, n, self.vocab, self.d, _dense(loss, torch.float32, n), self._ws, self._nws,
-            self._status, _stream(stream)))
+            self._status, self._on(stream)))
 
     def train(self, h: torch.Tensor, targets: torch.Tensor, row_weight: torch.Tensor,
               loss: torch.Tensor, dh: torch.Tensor, dw: Optional[torch.Tensor] = None,
@@ -804,7 +818,7 @@ class VocabLoss(_TextOperator):
         if dw is not None:
             _bf16(dw, self.vocab, self.d)
             grads[2:] = [dw.data_ptr(), dw.stride(0)]
-        J.check(J.lib().jnx_op_vocab_loss_train(
+        J.check(self._lib.jnx_op_vocab_loss_train(
             *args, _dense(row_weight, torch.float32, n), n, self.vocab, self.d, self.piece_rows,
             _dense(loss, torch.float32, n), *grads, self._ws, self._nws, self._status,
-            _stream(stream)))
+            self._on(stream)))

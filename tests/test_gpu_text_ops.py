@@ -501,6 +501,29 @@ def test_decode_attention_bits_do_not_depend_on_the_batch():
         assert torch.equal(alone[0], out[i])
 
 
+def test_decode_attention_batches_of_all_sizes_share_a_workspace():
+    """Large and small batches in turn on one object: what a call leaves behind is what the
+    next expects."""
+    heads, n = (8, 2, 128), [900, 30, 0, 2222, 513, 1300] * 20
+    h, hkv, hd = heads
+    g = gen(11)
+    kc, vc = normal(g, 6, 2300, hkv, hd), normal(g, 6, 2300, hkv, hd)
+    q = normal(g, len(n), h, hd)
+    slot = torch.arange(len(n), device="cuda", dtype=torch.int32) % 6
+    lens = torch.tensor(n, device="cuda", dtype=torch.int32)
+    op = _r().DecodeAttention(*heads, max_batch=len(n))
+    outs = []
+    for b in (120, 1, 120, 5, 33, 120):
+        out = empty(b, h, hd)
+        op.forward(q[:b], kc, vc, slot[:b], lens[:b], out)
+        outs.append(out)
+    op.check()
+    for out in outs:
+        assert torch.equal(out, outs[0][:out.shape[0]])
+    want = decode_want(q[:6], kc, vc, slot[:6], n[:6])
+    T.close(outs[0][:6], want["out"], want["out_tol"])
+
+
 def test_decode_matches_the_prompt():
     """A sequence's last row alone against its cache, and inside its prompt."""
     heads, n = (8, 2, 128), 777
