@@ -6,10 +6,11 @@
 // with dn = R^T dy the gradients are dgamma = sum dn x r over all rows and
 // dx = r (gamma dn) - x r^3 mean(gamma dn x).
 //
-// Bound by HBM: 4 bytes an element forward (6 backward).  hd / 16 lanes hold a row, each
-// 8 elements of either half (two 16-byte loads), so a pair meets in one lane and the
-// norm's sum is log2(hd / 16) shuffles.  The angles of a CTA's tokens are computed once
-// into shared memory and serve all of a token's heads.
+// Bound by HBM: 4 bytes an element forward (6 backward).  A lane holds E elements of
+// either half of a row, so a pair meets in one lane and the norm's sum is a few shuffles;
+// the rows of the next pass are under way while one is worked on.  The angles of a CTA's
+// tokens are computed once into shared memory and serve all of a token's heads, laid out
+// so that a row's lanes read neighbours (they were 4 to 8 ways in conflict as they come).
 //
 // An angle is taken modulo whole turns before it is rounded: the frequency is a 64-bit
 // fraction of a turn, so position times frequency in wrapping 64-bit integers is the
@@ -47,7 +48,8 @@ struct Args {
     int* status;
     // backward
     uint16_t* dqkv;
-    float* partial;  // [grid][2][hd]
+    int q_ctas;      // CTAs on query rows; the others take key rows
+    float* partial;  // [hd][grid]
     // frequency i as a 64-bit fraction of a turn, and its axis
     unsigned long long turn[MAX_HALF];
     unsigned char axis[MAX_HALF];
@@ -65,96 +67,152 @@ __device__ __forceinline__ float2 angle(const Args& a, int t, int i) {
     return cs;
 }
 
-__device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8]) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+// N bf16 elements (a multiple of 4) as loaded, and as floats.
+template <int N>
+struct Pack {
+    uint32_t w[N / 2];
+    __device__ __forceinline__ void load(const uint16_t* p) {
+        if constexpr (N == 8) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[0] = v.x, w[1] = v.y;
+        }
     }
-}
+    __device__ __forceinline__ void store(uint16_t* p) const {
+        if constexpr (N == 8)
+            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    }
+    // elements 2 i and 2 i + 1 as an fp32 pair
+    __device__ __forceinline__ uint64_t pair(int i) const {
+        return f2_pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    }
+    __device__ __forceinline__ void set(int i, uint64_t f) {
+        float a, b;
+        f2_unpack(f, a, b);
+        w[i] = pack_bf2(a, b);
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) w[i] = 0;
+    }
+};
 
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-    return make_uint4(pack_bf2(f[0], f[1]), pack_bf2(f[2], f[3]), pack_bf2(f[4], f[5]),
-                      pack_bf2(f[6], f[7]));
-}
-
-// Sum over the hd / 16 lanes of a row.
-template <int HD>
+// Sum over the LPR lanes of a row.
+template <int LPR>
 __device__ __forceinline__ float row_sum(float v) {
 #pragma unroll
-    for (int o = HD / 32; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = LPR / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-}  // namespace rope
 
-// Tokens a CTA takes: their angles are two a thread (one at hd = 64).
-template <int HD>
-struct RopeCfg {
-    static constexpr int TOK = HD == 64 ? 8 : HD == 128 ? 4 : 2;
-    static constexpr int LPR = HD / 16;                   // lanes a row
-    static constexpr int RPP = rope::THREADS / LPR;       // rows a pass
+// E: elements of either half a lane holds; TOK: tokens of a block.
+template <int HD, int E_, int TOK_>
+struct Cfg {
+    static constexpr int E = E_, TOK = TOK_;
+    static constexpr int LPR = HD / 2 / E;        // lanes a row
+    static constexpr int RPP = THREADS / LPR;     // rows a pass
+    // angles of TOK tokens from t0 on: [t][e][l] holds cos, cos, sin, sin of lane l's
+    // elements 2 e and 2 e + 1
+    static __device__ __forceinline__ void angles(const Args& a, int t0, int nt, float4* cs) {
+        float* at = reinterpret_cast<float*>(cs);
+        for (int i = threadIdx.x; i < nt * (HD / 2); i += THREADS) {
+            const int t = i / (HD / 2), f = i % (HD / 2);
+            const float2 v = angle(a, t0 + t, f);
+            float* to = at + ((t * (E / 2) + f % E / 2) * LPR + f / E) * 4 + (f & 1);
+            to[0] = v.x;
+            to[2] = v.y;
+        }
+    }
+    static __device__ __forceinline__ void read(const float4* cs, int t, int e, int l, uint64_t& c,
+                                                uint64_t& s) {
+        const float4 v = cs[(t * (E / 2) + e) * LPR + l];
+        c = f2_pack(v.x, v.y);
+        s = f2_pack(v.z, v.w);
+    }
 };
+template <int HD>
+using Forward = Cfg<HD, 8, HD == 64 ? 8 : HD == 128 ? 4 : 2>;
+template <int HD>
+using Backward = Cfg<HD, 4, HD == 64 ? 16 : HD == 128 ? 8 : 4>;
+}  // namespace rope
 
 template <int HD, bool APPEND>
 __global__ void __launch_bounds__(rope::THREADS)
     k_qk_norm_rope(const __grid_constant__ rope::Args a) {
-    using C = RopeCfg<HD>;
-    __shared__ float2 cs[C::TOK][HD / 2];
+    using C = rope::Forward<HD>;
+    constexpr int E = C::E;
+    __shared__ float4 cs[C::TOK * HD / 4];
     pdl_entry();
     const int t0 = blockIdx.x * C::TOK, nt = min(C::TOK, a.n_tokens - t0);
-    for (int i = threadIdx.x; i < nt * (HD / 2); i += rope::THREADS)
-        cs[i / (HD / 2)][i % (HD / 2)] = rope::angle(a, t0 + i / (HD / 2), i % (HD / 2));
-    __syncthreads();
     // rows of the CTA's tokens, token-major; an append's value heads come after the keys'
     const int heads = a.H + (APPEND ? 2 : 1) * a.Hkv;
-    const int part = threadIdx.x % C::LPR * 8;  // this lane's elements of each half
-    for (int r0 = 0; r0 < nt * heads; r0 += C::RPP) {
-        const int r = r0 + threadIdx.x / C::LPR;
-        const bool live = r < nt * heads;
-        const int t = live ? r / heads : 0, head = live ? r % heads : 0;
-        const size_t tok = t0 + t;
-        float lo[8] = {}, hi[8] = {};
-        uint4 ulo = make_uint4(0, 0, 0, 0), uhi = ulo;
-        if (live) {
-            const uint16_t* x = a.qkv + tok * a.ldqkv + (size_t)head * HD + part;
-            ulo = *reinterpret_cast<const uint4*>(x);
-            uhi = *reinterpret_cast<const uint4*>(x + HD / 2);
+    const int l = threadIdx.x % C::LPR, part = l * E;  // this lane's elements of each half
+    // (token, head) of this lane's row in a pass
+    int t = (threadIdx.x / C::LPR) / heads, head = (threadIdx.x / C::LPR) % heads;
+    rope::Pack<E> lo, hi, g[2][2];
+    auto load = [&]() {
+        lo.clear();
+        hi.clear();
+        if (t >= nt) return;
+        const uint16_t* x = a.qkv + (size_t)(t0 + t) * a.ldqkv + (size_t)head * HD + part;
+        lo.load(x);
+        hi.load(x + HD / 2);
+    };
+    load();
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+        if (const uint16_t* gamma = w ? a.gk : a.gq) {
+            g[w][0].load(gamma + part);
+            g[w][1].load(gamma + HD / 2 + part);
         }
-        rope::unpack8(ulo, lo);
-        rope::unpack8(uhi, hi);
-        const bool is_q = head < a.H, is_v = head >= a.H + a.Hkv;
-        const uint16_t* gamma = is_q ? a.gq : a.gk;
-        float ss = 0.f;
+    C::angles(a, t0, nt, cs);
+    __syncthreads();
+    for (int r0 = 0; r0 < nt * heads; r0 += C::RPP) {
+        const int tw = t, hw = head;
+        uint64_t x[E / 2], y[E / 2], ss2 = f2_pack(0.f, 0.f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss += lo[e] * lo[e] + hi[e] * hi[e];
-        ss = rope::row_sum<HD>(ss);
-        if (!live) continue;
+        for (int e = 0; e < E / 2; ++e) {
+            x[e] = lo.pair(e);
+            y[e] = hi.pair(e);
+            ss2 = f2_fma(x[e], x[e], ss2);
+            ss2 = f2_fma(y[e], y[e], ss2);
+        }
+        float s0, s1;
+        f2_unpack(ss2, s0, s1);
+        const rope::Pack<E> raw[2] = {lo, hi};
+        for (head += C::RPP; head >= heads; head -= heads) ++t;
+        load();  // the next pass's row
+        const float ss = rope::row_sum<C::LPR>(s0 + s1);
+        if (tw >= nt) continue;
+        const size_t tok = t0 + tw;
+        const bool is_q = hw < a.H, is_v = APPEND && hw >= a.H + a.Hkv;
+        rope::Pack<E> olo = raw[0], ohi = raw[1];
         if (!is_v) {
-            if (gamma) {
+            if (is_q ? a.gq : a.gk) {
                 const float s = rsqrtf(ss * (1.f / HD) + a.eps);
-                float gl[8], gh[8];
-                rope::unpack8(*reinterpret_cast<const uint4*>(gamma + part), gl);
-                rope::unpack8(*reinterpret_cast<const uint4*>(gamma + HD / 2 + part), gh);
+                const uint64_t sp = f2_pack(s, s);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    lo[e] *= s * gl[e];
-                    hi[e] *= s * gh[e];
+                for (int e = 0; e < E / 2; ++e) {
+                    x[e] = f2_mul(f2_mul(x[e], sp), (is_q ? g[0][0] : g[1][0]).pair(e));
+                    y[e] = f2_mul(f2_mul(y[e], sp), (is_q ? g[0][1] : g[1][1]).pair(e));
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float2 c = cs[t][part + e];
-                const float x = lo[e], y = hi[e];
-                lo[e] = x * c.x - y * c.y;
-                hi[e] = y * c.x + x * c.y;
+            for (int e = 0; e < E / 2; ++e) {
+                uint64_t c, s;
+                C::read(cs, tw, e, l, c, s);
+                const uint64_t ns = s ^ 0x8000000080000000ull;
+                olo.set(e, f2_fma(x[e], c, f2_mul(y[e], ns)));
+                ohi.set(e, f2_fma(y[e], c, f2_mul(x[e], s)));
             }
-            ulo = rope::pack8(lo);
-            uhi = rope::pack8(hi);
         }
         uint16_t* o;
         if (is_q) {
-            o = a.q + tok * a.q_row + head * a.q_head;
+            o = a.q + tok * a.q_row + hw * a.q_head;
         } else if (APPEND) {
             const int slot = a.slot[tok], at = a.at[tok];
             if (slot < 0 || slot >= a.n_slots || at < 0 || at >= a.room) {
@@ -162,130 +220,142 @@ __global__ void __launch_bounds__(rope::THREADS)
                 continue;
             }
             o = (is_v ? a.v : a.k) + slot * a.slot_stride + at * a.k_row +
-                (head - a.H - (is_v ? a.Hkv : 0)) * a.k_head;
+                (hw - a.H - (is_v ? a.Hkv : 0)) * a.k_head;
         } else {
-            o = a.k + tok * a.k_row + (head - a.H) * a.k_head;
+            o = a.k + tok * a.k_row + (hw - a.H) * a.k_head;
         }
-        *reinterpret_cast<uint4*>(o + part) = ulo;
-        *reinterpret_cast<uint4*>(o + HD / 2 + part) = uhi;
+        olo.store(o + part);
+        ohi.store(o + HD / 2 + part);
     }
 }
 
-// Gradients.  A CTA walks blocks of TOK tokens; the gains' gradients stay in its lanes'
-// registers, query heads' and key heads' rows apart, and are added over the CTA's rows
-// in a fixed order at the end.
+// Gradients.  A CTA takes query rows or key rows, blocks of TOK tokens in turn; their
+// gains' gradients stay in its lanes' registers and are added over its rows in a fixed
+// order at the end.
 template <int HD>
-__global__ void __launch_bounds__(rope::THREADS)
+__global__ void __launch_bounds__(rope::THREADS, 4)
     k_qk_norm_rope_bwd(const __grid_constant__ rope::Args a) {
-    using C = RopeCfg<HD>;
-    __shared__ float2 cs[C::TOK][HD / 2];
+    using C = rope::Backward<HD>;
+    constexpr int E = C::E;
+    __shared__ float4 cs[C::TOK * HD / 4];
     __shared__ float sums[C::RPP][HD];
     pdl_entry();
-    const int heads = a.H + a.Hkv;
-    const int part = threadIdx.x % C::LPR * 8, lane_row = threadIdx.x / C::LPR;
-    float gacc[2][16] = {};
-    for (int t0 = blockIdx.x * C::TOK; t0 < a.n_tokens; t0 += gridDim.x * C::TOK) {
+    const bool is_q = (int)blockIdx.x < a.q_ctas;
+    const int heads = is_q ? a.H : a.Hkv, first = is_q ? 0 : a.H;
+    const int part_cta = is_q ? blockIdx.x : blockIdx.x - a.q_ctas;
+    const int ctas = is_q ? a.q_ctas : gridDim.x - a.q_ctas;
+    const uint16_t* dy = is_q ? a.q : a.k;
+    const long long dy_row = is_q ? a.q_row : a.k_row, dy_head = is_q ? a.q_head : a.k_head;
+    const uint16_t* gamma = is_q ? a.gq : a.gk;
+    const int l = threadIdx.x % C::LPR, part = l * E, lane_row = threadIdx.x / C::LPR;
+    uint64_t gain[E] = {}, gacc[E] = {};
+    if (gamma) {
+        rope::Pack<E> gl, gh;
+        gl.load(gamma + part);
+        gh.load(gamma + HD / 2 + part);
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) {
+            gain[e] = gl.pair(e);
+            gain[E / 2 + e] = gh.pair(e);
+        }
+    }
+    for (int t0 = part_cta * C::TOK; heads > 0 && t0 < a.n_tokens; t0 += ctas * C::TOK) {
         const int nt = min(C::TOK, a.n_tokens - t0);
-        __syncthreads();
-        for (int i = threadIdx.x; i < nt * (HD / 2); i += rope::THREADS)
-            cs[i / (HD / 2)][i % (HD / 2)] = rope::angle(a, t0 + i / (HD / 2), i % (HD / 2));
+        int t = lane_row / heads, head = lane_row % heads;
+        rope::Pack<E> xl, xh, yl, yh;
+        auto load = [&]() {
+            xl.clear(), xh.clear(), yl.clear(), yh.clear();
+            if (t >= nt) return;
+            const uint16_t* x = a.qkv + (size_t)(t0 + t) * a.ldqkv + (size_t)(first + head) * HD + part;
+            const uint16_t* y = dy + (t0 + t) * dy_row + head * dy_head + part;
+            xl.load(x);
+            xh.load(x + HD / 2);
+            yl.load(y);
+            yh.load(y + HD / 2);
+        };
+        load();
+        __syncthreads();  // the last block's angles have been read
+        C::angles(a, t0, nt, cs);
         __syncthreads();
         for (int r0 = 0; r0 < nt * heads; r0 += C::RPP) {
-            const int r = r0 + lane_row;
-            const bool live = r < nt * heads;
-            const int t = live ? r / heads : 0, head = live ? r % heads : 0;
-            const size_t tok = t0 + t;
-            const bool is_q = head < a.H;
-            uint4 xl = make_uint4(0, 0, 0, 0), xh = xl, yl = xl, yh = xl;
-            if (live) {
-                const uint16_t* x = a.qkv + tok * a.ldqkv + (size_t)head * HD + part;
-                const uint16_t* dy = is_q ? a.q + tok * a.q_row + head * a.q_head
-                                          : a.k + tok * a.k_row + (head - a.H) * a.k_head;
-                xl = *reinterpret_cast<const uint4*>(x);
-                xh = *reinterpret_cast<const uint4*>(x + HD / 2);
-                yl = *reinterpret_cast<const uint4*>(dy + part);
-                yh = *reinterpret_cast<const uint4*>(dy + HD / 2 + part);
-            }
-            float lo[8], hi[8], dl[8], dh[8];
-            rope::unpack8(xl, lo);
-            rope::unpack8(xh, hi);
-            rope::unpack8(yl, dl);
-            rope::unpack8(yh, dh);
+            const int tw = t, hw = head;
+            uint64_t x[E], d[E];  // pairs of the lower half, then of the upper
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {  // back by the same angle
-                const float2 c = cs[t][part + e];
-                const float x = dl[e], y = dh[e];
-                dl[e] = x * c.x + y * c.y;
-                dh[e] = y * c.x - x * c.y;
+            for (int e = 0; e < E / 2; ++e) {
+                uint64_t c, s;
+                C::read(cs, min(tw, nt - 1), e, l, c, s);
+                const uint64_t ns = s ^ 0x8000000080000000ull, u = yl.pair(e), v = yh.pair(e);
+                x[e] = xl.pair(e);
+                x[E / 2 + e] = xh.pair(e);
+                d[e] = f2_fma(u, c, f2_mul(v, s));  // back by the same angle
+                d[E / 2 + e] = f2_fma(v, c, f2_mul(u, ns));
             }
-            const uint16_t* gamma = is_q ? a.gq : a.gk;
-            float ss = 0.f, dot = 0.f, gl[8] = {}, gh[8] = {};
+            for (head += C::RPP; head >= heads; head -= heads) ++t;
+            load();  // the next pass's row
+            uint16_t* o = a.dqkv + (size_t)(t0 + tw) * a.ldqkv + (size_t)(first + hw) * HD + part;
             if (gamma) {
-                rope::unpack8(*reinterpret_cast<const uint4*>(gamma + part), gl);
-                rope::unpack8(*reinterpret_cast<const uint4*>(gamma + HD / 2 + part), gh);
-            }
+                uint64_t ss2 = f2_pack(0.f, 0.f), dot2 = ss2, dx[E];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ss += lo[e] * lo[e] + hi[e] * hi[e];
-                dot += gl[e] * dl[e] * lo[e] + gh[e] * dh[e] * hi[e];
-            }
-            ss = rope::row_sum<HD>(ss);
-            dot = rope::row_sum<HD>(dot);
-            if (!live) continue;
-            if (gamma) {
-                const float s = rsqrtf(ss * (1.f / HD) + a.eps);
-                const float m = dot * (1.f / HD) * s * s * s;
+                for (int e = 0; e < E; ++e) {
+                    dx[e] = f2_mul(d[e], x[e]);
+                    ss2 = f2_fma(x[e], x[e], ss2);
+                    dot2 = f2_fma(gain[e], dx[e], dot2);
+                }
+                float s0, s1, d0, d1;
+                f2_unpack(ss2, s0, s1);
+                f2_unpack(dot2, d0, d1);
+                const float ss = rope::row_sum<C::LPR>(s0 + s1), dot = rope::row_sum<C::LPR>(d0 + d1);
+                const float s = tw < nt ? rsqrtf(ss * (1.f / HD) + a.eps) : 0.f;
+                const float m = -dot * (1.f / HD) * s * s * s;
+                const uint64_t sp = f2_pack(s, s), mp = f2_pack(m, m);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float vl = dl[e] * lo[e] * s, vh = dh[e] * hi[e] * s;
-                    if (is_q) {
-                        gacc[0][e] += vl;
-                        gacc[0][8 + e] += vh;
-                    } else {
-                        gacc[1][e] += vl;
-                        gacc[1][8 + e] += vh;
-                    }
-                    dl[e] = s * gl[e] * dl[e] - lo[e] * m;
-                    dh[e] = s * gh[e] * dh[e] - hi[e] * m;
+                for (int e = 0; e < E; ++e) {  // a lane without a row adds zeros
+                    gacc[e] = f2_fma(dx[e], sp, gacc[e]);
+                    d[e] = f2_fma(f2_mul(gain[e], sp), d[e], f2_mul(x[e], mp));
                 }
             }
-            uint16_t* o = a.dqkv + tok * a.ldqkv + (size_t)head * HD + part;
-            *reinterpret_cast<uint4*>(o) = rope::pack8(dl);
-            *reinterpret_cast<uint4*>(o + HD / 2) = rope::pack8(dh);
+            if (tw < nt) {
+                rope::Pack<E> ol, oh;
+#pragma unroll
+                for (int e = 0; e < E / 2; ++e) {
+                    ol.set(e, d[e]);
+                    oh.set(e, d[E / 2 + e]);
+                }
+                ol.store(o);
+                oh.store(o + HD / 2);
+            }
         }
     }
     if (!a.partial) return;
-    for (int w = 0; w < 2; ++w) {
-        __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            sums[lane_row][part + e] = gacc[w][e];
-            sums[lane_row][HD / 2 + part + e] = gacc[w][8 + e];
-        }
-        __syncthreads();
-        for (int c = threadIdx.x; c < HD; c += rope::THREADS) {
-            float s = 0.f;
-            for (int r = 0; r < C::RPP; ++r) s += sums[r][c];
-            a.partial[((size_t)blockIdx.x * 2 + w) * HD + c] = s;
-        }
+    for (int e = 0; e < E / 2; ++e) {
+        float* to = &sums[lane_row][part + 2 * e];
+        f2_unpack(gacc[e], to[0], to[1]);
+        f2_unpack(gacc[E / 2 + e], to[HD / 2], to[HD / 2 + 1]);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < HD; c += rope::THREADS) {
+        float s = 0.f;
+        for (int r = 0; r < C::RPP; ++r) s += sums[r][c];
+        a.partial[(size_t)c * gridDim.x + blockIdx.x] = s;
     }
 }
 
 // dgamma = sum of the CTAs' parts, each column's in a fixed order: 32 lanes take the
-// parts in turn, then add up.  One warp a column.
+// parts in turn, then add up.  A warp a column of the queries' or the keys' gains.
 __global__ void __launch_bounds__(256)
-    k_qk_gain_sum(const float* partial, int parts, int hd, float* dgq, float* dgk) {
+    k_qk_gain_sum(const float* partial, int q_ctas, int ctas, int hd, float* dgq, float* dgk) {
     pdl_entry();
-    const int c = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (c >= 2 * hd) return;
+    const int w = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (w >= 2 * hd) return;
+    const int c = w < hd ? w : w - hd, from = w < hd ? 0 : q_ctas, to = w < hd ? q_ctas : ctas;
     float s = 0.f;
-    for (int i = lane; i < parts; i += 32) s += partial[(size_t)i * 2 * hd + c];
+#pragma unroll 4
+    for (int i = from + lane; i < to; i += 32) s += partial[(size_t)c * ctas + i];
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) {
-        if (c < hd && dgq) dgq[c] = s;
-        if (c >= hd && dgk) dgk[c - hd] = s;
-    }
+    float* out = w < hd ? dgq : dgk;
+    if (lane == 0 && out) out[c] = s;
 }
 
 static jnx_status rope_args(const jnx_qk_rope* p, const uint16_t* qkv, int64_t ldqkv,
@@ -334,24 +404,31 @@ static jnx_status rope_args(const jnx_qk_rope* p, const uint16_t* qkv, int64_t l
     return JNX_OK;
 }
 
+template <int HD, bool APPEND>
+static void launch_rope_hd(const rope::Args& a, cudaStream_t s) {
+    constexpr int TOK = rope::Forward<HD>::TOK;
+    pdl(k_qk_norm_rope<HD, APPEND>, (a.n_tokens + TOK - 1) / TOK, rope::THREADS, 0, s)(a);
+}
+
 template <bool APPEND>
 static jnx_status launch_rope(const rope::Args& a, int hd, const char* what, cudaStream_t s) {
-    const int tok = hd == 64 ? RopeCfg<64>::TOK : hd == 128 ? RopeCfg<128>::TOK : RopeCfg<256>::TOK;
-    const int grid = (a.n_tokens + tok - 1) / tok;
+    if (!a.H && !a.Hkv) return JNX_OK;
     TraceScope ts(JNX_K_QK_ROPE, 0.0, s);
-    if (hd == 64)
-        pdl(k_qk_norm_rope<64, APPEND>, grid, rope::THREADS, 0, s)(a);
-    else if (hd == 128)
-        pdl(k_qk_norm_rope<128, APPEND>, grid, rope::THREADS, 0, s)(a);
-    else
-        pdl(k_qk_norm_rope<256, APPEND>, grid, rope::THREADS, 0, s)(a);
+    if (hd == 64) launch_rope_hd<64, APPEND>(a, s);
+    else if (hd == 128) launch_rope_hd<128, APPEND>(a, s);
+    else launch_rope_hd<256, APPEND>(a, s);
     return launched(what);
 }
 
-// CTAs of the gradient kernel: what the SMs hold at once, or one a block of tokens.
-static int rope_bwd_grid(int hd, int n_tokens) {
-    const int tok = hd == 64 ? RopeCfg<64>::TOK : hd == 128 ? RopeCfg<128>::TOK : RopeCfg<256>::TOK;
-    return std::max(1, std::min((n_tokens + tok - 1) / tok, 152 * 3));
+// CTAs of the gradient kernel, at most what 152 SMs hold at once, shared out by rows;
+// each kind has one at least.
+static int rope_bwd_grid(const jnx_qk_rope* p, int n_tokens, int& q_ctas) {
+    const int hd = p->head_dim, h = p->n_heads, hkv = p->n_kv_heads;
+    const int tok = hd == 64 ? rope::Backward<64>::TOK
+                             : hd == 128 ? rope::Backward<128>::TOK : rope::Backward<256>::TOK;
+    const int blocks = std::max(1, (n_tokens + tok - 1) / tok), most = 152 * 4;
+    q_ctas = std::min(blocks, std::max(1, (int)((long long)most * h / std::max(1, h + hkv))));
+    return q_ctas + std::min(blocks, std::max(1, most - q_ctas));
 }
 
 }  // namespace jnx
@@ -402,8 +479,9 @@ extern "C" jnx_status jnx_op_qk_norm_rope_append(const jnx_qk_rope* p, const uin
 
 extern "C" size_t jnx_op_qk_norm_rope_backward_workspace_bytes(const jnx_qk_rope* p,
                                                                int32_t n_tokens) {
-    if (!p || n_tokens < 0 || p->head_dim <= 0) return 0;
-    return (size_t)rope_bwd_grid(p->head_dim, n_tokens) * 2 * p->head_dim * sizeof(float);
+    if (!p || n_tokens < 0 || p->head_dim <= 0 || p->n_heads < 0 || p->n_kv_heads < 0) return 0;
+    int q_ctas;
+    return (size_t)rope_bwd_grid(p, n_tokens, q_ctas) * p->head_dim * sizeof(float);
 }
 
 extern "C" jnx_status jnx_op_qk_norm_rope_backward(const jnx_qk_rope* p, const uint16_t* qkv,
@@ -436,16 +514,14 @@ extern "C" jnx_status jnx_op_qk_norm_rope_backward(const jnx_qk_rope* p, const u
     if (a.Hkv) a.k = dk->ptr, a.k_row = dk->row_stride, a.k_head = dk->head_stride;
     a.dqkv = dqkv;
     a.partial = gains ? static_cast<float*>(workspace) : nullptr;
-    const int grid = rope_bwd_grid(hd, n_tokens);
+    const int grid = rope_bwd_grid(p, n_tokens, a.q_ctas);
     TraceScope ts(JNX_K_QK_ROPE, 0.0, s);
-    if (hd == 64)
-        pdl(k_qk_norm_rope_bwd<64>, grid, rope::THREADS, 0, s)(a);
-    else if (hd == 128)
-        pdl(k_qk_norm_rope_bwd<128>, grid, rope::THREADS, 0, s)(a);
-    else
-        pdl(k_qk_norm_rope_bwd<256>, grid, rope::THREADS, 0, s)(a);
+    if (hd == 64) pdl(k_qk_norm_rope_bwd<64>, grid, rope::THREADS, 0, s)(a);
+    else if (hd == 128) pdl(k_qk_norm_rope_bwd<128>, grid, rope::THREADS, 0, s)(a);
+    else pdl(k_qk_norm_rope_bwd<256>, grid, rope::THREADS, 0, s)(a);
     if (gains)
-        pdl(k_qk_gain_sum, (2 * hd + 7) / 8, 256, 0, s)(a.partial, grid, hd, a.gq ? dgamma_q : nullptr,
+        pdl(k_qk_gain_sum, (2 * hd + 7) / 8, 256, 0, s)(a.partial, a.q_ctas, grid, hd,
+                                                       a.gq ? dgamma_q : nullptr,
                                                        a.gk ? dgamma_k : nullptr);
     return launched("qk norm rope backward");
 }
