@@ -253,10 +253,10 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
             }
 #pragma unroll
             for (int t = 0; t < TILE / 16; ++t) {
-                const uint32_t p0 = pack_bf2(sc[2 * t][0], sc[2 * t][1]);
-                const uint32_t p1 = pack_bf2(sc[2 * t][2], sc[2 * t][3]);
-                const uint32_t p2 = pack_bf2(sc[2 * t + 1][0], sc[2 * t + 1][1]);
-                const uint32_t p3 = pack_bf2(sc[2 * t + 1][2], sc[2 * t + 1][3]);
+                const uint32_t p0 = cvt_bf2(sc[2 * t][0], sc[2 * t][1]);
+                const uint32_t p1 = cvt_bf2(sc[2 * t][2], sc[2 * t][3]);
+                const uint32_t p2 = cvt_bf2(sc[2 * t + 1][0], sc[2 * t + 1][1]);
+                const uint32_t p3 = cvt_bf2(sc[2 * t + 1][2], sc[2 * t + 1][3]);
 #pragma unroll
                 for (int c = 0; c < HD / 16; ++c) {
                     const int r = t * 16 + (lane & 15);
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
 #pragma unroll
                 for (int c = 0; c < HD / 8; ++c)
                     *reinterpret_cast<uint32_t*>(dst + c * 8) =
-                        pack_bf2(o[c][2 * i] * inv, o[c][2 * i + 1] * inv);
+                        cvt_bf2(o[c][2 * i] * inv, o[c][2 * i + 1] * inv);
             } else {
                 float* dst = a.part + (((size_t)x.b * a.H + h) * MAX_RUNS + x.run) * (HD + 2);
 #pragma unroll
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(128) k_decode_join(const __grid_constant__ Dec
     uint16_t* o = a.out + b * a.o_row + h * a.o_head + lane * 2;
 #pragma unroll
     for (int e = 0; e < E; e += 2)
-        *reinterpret_cast<uint32_t*>(o + e * 32) = pack_bf2(acc[e] * inv, acc[e + 1] * inv);
+        *reinterpret_cast<uint32_t*>(o + e * 32) = cvt_bf2(acc[e] * inv, acc[e + 1] * inv);
 }
 
 template <int HD>

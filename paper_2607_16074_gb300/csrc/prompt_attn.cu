@@ -189,11 +189,11 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             const PromptWork x = prompt_uniform(nxt);
             nxt = prompt_fetch(a, r + 1);
             if (!x.valid) continue;
-            int n = 0;
+            const int n = max(x.key_tiles(0, T), NST == 2 ? x.key_tiles(1, T) : 0);
+            // the first keys do not wait for the last item's Q tiles to be free
+            if (n > 0) ok = load_tile(false, x, 0);
             for (int t = 0; t < NST && ok; ++t) {
-                const int nt = x.key_tiles(t, T);
-                n = max(n, nt);
-                if (nt == 0) continue;
+                if (x.key_tiles(t, T) == 0) continue;
                 if (nq[t] > 0 && !(ok = mbar_wait_warp(&bar[Q_EMPTY + t], (nq[t] - 1) & 1))) break;
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&bar[Q_FULL + t], qbytes);
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             }
             // K runs ahead of V by as many tiles as S runs ahead of PV
             constexpr int AHEAD = NST == 1 ? 2 : 1;
-            for (int kt = 0; kt < AHEAD && kt < n && ok; ++kt) ok = load_tile(false, x, kt);
+            for (int kt = 1; kt < AHEAD && kt < n && ok; ++kt) ok = load_tile(false, x, kt);
             for (int kt = 0; kt < n && ok; ++kt) {
                 ok = load_tile(true, x, kt);
                 if (ok && kt + AHEAD < n) ok = load_tile(false, x, kt + AHEAD);
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                             p0 = ex2_approx(x0);
                             p1 = ex2_approx(x1);
                             rs[(e >> 1) & 1] = f2_add(rs[(e >> 1) & 1], f2_pack(p0, p1));
-                            pk[c * 16 + e / 2] = pack_bf2(p0, p1);
+                            pk[c * 16 + e / 2] = cvt_bf2(p0, p1);
                         }
                     tmem_st32(tS + h * 32, pk);
                 }
@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             // a row without keys: O holds products of zeros
-                            qp[e] = l > 0.f ? pack_bf2(__uint_as_float(w[8 * j + 2 * e]) * inv,
+                            qp[e] = l > 0.f ? cvt_bf2(__uint_as_float(w[8 * j + 2 * e]) * inv,
                                                        __uint_as_float(w[8 * j + 2 * e + 1]) * inv)
                                             : 0u;
                         *reinterpret_cast<uint4*>(o + c * 32 + j * 8) = q;

@@ -476,7 +476,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 if (KP) {
                     uint32_t pk[32];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) pk[e] = pack_bf2(pr[2 * e], pr[2 * e + 1]);
+                    for (int e = 0; e < 32; ++e) pk[e] = cvt_bf2(pr[2 * e], pr[2 * e + 1]);
                     tmem_st32(tS, pk);
                     tmem_st_wait();
                 }
@@ -504,8 +504,8 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                             // V beyond the sequence's keys may be NaN
                             if (!KP && !whole && pr[c * 32 + e + u] == 0.f) v[u] = 0.f;
                         }
-                        dk[c * 16 + e / 2] = pack_bf2(v[0], v[1]);
-                        dk[c * 16 + e / 2 + 1] = pack_bf2(v[2], v[3]);
+                        dk[c * 16 + e / 2] = cvt_bf2(v[0], v[1]);
+                        dk[c * 16 + e / 2 + 1] = cvt_bf2(v[2], v[3]);
                     }
                 }
                 tmem_st32(tP, dk);
@@ -551,10 +551,10 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             *reinterpret_cast<uint4*>(o + c * 32 + e * 8) = make_uint4(
-                                pack_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
-                                pack_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
-                                pack_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
-                                pack_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
+                                cvt_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
+                                cvt_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
+                                cvt_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
+                                cvt_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
                     }
                 }
             }
@@ -1060,8 +1060,8 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                             if (hidden) v[u] = 0.f;
                         }
                     }
-                    pk[e / 2] = pack_bf2(v[0], v[1]);
-                    pk[e / 2 + 1] = pack_bf2(v[2], v[3]);
+                    pk[e / 2] = cvt_bf2(v[0], v[1]);
+                    pk[e / 2 + 1] = cvt_bf2(v[2], v[3]);
                 }
                 tmem_st16(tS, pk);
                 tmem_st_wait();
@@ -1103,10 +1103,10 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         *reinterpret_cast<uint4*>(o + c * 32 + e * 8) = make_uint4(
-                            pack_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
-                            pack_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
-                            pack_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
-                            pack_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
+                            cvt_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
+                            cvt_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
+                            cvt_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
+                            cvt_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
                 }
             }
             if (n > 0) {

@@ -93,7 +93,7 @@ struct Pack {
     __device__ __forceinline__ void set(int i, uint64_t f) {
         float a, b;
         f2_unpack(f, a, b);
-        w[i] = pack_bf2(a, b);
+        w[i] = cvt_bf2(a, b);
     }
     __device__ __forceinline__ void clear() {
 #pragma unroll

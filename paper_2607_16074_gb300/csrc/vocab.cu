@@ -347,7 +347,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                             if (at_col >= cols) x0 = 0.f;
                             if (at_col + 1 >= cols) x1 = 0.f;
                             s += x0 + x1;
-                            pk[d * 16 + e / 2] = pack_bf2(x0, x1);
+                            pk[d * 16 + e / 2] = cvt_bf2(x0, x1);
                         }
                     }
                     if (p.G)
@@ -399,7 +399,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                             }
                             if (p.last)
                                 *reinterpret_cast<uint2*>(p.out + o / N * p.ldo + o % N) =
-                                    make_uint2(pack_bf2(w.x, w.y), pack_bf2(w.z, w.w));
+                                    make_uint2(cvt_bf2(w.x, w.y), cvt_bf2(w.z, w.w));
                             else
                                 *at = w;
                         });
@@ -417,7 +417,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
 #pragma unroll
                         for (int e = 0; e < 32; e += 2)
                             pk[d * 16 + e / 2] =
-                                summed ? pack_bf2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]))
+                                summed ? cvt_bf2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]))
                                        : 0u;
                     }
                     const int col = col0 + c * 64;
@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(256)
             float a = f * __uint_as_float(v[e] << 16), b = f * __uint_as_float(v[e] & 0xffff0000u);
             if (hit && (t & 7) == 2 * e) a = w * expm1f(-ls);
             if (hit && (t & 7) == 2 * e + 1) b = w * expm1f(-ls);
-            v[e] = pack_bf2(a, b);
+            v[e] = cvt_bf2(a, b);
         }
         *reinterpret_cast<uint4*>(g + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
@@ -582,7 +582,7 @@ __global__ void __launch_bounds__(256)
                 p.acc + ((size_t)k * p.rows_max + r) * p.d + c);
             s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
         }
-        *reinterpret_cast<uint2*>(o + c) = make_uint2(pack_bf2(s.x, s.y), pack_bf2(s.z, s.w));
+        *reinterpret_cast<uint2*>(o + c) = make_uint2(cvt_bf2(s.x, s.y), cvt_bf2(s.z, s.w));
     }
 }
 
