@@ -19,6 +19,7 @@
 //   warp 1       MMA issuer.  Two tiles: S of a tile overwrites its P once PV is issued
 //                and the other tile's products run while this one's softmax does.  One
 //                tile (head dim 256): two score buffers, S two key tiles ahead of PV.
+//   warp 3       hands out the items, looked up ahead
 //   warps 4-     softmax and epilogue, a warpgroup a tile, a thread a row: the row's 128
 //                scores are in registers, so no row quantity is exchanged
 // P (bf16) overwrites the first 64 columns of its scores and is the TMEM A operand of
@@ -39,11 +40,13 @@ namespace jnx {
 namespace pattn {
 constexpr int BM = 128, BN = 128;
 constexpr int UNIT = 16384;  // bytes of a ring unit
-constexpr int RING = 10;
+constexpr int RING = 9;
+constexpr int STAGE = 2048;  // epilogue staging of a softmax warp: 32 rows x 32 columns
 constexpr float kLazy = 8.0f;  // log2 growth of the maximum that moves it
 // barriers: ring full / empty, then
-enum { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_FULL = 6, PV_DONE = 8, O_FULL = 10, O_FREE = 12,
-       DRAIN = 14, N_BARS = 15 };
+enum { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_HALF = 6, P_FULL = 8, O_FREE = 10, PV_DONE = 12,
+       O_FULL = 14, DRAIN = 16, W_FULL = 17, W_EMPTY = 20, N_BARS = 23 };
+constexpr int ITEMS = 3;  // items handed out at a time
 }  // namespace pattn
 
 template <int HD>
@@ -53,8 +56,9 @@ struct PromptCfg {
     static constexpr int VKEYS = pattn::BN / NU;   // keys of a V unit
     static constexpr int QB = pattn::BM * HD * 2;
     static constexpr int OFF_RING = NST * QB;
-    static constexpr int OFF_BAR = OFF_RING + pattn::RING * pattn::UNIT;
-    static constexpr int SMEM = OFF_BAR + (2 * pattn::RING + pattn::N_BARS) * 8 + 16 + 1024;
+    static constexpr int OFF_STG = OFF_RING + pattn::RING * pattn::UNIT;
+    static constexpr int OFF_BAR = OFF_STG + 4 * NST * pattn::STAGE;
+    static constexpr int SMEM = OFF_BAR + (2 * pattn::RING + pattn::N_BARS) * 8 + 16 + pattn::ITEMS * 32 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
     static constexpr int THREADS = 128 + 128 * NST;
     static constexpr uint32_t O_COL = 256;
@@ -73,8 +77,7 @@ struct PromptArgs {
 
 // One item: rows from token i0 of a sequence (global row q0 + i0) over its keys.
 struct PromptWork {
-    int q0, i0, Lq, k0, Lk, pre, kvh;
-    bool valid;
+    int q0, i0, Lq, k0, Lk, pre, kvh;  // i0 < 0: no more
 
     // key tiles that row tile t (T tokens) visits
     __device__ __forceinline__ int key_tiles(int t, int T) const {
@@ -83,35 +86,6 @@ struct PromptWork {
         return (keys_seen(min(a + T, Lq) - 1, Lq, Lk, pre) + pattn::BN - 1) / pattn::BN;
     }
 };
-
-__device__ __forceinline__ PromptWork prompt_fetch(const PromptArgs& a, int round) {
-    const int G = gridDim.x, b = blockIdx.x;
-    const int w = round * G + ((round & 1) ? G - 1 - b : b);
-    PromptWork x{0, 0, 0, 0, 0, 0, 0, false};
-    if (w >= a.n_work) return x;
-    const int2 it = a.items[w / a.Hkv];
-    x.kvh = w % a.Hkv;
-    x.i0 = it.y;
-    x.q0 = a.cu_q[it.x];
-    x.Lq = a.cu_q[it.x + 1] - x.q0;
-    x.k0 = a.cu_kv[it.x];
-    x.Lk = a.cu_kv[it.x + 1] - x.k0;
-    x.pre = a.prefix ? a.prefix[it.x] : 0;
-    x.valid = true;
-    return x;
-}
-
-__device__ __forceinline__ PromptWork prompt_uniform(PromptWork x) {
-    x.q0 = warp_uniform(x.q0);
-    x.i0 = warp_uniform(x.i0);
-    x.Lq = warp_uniform(x.Lq);
-    x.k0 = warp_uniform(x.k0);
-    x.Lk = warp_uniform(x.Lk);
-    x.pre = warp_uniform(x.pre);
-    x.kvh = warp_uniform(x.kvh);
-    x.valid = warp_uniform(x.valid);
-    return x;
-}
 
 template <int HD>
 __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
@@ -135,8 +109,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2 * RING; ++i) mbar_init(&full[i], 1);
         for (int i = 0; i < N_BARS; ++i)
-            mbar_init(&bar[i], i == P_FULL || i == P_FULL + 1 || i == O_FREE || i == O_FREE + 1 ? BM
-                                                                                              : 1);
+            mbar_init(&bar[i], i >= P_HALF && i < PV_DONE ? BM : i >= W_EMPTY ? 2 + 4 * NST : 1);
         *fail_flag = 0;
         fence_barrier_init();
         fence_proxy_async();
@@ -150,7 +123,23 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tbase = warp_uniform(*tmem_slot);
-    const int rounds = (a.n_work + gridDim.x - 1) / gridDim.x;
+    volatile int* slots = fail_flag + 1;  // [ITEMS][8]
+    // the next item as warp 3 hands it out; done() gives its slot back
+    int seen = 0;
+    auto next_item = [&](bool& ok) -> PromptWork {
+        const int b = seen % ITEMS;
+        if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen / ITEMS) & 1)))
+            return PromptWork{0, -1, 0, 0, 0, 0, 0};
+        const volatile int* s = slots + 8 * b;
+        return PromptWork{warp_uniform(s[0]), warp_uniform(s[1]), warp_uniform(s[2]), warp_uniform(s[3]),
+                          warp_uniform(s[4]), warp_uniform(s[5]), warp_uniform(s[6])};
+    };
+    auto item_done = [&]() {
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&bar[W_EMPTY + seen % ITEMS]);
+        __syncwarp();
+        ++seen;
+    };
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
@@ -184,11 +173,10 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             }
             return true;
         };
-        PromptWork nxt = prompt_fetch(a, 0);
-        for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
-            const PromptWork x = prompt_uniform(nxt);
-            nxt = prompt_fetch(a, r + 1);
-            if (!x.valid) continue;
+        while (ok) {
+            const PromptWork x = next_item(ok);
+            if (!ok || x.i0 < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            item_done();
             const int n = max(x.key_tiles(0, T), NST == 2 ? x.key_tiles(1, T) : 0);
             // the first keys do not wait for the last item's Q tiles to be free
             if (n > 0) ok = load_tile(false, x, 0);
@@ -262,15 +250,16 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             __syncwarp();
             issued = true;
         };
-        // O (columns d) += P (columns p) times the V tile in units [first, first + NU)
-        auto issue_pv = [&](uint32_t p, uint32_t first, uint32_t d, bool accumulate) {
+        // O (columns d) += P (columns p) times half h of the V tile in units [first, first + NU)
+        auto issue_pv = [&](int h, uint32_t p, uint32_t first, uint32_t d, bool accumulate) {
             if (elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < BN / 16; ++ks) {
+                for (int k = 0; k < BN / 32; ++k) {
+                    const int ks = h * (BN / 32) + k;
                     const int un = ks * 16 / C::VKEYS, off = ks * 16 % C::VKEYS;
                     const uint32_t va = smem_u32(ring) + ((first + un) % RING) * UNIT + off * 128;
                     tc_mma_f16_ts(d, p + ks * 8, sw128_desc_mn(va, C::VKEYS * 128, 1024), IDESC_PV,
-                                  accumulate || ks > 0);
+                                  accumulate || k > 0);
                 }
             }
             __syncwarp();
@@ -286,11 +275,10 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             fence_proxy_async();
             __syncwarp();
         };
-        PromptWork nxt = prompt_fetch(a, 0);
-        for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
-            const PromptWork x = prompt_uniform(nxt);
-            nxt = prompt_fetch(a, r + 1);
-            if (!x.valid) continue;
+        while (ok) {
+            const PromptWork x = next_item(ok);
+            if (!ok || x.i0 < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            item_done();
             int nt[2] = {x.key_tiles(0, T), NST == 2 ? x.key_tiles(1, T) : 0};
             const int n = max(nt[0], nt[1]);
             if (n == 0) continue;
@@ -314,8 +302,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                     bool have_v = false, have_k = false;
                     for (int t = 0; t < 2; ++t) {
                         if (kt >= nt[t]) continue;
-                        if (!(ok = mbar_wait_warp(&bar[P_FULL + t], gp[t] & 1))) break;
-                        ++gp[t];
+                        if (!(ok = mbar_wait_warp(&bar[P_HALF + t], gp[t] & 1))) break;
                         // the item's first product overwrites O: the last epilogue has read it
                         if (kt == 0) {
                             if (no[t] > 0 && !(ok = mbar_wait_warp(&bar[O_FREE + t], (no[t] - 1) & 1)))
@@ -328,7 +315,11 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                             have_v = true;
                         }
                         tc_fence_after();
-                        issue_pv(tbase + t * BN, uv, tbase + C::O_COL + t * HD, kt > 0);
+                        issue_pv(0, tbase + t * BN, uv, tbase + C::O_COL + t * HD, kt > 0);
+                        if (!(ok = mbar_wait_warp(&bar[P_FULL + t], gp[t] & 1))) break;
+                        ++gp[t];
+                        tc_fence_after();
+                        issue_pv(1, tbase + t * BN, uv, tbase + C::O_COL + t * HD, true);
                         if (kt + 1 < nt[t]) {
                             if (!have_k) {
                                 if (!(ok = wait_units(uk))) break;
@@ -362,15 +353,18 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                 ok = ok && next_s(0) && (n < 2 || next_s(1));
                 for (int kt = 0; kt < n && ok; ++kt) {
                     const uint32_t b = gp[0] & 1;
-                    if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (gp[0] >> 1) & 1))) break;
-                    ++gp[0];
+                    if (!(ok = mbar_wait_warp(&bar[P_HALF + b], (gp[0] >> 1) & 1))) break;
                     if (kt == 0) {
                         if (no[0] > 0 && !(ok = mbar_wait_warp(&bar[O_FREE], (no[0] - 1) & 1))) break;
                         ++no[0];
                     }
                     if (!(ok = wait_units(u))) break;
                     if (x.Lk - kt * BN < BN) zero_tail(u, x.Lk - kt * BN);
-                    issue_pv(tbase + b * BN, u, tbase + C::O_COL, kt > 0);
+                    issue_pv(0, tbase + b * BN, u, tbase + C::O_COL, kt > 0);
+                    if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (gp[0] >> 1) & 1))) break;
+                    ++gp[0];
+                    tc_fence_after();
+                    issue_pv(1, tbase + b * BN, u, tbase + C::O_COL, true);
                     commit(&bar[PV_DONE + b]);
                     free_units(u);
                     u += NU;
@@ -384,6 +378,46 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             commit(&bar[DRAIN]);
             mbar_wait_warp(&bar[DRAIN], 0, 100000000LL);
         }
+    } else if (warp == 3) {
+        // ---------------- items ----------------
+        // the longest first, forwards and backwards in turn over the CTAs
+        bool ok = true;
+        auto work = [&](int r) {
+            const int G = gridDim.x, b = blockIdx.x;
+            return r * G + ((r & 1) ? G - 1 - b : b);
+        };
+        auto entry = [&](int w) { return w < a.n_work ? a.items[w / a.Hkv] : make_int2(-1, 0); };
+        const int rounds = (a.n_work + gridDim.x - 1) / gridDim.x;
+        int2 e = entry(work(0));
+        int told = 0;
+        auto tell = [&](const PromptWork& x) {
+            const int b = told % ITEMS;
+            if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told / ITEMS) & 1) ^ 1)) return false;
+            if (elect_one()) {
+                volatile int* s = slots + 8 * b;
+                s[0] = x.q0;
+                s[1] = x.i0;
+                s[2] = x.Lq;
+                s[3] = x.k0;
+                s[4] = x.Lk;
+                s[5] = x.pre;
+                s[6] = x.kvh;
+                mbar_arrive(&bar[W_FULL + b]);
+            }
+            __syncwarp();
+            ++told;
+            return true;
+        };
+        for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
+            const int2 c = e;
+            const int w = work(r);
+            e = entry(work(r + 1));
+            if (c.x < 0) continue;
+            const int q0 = a.cu_q[c.x], k0 = a.cu_kv[c.x];
+            ok = tell(PromptWork{q0, c.y, a.cu_q[c.x + 1] - q0, k0, a.cu_kv[c.x + 1] - k0,
+                                 a.prefix ? a.prefix[c.x] : 0, w % a.Hkv});
+        }
+        if (!ok || !tell(PromptWork{0, -1, 0, 0, 0, 0, 0})) *fail_flag = 1;
     } else if (warp >= 4) {
         // ---------------- softmax + epilogue of row tile t ----------------
         const int t = (warp - 4) >> 2;
@@ -393,16 +427,17 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
         uint32_t g = 0, items_done = 0;  // score tiles, items with keys
         bool ok = true;
         const int tok = row / a.group, hg = row % a.group;
-        PromptWork nxt = prompt_fetch(a, 0);
-        for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
-            const PromptWork x = nxt;
-            nxt = prompt_fetch(a, r + 1);
-            if (!x.valid) continue;
-            const int n = x.key_tiles(t, T);
-            const int i = x.i0 + t * T + tok;
-            const bool live = tok < T && i < x.Lq;
-            // keys of this row; a row that is none of the tile's has no say in the masks
-            const int lim = live ? keys_seen(i, x.Lq, x.Lk, x.pre) : 0x7fffffff;
+        uint8_t* stg = sm + C::OFF_STG + (warp - 4) * STAGE;
+        while (ok) {
+            int n, lim;
+            {
+                const PromptWork x = next_item(ok);
+                if (!ok || x.i0 < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+                n = x.key_tiles(t, T);
+                const int i = x.i0 + t * T + tok;
+                // keys of this row; a row that is none of the tile's has no say in the masks
+                lim = tok < T && i < x.Lq ? keys_seen(i, x.Lq, x.Lk, x.pre) : 0x7fffffff;
+            }
             float m = -INFINITY, l = 0.f;
             for (int kt = 0; kt < n; ++kt) {
                 const uint32_t b = NST == 1 ? g & 1 : t;
@@ -484,13 +519,15 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                             pk[c * 16 + e / 2] = cvt_bf2(p0, p1);
                         }
                     tmem_st32(tS + h * 32, pk);
+                    // the first 64 keys' product starts while the others' P is formed
+                    tmem_st_wait();
+                    tc_fence_before();
+                    if (h == 0) mbar_arrive(&bar[P_HALF + b]);
                 }
                 float r0, r1, r2, r3;
                 f2_unpack(rs[0], r0, r1);
                 f2_unpack(rs[1], r2, r3);
                 l = l * alpha + ((r0 + r1) + (r2 + r3));
-                tmem_st_wait();
-                tc_fence_before();
                 mbar_arrive(&bar[P_FULL + b]);
                 ++g;
             }
@@ -500,10 +537,18 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                 tc_fence_after();
                 ++items_done;
             }
-            const int h = x.kvh * a.group + hg;
-            uint16_t* o = a.out + (long long)(x.q0 + i) * a.o_row + h * a.o_head;
+            const volatile int* s = slots + 8 * (seen % ITEMS);
+            const int i = s[1] + t * T + tok, row0 = s[0], h = s[6] * a.group + hg;
+            const bool live = tok < T && i < s[2];
+            item_done();
+            if (live && a.lse) a.lse[(size_t)(row0 + i) * a.H + h] = m + log2f(l);
             const float inv = l > 0.f ? 1.f / l : 0.f;
-            if (live && a.lse) a.lse[(size_t)(x.q0 + i) * a.H + h] = m + log2f(l);
+            // out through the warp's staging, 32 columns at a time: this lane writes its
+            // row's four units and stores unit lane % 4 of rows lane / 4 + 8 j
+            long long o = live ? (long long)(row0 + i) * a.o_row + h * a.o_head : -1;
+            long long to[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[j] = __shfl_sync(0xffffffffu, o, 8 * j + (lane >> 2));
 #pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
                 uint32_t w[32];
@@ -518,20 +563,27 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
 #pragma unroll
                     for (int e = 0; e < 32; ++e) w[e] = 0;
                 }
-                if (live) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint4 q;
-                        uint32_t* qp = &q.x;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t q[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            // a row without keys: O holds products of zeros
-                            qp[e] = l > 0.f ? cvt_bf2(__uint_as_float(w[8 * j + 2 * e]) * inv,
-                                                       __uint_as_float(w[8 * j + 2 * e + 1]) * inv)
-                                            : 0u;
-                        *reinterpret_cast<uint4*>(o + c * 32 + j * 8) = q;
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        // a row without keys: O holds products of zeros
+                        q[e] = l > 0.f ? cvt_bf2(__uint_as_float(w[8 * j + 2 * e]) * inv,
+                                                 __uint_as_float(w[8 * j + 2 * e + 1]) * inv)
+                                       : 0u;
+                    *reinterpret_cast<uint4*>(stg + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) =
+                        make_uint4(q[0], q[1], q[2], q[3]);
                 }
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int rr = 8 * j + (lane >> 2), un = lane & 3;
+                    const uint4 q = *reinterpret_cast<const uint4*>(
+                        stg + rr * 64 + ((un ^ ((rr >> 1) & 3)) << 4));
+                    if (to[j] >= 0) *reinterpret_cast<uint4*>(a.out + to[j] + c * 32 + un * 8) = q;
+                }
+                __syncwarp();
             }
         }
         if (!ok) *fail_flag = 1;
