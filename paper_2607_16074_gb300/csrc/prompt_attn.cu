@@ -14,8 +14,9 @@
 // One CTA per SM, persistent, over the items from the longest to the shortest, forwards
 // and backwards in turn so that the rounds' inequalities cancel.  Roles:
 //   warp 0       TMA: the item's Q tiles (3-D boxes: 64 columns x heads x tokens), then
-//                K and V through one ring of 16 KB units (K: 128 keys x 64 columns,
-//                V: 8,192 / hd keys x hd columns), in the order the MMAs take them
+//                K and V through one ring of whole tiles, or of 16 KB quarters at head
+//                dim 256 (K: 128 keys x 64 columns, V: 32 keys x 256 columns), in the
+//                order the MMAs take them
 //   warp 1       MMA issuer.  Two tiles: S of a tile overwrites its P once PV is issued
 //                and the other tile's products run while this one's softmax does.  One
 //                tile (head dim 256): two score buffers, S two key tiles ahead of PV.
@@ -39,8 +40,6 @@ namespace jnx {
 
 namespace pattn {
 constexpr int BM = 128, BN = 128;
-constexpr int UNIT = 16384;  // bytes of a ring unit
-constexpr int RING = 9;
 constexpr int STAGE = 2048;  // epilogue staging of a softmax warp: 32 rows x 32 columns
 constexpr float kLazy = 8.0f;  // log2 growth of the maximum that moves it
 // barriers: ring full / empty, then
@@ -52,13 +51,19 @@ constexpr int ITEMS = 3;  // items handed out at a time
 template <int HD>
 struct PromptCfg {
     static constexpr int NST = HD == 256 ? 1 : 2;  // row tiles of an item
-    static constexpr int NU = HD / 64;             // units of a K or V tile
+    static constexpr int NCH = HD / 64;            // 64-column chunks of a row
+    // ring units: whole K and V tiles, or at head dim 256, where two tiles would fill the
+    // ring, quarters
+    static constexpr int NU = HD == 256 ? 4 : 1;   // units of a K or V tile
+    static constexpr int UNIT = pattn::BN * HD * 2 / NU;
+    static constexpr int RING = HD == 256 ? 9 : HD == 128 ? 4 : 8;
+    static constexpr int KCH = NCH / NU;           // chunks of a K unit
     static constexpr int VKEYS = pattn::BN / NU;   // keys of a V unit
     static constexpr int QB = pattn::BM * HD * 2;
     static constexpr int OFF_RING = NST * QB;
-    static constexpr int OFF_STG = OFF_RING + pattn::RING * pattn::UNIT;
+    static constexpr int OFF_STG = OFF_RING + RING * UNIT;
     static constexpr int OFF_BAR = OFF_STG + 4 * NST * pattn::STAGE;
-    static constexpr int SMEM = OFF_BAR + (2 * pattn::RING + pattn::N_BARS) * 8 + 16 + pattn::ITEMS * 32 + 1024;
+    static constexpr int SMEM = OFF_BAR + (2 * RING + pattn::N_BARS) * 8 + 16 + pattn::ITEMS * 32 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
     static constexpr int THREADS = 128 + 128 * NST;
     static constexpr uint32_t O_COL = 256;
@@ -93,7 +98,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                   const __grid_constant__ CUtensorMap tv, const __grid_constant__ PromptArgs a) {
     using C = PromptCfg<HD>;
     using namespace pattn;
-    constexpr int NST = C::NST, NU = C::NU;
+    constexpr int NST = C::NST, NU = C::NU, UNIT = C::UNIT, RING = C::RING, NCH = C::NCH;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -161,10 +166,13 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                     uint8_t* dst = ring + s * UNIT;
                     const int row = x.k0 + kt * BN;
                     if (!is_v) {
-                        tma_load_3d(dst, &tk, c * 64, x.kvh, row, &full[s]);
+#pragma unroll
+                        for (int j = 0; j < C::KCH; ++j)
+                            tma_load_3d(dst + j * BN * 128, &tk, (c * C::KCH + j) * 64, x.kvh, row,
+                                        &full[s]);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < NU; ++j)
+                        for (int j = 0; j < NCH; ++j)
                             tma_load_3d(dst + j * C::VKEYS * 128, &tv, j * 64, x.kvh,
                                         row + c * C::VKEYS, &full[s]);
                     }
@@ -186,7 +194,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&bar[Q_FULL + t], qbytes);
 #pragma unroll
-                    for (int c = 0; c < NU; ++c)
+                    for (int c = 0; c < NCH; ++c)
                         tma_load_3d(sm + t * C::QB + c * BM * 128, &tq, c * 64, x.kvh * a.group,
                                     x.q0 + x.i0 + t * T, &bar[Q_FULL + t]);
                 }
@@ -236,8 +244,9 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
         auto issue_s = [&](int t, uint32_t first, uint32_t d, uint64_t* done) {
             if (elect_one()) {
 #pragma unroll
-                for (int c = 0; c < NU; ++c) {
-                    const uint32_t k_lo = r_lo + ((first + c) % RING) * (UNIT >> 4);
+                for (int c = 0; c < NCH; ++c) {
+                    const uint32_t k_lo = r_lo + ((first + c / C::KCH) % RING) * (UNIT >> 4) +
+                                          c % C::KCH * (BN * 128 >> 4);
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
                         tc_mma_f16(d,
@@ -299,7 +308,11 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                 u += NU;
                 for (int kt = 0; kt < n && ok; ++kt) {
                     const uint32_t uv = u, uk = u + NU;  // V(kt), K(kt + 1)
-                    bool have_v = false, have_k = false;
+                    // the tiles that the products below take, waited for before P: they are
+                    // mostly there, and P is what the tensor core then waits for
+                    if (!(ok = wait_units(uv))) break;
+                    if (x.Lk - kt * BN < BN) zero_tail(uv, x.Lk - kt * BN);
+                    if (kt + 1 < n && !(ok = wait_units(uk))) break;
                     for (int t = 0; t < 2; ++t) {
                         if (kt >= nt[t]) continue;
                         if (!(ok = mbar_wait_warp(&bar[P_HALF + t], gp[t] & 1))) break;
@@ -309,11 +322,6 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                                 break;
                             ++no[t];
                         }
-                        if (!have_v) {
-                            if (!(ok = wait_units(uv))) break;
-                            if (x.Lk - kt * BN < BN) zero_tail(uv, x.Lk - kt * BN);
-                            have_v = true;
-                        }
                         tc_fence_after();
                         issue_pv(0, tbase + t * BN, uv, tbase + C::O_COL + t * HD, kt > 0);
                         if (!(ok = mbar_wait_warp(&bar[P_FULL + t], gp[t] & 1))) break;
@@ -321,10 +329,6 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                         tc_fence_after();
                         issue_pv(1, tbase + t * BN, uv, tbase + C::O_COL + t * HD, true);
                         if (kt + 1 < nt[t]) {
-                            if (!have_k) {
-                                if (!(ok = wait_units(uk))) break;
-                                have_k = true;
-                            }
                             issue_s(t, uk, tbase + t * BN, &bar[S_FULL + t]);
                             if (kt + 2 == nt[t]) commit(&bar[Q_EMPTY + t]);
                         } else {
@@ -353,13 +357,14 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                 ok = ok && next_s(0) && (n < 2 || next_s(1));
                 for (int kt = 0; kt < n && ok; ++kt) {
                     const uint32_t b = gp[0] & 1;
+                    if (!(ok = wait_units(u))) break;
+                    if (x.Lk - kt * BN < BN) zero_tail(u, x.Lk - kt * BN);
                     if (!(ok = mbar_wait_warp(&bar[P_HALF + b], (gp[0] >> 1) & 1))) break;
                     if (kt == 0) {
                         if (no[0] > 0 && !(ok = mbar_wait_warp(&bar[O_FREE], (no[0] - 1) & 1))) break;
                         ++no[0];
                     }
-                    if (!(ok = wait_units(u))) break;
-                    if (x.Lk - kt * BN < BN) zero_tail(u, x.Lk - kt * BN);
+                    tc_fence_after();
                     issue_pv(0, tbase + b * BN, u, tbase + C::O_COL, kt > 0);
                     if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (gp[0] >> 1) & 1))) break;
                     ++gp[0];
