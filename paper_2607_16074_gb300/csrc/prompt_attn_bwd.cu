@@ -23,7 +23,7 @@
 //   0     claims items and hands them out; TMA: the item's outer tiles (K and V, or Q
 //         and dO), inner tiles through two rings of two or three
 //   1     MMA issuer
-//   2     the rows' lse, D and key limits of each inner row tile (keys pass)
+//   2     the rows' lse and D of each inner row tile (keys pass)
 //   4-11  elementwise: warps 4-7 a tile's first 64 columns, 8-11 the others; then the
 //         accumulators out
 // Inner rows past a sequence's end belong to others and may be NaN: they are zeroed in
@@ -45,7 +45,8 @@ enum { KEYS = 0, QUERIES = 1 };
 // barriers of a pass
 enum { O_FULL = 0, O_EMPTY = 1, B1_FULL = 2, B1_EMPTY = 5, B2_FULL = 8, B2_EMPTY = 11, S_FULL = 14,
        DP_FULL = 15, P_FULL = 16, DS_FULL = 17, ACC_FULL = 18, ACC_FREE = 19, DRAIN = 20,
-       ST_FULL = 21, ST_EMPTY = 23, W_FULL = 25, W_EMPTY = 27, N_BARS = 29 };
+       ST_FULL = 21, ST_EMPTY = 25, W_FULL = 29, W_EMPTY = 31, N_BARS = 33 };
+constexpr int ST = 4;  // slots of row values
 constexpr int THREADS = 384, EW = 8;
 constexpr int READERS = 2 + EW;  // warps that an item is handed to: MMA, row values, elementwise
 }  // namespace pbwd
@@ -56,8 +57,9 @@ struct PromptBwdCfg {
     static constexpr int TILE = pbwd::BM * HD * 2;
     static constexpr int SLOTS = HD == 64 ? 3 : 2;  // of each ring
     static constexpr int OFF_B1 = 2 * TILE, OFF_B2 = OFF_B1 + SLOTS * TILE;
-    static constexpr int OFF_ST = OFF_B2 + SLOTS * TILE;  // [2][lse, D, limit][128]
-    static constexpr int OFF_BAR = OFF_ST + 2 * 3 * pbwd::BM * 4;
+    static constexpr int OFF_STG = OFF_B2 + SLOTS * TILE;  // 2 KB an elementwise warp
+    static constexpr int OFF_ST = OFF_STG + pbwd::EW * 2048;  // [ST][-lse, -D][128]
+    static constexpr int OFF_BAR = OFF_ST + pbwd::ST * 2 * pbwd::BM * 4;
     static constexpr int SMEM = OFF_BAR + 2 * pbwd::N_BARS * 8 + 80 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
     static constexpr uint32_t S_COL = 0, DP_COL = 128, ACC_COL = 256;
@@ -69,7 +71,8 @@ struct PromptBwdArgs {
     int n_keys, n_queries, H, Hkv, group;
     int* claimed;       // items taken beyond the grid's first: 0 at launch
     float scale_log2, scale;
-    const float2* row;  // [rows][H]: lse (+inf where a row sees no key), D
+    const float2* row;  // [Hkv][rows][group]: lse (+inf where a row sees no key), D
+    int rows;
     jnx_head_rows dq, dk, dv;
     int* status;
 };
@@ -82,7 +85,7 @@ struct PromptBwdItem {
 // The rows' (lse, D), and the claim counter to zero.  A warp a (row, head).
 __global__ void __launch_bounds__(256)
     k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, const float* lse, int rows, int H,
-                      int hd, float2* row, int* claimed) {
+                      int group, int hd, float2* row, int* claimed) {
     pdl_entry();
     if (blockIdx.x == 0 && threadIdx.x == 0) *claimed = 0;
     // hd / 8 lanes a row, 16 bytes each
@@ -106,8 +109,31 @@ __global__ void __launch_bounds__(256)
     for (int o = lanes / 2; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
     if (w < (long long)rows * H && c == 0) {
         const float l = lse[w];
-        row[w] = l == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(l, d);
+        const int h = (int)(w % H);
+        row[((long long)(h / group) * rows + w / H) * group + h % group] =
+            l == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(l, d);
     }
+}
+
+// 32 fp32 columns of a warp's 32 rows (a lane a row), scaled, out as bf16 through 2 KB of
+// staging: lane l writes unit l % 4 of rows l / 4 + 8 u to base + at[u] (-1: no row).
+__device__ __forceinline__ void bwd_rows_out(uint8_t* stg, int lane, const uint32_t (&v)[32], float f,
+                                             uint16_t* base, const long long (&at)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<uint4*>(stg + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(
+            cvt_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
+            cvt_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
+            cvt_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
+            cvt_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
+    __syncwarp();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int r = 8 * u + (lane >> 2), un = lane & 3;
+        const uint4 q = *reinterpret_cast<const uint4*>(stg + r * 64 + ((un ^ ((r >> 1) & 3)) << 4));
+        if (at[u] >= 0) *reinterpret_cast<uint4*>(base + at[u] + un * 8) = q;
+    }
+    __syncwarp();
 }
 
 template <int HD, int PASS>
@@ -316,31 +342,43 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             auto valid = [&](int j) {
                 return KP ? min(T, x.Lq - i0 - j * T) * p.group : min(BM, x.Lk - j * BM);
             };
-            auto next_s = [&](int j) -> bool {
+            // a tile is waited for before the P or dS that its product follows in the queue:
+            // it is mostly there, and those are what the tensor core then waits for
+            auto wait_b1 = [&](int j) -> bool {
                 const int s = g1 % SLOTS;
                 if (!mbar_wait_warp(&bar[B1_FULL + s], (g1 / SLOTS) & 1)) return false;
                 if (valid(j) < box) zero_tail(b1 + s * C::TILE, valid(j), box);
+                return true;
+            };
+            auto wait_b2 = [&](int j) -> bool {
+                const int s = g2 % SLOTS;
+                if (!mbar_wait_warp(&bar[B2_FULL + s], (g2 / SLOTS) & 1)) return false;
+                if (KP && valid(j) < box) zero_tail(b2 + s * C::TILE, valid(j), box);
+                return true;
+            };
+            auto next_s = [&]() {
+                const int s = g1 % SLOTS;
                 tc_fence_after();
                 score(tbase + C::S_COL, o1, b1 + s * C::TILE);
                 commit(&bar[S_FULL]);
                 ++g1;
-                return true;
             };
-            auto next_dp = [&](int j) -> bool {
+            auto next_dp = [&]() {
                 const int s = g2 % SLOTS;
-                if (!mbar_wait_warp(&bar[B2_FULL + s], (g2 / SLOTS) & 1)) return false;
-                if (KP && valid(j) < box) zero_tail(b2 + s * C::TILE, valid(j), box);
                 tc_fence_after();
                 score(tbase + C::DP_COL, o2, b2 + s * C::TILE);
                 commit(&bar[DP_FULL]);
                 if (!KP) commit(&bar[B2_EMPTY + s]);  // V is done with
                 ++g2;
-                return true;
             };
-            ok = next_s(0) && next_dp(0);
-            if (ok && n == 1) commit(&bar[O_EMPTY]);
+            if (!(ok = wait_b1(0))) break;
+            next_s();
+            if (!(ok = wait_b2(0))) break;
+            next_dp();
+            if (n == 1) commit(&bar[O_EMPTY]);
             for (int j = 0; j < n && ok; ++j, ++gp) {
                 const int s = gp % SLOTS;
+                if (j + 1 < n && !(ok = wait_b1(j + 1))) break;
                 // P^T over S (keys pass), or S read (queries pass)
                 if (!(ok = mbar_wait_warp(&bar[P_FULL], gp & 1))) break;
                 // the item's first sums overwrite the accumulators: the last epilogue has read them
@@ -350,13 +388,16 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                     gather(tbase + C::ACC_COL + HD, tbase + C::S_COL, b2 + s * C::TILE, j > 0);
                     commit(&bar[B2_EMPTY + s]);
                 }
-                if (j + 1 < n && !(ok = next_s(j + 1))) break;
+                if (j + 1 < n) {
+                    next_s();
+                    if (!(ok = wait_b2(j + 1))) break;
+                }
                 if (!(ok = mbar_wait_warp(&bar[DS_FULL], gp & 1))) break;
                 tc_fence_after();
                 gather(tbase + C::ACC_COL, tbase + C::DP_COL, b1 + s * C::TILE, j > 0);
                 commit(&bar[B1_EMPTY + s]);
                 if (j + 1 < n) {
-                    if (!(ok = next_dp(j + 1))) break;
+                    next_dp();
                     if (j + 2 == n) commit(&bar[O_EMPTY]);
                 }
             }
@@ -379,24 +420,21 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             if (!KP) continue;
             const int n = n_inner(x), i0 = first_tok(x);
             for (int j = 0; j < n; ++j, ++g) {
-                const int b = g & 1;
+                const int b = g % ST;
                 float2 v[4];
-                int lim[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = e * 32 + lane, t = r / p.group, i = i0 + j * T + t;
                     const bool live = t < T && i < x.Lq;
-                    v[e] = live ? p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + r % p.group]
+                    v[e] = live ? p.row[((size_t)x.kvh * p.rows + x.q0 + i0 + j * T) * p.group + r]
                                 : make_float2(INFINITY, 0.f);
-                    lim[e] = live ? keys_seen(i, x.Lq, x.Lk, x.pre) : 0;
                 }
-                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g >> 1) & 1) ^ 1))) break;
+                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g / ST) & 1) ^ 1))) break;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = e * 32 + lane;
-                    st[b * 384 + r] = v[e].x;
-                    st[b * 384 + 128 + r] = v[e].y;
-                    st[b * 384 + 256 + r] = __int_as_float(lim[e]);
+                    st[b * 256 + r] = -v[e].x;
+                    st[b * 256 + 128 + r] = -v[e].y;
                 }
                 mbar_arrive(&bar[ST_FULL + b]);
             }
@@ -409,6 +447,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         const uint32_t tS = tbase + lane_base + C::S_COL + half * 64;
         const uint32_t tP = tbase + lane_base + C::DP_COL + half * 64;
         const int r = quarter * 32 + lane;
+        uint8_t* stg = sm + C::OFF_STG + (warp - 4) * 2048;
         uint32_t g = 0;
         int done = 0;
         bool ok = true;
@@ -420,63 +459,75 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             const int tok = r / p.group, hg = r % p.group;
             const int key = x.at + r, i = x.at + tok;
             const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
-            float lse = INFINITY, D = 0.f;
+            float nlse = -INFINITY, nD = 0.f;
+            // what counts of an outer row: a query's keys below lim, a key's rows from `from` on
             int lim = 0x7fffffff;
+            const int from = KP ? (first_row(key, x.Lq, x.Lk, x.pre) - i0) * p.group : 0;
             if (!KP && live) {
-                const float2 v = p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + hg];
-                lse = v.x;
-                D = v.y;
+                const float2 v = p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + hg];
+                nlse = -v.x;
+                nD = -v.y;
                 lim = keys_seen(i, x.Lq, x.Lk, x.pre);
             }
             for (int j = 0; j < n; ++j, ++g) {
-                const float* sv = st + (g & 1) * 384 + half * 64;
+                const float* sv = st + g % ST * 256 + half * 64;
                 bool whole;  // every score of the tile counts
                 if (KP) {
                     whole = keys_seen(min(i0 + j * T, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
                             min(x.at + BM, x.Lk);
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + (g & 1)], (g >> 1) & 1))))
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + g % ST], (g / ST) & 1))))
                         break;
                 } else {
                     whole = __all_sync(0xffffffffu, lim >= (j + 1) * BM);
                 }
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[S_FULL], g & 1)))) break;
                 tc_fence_after();
-                float pr[64];
+                uint64_t pr[32];  // P, pairs of columns
                 {
                     uint32_t s[2][32];
                     tmem_ld32(tS, s[0]);
                     tmem_ld32(tS + 32, s[1]);
                     tmem_ld_wait_regs(s[0]);
                     tmem_ld_wait_regs(s[1]);
+                    const uint64_t c2 = f2_pack(p.scale_log2, p.scale_log2);
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
-                            float4 l4 = make_float4(lse, lse, lse, lse);
+                            float4 l4 = make_float4(nlse, nlse, nlse, nlse);
                             if (KP) l4 = *reinterpret_cast<const float4*>(sv + c * 32 + e);
-                            const float* lp = &l4.x;
+                            const uint64_t l2[2] = {f2_pack(l4.x, l4.y), f2_pack(l4.z, l4.w)};
 #pragma unroll
-                            for (int u = 0; u < 4; ++u)
-                                pr[c * 32 + e + u] =
-                                    ex2_approx(fmaf(__uint_as_float(s[c][e + u]), p.scale_log2, -lp[u]));
+                            for (int u = 0; u < 2; ++u) {
+                                float x0, x1;
+                                f2_unpack(f2_fma(f2_pack(__uint_as_float(s[c][e + 2 * u]),
+                                                         __uint_as_float(s[c][e + 2 * u + 1])),
+                                                 c2, l2[u]),
+                                          x0, x1);
+                                pr[c * 16 + e / 2 + u] = f2_pack(ex2_approx(x0), ex2_approx(x1));
+                            }
                         }
                 }
                 if (!whole) {
-                    if (KP) {
-                        const int* lm = reinterpret_cast<const int*>(sv + 256);
+                    // columns that count: [0, hi) of a query, [lo, 64) of a key
+                    const int lo = from - j * T * p.group - half * 64, hi = lim - j * BM - half * 64;
 #pragma unroll
-                        for (int e = 0; e < 64; ++e)
-                            if (key >= lm[e]) pr[e] = 0.f;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 64; ++e)
-                            if (j * BM + half * 64 + e >= lim) pr[e] = 0.f;
+                    for (int e = 0; e < 32; ++e) {
+                        float a, b;
+                        f2_unpack(pr[e], a, b);
+                        if (KP ? 2 * e < lo : 2 * e >= hi) a = 0.f;
+                        if (KP ? 2 * e + 1 < lo : 2 * e + 1 >= hi) b = 0.f;
+                        pr[e] = f2_pack(a, b);
                     }
                 }
                 if (KP) {
                     uint32_t pk[32];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) pk[e] = cvt_bf2(pr[2 * e], pr[2 * e + 1]);
+                    for (int e = 0; e < 32; ++e) {
+                        float a, b;
+                        f2_unpack(pr[e], a, b);
+                        pk[e] = cvt_bf2(a, b);
+                    }
                     tmem_st32(tS, pk);
                     tmem_st_wait();
                 }
@@ -494,18 +545,25 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                     tmem_ld_wait_regs(d);
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
-                        float4 d4 = make_float4(D, D, D, D);
+                        float4 d4 = make_float4(nD, nD, nD, nD);
                         if (KP) d4 = *reinterpret_cast<const float4*>(sv + 128 + c * 32 + e);
-                        const float* dp = &d4.x;
-                        float v[4];
+                        const uint64_t d2[2] = {f2_pack(d4.x, d4.y), f2_pack(d4.z, d4.w)};
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            v[u] = pr[c * 32 + e + u] * (__uint_as_float(d[e + u]) - dp[u]);
-                            // V beyond the sequence's keys may be NaN
-                            if (!KP && !whole && pr[c * 32 + e + u] == 0.f) v[u] = 0.f;
+                        for (int u = 0; u < 2; ++u) {
+                            const uint64_t pp = pr[c * 16 + e / 2 + u];
+                            float a, b;
+                            f2_unpack(f2_mul(pp, f2_add(f2_pack(__uint_as_float(d[e + 2 * u]),
+                                                                __uint_as_float(d[e + 2 * u + 1])),
+                                                        d2[u])),
+                                      a, b);
+                            if (!KP && !whole) {  // V beyond the sequence's keys may be NaN
+                                float p0, p1;
+                                f2_unpack(pp, p0, p1);
+                                if (p0 == 0.f) a = 0.f;
+                                if (p1 == 0.f) b = 0.f;
+                            }
+                            dk[c * 16 + e / 2 + u] = cvt_bf2(a, b);
                         }
-                        dk[c * 16 + e / 2] = cvt_bf2(v[0], v[1]);
-                        dk[c * 16 + e / 2 + 1] = cvt_bf2(v[2], v[3]);
                     }
                 }
                 tmem_st32(tP, dk);
@@ -514,7 +572,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 __syncwarp();
                 if (elect_one()) {
                     mbar_arrive(&bar[DS_FULL]);
-                    if (KP) mbar_arrive(&bar[ST_EMPTY + (g & 1)]);
+                    if (KP) mbar_arrive(&bar[ST_EMPTY + g % ST]);
                 }
                 __syncwarp();
             }
@@ -525,37 +583,29 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 tc_fence_after();
                 ++done;
             }
-#pragma unroll
             for (int acc = 0; acc < (KP ? 2 : 1); ++acc) {
                 const float f = acc ? 1.f : p.scale;
-                uint16_t* o;
-                if (KP) {
-                    const jnx_head_rows& to = acc ? p.dv : p.dk;
-                    o = to.ptr + (long long)(x.k0 + key) * to.row_stride + x.kvh * to.head_stride;
-                } else {
-                    o = p.dq.ptr + (long long)(x.q0 + i) * p.dq.row_stride +
-                        (x.kvh * p.group + hg) * p.dq.head_stride;
-                }
-                o += half * (HD / 2);
+                const jnx_head_rows& to = !KP ? p.dq : acc ? p.dv : p.dk;
+                const long long o = !live ? -1
+                                    : KP  ? (x.k0 + key) * to.row_stride + x.kvh * to.head_stride
+                                          : (x.q0 + i) * to.row_stride + (x.kvh * p.group + hg) * to.head_stride;
+                // this lane's row's four units into the warp's staging, out unit lane % 4 of
+                // rows lane / 4 + 8 u
+                long long at[4];
 #pragma unroll
+                for (int u = 0; u < 4; ++u) at[u] = __shfl_sync(0xffffffffu, o, 8 * u + (lane >> 2));
+#pragma unroll 1
                 for (int c = 0; c < HD / 64; ++c) {
+                    const int col = half * (HD / 2) + c * 32;
                     uint32_t v[32];
                     if (n > 0) {
-                        tmem_ld32(tbase + lane_base + C::ACC_COL + acc * HD + half * (HD / 2) + c * 32, v);
+                        tmem_ld32(tbase + lane_base + C::ACC_COL + acc * HD + col, v);
                         tmem_ld_wait_regs(v);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0;
                     }
-                    if (live) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            *reinterpret_cast<uint4*>(o + c * 32 + e * 8) = make_uint4(
-                                cvt_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
-                                cvt_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
-                                cvt_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
-                                cvt_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
-                    }
+                    bwd_rows_out(stg, lane, v, f, to.ptr + col, at);
                 }
             }
             if (n > 0) {
@@ -673,12 +723,13 @@ enum { DK = 0, DV = 1, DQ = 2 };
 constexpr int OB = BM * HD * 2, IB = BN * HD * 2;
 // barriers of a pass
 enum { O_FULL = 0, O_EMPTY = 1, B1_FULL = 2, B1_EMPTY = 4, B2_FULL = 6, B2_EMPTY = 8, S_FULL = 10,
-       P_FULL = 12, ACC_FULL = 14, ACC_FREE = 15, DRAIN = 16, ST_FULL = 17, ST_EMPTY = 19, W_FULL = 21,
-       W_EMPTY = 23, N_BARS = 25 };
+       P_FULL = 12, ACC_FULL = 14, ACC_FREE = 15, DRAIN = 16, ST_FULL = 17, ST_EMPTY = 20, W_FULL = 23,
+       W_EMPTY = 25, N_BARS = 27 };
+constexpr int ST = 3;                    // slots of row values
 constexpr int OFF_B1 = 2 * OB;           // two slots
 constexpr int OFF_B2 = OFF_B1 + 2 * IB;  // one; DV has two in the second outer tile's place
-constexpr int OFF_ST = OFF_B2 + IB;      // [2][lse, D, limit][64]
-constexpr int OFF_BAR = OFF_ST + 2 * 3 * BN * 4;
+constexpr int OFF_ST = OFF_B2 + IB;      // [ST][-lse, -D][64]
+constexpr int OFF_BAR = OFF_ST + ST * 2 * BN * 4;
 constexpr int SMEM = OFF_BAR + N_BARS * 8 + 80 + 1024;
 static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
 constexpr int THREADS = 384, EW = 8, READERS = 2 + EW;
@@ -974,24 +1025,21 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             if (!KP) continue;
             const int n = n_inner(x), i0 = first_tok(x);
             for (int j = 0; j < n; ++j, ++g) {
-                const int b = g & 1;
+                const int b = g % ST;
                 float2 v[2];
-                int lim[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = e * 32 + lane, t = r / p.group, i = i0 + j * Ti + t;
                     const bool live = t < Ti && i < x.Lq;
-                    v[e] = live ? p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + r % p.group]
+                    v[e] = live ? p.row[((size_t)x.kvh * p.rows + x.q0 + i0 + j * Ti) * p.group + r]
                                 : make_float2(INFINITY, 0.f);
-                    lim[e] = live ? keys_seen(i, x.Lq, x.Lk, x.pre) : 0;
                 }
-                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g >> 1) & 1) ^ 1))) break;
+                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g / ST) & 1) ^ 1))) break;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = e * 32 + lane;
-                    st[b * 192 + r] = v[e].x;
-                    st[b * 192 + 64 + r] = v[e].y;
-                    st[b * 192 + 128 + r] = __int_as_float(lim[e]);
+                    st[b * 128 + r] = -v[e].x;
+                    st[b * 128 + 64 + r] = -v[e].y;
                 }
                 mbar_arrive(&bar[ST_FULL + b]);
             }
@@ -1012,16 +1060,18 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             const int tok = r / p.group, hg = r % p.group;
             const int key = x.at + r, i = x.at + tok;
             const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
-            float lse = INFINITY, D = 0.f;
+            float nlse = -INFINITY, nD = 0.f;
+            // what counts of an outer row: a query's keys below lim, a key's rows from `from` on
             int lim = 0x7fffffff;
+            const int from = KP ? (first_row(key, x.Lq, x.Lk, x.pre) - i0) * p.group : 0;
             if (!KP && live) {
-                const float2 v = p.row[(size_t)(x.q0 + i) * p.H + x.kvh * p.group + hg];
-                lse = v.x;
-                D = v.y;
+                const float2 v = p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + hg];
+                nlse = -v.x;
+                nD = -v.y;
                 lim = keys_seen(i, x.Lq, x.Lk, x.pre);
             }
             for (int j = 0; j < n; ++j, ++g) {
-                const float* sv = st + (g & 1) * 192 + half * 32;
+                const float* sv = st + g % ST * 128 + half * 32;
                 const uint32_t b = g & 1, ph = (g >> 1) & 1;
                 const uint32_t tS = tbase + lane_base + S_COL + b * BN + half * 32;
                 const uint32_t tP = tbase + lane_base + DP_COL + b * BN + half * 32;
@@ -1029,7 +1079,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                 if (KP) {
                     whole = keys_seen(min(i0 + j * Ti, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
                             min(x.at + BM, x.Lk);
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + b], ph)))) break;
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + g % ST], (g / ST) & 1)))) break;
                 } else {
                     whole = __all_sync(0xffffffffu, lim >= (j + 1) * BN);
                 }
@@ -1040,28 +1090,38 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                 if (NEED_DP) tmem_ld32(tP, d);
                 tmem_ld_wait_regs(s);
                 if (NEED_DP) tmem_ld_wait_regs(d);
+                const uint64_t c2 = f2_pack(p.scale_log2, p.scale_log2);
+                // columns that count: [0, hi) of a query, [lo, 32) of a key
+                const int lo = from - j * Ti * p.group - half * 32, hi = lim - j * BN - half * 32;
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
-                    float4 l4 = make_float4(lse, lse, lse, lse), d4 = make_float4(D, D, D, D);
+                    float4 l4 = make_float4(nlse, nlse, nlse, nlse), d4 = make_float4(nD, nD, nD, nD);
                     if (KP) {
                         l4 = *reinterpret_cast<const float4*>(sv + e);
                         if (NEED_DP) d4 = *reinterpret_cast<const float4*>(sv + 64 + e);
                     }
-                    const float *lp = &l4.x, *dp = &d4.x;
-                    float v[4];
+                    const uint64_t l2[2] = {f2_pack(l4.x, l4.y), f2_pack(l4.z, l4.w)};
+                    const uint64_t d2[2] = {f2_pack(d4.x, d4.y), f2_pack(d4.z, d4.w)};
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const float pr =
-                            ex2_approx(fmaf(__uint_as_float(s[e + u]), p.scale_log2, -lp[u]));
-                        v[u] = NEED_DP ? pr * (__uint_as_float(d[e + u]) - dp[u]) : pr;
+                    for (int u = 0; u < 2; ++u) {
+                        const int k = e + 2 * u;
+                        float a, b;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2,
+                                         l2[u]),
+                                  a, b);
+                        a = ex2_approx(a);
+                        b = ex2_approx(b);
+                        if (NEED_DP)
+                            f2_unpack(f2_mul(f2_pack(a, b),
+                                             f2_add(f2_pack(__uint_as_float(d[k]), __uint_as_float(d[k + 1])),
+                                                    d2[u])),
+                                      a, b);
                         if (!whole) {
-                            const bool hidden = KP ? key >= __float_as_int(sv[128 + e + u])
-                                                   : j * BN + half * 32 + e + u >= lim;
-                            if (hidden) v[u] = 0.f;
+                            if (KP ? k < lo : k >= hi) a = 0.f;
+                            if (KP ? k + 1 < lo : k + 1 >= hi) b = 0.f;
                         }
+                        pk[k / 2] = cvt_bf2(a, b);
                     }
-                    pk[e / 2] = cvt_bf2(v[0], v[1]);
-                    pk[e / 2 + 1] = cvt_bf2(v[2], v[3]);
                 }
                 tmem_st16(tS, pk);
                 tmem_st_wait();
@@ -1069,7 +1129,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                 __syncwarp();
                 if (elect_one()) {
                     mbar_arrive(&bar[P_FULL + b]);
-                    if (KP) mbar_arrive(&bar[ST_EMPTY + b]);
+                    if (KP) mbar_arrive(&bar[ST_EMPTY + g % ST]);
                 }
                 __syncwarp();
             }
@@ -1267,13 +1327,13 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
                     reinterpret_cast<const int2*>(p->items) + p->n_forward, p->n_keys, p->n_queries,
                     n_heads, n_kv_heads, n_heads / n_kv_heads, claimed,
                     (float)(1.4426950408889634 / sqrt((double)head_dim)),
-                    (float)(1.0 / sqrt((double)head_dim)), row, or_none(dq, rows),
+                    (float)(1.0 / sqrt((double)head_dim)), row, rows, or_none(dq, rows),
                     or_none(dk, keys), or_none(dv, keys), status};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN_BWD, 0.0, s);
     const int per = 256 / (head_dim / 8);
     pdl(k_prompt_bwd_rows, std::max(1, (int)(((long long)rows * n_heads + per - 1) / per)), 256, 0,
-        s)(or_none(out, rows), or_none(dout, rows), lse, rows, n_heads, head_dim, row, claimed);
+        s)(or_none(out, rows), or_none(dout, rows), lse, rows, n_heads, a.group, head_dim, row, claimed);
     // where there are no rows or keys nothing is loaded, but the maps want an address
     const jnx_head_rows& any = rows ? *q : *k;
     const jnx_head_rows qq = rows ? *q : any, dd = rows ? *dout : any, kk = keys ? *k : any,
