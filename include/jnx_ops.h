@@ -274,11 +274,13 @@ typedef struct {
     const int32_t *cu_q, *cu_kv, *prefix;
     const int32_t *h_cu_q, *h_cu_kv, *h_prefix;
     const int32_t* items;
-    int32_t n_forward, n_keys, n_queries; /* items of each pass, as jnx_prompt_items sets them */
+    /* items of each pass, and parts that the gradients sum a key's rows in, at most: as
+     * jnx_prompt_items sets them */
+    int32_t n_forward, n_keys, n_queries, n_parts;
 } jnx_prompt;
 
 /* The work list of a prompt for a head layout: writes up to cap pairs of int32 to out
- * (NULL: none), sets p's n_forward, n_keys, n_queries and returns the number of pairs,
+ * (NULL: none), sets p's n_forward, n_keys, n_queries, n_parts and returns the number of pairs,
  * the longest work first in each pass.  Negative: a jnx_status. */
 int32_t jnx_prompt_items(jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                          int32_t* out, int32_t cap);
@@ -296,7 +298,8 @@ jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_heads, int32_t
 
 /* Gradients of q, k and v from out's gradient dout, with the forward's out and lse.  The
  * same bits whatever else is packed beside a sequence. */
-size_t jnx_op_prompt_attention_backward_workspace_bytes(int32_t n_q, int32_t n_heads);
+size_t jnx_op_prompt_attention_backward_workspace_bytes(const jnx_prompt* p, int32_t n_heads,
+                                                        int32_t n_kv_heads, int32_t head_dim);
 jnx_status jnx_op_prompt_attention_backward(const jnx_prompt* p, int32_t n_heads,
                                             int32_t n_kv_heads, int32_t head_dim,
                                             const jnx_head_rows* q, const jnx_head_rows* k,

@@ -48,6 +48,18 @@ __host__ __device__ inline int item_tiles(int head_dim) { return head_dim == 256
 
 constexpr int kMaxGroup = 64;
 
+// Parts that the gradients' keys pass takes a 128-key tile's rows in: one where a sequence
+// has a tile for every SM by itself, else 2,048 rows each (token, head of the group).  Of
+// the sequence and the heads alone, so that a sequence's bits do not depend on others.  A
+// part is item (sequence, first key + part): a tile's first key is a multiple of 128.
+constexpr int kMaxParts = 64;
+__host__ __device__ inline int key_parts(int at, int Lq, int Lk, int prefix, int group, int Hkv) {
+    if ((long long)Hkv * ((Lk + 127) / 128) >= 152) return 1;
+    const long long rows = (long long)(Lq - first_row(at, Lq, Lk, prefix)) * group;
+    const long long n = (rows + 2047) / 2048;
+    return n < 1 ? 1 : n < kMaxParts ? (int)n : kMaxParts;
+}
+
 jnx_status heads_ok(int n_heads, int n_kv_heads, int head_dim, const char* what);
 
 }  // namespace jnx

@@ -650,7 +650,8 @@ jnx_status prompt_launchable(const jnx_prompt* p, const char* what, int& rows, i
     if (jnx_status st = prompt_ok(p, what, rows, keys)) return st;
     if (rows > 0 && (!p->cu_q || !p->cu_kv || !p->items || (p->h_prefix && !p->prefix)))
         return fail(JNX_ERR_INVALID_ARG, "%s: null device arrays", what);
-    if (p->n_forward < 0 || p->n_keys < 0 || p->n_queries < 0)
+    if (p->n_forward < 0 || p->n_keys < 0 || p->n_queries < 0 || p->n_parts < 0 ||
+        p->n_parts > kMaxParts)
         return fail(JNX_ERR_INVALID_ARG, "%s: bad work list", what);
     return JNX_OK;
 }
@@ -673,7 +674,7 @@ extern "C" int32_t jnx_prompt_items(jnx_prompt* p, int32_t n_heads, int32_t n_kv
         std::vector<Item> all;
         const int T = tile_tokens(n_heads / n_kv_heads);
         const int step[3] = {T * item_tiles(head_dim), 128, T};
-        int count[3];
+        int count[3], parts = 1;
         for (int pass = 0; pass < 3; ++pass) {
             const size_t first = all.size();
             for (int s = 0; s < p->n_seqs; ++s) {
@@ -683,9 +684,13 @@ extern "C" int32_t jnx_prompt_items(jnx_prompt* p, int32_t n_heads, int32_t n_kv
                 const int end = pass == 1 ? Lk : Lq;
                 for (long long at = 0; at < end; at += step[pass]) {
                     const int last = (int)std::min<long long>(at + step[pass], end) - 1;
-                    const long long cost = pass == 1 ? Lq - first_row((int)at, Lq, Lk, pre)
+                    const int np = pass == 1 ? key_parts((int)at, Lq, Lk, pre, n_heads / n_kv_heads,
+                                                         n_kv_heads)
+                                             : 1;
+                    const long long cost = pass == 1 ? (Lq - first_row((int)at, Lq, Lk, pre)) / np
                                                      : keys_seen(last, Lq, Lk, pre);
-                    all.push_back({s, (int)at, cost});
+                    parts = std::max(parts, np);
+                    for (int k = 0; k < np; ++k) all.push_back({s, (int)at + k, cost});
                 }
             }
             std::stable_sort(all.begin() + first, all.end(),
@@ -696,6 +701,7 @@ extern "C" int32_t jnx_prompt_items(jnx_prompt* p, int32_t n_heads, int32_t n_kv
         p->n_forward = count[0];
         p->n_keys = count[1];
         p->n_queries = count[2];
+        p->n_parts = parts;
         if (out && cap >= (int)all.size())
             for (size_t i = 0; i < all.size(); ++i) {
                 out[2 * i] = all[i].seq;

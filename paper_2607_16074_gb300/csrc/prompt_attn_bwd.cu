@@ -37,6 +37,7 @@
 
 namespace jnx {
 
+jnx_status prompt_ok(const jnx_prompt* p, const char* what, int& rows, int& keys);
 jnx_status prompt_launchable(const jnx_prompt* p, const char* what, int& rows, int& keys);
 
 namespace pbwd {
@@ -74,12 +75,29 @@ struct PromptBwdArgs {
     const float2* row;  // [Hkv][rows][group]: lse (+inf where a row sees no key), D
     int rows;
     jnx_head_rows dq, dk, dv;
+    float* part;  // [dk, dv][n_parts][keys][Hkv][hd]: the sums of tiles taken in parts
+    long long part_stride;  // of a part
+    int n_parts;
     int* status;
 };
 
 // What the warps of a CTA are told of an item.
 struct PromptBwdItem {
     int at, kvh, q0, Lq, k0, Lk, pre;  // at: first key or row; Lq < 0: no more in this pass
+    int part;                          // keys pass
+
+    // keys pass: parts of the tile, and this part's inner tiles [j0, j1) of T tokens from the
+    // first row that sees the tile's first key
+    __device__ __forceinline__ int parts(int group, int Hkv) const {
+        return key_parts(at, Lq, Lk, pre, group, Hkv);
+    }
+    __device__ __forceinline__ void range(int group, int Hkv, int T, int& i0, int& n) const {
+        const int first = first_row(at, Lq, Lk, pre), np = parts(group, Hkv);
+        const int all = (Lq - first + T - 1) / T;
+        const int j0 = (int)((long long)all * part / np), j1 = (int)((long long)all * (part + 1) / np);
+        i0 = first + j0 * T;
+        n = j1 - j0;
+    }
 };
 
 // The rows' (lse, D), and the claim counter to zero.  A warp a (row, head).
@@ -136,6 +154,57 @@ __device__ __forceinline__ void bwd_rows_out(uint8_t* stg, int lane, const uint3
     __syncwarp();
 }
 
+// The same in fp32, unscaled, 16 columns at a time.
+__device__ __forceinline__ void bwd_rows_part(uint8_t* stg, int lane, const uint32_t (&v)[32], float* base,
+                                              const long long (&at)[4]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<uint4*>(stg + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) =
+                make_uint4(v[16 * c + 4 * e], v[16 * c + 4 * e + 1], v[16 * c + 4 * e + 2],
+                           v[16 * c + 4 * e + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int r = 8 * u + (lane >> 2), un = lane & 3;
+            const uint4 q = *reinterpret_cast<const uint4*>(stg + r * 64 + ((un ^ ((r >> 1) & 3)) << 4));
+            if (at[u] >= 0) *reinterpret_cast<uint4*>(base + at[u] + c * 16 + un * 4) = q;
+        }
+        __syncwarp();
+    }
+}
+
+// dk and dv of the tiles taken in parts: their sums in the parts' order.  A CTA 8 keys of a
+// tile and key head, of either gradient.
+__global__ void __launch_bounds__(256) k_prompt_bwd_join(const __grid_constant__ PromptBwdArgs p, int hd) {
+    pdl_entry();
+    const int2 e = p.items[blockIdx.x / p.Hkv];
+    if (e.y & 127) return;
+    const int kvh = blockIdx.x % p.Hkv, k0 = p.cu_kv[e.x], Lk = p.cu_kv[e.x + 1] - k0;
+    const int Lq = p.cu_q[e.x + 1] - p.cu_q[e.x];
+    const int np = key_parts(e.y, Lq, Lk, p.prefix ? p.prefix[e.x] : 0, p.group, p.Hkv);
+    if (np == 1) return;
+    const int cols = hd / 4, which = blockIdx.z;
+    for (int i = threadIdx.x; i < 8 * cols; i += 256) {
+        const int r = blockIdx.y * 8 + i / cols, c = i % cols * 4;
+        if (e.y + r >= Lk) return;
+        const long long key = k0 + e.y + r;
+        const float* from = p.part + (long long)which * p.n_parts * p.part_stride +
+                            (key * p.Hkv + kvh) * hd + c;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < np; ++k) {
+            const float4 v = *reinterpret_cast<const float4*>(from + k * p.part_stride);
+            s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+        }
+        const float f = which ? 1.f : p.scale;
+        const jnx_head_rows& to = which ? p.dv : p.dk;
+        *reinterpret_cast<uint2*>(to.ptr + key * to.row_stride + kvh * to.head_stride + c) =
+            make_uint2(cvt_bf2(s.x * f, s.y * f), cvt_bf2(s.z * f, s.w * f));
+    }
+}
+
 template <int HD, int PASS>
 __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUtensorMap& tk,
                                                const CUtensorMap& tv, const CUtensorMap& tdo,
@@ -158,7 +227,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
     int seen = 0;
     auto next_item = [&](bool& ok) -> PromptBwdItem {
         const int b = seen & 1;
-        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0};
+        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0, 0};
         if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen >> 1) & 1))) return x;
         x.at = warp_uniform(slot[8 * b]);
         x.kvh = warp_uniform(slot[8 * b + 1]);
@@ -167,16 +236,20 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         x.k0 = warp_uniform(slot[8 * b + 4]);
         x.Lk = warp_uniform(slot[8 * b + 5]);
         x.pre = warp_uniform(slot[8 * b + 6]);
+        x.part = warp_uniform(slot[8 * b + 7]);
         if (elect_one()) mbar_arrive(&bar[W_EMPTY + b]);
         __syncwarp();
         ++seen;
         return x;
     };
-    // keys pass: the first row that an item's tile j holds
-    auto first_tok = [&](const PromptBwdItem& x) { return first_row(x.at, x.Lq, x.Lk, x.pre); };
-    auto n_inner = [&](const PromptBwdItem& x) {
-        if (KP) return (x.Lq - first_tok(x) + T - 1) / T;
-        return (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BM - 1) / BM;
+    // an item's inner tiles, and the keys pass's first inner row
+    auto inner = [&](const PromptBwdItem& x, int& i0, int& n) {
+        if (KP) {
+            x.range(p.group, p.Hkv, T, i0, n);
+        } else {
+            i0 = x.at;
+            n = (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BM - 1) / BM;
+        }
     };
 
     if (warp == 0) {
@@ -194,6 +267,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 slot[8 * b + 4] = x.k0;
                 slot[8 * b + 5] = x.Lk;
                 slot[8 * b + 6] = x.pre;
+                slot[8 * b + 7] = x.part;
                 mbar_arrive(&bar[W_FULL + b]);
             }
             __syncwarp();
@@ -208,12 +282,13 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         };
         // the item claimed: its list entry, then its sequence's rows
         int2 e = make_int2(0, 0);
-        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0};
+        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0};
         auto fetch = [&]() {
             claim = __shfl_sync(0xffffffffu, claim, 0);
             if (claim - q_first >= n_work) return;
             e = items[(claim - q_first) / p.Hkv];
-            nx.at = e.y;
+            nx.at = KP ? e.y & ~127 : e.y;
+            nx.part = KP ? e.y & 127 : 0;
             nx.kvh = (claim - q_first) % p.Hkv;
             nx.q0 = p.cu_q[e.x];
             nx.Lq = p.cu_q[e.x + 1] - nx.q0;
@@ -235,10 +310,12 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             x.k0 = warp_uniform(nx.k0);
             x.Lk = warp_uniform(nx.Lk);
             x.pre = warp_uniform(nx.pre);
+            x.part = warp_uniform(nx.part);
             if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
             __syncwarp();
             if (!(ok = tell(x))) break;
-            const int n = n_inner(x), i0 = KP ? first_tok(x) : x.at;
+            int i0, n;
+            inner(x, i0, n);
             if (n > 0) {
                 if (no > 0 && !(ok = mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1))) break;
                 if (elect_one()) {
@@ -275,7 +352,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             if (!ok) break;
             fetch();
         }
-        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0});
+        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0});
         if (!ok) *fail_flag = 1;
         // every copy has landed before the pass ends (at once in a normal run)
         if (no > 0) mbar_wait_warp(&bar[O_FULL], (no - 1) & 1, 100000000LL);
@@ -331,7 +408,8 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         while (ok) {
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
-            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            int i0, n;
+            inner(x, i0, n);
             if (n == 0) continue;
             if (!(ok = mbar_wait_warp(&bar[O_FULL], no & 1))) break;
             ++no;
@@ -418,7 +496,8 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
             if (!KP) continue;
-            const int n = n_inner(x), i0 = first_tok(x);
+            int i0, n;
+            inner(x, i0, n);
             for (int j = 0; j < n; ++j, ++g) {
                 const int b = g % ST;
                 float2 v[4];
@@ -454,7 +533,8 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         while (ok) {
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
-            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            int i0, n;
+            inner(x, i0, n);
             // the outer row of this thread: a key, or a (token, head)
             const int tok = r / p.group, hg = r % p.group;
             const int key = x.at + r, i = x.at + tok;
@@ -583,17 +663,24 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 tc_fence_after();
                 ++done;
             }
+            const bool in_parts = KP && x.parts(p.group, p.Hkv) > 1;
+            float* part = p.part + x.part * p.part_stride;
             for (int acc = 0; acc < (KP ? 2 : 1); ++acc) {
                 const float f = acc ? 1.f : p.scale;
                 const jnx_head_rows& to = !KP ? p.dq : acc ? p.dv : p.dk;
                 const long long o = !live ? -1
                                     : KP  ? (x.k0 + key) * to.row_stride + x.kvh * to.head_stride
                                           : (x.q0 + i) * to.row_stride + (x.kvh * p.group + hg) * to.head_stride;
+                // (a tile taken in parts: its sums' rows)
+                const long long po = live ? ((long long)(x.k0 + key) * p.Hkv + x.kvh) * HD : -1;
                 // this lane's row's four units into the warp's staging, out unit lane % 4 of
                 // rows lane / 4 + 8 u
-                long long at[4];
+                long long at[4], pat[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) at[u] = __shfl_sync(0xffffffffu, o, 8 * u + (lane >> 2));
+                for (int u = 0; u < 4; ++u) {
+                    at[u] = __shfl_sync(0xffffffffu, o, 8 * u + (lane >> 2));
+                    if (KP) pat[u] = __shfl_sync(0xffffffffu, po, 8 * u + (lane >> 2));
+                }
 #pragma unroll 1
                 for (int c = 0; c < HD / 64; ++c) {
                     const int col = half * (HD / 2) + c * 32;
@@ -605,7 +692,10 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0;
                     }
-                    bwd_rows_out(stg, lane, v, f, to.ptr + col, at);
+                    if (in_parts)
+                        bwd_rows_part(stg, lane, v, part + acc * p.n_parts * p.part_stride + col, pat);
+                    else
+                        bwd_rows_out(stg, lane, v, f, to.ptr + col, at);
                 }
             }
             if (n > 0) {
@@ -763,7 +853,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
     int seen = 0;
     auto next_item = [&](bool& ok) -> PromptBwdItem {
         const int b = seen & 1;
-        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0};
+        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0, 0};
         if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen >> 1) & 1))) return x;
         x.at = warp_uniform(slot[8 * b]);
         x.kvh = warp_uniform(slot[8 * b + 1]);
@@ -772,15 +862,20 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
         x.k0 = warp_uniform(slot[8 * b + 4]);
         x.Lk = warp_uniform(slot[8 * b + 5]);
         x.pre = warp_uniform(slot[8 * b + 6]);
+        x.part = warp_uniform(slot[8 * b + 7]);
         if (elect_one()) mbar_arrive(&bar[W_EMPTY + b]);
         __syncwarp();
         ++seen;
         return x;
     };
-    auto first_tok = [&](const PromptBwdItem& x) { return first_row(x.at, x.Lq, x.Lk, x.pre); };
-    auto n_inner = [&](const PromptBwdItem& x) {
-        if (KP) return (x.Lq - first_tok(x) + Ti - 1) / Ti;
-        return (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BN - 1) / BN;
+    // an item's inner tiles, and the keys pass's first inner row
+    auto inner = [&](const PromptBwdItem& x, int& i0, int& n) {
+        if (KP) {
+            x.range(p.group, p.Hkv, Ti, i0, n);
+        } else {
+            i0 = x.at;
+            n = (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BN - 1) / BN;
+        }
     };
 
     if (warp == 0) {
@@ -798,6 +893,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                 slot[8 * b + 4] = x.k0;
                 slot[8 * b + 5] = x.Lk;
                 slot[8 * b + 6] = x.pre;
+                slot[8 * b + 7] = x.part;
                 mbar_arrive(&bar[W_FULL + b]);
             }
             __syncwarp();
@@ -811,12 +907,13 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             for (int c = 0; c < NCH; ++c) tma_load_3d(dst + c * rows * 128, m, c * 64, head, row, full);
         };
         int2 e = make_int2(0, 0);
-        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0};
+        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0};
         auto fetch = [&]() {
             claim = __shfl_sync(0xffffffffu, claim, 0);
             if (claim - q_first >= n_work) return;
             e = items[(claim - q_first) / p.Hkv];
-            nx.at = e.y;
+            nx.at = KP ? e.y & ~127 : e.y;
+            nx.part = KP ? e.y & 127 : 0;
             nx.kvh = (claim - q_first) % p.Hkv;
             nx.q0 = p.cu_q[e.x];
             nx.Lq = p.cu_q[e.x + 1] - nx.q0;
@@ -839,10 +936,12 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             x.k0 = warp_uniform(nx.k0);
             x.Lk = warp_uniform(nx.Lk);
             x.pre = warp_uniform(nx.pre);
+            x.part = warp_uniform(nx.part);
             if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
             __syncwarp();
             if (!(ok = tell(x))) break;
-            const int n = n_inner(x), i0 = KP ? first_tok(x) : x.at;
+            int i0, n;
+            inner(x, i0, n);
             const int qh = x.kvh * p.group;
             if (n > 0) {
                 if (no > 0 && !(ok = mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1))) break;
@@ -882,7 +981,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             if (!ok) break;
             fetch();
         }
-        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0});
+        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0});
         if (!ok) *fail_flag = 1;
         // every copy has landed before the pass ends (at once in a normal run)
         if (no > 0) mbar_wait_warp(&bar[O_FULL], (no - 1) & 1, 100000000LL);
@@ -945,7 +1044,8 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
         while (ok) {
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
-            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            int i0, n;
+            inner(x, i0, n);
             if (n == 0) continue;
             if (!(ok = mbar_wait_warp(&bar[O_FULL], no & 1))) break;
             ++no;
@@ -1023,7 +1123,8 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
             if (!KP) continue;
-            const int n = n_inner(x), i0 = first_tok(x);
+            int i0, n;
+            inner(x, i0, n);
             for (int j = 0; j < n; ++j, ++g) {
                 const int b = g % ST;
                 float2 v[2];
@@ -1056,7 +1157,8 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
         while (ok) {
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
-            const int n = n_inner(x), i0 = KP ? first_tok(x) : 0;
+            int i0, n;
+            inner(x, i0, n);
             const int tok = r / p.group, hg = r % p.group;
             const int key = x.at + r, i = x.at + tok;
             const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
@@ -1149,6 +1251,10 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                     (x.kvh * p.group + hg) * p.dq.head_stride;
             }
             o += half * (HD / 2);
+            // a tile taken in parts: its sums' row
+            const bool in_parts = KP && x.parts(p.group, p.Hkv) > 1;
+            float* part = p.part + (x.part + (PASS == DV ? p.n_parts : 0)) * p.part_stride +
+                          ((long long)(x.k0 + key) * p.Hkv + x.kvh) * HD + half * (HD / 2);
 #pragma unroll 1
             for (int c = 0; c < HD / 64; ++c) {
                 uint32_t v[32];
@@ -1159,7 +1265,12 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0;
                 }
-                if (live) {
+                if (live && in_parts) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        *reinterpret_cast<uint4*>(part + c * 32 + e * 4) =
+                            make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                } else if (live) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         *reinterpret_cast<uint4*>(o + c * 32 + e * 8) = make_uint4(
@@ -1291,9 +1402,25 @@ static jnx_status launch_prompt_bwd_wide(const PromptBwdArgs& a, const jnx_head_
 
 using namespace jnx;
 
-extern "C" size_t jnx_op_prompt_attention_backward_workspace_bytes(int32_t n_q, int32_t n_heads) {
-    if (n_q < 0 || n_heads <= 0) return 0;
-    return 256 + (size_t)n_q * n_heads * sizeof(float2);  // the claims; each row's lse and D
+// The claims; each row's lse and D; the parts' sums, dk's and dv's.
+static size_t bwd_row_bytes(int rows, int n_heads) {
+    return 256 + (((size_t)rows * n_heads * sizeof(float2) + 255) & ~(size_t)255);
+}
+static size_t bwd_part_floats(const jnx_prompt* p, int keys, int n_kv_heads, int head_dim) {
+    return p->n_parts > 1 ? (size_t)keys * n_kv_heads * head_dim : 0;
+}
+
+extern "C" size_t jnx_op_prompt_attention_backward_workspace_bytes(const jnx_prompt* p,
+                                                                   int32_t n_heads,
+                                                                   int32_t n_kv_heads,
+                                                                   int32_t head_dim) {
+    clear_error();
+    int rows, keys;
+    if (heads_ok(n_heads, n_kv_heads, head_dim, "prompt attention backward") ||
+        prompt_ok(p, "prompt attention backward", rows, keys))
+        return 0;
+    return bwd_row_bytes(rows, n_heads) +
+           2 * std::max(p->n_parts, 1) * bwd_part_floats(p, keys, n_kv_heads, head_dim) * sizeof(float);
 }
 
 extern "C" jnx_status jnx_op_prompt_attention_backward(
@@ -1311,8 +1438,8 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     if ((rows > 0 && (!rows_ok(q) || !rows_ok(out) || !rows_ok(dout) || !rows_ok(dq) || !lse)) ||
         (keys > 0 && (!rows_ok(k) || !rows_ok(v) || !rows_ok(dk) || !rows_ok(dv))))
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned rows", what);
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7) ||
-        ws_bytes < jnx_op_prompt_attention_backward_workspace_bytes(rows, n_heads))
+    if (!workspace || !aligned16(workspace) ||
+        ws_bytes < jnx_op_prompt_attention_backward_workspace_bytes(p, n_heads, n_kv_heads, head_dim))
         return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
     const long long n_work = ((long long)2 * p->n_keys + p->n_queries) * n_kv_heads;
     // (claims run past the last item by one for each CTA and pass)
@@ -1328,7 +1455,9 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
                     n_heads, n_kv_heads, n_heads / n_kv_heads, claimed,
                     (float)(1.4426950408889634 / sqrt((double)head_dim)),
                     (float)(1.0 / sqrt((double)head_dim)), row, rows, or_none(dq, rows),
-                    or_none(dk, keys), or_none(dv, keys), status};
+                    or_none(dk, keys), or_none(dv, keys),
+                    reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + bwd_row_bytes(rows, n_heads)),
+                    (long long)bwd_part_floats(p, keys, n_kv_heads, head_dim), p->n_parts, status};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN_BWD, 0.0, s);
     const int per = 256 / (head_dim / 8);
@@ -1339,7 +1468,10 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     const jnx_head_rows qq = rows ? *q : any, dd = rows ? *dout : any, kk = keys ? *k : any,
                         vv = keys ? *v : any;
     const int nr = std::max(rows, 1), nk = std::max(keys, 1);
-    if (head_dim == 64) return launch_prompt_bwd<64>(a, qq, kk, vv, dd, nr, nk, s);
-    if (head_dim == 128) return launch_prompt_bwd<128>(a, qq, kk, vv, dd, nr, nk, s);
-    return launch_prompt_bwd_wide(a, qq, kk, vv, dd, nr, nk, s);
+    const jnx_status st = head_dim == 64    ? launch_prompt_bwd<64>(a, qq, kk, vv, dd, nr, nk, s)
+                          : head_dim == 128 ? launch_prompt_bwd<128>(a, qq, kk, vv, dd, nr, nk, s)
+                                            : launch_prompt_bwd_wide(a, qq, kk, vv, dd, nr, nk, s);
+    if (st || p->n_parts <= 1) return st;
+    pdl(k_prompt_bwd_join, dim3(p->n_keys * n_kv_heads, 16, 2), 256, 0, s)(a, head_dim);
+    return launched(what);
 }

@@ -186,7 +186,7 @@ class jnx_prompt(C.Structure):
                [(n, C.c_void_p) for n in ("cu_q", "cu_kv", "prefix")] + \
                [(n, P32) for n in ("h_cu_q", "h_cu_kv", "h_prefix")] + \
                [("items", C.c_void_p)] + \
-               [(n, C.c_int32) for n in ("n_forward", "n_keys", "n_queries")]
+               [(n, C.c_int32) for n in ("n_forward", "n_keys", "n_queries", "n_parts")]
 
 
 _LIB: Optional[C.CDLL] = None
@@ -308,7 +308,7 @@ def lib() -> C.CDLL:
         "jnx_prompt_items": (i32, [prompt, i32, i32, i32, vp, i32]),
         "jnx_op_prompt_attention": (i32, [prompt, i32, i32, i32, rows, rows, rows, rows, vp, vp,
                                           vp]),
-        "jnx_op_prompt_attention_backward_workspace_bytes": (sz, [i32, i32]),
+        "jnx_op_prompt_attention_backward_workspace_bytes": (sz, [prompt, i32, i32, i32]),
         "jnx_op_prompt_attention_backward": (i32, [prompt, i32, i32, i32, rows, rows, rows, rows,
                                                    vp, rows, rows, rows, rows, vp, sz, vp, vp]),
         "jnx_op_decode_attention_workspace_bytes": (sz, [i32, i32, i32]),

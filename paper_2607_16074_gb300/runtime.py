@@ -703,7 +703,7 @@ class PromptPlan:
         """The prompt with its work lists for a head layout, and what they lie in."""
         ptrs = [x.data_ptr() for x in self.d] + [None] * (3 - len(self.d))
         host = [x.ctypes.data_as(J.P32) for x in self.h] + [None] * (3 - len(self.h))
-        p = J.jnx_prompt(self.n_seqs, *ptrs, *host, None, 0, 0, 0)
+        p = J.jnx_prompt(self.n_seqs, *ptrs, *host, None, 0, 0, 0, 0)
         L = J.lib()
         n = L.jnx_prompt_items(C.byref(p), n_heads, n_kv_heads, head_dim, None, 0)
         if n < 0:
@@ -724,7 +724,7 @@ class PromptAttention(_TextOperator):
         self.struct, self.items = plan.struct(*self.dims)
         self._ref = C.byref(self.struct)
         super().__init__(J.lib().jnx_op_prompt_attention_backward_workspace_bytes(
-            plan.n_q, n_heads) if gradients else 0, plan.device)
+            self._ref, *self.dims) if gradients else 0, plan.device)
 
     def _q(self, t):
         return C.byref(_rows(t, self.plan.n_q, self.dims[0], self.dims[2]))

@@ -33,7 +33,7 @@ def prompt(q=(5, 3), kv=(5, 3), prefix=None, device=True):
         keep.append(np.asarray(prefix, np.int32))
     host = [x.ctypes.data_as(J.P32) for x in keep] + [None] * (3 - len(keep))
     dev = [PTR if device else None] * 2 + [PTR if prefix is not None else None]
-    p = J.jnx_prompt(len(q), *dev, *host, PTR, 1, 1, 1)
+    p = J.jnx_prompt(len(q), *dev, *host, PTR, 1, 1, 1, 1)
     p.keep = keep
     return p
 
@@ -107,7 +107,7 @@ def test_prompt_attention_backward_refuses():
     refused(f(lse=None), INV)
     refused(f(dk=rows(None)), INV)
     refused(f(ws=None), WS)
-    refused(f(n=L.jnx_op_prompt_attention_backward_workspace_bytes(8, 8) - 1), WS)
+    refused(f(n=L.jnx_op_prompt_attention_backward_workspace_bytes(C.byref(prompt()), 8, 2, 128) - 1), WS)
     assert f(p=prompt(q=(0,), kv=(0,))) == J.JNX_OK
 
 
@@ -146,7 +146,8 @@ def test_vocab_loss_refuses():
 
 @pytest.mark.parametrize("heads", [(4, 4, 64), (8, 1, 256), (12, 4, 128), (14, 2, 64)])
 def test_work_lists_cover_every_row_and_key_once(heads):
-    """Each pass visits every row (or key) of every sequence, the longest work first."""
+    """Each pass visits every row (or key, in each part of its rows) of every sequence, the
+    longest work first."""
     h, hkv, hd = heads
     q, kv, pre = (300, 0, 1, 129, 40), (300, 7, 5, 60, 400), (0, 3, 0, 9, 390)
     p = prompt(q, kv, pre)
@@ -156,22 +157,32 @@ def test_work_lists_cover_every_row_and_key_once(heads):
     assert n == p.n_forward + p.n_keys + p.n_queries
     tok = 128 // (h // hkv)
     steps = (tok * (1 if hd == 256 else 2), 128, tok)
+
+    def visible(s, i):  # keys that row i sees
+        return max(0, min(kv[s], max(kv[s] - q[s] + i + 1, pre[s])))
+
+    def parts(s, a):  # of a key tile's rows
+        rows = sum(1 for i in range(q[s]) if visible(s, i) > a) * (h // hkv)
+        return max(1, -(-rows // 2048)) if hkv * -(-kv[s] // 128) < 152 else 1
+
     at = 0
     for count, step, lens, pass_ in zip((p.n_forward, p.n_keys, p.n_queries), steps, (q, kv, q), range(3)):
         items, at = out[at:at + count], at + count
         seen = set()
-        for s, a in items:
+        for s, y in items:
+            a, part = (y // 128 * 128, y % 128) if pass_ == 1 else (y, 0)
             for i in range(a, min(a + step, lens[s])):
-                assert (s, i) not in seen
-                seen.add((int(s), i))
-        assert seen == {(s, i) for s, n_ in enumerate(lens) for i in range(n_)}
-
-        def visible(s, i):  # keys that row i sees
-            return max(0, min(kv[s], max(kv[s] - q[s] + i + 1, pre[s])))
+                assert (s, i, part) not in seen
+                seen.add((int(s), int(i), int(part)))
+        assert seen == {(s, i, k) for s, n_ in enumerate(lens) for i in range(n_)
+                        for k in range(parts(s, i // 128 * 128) if pass_ == 1 else 1)}
+        if pass_ == 1:
+            assert p.n_parts == max(k for _, _, k in seen) + 1
 
         def cost(s, a):
             if pass_ == 1:
-                return sum(1 for i in range(q[s]) if visible(s, i) > a)
+                a = a // 128 * 128
+                return sum(1 for i in range(q[s]) if visible(s, i) > a) // parts(s, a)
             return visible(s, min(a + step, q[s]) - 1)
         costs = [cost(int(s), int(a)) for s, a in items]
         assert all(x >= y for x, y in itertools.pairwise(costs))
