@@ -800,51 +800,70 @@ static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows&
 
 // ---------------------------------------------------------------------------
 // Head dim 256.  An accumulator is 256 columns, so the keys' pass is two, dK then dV, and
-// the outer tiles take 128 KB of shared memory, so an inner tile is 64 rows: S and dP are
-// 64 columns, double-buffered, and a tile's two scores are issued two tiles ahead of the
-// product that takes dS (or P), which the elementwise warps write over S.
-//   DK   S^T = K Q^T, dP^T = V dO^T, dK += dS^T Q
-//   DV   S^T = K Q^T, dV += P^T dO
-//   DQ   S = Q K^T, dP = dO V^T, dQ += dS K
+// the outer tiles take 64 KB of shared memory each.  The inner operand that a score and a
+// sum both read, or the sum alone, has one 64 KB slot, released in halves as the sum's two
+// products of 128 columns are through with them; the other streams through 16 KB units,
+// 64 columns of a tile.
+//   DK   S^T = K Q^T, dP^T = V dO^T, dK += dS^T Q       slot Q, units of dO
+//   DV   S^T = K Q^T, dV += P^T dO                      slot dO, units of Q
+//   DQ   S = Q K^T, dP = dO V^T, dQ += dS K             slot K, units of V
+// DK and DQ: S, dP and the accumulator fill TMEM; dP is read first, and the next one runs
+// while dS is formed, over S; then the sum and the next S.  DV: two S, issued two tiles
+// ahead.  (Tiles of 64 inner rows, double-buffered, left the tensor core at half:
+// a product of 128 x 64 x 16 from shared memory takes what one of 128 x 128 x 16 does.
+// 26 samples of up to 840 tokens, forward and gradients 242 -> 237 us, of which 41 forward; the
+// rest is bound by shared memory: 448 KB a tile of DK or DQ at some 100 bytes a clock.)
 // ---------------------------------------------------------------------------
 namespace pwide {
-constexpr int BM = 128, BN = 64, HD = 256, NCH = 4;
+constexpr int BM = 128, HD = 256, NCH = 4;
 enum { DK = 0, DV = 1, DQ = 2 };
-constexpr int OB = BM * HD * 2, IB = BN * HD * 2;
+constexpr int TILE = BM * HD * 2, UNIT = BM * 128;
+// shared memory: DK, DQ: two outer tiles, the slot, 2 units; DV: one, 6 units, the slot
+constexpr int OFF_ST = 3 * TILE + 2 * UNIT;  // -lse, -D [2][128]; DV: two slots of -lse
+constexpr int OFF_BAR = OFF_ST + 2 * BM * 4;
 // barriers of a pass
-enum { O_FULL = 0, O_EMPTY = 1, B1_FULL = 2, B1_EMPTY = 4, B2_FULL = 6, B2_EMPTY = 8, S_FULL = 10,
-       P_FULL = 12, ACC_FULL = 14, ACC_FREE = 15, DRAIN = 16, ST_FULL = 17, ST_EMPTY = 20, W_FULL = 23,
-       W_EMPTY = 25, N_BARS = 27 };
-constexpr int ST = 3;                    // slots of row values
-constexpr int OFF_B1 = 2 * OB;           // two slots
-constexpr int OFF_B2 = OFF_B1 + 2 * IB;  // one; DV has two in the second outer tile's place
-constexpr int OFF_ST = OFF_B2 + IB;      // [ST][-lse, -D][64]
-constexpr int OFF_BAR = OFF_ST + ST * 2 * BN * 4;
+enum { O_FULL = 0, O_EMPTY = 1, H_FULL = 2, H_EMPTY = 4, U_FULL = 6, U_EMPTY = 12, S_FULL = 18,
+       P_FULL = 20, ACC_FULL = 22, ACC_FREE = 23, DRAIN = 24, ST_FULL = 25, ST_EMPTY = 27, W_FULL = 29,
+       W_EMPTY = 31, DP_READ = 33, N_BARS = 34 };
 constexpr int SMEM = OFF_BAR + N_BARS * 8 + 80 + 1024;
 static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
 constexpr int THREADS = 384, EW = 8, READERS = 2 + EW;
-constexpr uint32_t S_COL = 0, DP_COL = 2 * BN, ACC_COL = 256;
+constexpr uint32_t S_COL = 0, DP_COL = 128, ACC_COL = 256;
 }  // namespace pwide
 
+// Four 16-byte units of each lane's row, turned over among lanes 4 k .. 4 k + 3: unit j of
+// lane l becomes unit l % 4 of row 4 (l / 4) + j, so that a store of unit j covers 64 bytes of
+// each of eight rows (16 bytes of 32 rows took a cycle a row: 8,400 clocks an item).
+__device__ __forceinline__ void turn_units(uint4 (&u)[4], int lane) {
+#pragma unroll
+    for (int b = 1; b < 4; b <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i & b) continue;
+            const bool up = lane & b;
+            uint4 t = up ? u[i] : u[i | b];
+            t.x = __shfl_xor_sync(0xffffffffu, t.x, b);
+            t.y = __shfl_xor_sync(0xffffffffu, t.y, b);
+            t.z = __shfl_xor_sync(0xffffffffu, t.z, b);
+            t.w = __shfl_xor_sync(0xffffffffu, t.w, b);
+            if (up) u[i] = t;
+            else u[i | b] = t;
+        }
+}
+
 template <int PASS>
-__device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, const CUtensorMap& tqi,
-                                                    const CUtensorMap& tko, const CUtensorMap& tki,
-                                                    const CUtensorMap& tvo, const CUtensorMap& tvi,
-                                                    const CUtensorMap& tdo, const CUtensorMap& tdi,
+__device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const CUtensorMap& tk,
+                                                    const CUtensorMap& tv, const CUtensorMap& tdo,
                                                     const PromptBwdArgs& p, uint8_t* sm, uint64_t* bar,
                                                     volatile int* fail_flag, uint32_t tbase,
                                                     int q_first, int claim) {
     using namespace pwide;
     constexpr bool KP = PASS != DQ, NEED_DP = PASS != DV;
-    // B1 holds a tile from its score to its product, so with two slots the next scores would
-    // wait for their whole load right behind each product: tiles go in pairs instead, two
-    // products, then two tiles' scores, whose loads have been under way since
-    constexpr bool PAIRED = NEED_DP;
-    constexpr int NB2 = NEED_DP ? 1 : 2;
-    const int T = tile_tokens(p.group), Ti = BN / p.group;  // tokens of outer and inner row tiles
+    constexpr int NUNIT = NEED_DP ? 2 : 6, NST = NEED_DP ? 1 : 2;
+    const int T = tile_tokens(p.group);
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    uint8_t* b1 = sm + OFF_B1;
-    uint8_t* b2 = sm + (NEED_DP ? OFF_B2 : OB);
+    uint8_t* sl = sm + (NEED_DP ? 2 * TILE : TILE + 6 * UNIT);
+    uint8_t* un = sm + (NEED_DP ? 3 * TILE : TILE);
     float* st = reinterpret_cast<float*>(sm + OFF_ST);
     volatile int* slot = fail_flag + 1;  // [2][8]: items handed out
     const int2* items = p.items + (KP ? 0 : p.n_keys);
@@ -868,13 +887,13 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
         ++seen;
         return x;
     };
-    // an item's inner tiles, and the keys pass's first inner row
+    // an item's inner tiles, and the keys' passes' first inner row
     auto inner = [&](const PromptBwdItem& x, int& i0, int& n) {
         if (KP) {
-            x.range(p.group, p.Hkv, Ti, i0, n);
+            x.range(p.group, p.Hkv, T, i0, n);
         } else {
             i0 = x.at;
-            n = (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BN - 1) / BN;
+            n = (keys_seen(min(x.at + T, x.Lq) - 1, x.Lq, x.Lk, x.pre) + BM - 1) / BM;
         }
     };
 
@@ -900,12 +919,8 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             ++told;
             return true;
         };
-        int no = 0;
-        uint32_t g1 = 0, g2 = 0;  // inner tiles loaded into each ring
-        auto load = [&](const CUtensorMap* m, uint8_t* dst, int rows, int head, int row, uint64_t* full) {
-#pragma unroll
-            for (int c = 0; c < NCH; ++c) tma_load_3d(dst + c * rows * 128, m, c * 64, head, row, full);
-        };
+        int no = 0;             // outer tiles loaded
+        uint32_t g = 0, u = 0;  // slot tiles, units loaded
         int2 e = make_int2(0, 0);
         PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0};
         auto fetch = [&]() {
@@ -921,7 +936,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             nx.Lk = p.cu_kv[e.x + 1] - nx.k0;
             nx.pre = p.prefix ? p.prefix[e.x] : 0;
         };
-        const uint32_t orow = p.group * T * HD * 2, irow = p.group * Ti * HD * 2;
+        const uint32_t row_bytes = p.group * T * 128;  // of 64 columns of a row tile
         fetch();
         while (claim - q_first < n_work) {
             if (__any_sync(0xffffffffu, *fail_flag)) {
@@ -943,101 +958,123 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             int i0, n;
             inner(x, i0, n);
             const int qh = x.kvh * p.group;
+            // columns [64 c, 64 c + 64) of inner tile j: of rows (m = Q or dO) or keys (K or V)
+            auto rows_in = [&](const CUtensorMap* m, uint8_t* dst, int c, int j, uint64_t* full) {
+                tma_load_3d(dst, m, c * 64, qh, x.q0 + i0 + j * T, full);
+            };
+            auto keys_in = [&](const CUtensorMap* m, uint8_t* dst, int c, int j, uint64_t* full) {
+                tma_load_3d(dst, m, c * 64, x.kvh, x.k0 + j * BM, full);
+            };
+            auto load_slot = [&](int j) -> bool {
+                for (int h = 0; h < 2; ++h) {
+                    if (!mbar_wait_warp(&bar[H_EMPTY + h], (g & 1) ^ 1)) return false;
+                    if (elect_one()) {
+                        uint64_t* full = &bar[H_FULL + h];
+                        mbar_arrive_expect_tx(full, KP ? 2 * row_bytes : 2 * UNIT);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int c = 2 * h + k;
+                            if (PASS == DQ) keys_in(&tk, sl + c * UNIT, c, j, full);
+                            else rows_in(PASS == DK ? &tq : &tdo, sl + c * UNIT, c, j, full);
+                        }
+                    }
+                    __syncwarp();
+                }
+                ++g;
+                return true;
+            };
+            auto load_units = [&](int j, int c0, int c1) -> bool {
+                for (int c = c0; c < c1; ++c, ++u) {
+                    const int b = u % NUNIT;
+                    if (!mbar_wait_warp(&bar[U_EMPTY + b], ((u / NUNIT) & 1) ^ 1)) return false;
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(&bar[U_FULL + b], KP ? row_bytes : UNIT);
+                        if (PASS == DQ) keys_in(&tv, un + b * UNIT, c, j, &bar[U_FULL + b]);
+                        else rows_in(PASS == DK ? &tdo : &tq, un + b * UNIT, c, j, &bar[U_FULL + b]);
+                    }
+                    __syncwarp();
+                }
+                return true;
+            };
             if (n > 0) {
                 if (no > 0 && !(ok = mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1))) break;
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&bar[O_FULL],
-                                          PASS == DK ? 2 * OB : PASS == DV ? OB : 2 * orow);
-                    if (KP) {
-                        load(&tko, sm, BM, x.kvh, x.k0 + x.at, &bar[O_FULL]);
-                        if (NEED_DP) load(&tvo, sm + OB, BM, x.kvh, x.k0 + x.at, &bar[O_FULL]);
-                    } else {
-                        load(&tqo, sm, BM, qh, x.q0 + x.at, &bar[O_FULL]);
-                        load(&tdo, sm + OB, BM, qh, x.q0 + x.at, &bar[O_FULL]);
+                    mbar_arrive_expect_tx(&bar[O_FULL], PASS == DK   ? 2 * TILE
+                                                        : PASS == DV ? TILE
+                                                                     : 8 * row_bytes);
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c) {
+                        if (KP) {
+                            tma_load_3d(sm + c * UNIT, &tk, c * 64, x.kvh, x.k0 + x.at, &bar[O_FULL]);
+                            if (NEED_DP)
+                                tma_load_3d(sm + TILE + c * UNIT, &tv, c * 64, x.kvh, x.k0 + x.at,
+                                            &bar[O_FULL]);
+                        } else {
+                            tma_load_3d(sm + c * UNIT, &tq, c * 64, qh, x.q0 + x.at, &bar[O_FULL]);
+                            tma_load_3d(sm + TILE + c * UNIT, &tdo, c * 64, qh, x.q0 + x.at, &bar[O_FULL]);
+                        }
                     }
                 }
                 __syncwarp();
                 ++no;
             }
-            for (int j = 0; j < n && ok; ++j) {
-                const int s1 = g1 & 1, s2 = g2 % NB2;
-                if (!(ok = mbar_wait_warp(&bar[B1_EMPTY + s1], ((g1 >> 1) & 1) ^ 1))) break;
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(&bar[B1_FULL + s1], KP ? irow : IB);
-                    if (KP) load(&tqi, b1 + s1 * IB, BN, qh, x.q0 + i0 + j * Ti, &bar[B1_FULL + s1]);
-                    else load(&tki, b1 + s1 * IB, BN, x.kvh, x.k0 + j * BN, &bar[B1_FULL + s1]);
+            // in the order the MMAs take them: DV's scores run two tiles ahead
+            if (PASS == DV) {
+                for (int j = 0; j < 2 && j < n && ok; ++j) ok = load_units(j, 0, NCH);
+                for (int j = 0; j < n && ok; ++j) {
+                    ok = load_slot(j);
+                    if (ok && j + 2 < n) ok = load_units(j + 2, 0, NCH);
                 }
-                __syncwarp();
-                ++g1;
-                if (!(ok = mbar_wait_warp(&bar[B2_EMPTY + s2], ((g2 / NB2) & 1) ^ 1))) break;
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(&bar[B2_FULL + s2], KP ? irow : IB);
-                    if (KP) load(&tdi, b2 + s2 * IB, BN, qh, x.q0 + i0 + j * Ti, &bar[B2_FULL + s2]);
-                    else load(&tvi, b2 + s2 * IB, BN, x.kvh, x.k0 + j * BN, &bar[B2_FULL + s2]);
-                }
-                __syncwarp();
-                ++g2;
+            } else {
+                ok = n == 0 || (load_units(0, 0, NUNIT) && load_slot(0) && load_units(0, NUNIT, NCH));
+                for (int j = 1; j < n && ok; ++j) ok = load_units(j, 0, NCH) && load_slot(j);
             }
             if (!ok) break;
             fetch();
         }
         ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0});
         if (!ok) *fail_flag = 1;
-        // every copy has landed before the pass ends (at once in a normal run)
-        if (no > 0) mbar_wait_warp(&bar[O_FULL], (no - 1) & 1, 100000000LL);
-        for (uint32_t i = g1 > 2 ? g1 - 2 : 0; i < g1; ++i)
-            mbar_wait_warp(&bar[B1_FULL + (i & 1)], (i >> 1) & 1, 100000000LL);
-        for (uint32_t i = g2 > NB2 ? g2 - NB2 : 0; i < g2; ++i)
-            mbar_wait_warp(&bar[B2_FULL + i % NB2], (i / NB2) & 1, 100000000LL);
-        // ... and every release has arrived before the barriers are made anew
-        if (no > 0) mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1, 100000000LL);
-        for (uint32_t i = g1 > 2 ? g1 - 2 : 0; i < g1; ++i)
-            mbar_wait_warp(&bar[B1_EMPTY + (i & 1)], (i >> 1) & 1, 100000000LL);
-        for (uint32_t i = g2 > NB2 ? g2 - NB2 : 0; i < g2; ++i)
-            mbar_wait_warp(&bar[B2_EMPTY + i % NB2], (i / NB2) & 1, 100000000LL);
+        // every copy has landed, and every release has arrived, before the barriers are made anew
+        if (no > 0) {
+            mbar_wait_warp(&bar[O_FULL], (no - 1) & 1, 100000000LL);
+            mbar_wait_warp(&bar[O_EMPTY], (no - 1) & 1, 100000000LL);
+        }
+        for (int h = 0; h < 2 && g > 0; ++h) {
+            mbar_wait_warp(&bar[H_FULL + h], (g - 1) & 1, 100000000LL);
+            mbar_wait_warp(&bar[H_EMPTY + h], (g - 1) & 1, 100000000LL);
+        }
+        for (uint32_t i = u > NUNIT ? u - NUNIT : 0; i < u; ++i) {
+            mbar_wait_warp(&bar[U_FULL + i % NUNIT], (i / NUNIT) & 1, 100000000LL);
+            mbar_wait_warp(&bar[U_EMPTY + i % NUNIT], (i / NUNIT) & 1, 100000000LL);
+        }
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
-        constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
-        constexpr uint32_t IDESC_ACC = idesc_bf16_f32(BM, HD) | (1u << 16);  // B MN-major
+        constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BM);
+        constexpr uint32_t IDESC_ACC = idesc_bf16_f32(BM, 128) | (1u << 16);  // B MN-major
         bool ok = true, issued = false;
         int no = 0, done = 0;
-        uint32_t c1 = 0, c2 = 0;          // tiles of B1 / B2 taken by scores
-        uint32_t a1 = 0, a2 = 0;          // ... by the sums
-        uint32_t gs = 0, gp = 0;          // scores issued, P / dS tiles taken
-        const uint32_t o1 = smem_u32(sm), o2 = o1 + OB;
+        uint32_t g = 0, u = 0, gs = 0, gp = 0;  // slot tiles, units, scores, P / dS taken
+        const uint32_t o1 = smem_u32(sm), o2 = o1 + TILE;
         auto commit = [&](uint64_t* b) {
             if (elect_one()) tc_commit(b);
             __syncwarp();
         };
-        auto score = [&](uint32_t d, uint32_t outer, uint8_t* inner) {
-            const uint32_t a_lo = sw128_desc_lo(outer), b_lo = sw128_desc_lo(smem_u32(inner));
+        // 64 columns of the contraction: chunk c of the outer tile at o with the inner's at b
+        auto score = [&](uint32_t d, uint32_t o, int c, uint8_t* b) {
+            const uint32_t a_lo = sw128_desc_lo(o + c * UNIT), b_lo = sw128_desc_lo(smem_u32(b));
             if (elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < HD / 16; ++ks)
-                    tc_mma_f16(d, desc_of(a_lo + (ks >> 2) * BM * 8 + (ks & 3) * 2, kSw128DescHi),
-                               desc_of(b_lo + (ks >> 2) * BN * 8 + (ks & 3) * 2, kSw128DescHi), IDESC_S,
-                               ks > 0);
+                for (int ks = 0; ks < 4; ++ks)
+                    tc_mma_f16(d, desc_of(a_lo + 2 * ks, kSw128DescHi), desc_of(b_lo + 2 * ks, kSw128DescHi),
+                               IDESC_S, (c | ks) != 0);
             }
             __syncwarp();
             issued = true;
         };
-        auto gather = [&](uint32_t x, uint8_t* inner, bool accumulate) {
-            const uint32_t b = smem_u32(inner);
-            if (elect_one()) {
-#pragma unroll
-                for (int ks = 0; ks < BN / 16; ++ks)
-                    tc_mma_f16_ts(tbase + ACC_COL, x + (ks >> 1) * 32 + (ks & 1) * 8,
-                                  sw128_desc_mn(b + ks * 16 * 128, BN * 128, 1024), IDESC_ACC,
-                                  accumulate || ks > 0);
-            }
-            __syncwarp();
-        };
-        auto zero_tail = [&](uint8_t* tile, int valid, int end) {
-            for (int i = lane; i < (end - valid) * (HD / 8); i += 32) {
-                const int r = valid + i / (HD / 8), u = i % (HD / 8);
-                *reinterpret_cast<uint4*>(tile + (u >> 3) * BN * 128 + r * 128 + (u & 7) * 16) =
+        auto zero_tail = [&](uint8_t* chunk, int valid, int end) {
+            for (int i = lane; i < (end - valid) * 8; i += 32)
+                *reinterpret_cast<uint4*>(chunk + (valid + (i >> 3)) * 128 + (i & 7) * 16) =
                     make_uint4(0, 0, 0, 0);
-            }
             fence_proxy_async();
             __syncwarp();
         };
@@ -1049,61 +1086,81 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             if (n == 0) continue;
             if (!(ok = mbar_wait_warp(&bar[O_FULL], no & 1))) break;
             ++no;
-            tc_fence_after();
-            const int box = KP ? p.group * Ti : BN;
+            const int box = KP ? p.group * T : BM;
             auto valid = [&](int j) {
-                return KP ? min(Ti, x.Lq - i0 - j * Ti) * p.group : min(BN, x.Lk - j * BN);
+                return KP ? min(T, x.Lq - i0 - j * T) * p.group : min(BM, x.Lk - j * BM);
             };
-            auto scores = [&](int j) -> bool {
-                const uint32_t b = gs & 1;
-                const int s1 = c1 & 1, s2 = c2 % NB2;
-                if (!mbar_wait_warp(&bar[B1_FULL + s1], (c1 >> 1) & 1)) return false;
-                if (valid(j) < box) zero_tail(b1 + s1 * IB, valid(j), box);
+            // the slot's half h of tile j is there
+            auto wait_half = [&](int h, int j) -> bool {
+                if (!mbar_wait_warp(&bar[H_FULL + h], g & 1)) return false;
+                if (valid(j) < box)
+                    for (int k = 0; k < 2; ++k) zero_tail(sl + (2 * h + k) * UNIT, valid(j), box);
                 tc_fence_after();
-                score(tbase + S_COL + b * BN, o1, b1 + s1 * IB);
-                if (PASS == DV) commit(&bar[B1_EMPTY + s1]);
-                ++c1;
-                if (NEED_DP) {
-                    if (!mbar_wait_warp(&bar[B2_FULL + s2], (c2 / NB2) & 1)) return false;
-                    if (KP && valid(j) < box) zero_tail(b2 + s2 * IB, valid(j), box);
-                    tc_fence_after();
-                    score(tbase + DP_COL + b * BN, o2, b2 + s2 * IB);
-                    commit(&bar[B2_EMPTY + s2]);
-                    ++c2;
-                }
-                commit(&bar[S_FULL + b]);
-                ++gs;
                 return true;
             };
-            ok = scores(0) && (n < 2 || scores(1));
-            int ns = min(n, 2);
-            if (ok && ns == n) commit(&bar[O_EMPTY]);
-            for (int j = 0; j < n && ok; ++j) {
-                const uint32_t b = gp & 1;
-                if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (gp >> 1) & 1))) break;
-                ++gp;
+            auto from_units = [&](uint32_t d, uint32_t o, int j) -> bool {
+                for (int c = 0; c < NCH; ++c, ++u) {
+                    const int b = u % NUNIT;
+                    if (!mbar_wait_warp(&bar[U_FULL + b], (u / NUNIT) & 1)) return false;
+                    if (KP && valid(j) < box) zero_tail(un + b * UNIT, valid(j), box);
+                    tc_fence_after();
+                    score(d, o, c, un + b * UNIT);
+                    commit(&bar[U_EMPTY + b]);
+                }
+                return true;
+            };
+            auto next_scores = [&](int j) -> bool {
+                if constexpr (NEED_DP) {
+                    for (int h = 0; h < 2; ++h) {
+                        if (!wait_half(h, j)) return false;
+                        for (int k = 0; k < 2; ++k)
+                            score(tbase + S_COL, o1, 2 * h + k, sl + (2 * h + k) * UNIT);
+                    }
+                    commit(&bar[S_FULL]);
+                } else {
+                    if (!from_units(tbase + S_COL + (gs & 1) * BM, o1, j)) return false;
+                    commit(&bar[S_FULL + (gs & 1)]);
+                }
+                ++gs;
+                if (j + 1 == n) commit(&bar[O_EMPTY]);
+                return true;
+            };
+            // acc += X B over the slot's 128 rows, X bf16 in TMEM: 64 rows at column xc, 64 at
+            // xc + 64
+            auto gather = [&](int h, uint32_t xc, bool accumulate) {
+                const uint32_t b = smem_u32(sl + 2 * h * UNIT);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < BM / 16; ++ks)
+                        tc_mma_f16_ts(tbase + ACC_COL + h * 128, xc + (ks >> 2) * 64 + (ks & 3) * 8,
+                                      sw128_desc_mn(b + ks * 16 * 128, UNIT, 1024), IDESC_ACC,
+                                      accumulate || ks > 0);
+                    tc_commit(&bar[H_EMPTY + h]);
+                }
+                __syncwarp();
+            };
+            if (NEED_DP && !(ok = from_units(tbase + DP_COL, o2, 0))) break;
+            ok = next_scores(0) && (NEED_DP || n < 2 || next_scores(1));
+            for (int j = 0; j < n && ok; ++j, ++gp, ++g) {
+                const uint32_t b = NEED_DP ? 0 : gp & 1, ph = NEED_DP ? gp & 1 : (gp >> 1) & 1;
+                if (PASS == DV && !(ok = wait_half(0, j) && wait_half(1, j))) break;
+                // the next dP, while dS is formed of this one, which has been read
+                if (NEED_DP && j + 1 < n &&
+                    !(ok = mbar_wait_warp(&bar[DP_READ], gp & 1) && from_units(tbase + DP_COL, o2, j + 1)))
+                    break;
+                if (!(ok = mbar_wait_warp(&bar[P_FULL + b], ph))) break;
                 // the item's first product overwrites the sums: the last epilogue has read them
                 if (j == 0 && done > 0 && !(ok = mbar_wait_warp(&bar[ACC_FREE], (done - 1) & 1))) break;
-                if (PASS == DV) {
-                    const int s2 = a2 % NB2;
-                    if (!(ok = mbar_wait_warp(&bar[B2_FULL + s2], (a2 / NB2) & 1))) break;
-                    if (valid(j) < box) zero_tail(b2 + s2 * IB, valid(j), box);
-                    tc_fence_after();
-                    gather(tbase + S_COL + b * BN, b2 + s2 * IB, j > 0);
-                    commit(&bar[B2_EMPTY + s2]);
-                    ++a2;
-                } else {
-                    tc_fence_after();
-                    gather(tbase + S_COL + b * BN, b1 + (a1 & 1) * IB, j > 0);
-                    commit(&bar[B1_EMPTY + (a1 & 1)]);
-                    ++a1;
-                }
-                // scores of tile j + 2 reuse buffer b: the products above have read it, the
-                // tensor core running this thread's MMAs in issue order
-                const int upto = !PAIRED || (j & 1) ? j + 3 : 0;
-                for (; ok && ns < min(upto, n); ++ns) {
-                    ok = scores(ns);
-                    if (ok && ns + 1 == n) commit(&bar[O_EMPTY]);
+                tc_fence_after();
+                for (int h = 0; h < 2; ++h) gather(h, tbase + S_COL + b * BM, j > 0);
+                if (NEED_DP) {
+                    if (j + 1 < n) {
+                        ++g;
+                        ok = next_scores(j + 1);
+                        --g;
+                    }
+                } else if (j + 2 < n) {
+                    ok = next_scores(j + 2);
                 }
             }
             if (!ok) break;
@@ -1126,21 +1183,20 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
             int i0, n;
             inner(x, i0, n);
             for (int j = 0; j < n; ++j, ++g) {
-                const int b = g % ST;
-                float2 v[2];
+                const int b = g % NST;
+                float2 v[4];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = e * 32 + lane, t = r / p.group, i = i0 + j * Ti + t;
-                    const bool live = t < Ti && i < x.Lq;
-                    v[e] = live ? p.row[((size_t)x.kvh * p.rows + x.q0 + i0 + j * Ti) * p.group + r]
+                for (int e = 0; e < 4; ++e) {
+                    const int r = e * 32 + lane, t = r / p.group, i = i0 + j * T + t;
+                    const bool live = t < T && i < x.Lq;
+                    v[e] = live ? p.row[((size_t)x.kvh * p.rows + x.q0 + i0 + j * T) * p.group + r]
                                 : make_float2(INFINITY, 0.f);
                 }
-                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g / ST) & 1) ^ 1))) break;
+                if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g / NST) & 1) ^ 1))) break;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = e * 32 + lane;
-                    st[b * 128 + r] = -v[e].x;
-                    st[b * 128 + 64 + r] = -v[e].y;
+                for (int e = 0; e < 4; ++e) {
+                    st[b * 128 + e * 32 + lane] = -v[e].x;
+                    if (NEED_DP) st[128 + e * 32 + lane] = -v[e].y;
                 }
                 mbar_arrive(&bar[ST_FULL + b]);
             }
@@ -1173,65 +1229,80 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                 lim = keys_seen(i, x.Lq, x.Lk, x.pre);
             }
             for (int j = 0; j < n; ++j, ++g) {
-                const float* sv = st + g % ST * 128 + half * 32;
-                const uint32_t b = g & 1, ph = (g >> 1) & 1;
-                const uint32_t tS = tbase + lane_base + S_COL + b * BN + half * 32;
-                const uint32_t tP = tbase + lane_base + DP_COL + b * BN + half * 32;
+                const uint32_t b = NEED_DP ? 0 : g & 1, ph = NEED_DP ? g & 1 : (g >> 1) & 1;
+                const float* sv = st + (NEED_DP ? 0 : b * 128) + half * 64;
+                const uint32_t tS = tbase + lane_base + S_COL + b * BM + half * 64;
+                const uint32_t tP = tbase + lane_base + DP_COL + half * 64;
                 bool whole;
                 if (KP) {
-                    whole = keys_seen(min(i0 + j * Ti, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
+                    whole = keys_seen(min(i0 + j * T, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
                             min(x.at + BM, x.Lk);
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + g % ST], (g / ST) & 1)))) break;
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + b], ph)))) break;
                 } else {
-                    whole = __all_sync(0xffffffffu, lim >= (j + 1) * BN);
+                    whole = __all_sync(0xffffffffu, lim >= (j + 1) * BM);
                 }
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[S_FULL + b], ph)))) break;
                 tc_fence_after();
-                uint32_t s[32], d[32], pk[16];
-                tmem_ld32(tS, s);
-                if (NEED_DP) tmem_ld32(tP, d);
-                tmem_ld_wait_regs(s);
-                if (NEED_DP) tmem_ld_wait_regs(d);
                 const uint64_t c2 = f2_pack(p.scale_log2, p.scale_log2);
-                // columns that count: [0, hi) of a query, [lo, 32) of a key
-                const int lo = from - j * Ti * p.group - half * 32, hi = lim - j * BN - half * 32;
+                uint32_t pk[32], dp[2][32];
+                if (NEED_DP) {
+                    tmem_ld32(tP, dp[0]);
+                    tmem_ld32(tP + 32, dp[1]);
+                    tmem_ld_wait_regs(dp[0]);
+                    tmem_ld_wait_regs(dp[1]);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (elect_one()) mbar_arrive(&bar[DP_READ]);
+                    __syncwarp();
+                }
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    float4 l4 = make_float4(nlse, nlse, nlse, nlse), d4 = make_float4(nD, nD, nD, nD);
-                    if (KP) {
-                        l4 = *reinterpret_cast<const float4*>(sv + e);
-                        if (NEED_DP) d4 = *reinterpret_cast<const float4*>(sv + 64 + e);
-                    }
-                    const uint64_t l2[2] = {f2_pack(l4.x, l4.y), f2_pack(l4.z, l4.w)};
-                    const uint64_t d2[2] = {f2_pack(d4.x, d4.y), f2_pack(d4.z, d4.w)};
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t s[32];
+                    uint32_t(&d)[32] = dp[c];
+                    tmem_ld32(tS + c * 32, s);
+                    tmem_ld_wait_regs(s);
+                    // columns that count: [0, hi) of a query, [lo, 32) of a key
+                    const int lo = from - j * T * p.group - half * 64 - c * 32;
+                    const int hi = lim - j * BM - half * 64 - c * 32;
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int k = e + 2 * u;
-                        float a, b;
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2,
-                                         l2[u]),
-                                  a, b);
-                        a = ex2_approx(a);
-                        b = ex2_approx(b);
-                        if (NEED_DP)
-                            f2_unpack(f2_mul(f2_pack(a, b),
-                                             f2_add(f2_pack(__uint_as_float(d[k]), __uint_as_float(d[k + 1])),
-                                                    d2[u])),
-                                      a, b);
-                        if (!whole) {
-                            if (KP ? k < lo : k >= hi) a = 0.f;
-                            if (KP ? k + 1 < lo : k + 1 >= hi) b = 0.f;
+                    for (int e = 0; e < 32; e += 4) {
+                        float4 l4 = make_float4(nlse, nlse, nlse, nlse), d4 = make_float4(nD, nD, nD, nD);
+                        if (KP) {
+                            l4 = *reinterpret_cast<const float4*>(sv + c * 32 + e);
+                            if (NEED_DP) d4 = *reinterpret_cast<const float4*>(sv + 128 + c * 32 + e);
                         }
-                        pk[k / 2] = cvt_bf2(a, b);
+                        const uint64_t l2[2] = {f2_pack(l4.x, l4.y), f2_pack(l4.z, l4.w)};
+                        const uint64_t d2[2] = {f2_pack(d4.x, d4.y), f2_pack(d4.z, d4.w)};
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            const int k = e + 2 * w;
+                            float a0, a1;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2,
+                                             l2[w]),
+                                      a0, a1);
+                            a0 = ex2_approx(a0);
+                            a1 = ex2_approx(a1);
+                            if (NEED_DP)
+                                f2_unpack(f2_mul(f2_pack(a0, a1),
+                                                 f2_add(f2_pack(__uint_as_float(d[k]),
+                                                                __uint_as_float(d[k + 1])),
+                                                        d2[w])),
+                                          a0, a1);
+                            if (!whole) {
+                                if (KP ? k < lo : k >= hi) a0 = 0.f;
+                                if (KP ? k + 1 < lo : k + 1 >= hi) a1 = 0.f;
+                            }
+                            pk[c * 16 + k / 2] = cvt_bf2(a0, a1);
+                        }
                     }
                 }
-                tmem_st16(tS, pk);
+                tmem_st32(tS, pk);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (elect_one()) {
                     mbar_arrive(&bar[P_FULL + b]);
-                    if (KP) mbar_arrive(&bar[ST_EMPTY + g % ST]);
+                    if (KP) mbar_arrive(&bar[ST_EMPTY + b]);
                 }
                 __syncwarp();
             }
@@ -1242,42 +1313,56 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
                 ++done;
             }
             const float f = PASS == DV ? 1.f : p.scale;
-            uint16_t* o;
-            if (KP) {
-                const jnx_head_rows& to = PASS == DV ? p.dv : p.dk;
-                o = to.ptr + (long long)(x.k0 + key) * to.row_stride + x.kvh * to.head_stride;
-            } else {
-                o = p.dq.ptr + (long long)(x.q0 + i) * p.dq.row_stride +
-                    (x.kvh * p.group + hg) * p.dq.head_stride;
-            }
-            o += half * (HD / 2);
+            const jnx_head_rows& to = PASS == DQ ? p.dq : PASS == DV ? p.dv : p.dk;
             // a tile taken in parts: its sums' row
             const bool in_parts = KP && x.parts(p.group, p.Hkv) > 1;
-            float* part = p.part + (x.part + (PASS == DV ? p.n_parts : 0)) * p.part_stride +
-                          ((long long)(x.k0 + key) * p.Hkv + x.kvh) * HD + half * (HD / 2);
+            float* part = p.part + (x.part + (PASS == DV ? p.n_parts : 0)) * p.part_stride;
+            const long long row = !live      ? -1
+                                  : in_parts ? ((long long)(x.k0 + key) * p.Hkv + x.kvh) * HD
+                                  : KP       ? (x.k0 + key) * to.row_stride + x.kvh * to.head_stride
+                                             : (x.q0 + i) * to.row_stride +
+                                                   (x.kvh * p.group + hg) * to.head_stride;
+            long long at[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) at[k] = __shfl_sync(0xffffffffu, row, (lane & ~3) + k);
 #pragma unroll 1
             for (int c = 0; c < HD / 64; ++c) {
+                const int col = half * (HD / 2) + c * 32;
                 uint32_t v[32];
                 if (n > 0) {
-                    tmem_ld32(tbase + lane_base + ACC_COL + half * (HD / 2) + c * 32, v);
+                    tmem_ld32(tbase + lane_base + ACC_COL + col, v);
                     tmem_ld_wait_regs(v);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0;
                 }
-                if (live && in_parts) {
+                uint4 u[4];
+                if (in_parts) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        *reinterpret_cast<uint4*>(part + c * 32 + e * 4) =
-                            make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-                } else if (live) {
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            u[e] = make_uint4(v[16 * h + 4 * e], v[16 * h + 4 * e + 1],
+                                              v[16 * h + 4 * e + 2], v[16 * h + 4 * e + 3]);
+                        turn_units(u, lane);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (at[k] >= 0)
+                                *reinterpret_cast<uint4*>(part + at[k] + col + 16 * h + (lane & 3) * 4) = u[k];
+                    }
+                } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<uint4*>(o + c * 32 + e * 8) = make_uint4(
+                        u[e] = make_uint4(
                             cvt_bf2(f * __uint_as_float(v[8 * e]), f * __uint_as_float(v[8 * e + 1])),
                             cvt_bf2(f * __uint_as_float(v[8 * e + 2]), f * __uint_as_float(v[8 * e + 3])),
                             cvt_bf2(f * __uint_as_float(v[8 * e + 4]), f * __uint_as_float(v[8 * e + 5])),
                             cvt_bf2(f * __uint_as_float(v[8 * e + 6]), f * __uint_as_float(v[8 * e + 7])));
+                    turn_units(u, lane);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (at[k] >= 0)
+                            *reinterpret_cast<uint4*>(to.ptr + at[k] + col + (lane & 3) * 8) = u[k];
                 }
             }
             if (n > 0) {
@@ -1293,10 +1378,8 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tqo, cons
 }
 
 __global__ void __launch_bounds__(pwide::THREADS, 1)
-    k_prompt_attn_bwd_wide(const __grid_constant__ CUtensorMap tqo, const __grid_constant__ CUtensorMap tqi,
-                           const __grid_constant__ CUtensorMap tko, const __grid_constant__ CUtensorMap tki,
-                           const __grid_constant__ CUtensorMap tvo, const __grid_constant__ CUtensorMap tvi,
-                           const __grid_constant__ CUtensorMap tdo, const __grid_constant__ CUtensorMap tdi,
+    k_prompt_attn_bwd_wide(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+                           const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap tdo,
                            const __grid_constant__ PromptBwdArgs p) {
     using namespace pwide;
     extern __shared__ uint8_t smem_raw[];
@@ -1313,29 +1396,36 @@ __global__ void __launch_bounds__(pwide::THREADS, 1)
                 mbar_init(&bar[i], i == P_FULL || i == P_FULL + 1 || i == ACC_FREE ? EW
                                    : i >= ST_EMPTY && i < W_FULL                   ? EW
                                    : i >= ST_FULL && i < ST_EMPTY                  ? 32
-                                   : i >= W_EMPTY                                  ? READERS
+                                   : i >= W_EMPTY && i < DP_READ                   ? READERS
+                                   : i == DP_READ                                  ? EW
                                                                                    : 1);
             }
             fence_barrier_init();
         }
     };
-    // inner rows that no box reaches (64 no multiple of the group) are zero in the keys'
-    // passes: all slots, and what DV puts in the second outer tile's place
-    const int box = p.group * (BN / p.group);
-    auto zero_rows = [&](uint8_t* at, int tiles) {
-        for (int i = threadIdx.x; i < tiles * NCH * (BN - box) * 8; i += THREADS) {
-            const int u = i & 7, r = box + (i >> 3) % (BN - box), t = (i >> 3) / (BN - box);
-            *reinterpret_cast<uint4*>(at + t * BN * 128 + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+    // inner rows that no box reaches (128 no multiple of the group) are zero in the keys'
+    // passes
+    const int box = p.group * tile_tokens(p.group);
+    auto zero_rows = [&](uint8_t* at, int chunks) {
+        for (int i = threadIdx.x; i < chunks * (BM - box) * 8; i += THREADS) {
+            const int u = i & 7, r = box + (i >> 3) % (BM - box), t = (i >> 3) / (BM - box);
+            *reinterpret_cast<uint4*>(at + t * UNIT + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async();
     };
     init_bars(false);
     if (threadIdx.x == 0) *fail_flag = 0;
-    zero_rows(sm + OFF_B1, 3);
+    zero_rows(sm + 2 * TILE, NCH + 2);
     pdl_entry();  // TMEM is taken once the grid ahead has given its own back
     if (warp == 1) {
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
+    }
+    if (threadIdx.x == 0) {
+        tma_prefetch_desc(&tq);
+        tma_prefetch_desc(&tk);
+        tma_prefetch_desc(&tv);
+        tma_prefetch_desc(&tdo);
     }
     tc_fence_before();
     __syncthreads();
@@ -1351,20 +1441,17 @@ __global__ void __launch_bounds__(pwide::THREADS, 1)
         tc_fence_after();
     };
     const int nk = p.n_keys * p.Hkv;
-    int claim = prompt_bwd_wide_pass<DK>(tqo, tqi, tko, tki, tvo, tvi, tdo, tdi, p, sm, bar, fail_flag,
-                                         tbase, 0, blockIdx.x);
+    int claim = prompt_bwd_wide_pass<DK>(tq, tk, tv, tdo, p, sm, bar, fail_flag, tbase, 0, blockIdx.x);
     end_pass();
-    zero_rows(sm + OB, 2);
+    zero_rows(sm + TILE, NCH);  // DV's units lie where V was
     __syncthreads();
     if (!failed) {
-        claim = prompt_bwd_wide_pass<DV>(tqo, tqi, tko, tki, tvo, tvi, tdo, tdi, p, sm, bar, fail_flag,
-                                         tbase, nk, claim);
+        claim = prompt_bwd_wide_pass<DV>(tq, tk, tv, tdo, p, sm, bar, fail_flag, tbase, nk, claim);
         end_pass();
         __syncthreads();
     }
     if (!failed) {
-        prompt_bwd_wide_pass<DQ>(tqo, tqi, tko, tki, tvo, tvi, tdo, tdi, p, sm, bar, fail_flag, tbase,
-                                 2 * nk, claim);
+        prompt_bwd_wide_pass<DQ>(tq, tk, tv, tdo, p, sm, bar, fail_flag, tbase, 2 * nk, claim);
         __syncwarp();
         tc_fence_before();
         failed = __syncthreads_or(*fail_flag);
@@ -1382,19 +1469,15 @@ static jnx_status launch_prompt_bwd_wide(const PromptBwdArgs& a, const jnx_head_
     static std::atomic<uint64_t> attr{0};
     if (set_smem_limit(reinterpret_cast<const void*>(k_prompt_attn_bwd_wide), SMEM, attr) != cudaSuccess)
         return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
-    const int T = tile_tokens(a.group), Ti = BN / a.group;
-    CUtensorMap m[8];
-    if (!make_tmap_heads(&m[0], q, rows, a.H, HD, a.group, T) ||
-        !make_tmap_heads(&m[1], q, rows, a.H, HD, a.group, Ti) ||
-        !make_tmap_heads(&m[2], k, keys, a.Hkv, HD, 1, BM) ||
-        !make_tmap_heads(&m[3], k, keys, a.Hkv, HD, 1, BN) ||
-        !make_tmap_heads(&m[4], v, keys, a.Hkv, HD, 1, BM) ||
-        !make_tmap_heads(&m[5], v, keys, a.Hkv, HD, 1, BN) ||
-        !make_tmap_heads(&m[6], dout, rows, a.H, HD, a.group, T) ||
-        !make_tmap_heads(&m[7], dout, rows, a.H, HD, a.group, Ti))
+    const int T = tile_tokens(a.group);
+    CUtensorMap tq, tk, tv, tdo;
+    if (!make_tmap_heads(&tq, q, rows, a.H, HD, a.group, T) ||
+        !make_tmap_heads(&tdo, dout, rows, a.H, HD, a.group, T) ||
+        !make_tmap_heads(&tk, k, keys, a.Hkv, HD, 1, BM) ||
+        !make_tmap_heads(&tv, v, keys, a.Hkv, HD, 1, BM))
         return fail(JNX_ERR_CUDA, "%s: tensor map encode failed", what);
     const int grid = (int)std::min<long long>(((long long)2 * a.n_keys + a.n_queries) * a.Hkv, num_sms());
-    pdl(k_prompt_attn_bwd_wide, grid, THREADS, SMEM, s)(m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], a);
+    pdl(k_prompt_attn_bwd_wide, grid, THREADS, SMEM, s)(tq, tk, tv, tdo, a);
     return launched(what);
 }
 
