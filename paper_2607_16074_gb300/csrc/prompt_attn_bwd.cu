@@ -29,6 +29,7 @@
 // Inner rows past a sequence's end belong to others and may be NaN: they are zeroed in
 // shared memory, and their lse is +inf, which makes their probabilities zero.
 #include <algorithm>
+#include <type_traits>
 
 #include "jnx_dev.cuh"
 #include "jnx_kernels.h"
@@ -100,36 +101,110 @@ struct PromptBwdItem {
     }
 };
 
-// The rows' (lse, D), and the claim counter to zero.  A warp a (row, head).
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    float d = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        d += __uint_as_float(x[e] << 16) * __uint_as_float(y[e] << 16) +
+             __uint_as_float(x[e] & 0xffff0000u) * __uint_as_float(y[e] & 0xffff0000u);
+    return d;
+}
+__device__ __forceinline__ uint4 head_unit(const jnx_head_rows& r, long long at, int head, int c) {
+    return *reinterpret_cast<const uint4*>(r.ptr + at * r.row_stride + head * r.head_stride + c);
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float d) {
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    return d;
+}
+
+// The rows' (lse, D = rowsum(dO * O)), and the claim counter to zero.  HD / 8 lanes a row,
+// four rows of neighbouring heads a lane, whose loads are under way at once.  Bound by HBM.
+// (By tiles of a sequence and key head, 256 bytes a row: 52 us for 7,000 rows of 32 heads;
+// as they lie MEASUREDROWS.)
+template <int HD>
 __global__ void __launch_bounds__(256)
-    k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, const float* lse, int rows, int H,
-                      int group, int hd, float2* row, int* claimed) {
+    k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows rest, jnx_head_rows dout, const float* lse,
+                      int rows, int H, int group, float2* row, int* claimed) {
+    constexpr int LANES = HD / 8, PER = 256 / LANES;
     pdl_entry();
     if (blockIdx.x == 0 && threadIdx.x == 0) *claimed = 0;
-    // hd / 8 lanes a row, 16 bytes each
-    const int lanes = hd / 8, per = 256 / lanes;
-    const long long w = (long long)blockIdx.x * per + threadIdx.x / lanes;
-    const int c = threadIdx.x % lanes * 8;
-    float d = 0.f;
-    if (w < (long long)rows * H) {
-        const long long r = w / H;
-        const int h = (int)(w % H);
-        const uint4 a = *reinterpret_cast<const uint4*>(out.ptr + r * out.row_stride +
-                                                        h * out.head_stride + c);
-        const uint4 b = *reinterpret_cast<const uint4*>(dout.ptr + r * dout.row_stride +
-                                                        h * dout.head_stride + c);
-        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    const long long all = (long long)rows * H;
+    const long long w0 = (long long)blockIdx.x * PER * 4 + threadIdx.x / LANES;
+    const int c = threadIdx.x % LANES * 8;
+    uint4 g[4], o[4], e[4];
+    float l[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            d += __uint_as_float(x[e] << 16) * __uint_as_float(y[e] << 16) +
-                 __uint_as_float(x[e] & 0xffff0000u) * __uint_as_float(y[e] & 0xffff0000u);
+    for (int b = 0; b < 4; ++b) {
+        const long long w = w0 + b * PER;
+        g[b] = o[b] = e[b] = make_uint4(0, 0, 0, 0);
+        l[b] = 0.f;
+        if (w < all) {
+            const long long r = w / H;
+            const int h = (int)(w - r * H);
+            g[b] = head_unit(dout, r, h, c);
+            o[b] = head_unit(out, r, h, c);
+            if (rest.ptr) e[b] = head_unit(rest, r, h, c);
+            l[b] = lse[w];
+        }
     }
-    for (int o = lanes / 2; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-    if (w < (long long)rows * H && c == 0) {
-        const float l = lse[w];
-        const int h = (int)(w % H);
-        row[((long long)(h / group) * rows + w / H) * group + h % group] =
-            l == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(l, d);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const float d = lanes_sum<LANES>(dot8(o[b], g[b]) + dot8(e[b], g[b]));
+        const long long w = w0 + b * PER;
+        if (w < all && c == 0) {
+            const long long r = w / H;
+            const int h = (int)(w - r * H);
+            row[((long long)(h / group) * rows + r) * group + h % group] =
+                l[b] == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(l[b], d);
+        }
+    }
+}
+
+// Rows that see up to kFewKeys keys: their D over again, as the sum of P dP in fp32.  dS =
+// P (dP - D) adds up to zero over a row's keys only as far as D is what the kernel's own P
+// and dP add up to.  rowsum(dO * O) is off by the roundings of the forward's P (and of O,
+// without `rest`), which shows where few terms nearly cancel: dQ of sequences of two tokens
+// was off by 0.0050 of its norm, against 0.0024 that its own two roundings make.  A CTA a
+// sequence and key head.
+constexpr int kFewKeys = 8;
+template <int HD>
+__global__ void __launch_bounds__(256)
+    k_prompt_bwd_few(jnx_head_rows dout, jnx_head_rows q, jnx_head_rows k, jnx_head_rows v,
+                     const float* lse, const __grid_constant__ PromptBwdArgs p, float2* row) {
+    constexpr int LANES = HD / 8, PER = 256 / LANES;
+    pdl_entry();
+    const int sq = blockIdx.x / p.Hkv, kvh = blockIdx.x % p.Hkv;
+    const int q0 = p.cu_q[sq], Lq = p.cu_q[sq + 1] - q0, k0 = p.cu_kv[sq];
+    const int Lk = p.cu_kv[sq + 1] - k0, pre = p.prefix ? p.prefix[sq] : 0;
+    if (Lk == 0) return;
+    // rows [a, b): the first that sees a key, the first that sees too many
+    const int a = first_row(0, Lq, Lk, pre), b = Lk > kFewKeys ? first_row(kFewKeys, Lq, Lk, pre) : Lq;
+    const int c = threadIdx.x % LANES * 8, n = (b - a) * p.group;
+    for (int r0 = 0; r0 < n; r0 += PER) {
+        // a lane without a row of its own goes along with the last
+        const int r = min(r0 + (int)threadIdx.x / LANES, n - 1);
+        const int i = a + r / p.group, hg = r % p.group, h = kvh * p.group + hg;
+        const long long at = q0 + i;
+        const uint4 g = head_unit(dout, at, h, c), x = head_unit(q, at, h, c);
+        const float l = lse[at * p.H + h];
+        const int few = keys_seen(i, Lq, Lk, pre);
+        uint4 kk[kFewKeys], vv[kFewKeys];
+#pragma unroll
+        for (int j = 0; j < kFewKeys; ++j) {
+            kk[j] = head_unit(k, k0 + min(j, few - 1), kvh, c);
+            vv[j] = head_unit(v, k0 + min(j, few - 1), kvh, c);
+        }
+        float d = 0.f;
+#pragma unroll
+        for (int j = 0; j < kFewKeys; ++j) {
+            const float s = lanes_sum<LANES>(dot8(x, kk[j])), dp = lanes_sum<LANES>(dot8(g, vv[j]));
+            if (j < few) d += ex2_approx(fmaf(s, p.scale_log2, -l)) * dp;
+        }
+        if (c == 0 && r0 + (int)threadIdx.x / LANES < n)
+            row[((long long)kvh * p.rows + at) * p.group + hg] = make_float2(l, d);
     }
 }
 
@@ -543,11 +618,14 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             // what counts of an outer row: a query's keys below lim, a key's rows from `from` on
             int lim = 0x7fffffff;
             const int from = KP ? (first_row(key, x.Lq, x.Lk, x.pre) - i0) * p.group : 0;
+            // keys passes: rows before this one see one key at most, and their dS is zero
+            const int two = x.Lk > 1 ? first_row(1, x.Lq, x.Lk, x.pre) : x.Lq;
             if (!KP && live) {
                 const float2 v = p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + hg];
                 nlse = -v.x;
                 nD = -v.y;
                 lim = keys_seen(i, x.Lq, x.Lk, x.pre);
+                if (lim == 1) lim = 0;  // a softmax over one key does not move
             }
             for (int j = 0; j < n; ++j, ++g) {
                 const float* sv = st + g % ST * 256 + half * 64;
@@ -617,6 +695,17 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 __syncwarp();
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[DP_FULL], g & 1)))) break;
                 tc_fence_after();
+                if (KP && i0 + j * T < two) {  // P has gone to dV
+                    const int ones = (two - i0 - j * T) * p.group - half * 64;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        float a, b;
+                        f2_unpack(pr[e], a, b);
+                        if (2 * e < ones) a = 0.f;
+                        if (2 * e + 1 < ones) b = 0.f;
+                        pr[e] = f2_pack(a, b);
+                    }
+                }
                 uint32_t dk[32];
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -1221,12 +1310,15 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
             float nlse = -INFINITY, nD = 0.f;
             // what counts of an outer row: a query's keys below lim, a key's rows from `from` on
             int lim = 0x7fffffff;
-            const int from = KP ? (first_row(key, x.Lq, x.Lk, x.pre) - i0) * p.group : 0;
+            // (DK: rows that see one key at most have no dS)
+            const int two = PASS == DK ? (x.Lk > 1 ? first_row(1, x.Lq, x.Lk, x.pre) : x.Lq) : 0;
+            const int from = KP ? (max(first_row(key, x.Lq, x.Lk, x.pre), two) - i0) * p.group : 0;
             if (!KP && live) {
                 const float2 v = p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + hg];
                 nlse = -v.x;
                 nD = -v.y;
                 lim = keys_seen(i, x.Lq, x.Lk, x.pre);
+                if (lim == 1) lim = 0;  // a softmax over one key does not move
             }
             for (int j = 0; j < n; ++j, ++g) {
                 const uint32_t b = NEED_DP ? 0 : g & 1, ph = NEED_DP ? g & 1 : (g >> 1) & 1;
@@ -1235,8 +1327,8 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
                 const uint32_t tP = tbase + lane_base + DP_COL + half * 64;
                 bool whole;
                 if (KP) {
-                    whole = keys_seen(min(i0 + j * T, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
-                            min(x.at + BM, x.Lk);
+                    whole = i0 + j * T >= two && keys_seen(min(i0 + j * T, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
+                                                     min(x.at + BM, x.Lk);
                     if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + b], ph)))) break;
                 } else {
                     whole = __all_sync(0xffffffffu, lim >= (j + 1) * BM);
@@ -1509,7 +1601,7 @@ extern "C" size_t jnx_op_prompt_attention_backward_workspace_bytes(const jnx_pro
 extern "C" jnx_status jnx_op_prompt_attention_backward(
     const jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
     const jnx_head_rows* q, const jnx_head_rows* k, const jnx_head_rows* v,
-    const jnx_head_rows* out, const float* lse, const jnx_head_rows* dout,
+    const jnx_head_rows* out, const jnx_head_rows* rest, const float* lse, const jnx_head_rows* dout,
     const jnx_head_rows* dq, const jnx_head_rows* dk, const jnx_head_rows* dv, void* workspace,
     size_t ws_bytes, int32_t* status, void* stream) {
     clear_error();
@@ -1518,7 +1610,8 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     if (jnx_status st = heads_ok(n_heads, n_kv_heads, head_dim, what)) return st;
     if (jnx_status st = prompt_launchable(p, what, rows, keys)) return st;
     if (rows == 0 && keys == 0) return JNX_OK;
-    if ((rows > 0 && (!rows_ok(q) || !rows_ok(out) || !rows_ok(dout) || !rows_ok(dq) || !lse)) ||
+    if ((rows > 0 && (!rows_ok(q) || !rows_ok(out) || !rows_ok(dout) || !rows_ok(dq) || !lse ||
+                      (rest && !rows_ok(rest)))) ||
         (keys > 0 && (!rows_ok(k) || !rows_ok(v) || !rows_ok(dk) || !rows_ok(dv))))
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned rows", what);
     if (!workspace || !aligned16(workspace) ||
@@ -1543,9 +1636,18 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
                     (long long)bwd_part_floats(p, keys, n_kv_heads, head_dim), p->n_parts, status};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN_BWD, 0.0, s);
-    const int per = 256 / (head_dim / 8);
-    pdl(k_prompt_bwd_rows, std::max(1, (int)(((long long)rows * n_heads + per - 1) / per)), 256, 0,
-        s)(or_none(out, rows), or_none(dout, rows), lse, rows, n_heads, a.group, head_dim, row, claimed);
+    auto prologue = [&](auto width) {
+        constexpr int HD = decltype(width)::value, PER = 4 * 256 / (HD / 8);
+        const long long all = (long long)rows * n_heads;
+        pdl(k_prompt_bwd_rows<HD>, std::max(1, (int)((all + PER - 1) / PER)), 256, 0, s)(
+            or_none(out, rows), rest && rows ? *rest : none, or_none(dout, rows), lse, rows, n_heads,
+            a.group, row, claimed);
+        if (rows && keys)
+            pdl(k_prompt_bwd_few<HD>, p->n_seqs * n_kv_heads, 256, 0, s)(*dout, *q, *k, *v, lse, a, row);
+    };
+    if (head_dim == 64) prologue(std::integral_constant<int, 64>{});
+    else if (head_dim == 128) prologue(std::integral_constant<int, 128>{});
+    else prologue(std::integral_constant<int, 256>{});
     // where there are no rows or keys nothing is loaded, but the maps want an address
     const jnx_head_rows& any = rows ? *q : *k;
     const jnx_head_rows qq = rows ? *q : any, dd = rows ? *dout : any, kk = keys ? *k : any,

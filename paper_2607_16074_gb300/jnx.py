@@ -306,11 +306,11 @@ def lib() -> C.CDLL:
         "jnx_op_qk_norm_rope_backward": (i32, [qkr, vp, i64, vp, i32, rows, rows, vp, vp, vp, vp,
                                                sz, vp]),
         "jnx_prompt_items": (i32, [prompt, i32, i32, i32, vp, i32]),
-        "jnx_op_prompt_attention": (i32, [prompt, i32, i32, i32, rows, rows, rows, rows, vp, vp,
-                                          vp]),
+        "jnx_op_prompt_attention": (i32, [prompt, i32, i32, i32, rows, rows, rows, rows, rows, vp,
+                                          vp, vp]),
         "jnx_op_prompt_attention_backward_workspace_bytes": (sz, [prompt, i32, i32, i32]),
         "jnx_op_prompt_attention_backward": (i32, [prompt, i32, i32, i32, rows, rows, rows, rows,
-                                                   vp, rows, rows, rows, rows, vp, sz, vp, vp]),
+                                                   rows, vp, rows, rows, rows, rows, vp, sz, vp, vp]),
         "jnx_op_decode_attention_workspace_bytes": (sz, [i32, i32, i32]),
         "jnx_op_decode_attention": (i32, [cache, i32, i32, i32, i32, rows, vp, vp, rows, vp, sz,
                                           vp, vp]),

@@ -725,6 +725,9 @@ class PromptAttention(_TextOperator):
         self._ref = C.byref(self.struct)
         super().__init__(J.lib().jnx_op_prompt_attention_backward_workspace_bytes(
             self._ref, *self.dims) if gradients else 0, plan.device)
+        # what rounding leaves of the forward's output, for the gradients of the same inputs
+        self.rest = torch.empty(plan.n_q, n_heads, head_dim, dtype=_BF16,
+                                device=plan.device) if gradients else None
 
     def _q(self, t):
         return C.byref(_rows(t, self.plan.n_q, self.dims[0], self.dims[2]))
@@ -735,17 +738,21 @@ class PromptAttention(_TextOperator):
     def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
                 lse: Optional[torch.Tensor] = None, stream=None) -> None:
         """out [n_q, H, hd]; lse [n_q, H] fp32 where the gradients are wanted later."""
+        rest = None
         if lse is not None:
             lse = _dense(lse, torch.float32, self.plan.n_q, self.dims[0])
+            rest = self._q(self.rest) if self.rest is not None else None
         J.check(self._lib.jnx_op_prompt_attention(
-            self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out), lse,
+            self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out), rest, lse,
             self._status, self._on(stream)))
 
     def backward(self, q, k, v, out, lse, dout, dq, dk, dv, stream=None) -> None:
-        """dq, dk, dv from dout, with the forward's out and lse."""
+        """dq, dk, dv from dout, with out and lse of the forward, the last one of this object."""
+        if self.rest is None:
+            raise ValueError("made for the forward only (gradients=False)")
         J.check(self._lib.jnx_op_prompt_attention_backward(
             self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out),
-            _dense(lse, torch.float32, self.plan.n_q, self.dims[0]), self._q(dout), self._q(dq),
+            self._q(self.rest), _dense(lse, torch.float32, self.plan.n_q, self.dims[0]), self._q(dout), self._q(dq),
             self._kv(dk), self._kv(dv), self._ws, self._nws, self._status, self._on(stream)))
 
 

@@ -80,7 +80,7 @@ def test_rope_refuses_pointers_and_strides():
 
 
 def attend(p, h=8, hkv=2, hd=128, q=rows(), k=rows(), v=rows(), out=rows()):
-    return J.lib().jnx_op_prompt_attention(C.byref(p), h, hkv, hd, q, k, v, out, None, None, None)
+    return J.lib().jnx_op_prompt_attention(C.byref(p), h, hkv, hd, q, k, v, out, None, None, None, None)
 
 
 def test_prompt_attention_refuses():
@@ -102,7 +102,7 @@ def test_prompt_attention_refuses():
 def test_prompt_attention_backward_refuses():
     L = J.lib()
     f = lambda p=prompt(), lse=PTR, ws=PTR, n=1 << 16, dk=rows(): \
-        L.jnx_op_prompt_attention_backward(C.byref(p), 8, 2, 128, rows(), rows(), rows(), rows(), lse,
+        L.jnx_op_prompt_attention_backward(C.byref(p), 8, 2, 128, rows(), rows(), rows(), rows(), None, lse,
                                            rows(), rows(), dk, rows(), ws, n, None, None)
     refused(f(lse=None), INV)
     refused(f(dk=rows(None)), INV)
