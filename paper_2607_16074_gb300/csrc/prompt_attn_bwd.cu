@@ -47,7 +47,8 @@ enum { KEYS = 0, QUERIES = 1 };
 // barriers of a pass
 enum { O_FULL = 0, O_EMPTY = 1, B1_FULL = 2, B1_EMPTY = 5, B2_FULL = 8, B2_EMPTY = 11, S_FULL = 14,
        DP_FULL = 15, P_FULL = 16, DS_FULL = 17, ACC_FULL = 18, ACC_FREE = 19, DRAIN = 20,
-       ST_FULL = 21, ST_EMPTY = 25, W_FULL = 29, W_EMPTY = 31, N_BARS = 33 };
+       ST_FULL = 21, ST_EMPTY = 25, W_FULL = 29, W_EMPTY = 32, N_BARS = 35 };
+constexpr int ITEMS = 3;  // items handed out at a time
 constexpr int ST = 4;  // slots of row values
 constexpr int THREADS = 384, EW = 8;
 constexpr int READERS = 2 + EW;  // warps that an item is handed to: MMA, row values, elementwise
@@ -62,7 +63,7 @@ struct PromptBwdCfg {
     static constexpr int OFF_STG = OFF_B2 + SLOTS * TILE;  // 2 KB an elementwise warp
     static constexpr int OFF_ST = OFF_STG + pbwd::EW * 2048;  // [ST][-lse, -D][128]
     static constexpr int OFF_BAR = OFF_ST + pbwd::ST * 2 * pbwd::BM * 4;
-    static constexpr int SMEM = OFF_BAR + 2 * pbwd::N_BARS * 8 + 80 + 1024;
+    static constexpr int SMEM = OFF_BAR + 2 * pbwd::N_BARS * 8 + 16 + pbwd::ITEMS * 32 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
     static constexpr uint32_t S_COL = 0, DP_COL = 128, ACC_COL = 256;
 };
@@ -295,27 +296,28 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
     uint8_t* b1 = sm + C::OFF_B1;
     uint8_t* b2 = sm + C::OFF_B2;
     float* st = reinterpret_cast<float*>(sm + C::OFF_ST);
-    volatile int* slot = fail_flag + 1;  // [2][8]: items handed out
+    volatile int* slot = fail_flag + 1;  // [ITEMS][8]: items handed out
     const int2* items = p.items + (KP ? 0 : p.n_keys);
     const int n_work = (KP ? p.n_keys : p.n_queries) * p.Hkv;
 
+    // the next item as warp 0 hands it out; item_done() gives its slot back
     int seen = 0;
-    auto next_item = [&](bool& ok) -> PromptBwdItem {
-        const int b = seen & 1;
-        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0, 0};
-        if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen >> 1) & 1))) return x;
-        x.at = warp_uniform(slot[8 * b]);
-        x.kvh = warp_uniform(slot[8 * b + 1]);
-        x.q0 = warp_uniform(slot[8 * b + 2]);
-        x.Lq = warp_uniform(slot[8 * b + 3]);
-        x.k0 = warp_uniform(slot[8 * b + 4]);
-        x.Lk = warp_uniform(slot[8 * b + 5]);
-        x.pre = warp_uniform(slot[8 * b + 6]);
-        x.part = warp_uniform(slot[8 * b + 7]);
-        if (elect_one()) mbar_arrive(&bar[W_EMPTY + b]);
+    auto get_item = [&](int b) -> PromptBwdItem {
+        const volatile int* s = slot + 8 * b;
+        return PromptBwdItem{warp_uniform(s[0]), warp_uniform(s[1]), warp_uniform(s[2]), warp_uniform(s[3]),
+                             warp_uniform(s[4]), warp_uniform(s[5]), warp_uniform(s[6]), warp_uniform(s[7])};
+    };
+    auto item_done = [&]() {
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&bar[W_EMPTY + seen % ITEMS]);
         __syncwarp();
         ++seen;
-        return x;
+    };
+    auto next_item = [&](bool& ok) -> PromptBwdItem {
+        const int b = seen % ITEMS;
+        if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen / ITEMS) & 1)))
+            return PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0};
+        return get_item(b);
     };
     // an item's inner tiles, and the keys pass's first inner row
     auto inner = [&](const PromptBwdItem& x, int& i0, int& n) {
@@ -332,8 +334,8 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         bool ok = true;
         int told = 0;
         auto tell = [&](const PromptBwdItem& x) {
-            const int b = told & 1;
-            if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told >> 1) & 1) ^ 1)) return false;
+            const int b = told % ITEMS;
+            if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told / ITEMS) & 1) ^ 1)) return false;
             if (elect_one()) {
                 slot[8 * b] = x.at;
                 slot[8 * b + 1] = x.kvh;
@@ -483,6 +485,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         while (ok) {
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            item_done();
             int i0, n;
             inner(x, i0, n);
             if (n == 0) continue;
@@ -570,6 +573,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         while (ok) {
             const PromptBwdItem x = next_item(ok);
             if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+            item_done();
             if (!KP) continue;
             int i0, n;
             inner(x, i0, n);
@@ -606,33 +610,38 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         int done = 0;
         bool ok = true;
         while (ok) {
-            const PromptBwdItem x = next_item(ok);
-            if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
-            int i0, n;
-            inner(x, i0, n);
-            // the outer row of this thread: a key, or a (token, head)
-            const int tok = r / p.group, hg = r % p.group;
-            const int key = x.at + r, i = x.at + tok;
-            const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
+            // of the item, what the tiles need; the epilogue looks again
+            int n, lim = 0x7fffffff, from = 0, whole_j = 0, two = 0;
             float nlse = -INFINITY, nD = 0.f;
-            // what counts of an outer row: a query's keys below lim, a key's rows from `from` on
-            int lim = 0x7fffffff;
-            const int from = KP ? (first_row(key, x.Lq, x.Lk, x.pre) - i0) * p.group : 0;
-            // keys passes: rows before this one see one key at most, and their dS is zero
-            const int two = x.Lk > 1 ? first_row(1, x.Lq, x.Lk, x.pre) : x.Lq;
-            if (!KP && live) {
-                const float2 v = p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + hg];
-                nlse = -v.x;
-                nD = -v.y;
-                lim = keys_seen(i, x.Lq, x.Lk, x.pre);
-                if (lim == 1) lim = 0;  // a softmax over one key does not move
+            {
+                const PromptBwdItem x = next_item(ok);
+                if (!ok || x.Lq < 0 || __any_sync(0xffffffffu, *fail_flag)) break;
+                int i0;
+                inner(x, i0, n);
+                if (KP) {
+                    // columns that count of this thread's key: rows from `from` on (in tile 0);
+                    // tiles from whole_j on count whole; rows before `two` see one key at
+                    // most, and their dS is zero
+                    from = (first_row(x.at + r, x.Lq, x.Lk, x.pre) - i0) * p.group;
+                    whole_j = (first_row(min(x.at + BM, x.Lk) - 1, x.Lq, x.Lk, x.pre) - i0 + T - 1) / T;
+                    two = ((x.Lk > 1 ? first_row(1, x.Lq, x.Lk, x.pre) : x.Lq) - i0) * p.group;
+                } else if (r < T * p.group && x.at + r / p.group < x.Lq) {
+                    // keys that this thread's row sees; a softmax over one does not move
+                    const int i = x.at + r / p.group;
+                    const float2 v =
+                        p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + r % p.group];
+                    nlse = -v.x;
+                    nD = -v.y;
+                    lim = keys_seen(i, x.Lq, x.Lk, x.pre);
+                    if (lim == 1) lim = 0;
+                }
             }
+            const int box = T * p.group;
             for (int j = 0; j < n; ++j, ++g) {
                 const float* sv = st + g % ST * 256 + half * 64;
                 bool whole;  // every score of the tile counts
                 if (KP) {
-                    whole = keys_seen(min(i0 + j * T, x.Lq - 1), x.Lq, x.Lk, x.pre) >=
-                            min(x.at + BM, x.Lk);
+                    whole = j >= whole_j;
                     if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[ST_FULL + g % ST], (g / ST) & 1))))
                         break;
                 } else {
@@ -668,7 +677,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 }
                 if (!whole) {
                     // columns that count: [0, hi) of a query, [lo, 64) of a key
-                    const int lo = from - j * T * p.group - half * 64, hi = lim - j * BM - half * 64;
+                    const int lo = from - j * box - half * 64, hi = lim - j * BM - half * 64;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
                         float a, b;
@@ -695,8 +704,8 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 __syncwarp();
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[DP_FULL], g & 1)))) break;
                 tc_fence_after();
-                if (KP && i0 + j * T < two) {  // P has gone to dV
-                    const int ones = (two - i0 - j * T) * p.group - half * 64;
+                if (KP && j * box < two) {  // P has gone to dV
+                    const int ones = two - j * box - half * 64;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
                         float a, b;
@@ -752,6 +761,10 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 tc_fence_after();
                 ++done;
             }
+            const PromptBwdItem x = get_item(seen % ITEMS);
+            item_done();
+            const int tok = r / p.group, hg = r % p.group, key = x.at + r, i = x.at + tok;
+            const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
             const bool in_parts = KP && x.parts(p.group, p.Hkv) > 1;
             float* part = p.part + x.part * p.part_stride;
             for (int acc = 0; acc < (KP ? 2 : 1); ++acc) {
