@@ -5,6 +5,8 @@ call the library.  No arithmetic of the method happens here.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -553,7 +555,7 @@ class StepPipeline:
 # operators of text tenants
 # ---------------------------------------------------------------------------
 
-_BF16 = torch.bfloat16
+_BF16, _I32, _F32 = torch.bfloat16, torch.int32, torch.float32
 
 
 def _refuse(t: torch.Tensor, dtype, shape) -> None:
@@ -568,12 +570,12 @@ def _bf16(t: torch.Tensor, *shape) -> torch.Tensor:
     return t
 
 
-def _rows(t: torch.Tensor, *shape) -> J.jnx_head_rows:
-    """Head rows [n, heads, head_dim] of any row and head stride."""
+def _view(t: torch.Tensor, shape):
+    """Head rows [n, heads, head_dim] of any row and head stride: what jnx_head_rows holds."""
     s = t.stride()
     if t.dtype is not _BF16 or t.shape != shape or s[2] != 1 or not t.is_cuda:
         _refuse(t, _BF16, shape)
-    return J.jnx_head_rows(t.data_ptr(), s[0], s[1])
+    return t.data_ptr(), s[0], s[1]
 
 
 def _dense(t: torch.Tensor, dtype, *shape) -> int:
@@ -582,20 +584,35 @@ def _dense(t: torch.Tensor, dtype, *shape) -> int:
     return t.data_ptr()
 
 
-def _cache(k: torch.Tensor, v: torch.Tensor, n_kv_heads: int, head_dim: int) -> J.jnx_kv_cache:
-    """A cache [slots, room, kv heads, head_dim]; k and v with the same strides."""
+def _cache(k: torch.Tensor, v: torch.Tensor, heads):
+    """A cache [slots, room, kv heads, head_dim], k and v of one layout: jnx_kv_cache's fields."""
     s, shape = k.stride(), k.shape
     if k.dtype is not _BF16 or v.dtype is not _BF16 or v.shape != shape or v.stride() != s or \
-            shape[2:] != (n_kv_heads, head_dim) or s[3] != 1 or not k.is_cuda or not v.is_cuda:
-        raise ValueError(f"expected bf16 CUDA caches [slots, room, {n_kv_heads}, {head_dim}] of one "
+            shape[2:] != heads or s[3] != 1 or not k.is_cuda or not v.is_cuda:
+        raise ValueError(f"expected bf16 CUDA caches [slots, room, {heads[0]}, {heads[1]}] of one "
                          f"layout, got {k.dtype} {tuple(shape)} strides {s} and {v.dtype} "
                          f"{tuple(v.shape)} strides {v.stride()}")
-    return J.jnx_kv_cache(k.data_ptr(), v.data_ptr(), shape[0], shape[1], s[0], s[1], s[2])
+    return k.data_ptr(), v.data_ptr(), shape[0], shape[1], s[0], s[1], s[2]
+
+
+class _Views:
+    """The structs that a call's tensors are described in, filled in one go: making one of
+    each for every call took as long as the rest of a short call."""
+
+    def __init__(self, *kinds):
+        self._mem = C.create_string_buffer(sum(C.sizeof(k) for k in kinds))
+        at, self.refs, form = C.addressof(self._mem), [], "="
+        for k in kinds:
+            self.refs.append(C.cast(at, C.POINTER(k)))
+            at += C.sizeof(k)
+            form += "Qqq" if k is J.jnx_head_rows else "QQiiqqq"
+        self.fill = functools.partial(struct.Struct(form).pack_into, self._mem, 0)
 
 
 class _TextOperator:
     """What the operators share: the status word their kernels report to and scratch
-    memory, both the object's own (calls on several streams at once take an object each)."""
+    memory, both the object's own (calls on several streams or threads at once take an
+    object each)."""
 
     def __init__(self, ws_bytes: int = 0, device="cuda"):
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
@@ -638,45 +655,49 @@ class QKNormRope(_TextOperator):
         super().__init__(J.lib().jnx_op_qk_norm_rope_backward_workspace_bytes(self._ref, 1 << 30),
                          device)
 
+        rows, cache = J.jnx_head_rows, J.jnx_kv_cache
+        self._qk, self._qc = _Views(rows, rows), _Views(rows, cache)
+
     def _args(self, qkv: torch.Tensor, pos: torch.Tensor):
         h, hkv, hd = self.dims
         n = qkv.shape[0]
         _bf16(qkv, n, (h + 2 * hkv) * hd)
-        return n, self._ref, qkv.data_ptr(), qkv.stride(0), \
-            _dense(pos, torch.int32, len(self.sections), n)
+        return n, qkv.data_ptr(), qkv.stride(0), _dense(pos, _I32, len(self.sections), n)
 
     def forward(self, qkv: torch.Tensor, pos: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
                 stream=None) -> None:
         """q [n, H, hd] and k [n, Hkv, hd] from qkv [n, (H + 2 Hkv) hd] at pos [axes, n]."""
         h, hkv, hd = self.dims
-        n, ref, x, ld, p = self._args(qkv, pos)
-        J.check(self._lib.jnx_op_qk_norm_rope(ref, x, ld, p, n, C.byref(_rows(q, n, h, hd)),
-                                            C.byref(_rows(k, n, hkv, hd)), self._on(stream)))
+        n, x, ld, p = self._args(qkv, pos)
+        self._qk.fill(*_view(q, (n, h, hd)), *_view(k, (n, hkv, hd)))
+        J.check(self._lib.jnx_op_qk_norm_rope(self._ref, x, ld, p, n, *self._qk.refs,
+                                              self._on(stream)))
 
     def append(self, qkv: torch.Tensor, pos: torch.Tensor, q: torch.Tensor,
                k_cache: torch.Tensor, v_cache: torch.Tensor, slot: torch.Tensor,
                at: torch.Tensor, stream=None) -> None:
         """q as forward; key and value rows go to cache rows [slot[i], at[i]]."""
         h, hkv, hd = self.dims
-        n, ref, x, ld, p = self._args(qkv, pos)
+        n, x, ld, p = self._args(qkv, pos)
+        self._qc.fill(*_view(q, (n, h, hd)), *_cache(k_cache, v_cache, (hkv, hd)))
         J.check(self._lib.jnx_op_qk_norm_rope_append(
-            ref, x, ld, p, n, C.byref(_rows(q, n, h, hd)),
-            C.byref(_cache(k_cache, v_cache, hkv, hd)), _dense(slot, torch.int32, n),
-            _dense(at, torch.int32, n), self._status, self._on(stream)))
+            self._ref, x, ld, p, n, *self._qc.refs, _dense(slot, _I32, n),
+            _dense(at, _I32, n), self._status, self._on(stream)))
 
     def backward(self, qkv: torch.Tensor, pos: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
                  dqkv: torch.Tensor, dgamma_q: Optional[torch.Tensor] = None,
                  dgamma_k: Optional[torch.Tensor] = None, stream=None) -> None:
         """dqkv's query and key columns (same strides as qkv) and the gains' gradients."""
         h, hkv, hd = self.dims
-        n, ref, x, ld, p = self._args(qkv, pos)
+        n, x, ld, p = self._args(qkv, pos)
         _bf16(dqkv, *qkv.shape)
         if dqkv.stride(0) != ld:
             raise ValueError("dqkv and qkv differ in their row strides")
-        gains = [None if g is None else _dense(g, torch.float32, hd) for g in (dgamma_q, dgamma_k)]
+        gains = [None if g is None else _dense(g, _F32, hd) for g in (dgamma_q, dgamma_k)]
+        self._qk.fill(*_view(dq, (n, h, hd)), *_view(dk, (n, hkv, hd)))
         J.check(self._lib.jnx_op_qk_norm_rope_backward(
-            ref, x, ld, p, n, C.byref(_rows(dq, n, h, hd)), C.byref(_rows(dk, n, hkv, hd)),
-            dqkv.data_ptr(), *gains, self._ws, self._nws, self._on(stream)))
+            self._ref, x, ld, p, n, *self._qk.refs, dqkv.data_ptr(), *gains, self._ws, self._nws,
+            self._on(stream)))
 
 
 class PromptPlan:
@@ -729,31 +750,33 @@ class PromptAttention(_TextOperator):
         self.rest = torch.empty(plan.n_q, n_heads, head_dim, dtype=_BF16,
                                 device=plan.device) if gradients else None
 
-    def _q(self, t):
-        return C.byref(_rows(t, self.plan.n_q, self.dims[0], self.dims[2]))
-
-    def _kv(self, t):
-        return C.byref(_rows(t, self.plan.n_kv, self.dims[1], self.dims[2]))
+        rows = J.jnx_head_rows
+        self._qs, self._ks = (plan.n_q, n_heads, head_dim), (plan.n_kv, n_kv_heads, head_dim)
+        self._fwd, self._bwd, self._left = _Views(*[rows] * 4), _Views(*[rows] * 8), _Views(rows)
+        if gradients:
+            self._left.fill(*_view(self.rest, self._qs))
 
     def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
                 lse: Optional[torch.Tensor] = None, stream=None) -> None:
         """out [n_q, H, hd]; lse [n_q, H] fp32 where the gradients are wanted later."""
-        rest = None
+        qs, ks, rest = self._qs, self._ks, None
         if lse is not None:
-            lse = _dense(lse, torch.float32, self.plan.n_q, self.dims[0])
-            rest = self._q(self.rest) if self.rest is not None else None
-        J.check(self._lib.jnx_op_prompt_attention(
-            self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out), rest, lse,
-            self._status, self._on(stream)))
+            lse = _dense(lse, _F32, *qs[:2])
+            rest = self._left.refs[0] if self.rest is not None else None
+        self._fwd.fill(*_view(q, qs), *_view(k, ks), *_view(v, ks), *_view(out, qs))
+        J.check(self._lib.jnx_op_prompt_attention(self._ref, *self.dims, *self._fwd.refs, rest, lse,
+                                                  self._status, self._on(stream)))
 
     def backward(self, q, k, v, out, lse, dout, dq, dk, dv, stream=None) -> None:
         """dq, dk, dv from dout, with out and lse of the forward, the last one of this object."""
         if self.rest is None:
             raise ValueError("made for the forward only (gradients=False)")
+        qs, ks, r = self._qs, self._ks, self._bwd.refs
+        self._bwd.fill(*_view(q, qs), *_view(k, ks), *_view(v, ks), *_view(out, qs),
+                       *_view(dout, qs), *_view(dq, qs), *_view(dk, ks), *_view(dv, ks))
         J.check(self._lib.jnx_op_prompt_attention_backward(
-            self._ref, *self.dims, self._q(q), self._kv(k), self._kv(v), self._q(out),
-            self._q(self.rest), _dense(lse, torch.float32, self.plan.n_q, self.dims[0]), self._q(dout), self._q(dq),
-            self._kv(dk), self._kv(dv), self._ws, self._nws, self._status, self._on(stream)))
+            self._ref, *self.dims, *r[:4], self._left.refs[0], _dense(lse, _F32, *qs[:2]),
+            *r[4:], self._ws, self._nws, self._status, self._on(stream)))
 
 
 class DecodeAttention(_TextOperator):
@@ -765,6 +788,8 @@ class DecodeAttention(_TextOperator):
         super().__init__(J.lib().jnx_op_decode_attention_workspace_bytes(max_batch, n_heads,
                                                                          head_dim), device)
 
+        self._views = _Views(J.jnx_kv_cache, J.jnx_head_rows, J.jnx_head_rows)
+
     def forward(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
                 slot: torch.Tensor, n_cached: torch.Tensor, out: torch.Tensor,
                 stream=None) -> None:
@@ -774,11 +799,12 @@ class DecodeAttention(_TextOperator):
         b = q.shape[0]
         if b > self.max_batch:
             raise ValueError(f"batch of {b}, at most {self.max_batch}")
-        cache = _cache(k_cache, v_cache, hkv, hd)
+        rows, r = (b, h, hd), self._views.refs
+        self._views.fill(*_cache(k_cache, v_cache, (hkv, hd)), *_view(q, rows), *_view(out, rows))
         J.check(self._lib.jnx_op_decode_attention(
-            C.byref(cache), b, h, hkv, hd, C.byref(_rows(q, b, h, hd)),
-            _dense(slot, torch.int32, b), _dense(n_cached, torch.int32, b),
-            C.byref(_rows(out, b, h, hd)), self._ws, self._nws, self._status, self._on(stream)))
+            r[0], b, h, hkv, hd, r[1], _dense(slot, _I32, b),
+            _dense(n_cached, _I32, b), r[2], self._ws, self._nws, self._status,
+            self._on(stream)))
 
 
 class VocabLoss(_TextOperator):
@@ -802,14 +828,14 @@ class VocabLoss(_TextOperator):
             raise ValueError(f"{n} rows, at most {self.max_rows}")
         _bf16(h, n, self.d)
         return n, h.data_ptr(), h.stride(0), self.w.data_ptr(), self.w.stride(0), \
-            _dense(targets, torch.int32, n)
+            _dense(targets, _I32, n)
 
     def loss(self, h: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor,
              stream=None) -> None:
         """loss [n] fp32 of h [n, d]; 0 where targets [n] is negative."""
         n, *args = self._args(h, targets)
         J.check(self._lib.jnx_op_vocab_loss(
-            *args, n, self.vocab, self.d, _dense(loss, torch.float32, n), self._ws, self._nws,
+            *args, n, self.vocab, self.d, _dense(loss, _F32, n), self._ws, self._nws,
             self._status, self._on(stream)))
 
     def train(self, h: torch.Tensor, targets: torch.Tensor, row_weight: torch.Tensor,
@@ -826,6 +852,6 @@ class VocabLoss(_TextOperator):
             _bf16(dw, self.vocab, self.d)
             grads[2:] = [dw.data_ptr(), dw.stride(0)]
         J.check(self._lib.jnx_op_vocab_loss_train(
-            *args, _dense(row_weight, torch.float32, n), n, self.vocab, self.d, self.piece_rows,
-            _dense(loss, torch.float32, n), *grads, self._ws, self._nws, self._status,
+            *args, _dense(row_weight, _F32, n), n, self.vocab, self.d, self.piece_rows,
+            _dense(loss, _F32, n), *grads, self._ws, self._nws, self._status,
             self._on(stream)))

@@ -31,7 +31,7 @@ class TextTenant:
         self.w_o_t = self.w_o.T.contiguous()
         self.ones = torch.ones(d, device="cuda", dtype=BF)
         self.gains = torch.ones(2, 1, head_dim, device="cuda", dtype=BF)
-        self.words = rnd(1, vocab, d, std=0.3)  # [tenant slot, vocab, d]
+        self.words = rnd(1, vocab, d, std=0.05)  # [tenant slot, vocab, d]
         # time turns half of the frequencies, an image patch's row and column a quarter each
         q = head_dim // 8
         self.rope = R.QKNormRope(*self.dims, self.gains[0, 0], self.gains[1, 0],
@@ -172,13 +172,13 @@ def samples(tenant, images, texts, seed=1):
     for i, t in zip(images, texts):
         first, by = (int(torch.randint(1, 9, (1,), generator=g)) for _ in range(2))
         ids = (first + by * torch.arange(t + 1)) % tenant.vocab
-        image = torch.randn(i, tenant.d, generator=g) * 0.3
+        image = torch.randn(i, tenant.d, generator=g) * 0.05
         rows.append(torch.cat([image.cuda(), tenant.embed(ids[:-1].cuda())]))
         targets.append(torch.cat([torch.full((i,), -1), ids[1:]]))
     return torch.cat(rows), torch.cat(targets).to(I32).cuda()
 
 
-def main(steps=30, images=(16, 12, 0, 20), texts=(24, 40, 7, 33), lr=1e-2, verbose=True):
+def main(steps=30, images=(16, 12, 0, 20), texts=(24, 40, 7, 33), lr=3e-3, verbose=True):
     tenant = TextTenant()
     lens = [i + t for i, t in zip(images, texts)]
     plan = R.PromptPlan(lens, prefix=list(images))
