@@ -34,7 +34,7 @@ struct Args {
     const uint16_t* qkv;
     long long ldqkv;
     const int* pos;
-    int n_tokens, H, Hkv, half;
+    int n_tokens, H, Hkv, tok;  // tok: tokens of a block
     float eps;
     const uint16_t *gq, *gk;
     // forward: where rows go; backward: where the gradients of those rows come from
@@ -109,7 +109,7 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-// E: elements of either half a lane holds; TOK: tokens of a block.
+// E: elements of either half a lane holds; TOK: tokens of a block, at most.
 template <int HD, int E_, int TOK_>
 struct Cfg {
     static constexpr int E = E_, TOK = TOK_;
@@ -135,9 +135,9 @@ struct Cfg {
     }
 };
 template <int HD>
-using Forward = Cfg<HD, 8, HD == 64 ? 8 : HD == 128 ? 4 : 2>;
+using Forward = Cfg<HD, 8, HD == 64 ? 16 : 8>;
 template <int HD>
-using Backward = Cfg<HD, 4, HD == 64 ? 16 : HD == 128 ? 8 : 4>;
+using Backward = Cfg<HD, 4, HD == 64 ? 16 : 8>;
 }  // namespace rope
 
 template <int HD, bool APPEND>
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(rope::THREADS)
     constexpr int E = C::E;
     __shared__ float4 cs[C::TOK * HD / 4];
     pdl_entry();
-    const int t0 = blockIdx.x * C::TOK, nt = min(C::TOK, a.n_tokens - t0);
+    const int t0 = blockIdx.x * a.tok, nt = min(a.tok, a.n_tokens - t0);
     // rows of the CTA's tokens, token-major; an append's value heads come after the keys'
     const int heads = a.H + (APPEND ? 2 : 1) * a.Hkv;
     const int l = threadIdx.x % C::LPR, part = l * E;  // this lane's elements of each half
@@ -387,7 +387,6 @@ static jnx_status rope_args(const jnx_qk_rope* p, const uint16_t* qkv, int64_t l
     a.n_tokens = n_tokens;
     a.H = p->n_heads;
     a.Hkv = p->n_kv_heads;
-    a.half = p->head_dim / 2;
     a.eps = p->eps;
     a.gq = p->gamma_q;
     a.gk = p->gamma_k;
@@ -409,10 +408,15 @@ static jnx_status rope_args(const jnx_qk_rope* p, const uint16_t* qkv, int64_t l
     return JNX_OK;
 }
 
+// Tokens of a CTA: rows for four passes, fewer where that would leave SMs without a CTA.
+// (30,000 tokens of 9 heads of 256: 88 us with two tokens a CTA, a pass and an eighth, 63
+// with eight.)
 template <int HD, bool APPEND>
-static void launch_rope_hd(const rope::Args& a, cudaStream_t s) {
-    constexpr int TOK = rope::Forward<HD>::TOK;
-    pdl(k_qk_norm_rope<HD, APPEND>, (a.n_tokens + TOK - 1) / TOK, rope::THREADS, 0, s)(a);
+static void launch_rope_hd(rope::Args a, cudaStream_t s) {
+    using C = rope::Forward<HD>;
+    const int heads = a.H + (APPEND ? 2 : 1) * a.Hkv;
+    a.tok = std::max(1, std::min({C::TOK, (4 * C::RPP + heads - 1) / heads, a.n_tokens / (152 * 6)}));
+    pdl(k_qk_norm_rope<HD, APPEND>, (a.n_tokens + a.tok - 1) / a.tok, rope::THREADS, 0, s)(a);
 }
 
 template <bool APPEND>
@@ -425,14 +429,17 @@ static jnx_status launch_rope(const rope::Args& a, int hd, const char* what, cud
     return launched(what);
 }
 
-// CTAs of the gradient kernel, at most what 152 SMs hold at once, shared out by rows;
-// each kind has one at least.
+// CTAs of the gradient kernel, at most what 152 SMs hold at once, shared out between query
+// and key rows by what a block of either takes: its passes, and its angles and waits, worth
+// five passes (by rows alone the key rows of 8 heads on one, 256 wide, were the last by far:
+// 30,000 tokens 275 us, so 158; 32 heads on 8 of 128 212 and 187 us); each kind has one at
+// least.
 static int rope_bwd_grid(const jnx_qk_rope* p, int n_tokens, int& q_ctas) {
-    const int hd = p->head_dim, h = p->n_heads, hkv = p->n_kv_heads;
-    const int tok = hd == 64 ? rope::Backward<64>::TOK
-                             : hd == 128 ? rope::Backward<128>::TOK : rope::Backward<256>::TOK;
+    const int hd = p->head_dim, tok = hd == 64 ? 16 : 8, rows = rope::THREADS * 8 / hd;  // a pass
     const int blocks = std::max(1, (n_tokens + tok - 1) / tok), most = 152 * 4;
-    q_ctas = std::min(blocks, std::max(1, (int)((long long)most * h / std::max(1, h + hkv))));
+    auto passes = [&](int heads) { return (tok * heads + rows - 1) / rows + 5; };
+    const long long q = passes(p->n_heads), k = passes(p->n_kv_heads);
+    q_ctas = std::min(blocks, std::max(1, (int)(most * q / (q + k))));
     return q_ctas + std::min(blocks, std::max(1, most - q_ctas));
 }
 
