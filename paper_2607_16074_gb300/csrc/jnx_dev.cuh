@@ -647,6 +647,12 @@ __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t smem_addr, uint32_t m
     return d;
 }
 
+// The low word of sw128_desc_mn with 1,024 bytes between 8-row atoms along K: the high word
+// is kSw128DescHi, and 16 K-rows further is 128 more.
+__device__ __forceinline__ uint32_t sw128_desc_mn_lo(uint32_t smem_addr, uint32_t mn_stride) {
+    return ((smem_addr & 0x3FFFF) >> 4) | ((mn_stride >> 4) << 16);
+}
+
 // Instruction descriptor: kind::f16, A = B = bf16, D = f32, both K-major.
 __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) |

@@ -269,33 +269,41 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
         };
         // S (columns d) of row tile t against the K tile in units [first, first + NU)
         auto issue_s = [&](int t, uint32_t first, uint32_t d, uint64_t* done) {
+            const uint32_t a_lo = q_lo + t * (C::QB >> 4);
+            uint32_t k_lo[NU];
+#pragma unroll
+            for (int c = 0; c < NU; ++c) k_lo[c] = r_lo + ((first + c) % RING) * (UNIT >> 4);
             if (elect_one()) {
 #pragma unroll
-                for (int c = 0; c < NCH; ++c) {
-                    const uint32_t k_lo = r_lo + ((first + c / C::KCH) % RING) * (UNIT >> 4) +
-                                          c % C::KCH * (BN * 128 >> 4);
+                for (int c = 0; c < NCH; ++c)
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        tc_mma_f16(d,
-                                   desc_of(q_lo + ((t * C::QB + c * BM * 128) >> 4) + ks * 2,
+                        tc_mma_f16(d, desc_of(a_lo + c * (BM * 128 >> 4) + ks * 2, kSw128DescHi),
+                                   desc_of(k_lo[c / C::KCH] + c % C::KCH * (BN * 128 >> 4) + ks * 2,
                                            kSw128DescHi),
-                                   desc_of(k_lo + ks * 2, kSw128DescHi), IDESC_S, (c | ks) != 0);
-                }
+                                   IDESC_S, (c | ks) != 0);
                 tc_commit(done);
             }
             __syncwarp();
             issued = true;
         };
         // O (columns d) += P (columns p) times half h of the V tile in units [first, first + NU)
-        auto issue_pv = [&](int h, uint32_t p, uint32_t first, uint32_t d, bool accumulate) {
+        const uint32_t v_lo = sw128_desc_mn_lo(smem_u32(ring), C::VKEYS * 128);
+        auto issue_pv = [&](auto half, uint32_t p, uint32_t first, uint32_t d, bool accumulate) {
+            constexpr int h = decltype(half)::value, UH = NU == 1 ? 1 : NU / 2;  // units of a half
+            uint32_t lo[UH];
+#pragma unroll
+            for (int c = 0; c < UH; ++c)
+                lo[c] = v_lo + ((first + (NU == 1 ? 0 : h * UH + c)) % RING) * (UNIT >> 4);
             if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < BN / 32; ++k) {
                     const int ks = h * (BN / 32) + k;
-                    const int un = ks * 16 / C::VKEYS, off = ks * 16 % C::VKEYS;
-                    const uint32_t va = smem_u32(ring) + ((first + un) % RING) * UNIT + off * 128;
-                    tc_mma_f16_ts(d, p + ks * 8, sw128_desc_mn(va, C::VKEYS * 128, 1024), IDESC_PV,
-                                  accumulate || k > 0);
+                    tc_mma_f16_ts(d, p + ks * 8,
+                                  desc_of(lo[NU == 1 ? 0 : k * 16 / C::VKEYS] +
+                                              ks * 16 % C::VKEYS * (128 >> 4),
+                                          kSw128DescHi),
+                                  IDESC_PV, accumulate || k > 0);
                 }
             }
             __syncwarp();
@@ -350,11 +358,11 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                             ++no[t];
                         }
                         tc_fence_after();
-                        issue_pv(0, tbase + t * BN, uv, tbase + C::O_COL + t * HD, kt > 0);
+                        issue_pv(std::integral_constant<int, 0>{}, tbase + t * BN, uv, tbase + C::O_COL + t * HD, kt > 0);
                         if (!(ok = mbar_wait_warp(&bar[P_FULL + t], gp[t] & 1))) break;
                         ++gp[t];
                         tc_fence_after();
-                        issue_pv(1, tbase + t * BN, uv, tbase + C::O_COL + t * HD, true);
+                        issue_pv(std::integral_constant<int, 1>{}, tbase + t * BN, uv, tbase + C::O_COL + t * HD, true);
                         if (kt + 1 < nt[t]) {
                             issue_s(t, uk, tbase + t * BN, &bar[S_FULL + t]);
                             if (kt + 2 == nt[t]) commit(&bar[Q_EMPTY + t]);
@@ -392,11 +400,11 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                         ++no[0];
                     }
                     tc_fence_after();
-                    issue_pv(0, tbase + b * BN, u, tbase + C::O_COL, kt > 0);
+                    issue_pv(std::integral_constant<int, 0>{}, tbase + b * BN, u, tbase + C::O_COL, kt > 0);
                     if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (gp[0] >> 1) & 1))) break;
                     ++gp[0];
                     tc_fence_after();
-                    issue_pv(1, tbase + b * BN, u, tbase + C::O_COL, true);
+                    issue_pv(std::integral_constant<int, 1>{}, tbase + b * BN, u, tbase + C::O_COL, true);
                     commit(&bar[PV_DONE + b]);
                     free_units(u);
                     u += NU;

@@ -124,7 +124,7 @@ __device__ __forceinline__ float lanes_sum(float d) {
 // The rows' (lse, D = rowsum(dO * O)), and the claim counter to zero.  HD / 8 lanes a row,
 // four rows of neighbouring heads a lane, whose loads are under way at once.  Bound by HBM.
 // (By tiles of a sequence and key head, 256 bytes a row: 52 us for 7,000 rows of 32 heads;
-// as they lie MEASUREDROWS.)
+// as they lie 37.)
 template <int HD>
 __global__ void __launch_bounds__(256)
     k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows rest, jnx_head_rows dout, const float* lse,
@@ -463,12 +463,12 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
         };
         // acc += X B, X bf16 in TMEM: 64 inner rows at column x, 64 at x + 64
         auto gather = [&](uint32_t acc, uint32_t x, uint8_t* inner, bool accumulate) {
-            const uint32_t b = smem_u32(inner);
+            const uint32_t b_lo = sw128_desc_mn_lo(smem_u32(inner), BM * 128);
             if (elect_one()) {
 #pragma unroll
                 for (int ks = 0; ks < BM / 16; ++ks)
                     tc_mma_f16_ts(acc, x + (ks >> 2) * 64 + (ks & 3) * 8,
-                                  sw128_desc_mn(b + ks * 16 * 128, BM * 128, 1024), IDESC_ACC,
+                                  desc_of(b_lo + ks * 128, kSw128DescHi), IDESC_ACC,
                                   accumulate || ks > 0);
             }
             __syncwarp();
@@ -1230,12 +1230,12 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
             // acc += X B over the slot's 128 rows, X bf16 in TMEM: 64 rows at column xc, 64 at
             // xc + 64
             auto gather = [&](int h, uint32_t xc, bool accumulate) {
-                const uint32_t b = smem_u32(sl + 2 * h * UNIT);
+                const uint32_t b_lo = sw128_desc_mn_lo(smem_u32(sl + 2 * h * UNIT), UNIT);
                 if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < BM / 16; ++ks)
                         tc_mma_f16_ts(tbase + ACC_COL + h * 128, xc + (ks >> 2) * 64 + (ks & 3) * 8,
-                                      sw128_desc_mn(b + ks * 16 * 128, UNIT, 1024), IDESC_ACC,
+                                      desc_of(b_lo + ks * 128, kSw128DescHi), IDESC_ACC,
                                       accumulate || ks > 0);
                     tc_commit(&bar[H_EMPTY + h]);
                 }

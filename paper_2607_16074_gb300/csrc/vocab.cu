@@ -234,6 +234,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
         uint32_t phase = 0;
         bool ok = true;
         const uint32_t a0 = smem_u32(smem), b0 = a0 + A_BYTES;
+        const uint32_t a_lo = AMN ? sw128_desc_mn_lo(a0, A_BYTES / 2) : sw128_desc_lo(a0);
+        const uint32_t b_lo = BMN ? sw128_desc_mn_lo(b0, A_BYTES / 2) : sw128_desc_lo(b0);
         for (int tile = first; ok && tile < num_tiles && !__any_sync(0xffffffffu, *abort_flag);
              tile += step, ++local) {
             const VocabTile t = vocab_tile(tile, num_m, num_n);
@@ -250,19 +252,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                     break;
                 }
                 tc_fence_after();
-                const uint32_t off = (uint32_t)(stage * STAGE_BYTES);
+                const uint32_t off = (uint32_t)(stage * STAGE_BYTES) >> 4;
                 if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < BK / 16; ++kk) {
-                        // 16 K rows of an MN-major operand are two 8-row atoms
-                        const uint64_t da =
-                            AMN ? sw128_desc_mn(a0 + off + kk * 2048, A_BYTES / 2, 1024)
-                                : sw128_desc(a0 + off + kk * 32);
-                        const uint64_t db =
-                            BMN ? sw128_desc_mn(b0 + off + kk * 2048, A_BYTES / 2, 1024)
-                                : sw128_desc(b0 + off + kk * 32);
-                        tc_mma_f16_pair(dcol, da, db, IDESC, (kb - k0) | kk);
-                    }
+                    for (int kk = 0; kk < BK / 16; ++kk)
+                        // (16 K rows of an MN-major operand are two 8-row atoms)
+                        tc_mma_f16_pair(dcol, desc_of(a_lo + off + kk * (AMN ? 128 : 2), kSw128DescHi),
+                                        desc_of(b_lo + off + kk * (BMN ? 128 : 2), kSw128DescHi), IDESC,
+                                        (kb - k0) | kk);
                     tc_commit_pair(&empty[stage]);
                 }
                 __syncwarp();
