@@ -18,6 +18,13 @@
 // is double-buffered; instead the products and the elementwise warps take the halves of a
 // tile in turn: P^T (over S) feeds dV, and S of the next tile follows dV while dS is
 // formed; dS (over dP) feeds dK, and the next dP follows dK while P is formed.
+// (In the queries' pass, whose one accumulator leaves room, a second dP was slower: 564 ->
+// 598 us.)
+//
+// Six documents of up to 2,600 tokens, 32 heads of 128 (424 GFLOP with the forward): 427 us
+// the passes, 37 the rows' values and 6 the rows of few keys, 608 with the forward's 131.
+// The tensor core is busy for 42 % of it: the elementwise warps' P and dS and the products
+// wait for each other, as there is no TMEM to double-buffer either.
 //
 // Warps (one CTA an SM, items claimed from one queue, the longest of each pass first):
 //   0     claims items and hands them out; TMA: the item's outer tiles (K and V, or Q
@@ -912,9 +919,13 @@ static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows&
 // DK and DQ: S, dP and the accumulator fill TMEM; dP is read first, and the next one runs
 // while dS is formed, over S; then the sum and the next S.  DV: two S, issued two tiles
 // ahead.  (Tiles of 64 inner rows, double-buffered, left the tensor core at half:
-// a product of 128 x 64 x 16 from shared memory takes what one of 128 x 128 x 16 does.
-// 26 samples of up to 840 tokens, forward and gradients 242 -> 237 us, of which 41 forward; the
-// rest is bound by shared memory: 448 KB a tile of DK or DQ at some 100 bytes a clock.)
+// a product of 128 x 64 x 16 from shared memory takes 48 clocks and one of 128 x 128 x 16
+// takes 64, 128 bytes a clock of operands either way.)
+// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 156 us
+// the passes and 14 the parts' sums, 281 with the forward's 58 and the rows' values.  Eight
+// products for the gradients' five, and the tensor core busy for 37 %: an item is a few tiles,
+// and its first loads, its last products and its sums out are nobody's company, there being
+// neither TMEM nor shared memory for a second item.
 // ---------------------------------------------------------------------------
 namespace pwide {
 constexpr int BM = 128, HD = 256, NCH = 4;

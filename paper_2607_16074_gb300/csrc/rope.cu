@@ -11,6 +11,10 @@
 // the rows of the next pass are under way while one is worked on.  The angles of a CTA's
 // tokens are computed once into shared memory and serve all of a token's heads, laid out
 // so that a row's lanes read neighbours (they were 4 to 8 ways in conflict as they come).
+// 9,001 tokens, 32 and 8 heads of 128: 33.6 us, 5.5 TB/s.  30,011 tokens, 16 and 16 of 64:
+// 44 us forward (5.6 TB/s) and 88 its gradients (4.2).  One token each of 16 sequences, 8
+// heads and 1 of 256 into a cache: 2.65 us, a launch's latency.  (Rows through bulk copies
+// in shared memory were slower: 126 for 99 us forward at head dim 128, 356 for 212 back.)
 //
 // An angle is taken modulo whole turns before it is rounded: the frequency is a 64-bit
 // fraction of a turn, so position times frequency in wrapping 64-bit integers is the
