@@ -337,7 +337,7 @@ jnx_status jnx_op_vocab_loss(const uint16_t* h, int64_t ldh, const uint16_t* w, 
 /* The losses and the gradients of sum_i row_weight[i] loss[i]: dh [n_rows, d] (lddh) and
  * dw [vocab, d] (lddw; NULL: a frozen vocabulary), bf16, summed in fp32.  Rows are taken
  * in pieces of piece_rows (0: at most 8,192): the workspace holds one piece's
- * probabilities in bf16. */
+ * probabilities in bf16; one for so many rows serves fewer as well. */
 size_t jnx_op_vocab_loss_train_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d,
                                                int32_t piece_rows);
 jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw,

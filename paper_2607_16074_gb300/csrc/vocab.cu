@@ -628,16 +628,17 @@ static int vocab_piece(int n_rows, int piece_rows) {
 
 // Parts of dh's contraction over the vocabulary: as many as bring its tiles, d being
 // narrow, nearest to whole rounds of the SM pairs, a K step of a tile being 0.33 us and
-// the parts' sums passing memory twice at 6 TB/s.
+// the parts' sums passing memory twice at 6 TB/s.  Alike for all rows of a block.
 static int vocab_split(int rows, int vocab_size, int d) {
     using namespace vocab;
-    const long long tiles = (long long)((rows + BM - 1) / BM) * ((d + BN - 1) / BN);
+    const int row_blocks = (rows + BM - 1) / BM;
+    const long long tiles = (long long)row_blocks * ((d + BN - 1) / BN);
     const int pairs = 76, ksteps = (vocab_size + BK - 1) / BK;
     int best = 1;
     double best_us = 1e30;
     for (int s = 1; s <= 16 && s <= std::max(1, ksteps / 8); ++s) {
         const double us = 0.33 * ksteps * (double)((tiles * s + pairs - 1) / pairs) / s +
-                          (s > 1 ? 3.0 + (double)s * rows * d * 8 / 6e6 : 0.0);
+                          (s > 1 ? 3.0 + (double)s * row_blocks * BM * d * 8 / 6e6 : 0.0);
         if (us < best_us - 1e-9) {
             best_us = us;
             best = s;
@@ -657,7 +658,20 @@ struct VocabWs {
     float* acc;
     size_t bytes;
 };
-static VocabWs vocab_ws(void* base, int n, int vocab_size, int d, int piece, bool train) {
+// Rows of dh's parts of a piece, and the most that pieces of up to so many rows have: fewer
+// rows can have more parts.
+static size_t vocab_parts_rows(int piece, int vocab_size, int d) {
+    const int split = vocab_split(piece, vocab_size, d);
+    return split > 1 ? (size_t)split * piece : 0;
+}
+static size_t vocab_parts_rows_upto(int piece, int vocab_size, int d) {
+    size_t most = 0;
+    for (long long rows = vocab::BM; rows < piece + vocab::BM; rows += vocab::BM)
+        most = std::max(most, vocab_parts_rows((int)std::min<long long>(rows, piece), vocab_size, d));
+    return most;
+}
+static VocabWs vocab_ws(void* base, int n, int vocab_size, int d, int piece, bool train,
+                        size_t parts_rows) {
     using namespace vocab;
     VocabWs w{};
     uint8_t* at = static_cast<uint8_t*>(base);
@@ -677,8 +691,7 @@ static VocabWs vocab_ws(void* base, int n, int vocab_size, int d, int piece, boo
     w.at_target = reinterpret_cast<float*>(take(rows * 4));
     if (train) {
         w.G = reinterpret_cast<uint16_t*>(take(rows * ld_g(vocab_size) * 2));
-        const int split = vocab_split(piece, vocab_size, d);
-        w.parts = reinterpret_cast<float*>(take(split > 1 ? (size_t)split * piece * d * 4 : 0));
+        w.parts = reinterpret_cast<float*>(take(parts_rows * d * 4));
         w.acc = reinterpret_cast<float*>(take(n > piece ? (size_t)vocab_size * d * 4 : 0));
     }
     w.bytes = used + 255;
@@ -692,11 +705,14 @@ static void* align256(void* p) {
 static jnx_status vocab_run(const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw,
                             const int32_t* targets, const float* weight, int n, int vocab_size,
                             int d, int piece, float* loss, uint16_t* dh, int64_t lddh,
-                            uint16_t* dw, int64_t lddw, void* workspace, int* status,
-                            const char* what, cudaStream_t s) {
+                            uint16_t* dw, int64_t lddw, void* workspace, size_t ws_bytes,
+                            int* status, const char* what, cudaStream_t s) {
     using namespace vocab;
     const bool train = weight != nullptr;
-    const VocabWs ws = vocab_ws(align256(workspace), n, vocab_size, d, piece, train);
+    const VocabWs ws = vocab_ws(align256(workspace), n, vocab_size, d, piece, train,
+                                train ? vocab_parts_rows(piece, vocab_size, d) : 0);
+    if (!workspace || ws_bytes < ws.bytes)
+        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small", what);
     TraceScope ts(JNX_K_VOCAB, 0.0, s);
     pdl(k_vocab_pack, 1, 1024, 0, s)(targets, n, vocab_size, ws.count, ws.index, ws.packed, ws.place,
                                      status);
@@ -760,7 +776,7 @@ using namespace jnx;
 
 extern "C" size_t jnx_op_vocab_loss_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d) {
     if (n_rows < 0 || vocab <= 0 || d <= 0) return 0;
-    return vocab_ws(nullptr, n_rows, vocab, d, vocab_piece(n_rows, 0), false).bytes;
+    return vocab_ws(nullptr, n_rows, vocab, d, vocab_piece(n_rows, 0), false, 0).bytes;
 }
 
 extern "C" jnx_status jnx_op_vocab_loss(const uint16_t* h, int64_t ldh, const uint16_t* w,
@@ -771,17 +787,17 @@ extern "C" jnx_status jnx_op_vocab_loss(const uint16_t* h, int64_t ldh, const ui
     const char* what = "vocab loss";
     if (jnx_status st = vocab_check(h, ldh, w, ldw, targets, n_rows, vocab, d, loss, what)) return st;
     if (n_rows == 0) return JNX_OK;
-    if (!workspace || ws_bytes < jnx_op_vocab_loss_workspace_bytes(n_rows, vocab, d))
-        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small", what);
     return vocab_run(h, ldh, w, ldw, targets, nullptr, n_rows, vocab, d, vocab_piece(n_rows, 0), loss,
-                     nullptr, 0, nullptr, 0, workspace, status, what,
+                     nullptr, 0, nullptr, 0, workspace, ws_bytes, status, what,
                      static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t jnx_op_vocab_loss_train_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d,
                                                           int32_t piece_rows) {
     if (n_rows < 0 || vocab <= 0 || d <= 0) return 0;
-    return vocab_ws(nullptr, n_rows, vocab, d, vocab_piece(n_rows, piece_rows), true).bytes;
+    const int piece = vocab_piece(n_rows, piece_rows);
+    return vocab_ws(nullptr, n_rows, vocab, d, piece, true,
+                    vocab_parts_rows_upto(piece, vocab, d)).bytes;
 }
 
 extern "C" jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, const uint16_t* w,
@@ -798,9 +814,6 @@ extern "C" jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, co
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned gradients", what);
     if (dw && (!aligned16(dw) || lddw % 8 || lddw < d))
         return fail(JNX_ERR_INVALID_ARG, "%s: misaligned weight gradient", what);
-    if (n_rows > 0 && (!workspace || ws_bytes < jnx_op_vocab_loss_train_workspace_bytes(
-                                                    n_rows, vocab, d, piece_rows)))
-        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small", what);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (n_rows == 0) {
         if (dw && cudaMemset2DAsync(dw, lddw * 2, 0, (size_t)d * 2, vocab, s) != cudaSuccess)
@@ -808,6 +821,6 @@ extern "C" jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, co
         return JNX_OK;
     }
     return vocab_run(h, ldh, w, ldw, targets, row_weight, n_rows, vocab, d,
-                     vocab_piece(n_rows, piece_rows), loss, dh, lddh, dw, lddw, workspace, status,
-                     what, s);
+                     vocab_piece(n_rows, piece_rows), loss, dh, lddh, dw, lddw, workspace, ws_bytes,
+                     status, what, s);
 }

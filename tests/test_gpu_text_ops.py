@@ -620,6 +620,18 @@ def test_vocab_loss_train_in_pieces(piece):
     T.close(dw, want["dw"], want["dw_tol"], "dw")
 
 
+@pytest.mark.parametrize("most,n", [(168, 100), (256, 161), (700, 300)])
+def test_vocab_loss_train_of_fewer_rows_than_it_was_made_for(most, n):
+    """Fewer rows may take dh's sum over the vocabulary in more parts."""
+    h, w, t, rw = vocab_case(n, 8000, 1024, 6)
+    loss, dh, dw = vocab_train(h, w, t, rw)
+    loss2, dh2, dw2 = empty(n, dtype=torch.float32), empty(*h.shape), empty(*w.shape)
+    op = _r().VocabLoss(w, max_rows=most)
+    op.train(h, t, rw, loss2, dh2, dw2)
+    op.check()
+    assert torch.equal(loss, loss2) and torch.equal(dh, dh2) and torch.equal(dw, dw2)
+
+
 def test_vocab_loss_frozen_vocabulary():
     h, w, t, rw = vocab_case(150, 900, 128, 3)
     loss, dh, dw = vocab_train(h, w, t, rw)

@@ -186,3 +186,14 @@ def test_work_lists_cover_every_row_and_key_once(heads):
             return visible(s, min(a + step, q[s]) - 1)
         costs = [cost(int(s), int(a)) for s, a in items]
         assert all(x >= y for x, y in itertools.pairwise(costs))
+
+
+@pytest.mark.parametrize("vocab,d,piece", [(32000, 2048, 0), (32000, 4096, 256), (32000, 8192, 1000),
+                                           (50257, 512, 0), (151936, 1024, 1000), (300, 64, 0)])
+def test_vocab_workspaces_for_many_rows_hold_fewer(vocab, d, piece):
+    """A workspace made for so many rows serves every smaller call: sizes never fall."""
+    L = J.lib()
+    for size in (lambda n: L.jnx_op_vocab_loss_train_workspace_bytes(n, vocab, d, piece),
+                 lambda n: L.jnx_op_vocab_loss_workspace_bytes(n, vocab, d)):
+        sizes = [size(n) for n in range(0, 3000)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:]))
