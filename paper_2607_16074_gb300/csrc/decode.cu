@@ -313,21 +313,21 @@ __global__ void __launch_bounds__(128) k_decode_join(const __grid_constant__ Dec
     using namespace decode;
     constexpr int E = HD / 32, R = MAX_RUNS / 32;
     const int w = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    // the lengths are older than the grid ahead, which starts this one only once all its
-    // CTAs have waited for what came before: they need no wait
-    const int b = min(w / a.H, a.batch - 1), h = w % a.H;
-    const int n = decode_length(a, b, false), nr = runs(n);
     pdl_entry();
-    if (w >= a.batch * a.H || nr == 1) return;
+    if (w >= a.batch * a.H) return;
+    const int b = w / a.H, h = w % a.H;
+    // the first runs' sums are asked for along with the length that says which count
     const float* src = a.part + (size_t)w * MAX_RUNS * (HD + 2);
+    float2 ml = *reinterpret_cast<const float2*>(src + lane * (HD + 2) + HD);
+    const int nr = runs(decode_length(a, b, false));
+    if (nr == 1) return;
     float m[R], l[R], top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int r = i * 32 + lane;
-        const float2 ml = r < nr ? *reinterpret_cast<const float2*>(src + r * (HD + 2) + HD)
-                                 : make_float2(-INFINITY, 0.f);
-        m[i] = ml.x;
-        l[i] = ml.y;
+        if (i > 0 && r < nr) ml = *reinterpret_cast<const float2*>(src + r * (HD + 2) + HD);
+        m[i] = r < nr ? ml.x : -INFINITY;
+        l[i] = r < nr ? ml.y : 0.f;
         top = fmaxf(top, m[i]);
     }
 #pragma unroll
