@@ -13,8 +13,8 @@
 // (CTAs that share a unit and a join by the last CTA to finish took half as long again:
 // 307 us where the warps' own units and the second kernel take 206.)
 //
-// 64 sequences of up to 8,100 tokens, 32 heads on 8 of 128 (1.17 GB): 206 us, 5.65 TB/s.
-// 8 of up to 700, 8 heads on one of 256: 11.2 us, where memory is not what counts: the
+// 64 sequences of up to 8,100 tokens, 32 heads on 8 of 128 (1.17 GB): 203 us, 5.75 TB/s.
+// 8 of up to 700, 8 heads on one of 256: 9.2 us, where memory is not what counts: the
 // lengths, a unit's tiles, its sums and the join follow one another, 1-2 us each.
 #include <algorithm>
 
@@ -34,7 +34,9 @@ constexpr int MAX_RUNS = 128;  // runs of a sequence
 
 // Tokens of a sequence's runs: short ones for short sequences, so that a few sequences
 // reach many SMs; long enough beyond that a run's sums (hd + 2 floats a head) are a few
-// percent of what it reads.
+// percent of what it reads.  (Runs half as long from 1,024 tokens on: 64 sequences of up to
+// 4,000 tokens, 8 heads on one of 256, 38.6 us for 33.3; runs of 32 below, 128 of up to 700
+// 23.8 for 18.9.)
 __host__ __device__ inline int run_tokens(int n) {
     int r = n <= 1024 ? 64 : n <= 4096 ? 128 : 256;
     const int most = (n + MAX_RUNS - 1) / MAX_RUNS;
@@ -54,7 +56,9 @@ struct DecodeArgs {
     uint16_t* out;
     long long o_row, o_head;
     const int *slot, *n;
-    float* part;  // [batch][H][MAX_RUNS][hd + 2]: sums, maximum, sum of exponentials
+    int* first;   // [batch + 1]: a sequence's first run among all
+    float2* ml;   // [run][H]: maxima and sums of exponentials
+    float* part;  // [run][H][hd]: sums
     int* status;
 };
 
@@ -127,10 +131,16 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
                 const int x = __shfl_up_sync(0xffffffffu, run, o);
                 if (lane >= o) run += x;
             }
-            if (b < a.batch) first[b] = total + run - mine;
+            if (b < a.batch) {
+                first[b] = total + run - mine;
+                if (blockIdx.x == 0) a.first[b] = total + run - mine;
+            }
             total += __shfl_sync(0xffffffffu, run, 31);
         }
-        if (lane == 0) first[a.batch] = total;
+        if (lane == 0) {
+            first[a.batch] = total;
+            if (blockIdx.x == 0) a.first[a.batch] = total;
+        }
     }
     __syncthreads();
     const int per_run = a.Hkv * a.blocks;  // units of a run: its heads, which lie together
@@ -293,12 +303,13 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
                     *reinterpret_cast<uint32_t*>(dst + c * 8) =
                         cvt_bf2(o[c][2 * i] * inv, o[c][2 * i + 1] * inv);
             } else {
-                float* dst = a.part + (((size_t)x.b * a.H + h) * MAX_RUNS + x.run) * (HD + 2);
+                const size_t at = (size_t)(first[x.b] + x.run) * a.H + h;
+                float* dst = a.part + at * HD;
 #pragma unroll
                 for (int c = 0; c < HD / 8; ++c)
                     *reinterpret_cast<float2*>(dst + c * 8 + cq) =
                         make_float2(o[c][2 * i], o[c][2 * i + 1]);
-                if ((lane & 3) == 0) *reinterpret_cast<float2*>(dst + HD) = make_float2(m[i], l[i]);
+                if ((lane & 3) == 0) a.ml[at] = make_float2(m[i], l[i]);
             }
         }
     }
@@ -307,59 +318,117 @@ __global__ void __launch_bounds__(32 * decode::WARPS, 1)
     for (; taken < asked; ++taken) mbar_wait_warp(&full[taken % STAGES], (taken / STAGES) & 1, 100000000LL);
 }
 
-// A sequence's runs joined, a warp a query head.
-template <int HD>
-__global__ void __launch_bounds__(128) k_decode_join(const __grid_constant__ DecodeArgs a) {
+// A sequence's runs joined: the runs' sums in G turns, each turn's in order, then the turns'
+// in theirs.  WIDE: a CTA a query head and a group of threads a turn, so that all loads are
+// under way at once; else a group takes a head's turns by itself, for more heads than the SMs
+// hold CTAs of.  (8 sequences of up to 4,000 tokens, 8 heads on one of 256: 13.2 us wide, 16.8
+// a warp a head.)
+template <int HD, bool WIDE>
+__global__ void __launch_bounds__(256) k_decode_join(const __grid_constant__ DecodeArgs a) {
     using namespace decode;
-    constexpr int E = HD / 32, R = MAX_RUNS / 32;
-    const int w = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    constexpr int LANES = HD == 256 ? 64 : 32, E = HD / LANES, G = 256 / LANES;
+    constexpr int HEADS = WIDE ? 1 : G;  // of a CTA
+    __shared__ float sums[WIDE ? 256 * E : 1];
     pdl_entry();
+    const int t = threadIdx.x, lane = t & 31, g = t / LANES, c = t % LANES;
+    const int w = WIDE ? blockIdx.x : blockIdx.x * HEADS + g;
     if (w >= a.batch * a.H) return;
     const int b = w / a.H, h = w % a.H;
-    // the first runs' sums are asked for along with the length that says which count
-    const float* src = a.part + (size_t)w * MAX_RUNS * (HD + 2);
-    float2 ml = *reinterpret_cast<const float2*>(src + lane * (HD + 2) + HD);
-    const int nr = runs(decode_length(a, b, false));
+    const int r0 = a.first[b], nr = a.first[b + 1] - r0;
     if (nr == 1) return;
-    float m[R], l[R], top = -INFINITY, sum = 0.f;
+    const float2* ml = a.ml + (size_t)r0 * a.H + h;
+    const float* src = a.part + ((size_t)r0 * a.H + h) * HD + c * E;
+    const size_t step = (size_t)a.H * HD;
+    float m[MAX_RUNS / 32], l[MAX_RUNS / 32], top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
+    for (int i = 0; i < MAX_RUNS / 32; ++i) {
         const int r = i * 32 + lane;
-        if (i > 0 && r < nr) ml = *reinterpret_cast<const float2*>(src + r * (HD + 2) + HD);
-        m[i] = r < nr ? ml.x : -INFINITY;
-        l[i] = r < nr ? ml.y : 0.f;
+        const float2 x = r < nr ? ml[(size_t)r * a.H] : make_float2(-INFINITY, 0.f);
+        m[i] = x.x;
+        l[i] = x.y;
         top = fmaxf(top, m[i]);
     }
+    constexpr int R = 8;  // runs of a thread under way
+    float v[R][E];
+    auto load = [&](int i, int r) {
+        if (r >= nr) return;
+        if constexpr (E == 4) {
+            const float4 x = *reinterpret_cast<const float4*>(src + r * step);
+            v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
+        } else {
+            const float2 x = *reinterpret_cast<const float2*>(src + r * step);
+            v[i][0] = x.x, v[i][1] = x.y;
+        }
+    };
+    constexpr int STEP = WIDE ? G : 1;
+#pragma unroll
+    for (int i = 0; i < R; ++i) load(i, (WIDE ? g : 0) + i * STEP);
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
+    for (int i = 0; i < MAX_RUNS / 32; ++i) {
         m[i] = ex2_approx(m[i] - top);
         sum += l[i] * m[i];
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    float acc[E] = {};
+    const float inv = 1.f / sum;
+    auto factor = [&](int r) {
+        const int i = r >> 5;
+        const float x = i == 0 ? m[0] : i == 1 ? m[1] : i == 2 ? m[2] : m[3];
+        return __shfl_sync(0xffffffffu, x, r & 31);
+    };
+    static_assert(MAX_RUNS == 128, "factors of four registers");
+    float acc[HEADS][E] = {};  // WIDE: this group's turn, else every turn
+    for (int r = WIDE ? g : 0; r < nr; r += R * STEP) {
+        if (r >= R * STEP) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        if (i * 32 >= nr) break;
-#pragma unroll 8
-        for (int j = 0; j < min(32, nr - i * 32); ++j) {
-            const float f = __shfl_sync(0xffffffffu, m[i], j);
-            const float* s = src + (i * 32 + j) * (HD + 2) + lane * 2;
+            for (int i = 0; i < R; ++i) load(i, r + i * STEP);
+        }
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                const float2 v = *reinterpret_cast<const float2*>(s + e * 32);
-                acc[e] += f * v.x;
-                acc[e + 1] += f * v.y;
+        for (int i = 0; i < R; ++i) {
+            if (r + i * STEP >= nr) continue;
+            const float f = factor(r + i * STEP);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float& to = acc[WIDE ? 0 : i % G][e];  // (R is a multiple of G)
+                to = fmaf(f, v[i][e], to);
             }
         }
     }
-    const float inv = 1.f / sum;
-    uint16_t* o = a.out + b * a.o_row + h * a.o_head + lane * 2;
+    static_assert(R % G == 0, "turns of a batch");
+    float all[E];
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[e * 256 + t] = acc[0][e];
+        __syncthreads();
+        if (g > 0) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            all[e] = acc[0][e];
+#pragma unroll
+            for (int i = 1; i < G; ++i) all[e] += sums[e * 256 + i * LANES + c];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            all[e] = acc[0][e];
+#pragma unroll
+            for (int i = 1; i < G; ++i) all[e] += acc[i][e];
+        }
+    }
+    uint16_t* o = a.out + b * a.o_row + h * a.o_head + c * E;
 #pragma unroll
     for (int e = 0; e < E; e += 2)
-        *reinterpret_cast<uint32_t*>(o + e * 32) = cvt_bf2(acc[e] * inv, acc[e + 1] * inv);
+        *reinterpret_cast<uint32_t*>(o + e) = cvt_bf2(all[e] * inv, all[e + 1] * inv);
+}
+
+// The workspace: the first runs of a launch's sequences, then its runs' sums.
+static size_t decode_sums_at(int batch) {
+    return ((size_t)std::min(batch, decode::BATCH) + 1 + 3) / 4 * 16;
+}
+static size_t decode_runs(int batch) {
+    return (size_t)std::min(batch, decode::BATCH) * decode::MAX_RUNS;
 }
 
 template <int HD>
@@ -382,12 +451,13 @@ static jnx_status launch_decode(const jnx_kv_cache& c, DecodeArgs a, cudaStream_
         const long long units = (long long)a.batch * most * a.Hkv * a.blocks;
         const int grid = (int)std::min<long long>(units, num_sms());
         pdl(k_decode_attn<HD>, grid, 32 * WARPS, C::SMEM, s)(tk, tv, a);
-        if (most > 1) pdl(k_decode_join<HD>, (a.batch * a.H + 3) / 4, 128, 0, s)(a);
+        const int heads = a.batch * a.H, of_cta = HD == 256 ? 4 : 8;
+        if (most > 1 && heads <= num_sms() * 8) pdl(k_decode_join<HD, true>, heads, 256, 0, s)(a);
+        else if (most > 1) pdl(k_decode_join<HD, false>, (heads + of_cta - 1) / of_cta, 256, 0, s)(a);
         a.q += a.batch * a.q_row;
         a.out += a.batch * a.o_row;
         a.slot += a.batch;
         a.n += a.batch;
-        a.part += (size_t)a.batch * a.H * MAX_RUNS * (HD + 2);
     }
     return launched("decode attention");
 }
@@ -399,7 +469,7 @@ using namespace jnx;
 extern "C" size_t jnx_op_decode_attention_workspace_bytes(int32_t batch, int32_t n_heads,
                                                           int32_t head_dim) {
     if (batch < 0 || n_heads <= 0 || head_dim <= 0) return 0;
-    return (size_t)batch * n_heads * decode::MAX_RUNS * (head_dim + 2) * sizeof(float);
+    return decode_sums_at(batch) + decode_runs(batch) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
 extern "C" jnx_status jnx_op_decode_attention(const jnx_kv_cache* cache, int32_t batch,
@@ -418,14 +488,19 @@ extern "C" jnx_status jnx_op_decode_attention(const jnx_kv_cache* cache, int32_t
     if ((int64_t)batch * n_heads > 0x7fffff00 ||
         (int64_t)decode::BATCH * decode::MAX_RUNS * n_heads > 0x7fff0000)
         return fail(JNX_ERR_UNSUPPORTED, "%s: sizes", what);
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7) ||
+    if (!workspace || !aligned16(workspace) ||
         ws_bytes < jnx_op_decode_attention_workspace_bytes(batch, n_heads, head_dim))
         return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
     const int group = n_heads / n_kv_heads;
     DecodeArgs a{batch, n_heads, n_kv_heads, group, (group + decode::ROWS - 1) / decode::ROWS,
                  cache->n_slots, cache->room, (float)(1.4426950408889634 / sqrt((double)head_dim)),
                  q->ptr, q->row_stride, q->head_stride, out->ptr, out->row_stride,
-                 out->head_stride, slot, n_cached, static_cast<float*>(workspace), status};
+                 out->head_stride, slot, n_cached, static_cast<int*>(workspace), nullptr, nullptr,
+                 status};
+    // one launch's runs at a time: a launch starts when the one ahead is through
+    uint8_t* ws = static_cast<uint8_t*>(workspace) + decode_sums_at(batch);
+    a.part = reinterpret_cast<float*>(ws);
+    a.ml = reinterpret_cast<float2*>(a.part + decode_runs(batch) * n_heads * head_dim);
     // an empty cache has no tiles, but the maps want extents
     jnx_kv_cache c = *cache;
     c.n_slots = std::max(c.n_slots, 1);

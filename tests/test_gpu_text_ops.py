@@ -527,6 +527,25 @@ def test_decode_attention_bits_do_not_depend_on_the_batch():
         assert torch.equal(alone[0], out[i])
 
 
+@pytest.mark.parametrize("heads", [(64, 8, 64), (64, 8, 128), (64, 8, 256)])
+def test_decode_attention_bits_do_not_depend_on_how_many_heads_are_joined(heads):
+    """Sequences of 1 to 16 runs: among 1,920 heads, and each by itself."""
+    h, hkv, hd = heads
+    g = gen(12)
+    kc, vc = normal(g, 3, 1024, hkv, hd), normal(g, 3, 1024, hkv, hd)
+    q = normal(g, 30, h, hd)
+    i32 = lambda x: torch.tensor(x, device="cuda", dtype=torch.int32)  # noqa: E731
+    n = [1024, 64, 65, 700, 129, 0, 960, 1, 300, 513] * 3
+    op, out, alone = _r().DecodeAttention(*heads, max_batch=30), empty(30, h, hd), empty(1, h, hd)
+    op.forward(q, kc, vc, i32([i % 3 for i in range(30)]), i32(n), out)
+    for i in range(30):
+        op.forward(q[i:i + 1], kc, vc, i32([i % 3]), i32(n[i:i + 1]), alone)
+        assert torch.equal(alone[0], out[i])
+    op.check()
+    want = decode_want(q[:6], kc, vc, i32([i % 3 for i in range(6)]), n[:6])
+    T.close(out[:6], want["out"], want["out_tol"])
+
+
 def test_decode_attention_batches_of_all_sizes_share_a_workspace():
     """Large and small batches in turn on one object: what a call leaves behind is what the
     next expects."""
