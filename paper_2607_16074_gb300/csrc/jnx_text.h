@@ -48,6 +48,12 @@ __host__ __device__ inline int item_tiles(int head_dim) { return head_dim == 256
 
 constexpr int kMaxGroup = 64;
 
+// Rows that see up to so many keys have what rounding left of their output kept for the
+// gradients.  D = rowsum(dO * O) is a sum that dP nearly cancels against where few keys make a
+// row; beyond, the rounding of O is one of several alike: dQ off by 0.0027 of its norm for
+// 0.0025, where rows of two keys are off by 0.0055 for 0.0035.
+constexpr int kRestKeys = 64;
+
 // Parts that the gradients' keys pass takes a 128-key tile's rows in: one where a sequence
 // has a tile for every SM by itself, else 2,048 rows each (token, head of the group).  Of
 // the sequence and the heads alone, so that a sequence's bits do not depend on others.  A

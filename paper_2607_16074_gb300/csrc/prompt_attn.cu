@@ -124,7 +124,8 @@ __device__ __forceinline__ void stage_rows(uint8_t* stg, int lane, const uint32_
     __syncwarp();
 }
 
-// REST: a.rest is written, for which the inference's rows have no registers to spare.
+// REST: a.rest is written, of rows that see few keys, for which the inference's rows have no
+// registers to spare.
 template <int HD, bool REST>
 __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
     k_prompt_attn(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
@@ -586,6 +587,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             const volatile int* s = slots + 8 * (seen % ITEMS);
             const int i = s[1] + t * T + tok, row0 = s[0], h = s[6] * a.group + hg;
             const bool live = tok < T && i < s[2];
+            const bool few = REST && live && keys_seen(i, s[2], s[4], s[5]) <= kRestKeys;
             item_done();
             if (live && a.lse) a.lse[(size_t)(row0 + i) * a.H + h] = m + log2f(l);
             const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -595,8 +597,9 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             long long to[4], ro[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) to[j] = __shfl_sync(0xffffffffu, o, 8 * j + (lane >> 2));
+            const bool rest = __any_sync(0xffffffffu, few);
             if constexpr (REST) {
-                o = live ? (long long)(row0 + i) * a.r_row + h * a.r_head : -1;
+                o = few ? (long long)(row0 + i) * a.r_row + h * a.r_head : -1;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) ro[j] = __shfl_sync(0xffffffffu, o, 8 * j + (lane >> 2));
             }
@@ -619,7 +622,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                 for (int e = 0; e < 32; ++e)
                     w[e] = l > 0.f ? __float_as_uint(__uint_as_float(w[e]) * inv) : 0u;
                 stage_rows(stg, lane, w, a.out + c * 32, to);
-                if constexpr (REST) {
+                if (REST && rest) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         w[e] = __float_as_uint(__uint_as_float(w[e]) - bf2f(f2bf(__uint_as_float(w[e]))));

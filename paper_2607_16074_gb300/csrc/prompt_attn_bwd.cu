@@ -134,33 +134,32 @@ __device__ __forceinline__ float lanes_sum(float d) {
 // as they lie 37.)
 template <int HD>
 __global__ void __launch_bounds__(256)
-    k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows rest, jnx_head_rows dout, const float* lse,
-                      int rows, int H, int group, float2* row, int* claimed) {
+    k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, const float* lse, int rows, int H, int group,
+                      float2* row, int* claimed) {
     constexpr int LANES = HD / 8, PER = 256 / LANES;
     pdl_entry();
     if (blockIdx.x == 0 && threadIdx.x == 0) *claimed = 0;
     const long long all = (long long)rows * H;
     const long long w0 = (long long)blockIdx.x * PER * 4 + threadIdx.x / LANES;
     const int c = threadIdx.x % LANES * 8;
-    uint4 g[4], o[4], e[4];
+    uint4 g[4], o[4];
     float l[4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const long long w = w0 + b * PER;
-        g[b] = o[b] = e[b] = make_uint4(0, 0, 0, 0);
+        g[b] = o[b] = make_uint4(0, 0, 0, 0);
         l[b] = 0.f;
         if (w < all) {
             const long long r = w / H;
             const int h = (int)(w - r * H);
             g[b] = head_unit(dout, r, h, c);
             o[b] = head_unit(out, r, h, c);
-            if (rest.ptr) e[b] = head_unit(rest, r, h, c);
             l[b] = lse[w];
         }
     }
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-        const float d = lanes_sum<LANES>(dot8(o[b], g[b]) + dot8(e[b], g[b]));
+        const float d = lanes_sum<LANES>(dot8(o[b], g[b]));
         const long long w = w0 + b * PER;
         if (w < all && c == 0) {
             const long long r = w / H;
@@ -171,45 +170,57 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-// Rows that see up to kFewKeys keys: their D over again, as the sum of P dP in fp32.  dS =
-// P (dP - D) adds up to zero over a row's keys only as far as D is what the kernel's own P
-// and dP add up to.  rowsum(dO * O) is off by the roundings of the forward's P (and of O,
-// without `rest`), which shows where few terms nearly cancel: dQ of sequences of two tokens
-// was off by 0.0050 of its norm, against 0.0024 that its own two roundings make.  A CTA a
-// sequence and key head.
+// Rows that see few keys: their D over again.  dS = P (dP - D) adds up to zero over a row's
+// keys only as far as D is what the kernel's own P and dP add up to.  rowsum(dO * O) is off by
+// the roundings of O, which `rest` makes up for, and of the forward's P, which shows where few
+// terms nearly cancel: dQ of sequences of two tokens was off by 0.0050 of its norm, against
+// 0.0024 that its own two roundings make; up to kFewKeys keys D is the sum of P dP in fp32.
+// A CTA some rows of a sequence and key head.  (Looked up in the kernel above, where a row's
+// sequence is not at hand, these rows took 20 us of 7,000 rows of 32 heads, and here 5.)
 constexpr int kFewKeys = 8;
 template <int HD>
 __global__ void __launch_bounds__(256)
-    k_prompt_bwd_few(jnx_head_rows dout, jnx_head_rows q, jnx_head_rows k, jnx_head_rows v,
-                     const float* lse, const __grid_constant__ PromptBwdArgs p, float2* row) {
+    k_prompt_bwd_few(jnx_head_rows out, jnx_head_rows rest, jnx_head_rows dout, jnx_head_rows q,
+                     jnx_head_rows k, jnx_head_rows v, const float* lse,
+                     const __grid_constant__ PromptBwdArgs p, float2* row) {
     constexpr int LANES = HD / 8, PER = 256 / LANES;
     pdl_entry();
     const int sq = blockIdx.x / p.Hkv, kvh = blockIdx.x % p.Hkv;
     const int q0 = p.cu_q[sq], Lq = p.cu_q[sq + 1] - q0, k0 = p.cu_kv[sq];
     const int Lk = p.cu_kv[sq + 1] - k0, pre = p.prefix ? p.prefix[sq] : 0;
-    if (Lk == 0) return;
+    const int most = rest.ptr ? kRestKeys : kFewKeys;
     // rows [a, b): the first that sees a key, the first that sees too many
-    const int a = first_row(0, Lq, Lk, pre), b = Lk > kFewKeys ? first_row(kFewKeys, Lq, Lk, pre) : Lq;
-    const int c = threadIdx.x % LANES * 8, n = (b - a) * p.group;
-    for (int r0 = 0; r0 < n; r0 += PER) {
+    const int a = first_row(0, Lq, Lk, pre), b = Lk > most ? first_row(most, Lq, Lk, pre) : Lq;
+    const int c = threadIdx.x % LANES * 8, n = Lk > 0 ? (b - a) * p.group : 0;
+    for (int r0 = blockIdx.y * PER; r0 < n; r0 += gridDim.y * PER) {
         // a lane without a row of its own goes along with the last
         const int r = min(r0 + (int)threadIdx.x / LANES, n - 1);
         const int i = a + r / p.group, hg = r % p.group, h = kvh * p.group + hg;
         const long long at = q0 + i;
-        const uint4 g = head_unit(dout, at, h, c), x = head_unit(q, at, h, c);
+        const int seen = keys_seen(i, Lq, Lk, pre);
+        const uint4 g = head_unit(dout, at, h, c);
         const float l = lse[at * p.H + h];
-        const int few = keys_seen(i, Lq, Lk, pre);
-        uint4 kk[kFewKeys], vv[kFewKeys];
-#pragma unroll
-        for (int j = 0; j < kFewKeys; ++j) {
-            kk[j] = head_unit(k, k0 + min(j, few - 1), kvh, c);
-            vv[j] = head_unit(v, k0 + min(j, few - 1), kvh, c);
-        }
         float d = 0.f;
+        if (__any_sync(0xffffffffu, seen > kFewKeys)) {
+            d = dot8(head_unit(out, at, h, c), g);
+            if (rest.ptr) d += dot8(head_unit(rest, at, h, c), g);
+            d = lanes_sum<LANES>(d);
+        }
+        if (__any_sync(0xffffffffu, seen <= kFewKeys)) {
+            const uint4 x = head_unit(q, at, h, c);
+            uint4 kk[kFewKeys], vv[kFewKeys];
 #pragma unroll
-        for (int j = 0; j < kFewKeys; ++j) {
-            const float s = lanes_sum<LANES>(dot8(x, kk[j])), dp = lanes_sum<LANES>(dot8(g, vv[j]));
-            if (j < few) d += ex2_approx(fmaf(s, p.scale_log2, -l)) * dp;
+            for (int j = 0; j < kFewKeys; ++j) {
+                kk[j] = head_unit(k, k0 + min(j, seen - 1), kvh, c);
+                vv[j] = head_unit(v, k0 + min(j, seen - 1), kvh, c);
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < kFewKeys; ++j) {
+                const float s = lanes_sum<LANES>(dot8(x, kk[j])), dp = lanes_sum<LANES>(dot8(g, vv[j]));
+                if (j < seen) sum += ex2_approx(fmaf(s, p.scale_log2, -l)) * dp;
+            }
+            if (seen <= kFewKeys) d = sum;
         }
         if (c == 0 && r0 + (int)threadIdx.x / LANES < n)
             row[((long long)kvh * p.rows + at) * p.group + hg] = make_float2(l, d);
@@ -1664,10 +1675,13 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
         constexpr int HD = decltype(width)::value, PER = 4 * 256 / (HD / 8);
         const long long all = (long long)rows * n_heads;
         pdl(k_prompt_bwd_rows<HD>, std::max(1, (int)((all + PER - 1) / PER)), 256, 0, s)(
-            or_none(out, rows), rest && rows ? *rest : none, or_none(dout, rows), lse, rows, n_heads,
-            a.group, row, claimed);
-        if (rows && keys)
-            pdl(k_prompt_bwd_few<HD>, p->n_seqs * n_kv_heads, 256, 0, s)(*dout, *q, *k, *v, lse, a, row);
+            or_none(out, rows), or_none(dout, rows), lse, rows, n_heads, a.group, row, claimed);
+        if (rows && keys) {
+            constexpr int LINE = 256 / (HD / 8);
+            const int most = rest ? kRestKeys : kFewKeys;
+            pdl(k_prompt_bwd_few<HD>, dim3(p->n_seqs * n_kv_heads, (most * a.group + LINE - 1) / LINE),
+                256, 0, s)(*out, rest ? *rest : none, *dout, *q, *k, *v, lse, a, row);
+        }
     };
     if (head_dim == 64) prologue(std::integral_constant<int, 64>{});
     else if (head_dim == 128) prologue(std::integral_constant<int, 128>{});

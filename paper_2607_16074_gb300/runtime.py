@@ -746,7 +746,8 @@ class PromptAttention(_TextOperator):
         self._ref = C.byref(self.struct)
         super().__init__(J.lib().jnx_op_prompt_attention_backward_workspace_bytes(
             self._ref, *self.dims) if gradients else 0, plan.device)
-        # what rounding leaves of the forward's output, for the gradients of the same inputs
+        # what rounding leaves of the forward's output where a row sees few keys, for the
+        # gradients of the same inputs
         self.rest = torch.empty(plan.n_q, n_heads, head_dim, dtype=_BF16,
                                 device=plan.device) if gradients else None
 
