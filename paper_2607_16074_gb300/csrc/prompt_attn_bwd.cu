@@ -21,8 +21,8 @@
 // (In the queries' pass, whose one accumulator leaves room, a second dP was slower: 564 ->
 // 598 us.)
 //
-// Six documents of up to 2,600 tokens, 32 heads of 128 (424 GFLOP with the forward): 427 us
-// the passes, 37 the rows' values and 6 the rows of few keys, 608 with the forward's 131.
+// Six documents of up to 2,600 tokens, 32 heads of 128 (424 GFLOP with the forward): 422 us
+// the passes, 34 the rows' values and 5 the rows of few keys, 588 with the forward's 130.
 // The tensor core is busy for 42 % of it: the elementwise warps' P and dS and the products
 // wait for each other, as there is no TMEM to double-buffer either.
 //
@@ -131,7 +131,7 @@ __device__ __forceinline__ float lanes_sum(float d) {
 // The rows' (lse, D = rowsum(dO * O)), and the claim counter to zero.  HD / 8 lanes a row,
 // four rows of neighbouring heads a lane, whose loads are under way at once.  Bound by HBM.
 // (By tiles of a sequence and key head, 256 bytes a row: 52 us for 7,000 rows of 32 heads;
-// as they lie 37.)
+// as they lie 37, then still with `rest`.)
 template <int HD>
 __global__ void __launch_bounds__(256)
     k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, const float* lse, int rows, int H, int group,
@@ -270,7 +270,8 @@ __device__ __forceinline__ void bwd_rows_part(uint8_t* stg, int lane, const uint
 }
 
 // dk and dv of the tiles taken in parts: their sums in the parts' order.  A CTA 8 keys of a
-// tile and key head, of either gradient.
+// tile and key head, of either gradient.  (Bound by reading the sums: CTAs of 16 keys, or a
+// share of the keys to each part's item so that none is without work, take the same 15 us.)
 __global__ void __launch_bounds__(256) k_prompt_bwd_join(const __grid_constant__ PromptBwdArgs p, int hd) {
     pdl_entry();
     const int2 e = p.items[blockIdx.x / p.Hkv];
@@ -932,8 +933,8 @@ static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows&
 // ahead.  (Tiles of 64 inner rows, double-buffered, left the tensor core at half:
 // a product of 128 x 64 x 16 from shared memory takes 48 clocks and one of 128 x 128 x 16
 // takes 64, 128 bytes a clock of operands either way.)
-// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 156 us
-// the passes and 14 the parts' sums, 281 with the forward's 58 and the rows' values.  Eight
+// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 155 us
+// the passes and 15 the parts' sums, 247 with the forward's 54 and the rows' values.  Eight
 // products for the gradients' five, and the tensor core busy for 37 %: an item is a few tiles,
 // and its first loads, its last products and its sums out are nobody's company, there being
 // neither TMEM nor shared memory for a second item.
