@@ -12,8 +12,9 @@
 // tokens are computed once into shared memory and serve all of a token's heads, laid out
 // so that a row's lanes read neighbours (they were 4 to 8 ways in conflict as they come).
 // 9,001 tokens, 32 and 8 heads of 128: 33.6 us, 5.5 TB/s.  30,011 tokens, 16 and 16 of 64:
-// 44 us forward (5.6 TB/s) and 88 its gradients (4.2).  One token each of 16 sequences, 8
-// heads and 1 of 256 into a cache: 2.65 us, a launch's latency.  (Rows through bulk copies
+// 45 us forward (5.4 TB/s) and 86 its gradients (4.3); 8 and 1 of 256, where a token's 128
+// angles weigh as much as its rows, 53 and 154.  One token each of 16 sequences, 8
+// heads and 1 of 256 into a cache: 2.5 us, a launch's latency.  (Rows through bulk copies
 // in shared memory were slower: 126 for 99 us forward at head dim 128, 356 for 212 back.)
 //
 // An angle is taken modulo whole turns before it is rounded: the frequency is a 64-bit
@@ -59,17 +60,24 @@ struct Args {
     unsigned char axis[MAX_HALF];
 };
 
-// cos and sin of frequency i for token t.
-__device__ __forceinline__ float2 angle(const Args& a, int t, int i) {
-    const unsigned long long f = a.turn[i];
-    float2 cs = make_float2(1.f, 0.f);
-    if (f) {
-        const long long p = a.pos[(size_t)a.axis[i] * a.n_tokens + t];
-        const int frac = (int)((unsigned long long)p * f >> 32);  // 2^-32 turns, wrapped
-        sincospif((float)frac * 4.656612873077393e-10f, &cs.y, &cs.x);  // 2^-31 half turns
+// One frequency, whose turn and positions a thread looks up once for all of its tokens: lanes ask
+// for different entries of the arguments, which are served one after another.  (Looked up for
+// every token: 30,000 tokens of 9 heads of 256 64 us, so 53.)
+struct Frequency {
+    unsigned long long turn;
+    const int* pos;
+    __device__ __forceinline__ Frequency(const Args& a, int i)
+        : turn(a.turn[i]), pos(a.pos + (size_t)a.axis[i] * a.n_tokens) {}
+    // cos and sin for token t
+    __device__ __forceinline__ float2 angle(int t) const {
+        float2 cs = make_float2(1.f, 0.f);
+        if (turn) {
+            const int frac = (int)((unsigned long long)(long long)pos[t] * turn >> 32);  // 2^-32 turns, wrapped
+            sincospif((float)frac * 4.656612873077393e-10f, &cs.y, &cs.x);  // 2^-31 half turns
+        }
+        return cs;
     }
-    return cs;
-}
+};
 
 // N bf16 elements (a multiple of 4) as loaded, and as floats.
 template <int N>
@@ -121,14 +129,16 @@ struct Cfg {
     static constexpr int RPP = THREADS / LPR;     // rows a pass
     // angles of TOK tokens from t0 on: [t][e][l] holds cos, cos, sin, sin of lane l's
     // elements 2 e and 2 e + 1
+    static_assert(THREADS % (HD / 2) == 0, "a thread has one frequency");
     static __device__ __forceinline__ void angles(const Args& a, int t0, int nt, float4* cs) {
-        float* at = reinterpret_cast<float*>(cs);
-        for (int i = threadIdx.x; i < nt * (HD / 2); i += THREADS) {
-            const int t = i / (HD / 2), f = i % (HD / 2);
-            const float2 v = angle(a, t0 + t, f);
-            float* to = at + ((t * (E / 2) + f % E / 2) * LPR + f / E) * 4 + (f & 1);
-            to[0] = v.x;
-            to[2] = v.y;
+        const int i = threadIdx.x % (HD / 2);
+        if ((int)threadIdx.x / (HD / 2) >= nt) return;
+        const Frequency f(a, i);
+        float* at = reinterpret_cast<float*>(cs) + (i % E / 2 * LPR + i / E) * 4 + (i & 1);
+        for (int t = threadIdx.x / (HD / 2); t < nt; t += THREADS / (HD / 2)) {
+            const float2 v = f.angle(t0 + t);
+            at[t * (E / 2) * LPR * 4] = v.x;
+            at[t * (E / 2) * LPR * 4 + 2] = v.y;
         }
     }
     static __device__ __forceinline__ void read(const float4* cs, int t, int e, int l, uint64_t& c,
@@ -141,7 +151,7 @@ struct Cfg {
 template <int HD>
 using Forward = Cfg<HD, 8, HD == 64 ? 16 : 8>;
 template <int HD>
-using Backward = Cfg<HD, 4, HD == 64 ? 16 : 8>;
+using Backward = Cfg<HD, 4, HD == 128 ? 8 : 16>;
 }  // namespace rope
 
 template <int HD, bool APPEND>
@@ -233,9 +243,11 @@ __global__ void __launch_bounds__(rope::THREADS)
     }
 }
 
-// Gradients.  A CTA takes query rows or key rows, blocks of TOK tokens in turn; their
-// gains' gradients stay in its lanes' registers and are added over its rows in a fixed
-// order at the end.
+// Gradients.  A CTA takes query rows or key rows of its share of the tokens, blocks of TOK in
+// turn; their gains' gradients stay in its lanes' registers and are added over its rows in a
+// fixed order at the end.  (Both kinds of rows in one CTA, so that no angle is needed twice, and
+// two passes' loads under way each spill: 236 and 203 us for 188 at 30,000 tokens of 32 and 8
+// heads of 128.)
 template <int HD>
 __global__ void __launch_bounds__(rope::THREADS, 4)
     k_qk_norm_rope_bwd(const __grid_constant__ rope::Args a) {
@@ -263,8 +275,9 @@ __global__ void __launch_bounds__(rope::THREADS, 4)
             gain[E / 2 + e] = gh.pair(e);
         }
     }
-    for (int t0 = part_cta * C::TOK; heads > 0 && t0 < a.n_tokens; t0 += ctas * C::TOK) {
-        const int nt = min(C::TOK, a.n_tokens - t0);
+    const int end = (int)((long long)a.n_tokens * (part_cta + 1) / ctas);
+    for (int t0 = (int)((long long)a.n_tokens * part_cta / ctas); heads > 0 && t0 < end; t0 += C::TOK) {
+        const int nt = min(C::TOK, end - t0);
         int t = lane_row / heads, head = lane_row % heads;
         rope::Pack<E> xl, xh, yl, yh;
         auto load = [&]() {
@@ -434,15 +447,15 @@ static jnx_status launch_rope(const rope::Args& a, int hd, const char* what, cud
 }
 
 // CTAs of the gradient kernel, at most what 152 SMs hold at once, shared out between query
-// and key rows by what a block of either takes: its passes, and its angles and waits, worth
-// five passes (by rows alone the key rows of 8 heads on one, 256 wide, were the last by far:
-// 30,000 tokens 275 us, so 158; 32 heads on 8 of 128 212 and 187 us); each kind has one at
-// least.
+// and key rows by what a token of either takes: its rows' passes, its angles, and a share of a
+// block's waits (by rows alone the key rows of 8 heads on one, 256 wide, were the last by far:
+// 30,000 tokens 275 us, so 154; 32 heads on 8 of 128 212 and 187 us); each kind has one at
+// least, and a CTA tokens enough for a pass or two.
 static int rope_bwd_grid(const jnx_qk_rope* p, int n_tokens, int& q_ctas) {
-    const int hd = p->head_dim, tok = hd == 64 ? 16 : 8, rows = rope::THREADS * 8 / hd;  // a pass
-    const int blocks = std::max(1, (n_tokens + tok - 1) / tok), most = 152 * 4;
-    auto passes = [&](int heads) { return (tok * heads + rows - 1) / rows + 5; };
-    const long long q = passes(p->n_heads), k = passes(p->n_kv_heads);
+    const int hd = p->head_dim, tok = hd == 128 ? 8 : 16, least = hd == 64 ? 16 : 8;
+    const int blocks = std::max(1, (int)(((long long)n_tokens + least - 1) / least)), most = 152 * 4;
+    auto cost = [&](int heads) { return heads * hd / 2048.0 + 1.25 * hd / 512.0 + 1.0 / tok; };
+    const double q = cost(p->n_heads), k = cost(p->n_kv_heads);
     q_ctas = std::min(blocks, std::max(1, (int)(most * q / (q + k))));
     return q_ctas + std::min(blocks, std::max(1, most - q_ctas));
 }
