@@ -18,7 +18,7 @@
 //
 // Bound by the tensor cores and the power cap: 8,191 rows of 4,096 on 32,000 columns with
 // gradients take 3,610 us, 1,784 TFLOP/s over all (floor 3,400): the products 1,209, 1,220
-// and 1,098, the rows 169.  333 rows of 2,048 without gradients: 57 us, of which the logits
+// and 1,098, the rows 169.  333 rows of 2,048 without gradients: 55 us, of which the logits
 // 49.5, two row blocks of 256 for 1.3 and four rounds of tiles for 3.3.
 #include <algorithm>
 
@@ -449,24 +449,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
     if (warp == 1) tmem_dealloc_pair(tmem_base, 2 * BN);
 }
 
+constexpr int kCountRows = 8192;
+
+struct VocabRows {
+    const int* targets;
+    int n, vocab, d;
+    int *count, *index, *packed, *place, *status;
+};
+
 // Which rows count, in order: index[j] and the targets of packed row j, place[i] of row i
-// (-1: ignored) and their number.  One CTA, 8 rows a thread at a time.
+// (-1: ignored) and their number.  One CTA, 8 rows a thread at a time.  For calls of more than
+// kCountRows rows; up to there k_vocab_gather's CTAs count what is ahead of their rows.
 __global__ void __launch_bounds__(1024)
-    k_vocab_pack(const int* targets, int n, int vocab_size, int* count, int* index, int* packed,
-                 int* place, int* status) {
+    k_vocab_pack(const __grid_constant__ VocabRows p) {
     __shared__ int sums[32];
     __shared__ int total;
     pdl_entry();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) total = 0;
-    for (int base = 0; base < n; base += 8192) {
+    for (int base = 0; base < p.n; base += 8192) {
         const int i0 = base + threadIdx.x * 8;
         int t[8], mine = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            t[e] = i0 + e < n ? targets[i0 + e] : -1;
-            if (t[e] >= vocab_size) {
-                report(status, JNX_ERR_DEVICE_BOUNDS);
+            t[e] = i0 + e < p.n ? p.targets[i0 + e] : -1;
+            if (t[e] >= p.vocab) {
+                report(p.status, JNX_ERR_DEVICE_BOUNDS);
                 t[e] = -1;
             }
             mine += t[e] >= 0;
@@ -486,36 +494,63 @@ __global__ void __launch_bounds__(1024)
         if (threadIdx.x == 1023) total = at + mine;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (i0 + e >= n) break;
+            if (i0 + e >= p.n) break;
             if (t[e] >= 0) {
-                index[at] = i0 + e;
-                packed[at] = t[e];
+                p.index[at] = i0 + e;
+                p.packed[at] = t[e];
             }
-            place[i0 + e] = t[e] >= 0 ? at++ : -1;
+            p.place[i0 + e] = t[e] >= 0 ? at++ : -1;
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) *count = total;
+    if (threadIdx.x == 0) *p.count = total;
 }
 
 // h's rows to their packed places and zero rows behind them; ignored rows get loss 0 and
-// gradient 0.  A CTA a row.
+// gradient 0.  A CTA a row.  COUNT: it counts the rows ahead itself, a launch less: 56 us for 58
+// of 333 rows of 2,048 on 32,000 words, and training on 8,192 rows of 1,024 on 8,000 188 for
+// 200; the reads grow with the square of the rows, hence the limit.
+template <bool COUNT>
 __global__ void __launch_bounds__(256)
-    k_vocab_gather(const uint16_t* h, long long ldh, int n, int d, const int* place,
-                   const int* count, uint16_t* packed_h, float* loss, uint16_t* dh,
-                   long long lddh) {
+    k_vocab_gather(const uint16_t* h, long long ldh, const __grid_constant__ VocabRows p,
+                   uint16_t* packed_h, float* loss, uint16_t* dh, long long lddh) {
+    __shared__ int sums[8];
     pdl_entry();
     const int i = blockIdx.x;
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    const int to = i < n ? place[i] : *count + (i - n);
-    const uint16_t* from = i < n ? h + i * ldh : nullptr;
-    uint16_t* dst = to >= 0 ? packed_h + (size_t)to * d : dh ? dh + i * lddh : nullptr;
+    int to;
+    if constexpr (COUNT) {
+        auto counts = [&](int t) { return t >= 0 && t < p.vocab; };
+        const int mine = i < p.n ? p.targets[i] : 0;
+        int ahead = 0;
+#pragma unroll 4
+        for (int j = threadIdx.x; j < min(i, p.n); j += 256) ahead += counts(p.targets[j]);
+        ahead = __reduce_add_sync(0xffffffffu, ahead);
+        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = ahead;
+        __syncthreads();
+        ahead = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) ahead += sums[w];
+        to = i >= p.n ? ahead + (i - p.n) : counts(mine) ? ahead : -1;
+        if (threadIdx.x == 0) {
+            if (i == p.n) *p.count = ahead;
+            if (i < p.n && to >= 0) {
+                p.index[to] = i;
+                p.packed[to] = mine;
+            }
+            if (mine >= p.vocab) report(p.status, JNX_ERR_DEVICE_BOUNDS);
+        }
+    } else {
+        to = i < p.n ? p.place[i] : *p.count + (i - p.n);
+    }
+    const uint16_t* from = i < p.n ? h + i * ldh : nullptr;
+    uint16_t* dst = to >= 0 ? packed_h + (size_t)to * p.d : dh ? dh + i * lddh : nullptr;
     if (to < 0) {
         from = nullptr;
         if (threadIdx.x == 0) loss[i] = 0.f;
     }
     if (dst)
-        for (int c = threadIdx.x * 8; c < d; c += 2048)
+        for (int c = threadIdx.x * 8; c < p.d; c += 2048)
             *reinterpret_cast<uint4*>(dst + c) = from ? *reinterpret_cast<const uint4*>(from + c) : zero;
 }
 
@@ -714,9 +749,13 @@ static jnx_status vocab_run(const uint16_t* h, int64_t ldh, const uint16_t* w, i
     if (!workspace || ws_bytes < ws.bytes)
         return fail(JNX_ERR_WORKSPACE, "%s: workspace too small", what);
     TraceScope ts(JNX_K_VOCAB, 0.0, s);
-    pdl(k_vocab_pack, 1, 1024, 0, s)(targets, n, vocab_size, ws.count, ws.index, ws.packed, ws.place,
-                                     status);
-    pdl(k_vocab_gather, n + PAD, 256, 0, s)(h, ldh, n, d, ws.place, ws.count, ws.h, loss, dh, lddh);
+    const VocabRows vr{targets, n, vocab_size, d, ws.count, ws.index, ws.packed, ws.place, status};
+    if (n <= kCountRows) {
+        pdl(k_vocab_gather<true>, n + PAD, 256, 0, s)(h, ldh, vr, ws.h, loss, dh, lddh);
+    } else {
+        pdl(k_vocab_pack, 1, 1024, 0, s)(vr);
+        pdl(k_vocab_gather<false>, n + PAD, 256, 0, s)(h, ldh, vr, ws.h, loss, dh, lddh);
+    }
     CUtensorMap tw, twmn;
     if (!make_tmap_bf16(&tw, w, vocab_size, d, ldw, 128, 64) ||
         (train && !make_tmap_bf16(&twmn, w, vocab_size, d, ldw, 64, 64)))

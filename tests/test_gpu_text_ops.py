@@ -639,6 +639,18 @@ def test_vocab_loss_train_in_pieces(piece):
     T.close(dw, want["dw"], want["dw_tol"], "dw")
 
 
+@pytest.mark.parametrize("n", [8191, 8192, 8193, 20001])
+def test_vocab_loss_train_of_many_rows(n):
+    """Calls on either side of the length up to which rows are placed by counting."""
+    h, w, t, rw = vocab_case(n, 260, 64, 13)
+    loss, dh, dw = vocab_train(h, w, t, rw)
+    want = T.vocab(h, w, t, rw)
+    T.close(loss, want["loss"], want["loss_tol"], "loss")
+    T.close(dh, want["dh"], want["dh_tol"], "dh")
+    T.close(dw, want["dw"], want["dw_tol"], "dw")
+    assert (dh[t < 0] == 0).all() and (loss[t < 0] == 0).all()
+
+
 @pytest.mark.parametrize("most,n", [(168, 100), (256, 161), (700, 300)])
 def test_vocab_loss_train_of_fewer_rows_than_it_was_made_for(most, n):
     """Fewer rows may take dh's sum over the vocabulary in more parts."""
