@@ -203,7 +203,8 @@ jnx_status jnx_diag_bounded_wait(int64_t limit_cycles, int32_t arrive, int32_t* 
  * packed prompts, attention of single tokens against a cache, and next-token
  * losses over the vocabulary.  `status` (device int, may be NULL) receives what a
  * kernel detects: JNX_ERR_DEVICE_BOUNDS, JNX_ERR_TIMEOUT; the caller clears it.
- * No call uploads from host memory, so each can be captured into a CUDA graph. */
+ * No call uploads from host memory, so each can be captured into a CUDA graph.
+ * Workspaces are 16-byte aligned and serve one call at a time. */
 
 /* Rows of attention heads, bf16: element c of head h of row t is
  * ptr[t * row_stride + h * head_stride + c].  ptr is 16-byte aligned and the
