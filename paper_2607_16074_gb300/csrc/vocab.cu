@@ -6,11 +6,14 @@
 // image rows without a next token, and an ignored row's h may hold anything, which must
 // not meet G^T.  Then, for each piece of packed rows:
 //   logits   a 256 x 256 tile on a CTA pair, d deep; the epilogue leaves of each row's
-//            128 columns the maximum m and sum s of e^(x - m), the target's logit, and,
-//            for gradients, e^(x - m) in bf16 (no logit is stored)
-//   rows     each row's m and s into its log-sum-exp and loss, and the row of
-//            probabilities scaled to G in place; the target's entry is
-//            row_weight expm1(-loss), exact where its probability is near one
+//            128 columns the maximum m and the sum s of e^(x - m) without the target's, the
+//            target's logit, and, for gradients, e^(x - m) in bf16 (no logit is stored)
+//   rows     each row's m and s into its loss, and the row of probabilities scaled to G in
+//            place.  With o the others' sum and e the target's term, both against the row's
+//            maximum, loss = log1p(o / e) and the target's entry is -row_weight o / (o + e):
+//            where the target's probability is near one, o keeps its digits, which a sum
+//            with e in it, or a log-sum-exp at the size of the logits, would round away
+//            (1e-6 of other mass at a logit of 20 or 100 gave a loss of 0)
 //   dh       G w, the vocabulary deep: w is the MN-major B operand as it lies
 //   dw       G^T h, the rows deep: both operands MN-major as they lie
 // which is three products of 2 rows vocab d operations for the minimum's three; forming
@@ -53,7 +56,7 @@ struct VocabGemm {
     // LOGITS
     const int* targets;  // of the packed rows
     uint16_t* G;         // null: losses only
-    float2* stats;       // [rows][blocks]
+    float2* stats;       // [rows][blocks]: maximum, and sum without the target's term
     float* at_target;
     // DH, DW
     const int* index;  // packed row -> row (null: the same)
@@ -341,6 +344,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                         uint32_t v[32];
                         tmem_ld32(tc + c * 64 + d * 32, v);
                         tmem_ld_wait_regs(v);
+                        if (tg >> 5 == 2 * c + d) {  // the target's term is not the others'
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if ((tg & 31) == e) v[e] = 0xff800000u;  // -inf
+                        }
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             const int at_col = c * 64 + d * 32 + e;
@@ -554,8 +562,8 @@ __global__ void __launch_bounds__(256)
             *reinterpret_cast<uint4*>(dst + c) = from ? *reinterpret_cast<const uint4*>(from + c) : zero;
 }
 
-// A row's log-sum-exp and loss from its blocks' (m, s), and its probabilities scaled to
-// G.  A CTA a row.
+// A row's loss from its blocks' (m, s) and its target's logit, and its probabilities scaled
+// to G.  A CTA a row.
 __global__ void __launch_bounds__(256)
     k_vocab_rows(const float2* stats, const float* at_target, const __grid_constant__ VocabGemm p,
                  const float* weight, float* loss) {
@@ -579,27 +587,24 @@ __global__ void __launch_bounds__(256)
     __syncthreads();
     s = 0.f;
     for (int w = 0; w < 8; ++w) s += red[8 + w];
-    const float lse = m + logf(s);
-    const int t = p.targets[p.r0 + r], row = p.index ? p.index[p.r0 + r] : r;
-    const float ls = t >= 0 && t < p.vocab ? lse - at_target[r] : 0.f;
-    if (threadIdx.x == 0) {
-        loss[row] = ls;
-        if (t >= p.vocab) report(p.status, JNX_ERR_DEVICE_BOUNDS);
-    }
+    const int t = p.targets[p.r0 + r], row = p.index[p.r0 + r];  // (a packed row's target counts)
+    const float below = m - at_target[r], e = expf(-below), z = s + e;
+    // s / e may be large or overflow where the target is far below the maximum
+    if (threadIdx.x == 0) loss[row] = s <= e ? log1pf(s / e) : below + logf(z);
     if (!p.G) return;
-    const float w = weight[row];
+    const float w = weight[row], scale = w / z, at_t = -w * (s / z);
     uint16_t* g = p.G + (size_t)r * ((p.vocab + 63) / 64 * 64);
     for (int c = threadIdx.x * 8; c < p.vocab; c += 2048) {
-        const float f = w * expf(st[c / vocab::BLK].x - lse);
+        const float f = scale * expf(st[c / vocab::BLK].x - m);
         const uint4 u = *reinterpret_cast<const uint4*>(g + c);
         uint32_t v[4] = {u.x, u.y, u.z, u.w};
         const bool hit = (t & ~7) == c;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float a = f * __uint_as_float(v[e] << 16), b = f * __uint_as_float(v[e] & 0xffff0000u);
-            if (hit && (t & 7) == 2 * e) a = w * expm1f(-ls);
-            if (hit && (t & 7) == 2 * e + 1) b = w * expm1f(-ls);
-            v[e] = cvt_bf2(a, b);
+        for (int i = 0; i < 4; ++i) {
+            float a = f * __uint_as_float(v[i] << 16), b = f * __uint_as_float(v[i] & 0xffff0000u);
+            if (hit && (t & 7) == 2 * i) a = at_t;
+            if (hit && (t & 7) == 2 * i + 1) b = at_t;
+            v[i] = cvt_bf2(a, b);
         }
         *reinterpret_cast<uint4*>(g + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }

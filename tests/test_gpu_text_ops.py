@@ -691,6 +691,38 @@ def test_vocab_loss_of_far_apart_logits():
     T.close(dw, want["dw"], want["dw_tol"] * grow + 1e-6, "dw")
 
 
+@pytest.mark.parametrize("top", [0.0, 20.0, 60.0, 100.0])
+@pytest.mark.parametrize("other", [1e-8, 1e-6, 1e-4, 0.3, 30.0])
+def test_vocab_loss_of_sure_rows_keeps_its_digits(top, other):
+    """A target at or near the maximum and little mass beside it: loss and gradients are
+    right to their own size, not to the logits'."""
+    n, vocab, d = 24, 1000, 64
+    g = gen(14)
+    h = torch.zeros(n, d, device="cuda", dtype=BF)
+    h[torch.arange(n), torch.arange(n)] = 1  # row i's logits are the vocabulary's column i, exactly
+    w = torch.zeros(vocab, d, device="cuda", dtype=BF)
+    w[:, :n] = (top + math.log(other / vocab) + 0.3 * torch.randn(vocab, n, generator=g, device="cuda")).to(BF)
+    t = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    w[t.long(), torch.arange(n)] = top
+    loss, dh, dw = vocab_train(h, w, t, torch.ones(n, device="cuda"))
+    x = w[:, :n].T.to(T.F64)
+    mass = torch.exp(x - top)
+    mass[torch.arange(n), t.long()] = 0
+    want = torch.log1p(mass.sum(-1))
+    # the maximum times log2(e), 2^-17 of a unit at 100, a block's 128 terms added in turn,
+    # 2^-17 of their sum, and the exponentials: under 2^-15 in all
+    T.close(loss, want, 2.0 ** -14 * want, "loss")
+    r = T.vocab(h, w, t, torch.ones(n, device="cuda"))
+    T.close(dh, r["dh"], r["dh_tol"], "dh")
+    T.close(dw, r["dw"], r["dw_tol"], "dw")
+    only, rows = torch.empty_like(loss), torch.arange(n)
+    _r().VocabLoss(w, max_rows=n, gradients=False).loss(h, t, only)
+    assert torch.equal(only, loss)
+    # the target's own entry, which the vocabulary's gradient shows by itself: two roundings
+    share = mass.sum(-1) / (1 + mass.sum(-1))
+    T.close(-dw[t.long(), rows], share, 2 * T.U * share, "target")
+
+
 def test_vocab_loss_ignored_rows_hold_anything():
     h, w, t, rw = vocab_case(200, 500, 128, 6)
     clean = vocab_train(h, w, t, rw)
