@@ -48,10 +48,10 @@ __host__ __device__ inline int item_tiles(int head_dim) { return head_dim == 256
 
 constexpr int kMaxGroup = 64;
 
-// Rows that see up to so many keys have what rounding left of their output kept for the
-// gradients.  D = rowsum(dO * O) is a sum that dP nearly cancels against where few keys make a
-// row; beyond, the rounding of O is one of several alike: dQ off by 0.0027 of its norm for
-// 0.0025, where rows of two keys are off by 0.0055 for 0.0035.
+// Rows that see up to so many keys have what rounding left of their output written for the
+// gradients, where the caller gives it a place.  D = rowsum(dO * O) is a sum that dP nearly
+// cancels against where few keys make a row: sequences of 12 to 64 keys have dQ off by 0.0024
+// of its norm with it and 0.0026 without, of 400 keys 0.0025 either way.
 constexpr int kRestKeys = 64;
 
 // Parts that the gradients' keys pass takes a 128-key tile's rows in: one where a sequence

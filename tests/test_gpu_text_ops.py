@@ -328,6 +328,58 @@ def test_prompt_attention_backward_keeps_its_precision_on_short_sequences(heads,
         assert float((got.to(T.F64) - want[n]).norm() / want[n].norm()) < 0.003
 
 
+@pytest.mark.parametrize("with_rest", [False, True])
+@pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128), (8, 1, 256)])
+def test_prompt_attention_backward_belongs_to_its_own_forward(heads, with_rest):
+    """Several forwards of one plan, then their backwards in another order: each has the bits
+    that it has by itself, on an object of its own."""
+    R, lens = _r(), ([40] * 9 + [200], [40] * 9 + [200], [0] * 10)
+    plan = R.PromptPlan(*lens)
+    shared = R.PromptAttention(*heads, plan, gradients=True)
+
+    def forward(op, x):
+        out, lse = empty(*x[0].shape), empty(x[0].shape[0], heads[0], dtype=torch.float32)
+        rest = empty(*x[0].shape) if with_rest else None
+        op.forward(*x[:3], out, lse, rest=rest)
+        return out, lse, rest
+
+    def backward(op, x, out, lse, rest):
+        d = [empty(*y.shape) for y in x[:3]]
+        op.backward(*x[:3], out, lse, x[3], *d, rest=rest)
+        op.check()
+        return d
+
+    inputs = [attn_inputs(heads, lens, seed) for seed in (21, 22, 23)]
+    alone = []
+    for x in inputs:
+        op = R.PromptAttention(*heads, plan, gradients=True)
+        alone.append(backward(op, x, *forward(op, x)))
+    # the last one's forward by an object without gradients, as a frozen copy would run it
+    kept = [forward(shared, x) for x in inputs[:2]]
+    kept.append(forward(R.PromptAttention(*heads, plan), inputs[2]))
+    for i in (0, 2, 1):
+        for a, b in zip(alone[i], backward(shared, inputs[i], *kept[i])):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128), (8, 1, 256)])
+def test_prompt_attention_backward_with_rest_is_closer(heads):
+    """In rows of 9 to 64 keys, what rounding left of the output brings dq and dk nearer."""
+    lens = ([40] * 40, [40] * 40, [0] * 40)
+    x = attn_inputs(heads, lens, 24)
+    want, off = T.attention(*x[:3], lens, x[3]), {}
+    op = _r().PromptAttention(*heads, _r().PromptPlan(*lens), gradients=True)
+    for rest in (None, empty(*x[0].shape)):
+        out, lse = empty(*x[0].shape), empty(x[0].shape[0], heads[0], dtype=torch.float32)
+        d = [empty(*y.shape) for y in x[:3]]
+        op.forward(*x[:3], out, lse, rest=rest)
+        op.backward(*x[:3], out, lse, x[3], *d, rest=rest)
+        off[rest is not None] = [float((y.to(T.F64) - want[n]).norm() / want[n].norm())
+                                 for y, n in zip(d, ("dq", "dk"))]
+    op.check()
+    assert all(a < b < 0.003 for a, b in zip(off[True], off[False]))
+
+
 def test_prompt_attention_sharp_scores():
     """Scores of hundreds: a running maximum that rises in every tile, rows that put all
     their weight on one key."""
