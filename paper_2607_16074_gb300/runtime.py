@@ -627,10 +627,13 @@ class _TextOperator:
         return torch._C._cuda_getCurrentRawStream(self._device)
 
     def check(self) -> None:
-        """Raise what a kernel reported since the last check (waits for the device)."""
+        """Raise what kernels reported since the last check, of calls on any stream (waits for
+        the device: torch's streams do not order with one another)."""
+        torch.cuda.synchronize(self._device)
         code = int(self.status.item())
-        self.status.zero_()
         if code != J.JNX_OK:
+            self.status.zero_()
+            torch.cuda.synchronize(self._device)  # a later call's report is not wiped
             raise J.JnxError(code, "reported by a kernel")
 
 

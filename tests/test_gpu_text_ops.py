@@ -143,6 +143,27 @@ def test_norm_rope_append_reports_rows_outside():
     T.close(q, want[0], T.norm_rope_bound(want[0]))  # queries are written all the same
 
 
+def test_check_sees_a_call_on_another_stream():
+    """A report of a kernel that still waits for its turn on a stream of its own."""
+    from paper_2607_16074_gb300 import jnx as J
+    op, qkv, pos, _, _ = rope_case((4, 4, 64), 2, (32,))
+    kc = torch.zeros(3, 5, 4, 64, device="cuda", dtype=BF)
+    vc, q = torch.zeros_like(kc), empty(2, 4, 64)
+    i32 = lambda *v: torch.tensor(v, device="cuda", dtype=torch.int32)  # noqa: E731
+    good, bad, at, s = i32(0, 1), i32(0, 3), i32(4, 0), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for slots in (bad, good, bad):
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(50_000_000)  # some 25 ms
+        op.append(qkv, pos, q, kc, vc, slots, at, stream=s)
+        if slots is good:
+            op.check()
+            continue
+        with pytest.raises(J.JnxError) as e:
+            op.check()
+        assert e.value.code == J.JNX_ERR_DEVICE_BOUNDS
+
+
 def rope_gradients(qkv, heads, gains, pos, sections, dq, dk, theta=10000.0):
     """Definition's gradients by the chain rule, with bounds."""
     h, hkv, hd = heads
