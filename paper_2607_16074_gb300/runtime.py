@@ -620,11 +620,31 @@ class _TextOperator:
         self._status, self._ws, self._nws = (self.status.data_ptr(), self.ws.data_ptr(),
                                              self.ws.numel())
         self._lib, self._device = J.lib(), self.ws.device.index
+        self._held = [self.status, self.ws]  # the object's device memory
+        home = torch.cuda.current_stream(self._device)
+        self._known, self._made = {home.cuda_stream}, None
+        if not torch.cuda.is_current_stream_capturing():
+            self._made = torch.cuda.Event()
+            self._made.record(home)
 
     def _on(self, stream: Optional[torch.cuda.Stream]) -> int:
-        if stream is not None:
-            return stream.cuda_stream
-        return torch._C._cuda_getCurrentRawStream(self._device)
+        handle = (stream.cuda_stream if stream is not None
+                  else torch._C._cuda_getCurrentRawStream(self._device))
+        if handle not in self._known:
+            self._first_use(stream or torch.cuda.current_stream(self._device))
+        return handle
+
+    def _first_use(self, stream: torch.cuda.Stream) -> None:
+        """A stream other than the one that the object was made on: its memory is ready there,
+        and is not handed out again, once the object is gone, before the stream is through."""
+        for t in self._held:
+            t.record_stream(stream)
+        with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():
+                return  # (a capture cannot wait for what lies outside it)
+        if self._made is not None:
+            stream.wait_event(self._made)
+        self._known.add(stream.cuda_stream)
 
     def check(self) -> None:
         """Raise what kernels reported since the last check, of calls on any stream (waits for
@@ -749,6 +769,7 @@ class PromptAttention(_TextOperator):
         self._ref = C.byref(self.struct)
         super().__init__(J.lib().jnx_op_prompt_attention_backward_workspace_bytes(
             self._ref, *self.dims) if gradients else 0, plan.device)
+        self._held += [self.items, *plan.d]
         self.gradients = gradients
         rows = J.jnx_head_rows
         self._qs, self._ks = (plan.n_q, n_heads, head_dim), (plan.n_kv, n_kv_heads, head_dim)

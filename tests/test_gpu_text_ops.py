@@ -655,6 +655,37 @@ def test_decode_matches_the_prompt():
     T.close(out[-1:], want["out"], want["out_tol"])
 
 
+def test_objects_dropped_behind_a_call_on_another_stream():
+    """A call that still waits for its turn keeps its object's workspace and work list, though
+    the object is gone and others ask for memory."""
+    R, heads, lens = _r(), (8, 2, 128), ([300, 70] * 4, [300, 70] * 4, [20, 0] * 4)
+    h, hkv, hd = heads
+    q, k, v, dout = attn_inputs(heads, lens, 25)
+    want = attn_gradients(heads, lens, q, k, v, dout)
+    n = [900, 30, 0, 2222, 513]
+    q1, kc, vc, slot, want1 = decode(heads, n, 2300)
+    n = torch.tensor(n, device="cuda", dtype=torch.int32)
+    s, junk = torch.cuda.Stream(), []
+    got, got1 = [torch.empty_like(x) for x in want], torch.empty_like(want1)
+    s.wait_stream(torch.cuda.current_stream())
+
+    def call():
+        prompts = R.PromptAttention(*heads, R.PromptPlan(*lens), gradients=True)
+        one = R.DecodeAttention(*heads, max_batch=5)
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(50_000_000)  # some 25 ms
+        prompts.forward(q, k, v, got[0], got[1], stream=s)
+        prompts.backward(q, k, v, got[0], got[1], dout, *got[2:], stream=s)
+        one.forward(q1, kc, vc, slot, n, got1, stream=s)
+        return [x.numel() * x.element_size() for op in (prompts, one) for x in op._held]
+
+    for size in call() * 3:
+        junk.append(torch.full((size,), 255, device="cuda", dtype=torch.uint8))
+    torch.cuda.synchronize()
+    for a, b in zip([*want, want1], [*got, got1]):
+        assert torch.equal(a, b)
+
+
 # ---------------------------------------------------------------- vocabulary loss
 
 def vocab_case(n, vocab, d, seed=0, std=0.05, ignored=0.2):

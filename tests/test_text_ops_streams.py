@@ -1,5 +1,7 @@
 """The text operators' objects and streams: what they do on the host around a call, with the
 device's part played by stand-ins (no GPU needed)."""
+import contextlib
+
 import pytest
 import torch
 
@@ -55,3 +57,49 @@ def test_check_wipes_no_later_report(operator):
     with pytest.raises(J.JnxError) as e:
         operator.check()
     assert e.value.code == J.JNX_ERR_DEVICE_BOUNDS
+
+
+class Memory:
+    def __init__(self):
+        self.streams = []
+
+    def record_stream(self, stream):
+        self.streams.append(stream.cuda_stream)
+
+
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream, self.waited = handle, []
+
+    def wait_event(self, event):
+        self.waited.append(event)
+
+
+@pytest.fixture
+def made_on_11(monkeypatch):
+    op = R._TextOperator.__new__(R._TextOperator)
+    op._device, op._held, op._known, op._made = 0, [Memory(), Memory()], {11}, "made"
+    op.capturing = False
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: op.capturing)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 11, raising=False)
+    return op
+
+
+def test_memory_is_known_to_every_stream_that_uses_it(made_on_11):
+    op, other = made_on_11, Stream(22)
+    assert op._on(None) == 11 and op._on(Stream(11)) == 11
+    assert not any(m.streams for m in op._held)  # the allocator knows of its own stream
+    for _ in range(3):
+        assert op._on(other) == 22
+    assert all(m.streams == [22] for m in op._held) and other.waited == ["made"]
+
+
+def test_a_capturing_stream_does_not_wait_for_what_lies_outside(made_on_11):
+    op, other = made_on_11, Stream(22)
+    op.capturing = True
+    assert op._on(other) == 22
+    assert all(m.streams == [22] for m in op._held) and not other.waited
+    op.capturing = False
+    op._on(other)
+    assert other.waited == ["made"]
