@@ -684,10 +684,12 @@ jnx_status prompt_ok(const jnx_prompt* p, const char* what, int& rows, int& keys
     return JNX_OK;
 }
 
-// ... and its device arrays, for a launch.
-jnx_status prompt_launchable(const jnx_prompt* p, const char* what, int& rows, int& keys) {
+// ... and its device arrays, for a launch over its rows (gradients: over its keys too).
+jnx_status prompt_launchable(const jnx_prompt* p, const char* what, bool gradients, int& rows,
+                             int& keys) {
     if (jnx_status st = prompt_ok(p, what, rows, keys)) return st;
-    if (rows > 0 && (!p->cu_q || !p->cu_kv || !p->items || (p->h_prefix && !p->prefix)))
+    if ((rows > 0 || (gradients && keys > 0)) &&
+        (!p->cu_q || !p->cu_kv || !p->items || (p->h_prefix && !p->prefix)))
         return fail(JNX_ERR_INVALID_ARG, "%s: null device arrays", what);
     if (p->n_forward < 0 || p->n_keys < 0 || p->n_queries < 0 || p->n_parts < 0 ||
         p->n_parts > kMaxParts)
@@ -760,7 +762,7 @@ extern "C" jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_hea
     clear_error();
     int rows, keys;
     if (jnx_status st = heads_ok(n_heads, n_kv_heads, head_dim, "prompt attention")) return st;
-    if (jnx_status st = prompt_launchable(p, "prompt attention", rows, keys)) return st;
+    if (jnx_status st = prompt_launchable(p, "prompt attention", false, rows, keys)) return st;
     if (rows == 0) return JNX_OK;
     if (!rows_ok(q) || !rows_ok(out) || (rest && !rows_ok(rest)) || (keys > 0 && (!rows_ok(k) || !rows_ok(v))))
         return fail(JNX_ERR_INVALID_ARG, "prompt attention: null or misaligned rows");

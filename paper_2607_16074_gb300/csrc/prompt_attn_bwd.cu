@@ -46,7 +46,8 @@
 namespace jnx {
 
 jnx_status prompt_ok(const jnx_prompt* p, const char* what, int& rows, int& keys);
-jnx_status prompt_launchable(const jnx_prompt* p, const char* what, int& rows, int& keys);
+jnx_status prompt_launchable(const jnx_prompt* p, const char* what, bool gradients, int& rows,
+                             int& keys);
 
 namespace pbwd {
 constexpr int BM = 128;
@@ -1644,7 +1645,7 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     const char* what = "prompt attention backward";
     int rows, keys;
     if (jnx_status st = heads_ok(n_heads, n_kv_heads, head_dim, what)) return st;
-    if (jnx_status st = prompt_launchable(p, what, rows, keys)) return st;
+    if (jnx_status st = prompt_launchable(p, what, true, rows, keys)) return st;
     if (rows == 0 && keys == 0) return JNX_OK;
     if ((rows > 0 && (!rows_ok(q) || !rows_ok(out) || !rows_ok(dout) || !rows_ok(dq) || !lse ||
                       (rest && !rows_ok(rest)))) ||

@@ -111,6 +111,17 @@ def test_prompt_attention_backward_refuses():
     assert f(p=prompt(q=(0,), kv=(0,))) == J.JNX_OK
 
 
+@pytest.mark.parametrize("missing", ["cu_q", "cu_kv", "items", "prefix"])
+def test_prompt_attention_backward_refuses_keys_without_device_arrays(missing):
+    """Keys that no row reads still have gradients to write, by the device's arrays."""
+    p = prompt(q=(0, 0), kv=(5, 3), prefix=(1, 0))
+    J.lib().jnx_prompt_items(C.byref(p), 8, 2, 128, None, 0)
+    setattr(p, missing, None)
+    refused(J.lib().jnx_op_prompt_attention_backward(
+        C.byref(p), 8, 2, 128, rows(), rows(), rows(), rows(), None, PTR, rows(), rows(), rows(),
+        rows(), PTR, 1 << 16, None, None), INV)
+
+
 def test_decode_refuses():
     L = J.lib()
     cache = J.jnx_kv_cache(PTR, PTR, 2, 4, 1024, 256, 128)
