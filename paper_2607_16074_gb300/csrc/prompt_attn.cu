@@ -691,6 +691,9 @@ jnx_status prompt_launchable(const jnx_prompt* p, const char* what, bool gradien
     if ((rows > 0 || (gradients && keys > 0)) &&
         (!p->cu_q || !p->cu_kv || !p->items || (p->h_prefix && !p->prefix)))
         return fail(JNX_ERR_INVALID_ARG, "%s: null device arrays", what);
+    // the parts of a key tile's rows, and with them the workspace, follow from the prefix
+    if (gradients && p->prefix && !p->h_prefix)
+        return fail(JNX_ERR_INVALID_ARG, "%s: prefix on the device alone", what);
     if (p->n_forward < 0 || p->n_keys < 0 || p->n_queries < 0 || p->n_parts < 0 ||
         p->n_parts > kMaxParts)
         return fail(JNX_ERR_INVALID_ARG, "%s: bad work list", what);

@@ -122,6 +122,16 @@ def test_prompt_attention_backward_refuses_keys_without_device_arrays(missing):
         rows(), PTR, 1 << 16, None, None), INV)
 
 
+def test_prompt_attention_backward_refuses_a_prefix_that_the_host_does_not_know():
+    """The workspace is sized by the host's arrays, and used by the device's."""
+    p = prompt(q=(5, 3), kv=(900, 700), prefix=(800, 0))
+    p.h_prefix = None
+    J.lib().jnx_prompt_items(C.byref(p), 8, 2, 128, None, 0)
+    refused(J.lib().jnx_op_prompt_attention_backward(
+        C.byref(p), 8, 2, 128, rows(), rows(), rows(), rows(), None, PTR, rows(), rows(), rows(),
+        rows(), PTR, 1 << 30, None, None), INV)
+
+
 def test_decode_refuses():
     L = J.lib()
     cache = J.jnx_kv_cache(PTR, PTR, 2, 4, 1024, 256, 128)
