@@ -269,7 +269,10 @@ jnx_status jnx_op_qk_norm_rope_backward(const jnx_qk_rope* p, const uint16_t* qk
  * Lq sees keys j < min(Lk, max(Lk - Lq + i + 1, prefix[s])).  A row that sees none
  * has output 0, log-sum-exp -inf and gradient 0.  The arrays are on the device, the
  * h_ ones the same on the host; prefix may be NULL (0).  items: the work list of
- * jnx_prompt_items for the same heads, on the device. */
+ * jnx_prompt_items for the same heads, on the device.  A list of other lengths or heads is
+ * refused by its counts (JNX_ERR_INVALID_ARG); an entry that names no row or key of the
+ * prompt, or a sequence beyond the rows and keys of the host's arrays, is left out and
+ * reported. */
 typedef struct {
     int32_t n_seqs;
     const int32_t *cu_q, *cu_kv, *prefix;

@@ -66,6 +66,26 @@ __host__ __device__ inline int key_parts(int at, int Lq, int Lk, int prefix, int
     return n < 1 ? 1 : n < kMaxParts ? (int)n : kMaxParts;
 }
 
+// What a prompt's work list holds for a head layout: items of each pass, parts of a key tile
+// at most.
+struct PromptCounts {
+    long long forward = 0, keys = 0, queries = 0;
+    int parts = 1;
+};
+
+// A sequence's place among the packed rows and keys, as the device's arrays have it.
+struct PromptSeq {
+    int q0, Lq, k0, Lk, pre;
+};
+// False: no such sequence, or one beyond the rows and keys that the call was launched for.
+__device__ __forceinline__ bool prompt_seq(const int* cu_q, const int* cu_kv, const int* prefix, int n_seqs,
+                                           int rows, int keys, int s, PromptSeq& x) {
+    if (s < 0 || s >= n_seqs) return false;
+    const int q0 = cu_q[s], q1 = cu_q[s + 1], k0 = cu_kv[s], k1 = cu_kv[s + 1];
+    x = PromptSeq{q0, q1 - q0, k0, k1 - k0, prefix ? prefix[s] : 0};
+    return 0 <= q0 && q0 <= q1 && q1 <= rows && 0 <= k0 && k0 <= k1 && k1 <= keys;
+}
+
 jnx_status heads_ok(int n_heads, int n_kv_heads, int head_dim, const char* what);
 
 }  // namespace jnx

@@ -20,7 +20,7 @@
 //   warp 1       MMA issuer.  Two tiles: S of a tile overwrites its P once PV is issued
 //                and the other tile's products run while this one's softmax does.  One
 //                tile (head dim 256): two score buffers, S two key tiles ahead of PV.
-//   warp 3       hands out the items, looked up ahead
+//   warp 3       hands out the items, looked up ahead and checked
 //   warps 4-     softmax and epilogue, a warpgroup a tile, a thread a row: the row's 128
 //                scores are in registers, so no row quantity is exchanged
 // P (bf16) overwrites the first 64 columns of its scores and is the TMEM A operand of
@@ -79,6 +79,7 @@ struct PromptCfg {
 struct PromptArgs {
     const int *cu_q, *cu_kv, *prefix;
     const int2* items;
+    int n_seqs, rows, keys;  // what the items may name
     int n_work, H, Hkv, group;
     float scale_log2;
     uint16_t* out;
@@ -433,7 +434,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             const int G = gridDim.x, b = blockIdx.x;
             return r * G + ((r & 1) ? G - 1 - b : b);
         };
-        auto entry = [&](int w) { return w < a.n_work ? a.items[w / a.Hkv] : make_int2(-1, 0); };
+        auto entry = [&](int w) { return w < a.n_work ? a.items[w / a.Hkv] : make_int2(0, 0); };
         const int rounds = (a.n_work + gridDim.x - 1) / gridDim.x;
         int2 e = entry(work(0));
         int told = 0;
@@ -459,10 +460,14 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             const int2 c = e;
             const int w = work(r);
             e = entry(work(r + 1));
-            if (c.x < 0) continue;
-            const int q0 = a.cu_q[c.x], k0 = a.cu_kv[c.x];
-            ok = tell(PromptWork{q0, c.y, a.cu_q[c.x + 1] - q0, k0, a.cu_kv[c.x + 1] - k0,
-                                 a.prefix ? a.prefix[c.x] : 0, w % a.Hkv});
+            if (w >= a.n_work) continue;
+            PromptSeq x;
+            if (!prompt_seq(a.cu_q, a.cu_kv, a.prefix, a.n_seqs, a.rows, a.keys, c.x, x) ||
+                (unsigned)c.y >= (unsigned)x.Lq) {
+                if (lane == 0) report(a.status, JNX_ERR_DEVICE_BOUNDS);
+                continue;
+            }
+            ok = tell(PromptWork{x.q0, c.y, x.Lq, x.k0, x.Lk, x.pre, w % a.Hkv});
         }
         if (!ok || !tell(PromptWork{0, -1, 0, 0, 0, 0, 0})) *fail_flag = 1;
     } else if (warp >= 4) {
@@ -700,6 +705,24 @@ jnx_status prompt_launchable(const jnx_prompt* p, const char* what, bool gradien
     return JNX_OK;
 }
 
+PromptCounts prompt_counts(const jnx_prompt* p, int H, int Hkv, int hd, bool gradients) {
+    const int group = H / Hkv, T = tile_tokens(group), step = T * item_tiles(hd);
+    PromptCounts n;
+    for (int s = 0; s < p->n_seqs; ++s) {
+        const int Lq = p->h_cu_q[s + 1] - p->h_cu_q[s], Lk = p->h_cu_kv[s + 1] - p->h_cu_kv[s];
+        const int pre = p->h_prefix ? p->h_prefix[s] : 0;
+        n.forward += ((long long)Lq + step - 1) / step;
+        if (!gradients) continue;
+        n.queries += ((long long)Lq + T - 1) / T;
+        for (long long at = 0; at < Lk; at += 128) {
+            const int np = key_parts((int)at, Lq, Lk, pre, group, Hkv);
+            n.keys += np;
+            n.parts = std::max(n.parts, np);
+        }
+    }
+    return n;
+}
+
 }  // namespace jnx
 
 using namespace jnx;
@@ -772,15 +795,16 @@ extern "C" jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_hea
     const long long n_work = (long long)p->n_forward * n_kv_heads;
     if (n_work > 0x7FFFFFFFLL - 2 * num_sms())
         return fail(JNX_ERR_UNSUPPORTED, "prompt attention: too many work items");
-    if (n_work == 0) return JNX_OK;
+    if (p->n_forward != prompt_counts(p, n_heads, n_kv_heads, head_dim, false).forward)
+        return fail(JNX_ERR_INVALID_ARG, "prompt attention: a work list of other heads or lengths");
     // without any key no tile is loaded, but the maps want an address
     const jnx_head_rows kk = keys ? *k : *q, vv = keys ? *v : *q;
-    if (!keys) keys = 1;
-    PromptArgs a{p->cu_q, p->cu_kv, p->prefix, reinterpret_cast<const int2*>(p->items), (int)n_work,
-                 n_heads, n_kv_heads, n_heads / n_kv_heads,
+    PromptArgs a{p->cu_q, p->cu_kv, p->prefix, reinterpret_cast<const int2*>(p->items), p->n_seqs, rows,
+                 keys, (int)n_work, n_heads, n_kv_heads, n_heads / n_kv_heads,
                  (float)(1.4426950408889634 / sqrt((double)head_dim)), out->ptr, out->row_stride,
                  out->head_stride, rest ? rest->ptr : nullptr, rest ? rest->row_stride : 0,
                  rest ? rest->head_stride : 0, lse, status};
+    if (!keys) keys = 1;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN, 0.0, s);
     auto go = [&](auto with_rest) {

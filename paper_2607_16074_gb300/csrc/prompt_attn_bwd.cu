@@ -48,6 +48,7 @@ namespace jnx {
 jnx_status prompt_ok(const jnx_prompt* p, const char* what, int& rows, int& keys);
 jnx_status prompt_launchable(const jnx_prompt* p, const char* what, bool gradients, int& rows,
                              int& keys);
+PromptCounts prompt_counts(const jnx_prompt* p, int H, int Hkv, int hd, bool gradients);
 
 namespace pbwd {
 constexpr int BM = 128;
@@ -83,7 +84,7 @@ struct PromptBwdArgs {
     int* claimed;       // items taken beyond the grid's first: 0 at launch
     float scale_log2, scale;
     const float2* row;  // [Hkv][rows][group]: lse (+inf where a row sees no key), D
-    int rows;
+    int n_seqs, rows, keys;  // what the items may name
     jnx_head_rows dq, dk, dv;
     float* part;  // [dk, dv][n_parts][keys][Hkv][hd]: the sums of tiles taken in parts
     long long part_stride;  // of a part
@@ -109,6 +110,22 @@ struct PromptBwdItem {
         n = j1 - j0;
     }
 };
+
+// A claimed item's list entry: false, and reported, where it names no row, or no key and part,
+// of the prompt.
+template <bool KP>
+__device__ __forceinline__ bool bwd_item(const PromptBwdArgs& p, int2 e, int kvh, PromptBwdItem& x) {
+    PromptSeq s;
+    bool ok = prompt_seq(p.cu_q, p.cu_kv, p.prefix, p.n_seqs, p.rows, p.keys, e.x, s);
+    x = PromptBwdItem{KP ? e.y & ~127 : e.y, kvh, s.q0, s.Lq, s.k0, s.Lk, s.pre, KP ? e.y & 127 : 0};
+    ok = ok && (unsigned)x.at < (unsigned)(KP ? x.Lk : x.Lq);
+    if (ok && KP) {
+        const int np = x.parts(p.group, p.Hkv);
+        ok = np <= p.n_parts && x.part < np;
+    }
+    if (!ok && (threadIdx.x & 31) == 0) report(p.status, JNX_ERR_DEVICE_BOUNDS);
+    return ok;
+}
 
 __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
     const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
@@ -187,8 +204,12 @@ __global__ void __launch_bounds__(256)
     constexpr int LANES = HD / 8, PER = 256 / LANES;
     pdl_entry();
     const int sq = blockIdx.x / p.Hkv, kvh = blockIdx.x % p.Hkv;
-    const int q0 = p.cu_q[sq], Lq = p.cu_q[sq + 1] - q0, k0 = p.cu_kv[sq];
-    const int Lk = p.cu_kv[sq + 1] - k0, pre = p.prefix ? p.prefix[sq] : 0;
+    PromptSeq s;
+    if (!prompt_seq(p.cu_q, p.cu_kv, p.prefix, p.n_seqs, p.rows, p.keys, sq, s)) {
+        if (threadIdx.x == 0) report(p.status, JNX_ERR_DEVICE_BOUNDS);
+        return;
+    }
+    const int q0 = s.q0, Lq = s.Lq, k0 = s.k0, Lk = s.Lk, pre = s.pre;
     const int most = rest.ptr ? kRestKeys : kFewKeys;
     // rows [a, b): the first that sees a key, the first that sees too many
     const int a = first_row(0, Lq, Lk, pre), b = Lk > most ? first_row(most, Lq, Lk, pre) : Lq;
@@ -276,11 +297,13 @@ __device__ __forceinline__ void bwd_rows_part(uint8_t* stg, int lane, const uint
 __global__ void __launch_bounds__(256) k_prompt_bwd_join(const __grid_constant__ PromptBwdArgs p, int hd) {
     pdl_entry();
     const int2 e = p.items[blockIdx.x / p.Hkv];
-    if (e.y & 127) return;
-    const int kvh = blockIdx.x % p.Hkv, k0 = p.cu_kv[e.x], Lk = p.cu_kv[e.x + 1] - k0;
-    const int Lq = p.cu_q[e.x + 1] - p.cu_q[e.x];
-    const int np = key_parts(e.y, Lq, Lk, p.prefix ? p.prefix[e.x] : 0, p.group, p.Hkv);
-    if (np == 1) return;
+    PromptSeq s;  // (an item that names no tile has been reported)
+    if ((e.y & 127) || e.y < 0 ||
+        !prompt_seq(p.cu_q, p.cu_kv, p.prefix, p.n_seqs, p.rows, p.keys, e.x, s) || e.y >= s.Lk)
+        return;
+    const int kvh = blockIdx.x % p.Hkv, k0 = s.k0, Lk = s.Lk;
+    const int np = key_parts(e.y, s.Lq, Lk, s.pre, p.group, p.Hkv);
+    if (np == 1 || np > p.n_parts) return;
     const int cols = hd / 4, which = blockIdx.z;
     for (int i = threadIdx.x; i < 8 * cols; i += 256) {
         const int r = blockIdx.y * 8 + i / cols, c = i % cols * 4;
@@ -377,21 +400,15 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
 #pragma unroll
             for (int c = 0; c < NCH; ++c) tma_load_3d(dst + c * BM * 128, m, c * 64, head, row, full);
         };
-        // the item claimed: its list entry, then its sequence's rows
-        int2 e = make_int2(0, 0);
+        // the next item that names a tile
         PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0};
         auto fetch = [&]() {
-            claim = __shfl_sync(0xffffffffu, claim, 0);
-            if (claim - q_first >= n_work) return;
-            e = items[(claim - q_first) / p.Hkv];
-            nx.at = KP ? e.y & ~127 : e.y;
-            nx.part = KP ? e.y & 127 : 0;
-            nx.kvh = (claim - q_first) % p.Hkv;
-            nx.q0 = p.cu_q[e.x];
-            nx.Lq = p.cu_q[e.x + 1] - nx.q0;
-            nx.k0 = p.cu_kv[e.x];
-            nx.Lk = p.cu_kv[e.x + 1] - nx.k0;
-            nx.pre = p.prefix ? p.prefix[e.x] : 0;
+            for (;;) {
+                claim = __shfl_sync(0xffffffffu, claim, 0);
+                const int w = claim - q_first;
+                if (w >= n_work || bwd_item<KP>(p, items[w / p.Hkv], w % p.Hkv, nx)) return;
+                if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
+            }
         };
         fetch();
         while (claim - q_first < n_work) {
@@ -1047,20 +1064,14 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
         };
         int no = 0;             // outer tiles loaded
         uint32_t g = 0, u = 0;  // slot tiles, units loaded
-        int2 e = make_int2(0, 0);
         PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0};
         auto fetch = [&]() {
-            claim = __shfl_sync(0xffffffffu, claim, 0);
-            if (claim - q_first >= n_work) return;
-            e = items[(claim - q_first) / p.Hkv];
-            nx.at = KP ? e.y & ~127 : e.y;
-            nx.part = KP ? e.y & 127 : 0;
-            nx.kvh = (claim - q_first) % p.Hkv;
-            nx.q0 = p.cu_q[e.x];
-            nx.Lq = p.cu_q[e.x + 1] - nx.q0;
-            nx.k0 = p.cu_kv[e.x];
-            nx.Lk = p.cu_kv[e.x + 1] - nx.k0;
-            nx.pre = p.prefix ? p.prefix[e.x] : 0;
+            for (;;) {
+                claim = __shfl_sync(0xffffffffu, claim, 0);
+                const int w = claim - q_first;
+                if (w >= n_work || bwd_item<KP>(p, items[w / p.Hkv], w % p.Hkv, nx)) return;
+                if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
+            }
         };
         const uint32_t row_bytes = p.group * T * 128;  // of 64 columns of a row tile
         fetch();
@@ -1654,11 +1665,14 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     if (!workspace || !aligned16(workspace) ||
         ws_bytes < jnx_op_prompt_attention_backward_workspace_bytes(p, n_heads, n_kv_heads, head_dim))
         return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
+    const PromptCounts list = prompt_counts(p, n_heads, n_kv_heads, head_dim, true);
+    if (p->n_forward != list.forward || p->n_keys != list.keys || p->n_queries != list.queries ||
+        p->n_parts != list.parts)
+        return fail(JNX_ERR_INVALID_ARG, "%s: a work list of other heads or lengths", what);
     const long long n_work = ((long long)2 * p->n_keys + p->n_queries) * n_kv_heads;
     // (claims run past the last item by one for each CTA and pass)
     if (n_work > 0x7FFFFFFFLL - 4 * num_sms() || (long long)rows * n_heads > 0x7FFFFFF00LL)
         return fail(JNX_ERR_UNSUPPORTED, "%s: too many work items", what);
-    if (n_work == 0) return JNX_OK;
     const jnx_head_rows none{nullptr, 0, 0};
     auto or_none = [&](const jnx_head_rows* r, int n) { return n ? *r : none; };
     int* claimed = static_cast<int*>(workspace);
@@ -1667,7 +1681,7 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
                     reinterpret_cast<const int2*>(p->items) + p->n_forward, p->n_keys, p->n_queries,
                     n_heads, n_kv_heads, n_heads / n_kv_heads, claimed,
                     (float)(1.4426950408889634 / sqrt((double)head_dim)),
-                    (float)(1.0 / sqrt((double)head_dim)), row, rows, or_none(dq, rows),
+                    (float)(1.0 / sqrt((double)head_dim)), row, p->n_seqs, rows, keys, or_none(dq, rows),
                     or_none(dk, keys), or_none(dv, keys),
                     reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + bwd_row_bytes(rows, n_heads)),
                     (long long)bwd_part_floats(p, keys, n_kv_heads, head_dim), p->n_parts, status};

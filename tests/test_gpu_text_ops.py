@@ -469,6 +469,57 @@ def test_prompt_attention_strides():
         T.close(got, want[n], want[n + "_tol"], n)
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (8, 1, 256)])
+def test_prompt_attention_leaves_out_and_reports_what_its_list_does_not_name(heads):
+    """Entries of no sequence, row, key or part, and sequences beyond the packed rows: left out
+    and reported, the others as ever."""
+    from paper_2607_16074_gb300 import jnx as J
+    R, lens = _r(), ([300, 700, 40], [300, 700, 40], [0, 100, 0])
+    q, k, v, dout = attn_inputs(heads, lens, 26)
+    clean = attn_gradients(heads, lens, q, k, v, dout)
+    plan = R.PromptPlan(*lens)
+    op = R.PromptAttention(*heads, plan, gradients=True)
+    out, lse, *d = (torch.full_like(x, 7.0) for x in clean)
+
+    def call():
+        op.forward(q, k, v, out, lse)
+        op.backward(q, k, v, out, lse, dout, *d)
+        with pytest.raises(J.JnxError) as e:
+            op.check()
+        assert e.value.code == J.JNX_ERR_DEVICE_BOUNDS
+
+    items, own = op.items, op.items.clone()
+    s = op.struct
+    first = (0, s.n_forward, s.n_forward + s.n_keys)
+    last = (s.n_forward, s.n_forward + s.n_keys, s.n_forward + s.n_keys + s.n_queries)
+    # one entry of each pass at a time: (sequence, row or key and part)
+    for bad in ((3, 0), (-1, 0), (2 ** 31 - 1, 0), (1, 2 ** 31 - 1), (1, -1), (1, -128), (0, 384),
+                (2, 127), (1, 704)):
+        for a, b in zip(first, last):
+            items.copy_(own)
+            items[(a + b) // 2] = torch.tensor(bad, device="cuda", dtype=torch.int32)
+            call()
+    items.copy_(own)
+    # the middle sequence beyond the packed rows, or its keys: the others have their results
+    for x in (0, 1):
+        device, host = plan.d[x], plan.h[x]
+        for bad in (-5, 1041, 2 ** 31 - 1):
+            device[2] = bad
+            for y in (out, lse, *d):
+                y.fill_(7.0)
+            call()
+            device[2] = int(host[2])
+            if x:
+                continue
+            assert torch.equal(out[:300], clean[0][:300]) and torch.equal(d[1][:300], clean[3][:300])
+            assert (d[1][300:1000] == 7).all() and (d[0][300:] == 7).all()
+    op.forward(q, k, v, out, lse)
+    op.backward(q, k, v, out, lse, dout, *d)
+    op.check()
+    for a, b in zip(clean, (out, lse, *d)):
+        assert torch.equal(a, b)
+
+
 def test_prompt_attention_backward_against_differences():
     heads, lens = (8, 2, 64), ([90, 33], [140, 33], [0, 20])
     q, k, v, dout = attn_inputs(heads, lens, 6)

@@ -132,6 +132,46 @@ def test_prompt_attention_backward_refuses_a_prefix_that_the_host_does_not_know(
         rows(), PTR, 1 << 30, None, None), INV)
 
 
+def test_prompt_attention_refuses_a_list_that_is_not_its_own():
+    """A list of other heads or lengths, or with its counts changed: the kernels would leave rows
+    out, or write more parts than the workspace has."""
+    L = J.lib()
+    lens = dict(q=(900, 700), kv=(900, 700), prefix=(300, 0))
+
+    def listed(heads, **lens):
+        p = prompt(**lens)
+        assert L.jnx_prompt_items(C.byref(p), *heads, None, 0) > 0
+        return p
+
+    def forward(p, heads=(8, 1, 256)):
+        return L.jnx_op_prompt_attention(C.byref(p), *heads, rows(), rows(), rows(), rows(), None,
+                                         None, None, None)
+
+    def backward(p, heads=(8, 1, 256)):
+        return L.jnx_op_prompt_attention_backward(
+            C.byref(p), *heads, rows(), rows(), rows(), rows(), None, PTR, rows(), rows(), rows(), rows(),
+            PTR, 1 << 40, None, None)
+
+    for heads in ((16, 1, 256), (8, 8, 256), (8, 1, 64)):
+        other = listed(heads, **lens)
+        refused(forward(other), INV)
+        refused(backward(other), INV)
+    # as many row tiles, but other parts of the keys' rows
+    for other in (listed((8, 1, 256), q=(900, 700), kv=(1100, 700), prefix=(300, 0)),
+                  listed((8, 1, 256), q=(900, 700), kv=(900, 700), prefix=(0, 0))):
+        own = prompt(**lens)
+        for n in ("n_forward", "n_keys", "n_queries", "n_parts"):
+            setattr(own, n, getattr(other, n))
+        refused(backward(own), INV)
+    for n in ("n_forward", "n_keys", "n_queries", "n_parts"):
+        for by in (-1, 1):
+            p = listed((8, 1, 256), **lens)
+            setattr(p, n, getattr(p, n) + by)
+            refused(backward(p), INV)
+            if n == "n_forward":
+                refused(forward(p), INV)
+
+
 def test_decode_refuses():
     L = J.lib()
     cache = J.jnx_kv_cache(PTR, PTR, 2, 4, 1024, 256, 128)
