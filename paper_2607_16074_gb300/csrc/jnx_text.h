@@ -66,10 +66,15 @@ __host__ __device__ inline int key_parts(int at, int Lq, int Lk, int prefix, int
     return n < 1 ? 1 : n < kMaxParts ? (int)n : kMaxParts;
 }
 
+// What a key tile's item costs, by which the keys' pass is sorted: rows of its part.
+__host__ __device__ inline int part_rows(int at, int Lq, int Lk, int prefix, int np) {
+    return (Lq - first_row(at, Lq, Lk, prefix)) / np;
+}
+
 // What a prompt's work list holds for a head layout: items of each pass, parts of a key tile
-// at most.
+// at most, and items of the keys' pass up to the last one of a tile in parts.
 struct PromptCounts {
-    long long forward = 0, keys = 0, queries = 0;
+    long long forward = 0, keys = 0, queries = 0, slabs = 0;
     int parts = 1;
 };
 

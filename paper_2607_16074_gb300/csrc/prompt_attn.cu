@@ -708,6 +708,7 @@ jnx_status prompt_launchable(const jnx_prompt* p, const char* what, bool gradien
 PromptCounts prompt_counts(const jnx_prompt* p, int H, int Hkv, int hd, bool gradients) {
     const int group = H / Hkv, T = tile_tokens(group), step = T * item_tiles(hd);
     PromptCounts n;
+    int least = 0x7fffffff;  // rows of an item of a tile in parts
     for (int s = 0; s < p->n_seqs; ++s) {
         const int Lq = p->h_cu_q[s + 1] - p->h_cu_q[s], Lk = p->h_cu_kv[s + 1] - p->h_cu_kv[s];
         const int pre = p->h_prefix ? p->h_prefix[s] : 0;
@@ -718,6 +719,16 @@ PromptCounts prompt_counts(const jnx_prompt* p, int H, int Hkv, int hd, bool gra
             const int np = key_parts((int)at, Lq, Lk, pre, group, Hkv);
             n.keys += np;
             n.parts = std::max(n.parts, np);
+            if (np > 1) least = std::min(least, part_rows((int)at, Lq, Lk, pre, np));
+        }
+    }
+    // the list has the items of most rows first
+    for (int s = 0; s < p->n_seqs && n.parts > 1; ++s) {
+        const int Lq = p->h_cu_q[s + 1] - p->h_cu_q[s], Lk = p->h_cu_kv[s + 1] - p->h_cu_kv[s];
+        const int pre = p->h_prefix ? p->h_prefix[s] : 0;
+        for (long long at = 0; at < Lk; at += 128) {
+            const int np = key_parts((int)at, Lq, Lk, pre, group, Hkv);
+            if (part_rows((int)at, Lq, Lk, pre, np) >= least) n.slabs += np;
         }
     }
     return n;
@@ -754,12 +765,13 @@ extern "C" int32_t jnx_prompt_items(jnx_prompt* p, int32_t n_heads, int32_t n_kv
                     const int np = pass == 1 ? key_parts((int)at, Lq, Lk, pre, n_heads / n_kv_heads,
                                                          n_kv_heads)
                                              : 1;
-                    const long long cost = pass == 1 ? (Lq - first_row((int)at, Lq, Lk, pre)) / np
+                    const long long cost = pass == 1 ? part_rows((int)at, Lq, Lk, pre, np)
                                                      : keys_seen(last, Lq, Lk, pre);
                     parts = std::max(parts, np);
                     for (int k = 0; k < np; ++k) all.push_back({s, (int)at + k, cost});
                 }
             }
+            // (stable: a tile's parts stay together and in order)
             std::stable_sort(all.begin() + first, all.end(),
                              [](const Item& x, const Item& y) { return x.cost > y.cost; });
             count[pass] = (int)(all.size() - first);

@@ -72,7 +72,7 @@ struct PromptBwdCfg {
     static constexpr int OFF_STG = OFF_B2 + SLOTS * TILE;  // 2 KB an elementwise warp
     static constexpr int OFF_ST = OFF_STG + pbwd::EW * 2048;  // [ST][-lse, -D][128]
     static constexpr int OFF_BAR = OFF_ST + pbwd::ST * 2 * pbwd::BM * 4;
-    static constexpr int SMEM = OFF_BAR + 2 * pbwd::N_BARS * 8 + 16 + pbwd::ITEMS * 32 + 1024;
+    static constexpr int SMEM = OFF_BAR + 2 * pbwd::N_BARS * 8 + 16 + pbwd::ITEMS * 36 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
     static constexpr uint32_t S_COL = 0, DP_COL = 128, ACC_COL = 256;
 };
@@ -86,16 +86,17 @@ struct PromptBwdArgs {
     const float2* row;  // [Hkv][rows][group]: lse (+inf where a row sees no key), D
     int n_seqs, rows, keys;  // what the items may name
     jnx_head_rows dq, dk, dv;
-    float* part;  // [dk, dv][n_parts][keys][Hkv][hd]: the sums of tiles taken in parts
-    long long part_stride;  // of a part
-    int n_parts;
+    // the sums of tiles taken in parts, [item of the keys' pass][Hkv][dk, dv][128][hd], for the
+    // items up to the last one of such a tile
+    float* part;
+    int n_slabs;
     int* status;
 };
 
 // What the warps of a CTA are told of an item.
 struct PromptBwdItem {
     int at, kvh, q0, Lq, k0, Lk, pre;  // at: first key or row; Lq < 0: no more in this pass
-    int part;                          // keys pass
+    int part, unit;                    // keys pass; number among the items' key heads
 
     // keys pass: parts of the tile, and this part's inner tiles [j0, j1) of T tokens from the
     // first row that sees the tile's first key
@@ -114,14 +115,16 @@ struct PromptBwdItem {
 // A claimed item's list entry: false, and reported, where it names no row, or no key and part,
 // of the prompt.
 template <bool KP>
-__device__ __forceinline__ bool bwd_item(const PromptBwdArgs& p, int2 e, int kvh, PromptBwdItem& x) {
+__device__ __forceinline__ bool bwd_item(const PromptBwdArgs& p, int2 e, int unit, PromptBwdItem& x) {
+    const int item = unit / p.Hkv;
     PromptSeq s;
     bool ok = prompt_seq(p.cu_q, p.cu_kv, p.prefix, p.n_seqs, p.rows, p.keys, e.x, s);
-    x = PromptBwdItem{KP ? e.y & ~127 : e.y, kvh, s.q0, s.Lq, s.k0, s.Lk, s.pre, KP ? e.y & 127 : 0};
+    x = PromptBwdItem{KP ? e.y & ~127 : e.y, unit - item * p.Hkv, s.q0, s.Lq, s.k0, s.Lk, s.pre,
+                      KP ? e.y & 127 : 0, unit};
     ok = ok && (unsigned)x.at < (unsigned)(KP ? x.Lk : x.Lq);
-    if (ok && KP) {
+    if (KP && ok && (x.part > 0 || item >= p.n_slabs)) {
         const int np = x.parts(p.group, p.Hkv);
-        ok = np <= p.n_parts && x.part < np;
+        ok = x.part < np && (np == 1 || item < p.n_slabs);
     }
     if (!ok && (threadIdx.x & 31) == 0) report(p.status, JNX_ERR_DEVICE_BOUNDS);
     return ok;
@@ -291,9 +294,10 @@ __device__ __forceinline__ void bwd_rows_part(uint8_t* stg, int lane, const uint
     }
 }
 
-// dk and dv of the tiles taken in parts: their sums in the parts' order.  A CTA 8 keys of a
-// tile and key head, of either gradient.  (Bound by reading the sums: CTAs of 16 keys, or a
-// share of the keys to each part's item so that none is without work, take the same 15 us.)
+// dk and dv of the tiles taken in parts: their sums in the parts' order, whose items follow one
+// another in the list.  A CTA 8 keys of a tile and key head, of either gradient.  (Bound by
+// reading the sums: CTAs of 16 keys, or a share of the keys to each part's item so that none is
+// without work, take the same 15 us.)
 __global__ void __launch_bounds__(256) k_prompt_bwd_join(const __grid_constant__ PromptBwdArgs p, int hd) {
     pdl_entry();
     const int2 e = p.items[blockIdx.x / p.Hkv];
@@ -303,18 +307,18 @@ __global__ void __launch_bounds__(256) k_prompt_bwd_join(const __grid_constant__
         return;
     const int kvh = blockIdx.x % p.Hkv, k0 = s.k0, Lk = s.Lk;
     const int np = key_parts(e.y, s.Lq, Lk, s.pre, p.group, p.Hkv);
-    if (np == 1 || np > p.n_parts) return;
+    if (np == 1 || blockIdx.x / p.Hkv + np > p.n_slabs) return;
     const int cols = hd / 4, which = blockIdx.z;
     for (int i = threadIdx.x; i < 8 * cols; i += 256) {
         const int r = blockIdx.y * 8 + i / cols, c = i % cols * 4;
         if (e.y + r >= Lk) return;
         const long long key = k0 + e.y + r;
-        const float* from = p.part + (long long)which * p.n_parts * p.part_stride +
-                            (key * p.Hkv + kvh) * hd + c;
+        const float* from = p.part + ((long long)blockIdx.x * 2 + which) * 128 * hd + r * hd + c;
+        const long long step = (long long)p.Hkv * 2 * 128 * hd;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int k = 0; k < np; ++k) {
-            const float4 v = *reinterpret_cast<const float4*>(from + k * p.part_stride);
+            const float4 v = *reinterpret_cast<const float4*>(from + k * step);
             s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
         }
         const float f = which ? 1.f : p.scale;
@@ -339,16 +343,17 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
     uint8_t* b1 = sm + C::OFF_B1;
     uint8_t* b2 = sm + C::OFF_B2;
     float* st = reinterpret_cast<float*>(sm + C::OFF_ST);
-    volatile int* slot = fail_flag + 1;  // [ITEMS][8]: items handed out
+    volatile int* slot = fail_flag + 1;  // [ITEMS][9]: items handed out
     const int2* items = p.items + (KP ? 0 : p.n_keys);
     const int n_work = (KP ? p.n_keys : p.n_queries) * p.Hkv;
 
     // the next item as warp 0 hands it out; item_done() gives its slot back
     int seen = 0;
     auto get_item = [&](int b) -> PromptBwdItem {
-        const volatile int* s = slot + 8 * b;
+        const volatile int* s = slot + 9 * b;
         return PromptBwdItem{warp_uniform(s[0]), warp_uniform(s[1]), warp_uniform(s[2]), warp_uniform(s[3]),
-                             warp_uniform(s[4]), warp_uniform(s[5]), warp_uniform(s[6]), warp_uniform(s[7])};
+                             warp_uniform(s[4]), warp_uniform(s[5]), warp_uniform(s[6]), warp_uniform(s[7]),
+                             warp_uniform(s[8])};
     };
     auto item_done = [&]() {
         __syncwarp();
@@ -359,7 +364,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
     auto next_item = [&](bool& ok) -> PromptBwdItem {
         const int b = seen % ITEMS;
         if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen / ITEMS) & 1)))
-            return PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0};
+            return PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0, 0};
         return get_item(b);
     };
     // an item's inner tiles, and the keys pass's first inner row
@@ -380,14 +385,15 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             const int b = told % ITEMS;
             if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told / ITEMS) & 1) ^ 1)) return false;
             if (elect_one()) {
-                slot[8 * b] = x.at;
-                slot[8 * b + 1] = x.kvh;
-                slot[8 * b + 2] = x.q0;
-                slot[8 * b + 3] = x.Lq;
-                slot[8 * b + 4] = x.k0;
-                slot[8 * b + 5] = x.Lk;
-                slot[8 * b + 6] = x.pre;
-                slot[8 * b + 7] = x.part;
+                slot[9 * b] = x.at;
+                slot[9 * b + 1] = x.kvh;
+                slot[9 * b + 2] = x.q0;
+                slot[9 * b + 3] = x.Lq;
+                slot[9 * b + 4] = x.k0;
+                slot[9 * b + 5] = x.Lk;
+                slot[9 * b + 6] = x.pre;
+                slot[9 * b + 7] = x.part;
+                slot[9 * b + 8] = x.unit;
                 mbar_arrive(&bar[W_FULL + b]);
             }
             __syncwarp();
@@ -401,12 +407,12 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             for (int c = 0; c < NCH; ++c) tma_load_3d(dst + c * BM * 128, m, c * 64, head, row, full);
         };
         // the next item that names a tile
-        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0};
+        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0, 0};
         auto fetch = [&]() {
             for (;;) {
                 claim = __shfl_sync(0xffffffffu, claim, 0);
                 const int w = claim - q_first;
-                if (w >= n_work || bwd_item<KP>(p, items[w / p.Hkv], w % p.Hkv, nx)) return;
+                if (w >= n_work || bwd_item<KP>(p, items[w / p.Hkv], w, nx)) return;
                 if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
             }
         };
@@ -425,6 +431,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             x.Lk = warp_uniform(nx.Lk);
             x.pre = warp_uniform(nx.pre);
             x.part = warp_uniform(nx.part);
+            x.unit = warp_uniform(nx.unit);
             if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
             __syncwarp();
             if (!(ok = tell(x))) break;
@@ -466,7 +473,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             if (!ok) break;
             fetch();
         }
-        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0});
+        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0, 0});
         if (!ok) *fail_flag = 1;
         // every copy has landed before the pass ends (at once in a normal run)
         if (no > 0) mbar_wait_warp(&bar[O_FULL], (no - 1) & 1, 100000000LL);
@@ -803,7 +810,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
             const int tok = r / p.group, hg = r % p.group, key = x.at + r, i = x.at + tok;
             const bool live = KP ? key < x.Lk : tok < T && i < x.Lq;
             const bool in_parts = KP && x.parts(p.group, p.Hkv) > 1;
-            float* part = p.part + x.part * p.part_stride;
+            float* part = p.part + (long long)x.unit * 2 * BM * HD;
             for (int acc = 0; acc < (KP ? 2 : 1); ++acc) {
                 const float f = acc ? 1.f : p.scale;
                 const jnx_head_rows& to = !KP ? p.dq : acc ? p.dv : p.dk;
@@ -811,7 +818,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                                     : KP  ? (x.k0 + key) * to.row_stride + x.kvh * to.head_stride
                                           : (x.q0 + i) * to.row_stride + (x.kvh * p.group + hg) * to.head_stride;
                 // (a tile taken in parts: its sums' rows)
-                const long long po = live ? ((long long)(x.k0 + key) * p.Hkv + x.kvh) * HD : -1;
+                const long long po = live ? r * HD : -1;
                 // this lane's row's four units into the warp's staging, out unit lane % 4 of
                 // rows lane / 4 + 8 u
                 long long at[4], pat[4];
@@ -832,7 +839,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                         for (int e = 0; e < 32; ++e) v[e] = 0;
                     }
                     if (in_parts)
-                        bwd_rows_part(stg, lane, v, part + acc * p.n_parts * p.part_stride + col, pat);
+                        bwd_rows_part(stg, lane, v, part + acc * BM * HD + col, pat);
                     else
                         bwd_rows_out(stg, lane, v, f, to.ptr + col, at);
                 }
@@ -1008,23 +1015,24 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
     uint8_t* sl = sm + (NEED_DP ? 2 * TILE : TILE + 6 * UNIT);
     uint8_t* un = sm + (NEED_DP ? 3 * TILE : TILE);
     float* st = reinterpret_cast<float*>(sm + OFF_ST);
-    volatile int* slot = fail_flag + 1;  // [2][8]: items handed out
+    volatile int* slot = fail_flag + 1;  // [2][9]: items handed out
     const int2* items = p.items + (KP ? 0 : p.n_keys);
     const int n_work = (KP ? p.n_keys : p.n_queries) * p.Hkv;
 
     int seen = 0;
     auto next_item = [&](bool& ok) -> PromptBwdItem {
         const int b = seen & 1;
-        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0, 0};
+        PromptBwdItem x{0, 0, 0, -1, 0, 0, 0, 0, 0};
         if (!(ok = mbar_wait_warp(&bar[W_FULL + b], (seen >> 1) & 1))) return x;
-        x.at = warp_uniform(slot[8 * b]);
-        x.kvh = warp_uniform(slot[8 * b + 1]);
-        x.q0 = warp_uniform(slot[8 * b + 2]);
-        x.Lq = warp_uniform(slot[8 * b + 3]);
-        x.k0 = warp_uniform(slot[8 * b + 4]);
-        x.Lk = warp_uniform(slot[8 * b + 5]);
-        x.pre = warp_uniform(slot[8 * b + 6]);
-        x.part = warp_uniform(slot[8 * b + 7]);
+        x.at = warp_uniform(slot[9 * b]);
+        x.kvh = warp_uniform(slot[9 * b + 1]);
+        x.q0 = warp_uniform(slot[9 * b + 2]);
+        x.Lq = warp_uniform(slot[9 * b + 3]);
+        x.k0 = warp_uniform(slot[9 * b + 4]);
+        x.Lk = warp_uniform(slot[9 * b + 5]);
+        x.pre = warp_uniform(slot[9 * b + 6]);
+        x.part = warp_uniform(slot[9 * b + 7]);
+        x.unit = warp_uniform(slot[9 * b + 8]);
         if (elect_one()) mbar_arrive(&bar[W_EMPTY + b]);
         __syncwarp();
         ++seen;
@@ -1048,14 +1056,15 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
             const int b = told & 1;
             if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told >> 1) & 1) ^ 1)) return false;
             if (elect_one()) {
-                slot[8 * b] = x.at;
-                slot[8 * b + 1] = x.kvh;
-                slot[8 * b + 2] = x.q0;
-                slot[8 * b + 3] = x.Lq;
-                slot[8 * b + 4] = x.k0;
-                slot[8 * b + 5] = x.Lk;
-                slot[8 * b + 6] = x.pre;
-                slot[8 * b + 7] = x.part;
+                slot[9 * b] = x.at;
+                slot[9 * b + 1] = x.kvh;
+                slot[9 * b + 2] = x.q0;
+                slot[9 * b + 3] = x.Lq;
+                slot[9 * b + 4] = x.k0;
+                slot[9 * b + 5] = x.Lk;
+                slot[9 * b + 6] = x.pre;
+                slot[9 * b + 7] = x.part;
+                slot[9 * b + 8] = x.unit;
                 mbar_arrive(&bar[W_FULL + b]);
             }
             __syncwarp();
@@ -1064,12 +1073,12 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
         };
         int no = 0;             // outer tiles loaded
         uint32_t g = 0, u = 0;  // slot tiles, units loaded
-        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0};
+        PromptBwdItem nx{0, 0, 0, 0, 0, 0, 0, 0, 0};
         auto fetch = [&]() {
             for (;;) {
                 claim = __shfl_sync(0xffffffffu, claim, 0);
                 const int w = claim - q_first;
-                if (w >= n_work || bwd_item<KP>(p, items[w / p.Hkv], w % p.Hkv, nx)) return;
+                if (w >= n_work || bwd_item<KP>(p, items[w / p.Hkv], w, nx)) return;
                 if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
             }
         };
@@ -1089,6 +1098,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
             x.Lk = warp_uniform(nx.Lk);
             x.pre = warp_uniform(nx.pre);
             x.part = warp_uniform(nx.part);
+            x.unit = warp_uniform(nx.unit);
             if (lane == 0) claim = (int)gridDim.x + atomicAdd(p.claimed, 1);
             __syncwarp();
             if (!(ok = tell(x))) break;
@@ -1169,7 +1179,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
             if (!ok) break;
             fetch();
         }
-        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0});
+        ok = ok && tell(PromptBwdItem{0, 0, 0, -1, 0, 0, 0, 0, 0});
         if (!ok) *fail_flag = 1;
         // every copy has landed, and every release has arrived, before the barriers are made anew
         if (no > 0) {
@@ -1456,9 +1466,9 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
             const jnx_head_rows& to = PASS == DQ ? p.dq : PASS == DV ? p.dv : p.dk;
             // a tile taken in parts: its sums' row
             const bool in_parts = KP && x.parts(p.group, p.Hkv) > 1;
-            float* part = p.part + (x.part + (PASS == DV ? p.n_parts : 0)) * p.part_stride;
+            float* part = p.part + ((long long)x.unit * 2 + (PASS == DV)) * BM * HD;
             const long long row = !live      ? -1
-                                  : in_parts ? ((long long)(x.k0 + key) * p.Hkv + x.kvh) * HD
+                                  : in_parts ? r * HD
                                   : KP       ? (x.k0 + key) * to.row_stride + x.kvh * to.head_stride
                                              : (x.q0 + i) * to.row_stride +
                                                    (x.kvh * p.group + hg) * to.head_stride;
@@ -1625,12 +1635,15 @@ static jnx_status launch_prompt_bwd_wide(const PromptBwdArgs& a, const jnx_head_
 
 using namespace jnx;
 
-// The claims; each row's lse and D; the parts' sums, dk's and dv's.
+// The claims; each row's lse and D; the parts' sums, dk's and dv's.  (Room for every key as
+// often as the longest sequence has parts, which this is in place of, was 5.0 GB of one
+// sequence of 12,000 tokens beside 48 of 840, 8 heads on one of 256; 0.8 GB.)
 static size_t bwd_row_bytes(int rows, int n_heads) {
     return 256 + (((size_t)rows * n_heads * sizeof(float2) + 255) & ~(size_t)255);
 }
-static size_t bwd_part_floats(const jnx_prompt* p, int keys, int n_kv_heads, int head_dim) {
-    return p->n_parts > 1 ? (size_t)keys * n_kv_heads * head_dim : 0;
+static size_t bwd_bytes(int rows, const PromptCounts& list, int n_heads, int n_kv_heads, int head_dim) {
+    return bwd_row_bytes(rows, n_heads) +
+           (size_t)list.slabs * n_kv_heads * 2 * 128 * head_dim * sizeof(float);
 }
 
 extern "C" size_t jnx_op_prompt_attention_backward_workspace_bytes(const jnx_prompt* p,
@@ -1642,8 +1655,8 @@ extern "C" size_t jnx_op_prompt_attention_backward_workspace_bytes(const jnx_pro
     if (heads_ok(n_heads, n_kv_heads, head_dim, "prompt attention backward") ||
         prompt_ok(p, "prompt attention backward", rows, keys))
         return 0;
-    return bwd_row_bytes(rows, n_heads) +
-           2 * std::max(p->n_parts, 1) * bwd_part_floats(p, keys, n_kv_heads, head_dim) * sizeof(float);
+    return bwd_bytes(rows, prompt_counts(p, n_heads, n_kv_heads, head_dim, true), n_heads, n_kv_heads,
+                     head_dim);
 }
 
 extern "C" jnx_status jnx_op_prompt_attention_backward(
@@ -1662,10 +1675,10 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
                       (rest && !rows_ok(rest)))) ||
         (keys > 0 && (!rows_ok(k) || !rows_ok(v) || !rows_ok(dk) || !rows_ok(dv))))
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned rows", what);
-    if (!workspace || !aligned16(workspace) ||
-        ws_bytes < jnx_op_prompt_attention_backward_workspace_bytes(p, n_heads, n_kv_heads, head_dim))
-        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
     const PromptCounts list = prompt_counts(p, n_heads, n_kv_heads, head_dim, true);
+    if (!workspace || !aligned16(workspace) ||
+        ws_bytes < bwd_bytes(rows, list, n_heads, n_kv_heads, head_dim))
+        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
     if (p->n_forward != list.forward || p->n_keys != list.keys || p->n_queries != list.queries ||
         p->n_parts != list.parts)
         return fail(JNX_ERR_INVALID_ARG, "%s: a work list of other heads or lengths", what);
@@ -1684,7 +1697,7 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
                     (float)(1.0 / sqrt((double)head_dim)), row, p->n_seqs, rows, keys, or_none(dq, rows),
                     or_none(dk, keys), or_none(dv, keys),
                     reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + bwd_row_bytes(rows, n_heads)),
-                    (long long)bwd_part_floats(p, keys, n_kv_heads, head_dim), p->n_parts, status};
+                    (int)list.slabs, status};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN_BWD, 0.0, s);
     auto prologue = [&](auto width) {
@@ -1710,7 +1723,7 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     const jnx_status st = head_dim == 64    ? launch_prompt_bwd<64>(a, qq, kk, vv, dd, nr, nk, s)
                           : head_dim == 128 ? launch_prompt_bwd<128>(a, qq, kk, vv, dd, nr, nk, s)
                                             : launch_prompt_bwd_wide(a, qq, kk, vv, dd, nr, nk, s);
-    if (st || p->n_parts <= 1) return st;
-    pdl(k_prompt_bwd_join, dim3(p->n_keys * n_kv_heads, 16, 2), 256, 0, s)(a, head_dim);
+    if (st || list.slabs == 0) return st;
+    pdl(k_prompt_bwd_join, dim3((int)list.slabs * n_kv_heads, 16, 2), 256, 0, s)(a, head_dim);
     return launched(what);
 }

@@ -249,6 +249,38 @@ def test_work_lists_cover_every_row_and_key_once(heads):
         assert all(x >= y for x, y in itertools.pairwise(costs))
 
 
+@pytest.mark.parametrize("heads,lens", [
+    ((8, 1, 256), [12000]), ((8, 1, 256), [12000] + [840] * 48),
+    ((8, 1, 256), [16000] + [400] * 124), ((8, 1, 256), [840] * 26), ((4, 2, 128), [3000, 70] * 9),
+    ((64, 1, 64), [5000] + [20] * 500), ((64, 1, 64), [9, 5000, 90]), ((32, 8, 128), [2900] * 24)])
+def test_prompt_backward_workspace_holds_the_parts_alone(heads, lens):
+    """Sums are kept for tiles whose rows are taken in parts, and tiles of as many rows as one of
+    their parts; not for every key as often as the longest sequence has parts.  The parts of a
+    tile follow one another in the list, which the joining of their sums goes by."""
+    h, hkv, hd = heads
+    L, p = J.lib(), prompt(lens, lens)
+    n = L.jnx_prompt_items(C.byref(p), h, hkv, hd, None, 0)
+    out = np.zeros((n, 2), np.int32)
+    L.jnx_prompt_items(C.byref(p), h, hkv, hd, out.ctypes.data, n)
+    items = out[p.n_forward:p.n_forward + p.n_keys]
+    parts = {}
+    for s, y in items:
+        parts.setdefault((s, y // 128), []).append(y % 128)
+    assert all(x == list(range(len(x))) for x in parts.values())
+    for i, (s, y) in enumerate(items):
+        if y % 128:
+            assert items[i - 1][0] == s and items[i - 1][1] == y - 1
+    inside = [i for i, (s, y) in enumerate(items) if len(parts[s, y // 128]) > 1]
+    # an item of a tile in parts has over 1,024 rows; others of over 1,024 may lie among them
+    like = sum(1 for s, y in items if (lens[s] - y // 128 * 128) * (h // hkv) >= 1024)
+    slab = hkv * 2 * 128 * hd * 4
+    need = L.jnx_op_prompt_attention_backward_workspace_bytes(C.byref(p), h, hkv, hd)
+    rows = sum(lens) * h * 8 + 512
+    assert need <= rows + (like * slab if inside else 0)
+    if inside:
+        assert need >= rows - 512 + (max(inside) + 1) * slab
+
+
 @pytest.mark.parametrize("vocab,d,piece", [(32000, 2048, 0), (32000, 4096, 256), (32000, 8192, 1000),
                                            (50257, 512, 0), (151936, 1024, 1000), (300, 64, 0)])
 def test_vocab_workspaces_for_many_rows_hold_fewer(vocab, d, piece):
