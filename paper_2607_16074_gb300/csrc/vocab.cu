@@ -657,7 +657,8 @@ static jnx_status vocab_check(const void* h, int64_t ldh, const void* w, int64_t
         return fail(JNX_ERR_INVALID_ARG, "%s: d and strides must be multiples of 8", what);
     if (n_rows > 0 && (!h || !w || !targets || !loss || !aligned16(h) || !aligned16(w)))
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned argument", what);
-    if (vocab > 0x7fffff00 || n_rows > 0x7fffff00 || d > 0x7fffff00)
+    // (rows are counted in steps of 8,192 and padded by 256)
+    if (vocab > 0x7fffff00 || n_rows > 0x7fffff00 - 8192 || d > 0x7fffff00)
         return fail(JNX_ERR_UNSUPPORTED, "%s: sizes", what);
     return JNX_OK;
 }
@@ -765,8 +766,8 @@ static jnx_status vocab_run(const uint16_t* h, int64_t ldh, const uint16_t* w, i
     if (!make_tmap_bf16(&tw, w, vocab_size, d, ldw, 128, 64) ||
         (train && !make_tmap_bf16(&twmn, w, vocab_size, d, ldw, 64, 64)))
         return fail(JNX_ERR_CUDA, "%s: tensor map encode failed", what);
-    for (int r0 = 0; r0 < n; r0 += piece) {
-        const int rows = std::min(piece, n - r0);
+    for (int r0 = 0, rows; r0 < n; r0 += rows) {
+        rows = std::min(piece, n - r0);
         VocabGemm p{};
         p.rows_max = rows;
         p.count = ws.count;

@@ -205,6 +205,15 @@ def test_vocab_loss_refuses():
     assert f(n=0, dw=None) == J.JNX_OK
 
 
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 256, 2 ** 31 - 8192])
+def test_vocab_loss_refuses_rows_that_its_counts_cannot_hold(n):
+    """Rows are counted and launched for in 32 bits, beyond the last row too."""
+    L = J.lib()
+    refused(L.jnx_op_vocab_loss(PTR, 64, PTR, 64, PTR, n, 100, 64, PTR, PTR, 1 << 62, None, None), UNS)
+    refused(L.jnx_op_vocab_loss_train(PTR, 64, PTR, 64, PTR, PTR, n, 100, 64, 0, PTR, PTR, 64, PTR, 64, PTR,
+                                      1 << 62, None, None), UNS)
+
+
 @pytest.mark.parametrize("heads", [(4, 4, 64), (8, 1, 256), (12, 4, 128), (14, 2, 64)])
 def test_work_lists_cover_every_row_and_key_once(heads):
     """Each pass visits every row (or key, in each part of its rows) of every sequence, the
