@@ -417,6 +417,44 @@ def test_prompt_attention_sharp_scores():
         T.close(got, want[n], want[n + "_tol"] * (1 + off / T.U), n)
 
 
+def test_prompt_attention_backward_of_sharp_scores():
+    """The gradients' scores at large maxima: dq and dk of rows whose weight is nearly on one key."""
+    heads, lens = (4, 2, 128), ([520], [520], [0])
+    q, k, v, dout = attn_inputs(heads, lens, 2, std=30.0)
+    k *= torch.linspace(0.2, 6, 520, device="cuda").to(BF)[:, None, None]
+    _, _, dq, dk, _ = attn_gradients(heads, lens, q, k, v, dout)
+    want, dk_tol = T.attention(q, k, v, lens, dout), torch.zeros(520, 2, 128, device="cuda", dtype=T.F64)
+    # 32-bit scores of up to 2^11 are off by 2^-11 of a unit in the forward and in the gradients,
+    # the log-sum-exp is rounded by 2^-13 of one and the exponentials by as much: P by 2^-9
+    off, see = 2.0 ** -9, T.seen(520, 520, 0, "cuda")
+    for h in range(4):
+        a, b, c, do = (x.to(T.F64) for x in (q[:, h], k[:, h // 2], v[:, h // 2], dout[:, h]))
+        p = torch.softmax((a @ b.T / math.sqrt(128)).masked_fill(~see, -math.inf), -1)
+        o = p @ c
+        ds = p * (do @ c.T - (do * o).sum(-1, keepdim=True)) / math.sqrt(128)
+        # D is of an output whose P and sums were rounded, and whose scores were off
+        d_off = (do.abs() * (T.U * o.abs() + (T.U + off) * (p @ c.abs()))).sum(-1, keepdim=True)
+        eds = (T.U + off) * ds.abs() + p * d_off / math.sqrt(128)
+        T.close(dq[:, h], want["dq"][:, h], T.U * want["dq"][:, h].abs() + eds @ b.abs(), "dq")
+        dk_tol[:, h // 2] += eds.T @ a.abs()
+    T.close(dk, want["dk"], T.U * want["dk"].abs() + dk_tol, "dk")
+
+
+@pytest.mark.parametrize("heads,lens", [
+    # so many key tiles that each is one item, of several row tiles
+    ((32, 32, 64), ([700], [700], [0])), ((32, 32, 128), ([300, 641], [300, 641], [0, 77])),
+    ((31, 31, 256), ([620], [620], [50])),
+    # more rows than the most parts of a key tile hold at 2,048 each
+    ((64, 1, 64), ([2100], [2100], [0])), ((64, 1, 64), ([2500, 9], [130, 9], [0, 0])),
+    ((64, 1, 256), ([2100, 30], [300, 30], [129, 0]))])
+def test_prompt_attention_backward_at_the_ends_of_its_parts(heads, lens):
+    q, k, v, dout = attn_inputs(heads, lens, 27)
+    _, _, dq, dk, dv = attn_gradients(heads, lens, q, k, v, dout)
+    want = T.attention(q, k, v, lens, dout)
+    for got, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+        T.close(got, want[n], want[n + "_tol"], n)
+
+
 def test_prompt_attention_other_sequences_hold_anything():
     """NaN and infinities in the neighbours' rows reach no other sequence."""
     heads, lens = (8, 2, 128), ([100, 60, 200], [130, 60, 200], [0, 9, 50])
@@ -691,6 +729,30 @@ def test_decode_attention_batches_of_all_sizes_share_a_workspace():
         assert torch.equal(out, outs[0][:out.shape[0]])
     want = decode_want(q[:6], kc, vc, slot[:6], n[:6])
     T.close(outs[0][:6], want["out"], want["out_tol"])
+
+
+@pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128), (8, 1, 256)])
+@pytest.mark.parametrize("batch", [1024, 1025, 2049])
+def test_decode_attention_of_more_sequences_than_a_launch_takes(heads, batch):
+    """Sequences of one run and of several on both sides of a launch's last one, each with the bits
+    that it has by itself."""
+    h, hkv, hd = heads
+    g = gen(28)
+    kc, vc = normal(g, 40, 700, hkv, hd), normal(g, 40, 700, hkv, hd)
+    q = normal(g, batch, h, hd)
+    i32 = lambda x: torch.tensor(x, device="cuda", dtype=torch.int32)  # noqa: E731
+    n = [(3, 64, 0, 700, 65, 1, 129, 33, 512, 700)[i % 10] for i in range(batch)]
+    slot = [i * 7 % 40 for i in range(batch)]
+    op, out, alone = _r().DecodeAttention(*heads, max_batch=batch), empty(batch, h, hd), empty(1, h, hd)
+    op.forward(q, kc, vc, i32(slot), i32(n), out)
+    some = sorted({i for at in (0, 1024, 2048, batch) for i in range(at - 12, at + 12) if 0 <= i < batch})
+    for i in some:
+        op.forward(q[i:i + 1], kc, vc, i32([slot[i]]), i32([n[i]]), alone)
+        assert torch.equal(alone[0], out[i]), i
+    op.check()
+    want = decode_want(q[some], kc, vc, i32([slot[i] for i in some]), [n[i] for i in some])
+    T.close(out[some], want["out"], want["out_tol"], "out")
+    assert torch.isfinite(out).all()
 
 
 def test_decode_matches_the_prompt():
