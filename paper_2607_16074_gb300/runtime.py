@@ -586,8 +586,10 @@ def _dense(t: torch.Tensor, dtype, *shape) -> int:
 
 def _cache(k: torch.Tensor, v: torch.Tensor, heads):
     """A cache [slots, room, kv heads, head_dim], k and v of one layout: jnx_kv_cache's fields."""
-    s, shape = k.stride(), k.shape
-    if k.dtype is not _BF16 or v.dtype is not _BF16 or v.shape != shape or v.stride() != s or \
+    s, t, shape = k.stride(), v.stride(), k.shape
+    # (an axis of length one, as a single key head's, has no stride to agree on)
+    if k.dtype is not _BF16 or v.dtype is not _BF16 or v.shape != shape or \
+            (s != t and any(a != b for a, b, n in zip(s, t, shape) if n > 1)) or \
             shape[2:] != heads or s[3] != 1 or not k.is_cuda or not v.is_cuda:
         raise ValueError(f"expected bf16 CUDA caches [slots, room, {heads[0]}, {heads[1]}] of one "
                          f"layout, got {k.dtype} {tuple(shape)} strides {s} and {v.dtype} "

@@ -632,6 +632,26 @@ def test_decode_attention_long_single():
     T.close(out, want["out"], want["out_tol"], "out")
 
 
+@pytest.mark.parametrize("shape", [(4, 300, 1, 256), (1, 70, 1, 64), (1, 129, 2, 128), (5, 1, 1, 64)])
+def test_caches_agree_though_axes_of_length_one_differ_in_stride(shape):
+    """Head-major keys beside token-major values: with one key head they lie alike."""
+    slots, room, hkv, hd = shape
+    g, heads = gen(29), (4 * hkv, hkv, hd)
+    kc = normal(g, slots, hkv, room, hd).transpose(1, 2)
+    vc = normal(g, slots, room, hkv, hd)
+    i32 = lambda *v: torch.tensor(v, device="cuda", dtype=torch.int32)  # noqa: E731
+    q, out = normal(g, 1, *heads[::2]), empty(1, *heads[::2])
+    op = _r().DecodeAttention(*heads, max_batch=1)
+    if hkv > 1:
+        with pytest.raises(ValueError):
+            op.forward(q, kc, vc, i32(0), i32(room), out)
+        return
+    op.forward(q, kc, vc, i32(slots - 1), i32(room), out)
+    op.check()
+    want = T.attention(q, kc[-1], vc[-1], ([1], [room], [0]))
+    T.close(out, want["out"], want["out_tol"], "out")
+
+
 def test_decode_attention_reads_nothing_beyond_the_length():
     """What lies behind a length, or in other slots, may be anything."""
     heads, n = (8, 2, 128), (100, 0, 65, 333)
