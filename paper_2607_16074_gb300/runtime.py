@@ -716,7 +716,7 @@ class QKNormRope(_TextOperator):
         h, hkv, hd = self.dims
         n, x, ld, p = self._args(qkv, pos)
         _bf16(dqkv, *qkv.shape)
-        if dqkv.stride(0) != ld:
+        if n > 1 and dqkv.stride(0) != ld:
             raise ValueError("dqkv and qkv differ in their row strides")
         gains = [None if g is None else _dense(g, _F32, hd) for g in (dgamma_q, dgamma_k)]
         self._qk.fill(*_view(dq, (n, h, hd)), *_view(dk, (n, hkv, hd)))

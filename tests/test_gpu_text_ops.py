@@ -212,6 +212,25 @@ def test_norm_rope_backward(heads, n, norms):
     assert torch.equal(again, dqkv) and (not norms or torch.equal(dg[0], dg2[0]))
 
 
+def test_norm_rope_backward_of_one_row_has_no_row_stride():
+    op, qkv, pos, gains, _ = rope_case((4, 4, 64), 1, (32,), 9)
+    g = gen(30)
+    dq, dk = normal(g, 1, 4, 64), normal(g, 1, 4, 64)
+    wide = empty(3, 1000)
+    wide[1:2, :768] = qkv
+    got = []
+    for x in (qkv, wide[1:2, :768]):
+        d, dg = torch.zeros(1, 768, device="cuda", dtype=BF), [empty(64, dtype=torch.float32) for _ in range(2)]
+        op.backward(x, pos, dq, dk, d, *dg)
+        got.append([d, *dg])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    two = torch.zeros(2, 768, device="cuda", dtype=BF)
+    with pytest.raises(ValueError):
+        op.backward(wide[:2, :768], pos.expand(1, 2).contiguous(), dq.expand(2, 4, 64).contiguous(),
+                    dk.expand(2, 4, 64).contiguous(), two, *dg)
+
+
 def test_norm_rope_backward_against_differences():
     """The definition's directional derivative, by central differences in 64 bits."""
     heads, n, sections = (8, 2, 128), 13, (16, 24, 24)
