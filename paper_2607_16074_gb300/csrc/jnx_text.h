@@ -85,10 +85,10 @@ struct PromptSeq {
 // False: no such sequence, or one beyond the rows and keys that the call was launched for.
 __device__ __forceinline__ bool prompt_seq(const int* cu_q, const int* cu_kv, const int* prefix, int n_seqs,
                                            int rows, int keys, int s, PromptSeq& x) {
-    if (s < 0 || s >= n_seqs) return false;
-    const int q0 = cu_q[s], q1 = cu_q[s + 1], k0 = cu_kv[s], k1 = cu_kv[s + 1];
-    x = PromptSeq{q0, q1 - q0, k0, k1 - k0, prefix ? prefix[s] : 0};
-    return 0 <= q0 && q0 <= q1 && q1 <= rows && 0 <= k0 && k0 <= k1 && k1 <= keys;
+    const int t = (unsigned)s < (unsigned)n_seqs ? s : 0;  // (no branch ahead of the loads)
+    const int q0 = cu_q[t], q1 = cu_q[t + 1], k0 = cu_kv[t], k1 = cu_kv[t + 1];
+    x = PromptSeq{q0, q1 - q0, k0, k1 - k0, prefix ? prefix[t] : 0};
+    return t == s && 0 <= q0 && q0 <= q1 && q1 <= rows && 0 <= k0 && k0 <= k1 && k1 <= keys;
 }
 
 jnx_status heads_ok(int n_heads, int n_kv_heads, int head_dim, const char* what);

@@ -438,9 +438,11 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
         const int rounds = (a.n_work + gridDim.x - 1) / gridDim.x;
         int2 e = entry(work(0));
         int told = 0;
+        auto room = [&]() {
+            return mbar_wait_warp(&bar[W_EMPTY + told % ITEMS], ((told / ITEMS) & 1) ^ 1);
+        };
         auto tell = [&](const PromptWork& x) {
             const int b = told % ITEMS;
-            if (!mbar_wait_warp(&bar[W_EMPTY + b], ((told / ITEMS) & 1) ^ 1)) return false;
             if (elect_one()) {
                 volatile int* s = slots + 8 * b;
                 s[0] = x.q0;
@@ -454,7 +456,6 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             }
             __syncwarp();
             ++told;
-            return true;
         };
         for (int r = 0; r < rounds && ok && !__any_sync(0xffffffffu, *fail_flag); ++r) {
             const int2 c = e;
@@ -462,14 +463,16 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             e = entry(work(r + 1));
             if (w >= a.n_work) continue;
             PromptSeq x;
-            if (!prompt_seq(a.cu_q, a.cu_kv, a.prefix, a.n_seqs, a.rows, a.keys, c.x, x) ||
-                (unsigned)c.y >= (unsigned)x.Lq) {
-                if (lane == 0) report(a.status, JNX_ERR_DEVICE_BOUNDS);
-                continue;
-            }
-            ok = tell(PromptWork{x.q0, c.y, x.Lq, x.k0, x.Lk, x.pre, w % a.Hkv});
+            const bool known = prompt_seq(a.cu_q, a.cu_kv, a.prefix, a.n_seqs, a.rows, a.keys, c.x, x);
+            if (!(ok = room())) break;
+            if (known && (unsigned)c.y < (unsigned)x.Lq)
+                tell(PromptWork{x.q0, c.y, x.Lq, x.k0, x.Lk, x.pre, w % a.Hkv});
+            else if (lane == 0)
+                report(a.status, JNX_ERR_DEVICE_BOUNDS);
         }
-        if (!ok || !tell(PromptWork{0, -1, 0, 0, 0, 0, 0})) *fail_flag = 1;
+        ok = ok && room();
+        if (ok) tell(PromptWork{0, -1, 0, 0, 0, 0, 0});
+        else *fail_flag = 1;
     } else if (warp >= 4) {
         // ---------------- softmax + epilogue of row tile t ----------------
         const int t = (warp - 4) >> 2;
