@@ -221,7 +221,7 @@ typedef struct {
  * theta^(-2 i / head_dim), turns the pair (i, i + head_dim / 2) by the position on
  * the axis in whose section i lies (sections[0] frequencies belong to axis 0, the
  * next sections[1] to axis 1, ...); frequencies beyond the sections do not turn.
- * Positions are exact over the whole int32 range. */
+ * Positions count in full over the whole int32 range: an angle is off by 2^-50 of itself. */
 typedef struct {
     int32_t n_heads, n_kv_heads, head_dim;
     int32_t n_axes, sections[4];

@@ -24,8 +24,8 @@ __device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
     return (uint32_t)f2bf(a) | ((uint32_t)f2bf(b) << 16);
 }
 
-// The same in one conversion instruction: two conversions and a merge made up half of an
-// attention row's softmax (12,289 tokens, 32 heads of 128: 1,236 -> 845 us).
+// The same in one conversion instruction: with two conversions and a merge for each pair of P,
+// attention of 12,289 tokens, 32 heads of 128, took 1,236 us for 845.
 __device__ __forceinline__ uint32_t cvt_bf2(float a, float b) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));

@@ -11,8 +11,9 @@
 //            S^T = K Q^T, dP^T = V dO^T, dV += P^T dO, dK += dS^T Q
 //   queries  a row tile against the 128-key tiles it sees:
 //            S = Q K^T, dP = dO V^T, dQ += dS K
-// Seven products for the gradients' five; keeping dS for a second pass would move two
-// bytes a score and head twice, which costs more than the two products do.
+// Seven products for the gradients' five.  (Keeping dS for the second pass instead would move
+// two bytes a score and head twice, 0.59 ps at 6.79 TB/s; the two products are 0.27 ps at the
+// burst rate and 0.64 at the one reached.  Not built, not measured.)
 //
 // TMEM at head dim 128 holds S, dP and two accumulators of 128 columns each, so neither
 // is double-buffered; instead the products and the elementwise warps take the halves of a
@@ -21,8 +22,9 @@
 // (In the queries' pass, whose one accumulator leaves room, a second dP was slower: 564 ->
 // 598 us.)
 //
-// Six documents of up to 2,600 tokens, 32 heads of 128 (424 GFLOP with the forward): 422 us
-// the passes, 34 the rows' values and 5 the rows of few keys, 588 with the forward's 130.
+// Six documents of up to 2,600 tokens, 32 heads of 128 (424 GFLOP with the forward): 428 us
+// the passes, 30 the rows' values and 6 the rows of few keys, 581 with the forward's 121 (588
+// in longer runs).
 // The tensor core is busy for 42 % of it: the elementwise warps' P and dS and the products
 // wait for each other, as there is no TMEM to double-buffer either.
 //
@@ -297,7 +299,8 @@ __device__ __forceinline__ void bwd_rows_part(uint8_t* stg, int lane, const uint
 // dk and dv of the tiles taken in parts: their sums in the parts' order, whose items follow one
 // another in the list.  A CTA 8 keys of a tile and key head, of either gradient.  (Bound by
 // reading the sums: CTAs of 16 keys, or a share of the keys to each part's item so that none is
-// without work, take the same 15 us.)
+// without work, took the same time: 12 us of 26 samples of up to 840 tokens, 8 heads on one
+// of 256.)
 __global__ void __launch_bounds__(256) k_prompt_bwd_join(const __grid_constant__ PromptBwdArgs p, int hd) {
     pdl_entry();
     const int2 e = p.items[blockIdx.x / p.Hkv];
@@ -958,8 +961,8 @@ static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows&
 // ahead.  (Tiles of 64 inner rows, double-buffered, left the tensor core at half:
 // a product of 128 x 64 x 16 from shared memory takes 48 clocks and one of 128 x 128 x 16
 // takes 64, 128 bytes a clock of operands either way.)
-// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 155 us
-// the passes and 15 the parts' sums, 247 with the forward's 54 and the rows' values.  Eight
+// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 160 us
+// the passes and 12 the parts' sums, 243 with the forward's 46 and the rows' values.  Eight
 // products for the gradients' five, and the tensor core busy for 37 %: an item is a few tiles,
 // and its first loads, its last products and its sums out are nobody's company, there being
 // neither TMEM nor shared memory for a second item.

@@ -20,7 +20,8 @@
 // An angle is taken modulo whole turns before it is rounded: the frequency is a 64-bit
 // fraction of a turn, so position times frequency in wrapping 64-bit integers is the
 // turn's exact fraction (2^-33 of a turn kept), where a 32-bit float product is off by
-// 6e-8 of the angle itself, 1e-3 rad at position 16,000.
+// 6e-8 of the angle itself, 1e-3 rad at position 16,000.  What is left is the frequency's own
+// rounding as a double, 2^-50 of the angle: 2e-6 rad at position 2^31.
 #include <algorithm>
 #include <cmath>
 

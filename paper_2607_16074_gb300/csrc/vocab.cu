@@ -20,8 +20,8 @@
 // the logits again instead of keeping the piece's probabilities would be a fourth.
 //
 // Bound by the tensor cores and the power cap: 8,191 rows of 4,096 on 32,000 columns with
-// gradients take 3,650 us, 1,765 TFLOP/s over all (floor 3,400): the products 1,209, 1,220
-// and 1,098, the rows 169.  333 rows of 2,048 without gradients: 55 us, of which the logits
+// gradients take 3,610 us, 1,785 TFLOP/s over all (floor 3,400), 3,680 to 3,760 in longer runs:
+// the products 1,073, 1,124 and 1,021 each by itself, the rows 151.  333 rows of 2,048 without gradients: 55 us, of which the logits
 // 49.5, two row blocks of 256 for 1.3 and four rounds of tiles for 3.3.
 #include <algorithm>
 

@@ -20,7 +20,9 @@ BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
 
 
 class TextTenant:
-    """One pre-norm attention layer between a tied vocabulary's embeddings and logits."""
+    """One pre-norm attention layer between a vocabulary's embeddings and logits.  The words
+    are one table for both, but learn through the logits alone: the gradient that reaches them
+    through the embeddings, by the residual and the projections, is left out."""
 
     def __init__(self, d=512, heads=8, kv_heads=2, head_dim=64, vocab=1024, seed=0):
         self.d, self.vocab, self.dims = d, vocab, (heads, kv_heads, head_dim)
