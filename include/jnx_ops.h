@@ -292,19 +292,17 @@ int32_t jnx_prompt_items(jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads, int
 /* out = softmax(q k^T / sqrt(head_dim)) v over what each row sees; query head h reads
  * key/value head h / (n_heads / n_kv_heads).  n_heads / n_kv_heads <= 64, head_dim in
  * {64, 128, 256}.  lse [rows, n_heads] fp32 (NULL: not written): log2 of the row's sum
- * of 2^(s log2(e) / sqrt(head_dim)).  rest (NULL: not written): what rounding left of
- * out in rows that see up to 64 keys, bf16, for the gradients (other rows are not
- * written).  q, k, v are finite; other sequences' rows may hold anything. */
+ * of 2^(s log2(e) / sqrt(head_dim)).  rest is not used: NULL.  q, k, v are finite; other
+ * sequences' rows may hold anything. */
 jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads,
                                    int32_t head_dim, const jnx_head_rows* q,
                                    const jnx_head_rows* k, const jnx_head_rows* v,
                                    const jnx_head_rows* out, const jnx_head_rows* rest,
                                    float* lse, int32_t* status, void* stream);
 
-/* Gradients of q, k and v from out's gradient dout, with the forward's out, lse and rest
- * (NULL: the rowsum(dout * out) that a score's gradient is taken against is as exact as
- * out, in rows of few keys too).  A row that sees one key has no gradient at its scores: exactly zero.  The same
- * bits whatever else is packed beside a sequence. */
+/* Gradients of q, k and v from out's gradient dout, with the forward's out and lse (rest is
+ * not used: NULL).  A row that sees one key has no gradient at its scores: exactly zero.  The
+ * same bits whatever else is packed beside a sequence. */
 size_t jnx_op_prompt_attention_backward_workspace_bytes(const jnx_prompt* p, int32_t n_heads,
                                                         int32_t n_kv_heads, int32_t head_dim);
 jnx_status jnx_op_prompt_attention_backward(const jnx_prompt* p, int32_t n_heads,

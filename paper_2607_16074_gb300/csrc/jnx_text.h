@@ -48,12 +48,6 @@ __host__ __device__ inline int item_tiles(int head_dim) { return head_dim == 256
 
 constexpr int kMaxGroup = 64;
 
-// Rows that see up to so many keys have what rounding left of their output written for the
-// gradients, where the caller gives it a place.  D = rowsum(dO * O) is a sum that dP nearly
-// cancels against where few keys make a row: sequences of 12 to 64 keys have dQ off by 0.0024
-// of its norm with it and 0.0026 without, of 400 keys 0.0025 either way.
-constexpr int kRestKeys = 64;
-
 // Parts that the gradients' keys pass takes a 128-key tile's rows in: one where a sequence
 // has a tile for every SM by itself, else 2,048 rows each (token, head of the group).  Of
 // the sequence and the heads alone, so that a sequence's bits do not depend on others.  A

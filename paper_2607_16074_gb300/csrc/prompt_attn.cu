@@ -84,8 +84,6 @@ struct PromptArgs {
     float scale_log2;
     uint16_t* out;
     long long o_row, o_head;
-    uint16_t* rest;  // what out's rounding left
-    long long r_row, r_head;
     float* lse;
     int* status;
 };
@@ -125,9 +123,7 @@ __device__ __forceinline__ void stage_rows(uint8_t* stg, int lane, const uint32_
     __syncwarp();
 }
 
-// REST: a.rest is written, of rows that see few keys, for which the inference's rows have no
-// registers to spare.
-template <int HD, bool REST>
+template <int HD>
 __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
     k_prompt_attn(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
                   const __grid_constant__ CUtensorMap tv, const __grid_constant__ PromptArgs a) {
@@ -595,22 +591,15 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
             const volatile int* s = slots + 8 * (seen % ITEMS);
             const int i = s[1] + t * T + tok, row0 = s[0], h = s[6] * a.group + hg;
             const bool live = tok < T && i < s[2];
-            const bool few = REST && live && keys_seen(i, s[2], s[4], s[5]) <= kRestKeys;
             item_done();
             if (live && a.lse) a.lse[(size_t)(row0 + i) * a.H + h] = m + log2f(l);
             const float inv = l > 0.f ? 1.f / l : 0.f;
             // out through the warp's staging, 32 columns at a time: this lane writes its
             // row's four units and stores unit lane % 4 of rows lane / 4 + 8 j
-            long long o = live ? (long long)(row0 + i) * a.o_row + h * a.o_head : -1;
-            long long to[4], ro[4];
+            const long long o = live ? (long long)(row0 + i) * a.o_row + h * a.o_head : -1;
+            long long to[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) to[j] = __shfl_sync(0xffffffffu, o, 8 * j + (lane >> 2));
-            const bool rest = __any_sync(0xffffffffu, few);
-            if constexpr (REST) {
-                o = few ? (long long)(row0 + i) * a.r_row + h * a.r_head : -1;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) ro[j] = __shfl_sync(0xffffffffu, o, 8 * j + (lane >> 2));
-            }
 #pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
                 uint32_t w[32];
@@ -630,12 +619,6 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
                 for (int e = 0; e < 32; ++e)
                     w[e] = l > 0.f ? __float_as_uint(__uint_as_float(w[e]) * inv) : 0u;
                 stage_rows(stg, lane, w, a.out + c * 32, to);
-                if (REST && rest) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        w[e] = __float_as_uint(__uint_as_float(w[e]) - bf2f(f2bf(__uint_as_float(w[e]))));
-                    stage_rows(stg, lane, w, a.rest + c * 32, ro);
-                }
             }
         }
         if (!ok) *fail_flag = 1;
@@ -648,12 +631,12 @@ __global__ void __launch_bounds__(PromptCfg<HD>::THREADS, 1)
     if (warp == 1) tmem_dealloc(tbase, 512);
 }
 
-template <int HD, bool REST>
+template <int HD>
 static jnx_status launch_prompt(const PromptArgs& a, const jnx_head_rows& q, const jnx_head_rows& k,
                                 const jnx_head_rows& v, int rows, int keys, cudaStream_t s) {
     using C = PromptCfg<HD>;
     static std::atomic<uint64_t> attr{0};
-    if (set_smem_limit(reinterpret_cast<const void*>(k_prompt_attn<HD, REST>), C::SMEM, attr) != cudaSuccess)
+    if (set_smem_limit(reinterpret_cast<const void*>(k_prompt_attn<HD>), C::SMEM, attr) != cudaSuccess)
         return fail(JNX_ERR_CUDA, "prompt attention: smem attribute");
     CUtensorMap tq, tk, tv;
     if (!make_tmap_heads(&tq, q, rows, a.H, HD, a.group, tile_tokens(a.group)) ||
@@ -661,7 +644,7 @@ static jnx_status launch_prompt(const PromptArgs& a, const jnx_head_rows& q, con
         !make_tmap_heads(&tv, v, keys, a.Hkv, HD, 1, C::VKEYS))
         return fail(JNX_ERR_CUDA, "prompt attention: tensor map encode failed");
     const int grid = std::min(a.n_work, num_sms());
-    pdl(k_prompt_attn<HD, REST>, grid, C::THREADS, C::SMEM, s)(tq, tk, tv, a);
+    pdl(k_prompt_attn<HD>, grid, C::THREADS, C::SMEM, s)(tq, tk, tv, a);
     return launched("prompt attention");
 }
 
@@ -799,13 +782,14 @@ extern "C" jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_hea
                                               int32_t n_kv_heads, int32_t head_dim,
                                               const jnx_head_rows* q, const jnx_head_rows* k,
                                               const jnx_head_rows* v, const jnx_head_rows* out,
-                                              const jnx_head_rows* rest, float* lse, int32_t* status, void* stream) {
+                                              const jnx_head_rows* /* rest */, float* lse,
+                                              int32_t* status, void* stream) {
     clear_error();
     int rows, keys;
     if (jnx_status st = heads_ok(n_heads, n_kv_heads, head_dim, "prompt attention")) return st;
     if (jnx_status st = prompt_launchable(p, "prompt attention", false, rows, keys)) return st;
     if (rows == 0) return JNX_OK;
-    if (!rows_ok(q) || !rows_ok(out) || (rest && !rows_ok(rest)) || (keys > 0 && (!rows_ok(k) || !rows_ok(v))))
+    if (!rows_ok(q) || !rows_ok(out) || (keys > 0 && (!rows_ok(k) || !rows_ok(v))))
         return fail(JNX_ERR_INVALID_ARG, "prompt attention: null or misaligned rows");
     const long long n_work = (long long)p->n_forward * n_kv_heads;
     if (n_work > 0x7FFFFFFFLL - 2 * num_sms())
@@ -817,16 +801,11 @@ extern "C" jnx_status jnx_op_prompt_attention(const jnx_prompt* p, int32_t n_hea
     PromptArgs a{p->cu_q, p->cu_kv, p->prefix, reinterpret_cast<const int2*>(p->items), p->n_seqs, rows,
                  keys, (int)n_work, n_heads, n_kv_heads, n_heads / n_kv_heads,
                  (float)(1.4426950408889634 / sqrt((double)head_dim)), out->ptr, out->row_stride,
-                 out->head_stride, rest ? rest->ptr : nullptr, rest ? rest->row_stride : 0,
-                 rest ? rest->head_stride : 0, lse, status};
+                 out->head_stride, lse, status};
     if (!keys) keys = 1;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_PROMPT_ATTN, 0.0, s);
-    auto go = [&](auto with_rest) {
-        constexpr bool REST = decltype(with_rest)::value;
-        if (head_dim == 64) return launch_prompt<64, REST>(a, *q, kk, vv, rows, keys, s);
-        if (head_dim == 128) return launch_prompt<128, REST>(a, *q, kk, vv, rows, keys, s);
-        return launch_prompt<256, REST>(a, *q, kk, vv, rows, keys, s);
-    };
-    return rest ? go(std::true_type{}) : go(std::false_type{});
+    if (head_dim == 64) return launch_prompt<64>(a, *q, kk, vv, rows, keys, s);
+    if (head_dim == 128) return launch_prompt<128>(a, *q, kk, vv, rows, keys, s);
+    return launch_prompt<256>(a, *q, kk, vv, rows, keys, s);
 }

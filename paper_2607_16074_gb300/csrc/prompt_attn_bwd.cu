@@ -23,7 +23,7 @@
 // 598 us.)
 //
 // Six documents of up to 2,600 tokens, 32 heads of 128 (424 GFLOP with the forward): 428 us
-// the passes, 30 the rows' values and 6 the rows of few keys, 581 with the forward's 121 (588
+// the passes, 30 the rows' values and 7 the rows of few keys, 586 with the forward's 121 (590
 // in longer runs).
 // The tensor core is busy for 42 % of it: the elementwise warps' P and dS and the products
 // wait for each other, as there is no TMEM to double-buffer either.
@@ -153,8 +153,7 @@ __device__ __forceinline__ float lanes_sum(float d) {
 
 // The rows' (lse, D = rowsum(dO * O)), and the claim counter to zero.  HD / 8 lanes a row,
 // four rows of neighbouring heads a lane, whose loads are under way at once.  Bound by HBM.
-// (By tiles of a sequence and key head, 256 bytes a row: 52 us for 7,000 rows of 32 heads;
-// as they lie 37, then still with `rest`.)
+// (By tiles of a sequence and key head, 256 bytes a row, they were half as slow again.)
 template <int HD>
 __global__ void __launch_bounds__(256)
     k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, const float* lse, int rows, int H, int group,
@@ -193,20 +192,77 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-// Rows that see few keys: their D over again.  dS = P (dP - D) adds up to zero over a row's
-// keys only as far as D is what the kernel's own P and dP add up to.  rowsum(dO * O) is off by
-// the roundings of O, which `rest` makes up for, and of the forward's P, which shows where few
-// terms nearly cancel: dQ of sequences of two tokens was off by 0.0050 of its norm, against
-// 0.0024 that its own two roundings make; up to kFewKeys keys D is the sum of P dP in fp32.
-// A CTA some rows of a sequence and key head.  (Looked up in the kernel above, where a row's
-// sequence is not at hand, these rows took 20 us of 7,000 rows of 32 heads, and here 5.)
-constexpr int kFewKeys = 8;
+// Rows that see few keys: their D over again.  dS = P (dP - D) adds up to zero over a row's keys
+// only as far as D is what the kernel's own P and dP add up to.  rowsum(dO * O) is off by the
+// roundings of O and of the forward's P, which shows where few terms nearly cancel: dQ of
+// sequences of two tokens was off by 0.0050 of its norm, of 12 to 64 tokens by 0.0026, against
+// the 0.0024 that its own two roundings make.  Up to kFewKeys keys D is the sum of P dP in fp32;
+// beyond, the rounding of O is one of several alike (400 tokens: 0.0025).
+// Two warps 16 rows (token, head of the group) of a sequence and key head, 32 of the keys each,
+// by mma.sync: 32 columns of the contraction at a time, of which a lane holds eight neighbours of
+// each operand, so that both are loaded by 16 bytes and agree on which columns a product takes.
+// Bound by the loads' latency, a step after another: 9 us of 26 samples of up to 840 tokens, 8
+// heads on one of 256, 7 of six documents of 32 heads of 128.  (A warp for all 64 keys, a step's
+// loads ahead alone, 12 and 10.)
+constexpr int kFewKeys = 64, kFewTiles = 2;  // keys of a row, tiles of 16 rows a CTA, at most
+
+// A lane's two rows of such a tile.
+struct FewRows {
+    int at[2], head[2], seen[2];
+    float l[2];
+};
+// What 8 NT keys from k0 on make up of D of a tile's rows; the loads of two steps are under way
+// at once.
+template <int HD, int NT>
+__device__ __forceinline__ void few_rows(const jnx_head_rows& dout, const jnx_head_rows& q,
+                                         const jnx_head_rows& k, const jnx_head_rows& v, const PromptSeq& s,
+                                         int kvh, int k0, float scale_log2, const FewRows& r,
+                                         float (&d)[2]) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = (lane & 3) * 8;
+    float sc[NT][4] = {}, dp[NT][4] = {};
+#pragma unroll 2
+    for (int x = c; x < HD; x += 32) {
+        uint4 qa[2], ga[2], kk[NT], vv[NT];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            qa[e] = head_unit(q, r.at[e], r.head[e], x);
+            ga[e] = head_unit(dout, r.at[e], r.head[e], x);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const long long key = s.k0 + min(k0 + t * 8 + g, s.Lk - 1);
+            kk[t] = head_unit(k, key, kvh, x);
+            vv[t] = head_unit(v, key, kvh, x);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            mma_bf16(sc[t], qa[0].x, qa[1].x, qa[0].y, qa[1].y, kk[t].x, kk[t].y);
+            mma_bf16(sc[t], qa[0].z, qa[1].z, qa[0].w, qa[1].w, kk[t].z, kk[t].w);
+            mma_bf16(dp[t], ga[0].x, ga[1].x, ga[0].y, ga[1].y, vv[t].x, vv[t].y);
+            mma_bf16(dp[t], ga[0].z, ga[1].z, ga[0].w, ga[1].w, vv[t].z, vv[t].w);
+        }
+    }
+    d[0] = d[1] = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = i >> 1;
+            if (k0 + t * 8 + (lane & 3) * 2 + (i & 1) < r.seen[e])
+                d[e] += ex2_approx(fmaf(sc[t][i], scale_log2, -r.l[e])) * dp[t][i];
+        }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        d[e] += __shfl_xor_sync(0xffffffffu, d[e], 1);
+        d[e] += __shfl_xor_sync(0xffffffffu, d[e], 2);
+    }
+}
+
 template <int HD>
-__global__ void __launch_bounds__(256)
-    k_prompt_bwd_few(jnx_head_rows out, jnx_head_rows rest, jnx_head_rows dout, jnx_head_rows q,
-                     jnx_head_rows k, jnx_head_rows v, const float* lse,
-                     const __grid_constant__ PromptBwdArgs p, float2* row) {
-    constexpr int LANES = HD / 8, PER = 256 / LANES;
+__global__ void __launch_bounds__(64 * kFewTiles)
+    k_prompt_bwd_few(jnx_head_rows dout, jnx_head_rows q, jnx_head_rows k, jnx_head_rows v,
+                     const float* lse, const __grid_constant__ PromptBwdArgs p, float2* row) {
+    __shared__ float upper[kFewTiles][16];  // of keys from 32 on
     pdl_entry();
     const int sq = blockIdx.x / p.Hkv, kvh = blockIdx.x % p.Hkv;
     PromptSeq s;
@@ -214,43 +270,36 @@ __global__ void __launch_bounds__(256)
         if (threadIdx.x == 0) report(p.status, JNX_ERR_DEVICE_BOUNDS);
         return;
     }
-    const int q0 = s.q0, Lq = s.Lq, k0 = s.k0, Lk = s.Lk, pre = s.pre;
-    const int most = rest.ptr ? kRestKeys : kFewKeys;
     // rows [a, b): the first that sees a key, the first that sees too many
-    const int a = first_row(0, Lq, Lk, pre), b = Lk > most ? first_row(most, Lq, Lk, pre) : Lq;
-    const int c = threadIdx.x % LANES * 8, n = Lk > 0 ? (b - a) * p.group : 0;
-    for (int r0 = blockIdx.y * PER; r0 < n; r0 += gridDim.y * PER) {
-        // a lane without a row of its own goes along with the last
-        const int r = min(r0 + (int)threadIdx.x / LANES, n - 1);
-        const int i = a + r / p.group, hg = r % p.group, h = kvh * p.group + hg;
-        const long long at = q0 + i;
-        const int seen = keys_seen(i, Lq, Lk, pre);
-        const uint4 g = head_unit(dout, at, h, c);
-        const float l = lse[at * p.H + h];
-        float d = 0.f;
-        if (__any_sync(0xffffffffu, seen > kFewKeys)) {
-            d = dot8(head_unit(out, at, h, c), g);
-            if (rest.ptr) d += dot8(head_unit(rest, at, h, c), g);
-            d = lanes_sum<LANES>(d);
-        }
-        if (__any_sync(0xffffffffu, seen <= kFewKeys)) {
-            const uint4 x = head_unit(q, at, h, c);
-            uint4 kk[kFewKeys], vv[kFewKeys];
+    const int a = first_row(0, s.Lq, s.Lk, s.pre);
+    const int b = s.Lk > kFewKeys ? first_row(kFewKeys, s.Lq, s.Lk, s.pre) : s.Lq;
+    const int n = s.Lk > 0 ? (b - a) * p.group : 0;
+    const int lane = threadIdx.x & 31, g = lane >> 2;
+    const int tile = threadIdx.x >> 6, half = warp_uniform(threadIdx.x >> 5) & 1;
+    for (int c0 = blockIdx.y * kFewTiles * 16; c0 < n; c0 += gridDim.y * kFewTiles * 16) {
+        const int t0 = c0 + tile * 16;
+        FewRows r;  // one beyond the last goes along with it
 #pragma unroll
-            for (int j = 0; j < kFewKeys; ++j) {
-                kk[j] = head_unit(k, k0 + min(j, seen - 1), kvh, c);
-                vv[j] = head_unit(v, k0 + min(j, seen - 1), kvh, c);
-            }
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < kFewKeys; ++j) {
-                const float s = lanes_sum<LANES>(dot8(x, kk[j])), dp = lanes_sum<LANES>(dot8(g, vv[j]));
-                if (j < seen) sum += ex2_approx(fmaf(s, p.scale_log2, -l)) * dp;
-            }
-            if (seen <= kFewKeys) d = sum;
+        for (int e = 0; e < 2; ++e) {
+            const int w = min(t0 + g + 8 * e, n - 1), i = a + w / p.group;
+            r.at[e] = s.q0 + i;
+            r.head[e] = kvh * p.group + w % p.group;
+            r.seen[e] = keys_seen(i, s.Lq, s.Lk, s.pre);
+            r.l[e] = lse[(long long)r.at[e] * p.H + r.head[e]];
         }
-        if (c == 0 && r0 + (int)threadIdx.x / LANES < n)
-            row[((long long)kvh * p.rows + at) * p.group + hg] = make_float2(l, d);
+        // this half's keys that the tile's last row sees
+        const int most = keys_seen(a + min(t0 + 15, n - 1) / p.group, s.Lq, s.Lk, s.pre) - 32 * half;
+        float d[2] = {0.f, 0.f};
+        if (t0 < n && most > 16) few_rows<HD, 4>(dout, q, k, v, s, kvh, 32 * half, p.scale_log2, r, d);
+        else if (t0 < n && most > 0) few_rows<HD, 2>(dout, q, k, v, s, kvh, 32 * half, p.scale_log2, r, d);
+        if (half && (lane & 3) == 0) upper[tile][g] = d[0], upper[tile][g + 8] = d[1];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (!half && (lane & 3) == 0 && t0 + g + 8 * e < n)
+                row[((long long)kvh * p.rows + r.at[e]) * p.group + r.head[e] - kvh * p.group] =
+                    make_float2(r.l[e], d[e] + upper[tile][g + 8 * e]);
+        __syncthreads();
     }
 }
 
@@ -961,8 +1010,8 @@ static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows&
 // ahead.  (Tiles of 64 inner rows, double-buffered, left the tensor core at half:
 // a product of 128 x 64 x 16 from shared memory takes 48 clocks and one of 128 x 128 x 16
 // takes 64, 128 bytes a clock of operands either way.)
-// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 160 us
-// the passes and 12 the parts' sums, 243 with the forward's 46 and the rows' values.  Eight
+// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 157 us
+// the passes and 12 the parts' sums, 248 with the forward's 47 and the rows' values.  Eight
 // products for the gradients' five, and the tensor core busy for 37 %: an item is a few tiles,
 // and its first loads, its last products and its sums out are nobody's company, there being
 // neither TMEM nor shared memory for a second item.
@@ -1665,8 +1714,8 @@ extern "C" size_t jnx_op_prompt_attention_backward_workspace_bytes(const jnx_pro
 extern "C" jnx_status jnx_op_prompt_attention_backward(
     const jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
     const jnx_head_rows* q, const jnx_head_rows* k, const jnx_head_rows* v,
-    const jnx_head_rows* out, const jnx_head_rows* rest, const float* lse, const jnx_head_rows* dout,
-    const jnx_head_rows* dq, const jnx_head_rows* dk, const jnx_head_rows* dv, void* workspace,
+    const jnx_head_rows* out, const jnx_head_rows* /* rest */, const float* lse,
+    const jnx_head_rows* dout, const jnx_head_rows* dq, const jnx_head_rows* dk, const jnx_head_rows* dv, void* workspace,
     size_t ws_bytes, int32_t* status, void* stream) {
     clear_error();
     const char* what = "prompt attention backward";
@@ -1674,8 +1723,7 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     if (jnx_status st = heads_ok(n_heads, n_kv_heads, head_dim, what)) return st;
     if (jnx_status st = prompt_launchable(p, what, true, rows, keys)) return st;
     if (rows == 0 && keys == 0) return JNX_OK;
-    if ((rows > 0 && (!rows_ok(q) || !rows_ok(out) || !rows_ok(dout) || !rows_ok(dq) || !lse ||
-                      (rest && !rows_ok(rest)))) ||
+    if ((rows > 0 && (!rows_ok(q) || !rows_ok(out) || !rows_ok(dout) || !rows_ok(dq) || !lse)) ||
         (keys > 0 && (!rows_ok(k) || !rows_ok(v) || !rows_ok(dk) || !rows_ok(dv))))
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned rows", what);
     const PromptCounts list = prompt_counts(p, n_heads, n_kv_heads, head_dim, true);
@@ -1708,12 +1756,9 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
         const long long all = (long long)rows * n_heads;
         pdl(k_prompt_bwd_rows<HD>, std::max(1, (int)((all + PER - 1) / PER)), 256, 0, s)(
             or_none(out, rows), or_none(dout, rows), lse, rows, n_heads, a.group, row, claimed);
-        if (rows && keys) {
-            constexpr int LINE = 256 / (HD / 8);
-            const int most = rest ? kRestKeys : kFewKeys;
-            pdl(k_prompt_bwd_few<HD>, dim3(p->n_seqs * n_kv_heads, (most * a.group + LINE - 1) / LINE),
-                256, 0, s)(*out, rest ? *rest : none, *dout, *q, *k, *v, lse, a, row);
-        }
+        if (rows && keys)
+            pdl(k_prompt_bwd_few<HD>, dim3(p->n_seqs * n_kv_heads, kFewKeys * a.group / (16 * kFewTiles)),
+                64 * kFewTiles, 0, s)(*dout, *q, *k, *v, lse, a, row);
     };
     if (head_dim == 64) prologue(std::integral_constant<int, 64>{});
     else if (head_dim == 128) prologue(std::integral_constant<int, 128>{});

@@ -775,40 +775,29 @@ class PromptAttention(_TextOperator):
         self.gradients = gradients
         rows = J.jnx_head_rows
         self._qs, self._ks = (plan.n_q, n_heads, head_dim), (plan.n_kv, n_kv_heads, head_dim)
-        self._fwd, self._bwd, self._left = _Views(*[rows] * 4), _Views(*[rows] * 8), _Views(rows)
-
-    def _rest(self, rest: Optional[torch.Tensor]):
-        if rest is None:
-            return None
-        self._left.fill(*_view(rest, self._qs))
-        return self._left.refs[0]
+        self._fwd, self._bwd = _Views(*[rows] * 4), _Views(*[rows] * 8)
 
     def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
-                lse: Optional[torch.Tensor] = None, stream=None,
-                rest: Optional[torch.Tensor] = None) -> None:
-        """out [n_q, H, hd]; lse [n_q, H] fp32 where the gradients are wanted later; rest, of
-        out's shape: what rounding left of out in rows that see up to 64 keys (others' are not
-        written), with which their gradients are as exact as those of longer rows."""
+                lse: Optional[torch.Tensor] = None, stream=None) -> None:
+        """out [n_q, H, hd]; lse [n_q, H] fp32 where the gradients are wanted later."""
         qs, ks = self._qs, self._ks
         if lse is not None:
             lse = _dense(lse, _F32, *qs[:2])
         self._fwd.fill(*_view(q, qs), *_view(k, ks), *_view(v, ks), *_view(out, qs))
-        J.check(self._lib.jnx_op_prompt_attention(self._ref, *self.dims, *self._fwd.refs,
-                                                  self._rest(rest), lse, self._status,
-                                                  self._on(stream)))
+        J.check(self._lib.jnx_op_prompt_attention(self._ref, *self.dims, *self._fwd.refs, None, lse,
+                                                  self._status, self._on(stream)))
 
-    def backward(self, q, k, v, out, lse, dout, dq, dk, dv, stream=None,
-                 rest: Optional[torch.Tensor] = None) -> None:
-        """dq, dk, dv from dout, with out, lse and (None: done without) rest of the forward of
-        the same q, k and v.  Nothing is kept from a forward to its backward."""
+    def backward(self, q, k, v, out, lse, dout, dq, dk, dv, stream=None) -> None:
+        """dq, dk, dv from dout, with out and lse of the forward of the same q, k and v.  Nothing
+        is kept from a forward to its backward."""
         if not self.gradients:
             raise ValueError("made for the forward only (gradients=False)")
         qs, ks, r = self._qs, self._ks, self._bwd.refs
         self._bwd.fill(*_view(q, qs), *_view(k, ks), *_view(v, ks), *_view(out, qs),
                        *_view(dout, qs), *_view(dq, qs), *_view(dk, ks), *_view(dv, ks))
         J.check(self._lib.jnx_op_prompt_attention_backward(
-            self._ref, *self.dims, *r[:4], self._rest(rest), _dense(lse, _F32, *qs[:2]),
-            *r[4:], self._ws, self._nws, self._status, self._on(stream)))
+            self._ref, *self.dims, *r[:4], None, _dense(lse, _F32, *qs[:2]), *r[4:],
+            self._ws, self._nws, self._status, self._on(stream)))
 
 
 class DecodeAttention(_TextOperator):

@@ -90,14 +90,13 @@ class TextTenant:
         self.rope.forward(qkv, pos, q, k)
         op = R.PromptAttention(*self.dims, plan, gradients=gradients)
         lse = torch.empty(n, h, device="cuda", dtype=F32) if gradients else None
-        rest = torch.empty_like(att) if gradients else None
-        op.forward(q, k, self._values(qkv), att, lse, rest=rest)
+        op.forward(q, k, self._values(qkv), att, lse)
         op.check()
-        return self._out(x, att), (op, qkv, q, k, att, lse, rest)
+        return self._out(x, att), (op, qkv, q, k, att, lse)
 
     def train_step(self, plan, x, pos, targets, weight, lr):
         """One step on the weighted sum of the rows' losses; returns the losses."""
-        y, (op, qkv, q, k, att, lse, rest) = self.forward(plan, x, pos, gradients=True)
+        y, (op, qkv, q, k, att, lse) = self.forward(plan, x, pos, gradients=True)
         n = x.shape[0]
         loss = torch.empty(n, device="cuda", dtype=F32)
         dh, dw = torch.empty(n, self.d, device="cuda", dtype=BF), torch.empty_like(self.words[0])
@@ -115,8 +114,7 @@ class TextTenant:
         h, hkv, hd = self.dims
         rows = dqkv.view(n, h + 2 * hkv, hd)
         dq, dk = rows[:, :h], rows[:, h:h + hkv]
-        op.backward(q, k, self._values(qkv), att, lse, datt.view_as(att), dq, dk, rows[:, h + hkv:],
-                    rest=rest)
+        op.backward(q, k, self._values(qkv), att, lse, datt.view_as(att), dq, dk, rows[:, h + hkv:])
         op.check()
         self.rope.backward(qkv, pos, dq, dk, dqkv, self.d_gains[0, 0], self.d_gains[1, 0])
         self.d_words[0].copy_(dw)

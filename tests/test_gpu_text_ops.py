@@ -368,9 +368,8 @@ def test_prompt_attention_backward_keeps_its_precision_on_short_sequences(heads,
         assert float((got.to(T.F64) - want[n]).norm() / want[n].norm()) < 0.003
 
 
-@pytest.mark.parametrize("with_rest", [False, True])
 @pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128), (8, 1, 256)])
-def test_prompt_attention_backward_belongs_to_its_own_forward(heads, with_rest):
+def test_prompt_attention_backward_belongs_to_its_own_forward(heads):
     """Several forwards of one plan, then their backwards in another order: each has the bits
     that it has by itself, on an object of its own."""
     R, lens = _r(), ([40] * 9 + [200], [40] * 9 + [200], [0] * 10)
@@ -379,13 +378,12 @@ def test_prompt_attention_backward_belongs_to_its_own_forward(heads, with_rest):
 
     def forward(op, x):
         out, lse = empty(*x[0].shape), empty(x[0].shape[0], heads[0], dtype=torch.float32)
-        rest = empty(*x[0].shape) if with_rest else None
-        op.forward(*x[:3], out, lse, rest=rest)
-        return out, lse, rest
+        op.forward(*x[:3], out, lse)
+        return out, lse
 
-    def backward(op, x, out, lse, rest):
+    def backward(op, x, out, lse):
         d = [empty(*y.shape) for y in x[:3]]
-        op.backward(*x[:3], out, lse, x[3], *d, rest=rest)
+        op.backward(*x[:3], out, lse, x[3], *d)
         op.check()
         return d
 
@@ -402,22 +400,19 @@ def test_prompt_attention_backward_belongs_to_its_own_forward(heads, with_rest):
             assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128), (8, 1, 256)])
-def test_prompt_attention_backward_with_rest_is_closer(heads):
-    """In rows of 9 to 64 keys, what rounding left of the output brings dq and dk nearer."""
-    lens = ([40] * 40, [40] * 40, [0] * 40)
-    x = attn_inputs(heads, lens, 24)
-    want, off = T.attention(*x[:3], lens, x[3]), {}
-    op = _r().PromptAttention(*heads, _r().PromptPlan(*lens), gradients=True)
-    for rest in (None, empty(*x[0].shape)):
-        out, lse = empty(*x[0].shape), empty(x[0].shape[0], heads[0], dtype=torch.float32)
-        d = [empty(*y.shape) for y in x[:3]]
-        op.forward(*x[:3], out, lse, rest=rest)
-        op.backward(*x[:3], out, lse, x[3], *d, rest=rest)
-        off[rest is not None] = [float((y.to(T.F64) - want[n]).norm() / want[n].norm())
-                                 for y, n in zip(d, ("dq", "dk"))]
-    op.check()
-    assert all(a < b < 0.003 for a, b in zip(off[True], off[False]))
+@pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128), (8, 1, 256), (14, 2, 64), (64, 1, 64)])
+@pytest.mark.parametrize("lens", [[12], [40], [64], [5, 17, 33, 64], [9, 70]])
+@pytest.mark.parametrize("prefix", [False, True])
+def test_prompt_attention_backward_of_few_keys_is_as_close_as_its_roundings(heads, lens, prefix):
+    """Rows of up to 64 keys: dq and dk are off by the rounding of dS and their own, 0.0017 of
+    the norm each and 0.0024 together: under one and a half times a rounding."""
+    q = (lens * 40)[:40]
+    lens = (q, q, [x // 2 if prefix else 0 for x in q])
+    q, k, v, dout = attn_inputs(heads, lens, 24)
+    _, _, dq, dk, _ = attn_gradients(heads, lens, q, k, v, dout)
+    want = T.attention(q, k, v, lens, dout)
+    for got, n in ((dq, "dq"), (dk, "dk")):
+        assert float((got.to(T.F64) - want[n]).norm() / want[n].norm()) < 1.5 * 0.0017
 
 
 def test_prompt_attention_sharp_scores():
