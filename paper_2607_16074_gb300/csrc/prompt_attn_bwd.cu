@@ -23,8 +23,7 @@
 // 598 us.)
 //
 // Six documents of up to 2,600 tokens, 32 heads of 128 (424 GFLOP with the forward): 428 us
-// the passes, 30 the rows' values and 7 the rows of few keys, 586 with the forward's 121 (590
-// in longer runs).
+// the passes and 34 the rows' values, 579 with the forward's 121 (588 in longer runs).
 // The tensor core is busy for 42 % of it: the elementwise warps' P and dS and the products
 // wait for each other, as there is no TMEM to double-buffer either.
 //
@@ -86,6 +85,7 @@ struct PromptBwdArgs {
     int* claimed;       // items taken beyond the grid's first: 0 at launch
     float scale_log2, scale;
     const float2* row;  // [Hkv][rows][group]: lse (+inf where a row sees no key), D
+    const float* few;   // alike: D of rows of few keys, in place of the other
     int n_seqs, rows, keys;  // what the items may name
     jnx_head_rows dq, dk, dv;
     // the sums of tiles taken in parts, [item of the keys' pass][Hkv][dk, dv][128][hd], for the
@@ -132,6 +132,16 @@ __device__ __forceinline__ bool bwd_item(const PromptBwdArgs& p, int2 e, int uni
     return ok;
 }
 
+constexpr int kFewKeys = 64, kFewTiles = 2;  // keys of a row at most; tiles of 16 rows a CTA
+
+// lse and D of row i of an item's sequence and head hg of its group.
+__device__ __forceinline__ float2 row_values(const PromptBwdArgs& p, const PromptBwdItem& x, int i, int hg) {
+    const size_t at = ((size_t)x.kvh * p.rows + x.q0 + i) * p.group + hg;
+    const int seen = keys_seen(i, x.Lq, x.Lk, x.pre);
+    const float* d = 0 < seen && seen <= kFewKeys ? p.few + at : &p.row[at].y;  // (one load, no branch)
+    return make_float2(p.row[at].x, *d);
+}
+
 __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
     const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
     float d = 0.f;
@@ -151,76 +161,34 @@ __device__ __forceinline__ float lanes_sum(float d) {
     return d;
 }
 
-// The rows' (lse, D = rowsum(dO * O)), and the claim counter to zero.  HD / 8 lanes a row,
-// four rows of neighbouring heads a lane, whose loads are under way at once.  Bound by HBM.
-// (By tiles of a sequence and key head, 256 bytes a row, they were half as slow again.)
-template <int HD>
-__global__ void __launch_bounds__(256)
-    k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, const float* lse, int rows, int H, int group,
-                      float2* row, int* claimed) {
-    constexpr int LANES = HD / 8, PER = 256 / LANES;
-    pdl_entry();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *claimed = 0;
-    const long long all = (long long)rows * H;
-    const long long w0 = (long long)blockIdx.x * PER * 4 + threadIdx.x / LANES;
-    const int c = threadIdx.x % LANES * 8;
-    uint4 g[4], o[4];
-    float l[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const long long w = w0 + b * PER;
-        g[b] = o[b] = make_uint4(0, 0, 0, 0);
-        l[b] = 0.f;
-        if (w < all) {
-            const long long r = w / H;
-            const int h = (int)(w - r * H);
-            g[b] = head_unit(dout, r, h, c);
-            o[b] = head_unit(out, r, h, c);
-            l[b] = lse[w];
-        }
-    }
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const float d = lanes_sum<LANES>(dot8(o[b], g[b]));
-        const long long w = w0 + b * PER;
-        if (w < all && c == 0) {
-            const long long r = w / H;
-            const int h = (int)(w - r * H);
-            row[((long long)(h / group) * rows + r) * group + h % group] =
-                l[b] == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(l[b], d);
-        }
-    }
-}
-
 // Rows that see few keys: their D over again.  dS = P (dP - D) adds up to zero over a row's keys
 // only as far as D is what the kernel's own P and dP add up to.  rowsum(dO * O) is off by the
 // roundings of O and of the forward's P, which shows where few terms nearly cancel: dQ of
 // sequences of two tokens was off by 0.0050 of its norm, of 12 to 64 tokens by 0.0026, against
 // the 0.0024 that its own two roundings make.  Up to kFewKeys keys D is the sum of P dP in fp32;
 // beyond, the rounding of O is one of several alike (400 tokens: 0.0025).
-// Two warps 16 rows (token, head of the group) of a sequence and key head, 32 of the keys each,
+// Four warps 16 rows (token, head of the group) of a sequence and key head, 16 of the keys each,
 // by mma.sync: 32 columns of the contraction at a time, of which a lane holds eight neighbours of
 // each operand, so that both are loaded by 16 bytes and agree on which columns a product takes.
-// Bound by the loads' latency, a step after another: 9 us of 26 samples of up to 840 tokens, 8
-// heads on one of 256, 7 of six documents of 32 heads of 128.  (A warp for all 64 keys, a step's
-// loads ahead alone, 12 and 10.)
-constexpr int kFewKeys = 64, kFewTiles = 2;  // keys of a row, tiles of 16 rows a CTA, at most
-
+// Bound by the loads' latency, a step after another, while the other rows' loads keep HBM busy:
+// 26 us in all of 26 samples of up to 840 tokens, 8 heads on one of 256.  (By a launch of its
+// own, 24 and 9 us, or 26 with a warp for all 64 keys whose loads waited for one another.)
 // A lane's two rows of such a tile.
 struct FewRows {
     int at[2], head[2], seen[2];
     float l[2];
 };
-// What 8 NT keys from k0 on make up of D of a tile's rows; the loads of two steps are under way
+// What 16 keys from k0 on make up of D of a tile's rows; the loads of four steps are under way
 // at once.
-template <int HD, int NT>
+template <int HD>
 __device__ __forceinline__ void few_rows(const jnx_head_rows& dout, const jnx_head_rows& q,
                                          const jnx_head_rows& k, const jnx_head_rows& v, const PromptSeq& s,
                                          int kvh, int k0, float scale_log2, const FewRows& r,
                                          float (&d)[2]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = (lane & 3) * 8;
+    constexpr int NT = 2;  // of eight keys
     float sc[NT][4] = {}, dp[NT][4] = {};
-#pragma unroll 2
+#pragma unroll 4
     for (int x = c; x < HD; x += 32) {
         uint4 qa[2], ga[2], kk[NT], vv[NT];
 #pragma unroll
@@ -258,13 +226,13 @@ __device__ __forceinline__ void few_rows(const jnx_head_rows& dout, const jnx_he
     }
 }
 
+// A CTA's share, `of` CTAs a sequence and key head.
 template <int HD>
-__global__ void __launch_bounds__(64 * kFewTiles)
-    k_prompt_bwd_few(jnx_head_rows dout, jnx_head_rows q, jnx_head_rows k, jnx_head_rows v,
-                     const float* lse, const __grid_constant__ PromptBwdArgs p, float2* row) {
-    __shared__ float upper[kFewTiles][16];  // of keys from 32 on
-    pdl_entry();
-    const int sq = blockIdx.x / p.Hkv, kvh = blockIdx.x % p.Hkv;
+__device__ __forceinline__ void few_tiles(const jnx_head_rows& dout, const jnx_head_rows& q,
+                                          const jnx_head_rows& k, const jnx_head_rows& v, const float* lse,
+                                          const PromptBwdArgs& p, float* few, int cta, int of) {
+    __shared__ float part[kFewTiles][4][16];
+    const int sq = cta / of / p.Hkv, kvh = cta / of % p.Hkv;
     PromptSeq s;
     if (!prompt_seq(p.cu_q, p.cu_kv, p.prefix, p.n_seqs, p.rows, p.keys, sq, s)) {
         if (threadIdx.x == 0) report(p.status, JNX_ERR_DEVICE_BOUNDS);
@@ -275,8 +243,8 @@ __global__ void __launch_bounds__(64 * kFewTiles)
     const int b = s.Lk > kFewKeys ? first_row(kFewKeys, s.Lq, s.Lk, s.pre) : s.Lq;
     const int n = s.Lk > 0 ? (b - a) * p.group : 0;
     const int lane = threadIdx.x & 31, g = lane >> 2;
-    const int tile = threadIdx.x >> 6, half = warp_uniform(threadIdx.x >> 5) & 1;
-    for (int c0 = blockIdx.y * kFewTiles * 16; c0 < n; c0 += gridDim.y * kFewTiles * 16) {
+    const int tile = threadIdx.x >> 7, quarter = warp_uniform(threadIdx.x >> 5) & 3;
+    for (int c0 = cta % of * kFewTiles * 16; c0 < n; c0 += of * kFewTiles * 16) {
         const int t0 = c0 + tile * 16;
         FewRows r;  // one beyond the last goes along with it
 #pragma unroll
@@ -287,19 +255,70 @@ __global__ void __launch_bounds__(64 * kFewTiles)
             r.seen[e] = keys_seen(i, s.Lq, s.Lk, s.pre);
             r.l[e] = lse[(long long)r.at[e] * p.H + r.head[e]];
         }
-        // this half's keys that the tile's last row sees
-        const int most = keys_seen(a + min(t0 + 15, n - 1) / p.group, s.Lq, s.Lk, s.pre) - 32 * half;
+        // a warp's quarter of the keys, as far as the tile's last row sees them
+        const int most = keys_seen(a + min(t0 + 15, n - 1) / p.group, s.Lq, s.Lk, s.pre);
         float d[2] = {0.f, 0.f};
-        if (t0 < n && most > 16) few_rows<HD, 4>(dout, q, k, v, s, kvh, 32 * half, p.scale_log2, r, d);
-        else if (t0 < n && most > 0) few_rows<HD, 2>(dout, q, k, v, s, kvh, 32 * half, p.scale_log2, r, d);
-        if (half && (lane & 3) == 0) upper[tile][g] = d[0], upper[tile][g + 8] = d[1];
+        if (t0 < n && most > 16 * quarter)
+            few_rows<HD>(dout, q, k, v, s, kvh, 16 * quarter, p.scale_log2, r, d);
+        float(&sums)[4][16] = part[tile];
+        if ((lane & 3) == 0) sums[quarter][g] = d[0], sums[quarter][g + 8] = d[1];
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (!half && (lane & 3) == 0 && t0 + g + 8 * e < n)
-                row[((long long)kvh * p.rows + r.at[e]) * p.group + r.head[e] - kvh * p.group] =
-                    make_float2(r.l[e], d[e] + upper[tile][g + 8 * e]);
+        for (int e = 0; e < 2; ++e) {
+            const int u = g + 8 * e;
+            if (quarter == 0 && (lane & 3) == 0 && t0 + u < n)
+                few[((long long)kvh * p.rows + r.at[e]) * p.group + r.head[e] - kvh * p.group] =
+                    (sums[0][u] + sums[1][u]) + (sums[2][u] + sums[3][u]);
+        }
         __syncthreads();
+    }
+}
+
+// The rows' (lse, D = rowsum(dO * O)), D of rows of few keys beside it, and the claim counter to
+// zero.  HD / 8 lanes a row, four rows of neighbouring heads a lane, whose loads are under way at
+// once: bound by HBM.  (By tiles of a sequence and key head, 256 bytes a row, they were half as
+// slow again.)  The first n_few CTAs take the rows of few keys meanwhile, whose place in a
+// sequence the others do not know.
+template <int HD>
+__global__ void __launch_bounds__(256, 3)
+    k_prompt_bwd_rows(jnx_head_rows out, jnx_head_rows dout, jnx_head_rows q, jnx_head_rows k,
+                      jnx_head_rows v, const float* lse, const __grid_constant__ PromptBwdArgs p,
+                      float2* row, float* few, int n_few, int of) {
+    constexpr int LANES = HD / 8, PER = 256 / LANES;
+    pdl_entry();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.claimed = 0;
+    if ((int)blockIdx.x < n_few) {
+        few_tiles<HD>(dout, q, k, v, lse, p, few, blockIdx.x, of);
+        return;
+    }
+    const long long all = (long long)p.rows * p.H;
+    const long long w0 = (long long)(blockIdx.x - n_few) * PER * 4 + threadIdx.x / LANES;
+    const int c = threadIdx.x % LANES * 8;
+    uint4 g[4], o[4];
+    float l[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const long long w = w0 + b * PER;
+        g[b] = o[b] = make_uint4(0, 0, 0, 0);
+        l[b] = 0.f;
+        if (w < all) {
+            const long long r = w / p.H;
+            const int h = (int)(w - r * p.H);
+            g[b] = head_unit(dout, r, h, c);
+            o[b] = head_unit(out, r, h, c);
+            l[b] = lse[w];
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const float d = lanes_sum<LANES>(dot8(o[b], g[b]));
+        const long long w = w0 + b * PER;
+        if (w < all && c == 0) {
+            const long long r = w / p.H;
+            const int h = (int)(w - r * p.H);
+            row[((long long)(h / p.group) * p.rows + r) * p.group + h % p.group] =
+                l[b] == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(l[b], d);
+        }
     }
 }
 
@@ -680,8 +699,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 for (int e = 0; e < 4; ++e) {
                     const int r = e * 32 + lane, t = r / p.group, i = i0 + j * T + t;
                     const bool live = t < T && i < x.Lq;
-                    v[e] = live ? p.row[((size_t)x.kvh * p.rows + x.q0 + i0 + j * T) * p.group + r]
-                                : make_float2(INFINITY, 0.f);
+                    v[e] = live ? row_values(p, x, i, r - t * p.group) : make_float2(INFINITY, 0.f);
                 }
                 if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g / ST) & 1) ^ 1))) break;
 #pragma unroll
@@ -724,8 +742,7 @@ __device__ __forceinline__ int prompt_bwd_pass(const CUtensorMap& tq, const CUte
                 } else if (r < T * p.group && x.at + r / p.group < x.Lq) {
                     // keys that this thread's row sees; a softmax over one does not move
                     const int i = x.at + r / p.group;
-                    const float2 v =
-                        p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + r % p.group];
+                    const float2 v = row_values(p, x, i, r % p.group);
                     nlse = -v.x;
                     nD = -v.y;
                     lim = keys_seen(i, x.Lq, x.Lk, x.pre);
@@ -1010,8 +1027,8 @@ static jnx_status launch_prompt_bwd(const PromptBwdArgs& a, const jnx_head_rows&
 // ahead.  (Tiles of 64 inner rows, double-buffered, left the tensor core at half:
 // a product of 128 x 64 x 16 from shared memory takes 48 clocks and one of 128 x 128 x 16
 // takes 64, 128 bytes a clock of operands either way.)
-// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 157 us
-// the passes and 12 the parts' sums, 248 with the forward's 47 and the rows' values.  Eight
+// 26 samples of up to 840 tokens, 8 heads on one of 256 (108 GFLOP with the forward): 160 us
+// the passes and 12 the parts' sums, 241 with the forward's 46 and the rows' values.  Eight
 // products for the gradients' five, and the tensor core busy for 37 %: an item is a few tiles,
 // and its first loads, its last products and its sums out are nobody's company, there being
 // neither TMEM nor shared memory for a second item.
@@ -1388,8 +1405,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
                 for (int e = 0; e < 4; ++e) {
                     const int r = e * 32 + lane, t = r / p.group, i = i0 + j * T + t;
                     const bool live = t < T && i < x.Lq;
-                    v[e] = live ? p.row[((size_t)x.kvh * p.rows + x.q0 + i0 + j * T) * p.group + r]
-                                : make_float2(INFINITY, 0.f);
+                    v[e] = live ? row_values(p, x, i, r - t * p.group) : make_float2(INFINITY, 0.f);
                 }
                 if (!(ok = mbar_wait_warp(&bar[ST_EMPTY + b], ((g / NST) & 1) ^ 1))) break;
 #pragma unroll
@@ -1424,7 +1440,7 @@ __device__ __forceinline__ int prompt_bwd_wide_pass(const CUtensorMap& tq, const
             const int two = PASS == DK ? (x.Lk > 1 ? first_row(1, x.Lq, x.Lk, x.pre) : x.Lq) : 0;
             const int from = KP ? (max(first_row(key, x.Lq, x.Lk, x.pre), two) - i0) * p.group : 0;
             if (!KP && live) {
-                const float2 v = p.row[((size_t)x.kvh * p.rows + x.q0 + i) * p.group + hg];
+                const float2 v = row_values(p, x, i, hg);
                 nlse = -v.x;
                 nD = -v.y;
                 lim = keys_seen(i, x.Lq, x.Lk, x.pre);
@@ -1687,11 +1703,11 @@ static jnx_status launch_prompt_bwd_wide(const PromptBwdArgs& a, const jnx_head_
 
 using namespace jnx;
 
-// The claims; each row's lse and D; the parts' sums, dk's and dv's.  (Room for every key as
+// The claims; each row's lse and D, and the other D; the parts' sums, dk's and dv's.  (Room for every key as
 // often as the longest sequence has parts, which this is in place of, was 5.0 GB of one
 // sequence of 12,000 tokens beside 48 of 840, 8 heads on one of 256; 0.8 GB.)
 static size_t bwd_row_bytes(int rows, int n_heads) {
-    return 256 + (((size_t)rows * n_heads * sizeof(float2) + 255) & ~(size_t)255);
+    return 256 + (((size_t)rows * n_heads * (sizeof(float2) + sizeof(float)) + 255) & ~(size_t)255);
 }
 static size_t bwd_bytes(int rows, const PromptCounts& list, int n_heads, int n_kv_heads, int head_dim) {
     return bwd_row_bytes(rows, n_heads) +
@@ -1735,17 +1751,19 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
         return fail(JNX_ERR_INVALID_ARG, "%s: a work list of other heads or lengths", what);
     const long long n_work = ((long long)2 * p->n_keys + p->n_queries) * n_kv_heads;
     // (claims run past the last item by one for each CTA and pass)
-    if (n_work > 0x7FFFFFFFLL - 4 * num_sms() || (long long)rows * n_heads > 0x7FFFFFF00LL)
+    if (n_work > 0x7FFFFFFFLL - 4 * num_sms() || (long long)rows * n_heads > 0x7FFFFFF00LL ||
+        (long long)p->n_seqs * n_kv_heads > 0x3FFFFFFFLL)
         return fail(JNX_ERR_UNSUPPORTED, "%s: too many work items", what);
     const jnx_head_rows none{nullptr, 0, 0};
     auto or_none = [&](const jnx_head_rows* r, int n) { return n ? *r : none; };
     int* claimed = static_cast<int*>(workspace);
     float2* row = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + 256);
+    float* few = reinterpret_cast<float*>(row + (size_t)rows * n_heads);
     PromptBwdArgs a{p->cu_q, p->cu_kv, p->prefix,
                     reinterpret_cast<const int2*>(p->items) + p->n_forward, p->n_keys, p->n_queries,
                     n_heads, n_kv_heads, n_heads / n_kv_heads, claimed,
                     (float)(1.4426950408889634 / sqrt((double)head_dim)),
-                    (float)(1.0 / sqrt((double)head_dim)), row, p->n_seqs, rows, keys, or_none(dq, rows),
+                    (float)(1.0 / sqrt((double)head_dim)), row, few, p->n_seqs, rows, keys, or_none(dq, rows),
                     or_none(dk, keys), or_none(dv, keys),
                     reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + bwd_row_bytes(rows, n_heads)),
                     (int)list.slabs, status};
@@ -1753,12 +1771,15 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     TraceScope ts(JNX_K_PROMPT_ATTN_BWD, 0.0, s);
     auto prologue = [&](auto width) {
         constexpr int HD = decltype(width)::value, PER = 4 * 256 / (HD / 8);
-        const long long all = (long long)rows * n_heads;
-        pdl(k_prompt_bwd_rows<HD>, std::max(1, (int)((all + PER - 1) / PER)), 256, 0, s)(
-            or_none(out, rows), or_none(dout, rows), lse, rows, n_heads, a.group, row, claimed);
-        if (rows && keys)
-            pdl(k_prompt_bwd_few<HD>, dim3(p->n_seqs * n_kv_heads, kFewKeys * a.group / (16 * kFewTiles)),
-                64 * kFewTiles, 0, s)(*dout, *q, *k, *v, lse, a, row);
+        const long long all = (long long)rows * n_heads, heads = (long long)p->n_seqs * n_kv_heads;
+        // a sequence's rows of few keys are 2 group tiles' pairs at most: a CTA each, or fewer
+        // where there are sequences enough
+        const int of = (int)std::min<long long>(kFewKeys * a.group / (16 * kFewTiles),
+                                                std::max<long long>(1, 4 * 152 / heads));
+        const long long n_few = rows && keys ? heads * of : 0;
+        pdl(k_prompt_bwd_rows<HD>, (int)(n_few + std::max(1LL, (all + PER - 1) / PER)), 256, 0, s)(
+            or_none(out, rows), or_none(dout, rows), or_none(q, rows), or_none(k, keys),
+            or_none(v, keys), lse, a, row, few, (int)n_few, of);
     };
     if (head_dim == 64) prologue(std::integral_constant<int, 64>{});
     else if (head_dim == 128) prologue(std::integral_constant<int, 128>{});

@@ -20,9 +20,10 @@
 // the logits again instead of keeping the piece's probabilities would be a fourth.
 //
 // Bound by the tensor cores and the power cap: 8,191 rows of 4,096 on 32,000 columns with
-// gradients take 3,610 us, 1,785 TFLOP/s over all (floor 3,400), 3,680 to 3,760 in longer runs:
-// the products 1,073, 1,124 and 1,021 each by itself, the rows 151.  333 rows of 2,048 without gradients: 55 us, of which the logits
-// 49.5, two row blocks of 256 for 1.3 and four rounds of tiles for 3.3.
+// gradients take 3,590 us, 1,795 TFLOP/s over all (floor 3,400), 3,650 to 3,760 in longer runs:
+// the products 1,040, 1,175 and 1,070 each by itself, the rows 150.  333 rows of 2,048 without
+// gradients: 48 us, of which the logits 46 by themselves, two row blocks of 256 for 1.3 and four
+// rounds of tiles for 3.3.
 #include <algorithm>
 
 #include "jnx_dev.cuh"
@@ -522,8 +523,8 @@ __global__ void __launch_bounds__(1024)
 }
 
 // h's rows to their packed places and zero rows behind them; ignored rows get loss 0 and
-// gradient 0.  A CTA a row.  COUNT: it counts the rows ahead itself, a launch less: 56 us for 58
-// of 333 rows of 2,048 on 32,000 words, and training on 8,192 rows of 1,024 on 8,000 188 for
+// gradient 0.  A CTA a row.  COUNT: it counts the rows ahead itself, a launch less: 2 of some 50
+// us of 333 rows of 2,048 on 32,000 words, and training on 8,192 rows of 1,024 on 8,000 188 us for
 // 200; the reads grow with the square of the rows, hence the limit.
 template <bool COUNT>
 __global__ void __launch_bounds__(256)

@@ -284,7 +284,7 @@ def test_prompt_backward_workspace_holds_the_parts_alone(heads, lens):
     like = sum(1 for s, y in items if (lens[s] - y // 128 * 128) * (h // hkv) >= 1024)
     slab = hkv * 2 * 128 * hd * 4
     need = L.jnx_op_prompt_attention_backward_workspace_bytes(C.byref(p), h, hkv, hd)
-    rows = sum(lens) * h * 8 + 512
+    rows = sum(lens) * h * 12 + 512
     assert need <= rows + (like * slab if inside else 0)
     if inside:
         assert need >= rows - 512 + (max(inside) + 1) * slab
