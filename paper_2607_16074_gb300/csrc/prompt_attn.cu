@@ -32,8 +32,9 @@
 // Bound by the softmax that feeds the tensor cores: one prompt of 12,289 tokens, 32 heads
 // on 8 of 128, takes 751 us, 1,650 TFLOP/s of the pairs that count (floor 653); 24 of up to
 // 2,900 tokens, 461 us (floor 305), the diagonal's tiles and an item's first and last steps
-// weighing more; in longer runs, at the clock that the power cap leaves, 778 and 496.  Three stubs of up to 300 tokens, 8 heads on one of 256: 12.1 us, one
-// item's loads, products and softmax after one another.
+// weighing more; in longer runs, at the clock that the power cap leaves, 778 and 496.  Three
+// stubs of up to 300 tokens, 8 heads on one of 256: 12.1 us, one item's loads, products and
+// softmax after one another.
 #include <algorithm>
 #include <type_traits>
 #include <vector>

@@ -1731,8 +1731,8 @@ extern "C" jnx_status jnx_op_prompt_attention_backward(
     const jnx_prompt* p, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
     const jnx_head_rows* q, const jnx_head_rows* k, const jnx_head_rows* v,
     const jnx_head_rows* out, const jnx_head_rows* /* rest */, const float* lse,
-    const jnx_head_rows* dout, const jnx_head_rows* dq, const jnx_head_rows* dk, const jnx_head_rows* dv, void* workspace,
-    size_t ws_bytes, int32_t* status, void* stream) {
+    const jnx_head_rows* dout, const jnx_head_rows* dq, const jnx_head_rows* dk,
+    const jnx_head_rows* dv, void* workspace, size_t ws_bytes, int32_t* status, void* stream) {
     clear_error();
     const char* what = "prompt attention backward";
     int rows, keys;

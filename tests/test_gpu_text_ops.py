@@ -1025,3 +1025,37 @@ def test_vocab_loss_against_differences():
     terms = [dh.to(T.F64) * uh, dw.to(T.F64) * uw]
     mine = sum(x.sum() for x in terms)
     assert abs(mine - slope) < 6 * 2.0 ** -8 * math.sqrt(sum(float(x.norm()) ** 2 for x in terms))
+
+
+# ---------------------------------------------------------------- workspaces
+
+def test_what_a_workspace_held_before_does_not_matter():
+    """All bits set (NaN, huge counts) or none: every call has the same results."""
+    R, heads = _r(), (8, 2, 128)
+    lens = ([300, 9, 0, 900, 64], [300, 70, 5, 900, 64], [20, 0, 0, 500, 3])
+    q, k, v, dout = attn_inputs(heads, lens, 31)
+    rope, qkv, pos, _, _ = rope_case(heads, 300, (64,), 32)
+    h, w, t, rw = vocab_case(300, 4000, 1024, 33)
+    n = [900, 30, 0, 2222, 513]
+    q1, kc, vc, slot, _ = decode(heads, n, 2300)
+    n = torch.tensor(n, device="cuda", dtype=torch.int32)
+    prompts = R.PromptAttention(*heads, R.PromptPlan(*lens), gradients=True)
+    one, words = R.DecodeAttention(*heads, max_batch=9), R.VocabLoss(w, max_rows=400)
+    seen = []
+    for fill in (255, 0):
+        for op in (rope, prompts, one, words):
+            op.ws.fill_(fill)
+        out, lse = empty(*q.shape), empty(q.shape[0], 8, dtype=torch.float32)
+        d = [empty(*x.shape) for x in (q, k, v)]
+        prompts.forward(q, k, v, out, lse)
+        prompts.backward(q, k, v, out, lse, dout, *d)
+        o1, loss, dh, dw = empty(*q1.shape), empty(300, dtype=torch.float32), empty(*h.shape), empty(*w.shape)
+        one.forward(q1, kc, vc, slot, n, o1)
+        words.train(h, t, rw, loss, dh, dw)
+        dqkv, dg = torch.zeros_like(qkv), [empty(128, dtype=torch.float32) for _ in range(2)]
+        rope.backward(qkv, pos, q[:300], k[:300], dqkv, *dg)
+        for op in (rope, prompts, one, words):
+            op.check()
+        seen.append([out, lse, *d, o1, loss, dh, dw, dqkv, *dg])
+    for a, b in zip(*seen):
+        assert torch.equal(a, b) and not a.isnan().any()
