@@ -667,6 +667,8 @@ jnx_status jnx_pack_gate_up(const uint16_t* w_gate, const uint16_t* w_up, int32_
 #define JNX_K_PROMPT_ATTN_BWD 25 /* its gradients; work = 0 */
 #define JNX_K_DECODE_ATTN 26     /* single tokens against a cache; work = 0 */
 #define JNX_K_VOCAB 27           /* next-token losses and their gradients; work = 0 */
+#define JNX_K_TREE_ATTN 28       /* trees of drafted tokens against a cache; work = 0 */
+#define JNX_K_VERIFY 29          /* drafted tokens verified, their rows kept; work = 0 */
 
 /* While enabled on the calling thread, each kernel launch of the library is
  * bracketed by two CUDA events on its stream (up to `capacity` launches are

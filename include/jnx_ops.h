@@ -349,6 +349,109 @@ jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, const uint16_
                                    int64_t lddw, void* workspace, size_t ws_bytes,
                                    int32_t* status, void* stream);
 
+/* The same against a teacher's top logits.  Row i has up to `top` entries (1 to 128): words
+ * ids[i * top + k] with the teacher's logits teacher[i * top + k]; a negative id or a logit
+ * of -inf is no entry, an id >= vocab is reported and read as none, an id given twice has
+ * both entries' probability.  With T = softmax(teacher / temperature) over the row's entries
+ * and P = softmax(h w^T / temperature) over the vocabulary, loss[i] = sum_k T_k (log T_k -
+ * log P_k); 0 for a row without entries, whose h is not read into any sum.  Logits are finite
+ * or -inf; temperature > 0.  Otherwise as the next-token losses. */
+size_t jnx_op_vocab_distill_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d, int32_t top);
+jnx_status jnx_op_vocab_distill(const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw,
+                                const int32_t* ids, const float* teacher, int32_t top,
+                                float temperature, int32_t n_rows, int32_t vocab, int32_t d,
+                                float* loss, void* workspace, size_t ws_bytes, int32_t* status,
+                                void* stream);
+size_t jnx_op_vocab_distill_train_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d,
+                                                  int32_t top, int32_t piece_rows);
+jnx_status jnx_op_vocab_distill_train(const uint16_t* h, int64_t ldh, const uint16_t* w,
+                                      int64_t ldw, const int32_t* ids, const float* teacher,
+                                      int32_t top, float temperature, const float* row_weight,
+                                      int32_t n_rows, int32_t vocab, int32_t d,
+                                      int32_t piece_rows, float* loss, uint16_t* dh, int64_t lddh,
+                                      uint16_t* dw, int64_t lddw, void* workspace,
+                                      size_t ws_bytes, int32_t* status, void* stream);
+
+/* ---- answering with drafted tokens ----
+ * Several tokens a step: a live sequence's last known token and the tokens drafted behind
+ * it are the nodes of a tree, its root first and every node behind its parent.  Their keys
+ * and values are appended behind the sequence's cached ones, the tree is attended in one
+ * call, verified against the target's probabilities, and the accepted rows are kept.
+ * Node i of sequence s is row cu_nodes[s] + i of the nodes' tensors; a sequence has up to
+ * 64 nodes, or none.  The conventions of the text tenants' operators apply. */
+
+/* Where live sequences' tokens lie in a cache whose slots are pages: token t of sequence s
+ * in row t % room of page table[s * ld + t / room].  max_pages: entries of a sequence.  Only
+ * entries whose pages hold tokens of a call are read. */
+typedef struct {
+    const int32_t* table;
+    int64_t ld;
+    int32_t n_seqs, max_pages;
+} jnx_pages;
+
+/* jnx_op_qk_norm_rope_append to pages: token i's key and value heads go to token at[i] of
+ * sequence seq[i].  A token whose sequence, entry or page is not there is not written and
+ * reported.  No two tokens of a call have the same place. */
+jnx_status jnx_op_qk_norm_rope_append_paged(const jnx_qk_rope* p, const uint16_t* qkv,
+                                            int64_t ldqkv, const int32_t* pos, int32_t n_tokens,
+                                            const jnx_head_rows* q, const jnx_kv_cache* cache,
+                                            const jnx_pages* pages, const int32_t* seq,
+                                            const int32_t* at, int32_t* status, void* stream);
+
+/* out = softmax(q k^T / sqrt(head_dim)) v for every node of every sequence (n_rows rows of q
+ * and out hold them): node i of sequence s sees the n_cached[s] cached tokens and those nodes
+ * j of its sequence, at tokens n_cached[s] + j, whose bit j of sees[row] is set (its ancestors
+ * and itself, or any others).  A row that sees nothing has output 0, rows of no sequence stay
+ * as they were.  cu_nodes [n_seqs + 1], n_cached [n_seqs] and sees [n_rows] are on the device.
+ * A sequence whose rows are not among n_rows, or more than 64, is left out and reported; one
+ * whose tokens are more than its entries hold has output 0 and is reported; a page that is not
+ * there is read as zeros and reported.  A cache whose sequences have several pages has room a
+ * multiple of 16 (JNX_ERR_UNSUPPORTED otherwise).  The bits of a sequence do not depend on the
+ * others.  The workspace serves sequences of up to max_tokens tokens, nodes among them:
+ * max_pages * room of the call. */
+size_t jnx_op_tree_attention_workspace_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads,
+                                             int32_t head_dim, int64_t max_tokens);
+jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx_pages* pages,
+                                 int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t n_rows, const jnx_head_rows* q, const int32_t* cu_nodes,
+                                 const int32_t* n_cached, const uint64_t* sees,
+                                 const jnx_head_rows* out, void* workspace, size_t ws_bytes,
+                                 int32_t* status, void* stream);
+
+/* Verification of drafted trees by speculative sampling, so that the tokens are distributed
+ * as the target's own.  Row cu_nodes[s] + i of p [n_rows, vocab] fp32 (row stride ldp) holds
+ * the target's probabilities behind node i, of q (ldq) those that node i's children were
+ * drawn from, one by one and independently; q NULL: the children are certain guesses, each
+ * with probability one where it stands.  tokens and parent [n_rows]: a node's token and its
+ * parent's number in the sequence (the root's are not read); u [n_rows] in [0, 1).
+ * From the root on: the children of the node are tried in order.  With r = p and R = 1 at
+ * first, child c of token x is accepted if u[c] q(x) R < r(x), and the walk goes on at c; else
+ * r <- max(r - R q, 0) and R <- sum r.  Where no child is accepted, next[s] is the first word
+ * whose sum of r up to it is above u[root] sum r (r = p if nothing is left of it).
+ * path [n_seqs, max_nodes]: the root and the accepted nodes' numbers, then -1; n_kept[s] of
+ * them.  A sequence of no nodes has n_kept 0 and next -1.  Left out and reported: sequences
+ * whose rows are not among n_rows or more than max_nodes (as of no nodes), nodes whose parent
+ * is not ahead of them or whose token is no word (never accepted), sums that are not finite
+ * and positive (next -1). p and q are not negative; max_nodes in 1 to 64.  Sums are kept to
+ * 2^-44 of themselves or closer. */
+jnx_status jnx_op_verify_drafts(const float* p, int64_t ldp, const float* q, int64_t ldq,
+                                const int32_t* tokens, const int32_t* parent, const float* u,
+                                const int32_t* cu_nodes, int32_t n_seqs, int32_t n_rows,
+                                int32_t vocab, int32_t max_nodes, int32_t* path, int32_t* n_kept,
+                                int32_t* next, int32_t* status, void* stream);
+
+/* The accepted rows' keys and values to their places: token n_cached[s] + path[s * ld_path + k]
+ * goes to token n_cached[s] + k, for k < n_kept[s], in each of n_layers caches that are
+ * layer_stride elements apart.  A path increases and starts anywhere at or behind 0; n_kept up
+ * to max_kept <= 64 (path's columns).  A sequence with another path or whose places are not
+ * there is left as it was and reported.  No page serves two sequences of the call where rows
+ * are moved. */
+jnx_status jnx_op_keep_drafts(const jnx_kv_cache* cache, int32_t n_layers, int64_t layer_stride,
+                              const jnx_pages* pages, int32_t n_kv_heads, int32_t head_dim,
+                              const int32_t* n_cached, const int32_t* path, int64_t ld_path,
+                              const int32_t* n_kept, int32_t max_kept, int32_t* status,
+                              void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,7 @@ OBJ = os.path.join(ROOT, "_build", "obj")
 LIB = os.path.join(HERE, "libjnx.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["plan.cpp", "api.cu", "gemm.cu", "attn.cu", "norm.cu", "heads.cu", "trace.cu", "noalloc.cu", "lora.cu", "optim.cu", "bwd.cu", "attn_bwd.cu", "train.cu", "flow.cu", "diag.cu",
-           "rope.cu", "prompt_attn.cu", "prompt_attn_bwd.cu", "decode.cu", "vocab.cu"]
+           "rope.cu", "prompt_attn.cu", "prompt_attn_bwd.cu", "decode.cu", "vocab.cu", "tree.cu", "verify.cu"]
 
 
 def _nvcc() -> str:

@@ -21,6 +21,41 @@ inline bool cache_ok(const jnx_kv_cache* c) {
            c->head_stride % 8 == 0;
 }
 
+inline bool pages_ok(const jnx_pages* p) {
+    return p && p->n_seqs >= 0 && p->max_pages >= 0 &&
+           (p->n_seqs == 0 || p->max_pages == 0 || (p->table && p->ld >= 0));
+}
+
+// The page and row of a sequence's token; false: there is none.
+struct Pages {
+    const int* table;
+    long long ld;
+    int n_seqs, max_pages, n_pages, room;
+    Pages() = default;
+    Pages(const jnx_pages& p, const jnx_kv_cache& c)
+        : table(p.table), ld(p.ld), n_seqs(p.n_seqs), max_pages(p.max_pages), n_pages(c.n_slots),
+          room(c.room) {}
+    __device__ __forceinline__ bool find(int seq, int token, int& page, int& row) const {
+        if ((unsigned)seq >= (unsigned)n_seqs || token < 0 || room <= 0) return false;
+        const int entry = token / room;
+        row = token - entry * room;
+        if (entry >= max_pages) return false;
+        page = table[seq * ld + entry];
+        return (unsigned)page < (unsigned)n_pages;
+    }
+};
+
+constexpr int kMaxNodes = 64;  // of a sequence's tree
+
+// A sequence's rows [first, first + n) among the call's; false: it is left out.
+__device__ __forceinline__ bool tree_rows(const int* cu_nodes, int s, int n_rows, int most, int& first,
+                                          int& n) {
+    const int a = cu_nodes[s], b = cu_nodes[s + 1];
+    first = a;
+    n = b - a;
+    return 0 <= a && a <= b && b <= n_rows && n <= most;
+}
+
 inline jnx_status launched(const char* what) {
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? JNX_OK : fail(JNX_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));

@@ -49,8 +49,9 @@ struct Args {
     // append: the cache
     uint16_t* v;
     long long slot_stride;
-    const int *slot, *at;
+    const int *slot, *at;  // paged: slot is the sequence
     int n_slots, room;
+    Pages pages;
     int* status;
     // backward
     uint16_t* dqkv;
@@ -153,11 +154,15 @@ template <int HD>
 using Forward = Cfg<HD, 8, HD == 64 ? 16 : 8>;
 template <int HD>
 using Backward = Cfg<HD, 4, HD == 128 ? 8 : 16>;
+
+// Where keys go: rows of a tensor, rows of cache slots, or rows of the pages of sequences.
+enum { ROWS = 0, SLOTS = 1, PAGES = 2 };
 }  // namespace rope
 
-template <int HD, bool APPEND>
+template <int HD, int TO>
 __global__ void __launch_bounds__(rope::THREADS)
     k_qk_norm_rope(const __grid_constant__ rope::Args a) {
+    constexpr bool APPEND = TO != rope::ROWS;
     using C = rope::Forward<HD>;
     constexpr int E = C::E;
     __shared__ float4 cs[C::TOK * HD / 4];
@@ -229,8 +234,9 @@ __global__ void __launch_bounds__(rope::THREADS)
         if (is_q) {
             o = a.q + tok * a.q_row + hw * a.q_head;
         } else if (APPEND) {
-            const int slot = a.slot[tok], at = a.at[tok];
-            if (slot < 0 || slot >= a.n_slots || at < 0 || at >= a.room) {
+            int slot = a.slot[tok], at = a.at[tok];
+            if (TO == rope::PAGES ? !a.pages.find(slot, at, slot, at)
+                                  : slot < 0 || slot >= a.n_slots || at < 0 || at >= a.room) {
                 report(a.status, JNX_ERR_DEVICE_BOUNDS);
                 continue;
             }
@@ -429,22 +435,41 @@ static jnx_status rope_args(const jnx_qk_rope* p, const uint16_t* qkv, int64_t l
 // Tokens of a CTA: rows for four passes, fewer where that would leave SMs without a CTA.
 // (30,000 tokens of 9 heads of 256: 88 us with two tokens a CTA, a pass and an eighth, 63
 // with eight.)
-template <int HD, bool APPEND>
+template <int HD, int TO>
 static void launch_rope_hd(rope::Args a, cudaStream_t s) {
     using C = rope::Forward<HD>;
-    const int heads = a.H + (APPEND ? 2 : 1) * a.Hkv;
+    const int heads = a.H + (TO != rope::ROWS ? 2 : 1) * a.Hkv;
     a.tok = std::max(1, std::min({C::TOK, (4 * C::RPP + heads - 1) / heads, a.n_tokens / (152 * 6)}));
-    pdl(k_qk_norm_rope<HD, APPEND>, (a.n_tokens + a.tok - 1) / a.tok, rope::THREADS, 0, s)(a);
+    pdl(k_qk_norm_rope<HD, TO>, (a.n_tokens + a.tok - 1) / a.tok, rope::THREADS, 0, s)(a);
 }
 
-template <bool APPEND>
+template <int TO>
 static jnx_status launch_rope(const rope::Args& a, int hd, const char* what, cudaStream_t s) {
     if (!a.H && !a.Hkv) return JNX_OK;
     TraceScope ts(JNX_K_QK_ROPE, 0.0, s);
-    if (hd == 64) launch_rope_hd<64, APPEND>(a, s);
-    else if (hd == 128) launch_rope_hd<128, APPEND>(a, s);
-    else launch_rope_hd<256, APPEND>(a, s);
+    if (hd == 64) launch_rope_hd<64, TO>(a, s);
+    else if (hd == 128) launch_rope_hd<128, TO>(a, s);
+    else launch_rope_hd<256, TO>(a, s);
     return launched(what);
+}
+
+// Query rows and the cache that an append writes.
+static jnx_status rope_cache(rope::Args& a, const jnx_head_rows* q, const jnx_kv_cache* cache,
+                             const int32_t* slot, const int32_t* at, int32_t* status, const char* what) {
+    if ((a.H && !rows_ok(q)) || !cache_ok(cache) || !slot || !at)
+        return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned argument", what);
+    if (a.H) a.q = q->ptr, a.q_row = q->row_stride, a.q_head = q->head_stride;
+    a.k = cache->k;
+    a.v = cache->v;
+    a.k_row = cache->row_stride;
+    a.k_head = cache->head_stride;
+    a.slot_stride = cache->slot_stride;
+    a.n_slots = cache->n_slots;
+    a.room = cache->room;
+    a.slot = slot;
+    a.at = at;
+    a.status = status;
+    return JNX_OK;
 }
 
 // CTAs of the gradient kernel, at most what 152 SMs hold at once, shared out between query
@@ -477,7 +502,7 @@ extern "C" jnx_status jnx_op_qk_norm_rope(const jnx_qk_rope* p, const uint16_t* 
         return fail(JNX_ERR_INVALID_ARG, "qk norm rope: null or misaligned output rows");
     if (a.H) a.q = q->ptr, a.q_row = q->row_stride, a.q_head = q->head_stride;
     if (a.Hkv) a.k = k->ptr, a.k_row = k->row_stride, a.k_head = k->head_stride;
-    return launch_rope<false>(a, p->head_dim, "qk norm rope", static_cast<cudaStream_t>(stream));
+    return launch_rope<rope::ROWS>(a, p->head_dim, "qk norm rope", static_cast<cudaStream_t>(stream));
 }
 
 extern "C" jnx_status jnx_op_qk_norm_rope_append(const jnx_qk_rope* p, const uint16_t* qkv,
@@ -490,21 +515,24 @@ extern "C" jnx_status jnx_op_qk_norm_rope_append(const jnx_qk_rope* p, const uin
     rope::Args a{};
     if (jnx_status st = rope_args(p, qkv, ldqkv, pos, n_tokens, "qk norm rope append", a)) return st;
     if (n_tokens == 0) return JNX_OK;
-    if ((a.H && !rows_ok(q)) || !cache_ok(cache) || !slot || !at)
-        return fail(JNX_ERR_INVALID_ARG, "qk norm rope append: null or misaligned argument");
-    if (a.H) a.q = q->ptr, a.q_row = q->row_stride, a.q_head = q->head_stride;
-    a.k = cache->k;
-    a.v = cache->v;
-    a.k_row = cache->row_stride;
-    a.k_head = cache->head_stride;
-    a.slot_stride = cache->slot_stride;
-    a.n_slots = cache->n_slots;
-    a.room = cache->room;
-    a.slot = slot;
-    a.at = at;
-    a.status = status;
-    return launch_rope<true>(a, p->head_dim, "qk norm rope append",
-                             static_cast<cudaStream_t>(stream));
+    if (jnx_status st = rope_cache(a, q, cache, slot, at, status, "qk norm rope append")) return st;
+    return launch_rope<rope::SLOTS>(a, p->head_dim, "qk norm rope append",
+                                    static_cast<cudaStream_t>(stream));
+}
+
+extern "C" jnx_status jnx_op_qk_norm_rope_append_paged(
+    const jnx_qk_rope* p, const uint16_t* qkv, int64_t ldqkv, const int32_t* pos, int32_t n_tokens,
+    const jnx_head_rows* q, const jnx_kv_cache* cache, const jnx_pages* pages, const int32_t* seq,
+    const int32_t* at, int32_t* status, void* stream) {
+    clear_error();
+    const char* what = "qk norm rope append paged";
+    rope::Args a{};
+    if (jnx_status st = rope_args(p, qkv, ldqkv, pos, n_tokens, what, a)) return st;
+    if (n_tokens == 0) return JNX_OK;
+    if (jnx_status st = rope_cache(a, q, cache, seq, at, status, what)) return st;
+    if (!pages_ok(pages)) return fail(JNX_ERR_INVALID_ARG, "%s: bad pages", what);
+    a.pages = Pages(*pages, *cache);
+    return launch_rope<rope::PAGES>(a, p->head_dim, what, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t jnx_op_qk_norm_rope_backward_workspace_bytes(const jnx_qk_rope* p,

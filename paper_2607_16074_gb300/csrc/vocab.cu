@@ -1,6 +1,7 @@
 // Next-token losses over the vocabulary and their gradients: logits x = h w^T,
 // loss = logsumexp(x) - x_target, G = row_weight (softmax(x) - onehot),
-// dh = G w, dw = G^T h.
+// dh = G w, dw = G^T h.  And losses against a teacher's top logits: T over a row's entries in
+// place of the one-hot row, P = softmax(x / tau), G = row_weight / tau (P - T).
 //
 // The rows that count (target >= 0) are packed first: most rows of an observation are
 // image rows without a next token, and an ignored row's h may hold anything, which must
@@ -46,6 +47,8 @@ enum { LOGITS = 0, DH = 1, DW = 2 };
 inline int blocks(int v) { return (v + BLK - 1) / BLK; }
 inline int ld_g(int v) { return (v + 63) / 64 * 64; }
 inline int pad_rows(int n) { return (n + BM - 1) / BM * BM; }
+
+constexpr int TOP = 128;  // entries of a row's teacher, at most (places fit a byte)
 }  // namespace vocab
 
 struct VocabGemm {
@@ -58,7 +61,12 @@ struct VocabGemm {
     const int* targets;  // of the packed rows
     uint16_t* G;         // null: losses only
     float2* stats;       // [rows][blocks]: maximum, and sum without the target's term
-    float* at_target;
+    float* at_target;    // [rows]; of a teacher's entries [rows][top]
+    // a teacher: by row of the call, its entries' words in order, and where each block's start
+    const int* words;          // [n][top]
+    const uint8_t* starts;     // [n][blocks + 1]
+    int top;
+    float log2e;               // log2(e) / temperature
     // DH, DW
     const int* index;  // packed row -> row (null: the same)
     uint16_t* out;
@@ -133,7 +141,8 @@ __device__ __forceinline__ void vocab_each32(uint8_t* slot, int lane, const uint
     __syncwarp();
 }
 
-template <int MODE>
+// TEACHER: LOGITS with a teacher's entries as the targets.
+template <int MODE, bool TEACHER = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW, 1)
     k_vocab_gemm(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                  const __grid_constant__ VocabGemm p) {
@@ -311,10 +320,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
             const uint32_t tc = tmem_base + acc * BN + half * 128 + ((uint32_t)(q * 32) << 16);
             if constexpr (MODE == LOGITS) {
                 const int cols = min(BLK, N - col0);  // may be negative: nothing here
-                const int tg = row < M ? p.targets[p.r0 + row] - col0 : -1;
+                // a teacher's entries of these columns are places [tg, te) of its words
+                int tg, te = 0;
+                const int* words = nullptr;
+                uint32_t mine = 0;
+                if constexpr (TEACHER) {
+                    tg = 0;
+                    if (row < M && cols > 0) {
+                        const size_t src = p.index[p.r0 + row];
+                        const uint8_t* st = p.starts + src * ((N + BLK - 1) / BLK + 1) + col0 / BLK;
+                        tg = st[0], te = st[1];
+                        words = p.words + src * p.top;
+                        for (int k = tg; k < te; ++k) mine |= 1u << ((words[k] - col0) >> 5);
+                    }
+                } else {
+                    tg = row < M ? p.targets[p.r0 + row] - col0 : -1;
+                    mine = (unsigned)tg < (unsigned)BLK ? 1u << (tg >> 5) : 0u;
+                }
                 // the 32-column chunks that hold a target of the warp's rows
-                const uint32_t hit = __reduce_or_sync(
-                    0xffffffffu, (unsigned)tg < (unsigned)BLK ? 1u << (tg >> 5) : 0u);
+                const uint32_t hit = __reduce_or_sync(0xffffffffu, mine);
                 float m = -INFINITY, s = 0.f, at = 0.f;
 #pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
@@ -335,18 +359,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                     // loop below 208, with the sum over all terms 189: the logit was picked
                     // out by way of local memory)
                     if (hit >> c & 1) {
+                        if constexpr (TEACHER) {
+                            for (int col; tg < te && ((col = words[tg] - col0) >> 5) == c; ++tg) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (tg == c * 32 + e) {
-                                at = __uint_as_float(v[e]);
-                                v[e] = 0xff800000u;
+                                for (int e = 0; e < 32; ++e)
+                                    if (col == c * 32 + e) {
+                                        at = __uint_as_float(v[e]);
+                                        v[e] = 0xff800000u;
+                                    }
+                                p.at_target[(size_t)row * p.top + tg] = at;
                             }
+                            __syncwarp();
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (tg == c * 32 + e) {
+                                    at = __uint_as_float(v[e]);
+                                    v[e] = 0xff800000u;
+                                }
+                        }
                         tmem_st32(tc + c * 32, v);
                         tmem_st_wait();
                     }
                 }
-                constexpr float LOG2E = 1.4426950408889634f;
-                const float sub = m == -INFINITY ? 0.f : m * LOG2E;
+                const float LOG2E = TEACHER ? p.log2e : 1.4426950408889634f;
+                // (a teacher's loss is of all digits near zero: the difference first)
+                const float sub = m == -INFINITY ? 0.f : TEACHER ? m : m * LOG2E;
+                auto power = [&](uint32_t w) {
+                    const float x = __uint_as_float(w);
+                    return ex2_approx(TEACHER ? (x - sub) * LOG2E : fmaf(x, LOG2E, -sub));
+                };
                 uint16_t* g0 = p.G ? p.G + (size_t)row0 * ((N + 63) / 64 * 64) + col0 : nullptr;
 #pragma unroll 1
                 for (int c = 0; c < 2; ++c) {
@@ -360,8 +402,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             const int at_col = c * 64 + d * 32 + e;
-                            float x0 = ex2_approx(fmaf(__uint_as_float(v[e]), LOG2E, -sub));
-                            float x1 = ex2_approx(fmaf(__uint_as_float(v[e + 1]), LOG2E, -sub));
+                            float x0 = power(v[e]), x1 = power(v[e + 1]);
                             if (at_col >= cols) x0 = 0.f;
                             if (at_col + 1 >= cols) x1 = 0.f;
                             s += x0 + x1;
@@ -376,7 +417,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                 tc_fence_before();
                 if (row < M && cols > 0) {
                     p.stats[(size_t)row * ((N + BLK - 1) / BLK) + col0 / BLK] = make_float2(m, s);
-                    if (tg >= 0 && tg < cols) p.at_target[row] = at;
+                    if (!TEACHER && tg >= 0 && tg < cols) p.at_target[row] = at;
                 }
             } else if (MODE == DH && parts > 1) {
 #pragma unroll 1
@@ -619,6 +660,169 @@ __global__ void __launch_bounds__(256)
     }
 }
 
+// A row's teacher: the words of its entries in order, their probabilities and the logarithms of
+// these, and where each block's words start.  A warp a row; every entry counts those ahead of
+// it, top^2 comparisons in all.
+struct VocabTeacher {
+    const int* ids;
+    const float* logits;
+    int n, vocab, top;
+    float inv_tau;
+    int *words, *flag, *count;  // flag: 0 for a row that has entries, else -1
+    float *prob, *log_prob;
+    uint8_t* starts;
+    int* status;
+};
+__global__ void __launch_bounds__(128) k_vocab_teacher(const __grid_constant__ VocabTeacher a) {
+    using vocab::TOP;
+    __shared__ int id_s[4][TOP], word_s[4][TOP];
+    __shared__ float x_s[4][TOP];
+    pdl_entry();
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * 4 + w;
+    if (row >= a.n) return;
+    int* id = id_s[w];
+    float* x = x_s[w];
+    const size_t at = (size_t)row * a.top;
+    float top = -INFINITY;
+    for (int k = lane; k < a.top; k += 32) {
+        int v = a.ids[at + k];
+        const float l = a.logits[at + k];
+        if (v >= a.vocab) {
+            report(a.status, JNX_ERR_DEVICE_BOUNDS);
+            v = -1;
+        }
+        if (!(l > -INFINITY)) v = -1;
+        id[k] = v;
+        x[k] = l * a.inv_tau;
+        if (v >= 0) top = fmaxf(top, l * a.inv_tau);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float z = 0.f;
+    __syncwarp();
+    for (int k = lane; k < a.top; k += 32)
+        if (id[k] >= 0) z += expf(x[k] - top);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+    const float log_z = logf(z);
+    // an entry whose word was given before adds to that one
+    int count = 0;
+    for (int k = lane; k < a.top; k += 32) {
+        const int v = id[k];
+        int rank = 0, same = 0;
+        bool again = false;
+        float lp = x[k] - top - log_z, p = expf(lp), sum = p;
+        for (int j = 0; j < a.top; ++j) {
+            const int u = id[j];
+            if (u < 0 || j == k) continue;
+            if (u == v && j < k) again = true;
+            if (u == v && j > k) {
+                sum += expf(x[j] - top - log_z);
+                ++same;
+            }
+            if (u < v) {
+                bool first = true;  // counted once
+                for (int i = 0; i < j && first; ++i) first = id[i] != u;
+                rank += first;
+            }
+        }
+        if (v < 0 || again) continue;
+        ++count;
+        word_s[w][rank] = v;
+        a.words[at + rank] = v;
+        a.prob[at + rank] = same ? sum : p;
+        a.log_prob[at + rank] = same ? logf(sum) : lp;
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
+    __syncwarp();
+    const int nb = (a.vocab + vocab::BLK - 1) / vocab::BLK;
+    for (int b = lane; b <= nb; b += 32) {
+        int lo = 0, hi = count;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (word_s[w][mid] < b * vocab::BLK) lo = mid + 1;
+            else hi = mid;
+        }
+        a.starts[(size_t)row * (nb + 1) + b] = (uint8_t)lo;
+    }
+    if (lane == 0) {
+        a.count[row] = count;
+        a.flag[row] = count > 0 ? 0 : -1;
+    }
+}
+
+__device__ __forceinline__ float sum256(float v, float* red) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.f;
+    for (int w = 0; w < 8; ++w) v += red[w];
+    return v;
+}
+
+// k_vocab_rows with a teacher.  With d = log P - log T at an entry, the loss is the sum of
+// T (e^d - 1 - d) over the entries and of P over all other words: no term is negative, so
+// nothing cancels where the student is near the teacher.  (As sum T (log T - log P), each
+// rounded, a loss under 1e-6 was lost.)  A CTA a row; thread k has entry k.
+__global__ void __launch_bounds__(256)
+    k_vocab_rows_teacher(const float2* stats, const __grid_constant__ VocabGemm p,
+                         const int* count, const float* prob, const float* log_prob,
+                         const float* weight, float inv_tau, float* loss) {
+    __shared__ float red[8];
+    __shared__ int first_top;
+    pdl_entry();
+    const int r = blockIdx.x, t = threadIdx.x;
+    if (r >= vocab_rows(p)) return;
+    const int row = p.index[p.r0 + r], n = count[row];
+    const int nb = (p.vocab + vocab::BLK - 1) / vocab::BLK;
+    const float2* st = stats + (size_t)r * nb;
+    float m = -INFINITY, o = 0.f;
+    for (int b = t; b < nb; b += 256) m = fmaxf(m, st[b].x);
+#pragma unroll
+    for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+    if ((t & 31) == 0) red[t >> 5] = m;
+    if (t == 0) first_top = 256;
+    __syncthreads();
+    for (int w = 0; w < 8; ++w) m = fmaxf(m, red[w]);
+    for (int b = t; b < nb; b += 256) o += st[b].y * expf((st[b].x - m) * inv_tau);
+    o = sum256(o, red);
+    const size_t at = (size_t)row * p.top + t;
+    const float below = t < n ? (m - p.at_target[(size_t)r * p.top + t]) * inv_tau : 0.f;
+    const float e = t < n ? expf(-below) : 0.f;
+    // the maximum's own term is one: left out where an entry has it, so that a small rest
+    // keeps its digits
+    if (t < n && below == 0.f) atomicMin(&first_top, t);
+    __syncthreads();
+    const bool sure = first_top < 256;
+    const float rest = o + sum256(t == first_top ? 0.f : e, red);
+    const float z = sure ? 1.f + rest : rest, log_z = sure ? log1pf(rest) : logf(rest);
+    float g = 0.f, grad = 0.f;
+    if (t < n) {
+        const float T = prob[at], lt = log_prob[at], d = -below - log_z - lt;
+        const float P = e / z;
+        grad = d < 1.f ? T * expm1f(d) : P - T;
+        g = grad - T * d;
+    }
+    const float kl = sum256(g, red) + o / z;
+    if (t == 0) loss[row] = kl;
+    if (!p.G) return;
+    const float w = weight[row] * inv_tau, scale = w / z;
+    uint16_t* out = p.G + (size_t)r * ((p.vocab + 63) / 64 * 64);
+    for (int c = t * 8; c < p.vocab; c += 2048) {
+        const float f = scale * expf((st[c / vocab::BLK].x - m) * inv_tau);
+        const uint4 u = *reinterpret_cast<const uint4*>(out + c);
+        uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = cvt_bf2(f * __uint_as_float(v[i] << 16), f * __uint_as_float(v[i] & 0xffff0000u));
+        *reinterpret_cast<uint4*>(out + c) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    __syncthreads();
+    if (t < n) out[p.words[at]] = f2bf(w * grad);
+}
+
 // dh's rows from the parts' sums, in the parts' order.  A CTA a row.
 __global__ void __launch_bounds__(256)
     k_vocab_dh_sum(const __grid_constant__ VocabGemm p) {
@@ -641,19 +845,19 @@ __global__ void __launch_bounds__(256)
 // host side
 // ---------------------------------------------------------------------------
 
-template <int MODE>
+template <int MODE, bool TEACHER = false>
 static jnx_status vocab_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const VocabGemm& p,
                              const char* what, cudaStream_t s) {
     using namespace vocab;
     static std::atomic<uint64_t> attr{0};
-    if (set_smem_limit(reinterpret_cast<const void*>(k_vocab_gemm<MODE>), SMEM, attr) != cudaSuccess)
+    if (set_smem_limit(reinterpret_cast<const void*>(k_vocab_gemm<MODE, TEACHER>), SMEM, attr) != cudaSuccess)
         return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
     const long long m = MODE == DW ? p.vocab : p.rows_max, n = MODE == LOGITS ? p.vocab : p.d;
     const long long tiles =
         (m + BM - 1) / BM * ((n + BN - 1) / BN) * (MODE == DH ? p.split : 1);
     if (tiles > 0x7fff0000) return fail(JNX_ERR_UNSUPPORTED, "%s: too many tiles", what);
     const int grid = 2 * (int)std::min<long long>(tiles, num_sms() / 2);
-    pdl(k_vocab_gemm<MODE>, grid, 64 + 32 * EW, SMEM, s)(ta, tb, p);
+    pdl(k_vocab_gemm<MODE, TEACHER>, grid, 64 + 32 * EW, SMEM, s)(ta, tb, p);
     return launched(what);
 }
 
@@ -669,6 +873,29 @@ static jnx_status vocab_check(const void* h, int64_t ldh, const void* w, int64_t
     // (rows are counted in steps of 8,192 and padded by 256)
     if (vocab > 0x7fffff00 || n_rows > 0x7fffff00 - 8192 || d > 0x7fffff00)
         return fail(JNX_ERR_UNSUPPORTED, "%s: sizes", what);
+    return JNX_OK;
+}
+
+// The gradients' arguments; with no rows dw is set to zero here.
+static jnx_status vocab_grads(const float* row_weight, int n_rows, int vocab, int d,
+                              const uint16_t* dh, int64_t lddh, uint16_t* dw, int64_t lddw,
+                              const char* what, cudaStream_t s) {
+    if (n_rows > 0 && (!row_weight || !dh || !aligned16(dh) || lddh % 8 || lddh < d))
+        return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned gradients", what);
+    if (dw && (!aligned16(dw) || lddw % 8 || lddw < d))
+        return fail(JNX_ERR_INVALID_ARG, "%s: misaligned weight gradient", what);
+    if (n_rows == 0 && dw && cudaMemset2DAsync(dw, lddw * 2, 0, (size_t)d * 2, vocab, s) != cudaSuccess)
+        return launched(what);
+    return JNX_OK;
+}
+
+static jnx_status teacher_check(const int32_t* ids, const float* logits, int top, float temperature,
+                                int n_rows, const char* what) {
+    if (top < 1 || !(temperature > 0.f) || !(temperature < INFINITY) || !(1.f / temperature < INFINITY))
+        return fail(JNX_ERR_INVALID_ARG, "%s: %d entries, temperature %g", what, top, temperature);
+    if (top > vocab::TOP)
+        return fail(JNX_ERR_UNSUPPORTED, "%s: over %d entries a row", what, vocab::TOP);
+    if (n_rows > 0 && (!ids || !logits)) return fail(JNX_ERR_INVALID_ARG, "%s: null teacher", what);
     return JNX_OK;
 }
 
@@ -706,6 +933,10 @@ struct VocabWs {
     uint16_t* G;
     float* parts;
     float* acc;
+    // a teacher's rows
+    int *words, *flag, *entries;
+    float *prob, *log_prob;
+    uint8_t* starts;
     size_t bytes;
 };
 // Rows of dh's parts of a piece, and the most that pieces of up to so many rows have: fewer
@@ -721,7 +952,7 @@ static size_t vocab_parts_rows_upto(int piece, int vocab_size, int d) {
     return most;
 }
 static VocabWs vocab_ws(void* base, int n, int vocab_size, int d, int piece, bool train,
-                        size_t parts_rows) {
+                        size_t parts_rows, int top = 0) {
     using namespace vocab;
     VocabWs w{};
     uint8_t* at = static_cast<uint8_t*>(base);
@@ -738,7 +969,15 @@ static VocabWs vocab_ws(void* base, int n, int vocab_size, int d, int piece, boo
     w.place = reinterpret_cast<int*>(take((size_t)n * 4));
     w.h = reinterpret_cast<uint16_t*>(take(((size_t)n + PAD) * d * 2));
     w.stats = reinterpret_cast<float2*>(take(rows * blocks(vocab_size) * 8));
-    w.at_target = reinterpret_cast<float*>(take(rows * 4));
+    w.at_target = reinterpret_cast<float*>(take(rows * (top ? top : 1) * 4));
+    if (top) {
+        w.words = reinterpret_cast<int*>(take((size_t)n * top * 4));
+        w.flag = reinterpret_cast<int*>(take((size_t)n * 4));
+        w.entries = reinterpret_cast<int*>(take((size_t)n * 4));
+        w.prob = reinterpret_cast<float*>(take((size_t)n * top * 4));
+        w.log_prob = reinterpret_cast<float*>(take((size_t)n * top * 4));
+        w.starts = take((size_t)n * (blocks(vocab_size) + 1));
+    }
     if (train) {
         w.G = reinterpret_cast<uint16_t*>(take(rows * ld_g(vocab_size) * 2));
         w.parts = reinterpret_cast<float*>(take(parts_rows * d * 4));
@@ -752,18 +991,35 @@ static void* align256(void* p) {
     return reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(p) + 255) & ~(uintptr_t)255);
 }
 
+// What a call has in place of targets.
+struct TeacherSpec {
+    const int32_t* ids;
+    const float* logits;
+    int top;
+    float inv_tau;
+};
+
 static jnx_status vocab_run(const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw,
                             const int32_t* targets, const float* weight, int n, int vocab_size,
                             int d, int piece, float* loss, uint16_t* dh, int64_t lddh,
                             uint16_t* dw, int64_t lddw, void* workspace, size_t ws_bytes,
-                            int* status, const char* what, cudaStream_t s) {
+                            int* status, const char* what, cudaStream_t s,
+                            const TeacherSpec* teacher = nullptr) {
     using namespace vocab;
     const bool train = weight != nullptr;
     const VocabWs ws = vocab_ws(align256(workspace), n, vocab_size, d, piece, train,
-                                train ? vocab_parts_rows(piece, vocab_size, d) : 0);
+                                train ? vocab_parts_rows(piece, vocab_size, d) : 0,
+                                teacher ? teacher->top : 0);
     if (!workspace || ws_bytes < ws.bytes)
         return fail(JNX_ERR_WORKSPACE, "%s: workspace too small", what);
     TraceScope ts(JNX_K_VOCAB, 0.0, s);
+    if (teacher) {
+        const VocabTeacher t{teacher->ids, teacher->logits, n,       vocab_size, teacher->top,
+                             teacher->inv_tau, ws.words,    ws.flag, ws.entries, ws.prob,
+                             ws.log_prob,  ws.starts,       status};
+        pdl(k_vocab_teacher, (n + 3) / 4, 128, 0, s)(t);
+        targets = ws.flag;
+    }
     const VocabRows vr{targets, n, vocab_size, d, ws.count, ws.index, ws.packed, ws.place, status};
     if (n <= kCountRows) {
         pdl(k_vocab_gather<true>, n + PAD, 256, 0, s)(h, ldh, vr, ws.h, loss, dh, lddh);
@@ -796,8 +1052,18 @@ static jnx_status vocab_run(const uint16_t* h, int64_t ldh, const uint16_t* w, i
         CUtensorMap th, tg, tgmn, thmn;
         if (!make_tmap_bf16(&th, hp, map_rows, d, d, 128, 64))
             return fail(JNX_ERR_CUDA, "%s: tensor map encode failed", what);
-        if (jnx_status st = vocab_gemm<LOGITS>(th, tw, p, what, s)) return st;
-        pdl(k_vocab_rows, rows, 256, 0, s)(ws.stats, ws.at_target, p, weight, loss);
+        if (teacher) {
+            p.words = ws.words;
+            p.starts = ws.starts;
+            p.top = teacher->top;
+            p.log2e = 1.4426950408889634f * teacher->inv_tau;
+            if (jnx_status st = vocab_gemm<LOGITS, true>(th, tw, p, what, s)) return st;
+            pdl(k_vocab_rows_teacher, rows, 256, 0, s)(ws.stats, p, ws.entries, ws.prob, ws.log_prob,
+                                                       weight, teacher->inv_tau, loss);
+        } else {
+            if (jnx_status st = vocab_gemm<LOGITS>(th, tw, p, what, s)) return st;
+            pdl(k_vocab_rows, rows, 256, 0, s)(ws.stats, ws.at_target, p, weight, loss);
+        }
         if (jnx_status st = launched(what)) return st;
         if (!train) continue;
         const int gr = pad_rows(piece), gc = ld_g(vocab_size);
@@ -864,17 +1130,59 @@ extern "C" jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, co
     clear_error();
     const char* what = "vocab loss train";
     if (jnx_status st = vocab_check(h, ldh, w, ldw, targets, n_rows, vocab, d, loss, what)) return st;
-    if (n_rows > 0 && (!row_weight || !dh || !aligned16(dh) || lddh % 8 || lddh < d))
-        return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned gradients", what);
-    if (dw && (!aligned16(dw) || lddw % 8 || lddw < d))
-        return fail(JNX_ERR_INVALID_ARG, "%s: misaligned weight gradient", what);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (n_rows == 0) {
-        if (dw && cudaMemset2DAsync(dw, lddw * 2, 0, (size_t)d * 2, vocab, s) != cudaSuccess)
-            return launched(what);
-        return JNX_OK;
-    }
+    if (jnx_status st = vocab_grads(row_weight, n_rows, vocab, d, dh, lddh, dw, lddw, what, s)) return st;
+    if (n_rows == 0) return JNX_OK;
     return vocab_run(h, ldh, w, ldw, targets, row_weight, n_rows, vocab, d,
                      vocab_piece(n_rows, piece_rows), loss, dh, lddh, dw, lddw, workspace, ws_bytes,
                      status, what, s);
+}
+
+extern "C" size_t jnx_op_vocab_distill_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d,
+                                                       int32_t top) {
+    if (n_rows < 0 || vocab <= 0 || d <= 0 || top <= 0) return 0;
+    return vocab_ws(nullptr, n_rows, vocab, d, vocab_piece(n_rows, 0), false, 0, top).bytes;
+}
+
+extern "C" jnx_status jnx_op_vocab_distill(const uint16_t* h, int64_t ldh, const uint16_t* w,
+                                           int64_t ldw, const int32_t* ids, const float* teacher,
+                                           int32_t top, float temperature, int32_t n_rows,
+                                           int32_t vocab, int32_t d, float* loss, void* workspace,
+                                           size_t ws_bytes, int32_t* status, void* stream) {
+    clear_error();
+    const char* what = "vocab distill";
+    if (jnx_status st = vocab_check(h, ldh, w, ldw, ids, n_rows, vocab, d, loss, what)) return st;
+    if (jnx_status st = teacher_check(ids, teacher, top, temperature, n_rows, what)) return st;
+    if (n_rows == 0) return JNX_OK;
+    const TeacherSpec t{ids, teacher, top, 1.f / temperature};
+    return vocab_run(h, ldh, w, ldw, nullptr, nullptr, n_rows, vocab, d, vocab_piece(n_rows, 0), loss,
+                     nullptr, 0, nullptr, 0, workspace, ws_bytes, status, what,
+                     static_cast<cudaStream_t>(stream), &t);
+}
+
+extern "C" size_t jnx_op_vocab_distill_train_workspace_bytes(int32_t n_rows, int32_t vocab,
+                                                             int32_t d, int32_t top,
+                                                             int32_t piece_rows) {
+    if (n_rows < 0 || vocab <= 0 || d <= 0 || top <= 0) return 0;
+    const int piece = vocab_piece(n_rows, piece_rows);
+    return vocab_ws(nullptr, n_rows, vocab, d, piece, true, vocab_parts_rows_upto(piece, vocab, d),
+                    top).bytes;
+}
+
+extern "C" jnx_status jnx_op_vocab_distill_train(
+    const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw, const int32_t* ids,
+    const float* teacher, int32_t top, float temperature, const float* row_weight, int32_t n_rows,
+    int32_t vocab, int32_t d, int32_t piece_rows, float* loss, uint16_t* dh, int64_t lddh,
+    uint16_t* dw, int64_t lddw, void* workspace, size_t ws_bytes, int32_t* status, void* stream) {
+    clear_error();
+    const char* what = "vocab distill train";
+    if (jnx_status st = vocab_check(h, ldh, w, ldw, ids, n_rows, vocab, d, loss, what)) return st;
+    if (jnx_status st = teacher_check(ids, teacher, top, temperature, n_rows, what)) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (jnx_status st = vocab_grads(row_weight, n_rows, vocab, d, dh, lddh, dw, lddw, what, s)) return st;
+    if (n_rows == 0) return JNX_OK;
+    const TeacherSpec t{ids, teacher, top, 1.f / temperature};
+    return vocab_run(h, ldh, w, ldw, nullptr, row_weight, n_rows, vocab, d,
+                     vocab_piece(n_rows, piece_rows), loss, dh, lddh, dw, lddw, workspace, ws_bytes,
+                     status, what, s, &t);
 }

@@ -181,6 +181,11 @@ class jnx_kv_cache(C.Structure):
                 ("head_stride", C.c_int64)]
 
 
+class jnx_pages(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("ld", C.c_int64), ("n_seqs", C.c_int32),
+                ("max_pages", C.c_int32)]
+
+
 class jnx_prompt(C.Structure):
     _fields_ = [("n_seqs", C.c_int32)] + \
                [(n, C.c_void_p) for n in ("cu_q", "cu_kv", "prefix")] + \
@@ -213,7 +218,11 @@ EXPORTS = ("jnx_last_error", "jnx_version", "jnx_group_plan", "jnx_group_attn_it
            "jnx_op_prompt_attention_backward_workspace_bytes",
            "jnx_op_prompt_attention_backward", "jnx_op_decode_attention_workspace_bytes",
            "jnx_op_decode_attention", "jnx_op_vocab_loss_workspace_bytes", "jnx_op_vocab_loss",
-           "jnx_op_vocab_loss_train_workspace_bytes", "jnx_op_vocab_loss_train")
+           "jnx_op_vocab_loss_train_workspace_bytes", "jnx_op_vocab_loss_train",
+           "jnx_op_qk_norm_rope_append_paged", "jnx_op_tree_attention_workspace_bytes",
+           "jnx_op_tree_attention", "jnx_op_verify_drafts", "jnx_op_keep_drafts",
+           "jnx_op_vocab_distill_workspace_bytes", "jnx_op_vocab_distill",
+           "jnx_op_vocab_distill_train_workspace_bytes", "jnx_op_vocab_distill_train")
 
 
 def lib() -> C.CDLL:
@@ -226,8 +235,8 @@ def lib() -> C.CDLL:
                            "`python -m paper_2607_16074_gb300.build`")
     L = C.CDLL(LIB_PATH)
     vp, i32, i64, sz, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
-    qkr, rows, cache, prompt = (C.POINTER(x) for x in (jnx_qk_rope, jnx_head_rows, jnx_kv_cache,
-                                                       jnx_prompt))
+    qkr, rows, cache, prompt, pages = (C.POINTER(x) for x in (
+        jnx_qk_rope, jnx_head_rows, jnx_kv_cache, jnx_prompt, jnx_pages))
     sig = {
         "jnx_last_error": (C.c_char_p, []),
         "jnx_version": (i32, []),
@@ -319,6 +328,21 @@ def lib() -> C.CDLL:
         "jnx_op_vocab_loss_train_workspace_bytes": (sz, [i32, i32, i32, i32]),
         "jnx_op_vocab_loss_train": (i32, [vp, i64, vp, i64, vp, vp, i32, i32, i32, i32, vp, vp,
                                           i64, vp, i64, vp, sz, vp, vp]),
+        "jnx_op_vocab_distill_workspace_bytes": (sz, [i32, i32, i32, i32]),
+        "jnx_op_vocab_distill": (i32, [vp, i64, vp, i64, vp, vp, i32, f32, i32, i32, i32, vp, vp,
+                                       sz, vp, vp]),
+        "jnx_op_vocab_distill_train_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
+        "jnx_op_vocab_distill_train": (i32, [vp, i64, vp, i64, vp, vp, i32, f32, vp, i32, i32, i32,
+                                             i32, vp, vp, i64, vp, i64, vp, sz, vp, vp]),
+        "jnx_op_qk_norm_rope_append_paged": (i32, [qkr, vp, i64, vp, i32, rows, cache, pages, vp,
+                                                   vp, vp, vp]),
+        "jnx_op_tree_attention_workspace_bytes": (sz, [i32, i32, i32, i32, i64]),
+        "jnx_op_tree_attention": (i32, [cache, pages, i32, i32, i32, i32, rows, vp, vp, vp, rows,
+                                        vp, sz, vp, vp]),
+        "jnx_op_verify_drafts": (i32, [vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, i32, vp,
+                                       vp, vp, vp, vp]),
+        "jnx_op_keep_drafts": (i32, [cache, i32, i64, pages, i32, i32, vp, vp, i64, vp, i32, vp,
+                                     vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -449,7 +473,8 @@ KERNEL_NAMES = {1: "pack", 2: "rmsnorm", 3: "gemm_qkv_rope", 4: "attention", 5: 
                 14: "heads_adamw", 15: "gemm_bwd", 16: "attention_bwd", 17: "norm_bwd",
                 18: "lora_bwd", 19: "flow_gemm", 20: "flow_attention", 21: "flow_misc",
                 22: "flow_wgrad", 23: "qk_norm_rope", 24: "prompt_attention",
-                25: "prompt_attention_bwd", 26: "decode_attention", 27: "vocab_loss"}
+                25: "prompt_attention_bwd", 26: "decode_attention", 27: "vocab_loss",
+                28: "tree_attention", 29: "verify_drafts"}
 TENSOR_KERNELS = (3, 4, 5, 6, 7, 12, 13, 15, 16, 18, 19, 20, 22)
 
 

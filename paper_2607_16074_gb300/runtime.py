@@ -597,9 +597,20 @@ def _cache(k: torch.Tensor, v: torch.Tensor, heads):
     return k.data_ptr(), v.data_ptr(), shape[0], shape[1], s[0], s[1], s[2]
 
 
+def _pages(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, seqs: int, heads):
+    """Pages [pages, tokens, kv heads, head_dim] and the table [seqs, entries] of the sequences
+    that lie in them: jnx_kv_cache's fields, then jnx_pages'."""
+    if table.dtype is not _I32 or table.dim() != 2 or table.shape[0] != seqs or not table.is_cuda or \
+            (table.stride(1) != 1 and table.shape[1] > 1):
+        _refuse(table, _I32, (seqs, "entries"))
+    n = table.shape[1]
+    return *_cache(k, v, heads), table.data_ptr(), table.stride(0), seqs, n
+
+
 class _Views:
     """The structs that a call's tensors are described in, filled in one go: making one of
     each for every call took as long as the rest of a short call."""
+    FORMS = {J.jnx_head_rows: "Qqq", J.jnx_kv_cache: "QQiiqqq", J.jnx_pages: "Qqii"}
 
     def __init__(self, *kinds):
         self._mem = C.create_string_buffer(sum(C.sizeof(k) for k in kinds))
@@ -607,7 +618,7 @@ class _Views:
         for k in kinds:
             self.refs.append(C.cast(at, C.POINTER(k)))
             at += C.sizeof(k)
-            form += "Qqq" if k is J.jnx_head_rows else "QQiiqqq"
+            form += self.FORMS[k]
         self.fill = functools.partial(struct.Struct(form).pack_into, self._mem, 0)
 
 
@@ -682,6 +693,7 @@ class QKNormRope(_TextOperator):
 
         rows, cache = J.jnx_head_rows, J.jnx_kv_cache
         self._qk, self._qc = _Views(rows, rows), _Views(rows, cache)
+        self._qp = _Views(rows, cache, J.jnx_pages)
 
     def _args(self, qkv: torch.Tensor, pos: torch.Tensor):
         h, hkv, hd = self.dims
@@ -708,6 +720,20 @@ class QKNormRope(_TextOperator):
         J.check(self._lib.jnx_op_qk_norm_rope_append(
             self._ref, x, ld, p, n, *self._qc.refs, _dense(slot, _I32, n),
             _dense(at, _I32, n), self._status, self._on(stream)))
+
+    def append_paged(self, qkv: torch.Tensor, pos: torch.Tensor, q: torch.Tensor,
+                     k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor,
+                     seq: torch.Tensor, at: torch.Tensor, stream=None) -> None:
+        """q as forward; key and value rows go to token at[i] of sequence seq[i], whose tokens
+        lie in the pages [pages, tokens, Hkv, hd] that its row of table [sequences, entries]
+        names."""
+        h, hkv, hd = self.dims
+        n, x, ld, p = self._args(qkv, pos)
+        r = self._qp.refs
+        self._qp.fill(*_view(q, (n, h, hd)), *_pages(k_pages, v_pages, table, table.shape[0], (hkv, hd)))
+        J.check(self._lib.jnx_op_qk_norm_rope_append_paged(
+            self._ref, x, ld, p, n, *r, _dense(seq, _I32, n), _dense(at, _I32, n), self._status,
+            self._on(stream)))
 
     def backward(self, qkv: torch.Tensor, pos: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
                  dqkv: torch.Tensor, dgamma_q: Optional[torch.Tensor] = None,
@@ -876,3 +902,159 @@ class VocabLoss(_TextOperator):
             *args, _dense(row_weight, _F32, n), n, self.vocab, self.d, self.piece_rows,
             _dense(loss, _F32, n), *grads, self._ws, self._nws, self._status,
             self._on(stream)))
+
+
+class VocabDistill(_TextOperator):
+    """Losses of hidden rows over a vocabulary w [vocab, d] against a teacher's top logits, and
+    their gradients: T = softmax(teacher / temperature) over a row's entries, P = softmax(h w^T /
+    temperature), loss = sum T (log T - log P)."""
+
+    def __init__(self, w: torch.Tensor, max_rows: int, top: int, temperature: float = 1.0,
+                 gradients: bool = True, piece_rows: int = 0):
+        self.w, (self.vocab, self.d) = _bf16(w, *w.shape), w.shape
+        self.max_rows, self.top, self.temperature = max_rows, top, temperature
+        self.piece_rows, self.gradients = piece_rows, gradients
+        L = J.lib()
+        need = L.jnx_op_vocab_distill_workspace_bytes(max_rows, self.vocab, self.d, top)
+        if gradients:
+            need = max(need, L.jnx_op_vocab_distill_train_workspace_bytes(
+                max_rows, self.vocab, self.d, top, piece_rows))
+        super().__init__(need, w.device)
+
+    def _args(self, h: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor):
+        n = h.shape[0]
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, at most {self.max_rows}")
+        _bf16(h, n, self.d)
+        return n, h.data_ptr(), h.stride(0), self.w.data_ptr(), self.w.stride(0), \
+            _dense(ids, _I32, n, self.top), _dense(teacher, _F32, n, self.top), self.top, \
+            self.temperature
+
+    def loss(self, h: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, loss: torch.Tensor,
+             stream=None) -> None:
+        """loss [n] fp32 of h [n, d] against the words ids [n, top] with the teacher's logits
+        [n, top]; a negative id is no entry, a row without entries has loss 0."""
+        n, *args = self._args(h, ids, teacher)
+        J.check(self._lib.jnx_op_vocab_distill(
+            *args, n, self.vocab, self.d, _dense(loss, _F32, n), self._ws, self._nws,
+            self._status, self._on(stream)))
+
+    def train(self, h: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
+              row_weight: torch.Tensor, loss: torch.Tensor, dh: torch.Tensor,
+              dw: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Also the gradients of sum(row_weight * loss): dh [n, d] and dw [vocab, d] (None:
+        a frozen vocabulary), bf16."""
+        if not self.gradients:
+            raise ValueError("made for losses only (gradients=False)")
+        n, *args = self._args(h, ids, teacher)
+        _bf16(dh, n, self.d)
+        grads = [dh.data_ptr(), dh.stride(0), None, 0]
+        if dw is not None:
+            _bf16(dw, self.vocab, self.d)
+            grads[2:] = [dw.data_ptr(), dw.stride(0)]
+        J.check(self._lib.jnx_op_vocab_distill_train(
+            *args, _dense(row_weight, _F32, n), n, self.vocab, self.d, self.piece_rows,
+            _dense(loss, _F32, n), *grads, self._ws, self._nws, self._status,
+            self._on(stream)))
+
+
+# ---- answering with drafted tokens ----
+
+class TreeAttention(_TextOperator):
+    """Attention of trees of drafted tokens, one of up to 64 nodes for each live sequence,
+    over its pages: max_rows nodes in all, max_tokens tokens (nodes among them) of a sequence
+    at most."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, max_batch: int,
+                 max_rows: int, max_tokens: int, device="cuda"):
+        self.dims = (n_heads, n_kv_heads, head_dim)
+        self.max_batch, self.max_rows, self.max_tokens = max_batch, max_rows, max_tokens
+        super().__init__(J.lib().jnx_op_tree_attention_workspace_bytes(
+            max_batch, max_rows, n_heads, head_dim, max_tokens), device)
+        self._views = _Views(J.jnx_kv_cache, J.jnx_pages, J.jnx_head_rows, J.jnx_head_rows)
+
+    def forward(self, q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                table: torch.Tensor, cu_nodes: torch.Tensor, n_cached: torch.Tensor,
+                sees: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+        """out [n, H, hd] of q [n, H, hd]: rows [cu_nodes[s], cu_nodes[s + 1]) are sequence s's
+        nodes, whose keys and values lie behind its first n_cached[s] tokens; a row sees these
+        tokens and the nodes whose bits are set in sees [n] int64."""
+        h, hkv, hd = self.dims
+        n, b = q.shape[0], n_cached.shape[0]
+        if b > self.max_batch or n > self.max_rows:
+            raise ValueError(f"{n} nodes of {b} sequences, at most {self.max_rows} of {self.max_batch}")
+        rows, r = (n, h, hd), self._views.refs
+        if table.shape[-1] * k_pages.shape[1] > self.max_tokens:
+            raise ValueError(f"a table for {table.shape[-1] * k_pages.shape[1]} tokens, "
+                             f"at most {self.max_tokens}")
+        self._views.fill(*_pages(k_pages, v_pages, table, b, (hkv, hd)), *_view(q, rows),
+                         *_view(out, rows))
+        J.check(self._lib.jnx_op_tree_attention(
+            r[0], r[1], h, hkv, hd, n, r[2], _dense(cu_nodes, _I32, b + 1),
+            _dense(n_cached, _I32, b), _dense(sees, torch.int64, n), r[3], self._ws, self._nws,
+            self._status, self._on(stream)))
+
+
+def _probabilities(t: torch.Tensor, rows: int, vocab: int):
+    if t.dtype is not _F32 or t.shape != (rows, vocab) or not t.is_cuda or \
+            (t.stride(1) != 1 and vocab > 1):
+        _refuse(t, _F32, (rows, vocab))
+    return t.data_ptr(), t.stride(0)
+
+
+class VerifyDrafts(_TextOperator):
+    """Drafted tokens verified against the target's probabilities by speculative sampling."""
+
+    def __init__(self, vocab: int, device="cuda"):
+        self.vocab = vocab
+        super().__init__(0, device)
+
+    def forward(self, p: torch.Tensor, q: Optional[torch.Tensor], tokens: torch.Tensor,
+                parent: torch.Tensor, cu_nodes: torch.Tensor, u: torch.Tensor,
+                path: torch.Tensor, n_kept: torch.Tensor, next: torch.Tensor,
+                stream=None) -> None:
+        """path [b, nodes], n_kept [b] and next [b] of the trees in rows [cu_nodes[s],
+        cu_nodes[s + 1]) of tokens, parent, u and of the probabilities p and q [n, vocab] fp32 (q
+        None: certain guesses).  A root's u draws the next token.  With no drafts, a root alone,
+        next is a token drawn from p."""
+        n, b = tokens.shape[0], n_kept.shape[0]
+        J.check(self._lib.jnx_op_verify_drafts(
+            *_probabilities(p, n, self.vocab),
+            *((None, 0) if q is None else _probabilities(q, n, self.vocab)),
+            _dense(tokens, _I32, n), _dense(parent, _I32, n), _dense(u, _F32, n),
+            _dense(cu_nodes, _I32, b + 1), b, n, self.vocab, path.shape[1],
+            _dense(path, _I32, b, path.shape[1]), _dense(n_kept, _I32, b), _dense(next, _I32, b),
+            self._status, self._on(stream)))
+
+
+class KeepDrafts(_TextOperator):
+    """The accepted drafts' keys and values to the places behind the cached tokens."""
+
+    def __init__(self, n_kv_heads: int, head_dim: int, device="cuda"):
+        self.dims = (n_kv_heads, head_dim)
+        super().__init__(0, device)
+        self._views = _Views(J.jnx_kv_cache, J.jnx_pages)
+
+    def forward(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor,
+                n_cached: torch.Tensor, path: torch.Tensor, n_kept: torch.Tensor,
+                stream=None) -> None:
+        """Token n_cached[s] + path[s, k] of every sequence to token n_cached[s] + k, for k <
+        n_kept[s], in the pages [pages, tokens, Hkv, hd], or those of all layers
+        [layers, pages, tokens, Hkv, hd]."""
+        b, layers, step = n_cached.shape[0], 1, 0
+        if k_pages.dim() == 5:
+            layers, step = k_pages.shape[0], k_pages.stride(0) if k_pages.shape[0] > 1 else 0
+            if v_pages.shape != k_pages.shape or (layers > 1 and v_pages.stride(0) != step):
+                raise ValueError("caches of different layers")
+            if layers == 0:
+                return
+            k_pages, v_pages = k_pages[0], v_pages[0]
+        self._views.fill(*_pages(k_pages, v_pages, table, b, self.dims))
+        r = self._views.refs
+        if path.dim() != 2 or path.dtype is not _I32 or path.shape[0] != b or not path.is_cuda or \
+                (path.stride(1) != 1 and path.shape[1] > 1):
+            _refuse(path, _I32, (b, "nodes"))
+        J.check(self._lib.jnx_op_keep_drafts(
+            r[0], layers, step, r[1], *self.dims, _dense(n_cached, _I32, b), path.data_ptr(),
+            path.stride(0), _dense(n_kept, _I32, b), path.shape[1],
+            self._status, self._on(stream)))
