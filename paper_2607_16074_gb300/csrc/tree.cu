@@ -2,7 +2,25 @@
 //
 // Node i of a sequence sees the cached tokens and the nodes that its bits name, whose keys
 // and values lie behind the cached ones: O = softmax(Q K^T / sqrt(hd)) V over them, in one
-// pass with a running maximum and sum.
+// pass with a running maximum m and sum l.  P = 2^(S c - m), O <- O 2^(m_old - m) + P V; m
+// moves only when a tile's maximum is over 2^8 times the old one, which O / l does not show.
+//
+// Bound by reading the cache once.  A 128-row tile holds (node, query head of one group)
+// pairs, up to 128 / group nodes, so a key head's tokens are read once for all of them, and
+// at 48 rows or 128 the products are past what mma.sync could do at the cache's rate.  A unit
+// is such a tile over a run of its sequence's tokens.  Persistent CTAs take units in turn,
+// two to an SM (one at head dim 256, whose O leaves no TMEM for a second): while one's
+// softmax works, the other's keys come in.  Roles of a CTA:
+//   warp 0      TMA: Q, then K and V tiles of 64 tokens, 16 to 64 to a box by what divides a
+//               page, into a ring each; the table's entries are looked up ahead
+//   warp 1      MMA issuer: S two key tiles ahead of P V
+//   warps 2-5   softmax and epilogue, a thread a row
+// P (bf16) overwrites its scores and is the TMEM A operand of the P V product.
+//
+// The run's length depends on the sequence alone, so a sequence's bits do not depend on the
+// others; its runs' sums are joined in their order by a second kernel.
+#include <algorithm>
+
 #include "jnx_dev.cuh"
 #include "jnx_kernels.h"
 #include "jnx_text.h"
@@ -10,69 +28,645 @@
 
 namespace jnx {
 
+namespace tree {
+constexpr int KT = 64;         // tokens of a tile
+constexpr int RING = 2;        // tiles of either ring
+constexpr int BATCH = 256;     // sequences of one launch
+constexpr int MAX_RUNS = 64;   // of a sequence
+constexpr int THREADS = 192;
+constexpr int STAGE = 2048;    // epilogue staging of a softmax warp
+constexpr float kLazy = 8.0f;  // log2 growth of the maximum that moves it
+enum { K_FULL = 0, K_EMPTY = K_FULL + RING, V_FULL = K_EMPTY + RING, V_EMPTY = V_FULL + RING,
+       Q_FULL = V_EMPTY + RING, Q_EMPTY, S_FULL, P_FULL = S_FULL + 2, PV_DONE = P_FULL + 2,
+       O_FULL = PV_DONE + 2, O_FREE, DRAIN, N_BARS };
+
+__host__ __device__ inline int round_up(int n, int to) { return (n + to - 1) / to * to; }
+
+// Tokens of a run of L, for `rows` rows of a tile and `units` units of a run: a run's sums are
+// rows / tokens of what it reads, which is kept under a sixteenth, an eighth or so of short
+// sequences; a sequence that fills the card by itself has whole rounds of units.
+__host__ __device__ inline int run_tokens(int L, int rows, int units, int slots) {
+    int least = (L <= 2048 ? 4 : 16) * rows;
+    least = round_up(least < 128 ? 128 : least, KT);
+    int n = (L + least - 1) / least;
+    if (n > MAX_RUNS) n = MAX_RUNS;
+    if ((long long)n * units > slots) n = (int)((long long)n * units / slots * slots / units);
+    if (n < 1) n = 1;
+    return round_up((L + n - 1) / n, KT);
+}
+// More runs than any sequence of up to max_tokens has.
+inline long long most_runs(long long max_tokens) {
+    return std::max(1ll, std::min<long long>(MAX_RUNS, (max_tokens + 127) / 128));
+}
+}  // namespace tree
+
+template <int HD>
+struct TreeCfg {
+    static constexpr int NCH = HD / 64;                  // 64-column chunks of a row
+    static constexpr int CTAS = HD == 256 ? 1 : 2;       // of an SM
+    static constexpr int SLOTS = 152 * CTAS;
+    static constexpr int TILE = tree::KT * HD * 2;
+    static constexpr int QB = 128 * HD * 2;
+    static constexpr int OFF_K = QB, OFF_V = OFF_K + tree::RING * TILE;
+    static constexpr int OFF_STG = OFF_V + tree::RING * TILE;
+    static constexpr int OFF_SEQ = OFF_STG + 4 * tree::STAGE;
+    static constexpr int OFF_BAR = OFF_SEQ + (5 * tree::BATCH + 4) * 4;
+    static constexpr int SMEM = OFF_BAR + tree::N_BARS * 8 + 16 + 1024;
+    static_assert(SMEM <= (CTAS == 2 ? 113 : 226) * 1024, "shared memory per CTA");
+    static constexpr uint32_t COLS = HD == 256 ? 512 : 256, O_COL = HD == 256 ? 256 : 128;
+};
+
 struct TreeArgs {
-    const uint16_t *k, *v;
-    long long page_stride, kv_row, kv_head;
     Pages pages;
-    int H, Hkv, group, n_rows;
+    int n_seqs, s0;  // sequences of the launch, the first of them
+    int H, Hkv, group, n_rows, box;
     float scale_log2;
-    const uint16_t* q;
-    long long q_row, q_head;
     uint16_t* out;
     long long o_row, o_head;
     const int *cu_nodes, *n_cached;
     const unsigned long long* sees;
+    int* base;    // [n_seqs]: a sequence's first (run, node) among the sums
+    float* part;  // [run, node][H][hd]: sums
+    float2* ml;   // [run, node][H]: maxima and sums of exponentials
     int* status;
 };
 
-// A warp a node and head, a token at a time.
+// A sequence's nodes, cached tokens and runs.
+struct TreeSeq {
+    int row0, n, old, L, run, runs, tiles;
+};
 template <int HD>
-__global__ void __launch_bounds__(128) k_tree_attn(const __grid_constant__ TreeArgs a) {
+__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& a, int row0, int n, int old) {
+    TreeSeq x{row0, n, old, 0, tree::KT, 1, 0};
+    const int T = tile_tokens(a.group);
+    x.tiles = (n + T - 1) / T;
+    if (n > 0 && old >= 0) {  // else no token is seen
+        x.L = old + n;
+        x.run = tree::run_tokens(x.L, min(n, T) * a.group, a.Hkv * x.tiles, TreeCfg<HD>::SLOTS);
+        x.runs = (x.L + x.run - 1) / x.run;
+    }
+    return x;
+}
+
+// Rows [i0, ...) of a sequence for one key head, over its tokens [at, end).
+struct TreeUnit {
+    int s, i0, kvh, run, at, end;
+    TreeSeq q;
+    __device__ __forceinline__ int tiles() const { return (end - at + tree::KT - 1) / tree::KT; }
+};
+
+// A sequence's nodes and cached tokens as they count: false is reported; old < 0: none is seen.
+__device__ __forceinline__ bool tree_lengths(const TreeArgs& a, int s, int& row0, int& n, int& old) {
+    old = -1;
+    if (!tree_rows(a.cu_nodes, a.s0 + s, a.n_rows, kMaxNodes, row0, n)) {
+        n = 0;
+        return false;
+    }
+    if (n == 0) return true;
+    const int c = a.n_cached[a.s0 + s];
+    if (c < 0 || (long long)c + n > (long long)a.pages.max_pages * a.pages.room) return false;
+    old = c;
+    return true;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
+    k_tree_attn(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+                const __grid_constant__ CUtensorMap tv, const __grid_constant__ TreeArgs a) {
+    using C = TreeCfg<HD>;
+    using namespace tree;
+    constexpr int NCH = C::NCH;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    int* first = reinterpret_cast<int*>(sm + C::OFF_SEQ);  // [n_seqs + 1]: first unit of each
+    int *rows0 = first + BATCH + 1, *nodes = rows0 + BATCH, *olds = nodes + BATCH, *base = olds + BATCH;
+    uint64_t* bar = reinterpret_cast<uint64_t*>(sm + C::OFF_BAR);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + N_BARS);
+    volatile int* fail_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int T = tile_tokens(a.group);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < N_BARS; ++i)
+            mbar_init(&bar[i], (i >= P_FULL && i < PV_DONE) || i == O_FREE ? 128 : 1);
+        *fail_flag = 0;
+        fence_barrier_init();
+        fence_proxy_async();
+    }
+    pdl_entry();  // TMEM is taken once the grid ahead has given its own back
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, C::COLS);
+        tmem_relinquish();
+    }
+    for (int s = threadIdx.x; s < a.n_seqs; s += THREADS) {
+        int row0, n, old;
+        if (!tree_lengths(a, s, row0, n, old) && blockIdx.x == 0) report(a.status, JNX_ERR_DEVICE_BOUNDS);
+        rows0[s] = row0, nodes[s] = n, olds[s] = old;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) {  // units and sums ahead of each sequence
+        int units = 0, sums = 0;
+        for (int b = 0; b < a.n_seqs; b += 32) {
+            const int s = b + lane;
+            int u = 0, v = 0;
+            if (s < a.n_seqs) {
+                const TreeSeq x = tree_seq<HD>(a, rows0[s], nodes[s], olds[s]);
+                u = x.runs * a.Hkv * x.tiles;
+                v = x.runs > 1 ? x.runs * x.n : 0;
+            }
+            int ru = u, rv = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, ru, o), z = __shfl_up_sync(0xffffffffu, rv, o);
+                if (lane >= o) ru += y, rv += z;
+            }
+            if (s < a.n_seqs) {
+                first[s] = units + ru - u;
+                base[s] = sums + rv - v;
+                if (blockIdx.x == 0) a.base[s] = sums + rv - v;
+            }
+            units += __shfl_sync(0xffffffffu, ru, 31);
+            sums += __shfl_sync(0xffffffffu, rv, 31);
+        }
+        if (lane == 0) first[a.n_seqs] = units;
+    }
+    __syncthreads();
+    const uint32_t tbase = warp_uniform(*tmem_slot);
+    const int n_units = warp_uniform(first[a.n_seqs]);
+
+    auto open = [&](int u) {
+        TreeUnit x{};
+        if (u >= n_units) return x;
+        int lo = 0, hi = a.n_seqs - 1;  // the last s with first[s] <= u
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= u) lo = mid;
+            else hi = mid - 1;
+        }
+        x.s = lo;
+        x.q = tree_seq<HD>(a, rows0[lo], nodes[lo], olds[lo]);
+        int rest = u - first[lo];  // a run's tiles lie together, then its heads
+        x.i0 = rest % x.q.tiles * T;
+        rest /= x.q.tiles;
+        x.kvh = rest % a.Hkv;
+        x.run = rest / a.Hkv;
+        x.at = x.run * x.q.run;
+        x.end = min(x.q.L, x.at + x.q.run);
+        return x;
+    };
+
+    if (warp == 0) {
+        // ---------------- TMA producer ----------------
+        if (elect_one()) {
+            tma_prefetch_desc(&tq);
+            tma_prefetch_desc(&tk);
+            tma_prefetch_desc(&tv);
+        }
+        bool ok = true;
+        uint32_t kt = 0, nq = 0;  // tiles and Q tiles loaded
+        const int qbytes = a.group * T * HD * 2, boxes = KT / a.box;
+        // pages of the boxes [32 c, 32 c + 32) of a unit, one a lane
+        auto look = [&](const TreeUnit& x, int c) {
+            int page = a.pages.n_pages, row = 0;  // no page: read as zeros
+            const long long token = x.at + (long long)(c * 32 + lane) * a.box;
+            if (token < x.end && !a.pages.find(a.s0 + x.s, (int)token, page, row)) {
+                page = a.pages.n_pages;
+                report(a.status, JNX_ERR_DEVICE_BOUNDS);
+            }
+            return page;
+        };
+        TreeUnit x = open(blockIdx.x);
+        int pages = look(x, 0);
+        for (int u = blockIdx.x; ok && u < n_units && !__any_sync(0xffffffffu, *fail_flag); u += gridDim.x) {
+            const int n = warp_uniform(x.tiles());
+            const TreeUnit next = open(u + gridDim.x);
+            const int next_pages = look(next, 0);
+            int more = look(x, 1);
+            if (n > 0) {
+                if (nq > 0 && !(ok = mbar_wait_warp(&bar[Q_EMPTY], (nq - 1) & 1))) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar[Q_FULL], qbytes);
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c)
+                        tma_load_3d(sm + c * 128 * 128, &tq, c * 64, x.kvh * a.group, x.q.row0 + x.i0,
+                                    &bar[Q_FULL]);
+                }
+                __syncwarp();
+                ++nq;
+            }
+            for (int t = 0; t < n && ok; ++t, ++kt) {
+                const int b0 = t * boxes;  // first box of the tile
+                if (t > 0 && b0 % 32 == 0) {
+                    pages = more;
+                    more = look(x, b0 / 32 + 1);
+                }
+                const int s = kt % RING, token = warp_uniform(x.at) + t * KT;
+                const int nb = min(boxes, (warp_uniform(x.end) - token + a.box - 1) / a.box);
+                const int row = token % a.pages.room;  // a box lies in one page
+                for (int v = 0; v < 2 && ok; ++v) {
+                    uint64_t* full = &bar[(v ? V_FULL : K_FULL) + s];
+                    if (!(ok = mbar_wait_warp(&bar[(v ? V_EMPTY : K_EMPTY) + s], ((kt / RING) & 1) ^ 1))) break;
+                    uint8_t* dst = sm + (v ? C::OFF_V : C::OFF_K) + s * C::TILE;
+                    if (elect_one()) mbar_arrive_expect_tx(full, nb * a.box * HD * 2);
+                    __syncwarp();
+                    int r = row;
+                    for (int i = 0; i < nb; ++i) {
+                        const int page = __shfl_sync(0xffffffffu, pages, (b0 + i) & 31);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int c = 0; c < NCH; ++c)
+                                tma_load_4d(dst + c * KT * 128 + i * a.box * 128, v ? &tv : &tk, c * 64, x.kvh,
+                                            r, page, full);
+                        }
+                        __syncwarp();
+                        r += a.box;
+                        if (r >= a.pages.room) r -= a.pages.room;
+                    }
+                }
+            }
+            x = next;
+            pages = next_pages;
+        }
+        if (!ok) *fail_flag = 1;
+        // every copy has landed before the CTA may exit (at once in a normal run)
+        if (nq > 0) mbar_wait_warp(&bar[Q_FULL], (nq - 1) & 1, 100000000LL);
+        for (uint32_t i = kt > RING ? kt - RING : 0; i < kt; ++i) {
+            mbar_wait_warp(&bar[K_FULL + i % RING], (i / RING) & 1, 100000000LL);
+            mbar_wait_warp(&bar[V_FULL + i % RING], (i / RING) & 1, 100000000LL);
+        }
+        if (!ok) {  // a K tile whose V was not asked for
+            const uint32_t i = kt;
+            mbar_wait_warp(&bar[K_FULL + i % RING], (i / RING) & 1, 100000000LL);
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        constexpr uint32_t IDESC_S = idesc_bf16_f32(128, KT);
+        constexpr uint32_t IDESC_PV = idesc_bf16_f32(128, HD) | (1u << 16);  // B MN-major
+        bool ok = true, issued = false;
+        uint32_t ks = 0, kv = 0, nu = 0;  // K tiles and V tiles taken, units with tokens
+        const uint32_t q_lo = sw128_desc_lo(smem_u32(sm)), k_lo = sw128_desc_lo(smem_u32(sm + C::OFF_K));
+        const uint32_t v_lo = sw128_desc_mn_lo(smem_u32(sm + C::OFF_V), KT * 128);
+        auto commit = [&](uint64_t* b) {
+            if (elect_one()) tc_commit(b);
+            __syncwarp();
+        };
+        // score tile ks goes to buffer ks % 2, whose P the product two tiles back has read
+        auto next_s = [&](bool last) -> bool {
+            const int s = ks % RING;
+            if (!mbar_wait_warp(&bar[K_FULL + s], (ks / RING) & 1)) return false;
+            tc_fence_after();
+            const uint32_t lo = k_lo + s * (C::TILE >> 4), d = tbase + (ks & 1) * KT;
+            if (elect_one()) {
+#pragma unroll
+                for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma_f16(d, desc_of(q_lo + c * (128 * 128 >> 4) + k * 2, kSw128DescHi),
+                                   desc_of(lo + c * (KT * 128 >> 4) + k * 2, kSw128DescHi), IDESC_S,
+                                   (c | k) != 0);
+                tc_commit(&bar[S_FULL + (ks & 1)]);
+                tc_commit(&bar[K_EMPTY + s]);
+                if (last) tc_commit(&bar[Q_EMPTY]);
+            }
+            __syncwarp();
+            issued = true;
+            ++ks;
+            return true;
+        };
+        for (int u = blockIdx.x; ok && u < n_units && !__any_sync(0xffffffffu, *fail_flag); u += gridDim.x) {
+            const TreeUnit x = open(u);
+            const int n = warp_uniform(x.tiles());
+            if (n == 0) continue;
+            if (!(ok = mbar_wait_warp(&bar[Q_FULL], nu & 1))) break;
+            tc_fence_after();
+            ok = next_s(n == 1) && (n < 2 || next_s(n == 2));
+            for (int t = 0; t < n && ok; ++t, ++kv) {
+                const int s = kv % RING;
+                const uint32_t b = kv & 1, p = tbase + b * KT;
+                if (!(ok = mbar_wait_warp(&bar[V_FULL + s], (kv / RING) & 1))) break;
+                const int valid = warp_uniform(x.end - x.at) - t * KT;
+                if (valid < KT) {
+                    // rows behind the run's last token may hold NaN: 0 * NaN would reach O
+                    uint8_t* tile = sm + C::OFF_V + s * C::TILE;
+                    for (int i = lane; i < (KT - valid) * (HD / 8); i += 32) {
+                        const int r = valid + i / (HD / 8), w = i % (HD / 8);
+                        *reinterpret_cast<uint4*>(tile + (w >> 3) * KT * 128 + r * 128 + (w & 7) * 16) =
+                            make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                if (!(ok = mbar_wait_warp(&bar[P_FULL + b], (kv >> 1) & 1))) break;
+                // the unit's first product overwrites O: the last epilogue has read it
+                if (t == 0 && nu > 0 && !(ok = mbar_wait_warp(&bar[O_FREE], (nu - 1) & 1))) break;
+                tc_fence_after();
+                const uint32_t lo = v_lo + s * (C::TILE >> 4);
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < KT / 16; ++k)
+                        tc_mma_f16_ts(tbase + C::O_COL, p + k * 8, desc_of(lo + k * 128, kSw128DescHi),
+                                      IDESC_PV, t > 0 || k > 0);
+                    tc_commit(&bar[PV_DONE + b]);
+                    tc_commit(&bar[V_EMPTY + s]);
+                    if (t + 1 == n) tc_commit(&bar[O_FULL]);
+                }
+                __syncwarp();
+                if (t + 2 < n) ok = next_s(t + 3 == n);
+            }
+            ++nu;
+        }
+        if (!ok) *fail_flag = 1;
+        if (issued) {
+            commit(&bar[DRAIN]);
+            mbar_wait_warp(&bar[DRAIN], 0, 100000000LL);
+        }
+    } else {
+        // ---------------- softmax + epilogue ----------------
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tO = tbase + lane_base + C::O_COL;
+        uint32_t g = 0, nu = 0;  // score tiles, units with tokens
+        bool ok = true;
+        const int tok = row / a.group, hg = row % a.group;
+        uint8_t* stg = sm + C::OFF_STG + (warp - 2) * STAGE;
+        for (int u = blockIdx.x; ok && u < n_units && !__any_sync(0xffffffffu, *fail_flag); u += gridDim.x) {
+            const TreeUnit x = open(u);
+            const int n = warp_uniform(x.tiles()), i = x.i0 + tok;
+            const bool live = tok < T && i < x.q.n;
+            // the nodes that this row sees; a row that is none of the tile's has no say in the masks
+            const unsigned long long all = x.q.n >= 64 ? ~0ull : (1ull << x.q.n) - 1;
+            const unsigned long long see = live ? a.sees[x.q.row0 + i] & all : all;
+            const bool work = __any_sync(0xffffffffu, live);  // else nobody reads the warp's rows
+            float m = -INFINITY, l = 0.f;
+            for (int t = 0; t < n; ++t, ++g) {
+                const uint32_t b = g & 1, tS = tbase + lane_base + b * KT;
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[S_FULL + b], (g >> 1) & 1)))) break;
+                if (!work) {
+                    mbar_arrive(&bar[P_FULL + b]);
+                    continue;
+                }
+                tc_fence_after();
+                uint32_t v[2][32];
+                tmem_ld32(tS, v[0]);
+                tmem_ld32(tS + 32, v[1]);
+                tmem_ld_wait_regs(v[0]);
+                tmem_ld_wait_regs(v[1]);
+                // tokens of the tile ahead of the nodes, then those of the nodes that are seen
+                const int ahead = x.q.old - (x.at + t * KT);
+                if (ahead < KT || x.end - (x.at + t * KT) < KT) {
+                    unsigned long long word = ahead >= 64 ? ~0ull
+                                              : ahead > 0 ? ((1ull << ahead) - 1) | (see << ahead)
+                                                          : see >> -ahead;
+                    const int valid = x.end - (x.at + t * KT);
+                    if (valid < KT) word &= (1ull << valid) - 1;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(word >> (c * 32 + e) & 1)) v[c][e] = 0xff800000u;  // -inf
+                }
+                float mx[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    mx[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+                    for (int e = 1; e < 31; e += 2)
+                        mx[c] = fmax3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
+                    mx[c] = fmaxf(mx[c], __uint_as_float(v[c][31]));
+                }
+                const float top = fmaxf(mx[0], mx[1]) * a.scale_log2;
+                float alpha = 1.f;
+                if (t == 0) {
+                    m = top;
+                } else if (top > m + kLazy) {
+                    alpha = ex2_approx(m - top);
+                    m = top;
+                }
+                if (t > 0 && __any_sync(0xffffffffu, alpha < 1.f)) {
+                    // every earlier P V of the unit is done
+                    if (!(ok = __all_sync(0xffffffffu,
+                                          mbar_wait(&bar[PV_DONE + (b ^ 1)], ((g - 1) >> 1) & 1))))
+                        break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < HD / 16; ++c) {
+                        uint32_t o16[16];
+                        tmem_ld16(tO + c * 16, o16);
+                        tmem_ld_wait_regs16(o16);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            o16[e] = __float_as_uint(__uint_as_float(o16[e]) * alpha);
+                        tmem_st16(tO + c * 16, o16);
+                    }
+                    tmem_st_wait();
+                }
+                // a row that has seen no token yet subtracts nothing
+                const float sub = m == -INFINITY ? 0.f : m;
+                const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2), nm2 = f2_pack(-sub, -sub);
+                uint64_t rs[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+                uint32_t pk[32];
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float x0, x1;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1])),
+                                         sc2, nm2),
+                                  x0, x1);
+                        const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                        rs[(e >> 1) & 1] = f2_add(rs[(e >> 1) & 1], f2_pack(p0, p1));
+                        pk[c * 16 + e / 2] = cvt_bf2(p0, p1);
+                    }
+                tmem_st32(tS, pk);
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(&bar[P_FULL + b]);
+                float r0, r1, r2, r3;
+                f2_unpack(rs[0], r0, r1);
+                f2_unpack(rs[1], r2, r3);
+                l = l * alpha + ((r0 + r1) + (r2 + r3));
+            }
+            if (!ok) break;
+            if (n > 0) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[O_FULL], nu & 1)))) break;
+                tc_fence_after();
+                ++nu;
+            }
+            const int h = x.kvh * a.group + hg;
+            const bool joined = x.q.runs > 1;
+            const long long slot =
+                live ? ((long long)base[x.s] + (long long)x.run * x.q.n + i) * a.H + h : -1;
+            if (joined && live) a.ml[slot] = make_float2(m, l);
+            const float inv = joined ? 1.f : l > 0.f ? 1.f / l : 0.f;
+            const long long o = !live ? -1
+                                : joined ? slot * HD
+                                         : (x.q.row0 + i) * a.o_row + h * a.o_head;
+            // out through the warp's staging, 16 fp32 columns or 32 bf16 at a time: this lane writes
+            // its row's four units and stores unit lane % 4 of rows lane / 4 + 8 j
+            long long to[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[j] = __shfl_sync(0xffffffffu, o, 8 * j + (lane >> 2));
+            const int un = lane & 3;
+            uint8_t* mine = stg + lane * 64;
+            const int flip = (lane >> 1) & 3;
+#pragma unroll 1
+            for (int c = 0; c < HD / 32; ++c) {
+                uint32_t w[32];
+                if (n > 0) {
+                    tmem_ld32(tO + c * 32, w);
+                    tmem_ld_wait_regs(w);
+                    if (c + 1 == HD / 32) {
+                        tc_fence_before();
+                        mbar_arrive(&bar[O_FREE]);
+                    }
+                }
+                // a row that saw nothing: O holds products of zeros
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    w[e] = n > 0 && l > 0.f ? __float_as_uint(__uint_as_float(w[e]) * inv) : 0u;
+                if (!work) continue;
+                if (joined) {
+#pragma unroll
+                    for (int d = 0; d < 2; ++d) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<uint4*>(mine + ((j ^ flip) << 4)) =
+                                make_uint4(w[16 * d + 4 * j], w[16 * d + 4 * j + 1], w[16 * d + 4 * j + 2],
+                                           w[16 * d + 4 * j + 3]);
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int rr = 8 * j + (lane >> 2);
+                            const uint4 y = *reinterpret_cast<const uint4*>(
+                                stg + rr * 64 + ((un ^ ((rr >> 1) & 3)) << 4));
+                            if (to[j] >= 0)
+                                *reinterpret_cast<uint4*>(a.part + to[j] + c * 32 + d * 16 + un * 4) = y;
+                        }
+                        __syncwarp();
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[e] = cvt_bf2(__uint_as_float(w[8 * j + 2 * e]), __uint_as_float(w[8 * j + 2 * e + 1]));
+                        *reinterpret_cast<uint4*>(mine + ((j ^ flip) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int rr = 8 * j + (lane >> 2);
+                        const uint4 y =
+                            *reinterpret_cast<const uint4*>(stg + rr * 64 + ((un ^ ((rr >> 1) & 3)) << 4));
+                        if (to[j] >= 0) *reinterpret_cast<uint4*>(a.out + to[j] + c * 32 + un * 8) = y;
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (!ok) *fail_flag = 1;
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (*fail_flag && threadIdx.x == 0) report(a.status, JNX_ERR_TIMEOUT);
+    if (warp == 1) tmem_dealloc(tbase, C::COLS);
+}
+
+// A sequence's runs joined in their order.  A warp a node and head.
+template <int HD>
+__global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeArgs a) {
+    using namespace tree;
     constexpr int E = HD / 32;
     pdl_entry();
-    const int s = blockIdx.x, lane = threadIdx.x & 31;
-    int first, n;
-    if (!tree_rows(a.cu_nodes, s, a.n_rows, kMaxNodes, first, n)) {
-        if (threadIdx.x == 0 && blockIdx.y == 0) report(a.status, JNX_ERR_DEVICE_BOUNDS);
-        return;
+    const int w = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int s = blockIdx.y;
+    int row0, n, old;
+    if (!tree_lengths(a, s, row0, n, old) || w >= n * a.H) return;
+    const TreeSeq x = tree_seq<HD>(a, row0, n, old);
+    if (x.runs == 1) return;
+    const int i = w / a.H, h = w % a.H;
+    const long long at = ((long long)a.base[s] + i) * a.H + h, step = (long long)n * a.H;
+    float m[MAX_RUNS / 32], l[MAX_RUNS / 32], top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < MAX_RUNS / 32; ++k) {
+        const int r = k * 32 + lane;
+        const float2 y = r < x.runs ? a.ml[at + r * step] : make_float2(-INFINITY, 0.f);
+        m[k] = y.x, l[k] = y.y;
+        top = fmaxf(top, m[k]);
     }
-    int old = a.n_cached[s], all = old + n;
-    if (old < 0 || (long long)old + n > (long long)a.pages.max_pages * a.pages.room) {
-        if (threadIdx.x == 0 && blockIdx.y == 0) report(a.status, JNX_ERR_DEVICE_BOUNDS);
-        old = all = 0;
-    }
-    for (int w = blockIdx.y * 4 + (threadIdx.x >> 5); w < n * a.H; w += gridDim.y * 4) {
-        const int i = w / a.H, h = w % a.H, g = h / a.group;
-        const unsigned long long see = a.sees[first + i];
-        float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
+    constexpr int R = 8;  // runs under way
+    float v[R][E], acc[E] = {};
+    auto load = [&](int k, int r) {
+        if (r >= x.runs) return;
+        const float* src = a.part + (at + r * step) * HD + lane * E;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            q[e] = bf2f(a.q[(first + i) * a.q_row + h * a.q_head + e * 32 + lane]);
-        for (int j = 0; j < all; ++j) {
-            if (j >= old && !(see >> (j - old) & 1)) continue;
-            int page, row;
-            const bool there = a.pages.find(s, j, page, row);
-            if (!there && lane == 0) report(a.status, JNX_ERR_DEVICE_BOUNDS);
-            const long long at = there ? page * a.page_stride + row * a.kv_row + g * a.kv_head : 0;
-            float x = 0.f;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (there) x = fmaf(q[e], bf2f(a.k[at + e * 32 + lane]), x);
-#pragma unroll
-            for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-            x *= a.scale_log2;
-            const float top = fmaxf(m, x), alpha = ex2_approx(m - top), p = ex2_approx(x - top);
-            m = top;
-            l = l * alpha + p;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                o[e] = o[e] * alpha + (there ? p * bf2f(a.v[at + e * 32 + lane]) : 0.f);
+        for (int e = 0; e < E; e += 2) {
+            const float2 y = *reinterpret_cast<const float2*>(src + e);
+            v[k][e] = y.x, v[k][e + 1] = y.y;
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+    };
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            a.out[(first + i) * a.o_row + h * a.o_head + e * 32 + lane] = f2bf(o[e] * inv);
+    for (int k = 0; k < R; ++k) load(k, k);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (top == -INFINITY) top = 0.f;  // no run's token was seen
+#pragma unroll
+    for (int k = 0; k < MAX_RUNS / 32; ++k) {
+        m[k] = ex2_approx(m[k] - top);
+        sum += l[k] * m[k];
     }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    for (int r = 0; r < x.runs; r += R) {
+        if (r > 0) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) load(k, r + k);
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (r + k >= x.runs) continue;
+            const float f = __shfl_sync(0xffffffffu, (r + k) >> 5 ? m[1] : m[0], (r + k) & 31);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(f, v[k][e], acc[e]);
+        }
+    }
+    static_assert(MAX_RUNS == 64, "factors of two registers");
+    uint16_t* o = a.out + (row0 + i) * a.o_row + h * a.o_head + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(o + e) = cvt_bf2(acc[e] * inv, acc[e + 1] * inv);
+}
+
+static size_t tree_sums_at() { return tree::BATCH * sizeof(int); }
+
+template <int HD>
+static jnx_status launch_tree(const jnx_kv_cache& c, const jnx_pages& p, const jnx_head_rows& q, TreeArgs a,
+                              long long runs, cudaStream_t s) {
+    using namespace tree;
+    using C = TreeCfg<HD>;
+    static std::atomic<uint64_t> attr{0};
+    if (set_smem_limit(reinterpret_cast<const void*>(k_tree_attn<HD>), C::SMEM, attr) != cudaSuccess)
+        return fail(JNX_ERR_CUDA, "tree attention: smem attribute");
+    CUtensorMap tq, tk, tv;
+    if (!make_tmap_heads(&tq, q, a.n_rows, a.H, HD, a.group, tile_tokens(a.group)) ||
+        !make_tmap_cache(&tk, c.k, c, a.Hkv, HD, a.box) || !make_tmap_cache(&tv, c.v, c, a.Hkv, HD, a.box))
+        return fail(JNX_ERR_CUDA, "tree attention: tensor map encode failed");
+    const int most = std::min(kMaxNodes, a.n_rows), T = tile_tokens(a.group);
+    for (int s0 = 0; s0 < p.n_seqs; s0 += BATCH) {
+        a.s0 = s0;
+        a.n_seqs = std::min(BATCH, p.n_seqs - s0);
+        const long long units = a.n_seqs * runs * a.Hkv * ((most + T - 1) / T);
+        const int grid = (int)std::min<long long>(units, (long long)num_sms() * C::CTAS);
+        pdl(k_tree_attn<HD>, grid, THREADS, C::SMEM, s)(tq, tk, tv, a);
+        if (runs > 1) pdl(k_tree_join<HD>, dim3((most * a.H + 3) / 4, a.n_seqs), 128, 0, s)(a);
+    }
+    return launched("tree attention");
 }
 
 }  // namespace jnx
@@ -82,8 +676,8 @@ using namespace jnx;
 extern "C" size_t jnx_op_tree_attention_workspace_bytes(int32_t n_seqs, int32_t n_rows,
                                                         int32_t n_heads, int32_t head_dim,
                                                         int64_t max_tokens) {
-    (void)n_seqs, (void)n_rows, (void)n_heads, (void)head_dim, (void)max_tokens;
-    return 0;
+    if (n_seqs < 0 || n_rows < 0 || n_heads <= 0 || head_dim <= 0 || max_tokens < 0) return 0;
+    return tree_sums_at() + (size_t)n_rows * tree::most_runs(max_tokens) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
 extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx_pages* pages,
@@ -95,7 +689,6 @@ extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx
                                             void* stream) {
     clear_error();
     const char* what = "tree attention";
-    (void)workspace, (void)ws_bytes;
     if (jnx_status st = heads_ok(n_heads, n_kv_heads, head_dim, what)) return st;
     if (n_rows < 0 || !pages_ok(pages)) return fail(JNX_ERR_INVALID_ARG, "%s: bad sizes or pages", what);
     if (n_rows == 0 || pages->n_seqs == 0) return JNX_OK;
@@ -103,18 +696,30 @@ extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned argument", what);
     if (pages->max_pages > 1 && cache->room % 16)
         return fail(JNX_ERR_UNSUPPORTED, "%s: pages of %d tokens, no multiple of 16", what, cache->room);
-    if ((int64_t)pages->max_pages * cache->room > 0x7fffff00)
-        return fail(JNX_ERR_UNSUPPORTED, "%s: sequences of over 2^31 tokens", what);
-    const TreeArgs a{cache->k, cache->v, cache->slot_stride, cache->row_stride, cache->head_stride,
-                     Pages(*pages, *cache), n_heads, n_kv_heads, n_heads / n_kv_heads, n_rows,
-                     (float)(1.4426950408889634 / sqrt((double)head_dim)), q->ptr, q->row_stride,
-                     q->head_stride, out->ptr, out->row_stride, out->head_stride, cu_nodes, n_cached,
-                     reinterpret_cast<const unsigned long long*>(sees), status};
+    const long long tokens = (long long)pages->max_pages * cache->room, runs = tree::most_runs(tokens);
+    if (tokens > 0x7fffff00 || (long long)n_rows * n_heads > 0x7fffff00 ||
+        (long long)n_rows * runs > 0x7fffff00 ||
+        tree::BATCH * runs * n_kv_heads * kMaxNodes > 0x7fffff00)
+        return fail(JNX_ERR_UNSUPPORTED, "%s: sizes", what);
+    if (!workspace || !aligned16(workspace) ||
+        ws_bytes < jnx_op_tree_attention_workspace_bytes(pages->n_seqs, n_rows, n_heads, head_dim, tokens))
+        return fail(JNX_ERR_WORKSPACE, "%s: workspace too small or misaligned", what);
+    // boxes of as many tokens as a tile and a page share
+    int box = tree::KT;
+    while (pages->max_pages > 1 && cache->room % box) box /= 2;
+    // an empty cache has no tiles, but the maps want extents
+    jnx_kv_cache c = *cache;
+    c.n_slots = std::max(c.n_slots, 1);
+    c.room = std::max(c.room, 1);
+    TreeArgs a{Pages(*pages, *cache), 0, 0, n_heads, n_kv_heads, n_heads / n_kv_heads, n_rows, box,
+               (float)(1.4426950408889634 / sqrt((double)head_dim)), out->ptr, out->row_stride,
+               out->head_stride, cu_nodes, n_cached, reinterpret_cast<const unsigned long long*>(sees),
+               static_cast<int*>(workspace), nullptr, nullptr, status};
+    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + tree_sums_at());
+    a.ml = reinterpret_cast<float2*>(a.part + (size_t)n_rows * runs * n_heads * head_dim);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_TREE_ATTN, 0.0, s);
-    const dim3 grid(pages->n_seqs, 64);
-    if (head_dim == 64) pdl(k_tree_attn<64>, grid, 128, 0, s)(a);
-    else if (head_dim == 128) pdl(k_tree_attn<128>, grid, 128, 0, s)(a);
-    else pdl(k_tree_attn<256>, grid, 128, 0, s)(a);
-    return launched(what);
+    if (head_dim == 64) return launch_tree<64>(c, *pages, *q, a, runs, s);
+    if (head_dim == 128) return launch_tree<128>(c, *pages, *q, a, runs, s);
+    return launch_tree<256>(c, *pages, *q, a, runs, s);
 }
