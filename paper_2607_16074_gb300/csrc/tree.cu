@@ -30,24 +30,26 @@ namespace jnx {
 
 namespace tree {
 constexpr int KT = 64;         // tokens of a tile
-constexpr int RING = 2;        // tiles of either ring
+constexpr int RINGS = 5;       // tiles of either ring, at most
 constexpr int BATCH = 256;     // sequences of one launch
 constexpr int MAX_RUNS = 64;   // of a sequence
 constexpr int THREADS = 192;
-constexpr int STAGE = 2048;    // epilogue staging of a softmax warp
 constexpr float kLazy = 8.0f;  // log2 growth of the maximum that moves it
-enum { K_FULL = 0, K_EMPTY = K_FULL + RING, V_FULL = K_EMPTY + RING, V_EMPTY = V_FULL + RING,
-       Q_FULL = V_EMPTY + RING, Q_EMPTY, S_FULL, P_FULL = S_FULL + 2, PV_DONE = P_FULL + 2,
+enum { K_FULL = 0, K_EMPTY = K_FULL + RINGS, V_FULL = K_EMPTY + RINGS, V_EMPTY = V_FULL + RINGS,
+       Q_FULL = V_EMPTY + RINGS, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2, PV_DONE = P_FULL + 2,
        O_FULL = PV_DONE + 2, O_FREE, DRAIN, N_BARS };
 
 __host__ __device__ inline int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
 // Tokens of a run of L, for `rows` rows of a tile and `units` units of a run: a run's sums are
-// rows / tokens of what it reads, which is kept under a sixteenth, an eighth or so of short
-// sequences; a sequence that fills the card by itself has whole rounds of units.
+// rows / tokens of what it reads, and its epilogue costs what two or three tiles do, hence long
+// runs of long sequences (64 trees over up to 8,100 tokens: 256 us with 16 rows' worth of tokens,
+// 196 with 32 or 1,024 at most, 230 with 64) and of short ones as many as reach more SMs (8 over
+// up to 700: 13.6 us, 20 with 32 rows' worth).  A sequence that fills the card by itself has
+// whole rounds of units.
 __host__ __device__ inline int run_tokens(int L, int rows, int units, int slots) {
-    int least = (L <= 2048 ? 4 : 16) * rows;
-    least = round_up(least < 128 ? 128 : least, KT);
+    int least = L <= 2048 ? 4 * rows : 32 * rows < 1024 ? 32 * rows : 1024;
+    least = round_up(least < 256 ? 256 : least, KT);
     int n = (L + least - 1) / least;
     if (n > MAX_RUNS) n = MAX_RUNS;
     if ((long long)n * units > slots) n = (int)((long long)n * units / slots * slots / units);
@@ -56,7 +58,7 @@ __host__ __device__ inline int run_tokens(int L, int rows, int units, int slots)
 }
 // More runs than any sequence of up to max_tokens has.
 inline long long most_runs(long long max_tokens) {
-    return std::max(1ll, std::min<long long>(MAX_RUNS, (max_tokens + 127) / 128));
+    return std::max(1ll, std::min<long long>(MAX_RUNS, (max_tokens + 255) / 256));
 }
 }  // namespace tree
 
@@ -66,11 +68,11 @@ struct TreeCfg {
     static constexpr int CTAS = HD == 256 ? 1 : 2;       // of an SM
     static constexpr int SLOTS = 152 * CTAS;
     static constexpr int TILE = tree::KT * HD * 2;
+    static constexpr int RING = HD == 64 ? 5 : 2;  // tiles of either ring
     static constexpr int QB = 128 * HD * 2;
-    static constexpr int OFF_K = QB, OFF_V = OFF_K + tree::RING * TILE;
-    static constexpr int OFF_STG = OFF_V + tree::RING * TILE;
-    static constexpr int OFF_SEQ = OFF_STG + 4 * tree::STAGE;
-    static constexpr int OFF_BAR = OFF_SEQ + (5 * tree::BATCH + 4) * 4;
+    static constexpr int OFF_K = QB, OFF_V = OFF_K + RING * TILE;
+    static constexpr int OFF_SEQ = OFF_V + RING * TILE;
+    static constexpr int OFF_BAR = OFF_SEQ + (6 * tree::BATCH + 4) * 4 + tree::BATCH * 4;
     static constexpr int SMEM = OFF_BAR + tree::N_BARS * 8 + 16 + 1024;
     static_assert(SMEM <= (CTAS == 2 ? 113 : 226) * 1024, "shared memory per CTA");
     static constexpr uint32_t COLS = HD == 256 ? 512 : 256, O_COL = HD == 256 ? 256 : 128;
@@ -85,9 +87,10 @@ struct TreeArgs {
     long long o_row, o_head;
     const int *cu_nodes, *n_cached;
     const unsigned long long* sees;
-    int* base;    // [n_seqs]: a sequence's first (run, node) among the sums
+    int4* where;  // [n_rows]: a row's first place among the sums, its sequence's nodes, runs, number
     float* part;  // [run, node][H][hd]: sums
     float2* ml;   // [run, node][H]: maxima and sums of exponentials
+    int places;   // of a run and node
     int* status;
 };
 
@@ -111,6 +114,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& a, int row0, int n, 
 // Rows [i0, ...) of a sequence for one key head, over its tokens [at, end).
 struct TreeUnit {
     int s, i0, kvh, run, at, end;
+    bool half;  // up to 64 rows: Q takes half of its place, and the next unit's the other half
     TreeSeq q;
     __device__ __forceinline__ int tiles() const { return (end - at + tree::KT - 1) / tree::KT; }
 };
@@ -129,18 +133,29 @@ __device__ __forceinline__ bool tree_lengths(const TreeArgs& a, int s, int& row0
     return true;
 }
 
+// 32 bytes, a sector, from registers.
+__device__ __forceinline__ void store8(float* p, const uint32_t (&w)[32], int i) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[i]),
+                 "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]),
+                 "r"(w[i + 7])
+                 : "memory");
+}
+
 template <int HD>
 __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
-    k_tree_attn(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
-                const __grid_constant__ CUtensorMap tv, const __grid_constant__ TreeArgs a) {
+    k_tree_attn(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tq64,
+                const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+                const __grid_constant__ TreeArgs a) {
     using C = TreeCfg<HD>;
     using namespace tree;
-    constexpr int NCH = C::NCH;
+    constexpr int NCH = C::NCH, RING = C::RING;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     int* first = reinterpret_cast<int*>(sm + C::OFF_SEQ);  // [n_seqs + 1]: first unit of each
     int *rows0 = first + BATCH + 1, *nodes = rows0 + BATCH, *olds = nodes + BATCH, *base = olds + BATCH;
+    int* run_of = base + BATCH;
+    uint16_t *runs_of = reinterpret_cast<uint16_t*>(run_of + BATCH), *tiles_of = runs_of + BATCH;
     uint64_t* bar = reinterpret_cast<uint64_t*>(sm + C::OFF_BAR);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + N_BARS);
     volatile int* fail_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -172,8 +187,9 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
         for (int b = 0; b < a.n_seqs; b += 32) {
             const int s = b + lane;
             int u = 0, v = 0;
+            TreeSeq x{};
             if (s < a.n_seqs) {
-                const TreeSeq x = tree_seq<HD>(a, rows0[s], nodes[s], olds[s]);
+                x = tree_seq<HD>(a, rows0[s], nodes[s], olds[s]);
                 u = x.runs * a.Hkv * x.tiles;
                 v = x.runs > 1 ? x.runs * x.n : 0;
             }
@@ -186,7 +202,7 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
             if (s < a.n_seqs) {
                 first[s] = units + ru - u;
                 base[s] = sums + rv - v;
-                if (blockIdx.x == 0) a.base[s] = sums + rv - v;
+                run_of[s] = x.run, runs_of[s] = (uint16_t)x.runs, tiles_of[s] = (uint16_t)x.tiles;
             }
             units += __shfl_sync(0xffffffffu, ru, 31);
             sums += __shfl_sync(0xffffffffu, rv, 31);
@@ -196,6 +212,12 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
     __syncthreads();
     const uint32_t tbase = warp_uniform(*tmem_slot);
     const int n_units = warp_uniform(first[a.n_seqs]);
+    // what the join needs of each row
+    for (int s = blockIdx.x; s < a.n_seqs; s += gridDim.x) {
+        const int i = threadIdx.x;
+        if (i >= nodes[s]) continue;
+        a.where[rows0[s] + i] = make_int4(base[s] + i, nodes[s], runs_of[s], a.s0 + s);
+    }
 
     auto open = [&](int u) {
         TreeUnit x{};
@@ -207,9 +229,11 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
             else hi = mid - 1;
         }
         x.s = lo;
-        x.q = tree_seq<HD>(a, rows0[lo], nodes[lo], olds[lo]);
+        const int old = olds[lo], nn = nodes[lo];
+        x.q = TreeSeq{rows0[lo], nn, old, old < 0 ? 0 : old + nn, run_of[lo], runs_of[lo], tiles_of[lo]};
         int rest = u - first[lo];  // a run's tiles lie together, then its heads
         x.i0 = rest % x.q.tiles * T;
+        x.half = min(x.q.n - x.i0, T) * a.group <= 64;
         rest /= x.q.tiles;
         x.kvh = rest % a.Hkv;
         x.run = rest / a.Hkv;
@@ -222,12 +246,14 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
         // ---------------- TMA producer ----------------
         if (elect_one()) {
             tma_prefetch_desc(&tq);
+            tma_prefetch_desc(&tq64);
             tma_prefetch_desc(&tk);
             tma_prefetch_desc(&tv);
         }
         bool ok = true;
-        uint32_t kt = 0, nq = 0;  // tiles and Q tiles loaded
-        const int qbytes = a.group * T * HD * 2, boxes = KT / a.box;
+        uint32_t nk = 0, nv = 0;  // K and V tiles loaded
+        uint32_t qn = 0, qodd = 0, qany = 0;  // the next half; whether odd, or any, Q tiles went to each
+        const int qrow = a.group * HD * 2, boxes = KT / a.box;
         // pages of the boxes [32 c, 32 c + 32) of a unit, one a lane
         auto look = [&](const TreeUnit& x, int c) {
             int page = a.pages.n_pages, row = 0;  // no page: read as zeros
@@ -236,71 +262,91 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
                 page = a.pages.n_pages;
                 report(a.status, JNX_ERR_DEVICE_BOUNDS);
             }
+            __syncwarp();
             return page;
         };
+        // tile t of a unit's tokens [at, end), whose first box's page is in lane `first` of pages
+        struct Tile {
+            int kvh, token, end, pages, first;
+        };
+        auto load = [&](bool v, const Tile& x) -> bool {
+            uint32_t& n = v ? nv : nk;
+            const int s = n % RING;
+            uint64_t* full = &bar[(v ? V_FULL : K_FULL) + s];
+            if (!mbar_wait_warp(&bar[(v ? V_EMPTY : K_EMPTY) + s], ((n / RING) & 1) ^ 1)) return false;
+            ++n;
+            uint8_t* dst = sm + (v ? C::OFF_V : C::OFF_K) + s * C::TILE;
+            const CUtensorMap* map = v ? &tv : &tk;
+            const int nb = min(boxes, (x.end - x.token + a.box - 1) / a.box);
+            if (elect_one()) mbar_arrive_expect_tx(full, nb * a.box * HD * 2);
+            __syncwarp();
+            int r = x.token % a.pages.room;  // a box lies in one page
+            for (int i = 0; i < nb; ++i) {
+                const int page = __shfl_sync(0xffffffffu, x.pages, x.first + i);
+                if (elect_one()) {
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c)
+                        tma_load_4d(dst + c * KT * 128 + i * a.box * 128, map, c * 64, x.kvh, r, page, full);
+                }
+                __syncwarp();
+                r += a.box;
+                if (r >= a.pages.room) r -= a.pages.room;
+            }
+            return true;
+        };
+        auto q_free = [&](int h) {
+            return !(qany >> h & 1) || mbar_wait_warp(&bar[Q_EMPTY + h], (qodd >> h & 1) ^ 1);
+        };
+        // V one tile behind K, as S is taken ahead of P V: so K is asked for two tiles ahead
+        Tile late{0, 0, 0, 0, -1};
         TreeUnit x = open(blockIdx.x);
         int pages = look(x, 0);
         for (int u = blockIdx.x; ok && u < n_units && !__any_sync(0xffffffffu, *fail_flag); u += gridDim.x) {
-            const int n = warp_uniform(x.tiles());
+            const int n = warp_uniform(x.tiles()), at = warp_uniform(x.at), end = warp_uniform(x.end);
+            const int kvh = warp_uniform(x.kvh);
             const TreeUnit next = open(u + gridDim.x);
             const int next_pages = look(next, 0);
             int more = look(x, 1);
             if (n > 0) {
-                if (nq > 0 && !(ok = mbar_wait_warp(&bar[Q_EMPTY], (nq - 1) & 1))) break;
+                const bool half = warp_uniform(x.half);
+                const int h = half ? qn : 0;
+                if (!(ok = q_free(h) && (half || q_free(1)))) break;
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&bar[Q_FULL], qbytes);
+                    mbar_arrive_expect_tx(&bar[Q_FULL + h], (half ? 64 / a.group : T) * qrow);
+                    if (!half) mbar_arrive(&bar[Q_FULL + 1]);
 #pragma unroll
                     for (int c = 0; c < NCH; ++c)
-                        tma_load_3d(sm + c * 128 * 128, &tq, c * 64, x.kvh * a.group, x.q.row0 + x.i0,
-                                    &bar[Q_FULL]);
+                        tma_load_3d(sm + h * (C::QB / 2) + c * (half ? 64 : 128) * 128, half ? &tq64 : &tq,
+                                    c * 64, kvh * a.group, x.q.row0 + x.i0, &bar[Q_FULL + h]);
                 }
                 __syncwarp();
-                ++nq;
+                const uint32_t both = half ? 1u << h : 3u;
+                qodd ^= both;
+                qany |= both;
+                qn = half ? qn ^ 1 : 0;
             }
-            for (int t = 0; t < n && ok; ++t, ++kt) {
+            for (int t = 0; t < n && ok; ++t) {
                 const int b0 = t * boxes;  // first box of the tile
                 if (t > 0 && b0 % 32 == 0) {
                     pages = more;
                     more = look(x, b0 / 32 + 1);
                 }
-                const int s = kt % RING, token = warp_uniform(x.at) + t * KT;
-                const int nb = min(boxes, (warp_uniform(x.end) - token + a.box - 1) / a.box);
-                const int row = token % a.pages.room;  // a box lies in one page
-                for (int v = 0; v < 2 && ok; ++v) {
-                    uint64_t* full = &bar[(v ? V_FULL : K_FULL) + s];
-                    if (!(ok = mbar_wait_warp(&bar[(v ? V_EMPTY : K_EMPTY) + s], ((kt / RING) & 1) ^ 1))) break;
-                    uint8_t* dst = sm + (v ? C::OFF_V : C::OFF_K) + s * C::TILE;
-                    if (elect_one()) mbar_arrive_expect_tx(full, nb * a.box * HD * 2);
-                    __syncwarp();
-                    int r = row;
-                    for (int i = 0; i < nb; ++i) {
-                        const int page = __shfl_sync(0xffffffffu, pages, (b0 + i) & 31);
-                        if (elect_one()) {
-#pragma unroll
-                            for (int c = 0; c < NCH; ++c)
-                                tma_load_4d(dst + c * KT * 128 + i * a.box * 128, v ? &tv : &tk, c * 64, x.kvh,
-                                            r, page, full);
-                        }
-                        __syncwarp();
-                        r += a.box;
-                        if (r >= a.pages.room) r -= a.pages.room;
-                    }
-                }
+                const Tile tile{kvh, at + t * KT, end, pages, b0 & 31};
+                ok = load(false, tile) && (late.first < 0 || load(true, late));
+                late = tile;
             }
             x = next;
             pages = next_pages;
         }
+        ok = ok && (late.first < 0 || load(true, late));
         if (!ok) *fail_flag = 1;
         // every copy has landed before the CTA may exit (at once in a normal run)
-        if (nq > 0) mbar_wait_warp(&bar[Q_FULL], (nq - 1) & 1, 100000000LL);
-        for (uint32_t i = kt > RING ? kt - RING : 0; i < kt; ++i) {
+        for (int h = 0; h < 2; ++h)
+            if (qany >> h & 1) mbar_wait_warp(&bar[Q_FULL + h], (qodd >> h & 1) ^ 1, 100000000LL);
+        for (uint32_t i = nk > RING ? nk - RING : 0; i < nk; ++i)
             mbar_wait_warp(&bar[K_FULL + i % RING], (i / RING) & 1, 100000000LL);
+        for (uint32_t i = nv > RING ? nv - RING : 0; i < nv; ++i)
             mbar_wait_warp(&bar[V_FULL + i % RING], (i / RING) & 1, 100000000LL);
-        }
-        if (!ok) {  // a K tile whose V was not asked for
-            const uint32_t i = kt;
-            mbar_wait_warp(&bar[K_FULL + i % RING], (i / RING) & 1, 100000000LL);
-        }
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
         constexpr uint32_t IDESC_S = idesc_bf16_f32(128, KT);
@@ -314,35 +360,50 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
             __syncwarp();
         };
         // score tile ks goes to buffer ks % 2, whose P the product two tiles back has read
-        auto next_s = [&](bool last) -> bool {
+        uint32_t qn = 0, qodd = 0;
+        // the 64 rows behind a half are whatever lies there, landed or not: rows of the tile that
+        // nobody reads
+        auto next_s = [&](int h, bool half, bool last) -> bool {
             const int s = ks % RING;
             if (!mbar_wait_warp(&bar[K_FULL + s], (ks / RING) & 1)) return false;
             tc_fence_after();
             const uint32_t lo = k_lo + s * (C::TILE >> 4), d = tbase + (ks & 1) * KT;
+            const uint32_t qa = q_lo + h * (C::QB / 2 >> 4), chunk = (half ? 64 : 128) * 128 >> 4;
             if (elect_one()) {
 #pragma unroll
                 for (int c = 0; c < NCH; ++c)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        tc_mma_f16(d, desc_of(q_lo + c * (128 * 128 >> 4) + k * 2, kSw128DescHi),
+                        tc_mma_f16(d, desc_of(qa + c * chunk + k * 2, kSw128DescHi),
                                    desc_of(lo + c * (KT * 128 >> 4) + k * 2, kSw128DescHi), IDESC_S,
                                    (c | k) != 0);
                 tc_commit(&bar[S_FULL + (ks & 1)]);
                 tc_commit(&bar[K_EMPTY + s]);
-                if (last) tc_commit(&bar[Q_EMPTY]);
+                if (last) {
+                    tc_commit(&bar[Q_EMPTY + h]);
+                    if (!half) tc_commit(&bar[Q_EMPTY + 1]);
+                }
             }
             __syncwarp();
             issued = true;
             ++ks;
             return true;
         };
+        TreeUnit next = open(blockIdx.x);
         for (int u = blockIdx.x; ok && u < n_units && !__any_sync(0xffffffffu, *fail_flag); u += gridDim.x) {
-            const TreeUnit x = open(u);
+            const TreeUnit x = next;
+            next = open(u + gridDim.x);
             const int n = warp_uniform(x.tiles());
             if (n == 0) continue;
-            if (!(ok = mbar_wait_warp(&bar[Q_FULL], nu & 1))) break;
+            const bool half = warp_uniform(x.half);
+            const int h = half ? qn : 0;
+            ok = mbar_wait_warp(&bar[Q_FULL + h], qodd >> h & 1) &&
+                 (half || mbar_wait_warp(&bar[Q_FULL + 1], qodd >> 1 & 1));
+            if (!ok) break;
+            qodd ^= half ? 1u << h : 3u;
+            qn = half ? qn ^ 1 : 0;
             tc_fence_after();
-            ok = next_s(n == 1) && (n < 2 || next_s(n == 2));
+            ok = next_s(h, half, n == 1) && (n < 2 || next_s(h, half, n == 2));
             for (int t = 0; t < n && ok; ++t, ++kv) {
                 const int s = kv % RING;
                 const uint32_t b = kv & 1, p = tbase + b * KT;
@@ -374,7 +435,7 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
                     if (t + 1 == n) tc_commit(&bar[O_FULL]);
                 }
                 __syncwarp();
-                if (t + 2 < n) ok = next_s(t + 3 == n);
+                if (t + 2 < n) ok = next_s(h, half, t + 3 == n);
             }
             ++nu;
         }
@@ -391,14 +452,19 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
         uint32_t g = 0, nu = 0;  // score tiles, units with tokens
         bool ok = true;
         const int tok = row / a.group, hg = row % a.group;
-        uint8_t* stg = sm + C::OFF_STG + (warp - 2) * STAGE;
+        // the nodes that this row sees; a row that is none of the tile's has no say in the masks
+        auto sight = [&](const TreeUnit& x) {
+            const int i = x.i0 + tok;
+            const unsigned long long all = x.q.n >= 64 ? ~0ull : (1ull << x.q.n) - 1;
+            return tok < T && i < x.q.n ? a.sees[x.q.row0 + i] & all : all;
+        };
+        TreeUnit next = open(blockIdx.x);
+        unsigned long long next_see = sight(next);
         for (int u = blockIdx.x; ok && u < n_units && !__any_sync(0xffffffffu, *fail_flag); u += gridDim.x) {
-            const TreeUnit x = open(u);
+            const TreeUnit x = next;
             const int n = warp_uniform(x.tiles()), i = x.i0 + tok;
             const bool live = tok < T && i < x.q.n;
-            // the nodes that this row sees; a row that is none of the tile's has no say in the masks
-            const unsigned long long all = x.q.n >= 64 ? ~0ull : (1ull << x.q.n) - 1;
-            const unsigned long long see = live ? a.sees[x.q.row0 + i] & all : all;
+            const unsigned long long see = next_see;
             const bool work = __any_sync(0xffffffffu, live);  // else nobody reads the warp's rows
             float m = -INFINITY, l = 0.f;
             for (int t = 0; t < n; ++t, ++g) {
@@ -490,6 +556,8 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
                 l = l * alpha + ((r0 + r1) + (r2 + r3));
             }
             if (!ok) break;
+            next = open(u + gridDim.x);
+            next_see = sight(next);
             if (n > 0) {
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar[O_FULL], nu & 1)))) break;
                 tc_fence_after();
@@ -504,67 +572,39 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
             const long long o = !live ? -1
                                 : joined ? slot * HD
                                          : (x.q.row0 + i) * a.o_row + h * a.o_head;
-            // out through the warp's staging, 16 fp32 columns or 32 bf16 at a time: this lane writes
-            // its row's four units and stores unit lane % 4 of rows lane / 4 + 8 j
-            long long to[4];
+            // straight from the registers, a lane its row: 32 columns a time, the next ones' under way
+            // (through staging, so that lanes write side by side: 1,000 cycles for every 32 columns)
+            uint32_t w[2][32];
+            if (n > 0) tmem_ld32(tO, w[0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) to[j] = __shfl_sync(0xffffffffu, o, 8 * j + (lane >> 2));
-            const int un = lane & 3;
-            uint8_t* mine = stg + lane * 64;
-            const int flip = (lane >> 1) & 3;
-#pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
-                uint32_t w[32];
+                uint32_t(&y)[32] = w[c & 1];
                 if (n > 0) {
-                    tmem_ld32(tO + c * 32, w);
-                    tmem_ld_wait_regs(w);
-                    if (c + 1 == HD / 32) {
+                    tmem_ld_wait_regs(y);
+                    if (c + 1 < HD / 32) {
+                        tmem_ld32(tO + (c + 1) * 32, w[(c + 1) & 1]);
+                    } else {
                         tc_fence_before();
                         mbar_arrive(&bar[O_FREE]);
                     }
                 }
+                if (!live) continue;
                 // a row that saw nothing: O holds products of zeros
+                const float f = n > 0 && l > 0.f ? inv : 0.f;
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    w[e] = n > 0 && l > 0.f ? __float_as_uint(__uint_as_float(w[e]) * inv) : 0u;
-                if (!work) continue;
+                for (int e = 0; e < 32; ++e) y[e] = f == 0.f ? 0u : __float_as_uint(__uint_as_float(y[e]) * f);
                 if (joined) {
 #pragma unroll
-                    for (int d = 0; d < 2; ++d) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            *reinterpret_cast<uint4*>(mine + ((j ^ flip) << 4)) =
-                                make_uint4(w[16 * d + 4 * j], w[16 * d + 4 * j + 1], w[16 * d + 4 * j + 2],
-                                           w[16 * d + 4 * j + 3]);
-                        __syncwarp();
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int rr = 8 * j + (lane >> 2);
-                            const uint4 y = *reinterpret_cast<const uint4*>(
-                                stg + rr * 64 + ((un ^ ((rr >> 1) & 3)) << 4));
-                            if (to[j] >= 0)
-                                *reinterpret_cast<uint4*>(a.part + to[j] + c * 32 + d * 16 + un * 4) = y;
-                        }
-                        __syncwarp();
-                    }
+                    for (int j = 0; j < 4; ++j) store8(a.part + o + c * 32 + j * 8, y, j * 8);
                 } else {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        uint32_t y[4];
+                        uint32_t z[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            y[e] = cvt_bf2(__uint_as_float(w[8 * j + 2 * e]), __uint_as_float(w[8 * j + 2 * e + 1]));
-                        *reinterpret_cast<uint4*>(mine + ((j ^ flip) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                            z[e] = cvt_bf2(__uint_as_float(y[8 * j + 2 * e]), __uint_as_float(y[8 * j + 2 * e + 1]));
+                        *reinterpret_cast<uint4*>(a.out + o + c * 32 + j * 8) = make_uint4(z[0], z[1], z[2], z[3]);
                     }
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int rr = 8 * j + (lane >> 2);
-                        const uint4 y =
-                            *reinterpret_cast<const uint4*>(stg + rr * 64 + ((un ^ ((rr >> 1) & 3)) << 4));
-                        if (to[j] >= 0) *reinterpret_cast<uint4*>(a.out + to[j] + c * 32 + un * 8) = y;
-                    }
-                    __syncwarp();
                 }
             }
         }
@@ -578,72 +618,101 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
     if (warp == 1) tmem_dealloc(tbase, C::COLS);
 }
 
-// A sequence's runs joined in their order.  A warp a node and head.
-template <int HD>
+// A sequence's runs joined: a warp a node and head and quarter of the runs, a fourth of them in
+// turn, then the quarters in their order.  Four warps to a CTA, of one node and head where the
+// card has room for as many, else of four (WIDE: no).
+template <int HD, bool WIDE>
 __global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeArgs a) {
     using namespace tree;
-    constexpr int E = HD / 32;
+    constexpr int E = HD / 32, R = 8;  // runs of a warp under way
+    __shared__ float sums[WIDE ? 4 : 1][HD];
     pdl_entry();
-    const int w = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int s = blockIdx.y;
-    int row0, n, old;
-    if (!tree_lengths(a, s, row0, n, old) || w >= n * a.H) return;
-    const TreeSeq x = tree_seq<HD>(a, row0, n, old);
-    if (x.runs == 1) return;
-    const int i = w / a.H, h = w % a.H;
-    const long long at = ((long long)a.base[s] + i) * a.H + h, step = (long long)n * a.H;
-    float m[MAX_RUNS / 32], l[MAX_RUNS / 32], top = -INFINITY, sum = 0.f;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int w = WIDE ? blockIdx.x : blockIdx.x * 4 + warp;
+    const int row = w / a.H, h = w % a.H;
+    if (row >= a.n_rows) return;
+    // a row of no sequence of the launch has no record but what lay there: nothing is read beyond
+    // the workspace for it, and nothing written
+    const int4 x = a.where[row];
+    const int runs = x.z;
+    if (runs <= 1 || runs > MAX_RUNS || x.x < 0 || x.y < 1 || x.y > kMaxNodes ||
+        x.x + (runs - 1) * x.y >= a.places || x.w < a.s0 || x.w >= a.s0 + a.n_seqs)
+        return;
+    int row0, n;
+    const bool known = tree_rows(a.cu_nodes, x.w, a.n_rows, kMaxNodes, row0, n) && row >= row0 && row < row0 + n;
+    const long long at = (long long)x.x * a.H + h, step = (long long)x.y * a.H;
+    float v[R][E], m[2], l[2], top = -INFINITY, sum = 0.f;
+    // runs first, first + by, ...: a warp of four has every fourth
+    constexpr int BY = WIDE ? 4 : 1;
+    const int mine = WIDE ? warp : 0;
+    auto load = [&](int first) {
 #pragma unroll
-    for (int k = 0; k < MAX_RUNS / 32; ++k) {
-        const int r = k * 32 + lane;
-        const float2 y = r < x.runs ? a.ml[at + r * step] : make_float2(-INFINITY, 0.f);
-        m[k] = y.x, l[k] = y.y;
-        top = fmaxf(top, m[k]);
-    }
-    constexpr int R = 8;  // runs under way
-    float v[R][E], acc[E] = {};
-    auto load = [&](int k, int r) {
-        if (r >= x.runs) return;
-        const float* src = a.part + (at + r * step) * HD + lane * E;
+        for (int k = 0; k < R; ++k) {
+            const int r = first + BY * k;
+            if (r >= runs) continue;
+            const float* src = a.part + (at + r * step) * HD + lane * E;
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            const float2 y = *reinterpret_cast<const float2*>(src + e);
-            v[k][e] = y.x, v[k][e + 1] = y.y;
+            for (int e = 0; e < E; e += 2) {
+                const float2 y = *reinterpret_cast<const float2*>(src + e);
+                v[k][e] = y.x, v[k][e + 1] = y.y;
+            }
         }
     };
 #pragma unroll
-    for (int k = 0; k < R; ++k) load(k, k);
+    for (int k = 0; k < 2; ++k) {
+        const int r = k * 32 + lane;
+        const float2 y = r < runs ? a.ml[at + r * step] : make_float2(-INFINITY, 0.f);
+        m[k] = y.x, l[k] = y.y;
+        top = fmaxf(top, m[k]);
+    }
+    load(mine);
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (top == -INFINITY) top = 0.f;  // no run's token was seen
 #pragma unroll
-    for (int k = 0; k < MAX_RUNS / 32; ++k) {
+    for (int k = 0; k < 2; ++k) {
         m[k] = ex2_approx(m[k] - top);
         sum += l[k] * m[k];
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    for (int r = 0; r < x.runs; r += R) {
-        if (r > 0) {
-#pragma unroll
-            for (int k = 0; k < R; ++k) load(k, r + k);
-        }
+    float acc[WIDE ? 1 : 4][E] = {}, all[E];  // the quarters' sums
+    for (int first = mine; first < runs; first += BY * R) {
+        if (first > mine) load(first);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            if (r + k >= x.runs) continue;
-            const float f = __shfl_sync(0xffffffffu, (r + k) >> 5 ? m[1] : m[0], (r + k) & 31);
+            const int r = first + BY * k;
+            if (r >= runs) continue;
+            const float f = __shfl_sync(0xffffffffu, r >> 5 ? m[1] : m[0], r & 31);
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(f, v[k][e], acc[e]);
+            for (int e = 0; e < E; ++e) {
+                float& to = acc[WIDE ? 0 : k & 3][e];  // (R is a multiple of four)
+                to = fmaf(f, v[k][e], to);
+            }
         }
     }
     static_assert(MAX_RUNS == 64, "factors of two registers");
-    uint16_t* o = a.out + (row0 + i) * a.o_row + h * a.o_head + lane * E;
+    if constexpr (WIDE) {
 #pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(o + e) = cvt_bf2(acc[e] * inv, acc[e + 1] * inv);
+        for (int e = 0; e < E; ++e) sums[warp][e * 32 + lane] = acc[0][e];
+        __syncthreads();
+        if (warp > 0) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            all[e] = (sums[0][e * 32 + lane] + sums[1][e * 32 + lane]) + (sums[2][e * 32 + lane] + sums[3][e * 32 + lane]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) all[e] = (acc[0][e] + acc[1][e]) + (acc[2][e] + acc[3][e]);
+    }
+    if (!known) return;
+    uint16_t* o = a.out + row * a.o_row + h * a.o_head + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(o + e) = cvt_bf2(all[e] * inv, all[e + 1] * inv);
 }
 
-static size_t tree_sums_at() { return tree::BATCH * sizeof(int); }
+// The workspace: the rows' records, then (at a sector's border) the sums.
+static size_t tree_sums_at(int n_rows) { return ((size_t)n_rows * sizeof(int4) + 31) & ~(size_t)31; }
 
 template <int HD>
 static jnx_status launch_tree(const jnx_kv_cache& c, const jnx_pages& p, const jnx_head_rows& q, TreeArgs a,
@@ -653,8 +722,9 @@ static jnx_status launch_tree(const jnx_kv_cache& c, const jnx_pages& p, const j
     static std::atomic<uint64_t> attr{0};
     if (set_smem_limit(reinterpret_cast<const void*>(k_tree_attn<HD>), C::SMEM, attr) != cudaSuccess)
         return fail(JNX_ERR_CUDA, "tree attention: smem attribute");
-    CUtensorMap tq, tk, tv;
+    CUtensorMap tq, tq64, tk, tv;
     if (!make_tmap_heads(&tq, q, a.n_rows, a.H, HD, a.group, tile_tokens(a.group)) ||
+        !make_tmap_heads(&tq64, q, a.n_rows, a.H, HD, a.group, 64 / a.group) ||
         !make_tmap_cache(&tk, c.k, c, a.Hkv, HD, a.box) || !make_tmap_cache(&tv, c.v, c, a.Hkv, HD, a.box))
         return fail(JNX_ERR_CUDA, "tree attention: tensor map encode failed");
     const int most = std::min(kMaxNodes, a.n_rows), T = tile_tokens(a.group);
@@ -663,8 +733,10 @@ static jnx_status launch_tree(const jnx_kv_cache& c, const jnx_pages& p, const j
         a.n_seqs = std::min(BATCH, p.n_seqs - s0);
         const long long units = a.n_seqs * runs * a.Hkv * ((most + T - 1) / T);
         const int grid = (int)std::min<long long>(units, (long long)num_sms() * C::CTAS);
-        pdl(k_tree_attn<HD>, grid, THREADS, C::SMEM, s)(tq, tk, tv, a);
-        if (runs > 1) pdl(k_tree_join<HD>, dim3((most * a.H + 3) / 4, a.n_seqs), 128, 0, s)(a);
+        pdl(k_tree_attn<HD>, grid, THREADS, C::SMEM, s)(tq, tq64, tk, tv, a);
+        const int heads = a.n_rows * a.H;
+        if (runs > 1 && heads <= num_sms() * 8) pdl(k_tree_join<HD, true>, heads, 128, 0, s)(a);
+        else if (runs > 1) pdl(k_tree_join<HD, false>, (heads + 3) / 4, 128, 0, s)(a);
     }
     return launched("tree attention");
 }
@@ -677,7 +749,8 @@ extern "C" size_t jnx_op_tree_attention_workspace_bytes(int32_t n_seqs, int32_t 
                                                         int32_t n_heads, int32_t head_dim,
                                                         int64_t max_tokens) {
     if (n_seqs < 0 || n_rows < 0 || n_heads <= 0 || head_dim <= 0 || max_tokens < 0) return 0;
-    return tree_sums_at() + (size_t)n_rows * tree::most_runs(max_tokens) * n_heads * (head_dim + 2) * sizeof(float);
+    return tree_sums_at(n_rows) + 32 +
+           (size_t)n_rows * tree::most_runs(max_tokens) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
 extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx_pages* pages,
@@ -714,8 +787,9 @@ extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx
     TreeArgs a{Pages(*pages, *cache), 0, 0, n_heads, n_kv_heads, n_heads / n_kv_heads, n_rows, box,
                (float)(1.4426950408889634 / sqrt((double)head_dim)), out->ptr, out->row_stride,
                out->head_stride, cu_nodes, n_cached, reinterpret_cast<const unsigned long long*>(sees),
-               static_cast<int*>(workspace), nullptr, nullptr, status};
-    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + tree_sums_at());
+               static_cast<int4*>(workspace), nullptr, nullptr, (int)(n_rows * runs), status};
+    const uintptr_t sums = reinterpret_cast<uintptr_t>(workspace) + tree_sums_at(n_rows) + 31;
+    a.part = reinterpret_cast<float*>(sums & ~(uintptr_t)31);
     a.ml = reinterpret_cast<float2*>(a.part + (size_t)n_rows * runs * n_heads * head_dim);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_TREE_ATTN, 0.0, s);
