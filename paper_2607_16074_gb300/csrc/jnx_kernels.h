@@ -25,13 +25,17 @@ template <class... P>
 struct PdlLaunch {
     void (*kernel)(P...);
     cudaLaunchConfig_t cfg;
+    int cluster = 0;  // CTAs of one, where the kernel does not say
     template <class... A>
     cudaError_t operator()(A&&... a) {
-        cudaLaunchAttribute attr{};
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr.val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
+        cudaLaunchAttribute attr[2]{};
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = cluster ? 2 : 1;
         return cudaLaunchKernelEx(&cfg, kernel, static_cast<A&&>(a)...);
     }
 };
