@@ -166,8 +166,17 @@ __global__ void __launch_bounds__(rope::THREADS)
     using C = rope::Forward<HD>;
     constexpr int E = C::E;
     __shared__ float4 cs[C::TOK * HD / 4];
+    __shared__ long long place[APPEND ? C::TOK : 1];  // where a token's keys go; -1: nowhere
     pdl_entry();
     const int t0 = blockIdx.x * a.tok, nt = min(a.tok, a.n_tokens - t0);
+    if (APPEND && (int)threadIdx.x < nt) {  // (looked up at every row: 39.3 us of 9,000 tokens for 38.3)
+        const int tok = t0 + threadIdx.x;
+        int slot = a.slot[tok], at = a.at[tok];
+        const bool there = TO == rope::PAGES ? a.pages.find(slot, at, slot, at)
+                                             : slot >= 0 && slot < a.n_slots && at >= 0 && at < a.room;
+        place[threadIdx.x] = there ? slot * a.slot_stride + at * a.k_row : -1;
+        if (!there) report(a.status, JNX_ERR_DEVICE_BOUNDS);
+    }
     // rows of the CTA's tokens, token-major; an append's value heads come after the keys'
     const int heads = a.H + (APPEND ? 2 : 1) * a.Hkv;
     const int l = threadIdx.x % C::LPR, part = l * E;  // this lane's elements of each half
@@ -234,14 +243,8 @@ __global__ void __launch_bounds__(rope::THREADS)
         if (is_q) {
             o = a.q + tok * a.q_row + hw * a.q_head;
         } else if (APPEND) {
-            int slot = a.slot[tok], at = a.at[tok];
-            if (TO == rope::PAGES ? !a.pages.find(slot, at, slot, at)
-                                  : slot < 0 || slot >= a.n_slots || at < 0 || at >= a.room) {
-                report(a.status, JNX_ERR_DEVICE_BOUNDS);
-                continue;
-            }
-            o = (is_v ? a.v : a.k) + slot * a.slot_stride + at * a.k_row +
-                (hw - a.H - (is_v ? a.Hkv : 0)) * a.k_head;
+            if (place[tw] < 0) continue;
+            o = (is_v ? a.v : a.k) + place[tw] + (hw - a.H - (is_v ? a.Hkv : 0)) * a.k_head;
         } else {
             o = a.k + tok * a.k_row + (hw - a.H) * a.k_head;
         }

@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(256)
 
 // A row's teacher: the words of its entries in order, their probabilities and the logarithms of
 // these, and where each block's words start.  A warp a row; every entry counts those ahead of
-// it, top^2 comparisons in all.
+// it, 2 top^2 comparisons in all.
 struct VocabTeacher {
     const int* ids;
     const float* logits;
@@ -675,63 +675,78 @@ struct VocabTeacher {
 };
 __global__ void __launch_bounds__(128) k_vocab_teacher(const __grid_constant__ VocabTeacher a) {
     using vocab::TOP;
-    __shared__ int id_s[4][TOP], word_s[4][TOP];
-    __shared__ float x_s[4][TOP];
+    constexpr int NONE = 0x7fffffff;
+    __shared__ int4 id_s[4][TOP / 4], key_s[4][TOP / 4];
+    __shared__ int word_s[4][TOP];
+    __shared__ float x_s[4][TOP], p_s[4][TOP], lp_s[4][TOP];
     pdl_entry();
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * 4 + w;
     if (row >= a.n) return;
-    int* id = id_s[w];
+    int *id = reinterpret_cast<int*>(id_s[w]), *key = reinterpret_cast<int*>(key_s[w]);
     float* x = x_s[w];
     const size_t at = (size_t)row * a.top;
+    const int quads = (a.top + 3) / 4;
     float top = -INFINITY;
-    for (int k = lane; k < a.top; k += 32) {
-        int v = a.ids[at + k];
-        const float l = a.logits[at + k];
-        if (v >= a.vocab) {
-            report(a.status, JNX_ERR_DEVICE_BOUNDS);
-            v = -1;
-        }
-        if (!(l > -INFINITY)) v = -1;
-        id[k] = v;
+    for (int k = lane; k < 4 * quads; k += 32) {
+        int v = k < a.top ? a.ids[at + k] : NONE;
+        const float l = k < a.top ? a.logits[at + k] : -INFINITY;
+        if (k < a.top && v >= a.vocab) report(a.status, JNX_ERR_DEVICE_BOUNDS);
+        if (v < 0 || v >= a.vocab || !(l > -INFINITY)) v = NONE;
+        id[k] = key[k] = v;
         x[k] = l * a.inv_tau;
-        if (v >= 0) top = fmaxf(top, l * a.inv_tau);
+        if (v != NONE) top = fmaxf(top, l * a.inv_tau);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     float z = 0.f;
     __syncwarp();
     for (int k = lane; k < a.top; k += 32)
-        if (id[k] >= 0) z += expf(x[k] - top);
+        if (id[k] != NONE) z += expf(x[k] - top);
 #pragma unroll
     for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
     const float log_z = logf(z);
-    // an entry whose word was given before adds to that one
-    int count = 0;
+    bool twice = false;
     for (int k = lane; k < a.top; k += 32) {
         const int v = id[k];
-        int rank = 0, same = 0;
-        bool again = false;
-        float lp = x[k] - top - log_z, p = expf(lp), sum = p;
-        for (int j = 0; j < a.top; ++j) {
-            const int u = id[j];
-            if (u < 0 || j == k) continue;
-            if (u == v && j < k) again = true;
-            if (u == v && j > k) {
-                sum += expf(x[j] - top - log_z);
-                ++same;
-            }
-            if (u < v) {
-                bool first = true;  // counted once
-                for (int i = 0; i < j && first; ++i) first = id[i] != u;
-                rank += first;
-            }
+        lp_s[w][k] = x[k] - top - log_z;
+        p_s[w][k] = expf(x[k] - top - log_z);
+        int same = 0;
+        for (int j = 0; j < quads; ++j) {
+            const int4 u = id_s[w][j];
+            same += (u.x == v) + (u.y == v) + (u.z == v) + (u.w == v);
         }
-        if (v < 0 || again) continue;
+        twice |= v != NONE && same > 1;
+    }
+    // an entry whose word was given before adds to that one, and is none by itself
+    if (__any_sync(0xffffffffu, twice)) {
+        for (int k = lane; k < a.top; k += 32) {
+            float sum = p_s[w][k];
+            int same = 0;
+            bool again = false;
+            for (int j = 0; j < a.top; ++j) {
+                if (id[j] != id[k] || j == k || id[k] == NONE) continue;
+                if (j < k) again = true;
+                else sum += expf(x[j] - top - log_z), ++same;
+            }
+            if (again) key[k] = NONE;
+            if (same) p_s[w][k] = sum, lp_s[w][k] = logf(sum);
+        }
+        __syncwarp();
+    }
+    int count = 0;
+    for (int k = lane; k < a.top; k += 32) {
+        const int v = key[k];
+        if (v == NONE) continue;
+        int rank = 0;
+        for (int j = 0; j < quads; ++j) {
+            const int4 u = key_s[w][j];
+            rank += (u.x < v) + (u.y < v) + (u.z < v) + (u.w < v);
+        }
         ++count;
         word_s[w][rank] = v;
         a.words[at + rank] = v;
-        a.prob[at + rank] = same ? sum : p;
-        a.log_prob[at + rank] = same ? logf(sum) : lp;
+        a.prob[at + rank] = p_s[w][k];
+        a.log_prob[at + rank] = lp_s[w][k];
     }
     count = __reduce_add_sync(0xffffffffu, count);
     __syncwarp();
@@ -751,75 +766,79 @@ __global__ void __launch_bounds__(128) k_vocab_teacher(const __grid_constant__ V
     }
 }
 
-__device__ __forceinline__ float sum256(float v, float* red) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int w = 0; w < 8; ++w) v += red[w];
-    return v;
-}
-
 // k_vocab_rows with a teacher.  With d = log P - log T at an entry, the loss is the sum of
 // T (e^d - 1 - d) over the entries and of P over all other words: no term is negative, so
 // nothing cancels where the student is near the teacher.  (As sum T (log T - log P), each
-// rounded, a loss under 1e-6 was lost.)  A CTA a row; thread k has entry k.
+// rounded, a loss under 1e-6 was lost.)  A CTA a row; thread k has entry k.  Bound by the
+// probabilities' way through memory: 8,191 rows of 32,000, nine tenths of them with entries, 187
+// us (the next-token losses' 173; with four loads ahead of the sums 211: fewer CTAs an SM).
 __global__ void __launch_bounds__(256)
     k_vocab_rows_teacher(const float2* stats, const __grid_constant__ VocabGemm p,
                          const int* count, const float* prob, const float* log_prob,
                          const float* weight, float inv_tau, float* loss) {
-    __shared__ float red[8];
-    __shared__ int first_top;
+    __shared__ float red[4][8];
     pdl_entry();
-    const int r = blockIdx.x, t = threadIdx.x;
+    const int r = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
     if (r >= vocab_rows(p)) return;
     const int row = p.index[p.r0 + r], n = count[row];
     const int nb = (p.vocab + vocab::BLK - 1) / vocab::BLK;
     const float2* st = stats + (size_t)r * nb;
-    float m = -INFINITY, o = 0.f;
+    uint16_t* out = p.G ? p.G + (size_t)r * ((p.vocab + 63) / 64 * 64) : nullptr;
+    const size_t at = (size_t)row * p.top + t;
+    const float x = t < n ? p.at_target[(size_t)r * p.top + t] : 0.f;
+    float m = -INFINITY;
     for (int b = t; b < nb; b += 256) m = fmaxf(m, st[b].x);
 #pragma unroll
     for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
-    if ((t & 31) == 0) red[t >> 5] = m;
-    if (t == 0) first_top = 256;
+    if (lane == 0) red[0][warp] = m;
     __syncthreads();
-    for (int w = 0; w < 8; ++w) m = fmaxf(m, red[w]);
-    for (int b = t; b < nb; b += 256) o += st[b].y * expf((st[b].x - m) * inv_tau);
-    o = sum256(o, red);
-    const size_t at = (size_t)row * p.top + t;
-    const float below = t < n ? (m - p.at_target[(size_t)r * p.top + t]) * inv_tau : 0.f;
-    const float e = t < n ? expf(-below) : 0.f;
-    // the maximum's own term is one: left out where an entry has it, so that a small rest
-    // keeps its digits
-    if (t < n && below == 0.f) atomicMin(&first_top, t);
+    for (int w = 0; w < 8; ++w) m = fmaxf(m, red[0][w]);
+    // the other words' sum, the entries' below the maximum, and how many have the maximum: their
+    // terms are one, and one of them is left out of what is added to it, so that it keeps its digits
+    float other = 0.f, mine = 0.f;
+    for (int b = t; b < nb; b += 256) other += st[b].y * expf((st[b].x - m) * inv_tau);
+    const float below = t < n ? (m - x) * inv_tau : 0.f, e = t < n ? expf(-below) : 0.f;
+    if (below > 0.f) mine = e;
+    const int at_top = __popc(__ballot_sync(0xffffffffu, t < n && !(below > 0.f)));
+#pragma unroll
+    for (int i = 16; i; i >>= 1) {
+        other += __shfl_xor_sync(0xffffffffu, other, i);
+        mine += __shfl_xor_sync(0xffffffffu, mine, i);
+    }
+    if (lane == 0) red[1][warp] = other, red[2][warp] = mine, red[3][warp] = (float)at_top;
     __syncthreads();
-    const bool sure = first_top < 256;
-    const float rest = o + sum256(t == first_top ? 0.f : e, red);
+    other = mine = 0.f;
+    float tops = 0.f;
+    for (int w = 0; w < 8; ++w) other += red[1][w], mine += red[2][w], tops += red[3][w];
+    const bool sure = tops > 0.f;
+    const float rest = other + mine + (sure ? tops - 1.f : 0.f);
     const float z = sure ? 1.f + rest : rest, log_z = sure ? log1pf(rest) : logf(rest);
-    float g = 0.f, grad = 0.f;
+    float g = 0.f, grad = 0.f;  // by the warps that have entries
     if (t < n) {
-        const float T = prob[at], lt = log_prob[at], d = -below - log_z - lt;
-        const float P = e / z;
-        grad = d < 1.f ? T * expm1f(d) : P - T;
+        const float T = prob[at], d = -below - log_z - log_prob[at];
+        grad = d < 1.f ? T * expm1f(d) : e / z - T;
         g = grad - T * d;
     }
-    const float kl = sum256(g, red) + o / z;
-    if (t == 0) loss[row] = kl;
-    if (!p.G) return;
+#pragma unroll
+    for (int i = 16; i; i >>= 1) g += __shfl_xor_sync(0xffffffffu, g, i);
+    if (lane == 0) red[0][warp] = g;  // (all have read the maxima: a barrier ago)
+    if (!out) {
+        __syncthreads();
+        if (t == 0) loss[row] = ((red[0][0] + red[0][1]) + (red[0][2] + red[0][3])) + other / z;
+        return;
+    }
     const float w = weight[row] * inv_tau, scale = w / z;
-    uint16_t* out = p.G + (size_t)r * ((p.vocab + 63) / 64 * 64);
     for (int c = t * 8; c < p.vocab; c += 2048) {
         const float f = scale * expf((st[c / vocab::BLK].x - m) * inv_tau);
-        const uint4 u = *reinterpret_cast<const uint4*>(out + c);
-        uint32_t v[4] = {u.x, u.y, u.z, u.w};
+        const uint4 y = *reinterpret_cast<const uint4*>(out + c);
+        uint32_t v[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             v[i] = cvt_bf2(f * __uint_as_float(v[i] << 16), f * __uint_as_float(v[i] & 0xffff0000u));
         *reinterpret_cast<uint4*>(out + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
     __syncthreads();
+    if (t == 0) loss[row] = ((red[0][0] + red[0][1]) + (red[0][2] + red[0][3])) + other / z;
     if (t < n) out[p.words[at]] = f2bf(w * grad);
 }
 

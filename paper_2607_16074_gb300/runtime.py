@@ -600,11 +600,27 @@ def _cache(k: torch.Tensor, v: torch.Tensor, heads):
 def _pages(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, seqs: int, heads):
     """Pages [pages, tokens, kv heads, head_dim] and the table [seqs, entries] of the sequences
     that lie in them: jnx_kv_cache's fields, then jnx_pages'."""
+    return *_cache(k, v, heads), *_table(table, seqs)
+
+
+def _table(table: torch.Tensor, seqs: int):
     if table.dtype is not _I32 or table.dim() != 2 or table.shape[0] != seqs or not table.is_cuda or \
             (table.stride(1) != 1 and table.shape[1] > 1):
         _refuse(table, _I32, (seqs, "entries"))
-    n = table.shape[1]
-    return *_cache(k, v, heads), table.data_ptr(), table.stride(0), seqs, n
+    return table.data_ptr(), table.stride(0), seqs, table.shape[1]
+
+
+def _layers(k: torch.Tensor, v: torch.Tensor, heads):
+    """Pages of every layer [layers, pages, tokens, kv heads, head_dim]: jnx_kv_cache's fields of
+    the first, the number of layers and the elements between them."""
+    s, shape = k.stride(), k.shape
+    if s == v.stride() and v.shape == shape and k.dtype is v.dtype is _BF16 and k.is_cuda and \
+            v.is_cuda and shape[3:] == heads and s[4] == 1:
+        return (k.data_ptr(), v.data_ptr(), shape[1], shape[2], *s[1:4]), shape[0], s[0]
+    if shape[0] > 0 and v.shape == shape and (shape[0] == 1 or s[0] == v.stride(0)):
+        return _cache(k[0], v[0], heads), shape[0], s[0]  # (axes of length one)
+    raise ValueError(f"caches of one layout, got {tuple(shape)} strides {s} and {tuple(v.shape)} "
+                     f"strides {v.stride()}")
 
 
 class _Views:
@@ -1043,18 +1059,15 @@ class KeepDrafts(_TextOperator):
         [layers, pages, tokens, Hkv, hd]."""
         b, layers, step = n_cached.shape[0], 1, 0
         if k_pages.dim() == 5:
-            layers, step = k_pages.shape[0], k_pages.stride(0) if k_pages.shape[0] > 1 else 0
-            if v_pages.shape != k_pages.shape or (layers > 1 and v_pages.stride(0) != step):
-                raise ValueError("caches of different layers")
-            if layers == 0:
-                return
-            k_pages, v_pages = k_pages[0], v_pages[0]
-        self._views.fill(*_pages(k_pages, v_pages, table, b, self.dims))
+            cache, layers, step = _layers(k_pages, v_pages, self.dims)
+        else:
+            cache = _cache(k_pages, v_pages, self.dims)
+        self._views.fill(*cache, *_table(table, b))
         r = self._views.refs
         if path.dim() != 2 or path.dtype is not _I32 or path.shape[0] != b or not path.is_cuda or \
                 (path.stride(1) != 1 and path.shape[1] > 1):
             _refuse(path, _I32, (b, "nodes"))
         J.check(self._lib.jnx_op_keep_drafts(
-            r[0], layers, step, r[1], *self.dims, _dense(n_cached, _I32, b), path.data_ptr(),
+            r[0], layers, step if layers > 1 else 0, r[1], *self.dims, _dense(n_cached, _I32, b), path.data_ptr(),
             path.stride(0), _dense(n_kept, _I32, b), path.shape[1],
             self._status, self._on(stream)))
