@@ -1,5 +1,5 @@
 """A text tenant from end to end on one attention layer: trained on the next token, then
-answering token by token.
+answering token by token, and several tokens a step with a drafter that learned from it.
 
     python -m paper_2607_16074_gb300.text_example
 
@@ -8,6 +8,11 @@ layer's projections are frozen, as the shared backbone's are; the tenant trains 
 own, the norms' gains of its query and key heads and its vocabulary.  Random weights and
 samples: the losses show that the gradients go downhill, the answers that a token against
 the cache gives what the whole prompt does.
+
+The drafter guesses the next word from the last one alone, by a vocabulary of its own that
+is distilled from the tenant's best logits.  A step of the drafted answer takes a small tree
+of its guesses through the layer at once, into a paged cache; what the verification accepts
+is kept, so that the answer is the tenant's own in fewer steps.
 """
 from __future__ import annotations
 
@@ -156,6 +161,111 @@ class TextTenant:
         return torch.stack(tokens, 1), torch.stack(seen, 1)
 
 
+class Drafter:
+    """The next word from the last one: its embedding against words of the drafter's own."""
+
+    def __init__(self, tenant, top=8, lr=2e-3, max_rows=1024):
+        self.tenant, self.lr, self.top = tenant, lr, top
+        self.words = (tenant.words * 0.5).contiguous()
+        self.d_words = torch.empty(self.words.shape, device="cuda", dtype=F32)
+        self.adamw = R.TenantAdamW([(self.words, self.d_words)])
+        self.head = R.VocabDistill(self.words[0], max_rows=max_rows, top=top, temperature=1.0)
+
+    def learn(self, ids, logits):
+        """One step towards the tenant's logits [n, vocab] behind the words ids [n] (negative:
+        no word stands there); returns the losses."""
+        n, t = ids.shape[0], self.tenant
+        best = torch.topk(logits, self.top, -1)
+        guesses = torch.where(ids[:, None] >= 0, best.indices, -1).to(I32).contiguous()
+        h = t._norm(t.embed(ids.clamp_min(0)))
+        loss = torch.empty(n, device="cuda", dtype=F32)
+        dh, dw = torch.empty(n, t.d, device="cuda", dtype=BF), torch.empty_like(self.words[0])
+        weight = torch.full((n,), 1.0 / n, device="cuda")
+        self.head.train(h, guesses, best.values.contiguous(), weight, loss, dh, dw)
+        self.head.check()
+        self.d_words[0].copy_(dw)
+        self.adamw.step([0], lr=self.lr)
+        return loss
+
+    def chances(self, ids):
+        t = self.tenant
+        out = torch.empty(ids.shape[0], t.vocab, device="cuda", dtype=F32)
+        return torch.softmax(t._gemm(t._norm(t.embed(ids)), self.words[0], out, J.JNX_EPI_F32), -1)
+
+
+# the root, two guesses behind it, and what follows the first of them
+TREE = (-1, 0, 0, 1, 1, 3)
+
+
+def answer_drafted(tenant, drafter, plan, x, pos, q_lens, steps, tree=TREE, page=16, seed=0,
+                   greedy=True):
+    """At least `steps` tokens behind every packed prompt, as lists, and the passes through the
+    layer that they took.  greedy: the tenant's best word is its only one."""
+    h, hkv, hd = tenant.dims
+    b, t, dev = len(q_lens), len(tree), "cuda"
+    g = torch.Generator(device=dev).manual_seed(seed)
+    depth = [0]
+    for i in range(1, t):
+        depth.append(depth[tree[i]] + 1)
+    sees = [0] * t
+    for i in range(t):
+        sees[i] = (sees[tree[i]] if i else 0) | 1 << i
+    each = lambda v, dtype=I32: torch.tensor(v, device=dev, dtype=dtype).repeat(b)  # noqa: E731
+    parent, sees, depth_t = each(tree), each(sees, torch.int64), each(depth)
+    nodes = torch.arange(t, device=dev, dtype=I32).repeat(b)
+    seq = torch.arange(b, device=dev, dtype=I32).repeat_interleave(t)
+    cu = torch.arange(b + 1, device=dev, dtype=I32) * t
+    up = (seq * t + parent.clamp_min(0)).long()
+    # pages for the prompt, the answer and a last tree, dealt out in turn
+    entries = (max(q_lens) + steps + 2 * t + page - 1) // page
+    table = torch.arange(entries * b, device=dev, dtype=I32).view(entries, b).T.contiguous()
+    kp = torch.empty(entries * b, page, hkv, hd, device=dev, dtype=BF)
+    vp = torch.empty_like(kp)
+    attend = R.TreeAttention(h, hkv, hd, max_batch=b, max_rows=b * t, max_tokens=entries * page)
+    verify, keep = R.VerifyDrafts(tenant.vocab), R.KeepDrafts(hkv, hd)
+
+    y, (_, qkv, q, *_) = tenant.forward(plan, x, pos)
+    of = torch.cat([torch.full((n,), i, device=dev, dtype=I32) for i, n in enumerate(q_lens)])
+    at = torch.cat([torch.arange(n, device=dev, dtype=I32) for n in q_lens])
+    tenant.rope.append_paged(qkv, pos, q, kp, vp, table, of, at)
+    n = torch.tensor(q_lens, device=dev, dtype=I32)
+    last = y[torch.tensor(q_lens, device=dev).cumsum(0) - 1].contiguous()
+    token = tenant.logits(last).argmax(1).to(I32)  # the first word of the answer
+    answers, passes = [[w] for w in token.tolist()], 1
+    path = torch.empty(b, t, device=dev, dtype=I32)
+    kept, word = torch.empty(b, device=dev, dtype=I32), torch.empty(b, device=dev, dtype=I32)
+    while min(map(len, answers)) < steps:
+        tokens = token.repeat_interleave(t)
+        for level in range(1, max(depth) + 1):  # guesses behind guesses
+            q_rows = drafter.chances(tokens)
+            drawn = torch.multinomial(q_rows[up], 1, generator=g)[:, 0].to(I32)
+            tokens = torch.where(depth_t == level, drawn, tokens)
+        chances = drafter.chances(tokens)
+        x1 = tenant.embed(tokens)
+        qkv, q, att = tenant._qkv(x1), tenant._rows(b * t, h), tenant._rows(b * t, h)
+        old = n.repeat_interleave(t)
+        tenant.rope.append_paged(qkv, (old + depth_t).expand(3, b * t).contiguous(), q, kp, vp, table,
+                                 seq, old + nodes)
+        attend.forward(q, kp, vp, table, cu, n, sees, att)
+        logits = tenant.logits(tenant._out(x1, att))
+        p = torch.zeros_like(logits).scatter_(1, logits.argmax(1, keepdim=True), 1.0) if greedy \
+            else torch.softmax(logits, -1)
+        u = torch.rand(b * t, generator=g, device=dev)
+        verify.forward(p, chances, tokens, parent, cu, u, path, kept, word)
+        keep.forward(kp, vp, table, n, path, kept)
+        for i, (nodes_i, k, w) in enumerate(zip(path.tolist(), kept.tolist(), word.tolist())):
+            if len(answers[i]) < steps:
+                answers[i] += [int(tokens[i * t + j]) for j in nodes_i[1:k]] + [w]
+        # a sequence that is through stays where it is
+        done = torch.tensor([len(a) >= steps for a in answers], device=dev)
+        n = torch.where(done, n, n + kept)
+        token = torch.where(done, token, word)
+        passes += 1
+    for op in (tenant.rope, attend, verify, keep):
+        op.check()
+    return [a[:steps] for a in answers], passes
+
+
 def positions(images, texts, grid=4):
     """Time, row and column of each packed row: image patches share their image's time."""
     out = []
@@ -200,5 +310,28 @@ def main(steps=30, images=(16, 12, 0, 20), texts=(24, 40, 7, 33), lr=3e-3, verbo
     return tenant, losses, (x, pos, lens, images, tokens, seen)
 
 
+def drafted(tenant, images, texts, steps=30, answer=12, verbose=True):
+    """A drafter that learns from the tenant on its samples, and answers of both together."""
+    lens = [i + t for i, t in zip(images, texts)]
+    plan, pos = R.PromptPlan(lens, prefix=list(images)), positions(images, texts)
+    drafter = Drafter(tenant)
+    x, targets = samples(tenant, images, texts)
+    # the word of a text row is the last one's target (a sample's first word is not asked about)
+    ids = targets.roll(1)
+    ids[torch.tensor(lens, device="cuda").cumsum(0) - torch.tensor(lens, device="cuda")] = -1
+    y, _ = tenant.forward(plan, x, pos)
+    # ... and what the tenant answers, a few words far
+    tokens, seen = tenant.answer(plan, x, pos, lens, 4)
+    ids = torch.cat([ids, tokens[:, :-1].flatten()])
+    logits = torch.cat([tenant.logits(y), seen[:, 1:].flatten(0, 1)])
+    losses = [float(drafter.learn(ids, logits).mean()) for _ in range(steps)]
+    answers, passes = answer_drafted(tenant, drafter, plan, x, pos, lens, answer)
+    if verbose:
+        print(f"drafter's loss {losses[0]:.4f} -> {losses[-1]:.4f}; {answer} words in {passes} passes: "
+              f"{answers}")
+    return drafter, losses, answers, passes
+
+
 if __name__ == "__main__":
-    main()
+    shapes = dict(images=(16, 12, 0, 20), texts=(24, 40, 7, 33))
+    drafted(main(**shapes)[0], **shapes)
