@@ -19,6 +19,15 @@
 //
 // The run's length depends on the sequence alone, so a sequence's bits do not depend on the
 // others; its runs' sums are joined in their order by a second kernel.
+//
+// 64 trees of up to 12 nodes over up to 8,100 tokens, 32 heads on 8 of 128: 196 us, 5.4 TB/s
+// (floor 158; the attention 192, the join's last CTAs 4).  One of 16 nodes over 60,001 tokens
+// 50.5 (floor 36.5; start, last unit and join 8 or so of it), 8 of up to 6 over up to 700, 8
+// heads on one of 256, 13.6: latency, two launches' chains of lookups, loads, three or four tiles
+// and sums.  24 of up to 64 nodes over up to 3,500: 28, the tensor cores' and softmax's, tiles of
+// 64 tokens for 128 rows (floor 6.7).  With the products the other way round, tokens as the rows
+// and the pairs as 64 columns, so that few pairs cost no more than they are, a unit's sums and
+// epilogue took 12,000 clocks: 260 us for 192 of the 64 trees' attention.
 #include <algorithm>
 
 #include "jnx_dev.cuh"
