@@ -141,13 +141,17 @@ __device__ __forceinline__ void vocab_each32(uint8_t* slot, int lane, const uint
     __syncwarp();
 }
 
-// TEACHER: LOGITS with a teacher's entries as the targets.
-template <int MODE, bool TEACHER = false>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW, 1)
-    k_vocab_gemm(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
-                 const __grid_constant__ VocabGemm p) {
+// TEACHER: LOGITS with a teacher's entries as the targets.  PAIR: a 256 x 256 tile on a CTA
+// pair; else one of 128 x 256 on one CTA.
+template <int MODE, bool TEACHER, bool PAIR>
+__device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtensorMap& tb, const VocabGemm& p) {
     using namespace vocab;
     constexpr bool AMN = MODE == DW, BMN = MODE != LOGITS;
+    static_assert(PAIR || (!AMN && !BMN), "a lone CTA's operands are K-major");
+    constexpr int BM = PAIR ? vocab::BM : vocab::BM / 2;
+    constexpr int STAGES = PAIR ? vocab::STAGES : 4;
+    constexpr int STAGE_BYTES = A_BYTES + (PAIR ? A_BYTES : 2 * A_BYTES);  // one CTA's of a stage
+    static_assert(STAGES * STAGE_BYTES == vocab::STAGES * vocab::STAGE_BYTES, "one shared memory size");
     constexpr uint32_t IDESC =
         idesc_bf16_f32(BM, BN) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u);
     extern __shared__ uint8_t smem_raw[];
@@ -163,7 +167,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(never + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -172,7 +176,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(&tfull[a], 1);
-            mbar_init(&tempty[a], 2 * EW);
+            mbar_init(&tempty[a], (PAIR ? 2 : 1) * EW);
         }
         mbar_init(drain, 1);
         mbar_init(never, 1);
@@ -182,15 +186,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
     }
     pdl_entry();  // TMEM is taken once the grid ahead has given its own back
     if (warp == 1) {
-        tmem_alloc_pair(tmem_slot, 2 * BN);
-        tmem_relinquish_pair();
+        if constexpr (PAIR) {
+            tmem_alloc_pair(tmem_slot, 2 * BN);
+            tmem_relinquish_pair();
+        } else {
+            tmem_alloc(tmem_slot, 2 * BN);
+            tmem_relinquish();
+        }
     }
     if (warp == 0 && lane == 0) {
         tma_prefetch_desc(&ta);
         tma_prefetch_desc(&tb);
     }
     tc_fence_before();
-    cluster_sync_all();
+    if constexpr (PAIR) cluster_sync_all();
+    else __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = warp_uniform(*tmem_slot);
 
@@ -201,7 +211,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
     const int all_k = (K + BK - 1) / BK;
     const int parts = MODE == DH ? p.split : 1;
     const int num_tiles = num_m * num_n * parts;
-    const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    const int first = blockIdx.x >> (PAIR ? 1 : 0), step = gridDim.x >> (PAIR ? 1 : 0);
     // K steps [k0, k1) of a part
     auto k_begin = [&](int part) { return (int)((long long)all_k * part / parts); };
 
@@ -212,7 +222,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
         for (int tile = first; ok && tile < num_tiles && !__any_sync(0xffffffffu, *abort_flag);
              tile += step) {
             const VocabTile t = vocab_tile(tile, num_m, num_n);
-            const int arow = t.mb * BM + rank * 128, brow = t.nb * BN + rank * 128;
+            const int arow = t.mb * BM + (int)rank * 128, brow = t.nb * BN + rank * 128;
             for (int kb = k_begin(t.part); kb < k_begin(t.part + 1); ++kb) {
                 if (!mbar_wait_warp(&empty[stage], phase ^ 1)) {
                     ok = false;
@@ -221,19 +231,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                 if (elect_one()) {
                     uint8_t* sa = smem + stage * STAGE_BYTES;
                     uint8_t* sb = sa + A_BYTES;
-                    const uint32_t bar = map_rank(&full[stage], 0);
-                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * STAGE_BYTES);
-                    if constexpr (AMN) {
-                        tma_load_2d_pair(sa, &ta, arow, kb * BK, bar);
-                        tma_load_2d_pair(sa + A_BYTES / 2, &ta, arow + 64, kb * BK, bar);
+                    if constexpr (!PAIR) {
+                        mbar_arrive_expect_tx(&full[stage], STAGE_BYTES);
+                        tma_load_2d(sa, &ta, kb * BK, arow, &full[stage]);
+                        tma_load_2d(sb, &tb, kb * BK, brow, &full[stage]);
+                        tma_load_2d(sb + A_BYTES, &tb, kb * BK, brow + 128, &full[stage]);
                     } else {
-                        tma_load_2d_pair(sa, &ta, kb * BK, arow, bar);
-                    }
-                    if constexpr (BMN) {
-                        tma_load_2d_pair(sb, &tb, brow, kb * BK, bar);
-                        tma_load_2d_pair(sb + A_BYTES / 2, &tb, brow + 64, kb * BK, bar);
-                    } else {
-                        tma_load_2d_pair(sb, &tb, kb * BK, brow, bar);
+                        const uint32_t bar = map_rank(&full[stage], 0);
+                        if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * STAGE_BYTES);
+                        if constexpr (AMN) {
+                            tma_load_2d_pair(sa, &ta, arow, kb * BK, bar);
+                            tma_load_2d_pair(sa + A_BYTES / 2, &ta, arow + 64, kb * BK, bar);
+                        } else {
+                            tma_load_2d_pair(sa, &ta, kb * BK, arow, bar);
+                        }
+                        if constexpr (BMN) {
+                            tma_load_2d_pair(sb, &tb, brow, kb * BK, bar);
+                            tma_load_2d_pair(sb + A_BYTES / 2, &tb, brow + 64, kb * BK, bar);
+                        } else {
+                            tma_load_2d_pair(sb, &tb, kb * BK, brow, bar);
+                        }
                     }
                 }
                 __syncwarp();
@@ -248,6 +265,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
             report(p.status, JNX_ERR_TIMEOUT);
         }
     } else if (warp == 1 && rank == 0) {
+        auto commit = [](uint64_t* b) {
+            if constexpr (PAIR) tc_commit_pair(b);
+            else tc_commit(b);
+        };
         int stage = 0, local = 0;
         uint32_t phase = 0;
         bool ok = true;
@@ -275,10 +296,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
 #pragma unroll
                     for (int kk = 0; kk < BK / 16; ++kk)
                         // (16 K rows of an MN-major operand are two 8-row atoms)
-                        tc_mma_f16_pair(dcol, desc_of(a_lo + off + kk * (AMN ? 128 : 2), kSw128DescHi),
-                                        desc_of(b_lo + off + kk * (BMN ? 128 : 2), kSw128DescHi), IDESC,
-                                        (kb - k0) | kk);
-                    tc_commit_pair(&empty[stage]);
+                        if constexpr (PAIR)
+                            tc_mma_f16_pair(dcol, desc_of(a_lo + off + kk * (AMN ? 128 : 2), kSw128DescHi),
+                                            desc_of(b_lo + off + kk * (BMN ? 128 : 2), kSw128DescHi), IDESC,
+                                            (kb - k0) | kk);
+                        else
+                            tc_mma_f16(dcol, desc_of(a_lo + off + kk * 2, kSw128DescHi),
+                                       desc_of(b_lo + off + kk * 2, kSw128DescHi), IDESC, (kb - k0) | kk);
+                    commit(&empty[stage]);
                 }
                 __syncwarp();
                 if (++stage == STAGES) {
@@ -287,7 +312,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                 }
             }
             if (!ok) break;
-            if (elect_one()) tc_commit_pair(&tfull[acc]);
+            if (elect_one()) commit(&tfull[acc]);
             __syncwarp();
         }
         if (!ok) {
@@ -295,7 +320,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
             report(p.status, JNX_ERR_TIMEOUT);
         }
         // no MMA still reads or writes either CTA after this
-        if (elect_one()) tc_commit_pair(drain);
+        if (elect_one()) commit(drain);
         __syncwarp();
         mbar_wait(drain, 0);
     } else if (warp == 1) {
@@ -311,6 +336,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
             const int row0 = t.mb * BM + rank * 128 + q * 32, row = row0 + lane;
             const int col0 = t.nb * BN + half * 128;
             const bool summed = k_begin(t.part + 1) > k_begin(t.part);  // else nothing was
+            // a teacher's entries of these columns are places [tg, te) of its words: looked up
+            // while the product is under way, the first two words too (a loop of lookups behind
+            // it: 102 us of 2,047 rows of 1,024 on 32,000 words for 93)
+            constexpr int AHEAD = 2;
+            int tg = 0, te = 0, ahead[TEACHER ? AHEAD : 1];
+            const int* words = nullptr;
+            uint32_t mine = 0;
+            if constexpr (TEACHER) {
+                const int cols = min(BLK, N - col0);
+                if (row < M && cols > 0) {
+                    const size_t src = p.index[p.r0 + row];
+                    const uint8_t* st = p.starts + src * ((N + BLK - 1) / BLK + 1) + col0 / BLK;
+                    tg = st[0], te = st[1];
+                    words = p.words + src * p.top + tg;
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k)
+                        if (tg + k < te) {
+                            ahead[k] = words[k] - col0;
+                            mine |= 1u << (ahead[k] >> 5);
+                        }
+                    for (int k = AHEAD; tg + k < te; ++k) mine |= 1u << ((words[k] - col0) >> 5);
+                }
+            }
             if (!mbar_wait(&tfull[acc], (local >> 1) & 1) || *abort_flag) {
                 *abort_flag = 1;
                 report(p.status, JNX_ERR_TIMEOUT);
@@ -320,23 +368,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
             const uint32_t tc = tmem_base + acc * BN + half * 128 + ((uint32_t)(q * 32) << 16);
             if constexpr (MODE == LOGITS) {
                 const int cols = min(BLK, N - col0);  // may be negative: nothing here
-                // a teacher's entries of these columns are places [tg, te) of its words
-                int tg, te = 0;
-                const int* words = nullptr;
-                uint32_t mine = 0;
-                if constexpr (TEACHER) {
-                    tg = 0;
-                    if (row < M && cols > 0) {
-                        const size_t src = p.index[p.r0 + row];
-                        const uint8_t* st = p.starts + src * ((N + BLK - 1) / BLK + 1) + col0 / BLK;
-                        tg = st[0], te = st[1];
-                        words = p.words + src * p.top;
-                        for (int k = tg; k < te; ++k) mine |= 1u << ((words[k] - col0) >> 5);
-                    }
-                } else {
+                if constexpr (!TEACHER) {
                     tg = row < M ? p.targets[p.r0 + row] - col0 : -1;
                     mine = (unsigned)tg < (unsigned)BLK ? 1u << (tg >> 5) : 0u;
                 }
+                int taken = 0;  // of the teacher's entries
                 // the 32-column chunks that hold a target of the warp's rows
                 const uint32_t hit = __reduce_or_sync(0xffffffffu, mine);
                 float m = -INFINITY, s = 0.f, at = 0.f;
@@ -360,14 +396,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                     // out by way of local memory)
                     if (hit >> c & 1) {
                         if constexpr (TEACHER) {
-                            for (int col; tg < te && ((col = words[tg] - col0) >> 5) == c; ++tg) {
+                            while (tg + taken < te) {
+                                int col = ahead[0];
+#pragma unroll
+                                for (int k = 1; k < AHEAD; ++k)
+                                    if (taken == k) col = ahead[k];
+                                if (taken >= AHEAD) col = words[taken] - col0;
+                                if (col >> 5 != c) break;
 #pragma unroll
                                 for (int e = 0; e < 32; ++e)
                                     if (col == c * 32 + e) {
                                         at = __uint_as_float(v[e]);
                                         v[e] = 0xff800000u;
                                     }
-                                p.at_target[(size_t)row * p.top + tg] = at;
+                                p.at_target[(size_t)row * p.top + tg + taken] = at;
+                                ++taken;
                             }
                             __syncwarp();
                         } else {
@@ -490,7 +533,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
                 tc_fence_before();
             }
             __syncwarp();
-            if (elect_one()) mbar_arrive_cluster(map_rank(&tempty[acc], 0));
+            if (elect_one()) {
+                if constexpr (PAIR) mbar_arrive_cluster(map_rank(&tempty[acc], 0));
+                else mbar_arrive(&tempty[acc]);
+            }
             __syncwarp();
         }
     }
@@ -501,9 +547,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW,
     // giving up: time for copies in flight to land before any CTA leaves
     if (*abort_flag && warp == 0) mbar_wait(never, 0, 100000000LL);
     __syncthreads();
-    cluster_sync_all();
+    if constexpr (PAIR) cluster_sync_all();
     tc_fence_after();
-    if (warp == 1) tmem_dealloc_pair(tmem_base, 2 * BN);
+    if (warp == 1) {
+        if constexpr (PAIR) tmem_dealloc_pair(tmem_base, 2 * BN);
+        else tmem_dealloc(tmem_base, 2 * BN);
+    }
+}
+
+template <int MODE, bool TEACHER = false>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW, 1)
+    k_vocab_gemm(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
+                 const __grid_constant__ VocabGemm p) {
+    vocab_tiles<MODE, TEACHER, true>(ta, tb, p);
+}
+
+// The logits of few rows against a teacher: blocks of 128 rows on single CTAs.
+__global__ void __launch_bounds__(64 + 32 * vocab::EW, 1)
+    k_vocab_teacher_gemm(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
+                         const __grid_constant__ VocabGemm p) {
+    vocab_tiles<vocab::LOGITS, true, false>(ta, tb, p);
 }
 
 constexpr int kCountRows = 8192;
@@ -880,6 +943,24 @@ static jnx_status vocab_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const
     return launched(what);
 }
 
+// Against a teacher, tiles of 128 rows on lone CTAs where they take fewer rounds of the card than
+// pairs' of 256, each as long: 333 rows of 1,024 on 32,000 words three for four (21 us for 26), up
+// to 128 one for two (12.7 for 17.5).  Equal rounds go to the pairs, which read the words half as often.
+static jnx_status vocab_logits(const CUtensorMap& th, const CUtensorMap& tw, const VocabGemm& p,
+                               const char* what, cudaStream_t s) {
+    using namespace vocab;
+    const int sms = num_sms();
+    const long long cols = (p.vocab + BN - 1) / BN;
+    const long long pairs = (p.rows_max + BM - 1) / BM * cols, lone = (p.rows_max + BM / 2 - 1) / (BM / 2) * cols;
+    if ((lone + sms - 1) / sms >= (pairs + sms / 2 - 1) / (sms / 2))
+        return vocab_gemm<LOGITS, true>(th, tw, p, what, s);
+    static std::atomic<uint64_t> attr{0};
+    if (set_smem_limit(reinterpret_cast<const void*>(k_vocab_teacher_gemm), SMEM, attr) != cudaSuccess)
+        return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
+    pdl(k_vocab_teacher_gemm, (int)std::min<long long>(lone, sms), 64 + 32 * EW, SMEM, s)(th, tw, p);
+    return launched(what);
+}
+
 static jnx_status vocab_check(const void* h, int64_t ldh, const void* w, int64_t ldw,
                               const void* targets, int n_rows, int vocab, int d, const void* loss,
                               const char* what) {
@@ -1076,7 +1157,7 @@ static jnx_status vocab_run(const uint16_t* h, int64_t ldh, const uint16_t* w, i
             p.starts = ws.starts;
             p.top = teacher->top;
             p.log2e = 1.4426950408889634f * teacher->inv_tau;
-            if (jnx_status st = vocab_gemm<LOGITS, true>(th, tw, p, what, s)) return st;
+            if (jnx_status st = vocab_logits(th, tw, p, what, s)) return st;
             pdl(k_vocab_rows_teacher, rows, 256, 0, s)(ws.stats, p, ws.entries, ws.prob, ws.log_prob,
                                                        weight, teacher->inv_tau, loss);
         } else {

@@ -639,6 +639,17 @@ def test_distill(n, d, v, k, tau):
     check_distill(*distill_case(n, d, v, k, seed=n), tau=tau)
 
 
+@pytest.mark.parametrize("n", [1, 77, 128, 129, 333, 640])
+@pytest.mark.parametrize("v", [19_999, 32_000])
+def test_distill_few_rows_of_many_words(n, v):
+    """More blocks of columns than the card takes at a time: tiles of 128 rows, or of 256."""
+    h, w, ids, t, rw = distill_case(n, 72, v, 17, seed=n)
+    if n > 8:
+        ids[3::8] = -1
+        h[3::8] = float("nan")
+    check_distill(h, w, ids, t, rw, tau=0.7)
+
+
 def test_distill_rows_and_entries_that_do_not_count():
     """Negative ids, logits of -inf, rows without entries whose h may be NaN, in pieces."""
     h, w, ids, t, rw = distill_case(300, 128, 900, 20, seed=1)
