@@ -25,6 +25,8 @@
 // the products 1,040, 1,175 and 1,070 each by itself, the rows 150.  333 rows of 2,048 without
 // gradients: 48 us, of which the logits 46 by themselves, two row blocks of 256 for 1.3 and four
 // rounds of tiles for 3.3.
+// Against a teacher's 32 entries a row, 8,191 rows of 2,048: 1,940 us (floor 1,671), the products
+// 505, 545 and 510, the rows 187; 333 rows of 1,024 without gradients 33, the logits 21.
 #include <algorithm>
 
 #include "jnx_dev.cuh"
