@@ -231,19 +231,21 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
     auto open = [&](int u) {
         TreeUnit x{};
         if (u >= n_units) return x;
-        int lo = 0, hi = a.n_seqs - 1;  // the last s with first[s] <= u
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (first[mid] <= u) lo = mid;
-            else hi = mid - 1;
+        int lo = -1;  // the last s with first[s] <= u, by all lanes
+        for (int b = 0; b < a.n_seqs; b += 32) {
+            const uint32_t ahead = __ballot_sync(0xffffffffu, b + lane < a.n_seqs && first[b + lane] <= u);
+            if (ahead) lo = b + 31 - __clz(ahead);
+            if (ahead != 0xffffffffu) break;
         }
         x.s = lo;
         const int old = olds[lo], nn = nodes[lo];
         x.q = TreeSeq{rows0[lo], nn, old, old < 0 ? 0 : old + nn, run_of[lo], runs_of[lo], tiles_of[lo]};
         int rest = u - first[lo];  // a run's tiles lie together, then its heads
-        x.i0 = rest % x.q.tiles * T;
+        if (x.q.tiles > 1) {
+            x.i0 = rest % x.q.tiles * T;
+            rest /= x.q.tiles;
+        }
         x.half = min(x.q.n - x.i0, T) * a.group <= 64;
-        rest /= x.q.tiles;
         x.kvh = rest % a.Hkv;
         x.run = rest / a.Hkv;
         x.at = x.run * x.q.run;
@@ -461,11 +463,11 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
         uint32_t g = 0, nu = 0;  // score tiles, units with tokens
         bool ok = true;
         const int tok = row / a.group, hg = row % a.group;
-        // the nodes that this row sees; a row that is none of the tile's has no say in the masks
+        // the bits of what this row sees, asked for ahead of the epilogue; a row that is none of the
+        // tile's has no say in the masks
         auto sight = [&](const TreeUnit& x) {
             const int i = x.i0 + tok;
-            const unsigned long long all = x.q.n >= 64 ? ~0ull : (1ull << x.q.n) - 1;
-            return tok < T && i < x.q.n ? a.sees[x.q.row0 + i] & all : all;
+            return tok < T && i < x.q.n ? a.sees[x.q.row0 + i] : ~0ull;
         };
         TreeUnit next = open(blockIdx.x);
         unsigned long long next_see = sight(next);
@@ -473,7 +475,7 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
             const TreeUnit x = next;
             const int n = warp_uniform(x.tiles()), i = x.i0 + tok;
             const bool live = tok < T && i < x.q.n;
-            const unsigned long long see = next_see;
+            const unsigned long long see = next_see & (x.q.n >= 64 ? ~0ull : (1ull << x.q.n) - 1);
             const bool work = __any_sync(0xffffffffu, live);  // else nobody reads the warp's rows
             float m = -INFINITY, l = 0.f;
             for (int t = 0; t < n; ++t, ++g) {
@@ -645,7 +647,7 @@ __global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeA
     const int4 x = a.where[row];
     const int runs = x.z;
     if (runs <= 1 || runs > MAX_RUNS || x.x < 0 || x.y < 1 || x.y > kMaxNodes ||
-        x.x + (runs - 1) * x.y >= a.places || x.w < a.s0 || x.w >= a.s0 + a.n_seqs)
+        (long long)x.x + (runs - 1) * x.y >= a.places || x.w < a.s0 || x.w >= a.s0 + a.n_seqs)
         return;
     int row0, n;
     const bool known = tree_rows(a.cu_nodes, x.w, a.n_rows, kMaxNodes, row0, n) && row >= row0 && row < row0 + n;

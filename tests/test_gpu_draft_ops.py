@@ -371,6 +371,24 @@ def test_tree_workspace_holds_anything():
     assert torch.equal(c.run(op), want)
 
 
+@pytest.mark.parametrize("first", [0, 5, 2 ** 31 - 1, -1])
+@pytest.mark.parametrize("number", [0, 1, 7])
+def test_tree_rows_of_nobody_whatever_the_workspace_held(first, number):
+    """Rows that no sequence has are left as they were, though the workspace may hold what looks
+    like an earlier call's record of them."""
+    c = Trees((8, 2, 128), 16, [900, 700], [3, 9], seed=4)
+    n = 40  # rows of the call
+    q = torch.cat([c.q, normal(gen(0), n - 12, 8, 128)])
+    sees = torch.cat([c.sees, c.sees.new_ones(n - 12)])
+    op = _r().TreeAttention(8, 2, 128, 2, n, c.table.shape[1] * 16)
+    op.ws[:16 * n].view(I32).view(n, 4).copy_(ints(first, 64, 64, number))
+    out = torch.full_like(q, 7.0)
+    op.forward(q, c.kp, c.vp, c.table, c.cu, c.n, sees, out)
+    op.check()
+    c.compare(out[:12])
+    assert (out[12:] == 7).all()
+
+
 # ---------------------------------------------------------------- verification
 
 def verify_case(vocab, nodes, seed=0, certain=False, chain=False, sharp=3.0, near=0.7, ld=0, drawn=True):
