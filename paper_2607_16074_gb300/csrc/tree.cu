@@ -20,14 +20,18 @@
 // The run's length depends on the sequence alone, so a sequence's bits do not depend on the
 // others; its runs' sums are joined in their order by a second kernel.
 //
-// 64 trees of up to 12 nodes over up to 8,100 tokens, 32 heads on 8 of 128: 196 us, 5.4 TB/s
-// (floor 158; the attention 192, the join's last CTAs 4).  One of 16 nodes over 60,001 tokens
-// 50.5 (floor 36.5; start, last unit and join 8 or so of it), 8 of up to 6 over up to 700, 8
-// heads on one of 256, 13.6: latency, two launches' chains of lookups, loads, three or four tiles
-// and sums.  24 of up to 64 nodes over up to 3,500: 28, the tensor cores' and softmax's, tiles of
-// 64 tokens for 128 rows (floor 6.7).  With the products the other way round, tokens as the rows
-// and the pairs as 64 columns, so that few pairs cost no more than they are, a unit's sums and
-// epilogue took 12,000 clocks: 260 us for 192 of the 64 trees' attention.
+// 64 trees of up to 12 nodes over up to 8,100 tokens, 32 heads on 8 of 128: 188 us, 5.7 TB/s
+// (floor 158; the attention 184, the join's last CTAs 4).  One of 16 nodes over 60,001 tokens
+// 50.3 (floor 36.5; start, last unit and join 8 or so of it), 8 of up to 6 over up to 700, 8
+// heads on one of 256, 13: latency, two launches' chains of lookups, loads, three or four tiles
+// and sums.  24 of up to 64 nodes over up to 3,500: 28.8, the tensor cores' and softmax's, tiles
+// of 64 tokens for 128 rows (floor 6.7).
+//
+// Not kept: the products the other way round, tokens as the rows and the pairs as 64 columns, so
+// that few pairs cost no more than they are (a unit's sums and epilogue took 12,000 clocks: 260 us
+// for 192 of the 64 trees' attention); tiles of 128 tokens at head dim 64 (64 of up to 20,000
+// tokens, 14 heads on 2: 104 us for 90); S of the next unit ahead of this one's last products, or
+// sequences in the order of their runs' lengths (no change, or 200 us for 195).
 #include <algorithm>
 
 #include "jnx_dev.cuh"
@@ -50,14 +54,21 @@ enum { K_FULL = 0, K_EMPTY = K_FULL + RINGS, V_FULL = K_EMPTY + RINGS, V_EMPTY =
 
 __host__ __device__ inline int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
-// Tokens of a run of L, for `rows` rows of a tile and `units` units of a run: a run's sums are
+// Tokens of a run of L, for `rows` rows of a tile and `units` units of a run.  A run's sums are
 // rows / tokens of what it reads, and its epilogue costs what two or three tiles do, hence long
-// runs of long sequences (64 trees over up to 8,100 tokens: 256 us with 16 rows' worth of tokens,
-// 196 with 32 or 1,024 at most, 230 with 64) and of short ones as many as reach more SMs (8 over
-// up to 700: 13.6 us, 20 with 32 rows' worth).  A sequence that fills the card by itself has
-// whole rounds of units.
-__host__ __device__ inline int run_tokens(int L, int rows, int units, int slots) {
-    int least = L <= 2048 ? 4 * rows : 32 * rows < 1024 ? 32 * rows : 1024;
+// runs of long sequences (64 trees over up to 8,100 tokens 188 us; 197 with 32 times the rows, 184
+// with 1,024 tokens of any, which takes a lone sequence of 4,000 18 us for 13.6), and as many of
+// short ones as reach more SMs (8 over up to 700 tokens 13 us, 20 with 32 times the rows).  At
+// head dim 256, where a tile's products are longer than its way from memory, a sequence of few
+// heads has runs for a fifth of the card (8 nodes over 8,000 tokens, one key head: 13.4 us, 22.6
+// without).  One that fills the card by itself has whole rounds of units.
+__host__ __device__ inline int run_tokens(int L, int rows, int units, int slots, bool wide) {
+    int least = L <= 2048 ? 4 * rows : L <= 4096 ? (8 * rows < 512 ? 512 : 8 * rows) : 1024;
+    if (wide && L > 2048) {
+        const int share = (int)((long long)L * units / 32 < 1024 ? (long long)L * units / 32 : 1024);
+        const int sums = (units > 1 || rows > 64 ? 8 : 4) * rows;
+        least = share > sums ? share : sums;
+    }
     least = round_up(least < 256 ? 256 : least, KT);
     int n = (L + least - 1) / least;
     if (n > MAX_RUNS) n = MAX_RUNS;
@@ -65,7 +76,7 @@ __host__ __device__ inline int run_tokens(int L, int rows, int units, int slots)
     if (n < 1) n = 1;
     return round_up((L + n - 1) / n, KT);
 }
-// More runs than any sequence of up to max_tokens has.
+// No sequence of up to max_tokens has more runs.
 inline long long most_runs(long long max_tokens) {
     return std::max(1ll, std::min<long long>(MAX_RUNS, (max_tokens + 255) / 256));
 }
@@ -114,7 +125,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& a, int row0, int n, 
     x.tiles = (n + T - 1) / T;
     if (n > 0 && old >= 0) {  // else no token is seen
         x.L = old + n;
-        x.run = tree::run_tokens(x.L, min(n, T) * a.group, a.Hkv * x.tiles, TreeCfg<HD>::SLOTS);
+        x.run = tree::run_tokens(x.L, min(n, T) * a.group, a.Hkv * x.tiles, TreeCfg<HD>::SLOTS, HD == 256);
         x.runs = (x.L + x.run - 1) / x.run;
     }
     return x;
