@@ -58,7 +58,7 @@ def pages_for(seed, lens, page, hkv, hd, spare=2):
 
 
 def place(table, page, b, tokens):
-    t = torch.as_tensor(tokens, device="cuda")
+    t = torch.as_tensor(tokens, device="cuda", dtype=torch.int64)
     return table[b].long()[t // page], t % page
 
 
@@ -243,6 +243,42 @@ def test_tree_does_not_depend_on_the_batch():
         op.check()
         assert torch.equal(one, out[rows])
     assert torch.equal(out, c.run())
+
+
+def test_tree_of_more_sequences_than_a_launch_takes():
+    rng = random.Random(5)
+    old = [rng.choice([0, 3, 70, 300, 900]) for _ in range(600)]
+    nodes = [rng.choice([0, 1, 2, 5, 17]) for _ in range(600)]
+    c = Trees((4, 1, 64), 16, old, nodes, seed=6)
+    out = c.run()
+    c.compare(out)
+    # a sequence of the last launch alone
+    b = max(i for i in range(600) if nodes[i] > 1 and old[i] == 900)
+    one, rows = empty(nodes[b], 4, 64), c.rows(b)
+    op = _r().TreeAttention(4, 1, 64, 1, 17, c.table.shape[1] * 16)
+    op.forward(c.q[rows].contiguous(), c.kp, c.vp, c.table[b:b + 1], ints(0, nodes[b]), c.n[b:b + 1],
+               c.sees[rows], one)
+    assert torch.equal(one, out[rows])
+
+
+def test_tree_sequences_that_share_their_past():
+    """One past for all, by a table whose rows are the same, and pages of their own behind it."""
+    heads, (h, hkv, hd) = (8, 2, 128), (8, 2, 128)
+    c = Trees(heads, 16, [320], [6], seed=8)
+    n, past = 3, c.table[0, :20]
+    kp, vp = empty(c.kp.shape[0] + 2 * n, 16, hkv, hd), empty(c.kp.shape[0] + 2 * n, 16, hkv, hd)
+    kp[:c.kp.shape[0]], vp[:c.kp.shape[0]] = c.kp, c.vp
+    table = torch.cat([past.expand(n, 20), ints(*range(c.kp.shape[0], c.kp.shape[0] + n))[:, None]], 1)
+    g = gen(3)
+    for b in range(n):
+        kp[table[b, 20].long(), :6], vp[table[b, 20].long(), :6] = normal(g, 6, hkv, hd), normal(g, 6, hkv, hd)
+    q, out = normal(g, 6 * n, h, hd, std=1.5), empty(6 * n, h, hd)
+    op = _r().TreeAttention(*heads, n, 6 * n, 21 * 16)
+    op.forward(q, kp, vp, table.contiguous(), ints(0, 6, 12, 18), ints(320, 320, 320), c.sees.repeat(n), out)
+    op.check()
+    for b in range(n):
+        where = place(table, 16, b, range(326))
+        T.close(out[6 * b:6 * b + 6], *D.tree(q[6 * b:6 * b + 6], kp[where], vp[where], 320, c.masks[0]))
 
 
 def test_tree_strides_and_rows_of_nobody():
