@@ -704,6 +704,19 @@ def test_distill_few_rows_of_many_words(n, v):
     check_distill(h, w, ids, t, rw, tau=0.7)
 
 
+@pytest.mark.parametrize("d", [1000, 2048])
+@pytest.mark.parametrize("v,k", [(1000, 100), (32_000, 16), (1000, 1)])
+def test_distill_digits_of_many_terms(d, v, k):
+    """Sums on the tensor cores lose up to 2^-23 of themselves at each of d / 16 steps, towards
+    zero: a fourth of 2^-24 on average, and so 2^-30 d of a logit, 2^-19 at d = 2,048, which the
+    loss of a sharp student has too.  Half of it may be left by the average's correction, and half
+    as much again by the exponentials and logarithms at d = 1,000: 2^-20 of the losses."""
+    h, w, ids, t, rw = distill_case(512, d, v, k, seed=d)
+    loss, *_ = check_distill(h, w, ids, t, rw, tau=0.5)
+    want = D.distill(h, w, ids, t, 0.5)["loss"]
+    assert float((loss.double() - want).norm()) <= 2.0 ** -20 * float(want.norm())
+
+
 def test_distill_rows_and_entries_that_do_not_count():
     """Negative ids, logits of -inf, rows without entries whose h may be NaN, in pieces."""
     h, w, ids, t, rw = distill_case(300, 128, 900, 20, seed=1)
