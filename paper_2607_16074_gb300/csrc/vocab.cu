@@ -793,19 +793,26 @@ __global__ void __launch_bounds__(128) k_vocab_teacher(const __grid_constant__ V
         }
         twice |= v != NONE && same > 1;
     }
-    // an entry whose word was given before adds to that one, and is none by itself
+    // an entry whose word was given before adds to that one, and is none by itself.  The
+    // logarithm is of what the word's entries are to the largest of them: their probabilities
+    // may all be zero in 32 bits, as a row's that is filled up with a word
     if (__any_sync(0xffffffffu, twice)) {
         for (int k = lane; k < a.top; k += 32) {
-            float sum = p_s[w][k];
+            if (id[k] == NONE) continue;
+            float sum = p_s[w][k], high = x[k];
             int same = 0;
             bool again = false;
             for (int j = 0; j < a.top; ++j) {
-                if (id[j] != id[k] || j == k || id[k] == NONE) continue;
+                if (id[j] != id[k] || j == k) continue;
                 if (j < k) again = true;
-                else sum += expf(x[j] - top - log_z), ++same;
+                else sum += expf(x[j] - top - log_z), high = fmaxf(high, x[j]), ++same;
             }
             if (again) key[k] = NONE;
-            if (same) p_s[w][k] = sum, lp_s[w][k] = logf(sum);
+            if (again || !same) continue;
+            float parts = 0.f;
+            for (int j = k; j < a.top; ++j)
+                if (id[j] == id[k]) parts += expf(x[j] - high);
+            p_s[w][k] = sum, lp_s[w][k] = high - top - log_z + logf(parts);
         }
         __syncwarp();
     }

@@ -1,0 +1,27 @@
+"""What calls of the drafted tokens' operators may hold beside the ordinary: teachers' entries
+that weigh nothing, students at their teacher, products with few terms, probabilities that are
+none, layouts whose strides run backwards, sequences that share rows, caches without pages."""
+import pytest
+import torch
+
+from tests import draft_ops_ref as D
+from tests import text_ops_ref as T
+from tests.test_gpu_draft_ops import (BF, F32, HEADS, I32, Trees, _r, _reports, by_hand, check_distill, distill_case,
+                                      empty, gen, ints, normal, run_verify, verify_case)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- distillation
+
+@pytest.mark.parametrize("far", [-90.0, -104.0, -120.0, -1e4, -1e9, -1e30])
+def test_distill_words_given_twice_far_below_the_top(far):
+    """Rows filled up with one word, as a padded batch has them: all of its entries together
+    weigh nothing, or almost nothing, and the loss is that of the others."""
+    h, w, ids, t, rw = distill_case(60, 64, 300, 8, seed=3)
+    ids[:, 5:], t[:, 5:] = 0, far
+    ids[10:20, 2] = 0  # the word of the filling is one of the row's own as well
+    ids[20:30, 4], t[20:30, 4] = 299, far - 1.0  # entries by themselves that weigh nothing
+    ids[30:40, 1:], t[30:40, 1:] = 17, far
+    loss, *_ = check_distill(h, w, ids, t, rw)
+    assert loss.isfinite().all()
