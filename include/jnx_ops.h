@@ -351,11 +351,12 @@ jnx_status jnx_op_vocab_loss_train(const uint16_t* h, int64_t ldh, const uint16_
 
 /* The same against a teacher's top logits.  Row i has up to `top` entries (1 to 128): words
  * ids[i * top + k] with the teacher's logits teacher[i * top + k]; a negative id or a logit
- * of -inf is no entry, an id >= vocab is reported and read as none, an id given twice has
- * both entries' probability.  With T = softmax(teacher / temperature) over the row's entries
- * and P = softmax(h w^T / temperature) over the vocabulary, loss[i] = sum_k T_k (log T_k -
- * log P_k); 0 for a row without entries, whose h is not read into any sum.  Logits over
- * the temperature are finite or -inf; temperature > 0.  Otherwise as the next-token losses. */
+ * that is -inf over the temperature in fp32 is no entry, an id >= vocab is reported and read
+ * as none, an id given twice has both entries' probability.  With T = softmax(teacher /
+ * temperature) over the row's entries and P = softmax(h w^T / temperature) over the
+ * vocabulary, loss[i] = sum_k T_k (log T_k - log P_k); 0 for a row without entries, whose h
+ * is not read into any sum.  Logits over the temperature are finite or -inf; temperature > 0.
+ * Otherwise as the next-token losses. */
 size_t jnx_op_vocab_distill_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t d, int32_t top);
 jnx_status jnx_op_vocab_distill(const uint16_t* h, int64_t ldh, const uint16_t* w, int64_t ldw,
                                 const int32_t* ids, const float* teacher, int32_t top,

@@ -765,12 +765,12 @@ __global__ void __launch_bounds__(128) k_vocab_teacher(const __grid_constant__ V
     float top = -INFINITY;
     for (int k = lane; k < 4 * quads; k += 32) {
         int v = k < a.top ? a.ids[at + k] : NONE;
-        const float l = k < a.top ? a.logits[at + k] : -INFINITY;
+        const float l = (k < a.top ? a.logits[at + k] : -INFINITY) * a.inv_tau;
         if (k < a.top && v >= a.vocab) report(a.status, JNX_ERR_DEVICE_BOUNDS);
         if (v < 0 || v >= a.vocab || !(l > -INFINITY)) v = NONE;
         id[k] = key[k] = v;
-        x[k] = l * a.inv_tau;
-        if (v != NONE) top = fmaxf(top, l * a.inv_tau);
+        x[k] = l;
+        if (v != NONE) top = fmaxf(top, l);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(256)
     if (t < n) {
         const float T = prob[at], d = -below - log_z - log_prob[at];
         grad = d < 1.f ? T * expm1f(d) : e / z - T;
-        g = grad - T * d;
+        g = grad - (T > 0.f ? T * d : 0.f);  // (where T is zero d may be beyond range)
     }
 #pragma unroll
     for (int i = 16; i; i >>= 1) g += __shfl_xor_sync(0xffffffffu, g, i);

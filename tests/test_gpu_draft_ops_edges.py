@@ -25,3 +25,25 @@ def test_distill_words_given_twice_far_below_the_top(far):
     ids[30:40, 1:], t[30:40, 1:] = 17, far
     loss, *_ = check_distill(h, w, ids, t, rw)
     assert loss.isfinite().all()
+
+
+@pytest.mark.parametrize("tau", [0.5, 0.25])
+def test_distill_logits_beyond_range_over_the_temperature(tau):
+    """A logit whose quotient by the temperature is -inf in 32 bits is no entry."""
+    h, w, ids, t, rw = distill_case(40, 64, 300, 6, seed=4)
+    t[:, 4] = -3.0e38
+    t[3::5] = -3.0e38
+    t[7] = -3.4e38
+    t[11, 1:], t[11, 0] = -2.0e38 * tau, 1.6e38 * tau  # (their difference is beyond range)
+    want = torch.where(t == t.clamp_min(-1e30), t, -float("inf"))
+    op = _r().VocabDistill(w, 40, 6, tau)
+    loss, again, dh, dw = empty(40, dtype=F32), empty(40, dtype=F32), empty(40, 64), empty(300, 64)
+    op.loss(h, ids, t, loss)
+    op.train(h, ids, t, rw, again, dh, dw)
+    op.check()
+    r = D.distill(h, w, ids, want, tau, rw)
+    T.close(loss, r["loss"], r["loss_tol"], "loss")
+    T.close(again, r["loss"], r["loss_tol"], "loss of the step")
+    T.close(dh, r["dh"], r["dh_tol"], "dh")
+    T.close(dw, r["dw"], r["dw_tol"], "dw")
+    assert (loss[3::5] == 0).all() and not dh[3::5].any()
