@@ -434,8 +434,8 @@ jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx_pages* pag
  * them.  A sequence of no nodes has n_kept 0 and next -1.  Left out and reported: sequences
  * whose rows are not among n_rows or more than max_nodes (as of no nodes), nodes whose parent
  * is not ahead of them or whose token is no word (never accepted), sums that are not finite
- * and positive (next -1). p and q are not negative; max_nodes in 1 to 64.  Sums are kept to
- * 2^-44 of themselves or closer. */
+ * and positive, as of a row of p or q with a NaN (next -1).  p and q are not negative;
+ * max_nodes in 1 to 64.  Sums are kept to 2^-44 of themselves or closer. */
 jnx_status jnx_op_verify_drafts(const float* p, int64_t ldp, const float* q, int64_t ldq,
                                 const int32_t* tokens, const int32_t* parent, const float* u,
                                 const int32_t* cu_nodes, int32_t n_seqs, int32_t n_rows,

@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(verify::THREADS)
             summed = true;
         }
         if (!summed) left = total();
-        if (k > 0 && !(left.hi > 0.f)) {
+        if (k > 0 && left.hi == 0.f) {  // (a NaN is not nothing: it is reported below)
             k = 0;
             held_k = -1;
             tried = 0;

@@ -47,3 +47,38 @@ def test_distill_logits_beyond_range_over_the_temperature(tau):
     T.close(dh, r["dh"], r["dh_tol"], "dh")
     T.close(dw, r["dw"], r["dw_tol"], "dw")
     assert (loss[3::5] == 0).all() and not dh[3::5].any()
+
+
+# ---------------------------------------------------------------- verification
+
+@pytest.mark.parametrize("vocab", [50, 5000, 40_000])
+@pytest.mark.parametrize("where", ["drafted", "other", "both"])
+@pytest.mark.parametrize("children", [1, 3])
+def test_verify_nan_in_the_drafters_chances_is_reported(vocab, where, children):
+    """A rejected draft's row of q with a NaN leaves sums that are none: no word is drawn."""
+    nodes = 1 + children
+    p, q = empty(2 * nodes, vocab, dtype=F32), empty(2 * nodes, vocab, dtype=F32)
+    p[:] = 1.0 / vocab
+    q[:] = 0.5 / vocab
+    q[:, 7] = 0.5
+    tokens = ints(*[7] * (2 * nodes))
+    parent = ints(*([-1] + [0] * children) * 2)
+    cu, u = ints(0, nodes, 2 * nodes), torch.full((2 * nodes,), 0.75, device="cuda")
+    good = run_verify(p, q, tokens, parent, cu, u, nodes)
+    assert good == by_hand(p, q, tokens, parent, cu, u, nodes) and good[1] == [1, 1]
+    q[0, {"drafted": [7], "other": [vocab - 1], "both": [7, 3]}[where]] = float("nan")
+    op = _r().VerifyDrafts(vocab)
+    path, kept, nxt = run_verify(p, q, tokens, parent, cu, u, nodes, op, check=False)
+    _reports(op)
+    assert kept == [1, 1] and path == good[0] and nxt == [-1, good[2][1]]
+
+
+@pytest.mark.parametrize("vocab", [50, 5000, 40_000])
+def test_verify_rows_that_no_sum_needs_may_hold_nan(vocab):
+    """q behind a leaf: there is no child that it could have been drawn for."""
+    p, q, tokens, parent, cu, u = verify_case(vocab, [3, 3], seed=2, chain=True, near=0.0)
+    u[1::3] = 0.5  # the target itself: all drafts are taken
+    good = run_verify(p, q, tokens, parent, cu, u, 3)
+    assert good[1] == [3, 3]
+    q[2::3] = float("nan")
+    assert run_verify(p, q, tokens, parent, cu, u, 3) == good
