@@ -404,13 +404,14 @@ jnx_status jnx_op_qk_norm_rope_append_paged(const jnx_qk_rope* p, const uint16_t
  * j of its sequence, at tokens n_cached[s] + j, whose bit j of sees[row] is set (its ancestors
  * and itself, or any others).  A row that sees nothing has output 0, rows of no sequence stay
  * as they were.  cu_nodes [n_seqs + 1], n_cached [n_seqs] and sees [n_rows] are on the device.
- * A sequence whose rows are not among n_rows, or more than 64, is left out and reported; one
- * whose tokens are more than its entries hold has output 0 and is reported; a page that is not
- * there is read as zeros and reported.  A cache whose sequences have several pages has room a
- * multiple of 16 (JNX_ERR_UNSUPPORTED otherwise).  q and the keys and values of cached tokens and
- * nodes are finite, whoever sees them; all other rows of the pages may hold anything.  The bits
- * of a sequence do not depend on the others.  The workspace serves sequences of up to max_tokens
- * tokens, nodes among them: max_pages * room of the call. */
+ * A sequence whose rows are not among n_rows, more than 64, or start ahead of an earlier one's
+ * end is left out and reported; one whose tokens are more than its entries hold has output 0
+ * and is reported; a page that is not there is read as zeros and reported.  A cache whose
+ * sequences have several pages has room a multiple of 16 (JNX_ERR_UNSUPPORTED otherwise).  q and
+ * the keys and values of cached tokens and nodes are finite, whoever sees them; all other rows of
+ * the pages may hold anything.  The bits of a sequence do not depend on the others.  The
+ * workspace serves sequences of up to max_tokens tokens, nodes among them: max_pages * room of
+ * the call. */
 size_t jnx_op_tree_attention_workspace_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads,
                                              int32_t head_dim, int64_t max_tokens);
 jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx_pages* pages,

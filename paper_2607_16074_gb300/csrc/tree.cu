@@ -108,6 +108,8 @@ struct TreeArgs {
     const int *cu_nodes, *n_cached;
     const unsigned long long* sees;
     int4* where;  // [n_rows]: a row's first place among the sums, its sequence's nodes, runs, number
+    int2* spans;  // [n_seqs]: first row and nodes of the launch's sequences, as they count
+    int* taken;   // [2]: where the last row so far ends, behind launches of even and of odd number
     float* part;  // [run, node][H][hd]: sums
     float2* ml;   // [run, node][H]: maxima and sums of exponentials
     int places;   // of a run and node
@@ -204,9 +206,25 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
     tc_fence_after();
     if (warp == 0) {  // units and sums ahead of each sequence
         int units = 0, sums = 0;
+        // Rows are one sequence's: one that starts ahead of an earlier one's end is left out, or its
+        // sums would be more than the workspace has places for.
+        const int launch = a.s0 / BATCH;
+        int taken = launch > 0 ? a.taken[(launch - 1) & 1] : 0;
         for (int b = 0; b < a.n_seqs; b += 32) {
             const int s = b + lane;
             int u = 0, v = 0;
+            int end = s < a.n_seqs && nodes[s] > 0 ? rows0[s] + nodes[s] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, end, o);
+                if (lane >= o) end = max(end, y);
+            }
+            const int ahead = __shfl_up_sync(0xffffffffu, end, 1);
+            if (s < a.n_seqs && nodes[s] > 0 && rows0[s] < max(taken, lane ? ahead : 0)) {
+                nodes[s] = 0, olds[s] = -1;
+                if (blockIdx.x == 0) report(a.status, JNX_ERR_DEVICE_BOUNDS);
+            }
+            taken = max(taken, __shfl_sync(0xffffffffu, end, 31));
             TreeSeq x{};
             if (s < a.n_seqs) {
                 x = tree_seq<HD>(a, rows0[s], nodes[s], olds[s]);
@@ -227,7 +245,10 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
             units += __shfl_sync(0xffffffffu, ru, 31);
             sums += __shfl_sync(0xffffffffu, rv, 31);
         }
-        if (lane == 0) first[a.n_seqs] = units;
+        if (lane == 0) {
+            first[a.n_seqs] = units;
+            if (blockIdx.x == 0) a.taken[launch & 1] = taken;
+        }
     }
     __syncthreads();
     const uint32_t tbase = warp_uniform(*tmem_slot);
@@ -235,6 +256,7 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
     // what the join needs of each row
     for (int s = blockIdx.x; s < a.n_seqs; s += gridDim.x) {
         const int i = threadIdx.x;
+        if (i == 0) a.spans[s] = make_int2(rows0[s], nodes[s]);
         if (i >= nodes[s]) continue;
         a.where[rows0[s] + i] = make_int4(base[s] + i, nodes[s], runs_of[s], a.s0 + s);
     }
@@ -660,8 +682,8 @@ __global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeA
     if (runs <= 1 || runs > MAX_RUNS || x.x < 0 || x.y < 1 || x.y > kMaxNodes ||
         (long long)x.x + (runs - 1) * x.y >= a.places || x.w < a.s0 || x.w >= a.s0 + a.n_seqs)
         return;
-    int row0, n;
-    const bool known = tree_rows(a.cu_nodes, x.w, a.n_rows, kMaxNodes, row0, n) && row >= row0 && row < row0 + n;
+    const int2 span = a.spans[x.w - a.s0];
+    const bool known = row >= span.x && row < span.x + span.y;
     const long long at = (long long)x.x * a.H + h, step = (long long)x.y * a.H;
     float v[R][E], m[2], l[2], top = -INFINITY, sum = 0.f;
     // runs first, first + by, ...: a warp of four has every fourth
@@ -733,8 +755,10 @@ __global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeA
     for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(o + e) = cvt_bf2(all[e] * inv, all[e + 1] * inv);
 }
 
-// The workspace: the rows' records, then (at a sector's border) the sums.
-static size_t tree_sums_at(int n_rows) { return ((size_t)n_rows * sizeof(int4) + 31) & ~(size_t)31; }
+// The workspace: the rows' records, a launch's sequences, then (at a sector's border) the sums.
+static size_t tree_sums_at(int n_rows) {
+    return ((size_t)n_rows * sizeof(int4) + tree::BATCH * sizeof(int2) + 2 * sizeof(int) + 31) & ~(size_t)31;
+}
 
 template <int HD>
 static jnx_status launch_tree(const jnx_kv_cache& c, const jnx_pages& p, const jnx_head_rows& q, TreeArgs a,
@@ -809,7 +833,9 @@ extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx
     TreeArgs a{Pages(*pages, *cache), 0, 0, n_heads, n_kv_heads, n_heads / n_kv_heads, n_rows, box,
                (float)(1.4426950408889634 / sqrt((double)head_dim)), out->ptr, out->row_stride,
                out->head_stride, cu_nodes, n_cached, reinterpret_cast<const unsigned long long*>(sees),
-               static_cast<int4*>(workspace), nullptr, nullptr, (int)(n_rows * runs), status};
+               static_cast<int4*>(workspace), nullptr, nullptr, nullptr, nullptr, (int)(n_rows * runs), status};
+    a.spans = reinterpret_cast<int2*>(a.where + n_rows);
+    a.taken = reinterpret_cast<int*>(a.spans + tree::BATCH);
     const uintptr_t sums = reinterpret_cast<uintptr_t>(workspace) + tree_sums_at(n_rows) + 31;
     a.part = reinterpret_cast<float*>(sums & ~(uintptr_t)31);
     a.ml = reinterpret_cast<float2*>(a.part + (size_t)n_rows * runs * n_heads * head_dim);

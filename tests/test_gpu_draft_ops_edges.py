@@ -7,7 +7,7 @@ import torch
 from tests import draft_ops_ref as D
 from tests import text_ops_ref as T
 from tests.test_gpu_draft_ops import (BF, F32, HEADS, I32, Trees, _r, _reports, by_hand, check_distill, distill_case,
-                                      empty, gen, ints, normal, run_verify, verify_case)
+                                      empty, gen, ints, normal, place, run_verify, verify_case)
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +82,63 @@ def test_verify_rows_that_no_sum_needs_may_hold_nan(vocab):
     assert good[1] == [3, 3]
     q[2::3] = float("nan")
     assert run_verify(p, q, tokens, parent, cu, u, 3) == good
+
+
+# ---------------------------------------------------------------- trees
+
+def guarded(op, room=1 << 20):
+    """The operator's workspace at the start of a larger one; returns what lies behind it."""
+    big = torch.full((op.ws.numel() + room,), 90, device="cuda", dtype=torch.uint8)
+    op._held.append(big)
+    op._ws, behind = big.data_ptr(), big[op.ws.numel():]
+    return behind
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (8, 8, 128), (4, 4, 64), (8, 1, 256)])
+@pytest.mark.parametrize("cu", [(0, 5, 4, 16), (0, 12, 0, 12), (4, 9, 0, 12), (0, 5, 2, 2)])
+def test_tree_sequences_that_share_rows_are_left_out(heads, cu):
+    """Rows are one sequence's, the first's: what would be another's is left out, and no sums are
+    written that the workspace has no place for."""
+    old = [2048 - 16] * 3
+    c = Trees(heads, 64, old, [16] * 3, seed=2)
+    op = _r().TreeAttention(*heads, 3, 16, c.table.shape[1] * 64)
+    behind = guarded(op)
+    out = torch.full((16, heads[0], heads[2]), 7.0, device="cuda", dtype=BF)
+    # (an earlier call's records lie in the workspace: every row was the third's)
+    op.forward(c.q[:16], c.kp, c.vp, c.table, ints(0, 0, 0, 16), c.n, c.sees[32:], out)
+    op.check()
+    out.fill_(7.0)
+    op.forward(c.q[:16], c.kp, c.vp, c.table, ints(*cu), c.n, c.sees[:16], out)
+    _reports(op)
+    rows = slice(cu[0], cu[1])
+    n = cu[1] - cu[0]
+    where = place(c.table, 64, 0, range(old[0] + n))
+    want, tol = D.tree(c.q[rows], c.kp[where], c.vp[where], old[0], c.sees[rows, None] >> torch.arange(n, device="cuda") & 1 == 1)
+    T.close(out[rows], want, tol, "the first sequence")
+    assert (out[:cu[0]] == 7).all() and (out[cu[1]:] == 7).all()
+    assert (behind == 90).all()
+
+
+def test_tree_rows_that_an_earlier_launch_had():
+    """More sequences than a launch takes: one of the second that shares rows with one of the first."""
+    heads, n = (4, 2, 64), 300
+    c = Trees(heads, 64, [600] * n, [1] * n, seed=3)
+    op = c.op()
+    behind, good = guarded(op), torch.empty_like(c.q)
+    c.run(op, good)
+    c.compare(good)
+    for first, left in ((100, 257), (0, 299), (200, 290)):
+        # sequence left - 1 counts backwards, those behind it have rows of earlier ones
+        cu = list(range(n + 1))
+        cu[left] = first
+        cu[left + 1:] = range(first + 1, first + 1 + n - left)
+        out = torch.full_like(good, 7.0)
+        op.forward(c.q, c.kp, c.vp, c.table, ints(*cu), c.n, c.sees, out)
+        _reports(op)
+        live = left - 1
+        assert torch.equal(out[:live], good[:live])
+        assert (out[live:] == 7).all()
+    assert (behind == 90).all()
+    out = torch.full_like(good, 7.0)
+    c.run(op, out)
+    assert torch.equal(out, good)
