@@ -100,6 +100,7 @@ struct TreeCfg {
 
 struct TreeArgs {
     Pages pages;
+    int no_page;     // outside of the maps: read as zeros
     int n_seqs, s0;  // sequences of the launch, the first of them
     int H, Hkv, group, n_rows, box;
     float scale_log2;
@@ -300,10 +301,10 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
         const int qrow = a.group * HD * 2, boxes = KT / a.box;
         // pages of the boxes [32 c, 32 c + 32) of a unit, one a lane
         auto look = [&](const TreeUnit& x, int c) {
-            int page = a.pages.n_pages, row = 0;  // no page: read as zeros
+            int page = a.no_page, row = 0;
             const long long token = x.at + (long long)(c * 32 + lane) * a.box;
             if (token < x.end && !a.pages.find(a.s0 + x.s, (int)token, page, row)) {
-                page = a.pages.n_pages;
+                page = a.no_page;
                 report(a.status, JNX_ERR_DEVICE_BOUNDS);
             }
             __syncwarp();
@@ -826,11 +827,11 @@ extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx
     // boxes of as many tokens as a tile and a page share
     int box = tree::KT;
     while (pages->max_pages > 1 && cache->room % box) box /= 2;
-    // an empty cache has no tiles, but the maps want extents
+    // the maps want extents: an empty cache's have a page that no sequence's tokens are looked for in
     jnx_kv_cache c = *cache;
     c.n_slots = std::max(c.n_slots, 1);
     c.room = std::max(c.room, 1);
-    TreeArgs a{Pages(*pages, *cache), 0, 0, n_heads, n_kv_heads, n_heads / n_kv_heads, n_rows, box,
+    TreeArgs a{Pages(*pages, *cache), c.n_slots, 0, 0, n_heads, n_kv_heads, n_heads / n_kv_heads, n_rows, box,
                (float)(1.4426950408889634 / sqrt((double)head_dim)), out->ptr, out->row_stride,
                out->head_stride, cu_nodes, n_cached, reinterpret_cast<const unsigned long long*>(sees),
                static_cast<int4*>(workspace), nullptr, nullptr, nullptr, nullptr, (int)(n_rows * runs), status};

@@ -142,3 +142,25 @@ def test_tree_rows_that_an_earlier_launch_had():
     out = torch.full_like(good, 7.0)
     c.run(op, out)
     assert torch.equal(out, good)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64), (8, 1, 256)])
+@pytest.mark.parametrize("entry", [0, -1, 1, 2 ** 31 - 1])
+def test_tree_over_a_cache_of_no_pages(heads, entry):
+    """Every page is one that is not there: read as zeros and reported, not what lies at the
+    pointers."""
+    from paper_2607_16074_gb300 import jnx as J
+    h, hkv, hd = heads
+    g, op = gen(0), _r().TreeAttention(*heads, 2, 9, 512)
+    kp, vp = normal(g, 4, 128, hkv, hd), normal(g, 4, 128, hkv, hd)
+    q, out = normal(g, 9, h, hd), empty(9, h, hd)
+    table = torch.full((2, 4), entry, device="cuda", dtype=I32)
+    cu, n, sees = ints(0, 4, 9), ints(100, 500), ints(*[1] * 9, dtype=torch.int64)
+    r = op._views.refs
+    op._views.fill(kp.data_ptr(), vp.data_ptr(), 0, 128, *kp.stride()[:3], table.data_ptr(), 4, 2, 4,
+                   q.data_ptr(), *q.stride()[:2], out.data_ptr(), *out.stride()[:2])
+    J.check(J.lib().jnx_op_tree_attention(
+        r[0], r[1], h, hkv, hd, 9, r[2], cu.data_ptr(), n.data_ptr(), sees.data_ptr(), r[3], op._ws, op._nws,
+        op._status, torch.cuda.current_stream().cuda_stream))
+    _reports(op)
+    assert (out == 0).all()
