@@ -23,6 +23,7 @@
 // 6e-8 of the angle itself, 1e-3 rad at position 16,000.  What is left is the frequency's own
 // rounding as a double, 2^-50 of the angle: 2e-6 rad at position 2^31.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "jnx_dev.cuh"
@@ -157,6 +158,7 @@ using Backward = Cfg<HD, 4, HD == 128 ? 8 : 16>;
 
 // Where keys go: rows of a tensor, rows of cache slots, or rows of the pages of sequences.
 enum { ROWS = 0, SLOTS = 1, PAGES = 2 };
+constexpr long long NOWHERE = LLONG_MIN;  // (any other place may be one: strides may be negative)
 }  // namespace rope
 
 template <int HD, int TO>
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(rope::THREADS)
     using C = rope::Forward<HD>;
     constexpr int E = C::E;
     __shared__ float4 cs[C::TOK * HD / 4];
-    __shared__ long long place[APPEND ? C::TOK : 1];  // where a token's keys go; -1: nowhere
+    __shared__ long long place[APPEND ? C::TOK : 1];  // where a token's keys go
     pdl_entry();
     const int t0 = blockIdx.x * a.tok, nt = min(a.tok, a.n_tokens - t0);
     if (APPEND && (int)threadIdx.x < nt) {  // (looked up at every row: 39.3 us of 9,000 tokens for 38.3)
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(rope::THREADS)
         int slot = a.slot[tok], at = a.at[tok];
         const bool there = TO == rope::PAGES ? a.pages.find(slot, at, slot, at)
                                              : slot >= 0 && slot < a.n_slots && at >= 0 && at < a.room;
-        place[threadIdx.x] = there ? slot * a.slot_stride + at * a.k_row : -1;
+        place[threadIdx.x] = there ? slot * a.slot_stride + at * a.k_row : rope::NOWHERE;
         if (!there) report(a.status, JNX_ERR_DEVICE_BOUNDS);
     }
     // rows of the CTA's tokens, token-major; an append's value heads come after the keys'
@@ -243,7 +245,7 @@ __global__ void __launch_bounds__(rope::THREADS)
         if (is_q) {
             o = a.q + tok * a.q_row + hw * a.q_head;
         } else if (APPEND) {
-            if (place[tw] < 0) continue;
+            if (place[tw] == rope::NOWHERE) continue;
             o = (is_v ? a.v : a.k) + place[tw] + (hw - a.H - (is_v ? a.Hkv : 0)) * a.k_head;
         } else {
             o = a.k + tok * a.k_row + (hw - a.H) * a.k_head;

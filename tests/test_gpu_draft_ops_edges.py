@@ -84,6 +84,39 @@ def test_verify_rows_that_no_sum_needs_may_hold_nan(vocab):
     assert run_verify(p, q, tokens, parent, cu, u, 3) == good
 
 
+# ---------------------------------------------------------------- appends
+
+@pytest.mark.parametrize("backwards", ["rows", "slots", "heads"])
+@pytest.mark.parametrize("paged", [False, True])
+def test_append_to_a_cache_that_runs_backwards(backwards, paged):
+    """A caller's cache may have its last row, slot or head at the lowest address."""
+    from paper_2607_16074_gb300 import jnx as J
+    h, hkv, hd, slots, room, n = 4, 2, 64, 3, 16, 9
+    g, op = gen(1), _r().QKNormRope(h, hkv, hd)
+    qkv, q = normal(g, n, (h + 2 * hkv) * hd), empty(n, h, hd)
+    slot, at = ints(0, 1, 2, 0, 1, 2, 0, 0, 2), ints(0, 3, 15, 1, 0, 7, 15, 8, 0)
+    want = empty(2, slots, room, hkv, hd)
+    op.append(qkv, at[None].contiguous(), q, want[0], want[1], slot, at)
+    axis = {"slots": 0, "rows": 1, "heads": 2}[backwards]
+    out = empty(2, slots, room, hkv, hd)
+    s = list(out[0].stride())
+    first = (out.shape[1 + axis] - 1) * s[axis] * 2  # bytes to the place of the first
+    s[axis] = -s[axis]
+    pos, table = at[None].contiguous(), ints([0], [1], [2])
+    cache = (out[0].data_ptr() + first, out[1].data_ptr() + first, slots, room, *s[:3])
+    rows = (q.data_ptr(), *q.stride()[:2])
+    head = (op._ref, qkv.data_ptr(), qkv.stride(0), pos.data_ptr(), n)
+    tail = (slot.data_ptr(), at.data_ptr(), op._status, torch.cuda.current_stream().cuda_stream)
+    if paged:
+        op._qp.fill(*rows, *cache, table.data_ptr(), 1, slots, 1)
+        J.check(J.lib().jnx_op_qk_norm_rope_append_paged(*head, *op._qp.refs, *tail))
+    else:
+        op._qc.fill(*rows, *cache)
+        J.check(J.lib().jnx_op_qk_norm_rope_append(*head, *op._qc.refs, *tail))
+    op.check()
+    assert torch.equal(out.flip(1 + axis).nan_to_num(99.0), want.nan_to_num(99.0))
+
+
 # ---------------------------------------------------------------- trees
 
 def guarded(op, room=1 << 20):
