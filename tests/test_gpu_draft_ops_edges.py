@@ -49,6 +49,35 @@ def test_distill_logits_beyond_range_over_the_temperature(tau):
     assert (loss[3::5] == 0).all() and not dh[3::5].any()
 
 
+@pytest.mark.parametrize("k", [2, 8])
+def test_distill_near_its_teacher_no_loss_is_below_zero(k):
+    """A vocabulary of the entries alone, logits exact: hidden rows of a single one.  The
+    teacher's are theirs plus 1e-7 to 1.  d = log P - log T is off by under 2^-18: of each of its
+    sides, of logits up to 8, the difference to the maximum and that to the logarithm are rounded
+    at up to 16 (2^-21 each), the logarithm off by 2^-22 and its sum's terms by as much.  A term
+    moves by T (e^d - 1) = P - T of that, and by half its square; its own arithmetic and T's are
+    under 2^-19 of it."""
+    n, d = 4096, 64
+    g = gen(k)
+    w = empty(k, d)
+    w[:] = 0
+    w[:, :n // 64] = normal(g, k, n // 64, std=1.5).clamp(-5, 5)
+    h = torch.zeros(n, d, device="cuda", dtype=BF)
+    h[torch.arange(n, device="cuda"), torch.arange(n, device="cuda") % 64] = 1
+    x = h.float() @ w.float().T
+    scale = 10.0 ** (torch.rand(n, 1, generator=g, device="cuda") * 7 - 7)
+    t = x + scale * torch.randn(n, k, generator=g, device="cuda").clamp(-3, 3)
+    ids = torch.arange(k, device="cuda", dtype=I32).expand(n, k).contiguous()
+    op, loss = _r().VocabDistill(w, n, k, gradients=False), empty(n, dtype=F32)
+    op.loss(h, ids, t, loss)
+    op.check()
+    logp, logt = torch.log_softmax(x.double(), -1), torch.log_softmax(t.double(), -1)
+    want = (logt.exp() * (logt - logp)).sum(-1)
+    off = (logt.exp() - logp.exp()).abs().sum(-1)
+    assert (loss >= 0).all(), int((loss < 0).sum())
+    T.close(loss, want, 2.0 ** -18 * off + 2.0 ** -36 + 2.0 ** -19 * want, "loss")
+
+
 # ---------------------------------------------------------------- verification
 
 @pytest.mark.parametrize("vocab", [50, 5000, 40_000])
