@@ -390,6 +390,17 @@ __device__ __forceinline__ void tc_commit(uint64_t* bar) {
         : "memory");
 }
 
+// A warpgroup gives registers back, or takes some that others gave: N a thread from here on.
+// The shares of all warpgroups are at most what the launch has, or a taker waits for ever.
+template <int N>
+__device__ __forceinline__ void reg_dealloc() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void reg_alloc() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // 32 lanes x 32 consecutive 32-bit columns: thread i of the warp receives
 // row (lane base + i), columns [col, col + 32).
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {

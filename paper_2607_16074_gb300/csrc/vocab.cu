@@ -52,16 +52,20 @@ inline int pad_rows(int n) { return (n + BM - 1) / BM * BM; }
 
 constexpr int TOP = 128;  // entries of a row's teacher, at most (places fit a byte)
 
-// The tensor cores' sums drop what lies below their last place, so that a logit falls short of
-// its value, by a part that grows with its terms: 2^-30 of it a term (the least squares' slope
-// over 512 x 4,096 logits of centred rows: 0.82 of that at 64 terms, 0.90 at 1,000, 0.96 at 2,048,
-// 1.04 at 8,192; rows of a mean 0.85 to 1.1, of positive terms only 1.3 to 3).  A teacher's losses
-// count it in: 512 of rows of 2,048 on 32,000 words at a temperature of a half are off by 2.6e-7
-// in norm, 1.6e-6 without.
-inline double vocab_scale(int d, float inv_tau) {
-    return (1.0 + std::min(d, 1 << 14) * (1.0 / (1 << 30))) * inv_tau;
-}
-inline float finite(double x) { return (float)std::min(x, 3e38); }
+// The tensor cores' sums are cut off below their last place, so that a logit falls short of its
+// value by a part that grows with its terms: some 2^-30 of it a term where they are centred, up to
+// three times that where all are positive, nothing where the sums are exact.  Of rows of 2,048 that
+// is more than a teacher's losses are off by otherwise, so the logits against a teacher are sums
+// of up to 768 terms on the tensor cores, added up in fp32 with rounding: losses of 512 rows of
+// 2,048 on 32,000 words at a temperature of a half are off by 5.2e-7 in norm, 1.6e-6 as one sum,
+// at 1 to 2 % of the time (8,191 rows).  The first sum is the longest: the epilogue of the tile
+// before works under it.
+constexpr int FIRST_K = 12, MORE_K = 10;  // K steps of the first such sum and of those behind it
+// A warpgroup for the copies and the products, and two for the epilogue, whose 128 logits a
+// thread stay in registers: each has its share of what the launch has (168 for each of 384).
+constexpr int TEACHER_THREADS = 128 + 32 * EW, FEW_REGS = 56, MANY_REGS = 224;
+static_assert(128 * FEW_REGS + 32 * EW * MANY_REGS <= 168 * TEACHER_THREADS, "registers of the launch");
+__host__ __device__ constexpr int threads(bool teacher) { return teacher ? TEACHER_THREADS : 64 + 32 * EW; }
 }  // namespace vocab
 
 struct VocabGemm {
@@ -227,167 +231,305 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
     const int first = blockIdx.x >> (PAIR ? 1 : 0), step = gridDim.x >> (PAIR ? 1 : 0);
     // K steps [k0, k1) of a part
     auto k_begin = [&](int part) { return (int)((long long)all_k * part / parts); };
+    // sums of a tile, each in an accumulator of its own
+    const int pieces = !TEACHER || all_k <= FIRST_K ? 1 : 1 + (all_k - FIRST_K + MORE_K - 1) / MORE_K;
+    constexpr int EW0 = TEACHER ? 4 : 2;  // the first epilogue warp
 
-    if (warp == 0) {
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int tile = first; ok && tile < num_tiles && !__any_sync(0xffffffffu, *abort_flag);
-             tile += step) {
-            const VocabTile t = vocab_tile(tile, num_m, num_n);
-            const int arow = t.mb * BM + (int)rank * 128, brow = t.nb * BN + rank * 128;
-            for (int kb = k_begin(t.part); kb < k_begin(t.part + 1); ++kb) {
-                if (!mbar_wait_warp(&empty[stage], phase ^ 1)) {
-                    ok = false;
-                    break;
-                }
-                if (elect_one()) {
-                    uint8_t* sa = smem + stage * STAGE_BYTES;
-                    uint8_t* sb = sa + A_BYTES;
-                    if constexpr (!PAIR) {
-                        mbar_arrive_expect_tx(&full[stage], STAGE_BYTES);
-                        tma_load_2d(sa, &ta, kb * BK, arow, &full[stage]);
-                        tma_load_2d(sb, &tb, kb * BK, brow, &full[stage]);
-                        tma_load_2d(sb + A_BYTES, &tb, kb * BK, brow + 128, &full[stage]);
-                    } else {
-                        const uint32_t bar = map_rank(&full[stage], 0);
-                        if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * STAGE_BYTES);
-                        if constexpr (AMN) {
-                            tma_load_2d_pair(sa, &ta, arow, kb * BK, bar);
-                            tma_load_2d_pair(sa + A_BYTES / 2, &ta, arow + 64, kb * BK, bar);
+    if (warp < EW0) {
+        if constexpr (TEACHER) reg_dealloc<FEW_REGS>();
+        if (warp == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int tile = first; ok && tile < num_tiles && !__any_sync(0xffffffffu, *abort_flag);
+                 tile += step) {
+                const VocabTile t = vocab_tile(tile, num_m, num_n);
+                const int arow = t.mb * BM + (int)rank * 128, brow = t.nb * BN + rank * 128;
+                for (int kb = k_begin(t.part); kb < k_begin(t.part + 1); ++kb) {
+                    if (!mbar_wait_warp(&empty[stage], phase ^ 1)) {
+                        ok = false;
+                        break;
+                    }
+                    if (elect_one()) {
+                        uint8_t* sa = smem + stage * STAGE_BYTES;
+                        uint8_t* sb = sa + A_BYTES;
+                        if constexpr (!PAIR) {
+                            mbar_arrive_expect_tx(&full[stage], STAGE_BYTES);
+                            tma_load_2d(sa, &ta, kb * BK, arow, &full[stage]);
+                            tma_load_2d(sb, &tb, kb * BK, brow, &full[stage]);
+                            tma_load_2d(sb + A_BYTES, &tb, kb * BK, brow + 128, &full[stage]);
                         } else {
-                            tma_load_2d_pair(sa, &ta, kb * BK, arow, bar);
-                        }
-                        if constexpr (BMN) {
-                            tma_load_2d_pair(sb, &tb, brow, kb * BK, bar);
-                            tma_load_2d_pair(sb + A_BYTES / 2, &tb, brow + 64, kb * BK, bar);
-                        } else {
-                            tma_load_2d_pair(sb, &tb, kb * BK, brow, bar);
+                            const uint32_t bar = map_rank(&full[stage], 0);
+                            if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * STAGE_BYTES);
+                            if constexpr (AMN) {
+                                tma_load_2d_pair(sa, &ta, arow, kb * BK, bar);
+                                tma_load_2d_pair(sa + A_BYTES / 2, &ta, arow + 64, kb * BK, bar);
+                            } else {
+                                tma_load_2d_pair(sa, &ta, kb * BK, arow, bar);
+                            }
+                            if constexpr (BMN) {
+                                tma_load_2d_pair(sb, &tb, brow, kb * BK, bar);
+                                tma_load_2d_pair(sb + A_BYTES / 2, &tb, brow + 64, kb * BK, bar);
+                            } else {
+                                tma_load_2d_pair(sb, &tb, kb * BK, brow, bar);
+                            }
                         }
                     }
-                }
-                __syncwarp();
-                if (++stage == STAGES) {
-                    stage = 0;
-                    phase ^= 1;
+                    __syncwarp();
+                    if (++stage == STAGES) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
                 }
             }
-        }
-        if (!ok) {
-            *abort_flag = 1;
-            report(p.status, JNX_ERR_TIMEOUT);
-        }
-    } else if (warp == 1 && rank == 0) {
-        auto commit = [](uint64_t* b) {
-            if constexpr (PAIR) tc_commit_pair(b);
-            else tc_commit(b);
-        };
-        int stage = 0, local = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        const uint32_t a0 = smem_u32(smem), b0 = a0 + A_BYTES;
-        const uint32_t a_lo = AMN ? sw128_desc_mn_lo(a0, A_BYTES / 2) : sw128_desc_lo(a0);
-        const uint32_t b_lo = BMN ? sw128_desc_mn_lo(b0, A_BYTES / 2) : sw128_desc_lo(b0);
-        for (int tile = first; ok && tile < num_tiles && !__any_sync(0xffffffffu, *abort_flag);
-             tile += step, ++local) {
-            const VocabTile t = vocab_tile(tile, num_m, num_n);
-            const int k0 = k_begin(t.part), k1 = k_begin(t.part + 1), acc = local & 1;
-            if (!mbar_wait_cluster_warp(&tempty[acc], ((local >> 1) & 1) ^ 1)) {
-                ok = false;
-                break;
+            if (!ok) {
+                *abort_flag = 1;
+                report(p.status, JNX_ERR_TIMEOUT);
             }
-            tc_fence_after();
-            const uint32_t dcol = tmem_base + acc * BN;
-            for (int kb = k0; kb < k1; ++kb) {
-                if (!mbar_wait_cluster_warp(&full[stage], phase)) {
+        } else if (warp == 1 && rank == 0) {
+            auto commit = [](uint64_t* b) {
+                if constexpr (PAIR) tc_commit_pair(b);
+                else tc_commit(b);
+            };
+            int stage = 0, local = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            const uint32_t a0 = smem_u32(smem), b0 = a0 + A_BYTES;
+            const uint32_t a_lo = AMN ? sw128_desc_mn_lo(a0, A_BYTES / 2) : sw128_desc_lo(a0);
+            const uint32_t b_lo = BMN ? sw128_desc_mn_lo(b0, A_BYTES / 2) : sw128_desc_lo(b0);
+            for (int tile = first, piece = 0;
+                 ok && tile < num_tiles && !__any_sync(0xffffffffu, *abort_flag); ++local) {
+                const VocabTile t = vocab_tile(tile, num_m, num_n);
+                const int k0 = !TEACHER ? k_begin(t.part) : piece ? FIRST_K + (piece - 1) * MORE_K : 0;
+                const int k1 = TEACHER ? min(all_k, FIRST_K + piece * MORE_K) : k_begin(t.part + 1);
+                const int acc = local & 1;
+                if (++piece == pieces) piece = 0, tile += step;
+                if (!mbar_wait_cluster_warp(&tempty[acc], ((local >> 1) & 1) ^ 1)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint32_t off = (uint32_t)(stage * STAGE_BYTES) >> 4;
-                if (elect_one()) {
+                const uint32_t dcol = tmem_base + acc * BN;
+                for (int kb = k0; kb < k1; ++kb) {
+                    if (!mbar_wait_cluster_warp(&full[stage], phase)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t off = (uint32_t)(stage * STAGE_BYTES) >> 4;
+                    if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < BK / 16; ++kk)
-                        // (16 K rows of an MN-major operand are two 8-row atoms)
-                        if constexpr (PAIR)
-                            tc_mma_f16_pair(dcol, desc_of(a_lo + off + kk * (AMN ? 128 : 2), kSw128DescHi),
-                                            desc_of(b_lo + off + kk * (BMN ? 128 : 2), kSw128DescHi), IDESC,
-                                            (kb - k0) | kk);
-                        else
-                            tc_mma_f16(dcol, desc_of(a_lo + off + kk * 2, kSw128DescHi),
-                                       desc_of(b_lo + off + kk * 2, kSw128DescHi), IDESC, (kb - k0) | kk);
-                    commit(&empty[stage]);
+                        for (int kk = 0; kk < BK / 16; ++kk)
+                            // (16 K rows of an MN-major operand are two 8-row atoms)
+                            if constexpr (PAIR)
+                                tc_mma_f16_pair(dcol, desc_of(a_lo + off + kk * (AMN ? 128 : 2), kSw128DescHi),
+                                                desc_of(b_lo + off + kk * (BMN ? 128 : 2), kSw128DescHi), IDESC,
+                                                (kb - k0) | kk);
+                            else
+                                tc_mma_f16(dcol, desc_of(a_lo + off + kk * 2, kSw128DescHi),
+                                           desc_of(b_lo + off + kk * 2, kSw128DescHi), IDESC, (kb - k0) | kk);
+                        commit(&empty[stage]);
+                    }
+                    __syncwarp();
+                    if (++stage == STAGES) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
                 }
+                if (!ok) break;
+                if (elect_one()) commit(&tfull[acc]);
                 __syncwarp();
-                if (++stage == STAGES) {
-                    stage = 0;
-                    phase ^= 1;
-                }
             }
-            if (!ok) break;
-            if (elect_one()) commit(&tfull[acc]);
+            if (!ok) {
+                *abort_flag = 1;
+                report(p.status, JNX_ERR_TIMEOUT);
+            }
+            // no MMA still reads or writes either CTA after this
+            if (elect_one()) commit(drain);
             __syncwarp();
+            mbar_wait(drain, 0);
+        } else if (warp == 1) {
+            mbar_wait(drain, 0);  // the leader's last commit has reached this CTA
         }
-        if (!ok) {
-            *abort_flag = 1;
-            report(p.status, JNX_ERR_TIMEOUT);
-        }
-        // no MMA still reads or writes either CTA after this
-        if (elect_one()) commit(drain);
-        __syncwarp();
-        mbar_wait(drain, 0);
-    } else if (warp == 1) {
-        mbar_wait(drain, 0);  // the leader's last commit has reached this CTA
     } else {
-        const int q = warp & 3;           // TMEM lane quarter this warp may access
-        const int half = (warp - 2) >> 2; // its 128 of the tile's columns
-        uint8_t* slot = slots + (warp - 2) * SLOT;
+        if constexpr (TEACHER) reg_alloc<MANY_REGS>();
+        const int q = warp & 3;             // TMEM lane quarter this warp may access
+        const int half = (warp - EW0) >> 2; // its 128 of the tile's columns
+        uint8_t* slot = slots + (warp - EW0) * SLOT;
         int local = 0;
-        for (int tile = first; tile < num_tiles; tile += step, ++local) {
+        // A teacher's entries of a row of a tile: their number and the first two's columns, 8 bits
+        // each, the first one's place among the row's, and the 32-column chunks that hold any.
+        // They are looked up a tile ahead, a step of the chain between parts of this tile's work
+        // (a loop of lookups behind the product: 102 us of 2,047 rows of 1,024 on 32,000 words for 93)
+        constexpr int AHEAD = 2;
+        int tg = 0, te = 0, src = -1, next_col0 = 0;
+        uint32_t seen = 0, mine = 0;
+        auto look_row = [&](int tile) {
+            src = -1;
+            if (tile >= num_tiles) return;
             const VocabTile t = vocab_tile(tile, num_m, num_n);
-            const int acc = local & 1;
+            const int row = t.mb * BM + (int)rank * 128 + q * 32 + lane;
+            next_col0 = t.nb * BN + half * 128;
+            if (row < M && next_col0 < N) src = p.index[p.r0 + row];
+        };
+        auto look_places = [&]() {
+            tg = te = 0;
+            if (src < 0) return;
+            const uint8_t* st = p.starts + (size_t)src * ((N + BLK - 1) / BLK + 1) + next_col0 / BLK;
+            tg = st[0], te = st[1];
+        };
+        auto look_words = [&]() {
+            seen = te - tg, mine = 0;
+            const int* words = p.words + (size_t)src * p.top + tg;
+            for (int k = 0; tg + k < te; ++k) {
+                const int col = words[k] - next_col0;
+                mine |= 1u << (col >> 5);
+                if (k < AHEAD) seen |= col << (8 + 8 * k);
+            }
+        };
+        if constexpr (TEACHER) {
+            look_row(first);
+            look_places();
+            look_words();
+        }
+        for (int tile = first; tile < num_tiles; tile += step) {
+            const VocabTile t = vocab_tile(tile, num_m, num_n);
             const int row0 = t.mb * BM + rank * 128 + q * 32, row = row0 + lane;
             const int col0 = t.nb * BN + half * 128;
             const bool summed = k_begin(t.part + 1) > k_begin(t.part);  // else nothing was
-            // a teacher's entries of these columns are places [tg, te) of its words: looked up
-            // while the product is under way, the first two words too (a loop of lookups behind
-            // it: 102 us of 2,047 rows of 1,024 on 32,000 words for 93)
-            constexpr int AHEAD = 2;
-            int tg = 0, te = 0, ahead[TEACHER ? AHEAD : 1];
-            const int* words = nullptr;
-            uint32_t mine = 0;
-            if constexpr (TEACHER) {
-                const int cols = min(BLK, N - col0);
-                if (row < M && cols > 0) {
-                    const size_t src = p.index[p.r0 + row];
-                    const uint8_t* st = p.starts + src * ((N + BLK - 1) / BLK + 1) + col0 / BLK;
-                    tg = st[0], te = st[1];
-                    words = p.words + src * p.top + tg;
-#pragma unroll
-                    for (int k = 0; k < AHEAD; ++k)
-                        if (tg + k < te) {
-                            ahead[k] = words[k] - col0;
-                            mine |= 1u << (ahead[k] >> 5);
-                        }
-                    for (int k = AHEAD; tg + k < te; ++k) mine |= 1u << ((words[k] - col0) >> 5);
+            const auto full = [&]() {
+                if (mbar_wait(&tfull[local & 1], (local >> 1) & 1) && !*abort_flag) {
+                    tc_fence_after();
+                    return true;
                 }
-            }
-            if (!mbar_wait(&tfull[acc], (local >> 1) & 1) || *abort_flag) {
                 *abort_flag = 1;
                 report(p.status, JNX_ERR_TIMEOUT);
-                break;
+                return false;
+            };
+            const auto empty_again = [&]() {
+                __syncwarp();
+                if (elect_one()) {
+                    if constexpr (PAIR) mbar_arrive_cluster(map_rank(&tempty[local & 1], 0));
+                    else mbar_arrive(&tempty[local & 1]);
+                }
+                __syncwarp();
+            };
+            const auto columns = [&]() {
+                return tmem_base + (local & 1) * BN + half * 128 + ((uint32_t)(q * 32) << 16);
+            };
+            const uint32_t tc = columns();
+            if constexpr (TEACHER) {
+                // the logits gather in registers, and an accumulator is free again as soon as its
+                // part is added
+                uint32_t x[4][32];
+                bool ok = true;
+                for (int i = 0; i < pieces && (ok = __all_sync(0xffffffffu, full())); ++i) {
+                    const uint32_t from = columns();
+                    if (i == 0) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_ld32(from + c * 32, x[c]);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_ld_wait_regs(x[c]);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t v[16];
+                            tmem_ld16(from + c * 16, v);
+                            tmem_ld_wait_regs16(v);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                uint32_t* to = &x[c >> 1][(c & 1) * 16 + e];
+                                float x0, x1;
+                                f2_unpack(f2_add(f2_pack(__uint_as_float(to[0]), __uint_as_float(to[1])),
+                                                 f2_pack(__uint_as_float(v[e]), __uint_as_float(v[e + 1]))),
+                                          x0, x1);
+                                to[0] = __float_as_uint(x0), to[1] = __float_as_uint(x1);
+                            }
+                        }
+                    }
+                    tc_fence_before();
+                    empty_again();
+                    ++local;
+                }
+                if (!ok) break;
+                const int cols = min(BLK, N - col0);  // may be negative: nothing here
+                const int here = seen & 255, first_place = tg;
+                int taken = 0;  // of the entries here
+                // the 32-column chunks that hold an entry of the warp's rows
+                const uint32_t hit = __reduce_or_sync(0xffffffffu, mine);
+                look_row(tile + step);
+                float m = -INFINITY;
+                if (cols < BLK) {  // no columns: -inf is no maximum and no term
+#pragma unroll
+                    for (int e = 0; e < BLK; ++e)
+                        if (e >= cols) x[e / 32][e % 32] = 0xff800000u;
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2)
+                        m = fmax3(m, __uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1]));
+                    // an entry's logit is taken out: -inf is no term of the sum
+                    if (hit >> c & 1) {
+                        while (taken < here) {
+                            const size_t place = (size_t)row * p.top + first_place + taken;
+                            int col = seen >> (8 + 8 * taken) & 255;
+                            if (taken >= AHEAD)
+                                col = p.words[(size_t)p.index[p.r0 + row] * p.top + first_place + taken] - col0;
+                            if (col >> 5 != c) break;
+                            float at = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (col == c * 32 + e) {
+                                    at = __uint_as_float(x[c][e]);
+                                    x[c][e] = 0xff800000u;
+                                }
+                            p.at_target[place] = at;
+                            ++taken;
+                        }
+                        __syncwarp();
+                    }
+                }
+                look_places();
+                // (a loss is of all digits near zero: the difference to the maximum first)
+                const float sub = m == -INFINITY ? 0.f : m;
+                const uint64_t nm2 = f2_pack(-sub, -sub), to2 = f2_pack(p.log2e, p.log2e);
+                uint64_t sums = f2_pack(0.f, 0.f);
+                uint16_t* g0 = p.G ? p.G + (size_t)row0 * ((N + 63) / 64 * 64) + col0 : nullptr;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (c * 64 >= cols) break;
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int e = 0; e < 64; e += 2) {
+                        const uint32_t* y = &x[2 * c + e / 32][e % 32];
+                        float x0, x1;
+                        f2_unpack(f2_mul(f2_add(f2_pack(__uint_as_float(y[0]), __uint_as_float(y[1])), nm2), to2),
+                                  x0, x1);
+                        x0 = ex2_approx(x0), x1 = ex2_approx(x1);
+                        sums = f2_add(sums, f2_pack(x0, x1));
+                        pk[e / 2] = cvt_bf2(x0, x1);
+                    }
+                    if (p.G)
+                        vocab_store64(slot, lane, pk, 8, [&](int r) {
+                            return g0 + (size_t)r * ((N + 63) / 64 * 64) + c * 64;
+                        });
+                }
+                float s0, s1;
+                f2_unpack(sums, s0, s1);
+                if (row < M && cols > 0)
+                    p.stats[(size_t)row * ((N + BLK - 1) / BLK) + col0 / BLK] = make_float2(m, s0 + s1);
+                look_words();
+                __syncwarp();
+                continue;
             }
-            tc_fence_after();
-            const uint32_t tc = tmem_base + acc * BN + half * 128 + ((uint32_t)(q * 32) << 16);
+            if (!full()) break;
             if constexpr (MODE == LOGITS) {
                 const int cols = min(BLK, N - col0);  // may be negative: nothing here
-                if constexpr (!TEACHER) {
-                    tg = row < M ? p.targets[p.r0 + row] - col0 : -1;
-                    mine = (unsigned)tg < (unsigned)BLK ? 1u << (tg >> 5) : 0u;
-                }
-                int taken = 0;  // of the teacher's entries
+                const int tg = row < M ? p.targets[p.r0 + row] - col0 : -1;
                 // the 32-column chunks that hold a target of the warp's rows
-                const uint32_t hit = __reduce_or_sync(0xffffffffu, mine);
+                const uint32_t hit = __reduce_or_sync(
+                    0xffffffffu, (unsigned)tg < (unsigned)BLK ? 1u << (tg >> 5) : 0u);
                 float m = -INFINITY, s = 0.f, at = 0.f;
 #pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
@@ -408,43 +550,18 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
                     // loop below 208, with the sum over all terms 189: the logit was picked
                     // out by way of local memory)
                     if (hit >> c & 1) {
-                        if constexpr (TEACHER) {
-                            while (tg + taken < te) {
-                                int col = ahead[0];
 #pragma unroll
-                                for (int k = 1; k < AHEAD; ++k)
-                                    if (taken == k) col = ahead[k];
-                                if (taken >= AHEAD) col = words[taken] - col0;
-                                if (col >> 5 != c) break;
-#pragma unroll
-                                for (int e = 0; e < 32; ++e)
-                                    if (col == c * 32 + e) {
-                                        at = __uint_as_float(v[e]);
-                                        v[e] = 0xff800000u;
-                                    }
-                                p.at_target[(size_t)row * p.top + tg + taken] = at;
-                                ++taken;
+                        for (int e = 0; e < 32; ++e)
+                            if (tg == c * 32 + e) {
+                                at = __uint_as_float(v[e]);
+                                v[e] = 0xff800000u;
                             }
-                            __syncwarp();
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (tg == c * 32 + e) {
-                                    at = __uint_as_float(v[e]);
-                                    v[e] = 0xff800000u;
-                                }
-                        }
                         tmem_st32(tc + c * 32, v);
                         tmem_st_wait();
                     }
                 }
-                const float LOG2E = TEACHER ? p.log2e : 1.4426950408889634f;
-                // (a teacher's loss is of all digits near zero: the difference first)
-                const float sub = m == -INFINITY ? 0.f : TEACHER ? m : m * LOG2E;
-                auto power = [&](uint32_t w) {
-                    const float x = __uint_as_float(w);
-                    return ex2_approx(TEACHER ? (x - sub) * LOG2E : fmaf(x, LOG2E, -sub));
-                };
+                constexpr float LOG2E = 1.4426950408889634f;
+                const float sub = m == -INFINITY ? 0.f : m * LOG2E;
                 uint16_t* g0 = p.G ? p.G + (size_t)row0 * ((N + 63) / 64 * 64) + col0 : nullptr;
 #pragma unroll 1
                 for (int c = 0; c < 2; ++c) {
@@ -458,7 +575,8 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             const int at_col = c * 64 + d * 32 + e;
-                            float x0 = power(v[e]), x1 = power(v[e + 1]);
+                            float x0 = ex2_approx(fmaf(__uint_as_float(v[e]), LOG2E, -sub));
+                            float x1 = ex2_approx(fmaf(__uint_as_float(v[e + 1]), LOG2E, -sub));
                             if (at_col >= cols) x0 = 0.f;
                             if (at_col + 1 >= cols) x1 = 0.f;
                             s += x0 + x1;
@@ -473,7 +591,7 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
                 tc_fence_before();
                 if (row < M && cols > 0) {
                     p.stats[(size_t)row * ((N + BLK - 1) / BLK) + col0 / BLK] = make_float2(m, s);
-                    if (!TEACHER && tg >= 0 && tg < cols) p.at_target[row] = at;
+                    if (tg >= 0 && tg < cols) p.at_target[row] = at;
                 }
             } else if (MODE == DH && parts > 1) {
 #pragma unroll 1
@@ -545,12 +663,8 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
                 }
                 tc_fence_before();
             }
-            __syncwarp();
-            if (elect_one()) {
-                if constexpr (PAIR) mbar_arrive_cluster(map_rank(&tempty[acc], 0));
-                else mbar_arrive(&tempty[acc]);
-            }
-            __syncwarp();
+            empty_again();
+            ++local;
         }
     }
 
@@ -569,14 +683,14 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
 }
 
 template <int MODE, bool TEACHER = false>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(64 + 32 * vocab::EW, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(vocab::threads(TEACHER), 1)
     k_vocab_gemm(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                  const __grid_constant__ VocabGemm p) {
     vocab_tiles<MODE, TEACHER, true>(ta, tb, p);
 }
 
 // The logits of few rows against a teacher: blocks of 128 rows on single CTAs.
-__global__ void __launch_bounds__(64 + 32 * vocab::EW, 1)
+__global__ void __launch_bounds__(vocab::TEACHER_THREADS, 1)
     k_vocab_teacher_gemm(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                          const __grid_constant__ VocabGemm p) {
     vocab_tiles<vocab::LOGITS, true, false>(ta, tb, p);
@@ -978,7 +1092,7 @@ static jnx_status vocab_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const
         (m + BM - 1) / BM * ((n + BN - 1) / BN) * (MODE == DH ? p.split : 1);
     if (tiles > 0x7fff0000) return fail(JNX_ERR_UNSUPPORTED, "%s: too many tiles", what);
     const int grid = 2 * (int)std::min<long long>(tiles, num_sms() / 2);
-    pdl(k_vocab_gemm<MODE, TEACHER>, grid, 64 + 32 * EW, SMEM, s)(ta, tb, p);
+    pdl(k_vocab_gemm<MODE, TEACHER>, grid, threads(TEACHER), SMEM, s)(ta, tb, p);
     return launched(what);
 }
 
@@ -996,7 +1110,7 @@ static jnx_status vocab_logits(const CUtensorMap& th, const CUtensorMap& tw, con
     static std::atomic<uint64_t> attr{0};
     if (set_smem_limit(reinterpret_cast<const void*>(k_vocab_teacher_gemm), SMEM, attr) != cudaSuccess)
         return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
-    pdl(k_vocab_teacher_gemm, (int)std::min<long long>(lone, sms), 64 + 32 * EW, SMEM, s)(th, tw, p);
+    pdl(k_vocab_teacher_gemm, (int)std::min<long long>(lone, sms), TEACHER_THREADS, SMEM, s)(th, tw, p);
     return launched(what);
 }
 
@@ -1195,9 +1309,8 @@ static jnx_status vocab_run(const uint16_t* h, int64_t ldh, const uint16_t* w, i
             p.words = ws.words;
             p.starts = ws.starts;
             p.top = teacher->top;
-            const double scale = vocab_scale(d, teacher->inv_tau);
-            p.log2e = finite(1.4426950408889634 * scale);
-            p.scale = finite(scale);
+            p.log2e = (float)std::min(1.4426950408889634 * teacher->inv_tau, 3e38);
+            p.scale = teacher->inv_tau;
             if (jnx_status st = vocab_logits(th, tw, p, what, s)) return st;
             pdl(k_vocab_rows_teacher, rows, 256, 0, s)(ws.stats, p, ws.entries, ws.prob, ws.log_prob,
                                                        weight, teacher->inv_tau, loss);

@@ -78,6 +78,34 @@ def test_distill_near_its_teacher_no_loss_is_below_zero(k):
     T.close(loss, want, 2.0 ** -18 * off + 2.0 ** -36 + 2.0 ** -19 * want, "loss")
 
 
+@pytest.mark.parametrize("d", [64, 1000, 8192, 16_384])
+@pytest.mark.parametrize("terms", [1, 2])
+def test_distill_few_terms_are_exact_whatever_the_width(d, terms):
+    """Hidden rows with one or two values that are not zero, powers of two, far apart: products
+    and sums of them are exact, so the width is in no bound.  A logarithm of a probability is
+    then off by the rounding of logits' differences (2^-22 of them, twice) and by the
+    exponentials and their sums (2^-19)."""
+    n, v, k = 96, 600, 12
+    _, _, ids, t, rw = distill_case(n, 8, v, k, seed=d)
+    g = gen(d)
+    w = (normal(g, v, d).float() * 16).round().clamp(-64, 64).to(BF)  # whole numbers
+    h = torch.zeros(n, d, device="cuda", dtype=BF)
+    at = torch.randint(0, d // 2, (n,), generator=g, device="cuda")
+    h[torch.arange(n, device="cuda"), at] = 1
+    if terms == 2:
+        h[torch.arange(n, device="cuda"), d - 1 - at] = -0.5
+    op, loss = _r().VocabDistill(w, n, k, 0.5, gradients=False), empty(n, dtype=F32)
+    op.loss(h, ids, t, loss)
+    op.check()
+    want = D.distill(h, w, ids, t, 0.5)["loss"]
+    x = h.double() @ w.double().T / 0.5
+    logt = torch.log_softmax(t.double() / 0.5, -1)
+    span = x.amax(-1) - x.amin(-1) - logt.amin(-1)
+    # (the gradient's size, P - T, is two at most)
+    err = 2.0 ** -21 * span + 2.0 ** -19
+    T.close(loss, want, 2 * err + err * err + 2.0 ** -20 * want, "loss")
+
+
 # ---------------------------------------------------------------- verification
 
 @pytest.mark.parametrize("vocab", [50, 5000, 40_000])
