@@ -620,6 +620,7 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
             // straight from the registers, a lane its row: 32 columns a time, the next ones' under way
             // (through staging, so that lanes write side by side: 1,000 cycles for every 32 columns)
             uint32_t w[2][32];
+            __syncwarp();
             if (n > 0) tmem_ld32(tO, w[0]);
 #pragma unroll
             for (int c = 0; c < HD / 32; ++c) {
@@ -633,15 +634,14 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
                         mbar_arrive(&bar[O_FREE]);
                     }
                 }
-                if (!live) continue;
                 // a row that saw nothing: O holds products of zeros
                 const float f = n > 0 && l > 0.f ? inv : 0.f;
 #pragma unroll
                 for (int e = 0; e < 32; ++e) y[e] = f == 0.f ? 0u : __float_as_uint(__uint_as_float(y[e]) * f);
-                if (joined) {
+                if (live && joined) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) store8(a.part + o + c * 32 + j * 8, y, j * 8);
-                } else {
+                } else if (live) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t z[4];
@@ -651,6 +651,7 @@ __global__ void __launch_bounds__(tree::THREADS, TreeCfg<HD>::CTAS)
                         *reinterpret_cast<uint4*>(a.out + o + c * 32 + j * 8) = make_uint4(z[0], z[1], z[2], z[3]);
                     }
                 }
+                __syncwarp();  // the next columns are taken by all lanes
             }
         }
         if (!ok) *fail_flag = 1;
