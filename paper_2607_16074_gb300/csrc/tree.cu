@@ -684,8 +684,6 @@ __global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeA
     if (runs <= 1 || runs > MAX_RUNS || x.x < 0 || x.y < 1 || x.y > kMaxNodes ||
         (long long)x.x + (runs - 1) * x.y >= a.places || x.w < a.s0 || x.w >= a.s0 + a.n_seqs)
         return;
-    const int2 span = a.spans[x.w - a.s0];
-    const bool known = row >= span.x && row < span.x + span.y;
     const long long at = (long long)x.x * a.H + h, step = (long long)x.y * a.H;
     float v[R][E], m[2], l[2], top = -INFINITY, sum = 0.f;
     // runs first, first + by, ...: a warp of four has every fourth
@@ -712,6 +710,7 @@ __global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeA
         top = fmaxf(top, m[k]);
     }
     load(mine);
+    const int2 span = a.spans[x.w - a.s0];
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (top == -INFINITY) top = 0.f;  // no run's token was seen
@@ -751,15 +750,15 @@ __global__ void __launch_bounds__(128) k_tree_join(const __grid_constant__ TreeA
 #pragma unroll
         for (int e = 0; e < E; ++e) all[e] = (acc[0][e] + acc[1][e]) + (acc[2][e] + acc[3][e]);
     }
-    if (!known) return;
+    if (row < span.x || row >= span.x + span.y) return;
     uint16_t* o = a.out + row * a.o_row + h * a.o_head + lane * E;
 #pragma unroll
     for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(o + e) = cvt_bf2(all[e] * inv, all[e + 1] * inv);
 }
 
-// The workspace: the rows' records, a launch's sequences, then (at a sector's border) the sums.
+// The workspace: the rows' records, a launch's sequences, then (at 256 bytes) the sums.
 static size_t tree_sums_at(int n_rows) {
-    return ((size_t)n_rows * sizeof(int4) + tree::BATCH * sizeof(int2) + 2 * sizeof(int) + 31) & ~(size_t)31;
+    return ((size_t)n_rows * sizeof(int4) + tree::BATCH * sizeof(int2) + 2 * sizeof(int) + 255) & ~(size_t)255;
 }
 
 template <int HD>
@@ -797,7 +796,7 @@ extern "C" size_t jnx_op_tree_attention_workspace_bytes(int32_t n_seqs, int32_t 
                                                         int32_t n_heads, int32_t head_dim,
                                                         int64_t max_tokens) {
     if (n_seqs < 0 || n_rows < 0 || n_heads <= 0 || head_dim <= 0 || max_tokens < 0) return 0;
-    return tree_sums_at(n_rows) + 32 +
+    return tree_sums_at(n_rows) + 256 +
            (size_t)n_rows * tree::most_runs(max_tokens) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
@@ -838,8 +837,8 @@ extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx
                static_cast<int4*>(workspace), nullptr, nullptr, nullptr, nullptr, (int)(n_rows * runs), status};
     a.spans = reinterpret_cast<int2*>(a.where + n_rows);
     a.taken = reinterpret_cast<int*>(a.spans + tree::BATCH);
-    const uintptr_t sums = reinterpret_cast<uintptr_t>(workspace) + tree_sums_at(n_rows) + 31;
-    a.part = reinterpret_cast<float*>(sums & ~(uintptr_t)31);
+    const uintptr_t sums = reinterpret_cast<uintptr_t>(workspace) + tree_sums_at(n_rows) + 255;
+    a.part = reinterpret_cast<float*>(sums & ~(uintptr_t)255);
     a.ml = reinterpret_cast<float2*>(a.part + (size_t)n_rows * runs * n_heads * head_dim);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TraceScope ts(JNX_K_TREE_ATTN, 0.0, s);
