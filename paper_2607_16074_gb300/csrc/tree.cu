@@ -76,9 +76,11 @@ __host__ __device__ inline int run_tokens(int L, int rows, int units, int slots,
     if (n < 1) n = 1;
     return round_up((L + n - 1) / n, KT);
 }
-// No sequence of up to max_tokens has more runs.
-inline long long most_runs(long long max_tokens) {
-    return std::max(1ll, std::min<long long>(MAX_RUNS, (max_tokens + 255) / 256));
+// No sequence of up to max_tokens has more runs: at head dims 64 and 128 up to 8 of 256 tokens or
+// of 512, then of 1,024; at 256, where a unit's share counts, up to 33 of 256 to 1,024.
+inline long long most_runs(long long max_tokens, bool wide) {
+    const long long shorts = std::min(wide ? 33ll : 8ll, (max_tokens + 255) / 256);
+    return std::max({1ll, shorts, std::min<long long>(MAX_RUNS, (max_tokens + 1023) / 1024)});
 }
 }  // namespace tree
 
@@ -797,7 +799,7 @@ extern "C" size_t jnx_op_tree_attention_workspace_bytes(int32_t n_seqs, int32_t 
                                                         int64_t max_tokens) {
     if (n_seqs < 0 || n_rows < 0 || n_heads <= 0 || head_dim <= 0 || max_tokens < 0) return 0;
     return tree_sums_at(n_rows) + 256 +
-           (size_t)n_rows * tree::most_runs(max_tokens) * n_heads * (head_dim + 2) * sizeof(float);
+           (size_t)n_rows * tree::most_runs(max_tokens, head_dim == 256) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
 extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx_pages* pages,
@@ -816,7 +818,7 @@ extern "C" jnx_status jnx_op_tree_attention(const jnx_kv_cache* cache, const jnx
         return fail(JNX_ERR_INVALID_ARG, "%s: null or misaligned argument", what);
     if (pages->max_pages > 1 && cache->room % 16)
         return fail(JNX_ERR_UNSUPPORTED, "%s: pages of %d tokens, no multiple of 16", what, cache->room);
-    const long long tokens = (long long)pages->max_pages * cache->room, runs = tree::most_runs(tokens);
+    const long long tokens = (long long)pages->max_pages * cache->room, runs = tree::most_runs(tokens, head_dim == 256);
     if (tokens > 0x7fffff00 || (long long)n_rows * n_heads > 0x7fffff00 ||
         (long long)n_rows * runs > 0x7fffff00 ||
         tree::BATCH * runs * n_kv_heads * kMaxNodes > 0x7fffff00)

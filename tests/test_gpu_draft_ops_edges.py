@@ -254,3 +254,17 @@ def test_tree_over_a_cache_of_no_pages(heads, entry):
         op._status, torch.cuda.current_stream().cuda_stream))
     _reports(op)
     assert (out == 0).all()
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64), (8, 1, 256), (4, 4, 256)])
+@pytest.mark.parametrize("tokens", [257, 2048, 2049, 2113, 4097, 8192, 8193, 8321, 16_300, 33_000, 66_000])
+def test_tree_sums_stay_in_the_workspace(heads, tokens):
+    """Sequences of the most runs that their length may have, few nodes and many, in a workspace
+    of just what the operator asks for."""
+    page = 16 if tokens < 10_000 else 64
+    c = Trees(heads, page, [tokens - 1, 0, tokens - 5, 100], [1, 3, 5, 2], seed=tokens)
+    op = c.op()
+    behind, out = guarded(op), empty(*c.q.shape)
+    c.run(op, out)
+    c.compare(out)
+    assert (behind == 90).all()
