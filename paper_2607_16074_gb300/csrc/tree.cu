@@ -15,7 +15,9 @@
 //               page, into a ring each; the table's entries are looked up ahead
 //   warp 1      MMA issuer: S two key tiles ahead of P V
 //   warps 2-5   softmax and epilogue, a thread a row
-// P (bf16) overwrites its scores and is the TMEM A operand of the P V product.
+// P overwrites its scores and is the TMEM A operand of the P V product.  It is bf16, as V is (a
+// product's operands are of one type); l sums what was not rounded.  Against 64 bits the outputs
+// are off by 0.0017 to 0.0023 in norm, of which their own rounding is 0.0014 to 0.0017.
 //
 // The run's length depends on the sequence alone, so a sequence's bits do not depend on the
 // others; its runs' sums are joined in their order by a second kernel.

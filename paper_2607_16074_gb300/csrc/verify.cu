@@ -30,7 +30,9 @@ constexpr int CLUSTER = 8;     // CTAs of a sequence
 constexpr int ALONE = 4096;    // words up to which it is one
 constexpr int HELD = 4;        // groups of 128 words that a warp holds in registers
 
-// The sum of two fp32 values, hi = fl(hi + lo): 2^-48 of relative error an operation.
+// The sum of two fp32 values, hi = fl(hi + lo): 2^-48 of relative error an operation, by the
+// published error-free transformations (Knuth's sum of two, Dekker's where the larger is known, and
+// a product's error by a fused multiply-add).
 struct Two {
     float hi, lo;
 };

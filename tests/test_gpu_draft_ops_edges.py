@@ -6,8 +6,8 @@ import torch
 
 from tests import draft_ops_ref as D
 from tests import text_ops_ref as T
-from tests.test_gpu_draft_ops import (BF, F32, HEADS, I32, Trees, _r, _reports, by_hand, check_distill, distill_case,
-                                      empty, gen, ints, normal, place, run_verify, verify_case)
+from tests.test_gpu_draft_ops import (BF, F32, I32, Trees, _r, _reports, by_hand, check_distill, distill_case, empty,
+                                      gen, ints, normal, place, run_verify, verify_case)
 
 pytestmark = pytest.mark.gpu
 
@@ -104,6 +104,47 @@ def test_distill_few_terms_are_exact_whatever_the_width(d, terms):
     # (the gradient's size, P - T, is two at most)
     err = 2.0 ** -21 * span + 2.0 ** -19
     T.close(loss, want, 2 * err + err * err + 2.0 ** -20 * want, "loss")
+
+
+@pytest.mark.parametrize("d", [1000, 2048, 8192])
+@pytest.mark.parametrize("kind", ["centred", "mean", "positive", "normed", "sparse"])
+def test_distill_wide_rows_of_any_kind(d, kind):
+    """A logit is sums of up to 768 terms, 48 steps that lose up to 2^-23 each of what is there, of
+    at most its terms' sizes, and the rounding of adding those up (2^-24 each): the width is in
+    no bound but by the number of sums.  The rest as in the definitions' bound."""
+    h, w, ids, t, rw = distill_case(200, d, 700, 20, seed=d)
+    if kind == "mean":
+        h += 3
+    elif kind == "positive":
+        h, w = h.abs(), w.abs()
+    elif kind == "normed":
+        h = (h.float() * torch.rand(d, generator=gen(1), device="cuda") * 2).to(BF)
+        h = (h.float() * torch.rsqrt(h.float().square().mean(-1, keepdim=True))).to(BF)
+    elif kind == "sparse":
+        h[torch.rand(h.shape, generator=gen(2), device="cuda") < 0.98] = 0
+        h *= 7
+    op, loss = _r().VocabDistill(w, 200, 20, 0.5, gradients=False), empty(200, dtype=F32)
+    op.loss(h, ids, t, loss)
+    op.check()
+    want = D.distill(h, w, ids, t, 0.5)["loss"]
+    x, logt = h.double() @ w.double().T / 0.5, torch.log_softmax(t.double() / 0.5, -1)
+    T1 = torch.zeros_like(x).scatter_add_(1, ids.long(), logt.exp())
+    off = (T1 - torch.softmax(x, -1)).abs().sum(-1)
+    size = (h.double().abs() @ w.double().abs().T).amax(-1) / 0.5
+    span = x.amax(-1) - x.amin(-1) - logt.amin(-1)
+    err = (48 * 2.0 ** -23 + (d / 640 + 1) * 2.0 ** -24) * size + 2.0 ** -21 * span + 2.0 ** -19
+    T.close(loss, want, 2 * err * off + 2 * err * err + 2.0 ** -18 * want, "loss")
+
+
+@pytest.mark.parametrize("n", [8192, 8193, 17_000])
+def test_distill_more_rows_than_a_piece(n):
+    """Rows counted by blocks, in pieces of 8,192 and in one."""
+    h, w, _, t, rw = distill_case(n, 64, 200, 3, seed=1)
+    ids = torch.randint(0, 200, (n, 3), generator=gen(2), device="cuda", dtype=I32)
+    ids[1::3] = -1
+    h[1::3] = float("nan")
+    check_distill(h, w, ids, t, rw, tau=0.5)
+    check_distill(h, w, ids, t, rw, piece=n)
 
 
 # ---------------------------------------------------------------- verification
@@ -268,3 +309,11 @@ def test_tree_sums_stay_in_the_workspace(heads, tokens):
     c.run(op, out)
     c.compare(out)
     assert (behind == 90).all()
+
+
+@pytest.mark.parametrize("heads", [(8, 1, 256), (8, 2, 128), (14, 2, 64)])
+@pytest.mark.parametrize("room", [1, 5, 16, 33, 63, 64])
+def test_tree_of_a_short_page_a_sequence(heads, room):
+    old = [max(room - 4, 0), 0, room // 2]
+    c = Trees(heads, 0, old, [min(4, room), 1, min(3, room - room // 2)], seed=room, one_page=room)
+    c.compare(c.run())
