@@ -22,12 +22,13 @@
 // The run's length depends on the sequence alone, so a sequence's bits do not depend on the
 // others; its runs' sums are joined in their order by a second kernel.
 //
-// 64 trees of up to 12 nodes over up to 8,100 tokens, 32 heads on 8 of 128: 188 us, 5.7 TB/s
-// (floor 158; the attention 184, the join's last CTAs 4).  One of 16 nodes over 60,001 tokens
-// 50.3 (floor 36.5; start, last unit and join 8 or so of it), 8 of up to 6 over up to 700, 8
+// 64 trees of up to 12 nodes over up to 8,100 tokens, 32 heads on 8 of 128: 189 us, 5.7 TB/s
+// (floor 158; the attention 185, the join's last CTAs 4).  One of 16 nodes over 60,001 tokens
+// 51.3 (floor 36.5; start, last unit and join 8 or so of it), 8 of up to 6 over up to 700, 8
 // heads on one of 256, 13: latency, two launches' chains of lookups, loads, three or four tiles
-// and sums.  24 of up to 64 nodes over up to 3,500: 28.8, the tensor cores' and softmax's, tiles
-// of 64 tokens for 128 rows (floor 6.7).
+// and sums.  24 of up to 64 nodes over up to 3,500: 29.5, the tensor cores' and softmax's, tiles
+// of 64 tokens for 128 rows, and 148 units of which the longest has 15 tiles, the mean 9.7 (floor
+// 6.7).
 //
 // Not kept: the products the other way round, tokens as the rows and the pairs as 64 columns, so
 // that few pairs cost no more than they are (a unit's sums and epilogue took 12,000 clocks: 260 us

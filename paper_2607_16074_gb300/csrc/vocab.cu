@@ -25,8 +25,12 @@
 // the products 1,040, 1,175 and 1,070 each by itself, the rows 150.  333 rows of 2,048 without
 // gradients: 48 us, of which the logits 46 by themselves, two row blocks of 256 for 1.3 and four
 // rounds of tiles for 3.3.
-// Against a teacher's 32 entries a row, 8,191 rows of 2,048: 1,940 us (floor 1,671), the products
-// 505, 545 and 510, the rows 187; 333 rows of 1,024 without gradients 33, the logits 21.
+// Against a teacher's 32 entries a row, 8,191 rows of 2,048: 1,980 us (floor 1,671), the products
+// 544, 569 and 534, the rows 187; 333 rows of 1,024 without gradients 31, the logits 20.5.
+//
+// G is bf16, as its products' other operands are, and rounded twice: when it is formed, whose
+// row's maximum is not known yet (in 32 bits it would be twice the bytes of the rows' kernel), and
+// when it is scaled.
 #include <algorithm>
 
 #include "jnx_dev.cuh"
@@ -62,7 +66,9 @@ constexpr int TOP = 128;  // entries of a row's teacher, at most (places fit a b
 // before works under it.
 constexpr int FIRST_K = 12, MORE_K = 10;  // K steps of the first such sum and of those behind it
 // A warpgroup for the copies and the products, and two for the epilogue, whose 128 logits a
-// thread stay in registers: each has its share of what the launch has (168 for each of 384).
+// thread stay in registers: each has its share of what the launch has, 168 for each of 384 threads
+// (2,047 rows of 1,024 on 32,000 words without gradients: 99 us; 123 with 168 for all, which
+// spills; 148 with the sum written back to its accumulator, which the next products wait for).
 constexpr int TEACHER_THREADS = 128 + 32 * EW, FEW_REGS = 56, MANY_REGS = 224;
 static_assert(128 * FEW_REGS + 32 * EW * MANY_REGS <= 168 * TEACHER_THREADS, "registers of the launch");
 __host__ __device__ constexpr int threads(bool teacher) { return teacher ? TEACHER_THREADS : 64 + 32 * EW; }
@@ -360,7 +366,7 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
         // A teacher's entries of a row of a tile: their number and the first two's columns, 8 bits
         // each, the first one's place among the row's, and the 32-column chunks that hold any.
         // They are looked up a tile ahead, a step of the chain between parts of this tile's work
-        // (a loop of lookups behind the product: 102 us of 2,047 rows of 1,024 on 32,000 words for 93)
+        // (2,047 rows of 1,024 on 32,000 words: 102 us with lookups behind the product, 92 so)
         constexpr int AHEAD = 2;
         int tg = 0, te = 0, src = -1, next_col0 = 0;
         uint32_t seen = 0, mine = 0;
@@ -985,9 +991,10 @@ __device__ __forceinline__ float vocab_term(float T, float d, float grad) {
 // k_vocab_rows with a teacher.  With d = log P - log T at an entry, the loss is the sum of
 // T (e^d - 1 - d) over the entries and of P over all other words: no term is negative, so that
 // near the teacher a loss is off by what d is off by, times its gradient, and no more.  (As
-// sum T (log T - log P), each rounded, a loss under 1e-6 was lost.)  A CTA a row; thread k has entry k.  Bound by the
-// probabilities' way through memory: 8,191 rows of 32,000, nine tenths of them with entries, 187
-// us (the next-token losses' 173; with four loads ahead of the sums 211: fewer CTAs an SM).
+// sum T (log T - log P), each rounded, a loss under 1e-6 was lost.)  A CTA a row; thread k has
+// entry k.  Bound by the probabilities' way through memory: 8,191 rows of 32,000, nine tenths of
+// them with entries, 187 us (the next-token losses' 171; with four loads ahead of the sums 211:
+// fewer CTAs an SM).
 __global__ void __launch_bounds__(256)
     k_vocab_rows_teacher(const float2* stats, const __grid_constant__ VocabGemm p,
                          const int* count, const float* prob, const float* log_prob,
@@ -1097,8 +1104,8 @@ static jnx_status vocab_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const
 }
 
 // Against a teacher, tiles of 128 rows on lone CTAs where they take fewer rounds of the card than
-// pairs' of 256, each as long: 333 rows of 1,024 on 32,000 words three for four (21 us for 26), up
-// to 128 one for two (12.7 for 17.5).  Equal rounds go to the pairs, which read the words half as often.
+// pairs' of 256, each as long: 333 rows of 1,024 on 32,000 words three for four (20.5 us for 27.1),
+// up to 128 one for two (11.2 for 16.6).  Equal rounds go to the pairs, which read the words half as often.
 static jnx_status vocab_logits(const CUtensorMap& th, const CUtensorMap& tw, const VocabGemm& p,
                                const char* what, cudaStream_t s) {
     using namespace vocab;
