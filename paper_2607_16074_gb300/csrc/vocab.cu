@@ -479,9 +479,10 @@ __device__ __forceinline__ void vocab_tiles(const CUtensorMap& ta, const CUtenso
                     if (hit >> c & 1) {
                         while (taken < here) {
                             const size_t place = (size_t)row * p.top + first_place + taken;
-                            int col = seen >> (8 + 8 * taken) & 255;
-                            if (taken >= AHEAD)
-                                col = p.words[(size_t)p.index[p.r0 + row] * p.top + first_place + taken] - col0;
+                            const int col =
+                                taken < AHEAD
+                                    ? seen >> (8 + 8 * taken) & 255
+                                    : p.words[(size_t)p.index[p.r0 + row] * p.top + first_place + taken] - col0;
                             if (col >> 5 != c) break;
                             float at = 0.f;
 #pragma unroll
@@ -1087,6 +1088,18 @@ __global__ void __launch_bounds__(256)
 // host side
 // ---------------------------------------------------------------------------
 
+// Whether a teacher's kernel was compiled with the registers that its warpgroups share out: with
+// fewer, those that take some would wait for ever.
+static bool vocab_registers(const void* kernel, std::atomic<int>& known) {
+    if (known.load() == 0) {
+        cudaFuncAttributes at{};
+        if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess) return false;
+        using namespace vocab;
+        known = at.numRegs * TEACHER_THREADS >= 128 * FEW_REGS + 32 * EW * MANY_REGS ? 1 : -1;
+    }
+    return known.load() > 0;
+}
+
 template <int MODE, bool TEACHER = false>
 static jnx_status vocab_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const VocabGemm& p,
                              const char* what, cudaStream_t s) {
@@ -1094,6 +1107,11 @@ static jnx_status vocab_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const
     static std::atomic<uint64_t> attr{0};
     if (set_smem_limit(reinterpret_cast<const void*>(k_vocab_gemm<MODE, TEACHER>), SMEM, attr) != cudaSuccess)
         return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
+    if constexpr (TEACHER) {
+        static std::atomic<int> known{0};
+        if (!vocab_registers(reinterpret_cast<const void*>(k_vocab_gemm<MODE, TEACHER>), known))
+            return fail(JNX_ERR_CUDA, "%s: the kernel's registers are not those that it shares out", what);
+    }
     const long long m = MODE == DW ? p.vocab : p.rows_max, n = MODE == LOGITS ? p.vocab : p.d;
     const long long tiles =
         (m + BM - 1) / BM * ((n + BN - 1) / BN) * (MODE == DH ? p.split : 1);
@@ -1117,6 +1135,9 @@ static jnx_status vocab_logits(const CUtensorMap& th, const CUtensorMap& tw, con
     static std::atomic<uint64_t> attr{0};
     if (set_smem_limit(reinterpret_cast<const void*>(k_vocab_teacher_gemm), SMEM, attr) != cudaSuccess)
         return fail(JNX_ERR_CUDA, "%s: smem attribute", what);
+    static std::atomic<int> known{0};
+    if (!vocab_registers(reinterpret_cast<const void*>(k_vocab_teacher_gemm), known))
+        return fail(JNX_ERR_CUDA, "%s: the kernel's registers are not those that it shares out", what);
     pdl(k_vocab_teacher_gemm, (int)std::min<long long>(lone, sms), TEACHER_THREADS, SMEM, s)(th, tw, p);
     return launched(what);
 }
